@@ -125,9 +125,11 @@ def _quantise(x, storage):
     """Codes and scales of rows (the last axis): largest magnitude to the largest code."""
     a = x.abs().amax(-1)
     most = LARGEST_CODE[storage]
-    inverse = torch.where(a > 0, most / a, torch.zeros_like(a))
+    # (divided by a tensor: by a number, torch multiplies with its reciprocal, which is rounded once more)
+    whole = torch.full_like(a, most)
+    inverse = torch.where(a > 0, whole / a, torch.zeros_like(a))
     y = (x * inverse.unsqueeze(-1)).clamp_(-most, most)
-    return (y.round_() if storage == "i8" else y).to(STORED[storage]), a / most
+    return (y.round_() if storage == "i8" else y).to(STORED[storage]), a / whole
 
 
 def _pages(case, pages, g):
