@@ -397,6 +397,87 @@ int disc_graph_launch(disc_ctx* ctx, int32_t graph_id, const int64_t* dims, int 
                       void* hip_stream);
 
 
+/* ---- around a decoder's attention ---------------------------------------------------------------
+ * Operators that are no fusion pattern, because they gather, keep state between calls or multiply matrices:
+ * rotary positions, a cache of keys and values in pages (16-bit, or quantised to 8 bits as it is written), and
+ * attention over that cache.  They are registered and launched like patterns: what a model fixes (element type,
+ * head size, frequencies, storage) is given at registration and compiled once; batch, heads, lengths and strides
+ * are runtime values.  Launches take the arguments of disc_launch: `dims` and the pointer arrays are HOST memory,
+ * the pointers in them DEVICE memory of the context's device and owned by the caller; asynchronous on
+ * `hip_stream`, nothing allocated, nothing synchronised; a launch is kernels only and may be captured into a HIP
+ * graph.  Registering the same description again gives the same id.  A launch of nothing (no tokens, an empty
+ * batch) is a success.  Refused: DISC_ERR_SHAPE (sizes), DISC_ERR_INVALID_ARG (counts, pointers, alignment).
+ * What the library cannot see from the host -- slots, page tables, lengths, positions -- is checked on the
+ * device: a number out of its range never becomes an address. */
+typedef enum { DISC_ROTARY_HALF = 0, DISC_ROTARY_INTERLEAVED = 1 } disc_rotary_layout;
+typedef struct {
+  int32_t dtype;             /* DISC_F32, DISC_F16 or DISC_BF16: operands and results                       */
+  int32_t head_dim;          /* 2 .. 256                                                                    */
+  int32_t rotary_dim;        /* R: the first R elements of a head turn (even, 2 .. head_dim), the rest is copied */
+  int32_t layout;            /* which elements are a pair: (j, j + R/2), or (2j, 2j + 1)                    */
+  double magnitude;          /* factor on the turned elements (1: a rotation)                               */
+  const double* frequencies; /* R / 2 values (host, copied): radians a position of every pair                */
+} disc_rotary_desc;
+int disc_register_rotary(disc_ctx* ctx, const disc_rotary_desc* desc, int32_t* id_out);
+/* y = magnitude * turn(position * frequency) x for up to DISC_ROTARY_TENSORS tensors [tokens, heads, head_dim] of the
+ * same tokens (queries and keys).  dims = {tokens, bytes of a position (4 or 8, signed), backward}, then for every
+ * tensor {heads, token stride, head stride of x, token stride, head stride of y} in elements.  inputs = {positions,
+ * x...}, outputs = {y...}.  backward != 0: the turn goes the other way, which makes it the gradient (x is dL/dy, y
+ * is dL/dx).  y may be x with the same strides (in place); otherwise no row of a y may overlap any other row.
+ * No workspace. */
+enum { DISC_ROTARY_TENSORS = 4 };
+int disc_rotary(disc_ctx* ctx, int32_t id, const int64_t* dims, int n_dims, const void* const* inputs, int n_in,
+                void* const* outputs, int n_out, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+typedef enum {
+  DISC_STORAGE_SAME = 0,  /* elements of the activations' type, no scales                                     */
+  DISC_STORAGE_I8 = 1,    /* signed codes -127 .. 127                                                        */
+  DISC_STORAGE_E4M3 = 2   /* 8-bit floating point, 4 exponent bits, no infinity, largest value 448             */
+} disc_storage;
+typedef struct {
+  int32_t dtype;          /* DISC_F16 or DISC_BF16: keys, values, queries and results                        */
+  int32_t storage;        /* disc_storage                                                                    */
+  int32_t head_dim;       /* a multiple of 16, 16 .. 256                                                     */
+  double softmax_scale;   /* factor on q.k; 0: 1 / sqrt(head_dim)                                            */
+} disc_cache_desc;
+int disc_register_cache(disc_ctx* ctx, const disc_cache_desc* desc, int32_t* id_out);
+/* The cache is the caller's memory: k_pages and v_pages [pages, kv_heads, page_size, head_dim] in the storage's
+ * type, and for 8-bit storage k_scales and v_scales [pages, kv_heads, page_size] in fp32 -- dense, 16-byte aligned.
+ * page_size is a power of two, 8 .. 65536.  A slot (int64) is page * page_size + place.
+ *
+ * disc_cache_store: rows of keys and values [tokens, kv_heads, head_dim] into their slots.  dims = {tokens, kv_heads,
+ * pages, page_size, token stride, head stride of the keys, token stride, head stride of the values}; inputs = {slots,
+ * keys, values}; outputs = {k_pages, v_pages} and with 8-bit storage {.., k_scales, v_scales}.  The scale of a row is a
+ * / Q and the code of an element round(x * (Q / a)) -- a: its largest magnitude, Q = 127 or 448, both quotients and
+ * the product rounded to fp32, the code to nearest, ties to even.  A row of zeros has the scale 0; a row with an
+ * infinity or a NaN gets the scale NaN and reads back as NaN.  Slots outside the pages (negative ones: padding) are
+ * left out.  Slots of one call differ from each other; of a slot that is named twice, the row is either token's or a
+ * mixture of both.
+ * disc_cache_load: the rows of `slots` back, rounded once.  dims as above with the strides of the results; inputs =
+ * {slots, k_pages, v_pages} and {.., k_scales, v_scales}; outputs = {keys, values}.  A slot outside the pages gives
+ * zeros. */
+int disc_cache_store(disc_ctx* ctx, int32_t id, const int64_t* dims, int n_dims, const void* const* inputs, int n_in,
+                     void* const* outputs, int n_out, void* workspace, size_t workspace_bytes, void* hip_stream);
+int disc_cache_load(disc_ctx* ctx, int32_t id, const int64_t* dims, int n_dims, const void* const* inputs, int n_in,
+                    void* const* outputs, int n_out, void* workspace, size_t workspace_bytes, void* hip_stream);
+/* disc_cache_attend: out[b, h] = sum_t p_t v_t / sum_t p_t, p_t = exp(softmax_scale * q[b, h].k_t), over the tokens of a
+ * prefix that all sequences share (read once for the batch, not once a sequence) and of the sequence's own pages; query
+ * head h reads kv head h / (q_heads / kv_heads).  One query token a sequence.
+ * dims = {batch, q_heads, kv_heads, pages, page_size, table_width, prefix_length, prefix_width, sequence stride, head
+ * stride of q, sequence stride, head stride of out}.  inputs = {q [batch, q_heads, head_dim], lengths int32 [batch],
+ * table int32 [batch, table_width], k_pages, v_pages}, with 8-bit storage {.., k_scales, v_scales}, and with
+ * prefix_length > 0 {.., prefix_table int32 [prefix_width]}; outputs = {out}.  Sequence b has the tokens 0 .. lengths[b]
+ * - 1 of its own (at most table_width * page_size, which is at most 2^30); token t is at place t % page_size of the
+ * page table[b, t / page_size].  Entries behind the last token are not read as pages.  Tokens of an entry that is no page of
+ * the cache are left out.  A sequence without any token gets zeros.  What the places behind the last token hold does
+ * not matter.
+ * `workspace`: disc_cache_workspace_bytes, 16-byte aligned, free for other use once the stream has passed the launch;
+ * launches that may overlap in time (two streams, two captured graphs) each need their own. */
+int disc_cache_attend(disc_ctx* ctx, int32_t id, const int64_t* dims, int n_dims, const void* const* inputs, int n_in,
+                      void* const* outputs, int n_out, void* workspace, size_t workspace_bytes, void* hip_stream);
+/* Bytes of workspace that a disc_cache_attend of these dims takes (the same dims; pointers and strides do not count). */
+int disc_cache_workspace_bytes(disc_ctx* ctx, int32_t id, const int64_t* dims, int n_dims, size_t* out);
+
 int disc_get_stats(disc_ctx* ctx, disc_stats_t* out);
 
 /* Measurement helpers (not part of the method): a plain 16-byte-vector device copy used as the

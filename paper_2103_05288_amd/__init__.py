@@ -6,3 +6,4 @@ selection, launch) runs inside libdisc.so and its gfx950 kernels.
 """
 from .binding import (BoundCall, Context, DiscError, PatternHandle, lib_path, load_library,  # noqa: F401
                       OPCODE_IDS, DTYPE_IDS, VARIANTS, STATUS)
+from .decoder import CacheHandle, RotaryHandle, rotary_frequencies  # noqa: F401

@@ -73,6 +73,15 @@ class disc_stats_t(C.Structure):
                 ("host_launch_ns", C.c_int64)]
 
 
+class disc_rotary_desc(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("head_dim", C.c_int32), ("rotary_dim", C.c_int32), ("layout", C.c_int32), ("magnitude", C.c_double),
+                ("frequencies", C.POINTER(C.c_double))]
+
+
+class disc_cache_desc(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("storage", C.c_int32), ("head_dim", C.c_int32), ("softmax_scale", C.c_double)]
+
+
 class DiscError(RuntimeError):
     def __init__(self, code: int, message: str):
         super().__init__(f"DISC_ERR_{STATUS.get(code, code)}: {message}")
@@ -86,7 +95,8 @@ EXPORTS = ("disc_create", "disc_destroy", "disc_last_error", "disc_register_patt
            "disc_pattern_source", "disc_workspace_bytes", "disc_plan", "disc_launch", "disc_force_variant", "disc_test_option",
            "disc_static_scratch_init", "disc_launch_static_scratch",
            "disc_get_stats", "disc_util_copy", "disc_util_copy_nt", "disc_util_empty_launch", "disc_util_mix", "disc_register_graph", "disc_graph_info",
-           "disc_graph_workspace_bytes", "disc_graph_launch")
+           "disc_graph_workspace_bytes", "disc_graph_launch", "disc_register_rotary", "disc_rotary", "disc_register_cache", "disc_cache_store",
+           "disc_cache_load", "disc_cache_attend", "disc_cache_workspace_bytes")
 
 _lib = None
 _pylaunch = None        # the per-call part in C (csrc/pylaunch.cpp), loaded with the library
@@ -179,6 +189,11 @@ def load_library():
     lib.disc_util_copy_nt.argtypes = [vp, vp, vp, C.c_size_t, vp]
     lib.disc_util_empty_launch.argtypes = [vp, vp]
     lib.disc_util_mix.argtypes = [vp, C.c_int, C.c_int, C.c_int, C.c_int, vp, vp, vp, C.c_size_t, vp]
+    lib.disc_register_rotary.argtypes = [vp, C.POINTER(disc_rotary_desc), i32p]
+    lib.disc_register_cache.argtypes = [vp, C.POINTER(disc_cache_desc), i32p]
+    lib.disc_cache_workspace_bytes.argtypes = [vp, C.c_int32, i64p, C.c_int, C.POINTER(C.c_size_t)]
+    for launch in (lib.disc_rotary, lib.disc_cache_store, lib.disc_cache_load, lib.disc_cache_attend):
+        launch.argtypes = lib.disc_launch.argtypes
     _lib = lib
     return lib
 
@@ -336,6 +351,34 @@ class Context:
         pid = C.c_int32(-1)
         self._check(self.lib.disc_register_pattern_static(self.h, ops, n_ops, cs, n_cs, arr, n, C.byref(pid)))
         return PatternHandle(self, pid.value)
+
+    def register_rotary(self, dtype: str, head_dim: int, frequencies: Sequence, layout: str = "half", magnitude: float = 1.0):
+        """Rotary positions of heads of head_dim elements ("f32", "f16" or "bf16"), of which the first 2 * len(frequencies) turn;
+        frequencies and magnitude as rotary_frequencies() gives them.  layout: pairs (j, j + R/2), "half", or (2j, 2j + 1),
+        "interleaved"."""
+        from .decoder import LAYOUT_IDS, RotaryHandle
+        if dtype not in DTYPE_IDS or layout not in LAYOUT_IDS:
+            raise DiscError(-1, f"no such type or layout: {dtype!r}, {layout!r}")
+        n = len(frequencies)
+        values = (C.c_double * max(1, n))(*[float(f) for f in frequencies])
+        desc = disc_rotary_desc(DTYPE_IDS[dtype], int(head_dim), 2 * n, LAYOUT_IDS[layout], float(magnitude), values)
+        oid = C.c_int32(-1)
+        self._check(self.lib.disc_register_rotary(self.h, C.byref(desc), C.byref(oid)))
+        return RotaryHandle(self, oid.value, dtype, int(head_dim))
+
+    def register_cache(self, dtype: str, head_dim: int, storage: Optional[str] = None, softmax_scale: Optional[float] = None):
+        """A cache of keys and values in pages for heads of head_dim elements of "f16" or "bf16".  storage: "i8" or "e4m3" (codes
+        with a scale for every row), or None or the type itself (as they are)."""
+        from .decoder import STORAGE_IDS, CacheHandle
+        storage = dtype if storage is None else storage
+        if dtype not in DTYPE_IDS or (storage != dtype and storage not in STORAGE_IDS):
+            raise DiscError(-1, f"no such type or storage: {dtype!r}, {storage!r}")
+        if softmax_scale is not None and float(softmax_scale) == 0.0:
+            raise DiscError(-1, "a softmax scale of 0 makes every token alike")
+        desc = disc_cache_desc(DTYPE_IDS[dtype], STORAGE_IDS.get(storage, 0), int(head_dim), 0.0 if softmax_scale is None else float(softmax_scale))
+        oid = C.c_int32(-1)
+        self._check(self.lib.disc_register_cache(self.h, C.byref(desc), C.byref(oid)))
+        return CacheHandle(self, oid.value, dtype, int(head_dim), storage)
 
     def pattern_info(self, pid: int) -> dict:
         info = disc_pattern_info_t()

@@ -16,20 +16,24 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libdisc.so")
 PYLAUNCH = os.path.join(HERE, "_pylaunch" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
-SOURCES = ["checker.cpp", "codegen.cpp", "runtime.cpp"]
+SOURCES = ["checker.cpp", "codegen.cpp", "runtime.cpp", "decoder.cpp"]
+# device headers that become strings of the library: file -> the string's name
+EMBEDDED = {"disc_device.h": "kDeviceHeader", "decoder_device.h": "kDecoderHeader"}
 
 
 def _embed_header(build_dir: str) -> str:
-    with open(os.path.join(CSRC, "disc_device.h")) as f:
-        text = f.read().replace("#pragma once\n", "", 1)   # it becomes the head of the main file
-    assert ')DISCHDR"' not in text
     out = os.path.join(build_dir, "device_header_embed.cpp")
-    # raw string literals are limited to 64 KiB by some compilers: split in chunks
-    chunks = [text[i:i + 12000] for i in range(0, len(text), 12000)]
-    body = "\n".join('R"DISCHDR(%s)DISCHDR"' % c for c in chunks)
+    body = ""
+    for name, symbol in EMBEDDED.items():
+        with open(os.path.join(CSRC, name)) as f:
+            text = f.read().replace("#pragma once\n", "", 1)   # it becomes the head of the main file
+        assert ')DISCHDR"' not in text
+        # raw string literals are limited to 64 KiB by some compilers: split in chunks
+        chunks = [text[i:i + 12000] for i in range(0, len(text), 12000)]
+        body += "// generated from %s -- do not edit\nextern const char* const %s;\nconst char* const %s =\n%s;\n" % (
+            name, symbol, symbol, "\n".join('R"DISCHDR(%s)DISCHDR"' % c for c in chunks))
     with open(out, "w") as f:
-        f.write("// generated from disc_device.h -- do not edit\nnamespace disc {\n"
-                "extern const char* const kDeviceHeader;\nconst char* const kDeviceHeader =\n%s;\n}\n" % body)
+        f.write("namespace disc {\n%s}\n" % body)
     return out
 
 

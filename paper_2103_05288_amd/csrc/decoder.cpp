@@ -1,0 +1,531 @@
+// Host side of the operators around a decoder's attention (decoder_device.h): registration, the checks
+// of a launch, its launch dimensions.  No allocation and no lookup on a launch that succeeds.
+#include <hip/hip_runtime_api.h>
+
+#include <cmath>
+#include <cstdio>
+#include <cstring>
+#include <new>
+#include <stdexcept>
+
+#include "disc_internal.hpp"
+
+namespace disc {
+
+extern const char* const kDecoderHeader;   // decoder_device.h, embedded at build time
+
+namespace {
+
+// ---- what the device code takes; the layouts mirror decoder_device.h -------------------------------
+struct RotaryTensor {
+  const void* x;
+  void* y;
+  int64_t x_token, x_head, y_token, y_head;
+  int32_t heads, pad;
+};
+struct RotaryArgs {
+  RotaryTensor t[DISC_ROTARY_TENSORS];
+  const void* positions;
+  int64_t tokens;
+  int32_t n, position_bytes, backward, tokens_per_block;
+};
+struct RowsArgs {
+  const void* slots;
+  const void *k, *v;
+  const void *kp, *vp, *ks, *vs;
+  int64_t k_token, k_head, v_token, v_head, tokens, slots_end;
+  int32_t heads, shift;
+};
+struct AttendArgs {
+  const void *q, *lengths, *table, *kp, *vp, *ks, *vs, *prefix_table;
+  void* out;
+  float *part, *part_m;
+  int64_t q_row, q_head, o_row, o_head;
+  int32_t batch, heads, kv_heads, group, pages, shift, width, tiles;
+  int32_t target, parts, prefix_len, prefix_chunk, prefix_parts, pad;
+  double inv_target;
+};
+constexpr int kMaxBlockTokens = 8, kMostPages = 2048, kBlockStep = 128;
+
+enum { FN_ROTARY = 0 };
+enum { FN_STORE = 0, FN_LOAD, FN_ATTEND, FN_PREFIX, FN_JOIN };
+
+constexpr int64_t kMostElements = (int64_t)1 << 60;
+
+int refuse(disc_ctx* c, int code, const char* what) { return context_fail(c, code, what); }
+int refuse(disc_ctx* c, int code, const char* what, long long got) {
+  char buf[160];
+  snprintf(buf, sizeof buf, "%s (got %lld)", what, got);
+  return context_fail(c, code, buf);
+}
+
+// a * b of two sizes, or -1 where that is more than any memory holds
+int64_t times(int64_t a, int64_t b) {
+  if (a < 0 || b < 0) return -1;
+  if (a == 0 || b == 0) return 0;
+  return a > kMostElements / b ? -1 : a * b;
+}
+
+// rows [tokens][heads] of `d` elements: every stride is a size, and the extent fits
+bool strides_ok(int64_t tokens, int64_t token, int64_t heads, int64_t head, int64_t d) {
+  if (token < 0 || head < 0) return false;
+  const int64_t a = times(tokens - 1, token), b = times(heads - 1, head);
+  return a >= 0 && b >= 0 && a + b + d <= kMostElements;
+}
+// ... and no two of them overlap
+bool rows_apart(int64_t tokens, int64_t token, int64_t heads, int64_t head, int64_t d) {
+  if (tokens <= 1) return heads <= 1 || head >= d;
+  if (heads <= 1) return token >= d;
+  return (head >= d && token >= (heads - 1) * head + d) || (token >= d && head >= (tokens - 1) * token + d);
+}
+bool aligned(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
+
+Operator* get_operator(disc_ctx* c, int32_t id, Operator::Kind kind) {
+  auto& all = *context_operators(c);
+  if (id < 0 || id >= (int)all.size() || all[id]->kind != kind) return nullptr;
+  return all[id].get();
+}
+
+// The context's device is the current one while kernels are enqueued (the default stream is the current device's).
+struct OnDevice {
+  int before = -1;
+  bool ok = true;
+  explicit OnDevice(int device) {
+    int now = -1;
+    ok = hipGetDevice(&now) == hipSuccess;
+    if (ok && now != device) {
+      ok = hipSetDevice(device) == hipSuccess;
+      before = now;
+    }
+  }
+  ~OnDevice() {
+    if (before >= 0) (void)hipSetDevice(before);
+  }
+};
+
+int enqueue(disc_ctx* c, void* fn, uint64_t blocks, uint32_t y, const void* args, size_t size, void* stream) {
+  void* extra[] = {HIP_LAUNCH_PARAM_BUFFER_POINTER, const_cast<void*>(args), HIP_LAUNCH_PARAM_BUFFER_SIZE, &size, HIP_LAUNCH_PARAM_END};
+  const hipError_t e = hipModuleLaunchKernel((hipFunction_t)fn, (uint32_t)blocks, y, 1, 256, 1, 1, 0, (hipStream_t)stream, nullptr, extra);
+  if (e != hipSuccess) {
+    (void)hipGetLastError();
+    char buf[128];
+    snprintf(buf, sizeof buf, "hipModuleLaunchKernel: %s", hipGetErrorString(e));
+    return context_fail(c, DISC_ERR_HIP, buf);
+  }
+  return DISC_OK;
+}
+
+// Compiles the operator and enters it, or finds the one that was made of the same description.
+int enter(disc_ctx* c, std::unique_ptr<Operator> o, const std::string& macros, const char* const* names, int n, int32_t* id_out) {
+  auto& all = *context_operators(c);
+  for (size_t i = 0; i < all.size(); ++i)
+    if (all[i]->key == o->key) {
+      *id_out = (int32_t)i;
+      return DISC_OK;
+    }
+  std::vector<char> code;
+  const int rc = context_compile(c, macros + kDecoderHeader, &code);
+  if (rc) return rc;
+  all.reserve(all.size() + 1);
+  const int device = context_device(c);
+  if (device >= 0) {
+    OnDevice on(device);
+    if (!on.ok) return refuse(c, DISC_ERR_HIP, "hipSetDevice failed");
+    hipModule_t m = nullptr;
+    if (hipModuleLoadData(&m, code.data()) != hipSuccess) {
+      (void)hipGetLastError();
+      return refuse(c, DISC_ERR_HIP, "hipModuleLoadData failed");
+    }
+    o->module = m;
+    for (int i = 0; i < n; ++i) {
+      hipFunction_t f = nullptr;
+      if (hipModuleGetFunction(&f, m, names[i]) != hipSuccess) {
+        (void)hipGetLastError();
+        (void)hipModuleUnload(m);
+        return refuse(c, DISC_ERR_HIP, "hipModuleGetFunction failed");
+      }
+      o->fn[i] = f;
+    }
+  }
+  *id_out = (int32_t)all.size();
+  all.push_back(std::move(o));
+  return DISC_OK;
+}
+
+std::string text(const char* format, double x) {
+  char buf[64];
+  snprintf(buf, sizeof buf, format, x);
+  return buf;
+}
+
+// ---- rotary positions ------------------------------------------------------------------------------
+
+// elements of one access and accesses of one head, as the device code has them
+int rotary_units(const Operator& o) {
+  const int half = o.rotary_dim / 2, rest = o.head_dim - o.rotary_dim;
+  int w = 16 / dtype_bytes(o.dtype);
+  while (half % w || rest % w) w /= 2;
+  return half / w + rest / w;
+}
+
+int register_rotary(disc_ctx* c, const disc_rotary_desc* d, int32_t* id_out) {
+  if (!c) return DISC_ERR_INVALID_ARG;
+  if (!d || !id_out || !d->frequencies) return refuse(c, DISC_ERR_INVALID_ARG, "null pointer");
+  if (!is_float_dtype(d->dtype)) return refuse(c, DISC_ERR_INVALID_ARG, "rotary takes f32, f16 or bf16");
+  if (d->head_dim < 2 || d->head_dim > 256) return refuse(c, DISC_ERR_SHAPE, "head_dim is 2 .. 256", d->head_dim);
+  if (d->rotary_dim < 2 || d->rotary_dim > d->head_dim || d->rotary_dim % 2)
+    return refuse(c, DISC_ERR_SHAPE, "rotary_dim is even, 2 .. head_dim", d->rotary_dim);
+  if (d->layout != DISC_ROTARY_HALF && d->layout != DISC_ROTARY_INTERLEAVED) return refuse(c, DISC_ERR_INVALID_ARG, "bad rotary layout");
+  if (!std::isfinite(d->magnitude)) return refuse(c, DISC_ERR_INVALID_ARG, "magnitude is not finite");
+  std::string macros = "#define DISC_ROTARY 1\n";
+  macros += std::string("#define DISC_T ") + dtype_ctype(d->dtype) + "\n";
+  macros += "#define DISC_D " + std::to_string(d->head_dim) + "\n#define DISC_R " + std::to_string(d->rotary_dim) + "\n";
+  macros += "#define DISC_INTERLEAVED " + std::to_string(d->layout) + "\n#define DISC_MAGNITUDE " + text("%a", d->magnitude) + "\n";
+  macros += "__device__ const double kTurns[DISC_R / 2] = {";
+  for (int j = 0; j < d->rotary_dim / 2; ++j) {
+    const double f = d->frequencies[j];
+    if (!std::isfinite(f) || std::fabs(f) > 3.2) return refuse(c, DISC_ERR_INVALID_ARG, "a frequency is finite and at most half a turn a position");
+    macros += text("%a,", f * 0.63661977236758134308);   // quarter turns: f / (pi / 2)
+  }
+  macros += "};\n";
+  std::unique_ptr<Operator> o(new Operator);
+  o->kind = Operator::ROTARY;
+  o->key = macros;
+  o->dtype = d->dtype;
+  o->head_dim = d->head_dim;
+  o->rotary_dim = d->rotary_dim;
+  static const char* const names[] = {"disc_rotary_k"};
+  return enter(c, std::move(o), macros, names, 1, id_out);
+}
+
+int launch_rotary(disc_ctx* c, int32_t id, const int64_t* dims, int n_dims, const void* const* in, int n_in, void* const* out, int n_out,
+                  void* stream) {
+  if (!c) return DISC_ERR_INVALID_ARG;
+  const Operator* o = get_operator(c, id, Operator::ROTARY);
+  if (!o) return refuse(c, DISC_ERR_INVALID_ARG, "bad rotary id");
+  if (!dims || !in || !out) return refuse(c, DISC_ERR_INVALID_ARG, "null pointer array");
+  if (n_out < 1 || n_out > DISC_ROTARY_TENSORS || n_in != n_out + 1 || n_dims != 3 + 5 * n_out)
+    return refuse(c, DISC_ERR_INVALID_ARG, "rotary takes positions and 1 .. 4 tensors, as many results, and 3 + 5 dims a tensor");
+  RotaryArgs a;
+  memset(&a, 0, sizeof a);
+  a.tokens = dims[0];
+  a.position_bytes = dims[1] == 8 ? 8 : 4;
+  a.backward = dims[2] != 0;
+  a.n = n_out;
+  if (a.tokens < 0 || a.tokens >= (int64_t)1 << 31) return refuse(c, DISC_ERR_SHAPE, "tokens is 0 .. 2^31 - 1", a.tokens);
+  if (dims[1] != 4 && dims[1] != 8) return refuse(c, DISC_ERR_INVALID_ARG, "positions have 4 or 8 bytes", dims[1]);
+  const int size = dtype_bytes(o->dtype);
+  int64_t most = 0;
+  for (int k = 0; k < n_out; ++k) {
+    const int64_t* s = dims + 3 + 5 * k;
+    if (s[0] < 0 || s[0] > 1 << 20) return refuse(c, DISC_ERR_SHAPE, "heads is 0 .. 2^20", s[0]);
+    if (a.tokens > 0 && s[0] > 0) {
+      if (!strides_ok(a.tokens, s[1], s[0], s[2], o->head_dim) || !strides_ok(a.tokens, s[3], s[0], s[4], o->head_dim))
+        return refuse(c, DISC_ERR_SHAPE, "a stride is negative or an extent overflows");
+      if (!rows_apart(a.tokens, s[3], s[0], s[4], o->head_dim)) return refuse(c, DISC_ERR_SHAPE, "rows of a result overlap");
+      if (!in[1 + k] || !out[k]) return refuse(c, DISC_ERR_INVALID_ARG, "null tensor pointer");
+      if (!aligned(in[1 + k], size) || !aligned(out[k], size)) return refuse(c, DISC_ERR_INVALID_ARG, "a tensor is not aligned to its elements");
+      if (in[1 + k] == out[k] && ((a.tokens > 1 && s[1] != s[3]) || (s[0] > 1 && s[2] != s[4])))
+        return refuse(c, DISC_ERR_INVALID_ARG, "in place, both sides have the same strides");
+    }
+    a.t[k] = {in[1 + k], out[k], s[1], s[2], s[3], s[4], (int32_t)s[0], 0};
+    most = most > s[0] ? most : s[0];
+  }
+  if (a.tokens == 0 || most == 0) return context_device(c) < 0 ? refuse(c, DISC_ERR_INVALID_ARG, "host-only context cannot launch") : DISC_OK;
+  if (!in[0] || !aligned(in[0], a.position_bytes)) return refuse(c, DISC_ERR_INVALID_ARG, "positions: null or not aligned");
+  a.positions = in[0];
+  if (context_device(c) < 0) return refuse(c, DISC_ERR_INVALID_ARG, "host-only context cannot launch");
+  // Tokens a block: enough that every CU has eight blocks; their sines are computed once for all heads.
+  const int64_t blocks8 = (int64_t)context_cus(c) * 8;
+  int64_t per = a.tokens / blocks8;
+  per = per < 1 ? 1 : per > kMaxBlockTokens ? kMaxBlockTokens : per;
+  a.tokens_per_block = (int32_t)per;
+  const int64_t blocks = (a.tokens + per - 1) / per;
+  // Few tokens: the heads are shared out too, one pass of a block's rows each.
+  const int64_t rows = 256 / rotary_units(*o), passes = (most + rows - 1) / rows;
+  const uint32_t y = blocks * 2 <= context_cus(c) ? (uint32_t)(passes < 64 ? passes : 64) : 1;
+  OnDevice on(context_device(c));
+  if (!on.ok) return refuse(c, DISC_ERR_HIP, "hipSetDevice failed");
+  const int rc = enqueue(c, o->fn[FN_ROTARY], (uint64_t)blocks, y, &a, sizeof a, stream);
+  if (rc == DISC_OK) context_count(c, 1);
+  return rc;
+}
+
+// ---- the cache -------------------------------------------------------------------------------------
+
+int register_cache(disc_ctx* c, const disc_cache_desc* d, int32_t* id_out) {
+  if (!c) return DISC_ERR_INVALID_ARG;
+  if (!d || !id_out) return refuse(c, DISC_ERR_INVALID_ARG, "null pointer");
+  if (d->dtype != DISC_F16 && d->dtype != DISC_BF16) return refuse(c, DISC_ERR_INVALID_ARG, "a cache takes f16 or bf16 rows");
+  if (d->storage < DISC_STORAGE_SAME || d->storage > DISC_STORAGE_E4M3) return refuse(c, DISC_ERR_INVALID_ARG, "bad storage");
+  if (d->head_dim < 16 || d->head_dim > 256 || d->head_dim % 16) return refuse(c, DISC_ERR_SHAPE, "head_dim is a multiple of 16, 16 .. 256", d->head_dim);
+  if (!std::isfinite(d->softmax_scale)) return refuse(c, DISC_ERR_INVALID_ARG, "softmax_scale is not finite");
+  const double scale = d->softmax_scale != 0.0 ? d->softmax_scale : 1.0 / std::sqrt((double)d->head_dim);
+  std::string macros = "#define DISC_CACHE 1\n#define DISC_T_F16 " + std::to_string(d->dtype == DISC_F16 ? 1 : 0) + "\n";
+  macros += "#define DISC_STORAGE " + std::to_string(d->storage) + "\n#define DISC_D " + std::to_string(d->head_dim) + "\n";
+  macros += "#define DISC_SCALE_LOG2E " + text("%a", scale * 1.44269504088896340736) + "\n";
+  std::unique_ptr<Operator> o(new Operator);
+  o->kind = Operator::CACHE;
+  o->key = macros;
+  o->dtype = d->dtype;
+  o->storage = d->storage;
+  o->head_dim = d->head_dim;
+  static const char* const names[] = {"disc_store_k", "disc_load_k", "disc_attend_k", "disc_prefix_k", "disc_join_k"};
+  return enter(c, std::move(o), macros, names, 5, id_out);
+}
+
+// page_size = 1 << shift; -1: no page size
+int page_shift(int64_t page_size) {
+  for (int s = 3; s <= 16; ++s)
+    if (page_size == (int64_t)1 << s) return s;
+  return -1;
+}
+
+int check_pages(disc_ctx* c, const Operator& o, int64_t heads, int64_t pages, int64_t page_size, int* shift) {
+  if (heads < 1 || heads > 1 << 16) return refuse(c, DISC_ERR_SHAPE, "kv_heads is 1 .. 65536", heads);
+  *shift = page_shift(page_size);
+  if (*shift < 0) return refuse(c, DISC_ERR_SHAPE, "page_size is a power of two, 8 .. 65536", page_size);
+  if (pages < 1 || pages >= (int64_t)1 << 31) return refuse(c, DISC_ERR_SHAPE, "pages is 1 .. 2^31 - 1", pages);
+  const int64_t rows = times(times(pages, heads), page_size);
+  if (rows < 0 || times(rows, o.head_dim) < 0) return refuse(c, DISC_ERR_SHAPE, "the pages are larger than any memory");
+  return DISC_OK;
+}
+
+int launch_rows(disc_ctx* c, int32_t id, const int64_t* dims, int n_dims, const void* const* in, int n_in, void* const* out, int n_out,
+                void* stream, bool store) {
+  if (!c) return DISC_ERR_INVALID_ARG;
+  const Operator* o = get_operator(c, id, Operator::CACHE);
+  if (!o) return refuse(c, DISC_ERR_INVALID_ARG, "bad cache id");
+  if (!dims || !in || !out) return refuse(c, DISC_ERR_INVALID_ARG, "null pointer array");
+  const bool scaled = o->storage != DISC_STORAGE_SAME;
+  const int n_pages = scaled ? 4 : 2;
+  if (n_dims != 8 || n_in != (store ? 3 : 1 + n_pages) || n_out != (store ? n_pages : 2))
+    return refuse(c, DISC_ERR_INVALID_ARG, "a store or load takes 8 dims, slots, keys and values, the pages and with 8-bit storage their scales");
+  RowsArgs a;
+  memset(&a, 0, sizeof a);
+  a.tokens = dims[0];
+  if (a.tokens < 0 || a.tokens >= (int64_t)1 << 31) return refuse(c, DISC_ERR_SHAPE, "tokens is 0 .. 2^31 - 1", a.tokens);
+  int shift = 0;
+  if (const int rc = check_pages(c, *o, dims[1], dims[2], dims[3], &shift)) return rc;
+  a.heads = (int32_t)dims[1];
+  a.shift = shift;
+  a.slots_end = dims[2] << shift;
+  a.k_token = dims[4];
+  a.k_head = dims[5];
+  a.v_token = dims[6];
+  a.v_head = dims[7];
+  if (a.tokens == 0) return context_device(c) < 0 ? refuse(c, DISC_ERR_INVALID_ARG, "host-only context cannot launch") : DISC_OK;
+  if (!strides_ok(a.tokens, a.k_token, a.heads, a.k_head, o->head_dim) || !strides_ok(a.tokens, a.v_token, a.heads, a.v_head, o->head_dim))
+    return refuse(c, DISC_ERR_SHAPE, "a stride is negative or an extent overflows");
+  if (!store && (!rows_apart(a.tokens, a.k_token, a.heads, a.k_head, o->head_dim) || !rows_apart(a.tokens, a.v_token, a.heads, a.v_head, o->head_dim)))
+    return refuse(c, DISC_ERR_SHAPE, "rows of a result overlap");
+  a.slots = in[0];
+  a.k = store ? in[1] : out[0];
+  a.v = store ? in[2] : out[1];
+  const void* pages[4] = {nullptr, nullptr, nullptr, nullptr};
+  for (int i = 0; i < n_pages; ++i) {
+    pages[i] = store ? out[i] : in[1 + i];
+    if (!pages[i] || !aligned(pages[i], 16)) return refuse(c, DISC_ERR_INVALID_ARG, "pages or scales: null or not 16-byte aligned");
+  }
+  a.kp = pages[0];
+  a.vp = pages[1];
+  a.ks = pages[2];
+  a.vs = pages[3];
+  if (!a.slots || !aligned(a.slots, 8)) return refuse(c, DISC_ERR_INVALID_ARG, "slots: null or not 8-byte aligned");
+  if (!a.k || !a.v || !aligned(a.k, 2) || !aligned(a.v, 2)) return refuse(c, DISC_ERR_INVALID_ARG, "keys or values: null or not aligned to their elements");
+  int lanes = 2;
+  while (lanes * 8 < o->head_dim) lanes *= 2;
+  const int64_t threads = times(times(a.tokens, a.heads), lanes);
+  if (threads < 0 || (threads + 255) / 256 >= (int64_t)1 << 31) return refuse(c, DISC_ERR_SHAPE, "too many rows for one call");
+  if (context_device(c) < 0) return refuse(c, DISC_ERR_INVALID_ARG, "host-only context cannot launch");
+  OnDevice on(context_device(c));
+  if (!on.ok) return refuse(c, DISC_ERR_HIP, "hipSetDevice failed");
+  const int rc = enqueue(c, o->fn[store ? FN_STORE : FN_LOAD], (uint64_t)((threads + 255) / 256), 1, &a, sizeof a, stream);
+  if (rc == DISC_OK) context_count(c, 1);
+  return rc;
+}
+
+// The sizes of an attention call: its chunks, its rows of partial results.  (Pure host.)
+struct AttendPlan {
+  AttendArgs a;
+  int64_t attend_blocks, prefix_blocks, join_blocks;
+  size_t workspace;
+};
+
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+int plan_attend(disc_ctx* c, const Operator& o, const int64_t* d, int n_dims, AttendPlan* p) {
+  if (!d || n_dims != 12) return refuse(c, DISC_ERR_INVALID_ARG, "an attention call takes 12 dims");
+  AttendArgs& a = p->a;
+  memset(&a, 0, sizeof a);
+  const int64_t batch = d[0], heads = d[1], kv = d[2], width = d[5], prefix = d[6], prefix_width = d[7];
+  int shift = 0;
+  if (const int rc = check_pages(c, o, kv, d[3], d[4], &shift)) return rc;
+  if (batch < 0 || batch > 1 << 20) return refuse(c, DISC_ERR_SHAPE, "batch is 0 .. 2^20", batch);
+  if (heads < kv || heads % kv || heads > 1 << 20) return refuse(c, DISC_ERR_SHAPE, "q_heads is a multiple of kv_heads, at most 2^20", heads);
+  if (width < 0 || times(width, d[4]) < 0 || times(width, d[4]) > (int64_t)1 << 30)
+    return refuse(c, DISC_ERR_SHAPE, "table_width * page_size is 0 .. 2^30", width);
+  if (prefix < 0 || prefix > (int64_t)1 << 30) return refuse(c, DISC_ERR_SHAPE, "prefix_length is 0 .. 2^30", prefix);
+  if (prefix_width < ceil_div(prefix, d[4])) return refuse(c, DISC_ERR_SHAPE, "the prefix's table is shorter than the prefix", prefix_width);
+  a.batch = (int32_t)batch;
+  a.heads = (int32_t)heads;
+  a.kv_heads = (int32_t)kv;
+  a.group = (int32_t)(heads / kv);
+  a.pages = (int32_t)d[3];
+  a.shift = shift;
+  a.width = (int32_t)width;
+  a.tiles = (int32_t)ceil_div(a.group, 16);
+  a.prefix_len = (int32_t)prefix;
+  const int64_t cus = context_cus(c), per = kv * a.tiles;
+  // Sequences' own tokens: two blocks of a CU share all lengths, so that they end together whatever the lengths are.
+  a.target = (int32_t)(2 * cus / per > 1 ? 2 * cus / per : 1);
+  a.inv_target = 1.0 / a.target;
+  const int64_t cut = ceil_div(times(batch, width), kMostPages);
+  int64_t parts = batch + (a.target > cut ? a.target : cut);
+  const int64_t whole = times(batch, ceil_div(width << shift, kBlockStep));
+  if (whole >= 0 && whole < parts) parts = whole;
+  // The prefix: blocks of 64 or 128 query rows of a kv head.
+  const int64_t rows = batch * a.group, block_rows = o.head_dim <= 128 ? 128 : 64, row_blocks = ceil_div(rows, block_rows);
+  if (prefix > 0 && batch > 0) {
+    int64_t n = 2 * cus / (kv * row_blocks);
+    const int64_t steps = ceil_div(prefix, kBlockStep);
+    n = n < 1 ? 1 : n > steps ? steps : n;
+    int64_t chunk = ceil_div(ceil_div(prefix, n), kBlockStep) * kBlockStep;
+    const int64_t most = (int64_t)kMostPages << shift;
+    chunk = chunk > most ? most : chunk;
+    a.prefix_chunk = (int32_t)chunk;
+    a.prefix_parts = (int32_t)ceil_div(prefix, chunk);
+  }
+  if (parts >= (int64_t)1 << 31) return refuse(c, DISC_ERR_SHAPE, "too many chunks for one call");
+  a.parts = (int32_t)parts;
+  p->attend_blocks = batch > 0 ? times(parts, per) : 0;
+  p->prefix_blocks = times(a.prefix_parts, kv * row_blocks);
+  p->join_blocks = times(batch, heads);
+  const int64_t partial = times(parts, heads) + times(a.prefix_parts, times(batch, heads));
+  if (p->attend_blocks >= (int64_t)1 << 31 || p->prefix_blocks >= (int64_t)1 << 31 || p->join_blocks >= (int64_t)1 << 31 || times(partial, 4 * 256 + 8) < 0)
+    return refuse(c, DISC_ERR_SHAPE, "too many rows for one call");
+  p->workspace = batch > 0 ? (size_t)partial * ((size_t)o.head_dim * 4 + 8) : 0;
+  return DISC_OK;
+}
+
+int launch_attend(disc_ctx* c, int32_t id, const int64_t* dims, int n_dims, const void* const* in, int n_in, void* const* out, int n_out,
+                  void* workspace, size_t workspace_bytes, void* stream) {
+  if (!c) return DISC_ERR_INVALID_ARG;
+  const Operator* o = get_operator(c, id, Operator::CACHE);
+  if (!o) return refuse(c, DISC_ERR_INVALID_ARG, "bad cache id");
+  if (!dims || !in || !out) return refuse(c, DISC_ERR_INVALID_ARG, "null pointer array");
+  AttendPlan p;
+  if (const int rc = plan_attend(c, *o, dims, n_dims, &p)) return rc;
+  AttendArgs& a = p.a;
+  const bool scaled = o->storage != DISC_STORAGE_SAME;
+  const int want = 5 + (scaled ? 2 : 0) + (a.prefix_len > 0 ? 1 : 0);
+  if (n_in != want || n_out != 1)
+    return refuse(c, DISC_ERR_INVALID_ARG, "an attention call takes q, lengths, table, the pages, with 8-bit storage their scales, with a prefix its table, and one result");
+  a.q_row = dims[8];
+  a.q_head = dims[9];
+  a.o_row = dims[10];
+  a.o_head = dims[11];
+  if (a.batch == 0) return context_device(c) < 0 ? refuse(c, DISC_ERR_INVALID_ARG, "host-only context cannot launch") : DISC_OK;
+  if (!strides_ok(a.batch, a.q_row, a.heads, a.q_head, o->head_dim) || !strides_ok(a.batch, a.o_row, a.heads, a.o_head, o->head_dim))
+    return refuse(c, DISC_ERR_SHAPE, "a stride is negative or an extent overflows");
+  if (!rows_apart(a.batch, a.o_row, a.heads, a.o_head, o->head_dim)) return refuse(c, DISC_ERR_SHAPE, "rows of a result overlap");
+  a.q = in[0];
+  a.lengths = in[1];
+  a.table = in[2];
+  a.kp = in[3];
+  a.vp = in[4];
+  a.ks = scaled ? in[5] : nullptr;
+  a.vs = scaled ? in[6] : nullptr;
+  a.prefix_table = a.prefix_len > 0 ? in[n_in - 1] : nullptr;
+  a.out = out[0];
+  if (!a.q || !a.out || !aligned(a.q, 2) || !aligned(a.out, 2)) return refuse(c, DISC_ERR_INVALID_ARG, "q or out: null or not aligned to its elements");
+  if (!a.lengths || !aligned(a.lengths, 4) || (a.width > 0 && !a.table) || !aligned(a.table, 4) || (a.prefix_len > 0 && !a.prefix_table) ||
+      !aligned(a.prefix_table, 4))
+    return refuse(c, DISC_ERR_INVALID_ARG, "lengths or a table: null or not 4-byte aligned");
+  if (!a.kp || !a.vp || !aligned(a.kp, 16) || !aligned(a.vp, 16) || (scaled && (!a.ks || !a.vs)) || !aligned(a.ks, 16) || !aligned(a.vs, 16))
+    return refuse(c, DISC_ERR_INVALID_ARG, "pages or scales: null or not 16-byte aligned");
+  if (p.workspace > 0 && (!workspace || workspace_bytes < p.workspace)) return refuse(c, DISC_ERR_WORKSPACE, "workspace missing or too small");
+  if (!aligned(workspace, 16)) return refuse(c, DISC_ERR_INVALID_ARG, "the workspace is not 16-byte aligned");
+  a.part = (float*)workspace;
+  const int64_t partial = (int64_t)a.parts * a.heads + (int64_t)a.prefix_parts * a.batch * a.heads;
+  a.part_m = a.part + partial * o->head_dim;
+  if (context_device(c) < 0) return refuse(c, DISC_ERR_INVALID_ARG, "host-only context cannot launch");
+  OnDevice on(context_device(c));
+  if (!on.ok) return refuse(c, DISC_ERR_HIP, "hipSetDevice failed");
+  int rc = DISC_OK, n = 0;
+  if (p.prefix_blocks > 0) {
+    rc = enqueue(c, o->fn[FN_PREFIX], (uint64_t)p.prefix_blocks, 1, &a, sizeof a, stream);
+    ++n;
+  }
+  if (rc == DISC_OK && p.attend_blocks > 0) {
+    rc = enqueue(c, o->fn[FN_ATTEND], (uint64_t)p.attend_blocks, 1, &a, sizeof a, stream);
+    ++n;
+  }
+  if (rc == DISC_OK) rc = enqueue(c, o->fn[FN_JOIN], (uint64_t)p.join_blocks, 1, &a, sizeof a, stream);
+  if (rc == DISC_OK) context_count(c, n + 1);
+  return rc;
+}
+
+int fail_inside(disc_ctx* c, const char* what) noexcept {
+  char buf[160];
+  snprintf(buf, sizeof buf, "internal error: %s", what);
+  if (c) context_fail(c, DISC_ERR_INTERNAL, buf);
+  return DISC_ERR_INTERNAL;
+}
+
+// Nothing leaves a C function by exception.
+template <class F>
+int guarded(disc_ctx* c, F f) noexcept {
+  try {
+    return f();
+  } catch (const std::bad_alloc&) {
+    return fail_inside(c, "out of host memory");
+  } catch (const std::exception& e) {
+    return fail_inside(c, e.what());
+  } catch (...) {
+    return fail_inside(c, "unknown exception");
+  }
+}
+
+}  // namespace
+}  // namespace disc
+
+using namespace disc;
+
+extern "C" {
+
+int disc_register_rotary(disc_ctx* ctx, const disc_rotary_desc* desc, int32_t* id_out) {
+  return guarded(ctx, [&] { return register_rotary(ctx, desc, id_out); });
+}
+int disc_register_cache(disc_ctx* ctx, const disc_cache_desc* desc, int32_t* id_out) {
+  return guarded(ctx, [&] { return register_cache(ctx, desc, id_out); });
+}
+int disc_rotary(disc_ctx* ctx, int32_t id, const int64_t* dims, int n_dims, const void* const* inputs, int n_in, void* const* outputs, int n_out,
+                void*, size_t, void* hip_stream) {
+  return guarded(ctx, [&] { return launch_rotary(ctx, id, dims, n_dims, inputs, n_in, outputs, n_out, hip_stream); });
+}
+int disc_cache_store(disc_ctx* ctx, int32_t id, const int64_t* dims, int n_dims, const void* const* inputs, int n_in, void* const* outputs,
+                     int n_out, void*, size_t, void* hip_stream) {
+  return guarded(ctx, [&] { return launch_rows(ctx, id, dims, n_dims, inputs, n_in, outputs, n_out, hip_stream, true); });
+}
+int disc_cache_load(disc_ctx* ctx, int32_t id, const int64_t* dims, int n_dims, const void* const* inputs, int n_in, void* const* outputs,
+                    int n_out, void*, size_t, void* hip_stream) {
+  return guarded(ctx, [&] { return launch_rows(ctx, id, dims, n_dims, inputs, n_in, outputs, n_out, hip_stream, false); });
+}
+int disc_cache_attend(disc_ctx* ctx, int32_t id, const int64_t* dims, int n_dims, const void* const* inputs, int n_in, void* const* outputs,
+                      int n_out, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  return guarded(ctx, [&] { return launch_attend(ctx, id, dims, n_dims, inputs, n_in, outputs, n_out, workspace, workspace_bytes, hip_stream); });
+}
+int disc_cache_workspace_bytes(disc_ctx* ctx, int32_t id, const int64_t* dims, int n_dims, size_t* out) {
+  return guarded(ctx, [&] {
+    if (!ctx || !out) return (int)DISC_ERR_INVALID_ARG;
+    const Operator* o = get_operator(ctx, id, Operator::CACHE);
+    if (!o) return refuse(ctx, DISC_ERR_INVALID_ARG, "bad cache id");
+    AttendPlan p;
+    const int rc = plan_attend(ctx, *o, dims, n_dims, &p);
+    if (rc == DISC_OK) *out = p.workspace;
+    return rc;
+  });
+}
+
+}  // extern "C"

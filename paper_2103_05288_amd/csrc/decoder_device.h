@@ -1,0 +1,913 @@
+// Device code of the operators around a decoder's attention: rotary positions, the cache of keys and
+// values in pages, attention over it.  Compiled through hipRTC once per registration, with what never
+// changes between calls as macros (element types, head size, softmax scale, the rotation's frequencies);
+// batch, heads, lengths, page size and strides are arguments.
+//
+//   DISC_ROTARY:  DISC_T, DISC_D, DISC_R, DISC_INTERLEAVED, DISC_MAGNITUDE, kTurns[DISC_R / 2]
+//   DISC_CACHE:   DISC_T_F16 (0: bf16), DISC_STORAGE (0: as the activations, 1: i8, 2: e4m3), DISC_D, DISC_SCALE_LOG2E
+#pragma once
+typedef unsigned char u8;
+typedef unsigned short u16;
+typedef unsigned int u32;
+typedef long long i64;
+typedef unsigned long long u64;
+typedef u32 u32x2 __attribute__((ext_vector_type(2)));
+typedef u32 u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+#define DISC_DEV __device__ __forceinline__
+
+// wide accesses at any element's address (the operands' strides and pointers are the caller's)
+typedef u32x2 u32x2_u __attribute__((aligned(1)));
+typedef u32x4 u32x4_u __attribute__((aligned(1)));
+
+#ifdef DISC_ROTARY
+// =================================================================================================
+// Rotary positions.  Pair j of a head's first R elements turns by the angle p f_j of its token's
+// position p and is scaled by the magnitude; the gradient is the turn back with the same magnitude.
+//   y_a = m (x_a cos - x_b sin),  y_b = m (x_b cos + x_a sin),   (a, b) = (j, j + R/2) or (2j, 2j + 1)
+// kTurns[j] = f_j / (pi/2): quarter turns a position.  p kTurns[j] is formed in 64 bits (in 32 the angle
+// of position 10^6 would be off by 0.06), reduced to an eighth of a turn each side of a quarter, and only
+// then rounded to 32 bits.
+// One block: DISC_TOKENS tokens at most.  The sines are computed once for all heads of a token and kept
+// in LDS; then the block streams the heads' rows.  Bound by memory traffic (one read, one write).
+// =================================================================================================
+constexpr int kMaxTensors = 4;
+struct RotaryTensor {
+  const DISC_T* x;
+  DISC_T* y;
+  i64 x_token, x_head, y_token, y_head;   // strides in elements
+  int heads;
+};
+struct RotaryArgs {
+  RotaryTensor t[kMaxTensors];
+  const void* positions;
+  i64 tokens;
+  int n, position_bytes, backward, tokens_per_block;
+};
+
+constexpr int kD = DISC_D, kR = DISC_R, kH = kR / 2;
+constexpr int kMaxBlockTokens = 8;
+
+// elements of one access: 16 bytes, or less where the pairs or the rest of the head do not divide
+constexpr int vec_width() {
+  int w = 16 / (int)sizeof(DISC_T);
+  while (kH % w || (kD - kR) % w) w /= 2;
+  return w;
+}
+constexpr int kW = vec_width();
+constexpr int kTurnUnits = kH / kW, kUnits = kTurnUnits + (kD - kR) / kW;
+static_assert(kUnits <= 256, "a head is one pass of a block at most");
+
+typedef DISC_T vec_t __attribute__((ext_vector_type(kW)));
+typedef vec_t vec_u __attribute__((aligned(alignof(DISC_T))));
+
+extern "C" __global__ void __launch_bounds__(256) disc_rotary_k(RotaryArgs A) {
+  __shared__ float cs[kMaxBlockTokens][kH], sn[kMaxBlockTokens][kH];
+  const i64 t0 = (i64)blockIdx.x * A.tokens_per_block;
+  const int nt = (int)(A.tokens - t0 < A.tokens_per_block ? A.tokens - t0 : A.tokens_per_block);
+  for (int i = threadIdx.x; i < nt * kH; i += 256) {
+    const int t = i / kH, j = i - t * kH;
+    const double p = A.position_bytes == 8 ? (double)((const i64*)A.positions)[t0 + t] : (double)((const int*)A.positions)[t0 + t];
+    const double turns = p * kTurns[j], quarter = rint(turns);
+    float s, c;
+    sincospif((float)(turns - quarter) * 0.5f, &s, &c);
+    const int q = (int)((i64)quarter & 3);
+    const float sq = q & 1 ? c : s, cq = q & 1 ? s : c;      // sin, cos of the angle up to their signs
+    const float m = (float)DISC_MAGNITUDE;
+    cs[t][j] = (q == 1 || q == 2 ? -cq : cq) * m;
+    sn[t][j] = ((q & 2) != 0) != (A.backward != 0) ? -sq * m : sq * m;
+  }
+  __syncthreads();
+  constexpr int kRows = 256 / kUnits;                         // (token, head) rows of one pass
+  const int u = threadIdx.x % kUnits, r0 = threadIdx.x / kUnits;
+  if (r0 >= kRows) return;
+  for (int k = 0; k < A.n; ++k) {
+    const RotaryTensor& X = A.t[k];
+    // blockIdx.y: a share of the heads, for calls of few tokens
+    const int h_lo = (int)((i64)X.heads * blockIdx.y / gridDim.y), nh = (int)((i64)X.heads * (blockIdx.y + 1) / gridDim.y) - h_lo;
+    if (nh == 0) continue;
+    const bool apart = X.x != X.y;                            // in place, the rest of a head is there already
+    int t = r0 / nh, h = r0 - t * nh;
+    while (t < nt) {
+      const DISC_T* x = X.x + (t0 + t) * X.x_token + (h_lo + h) * X.x_head;
+      DISC_T* y = X.y + (t0 + t) * X.y_token + (h_lo + h) * X.y_head;
+      if (u < kTurnUnits) {
+        const int j = u * kW;
+        const int a = DISC_INTERLEAVED ? 2 * j : j, b = DISC_INTERLEAVED ? 2 * j + kW : kH + j;
+        const vec_t xa = *(const vec_u*)(x + a), xb = *(const vec_u*)(x + b);
+        vec_t ya, yb;
+#pragma unroll
+        for (int e = 0; e < kW; ++e) {
+          const float c = cs[t][j + e], s = sn[t][j + e];
+          if (DISC_INTERLEAVED && kW > 1) {
+            const int i = 2 * e % kW;
+            const float p0 = (float)(2 * e < kW ? xa[i] : xb[i]), p1 = (float)(2 * e < kW ? xa[i + 1] : xb[i + 1]);
+            const DISC_T v0 = (DISC_T)(p0 * c - p1 * s), v1 = (DISC_T)(p1 * c + p0 * s);
+            if (2 * e < kW) ya[i] = v0, ya[i + 1] = v1;
+            else yb[i] = v0, yb[i + 1] = v1;
+          } else {
+            const float p0 = (float)xa[e], p1 = (float)xb[e];
+            ya[e] = (DISC_T)(p0 * c - p1 * s);
+            yb[e] = (DISC_T)(p1 * c + p0 * s);
+          }
+        }
+        *(vec_u*)(y + a) = ya;
+        *(vec_u*)(y + b) = yb;
+      } else if (apart) {
+        const int a = kR + (u - kTurnUnits) * kW;
+        *(vec_u*)(y + a) = *(const vec_u*)(x + a);
+      }
+      h += kRows;
+      while (h >= nh) h -= nh, ++t;
+    }
+  }
+}
+#endif  // DISC_ROTARY
+
+#ifdef DISC_CACHE
+// =================================================================================================
+// The cache: keys and values in pages [page][kv head][place][D], and where they are quantised a scale
+// for every row [page][kv head][place].  A slot is page * page_size + place.
+// =================================================================================================
+#if DISC_T_F16
+typedef _Float16 T;
+#else
+typedef __bf16 T;
+#endif
+typedef T Tx2 __attribute__((ext_vector_type(2)));
+typedef T Tx8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+constexpr int kD = DISC_D;
+constexpr bool kQuantised = DISC_STORAGE != 0;
+constexpr int kSize = kQuantised ? 1 : 2;                  // bytes of a stored element
+constexpr float kMost = DISC_STORAGE == 1 ? 127.f : 448.f; // largest code
+
+struct RowsArgs {
+  const i64* slots;
+  T* k;                     // rows of activations (read by the store, written by the load)
+  T* v;
+  u8* kp;
+  u8* vp;
+  float* ks;
+  float* vs;
+  i64 k_token, k_head, v_token, v_head;
+  i64 tokens, slots_end;    // slots_end = pages * page_size
+  int heads, shift;         // page_size = 1 << shift
+};
+
+// First row of a slot in the pages, in rows: (page * heads + head) * page_size + place.
+DISC_DEV i64 page_row(i64 slot, int head, int heads, int shift) {
+  return ((((slot >> shift) * heads) + head) << shift) + (slot & ((1ll << shift) - 1));
+}
+
+constexpr int kLanes = kD <= 16 ? 2 : kD <= 32 ? 4 : kD <= 64 ? 8 : kD <= 128 ? 16 : 32;   // lanes of a row, eight elements each
+
+DISC_DEV float f32_of(u32 pair, int hi) {
+  return (float)__builtin_bit_cast(Tx2, pair)[hi];
+}
+
+// Eight values to eight codes.  x * inverse is rounded once to 32 bits and once to the code (half to even).
+DISC_DEV u32x2 encode(const u32x4& x, float inverse) {
+  u32x2 c;
+#pragma unroll
+  for (int w = 0; w < 2; ++w) {
+    float y[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = __builtin_amdgcn_fmed3f(f32_of(x[w * 2 + e / 2], e & 1) * inverse, -kMost, kMost);
+#if DISC_STORAGE == 2
+    int p = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
+    c[w] = (u32)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], p, true);
+#else
+    u32 p = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) p |= ((u32)(int)__builtin_rintf(y[e]) & 0xffu) << (8 * e);
+    c[w] = p;
+#endif
+  }
+  return c;
+}
+
+// Stores rows of keys and values.  Scale of a row: a / kMost with a its largest magnitude; code of an
+// element: round(x * (kMost / a)).  The magnitude is compared as the bits of |x|, so that a NaN counts as
+// larger than an infinity: a row that holds either gets the scale NaN and codes of zero, and reads back as
+// NaN.  A row of zeros has the scale 0.  Slots outside the pages are left out.
+// Keys and values of a (token, head) are one lane group's, so that two loads are in flight a lane.
+extern "C" __global__ void __launch_bounds__(256) disc_store_k(RowsArgs A) {
+  const i64 row = ((i64)blockIdx.x * 256 + threadIdx.x) / kLanes;
+  const int lane = threadIdx.x % kLanes;
+  const i64 t = row / A.heads;
+  const int h = (int)(row - t * A.heads);
+  if (t >= A.tokens) return;
+  const i64 slot = A.slots[t];
+  if (slot < 0 || slot >= A.slots_end) return;
+  const i64 to = page_row(slot, h, A.heads, A.shift);
+  const bool mine = lane * 8 < kD;
+  u32x4 x[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+  if (mine) {
+    x[0] = *(const u32x4_u*)(A.k + t * A.k_token + h * A.k_head + lane * 8);
+    x[1] = *(const u32x4_u*)(A.v + t * A.v_token + h * A.v_head + lane * 8);
+  }
+  if (!kQuantised) {
+    if (mine) {
+      *(u32x4*)(A.kp + (to * kD + lane * 8) * 2) = x[0];
+      *(u32x4*)(A.vp + (to * kD + lane * 8) * 2) = x[1];
+    }
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    // (the bits of 16-bit magnitudes order as the magnitudes do, NaN above infinity)
+    u32 a = 0;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const u32 lo = x[i][w] & 0x7fffu, hi = (x[i][w] >> 16) & 0x7fffu;
+      a = max(a, max(lo, hi));
+    }
+#pragma unroll
+    for (int s = 1; s < kLanes; s *= 2) a = max(a, (u32)__shfl_xor((int)a, s));
+    const float m = (float)__builtin_bit_cast(T, (u16)a);
+    const bool fine = m < __builtin_inff();
+    const float inverse = fine && m > 0.f ? kMost / m : 0.f;
+    u32x2 c = {0, 0};
+    if (fine) c = encode(x[i], inverse);
+    if (mine) *(u32x2*)((i ? A.vp : A.kp) + to * kD + lane * 8) = c;
+    if (lane == 0) (i ? A.vs : A.ks)[to] = fine ? m / kMost : __builtin_nanf("");
+  }
+}
+
+// Reads rows back: code * scale, rounded once.  A slot outside the pages gives a row of zeros.
+extern "C" __global__ void __launch_bounds__(256) disc_load_k(RowsArgs A) {
+  const i64 row = ((i64)blockIdx.x * 256 + threadIdx.x) / kLanes;
+  const int lane = threadIdx.x % kLanes;
+  const i64 t = row / A.heads;
+  const int h = (int)(row - t * A.heads);
+  if (t >= A.tokens || lane * 8 >= kD) return;
+  const i64 slot = A.slots[t];
+  const bool there = slot >= 0 && slot < A.slots_end;
+  const i64 from = there ? page_row(slot, h, A.heads, A.shift) : 0;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    u32x4 y = {0, 0, 0, 0};
+    if (there) {
+      if (!kQuantised) {
+        y = *(const u32x4*)((i ? A.vp : A.kp) + (from * kD + lane * 8) * 2);
+      } else {
+        const u32x2 c = *(const u32x2*)((i ? A.vp : A.kp) + from * kD + lane * 8);
+        const float s = (i ? A.vs : A.ks)[from];
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          float f[2];
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const int at = (w * 2 + e) % 4;
+#if DISC_STORAGE == 2
+            f[e] = at == 0   ? __builtin_amdgcn_cvt_f32_fp8((int)c[w / 2], 0)
+                   : at == 1 ? __builtin_amdgcn_cvt_f32_fp8((int)c[w / 2], 1)
+                   : at == 2 ? __builtin_amdgcn_cvt_f32_fp8((int)c[w / 2], 2)
+                             : __builtin_amdgcn_cvt_f32_fp8((int)c[w / 2], 3);
+#else
+            f[e] = (float)(signed char)(c[w / 2] >> (8 * at));
+#endif
+          }
+          const Tx2 p = {(T)(f[0] * s), (T)(f[1] * s)};
+          y[w] = __builtin_bit_cast(u32, p);
+        }
+      }
+    }
+    T* to = i ? A.v + t * A.v_token + h * A.v_head : A.k + t * A.k_token + h * A.k_head;
+    *(u32x4_u*)(to + lane * 8) = y;
+  }
+}
+
+// =================================================================================================
+// Attention of one query token a sequence over its pages:
+//   o = sum_t p_t v_t / sum_t p_t,   p_t = 2^(c q.k_t - m),   c = softmax scale * log2(e)
+// in one pass over the keys and values with the running maximum m.
+//
+// Products on the matrix cores, 16 x 16 x 32.  A step is 32 tokens; the 16 columns are the query heads
+// that share a kv head.  S^T = K Q^T: row i of tile mt takes the key of token 8 (i / 4) + 4 mt + i % 4, so
+// that a lane's results are the scores of eight neighbouring tokens 8 g + 0..7 (g = lane / 16) -- which is
+// what the second product O^T = V^T P^T wants as its operand: the probabilities never leave their
+// registers.  A lane reads, of those eight tokens, E neighbouring elements of the values; what is row
+// d of V^T in the matrix product is then spread over eight registers of the same lane, and byte permutes
+// put it together: the values need no LDS either.
+//
+// 8-bit codes are exact in 16-bit floating point; a key's scale multiplies its score, a value's scale
+// its probability.  Those products p * scale are taken to half precision relative to a power of two that
+// follows the largest scale seen, as the probabilities follow the largest score.
+// Where the probabilities would have no more bits than the result they are held as a sum of two 16-bit
+// numbers (hi + lo), so that the only rounding that counts is the result's.
+//
+// A block is four wavefronts; they take the steps of a chunk in turn and join in LDS at its end.  Chunks
+// are cut from the lengths, on the device, so that all blocks have about the same share.
+// =================================================================================================
+constexpr int kStep = 32;                     // tokens of a step
+constexpr int kMostPages = 2048;              // pages of a chunk, kept in LDS
+constexpr int kE = kD % 128 == 0 ? 8 : kD % 64 == 0 ? 4 : 8;    // neighbouring elements of a value that a lane reads
+constexpr int kNB = (kD + 16 * kE - 1) / (16 * kE);             // such groups of 16 lanes
+constexpr int kND = kE * kNB;                                   // 16-row tiles of O^T
+constexpr int kKE = 16 / kSize;                                 // elements of a key that a lane reads at once
+constexpr int kNK = (kD + 4 * kKE - 1) / (4 * kKE);             // such reads
+constexpr int kVW = kE * kSize / 4;                             // registers of one value read
+// type of the second product, and whether its probabilities are split
+#if DISC_T_F16
+constexpr bool kSplit = true;
+#else
+constexpr bool kSplit = !kQuantised;
+#endif
+
+struct AttendArgs {
+  const T* q;
+  const int* lengths;
+  const int* table;
+  const u8* kp;
+  const u8* vp;
+  const float* ks;
+  const float* vs;
+  const int* prefix_table;
+  T* out;
+  float* part;              // unnormalised results [part][heads of q of the kv heads][D]
+  float* part_m;            // their running maximum and sum, two floats a row
+  i64 q_row, q_head, o_row, o_head;
+  int batch, heads, kv_heads, group, pages, shift, width, tiles;
+  int target;               // chunks a kv head that the lengths are cut into, about
+  int parts;                // chunks there can be at most
+  int prefix_len, prefix_chunk, prefix_parts;
+  double inv_target;
+};
+
+struct Item {
+  int b, begin, end;        // sequence, its tokens [begin, end)
+  int first, count;         // the sequence's chunks
+};
+
+DISC_DEV int clamp_length(int n, int width, int shift) {
+  const i64 most = (i64)width << shift;
+  return n < 0 ? 0 : n > most ? (int)most : n;
+}
+DISC_DEV int chunk_of(double total, double inv_target, int shift) {
+  // tokens of a chunk: more than total / target, whole steps of four wavefronts
+  const i64 least = (i64)(total * inv_target) + 1;
+  const i64 whole = (least + 4 * kStep - 1) / (4 * kStep) * (4 * kStep);
+  const i64 most = (i64)kMostPages << shift;
+  return (int)(whole < most ? whole : most);
+}
+
+// The chunk number `item` (want_b < 0) or the chunks of sequence want_b; every lane of the wavefront gets it.
+DISC_DEV bool find_item(const AttendArgs& A, int item, int want_b, Item& I) {
+  const int lane = threadIdx.x & 63;
+  double total = 0;
+  for (int b0 = 0; b0 < A.batch; b0 += 64) {
+    const int b = b0 + lane;
+    int n = b < A.batch ? clamp_length(A.lengths[b], A.width, A.shift) : 0;
+    // (sums of 64 lengths fit 38 bits: exact in a double)
+    double s = (double)n;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) s += __shfl_xor(s, d);
+    total += s;
+  }
+  const int chunk = chunk_of(total, A.inv_target, A.shift);
+  int before = 0;
+  for (int b0 = 0; b0 < A.batch; b0 += 64) {
+    const int b = b0 + lane;
+    const int n = b < A.batch ? clamp_length(A.lengths[b], A.width, A.shift) : 0;
+    const int c = n ? (int)((u32)(n - 1) / (u32)chunk) + 1 : 0;
+    int incl = c;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+      const int x = __shfl_up(incl, d);
+      if (lane >= d) incl += x;
+    }
+    const int first = before + incl - c;
+    const bool hit = want_b >= 0 ? b == want_b : item >= first && item < first + c;
+    const u64 who = __ballot(hit);
+    if (who) {
+      const int l = __ffsll((unsigned long long)who) - 1;
+      I.b = b0 + l;
+      I.first = __builtin_amdgcn_readlane(first, l);
+      I.count = __builtin_amdgcn_readlane(c, l);
+      const int len = __builtin_amdgcn_readlane(n, l);
+      I.begin = want_b >= 0 ? 0 : (item - I.first) * chunk;
+      I.end = want_b >= 0 || len - I.begin < chunk ? len : I.begin + chunk;
+      return true;
+    }
+    before += __builtin_amdgcn_readlane(incl, 63);
+  }
+  return false;
+}
+
+#if DISC_T_F16
+DISC_DEV f32x4 mfma_q(u32x4 a, u32x4 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+#else
+DISC_DEV f32x4 mfma_q(u32x4 a, u32x4 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(Tx8, a), __builtin_bit_cast(Tx8, b), c, 0, 0, 0);
+}
+#endif
+// the second product: in half precision where the values are codes
+DISC_DEV f32x4 mfma_v(u32x4 a, u32x4 b, f32x4 c) {
+  if (kQuantised) return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+  return mfma_q(a, b, c);
+}
+
+// two bytes (the low bytes of each half of x) as half-precision numbers
+DISC_DEV u32 half_of_codes(u32 x) {
+#if DISC_STORAGE == 2
+  return 0;
+#else
+  // 0x6400 + u is the half 1024 + u; u = code + 128
+  const f16x2 y = __builtin_bit_cast(f16x2, x ^ 0x64806480u) - (f16x2){(_Float16)1152.f, (_Float16)1152.f};
+  return __builtin_bit_cast(u32, y);
+#endif
+}
+
+// Eight neighbouring codes (two registers) as eight elements of q's type.
+DISC_DEV u32x4 keys_of_codes(u32 a, u32 b) {
+  u32x4 r;
+#pragma unroll
+  for (int w = 0; w < 2; ++w) {
+    const u32 x = w ? b : a;
+#if DISC_STORAGE == 2
+#if DISC_T_F16
+    r[2 * w] = __builtin_bit_cast(u32, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)x, 1.f, false));
+    r[2 * w + 1] = __builtin_bit_cast(u32, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)x, 1.f, true));
+#else
+    r[2 * w] = __builtin_bit_cast(u32, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)x, 1.f, false));
+    r[2 * w + 1] = __builtin_bit_cast(u32, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)x, 1.f, true));
+#endif
+#elif DISC_T_F16
+    r[2 * w] = half_of_codes(__builtin_amdgcn_perm(x, x, 0x0c010c00u));
+    r[2 * w + 1] = half_of_codes(__builtin_amdgcn_perm(x, x, 0x0c030c02u));
+#else
+    float f[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) f[e] = (float)(signed char)(x >> (8 * e));
+    // (a code has eight significant bits at most: the upper half of its 32-bit form is exact)
+    r[2 * w] = __builtin_amdgcn_perm(__builtin_bit_cast(u32, f[1]), __builtin_bit_cast(u32, f[0]), 0x07060302u);
+    r[2 * w + 1] = __builtin_amdgcn_perm(__builtin_bit_cast(u32, f[3]), __builtin_bit_cast(u32, f[2]), 0x07060302u);
+#endif
+  }
+  return r;
+}
+
+template <int RT>
+struct Rows {                                // RT x 16 query rows of a wavefront
+  u32x4 q[RT][kNK * (kKE / 8)];
+  f32x4 o[RT][kND];
+  float m[RT], use[RT], l[RT];               // running maximum, the same or 0, this lane's share of the sum
+  float vinv, vlim;                          // power of two that values' scales are taken relative to
+};
+struct Keys {
+  u32x4 k[2][kNK];
+  float s[8];
+};
+struct Values {
+  u32 v[8][kNB * kVW];
+  float s[8];
+};
+
+DISC_DEV void load_scales(float (&s)[8], const float* p, i64 row) {
+  const f32x4 a = *(const f32x4*)(p + row), b = *(const f32x4*)(p + row + 4);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) s[j] = a[j], s[4 + j] = b[j];
+}
+
+// `ids`: the chunk's pages in LDS (-1: none), from the page of `begin` on; t0: the step's first token.
+DISC_DEV i64 row_of(const AttendArgs& A, const int* ids, int base, int t, int h, int& id) {
+  id = ids[(t >> A.shift) - base];
+  const int p = id < 0 ? 0 : id;
+  return ((((i64)p * A.kv_heads) + h) << A.shift) + (t & ((1 << A.shift) - 1));
+}
+
+DISC_DEV void load_keys(const AttendArgs& A, const int* ids, int base, int last, int t0, int h, Keys& K) {
+  const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
+  int id;
+  const int t = min(t0 + (m >> 2) * 8, last);
+  const i64 row = row_of(A, ids, base, t, h, id);
+#pragma unroll
+  for (int mt = 0; mt < 2; ++mt) {
+    const u8* p = A.kp + (row + mt * 4 + (m & 3)) * (kD * kSize) + g * 16;
+#pragma unroll
+    for (int i = 0; i < kNK; ++i) {
+      if ((i + 1) * 64 <= kD * kSize || i * 64 + g * 16 < kD * kSize) K.k[mt][i] = *(const u32x4*)(p + i * 64);
+      else K.k[mt][i] = (u32x4){0, 0, 0, 0};
+    }
+  }
+  if (kQuantised) {
+    const i64 srow = row_of(A, ids, base, min(t0 + g * 8, last), h, id);
+    load_scales(K.s, A.ks, srow);
+  }
+}
+
+DISC_DEV int load_values(const AttendArgs& A, const int* ids, int base, int last, int t0, int h, Values& V) {
+  const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
+  int id;
+  const int t = min(t0 + g * 8, last);
+  const i64 row = row_of(A, ids, base, t, h, id);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+#pragma unroll
+    for (int n = 0; n < kNB; ++n) {
+      const u8* p = A.vp + (row + j) * (kD * kSize) + (n * 16 + c) * kE * kSize;
+      const bool mine = (n + 1) * 16 * kE <= kD || (n * 16 + c) * kE < kD;
+      if (kVW == 4) {
+        u32x4 x = {0, 0, 0, 0};
+        if (mine) x = *(const u32x4*)p;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) V.v[j][n * kVW + w % kVW] = x[w];
+      } else if (kVW == 2) {
+        u32x2 x = {0, 0};
+        if (mine) x = *(const u32x2*)p;
+#pragma unroll
+        for (int w = 0; w < 2; ++w) V.v[j][n * kVW + w % kVW] = x[w];
+      } else {
+        V.v[j][n * kVW] = mine ? *(const u32*)p : 0u;
+      }
+    }
+  }
+  if (kQuantised) load_scales(V.s, A.vs, row);
+  return id;
+}
+
+// Row d of V^T: element i of the lane's eight tokens, as the second product's operand.
+DISC_DEV u32x4 column_of(const Values& V, int n, int i) {
+  u32x4 r;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    if (!kQuantised) {
+      const u32 a = V.v[2 * w][n * kVW + i / 2], b = V.v[2 * w + 1][n * kVW + i / 2];
+      r[w] = __builtin_amdgcn_perm(b, a, i & 1 ? 0x07060302u : 0x05040100u);
+    } else {
+      const u32 a = V.v[2 * w][n * kVW + i / 4], b = V.v[2 * w + 1][n * kVW + i / 4];
+      const u32 e = i & 3;
+#if DISC_STORAGE == 2
+      const u32 x = __builtin_amdgcn_perm(b, a, 0x0c0c0400u + 0x0101u * e);
+      r[w] = __builtin_bit_cast(u32, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)x, 1.f, false));
+#else
+      r[w] = half_of_codes(__builtin_amdgcn_perm(b, a, 0x0c040c00u + 0x00010001u * e));
+#endif
+    }
+  }
+  return r;
+}
+
+DISC_DEV float max_of_groups(float x) {      // over the four lane groups that share a query row
+  x = fmaxf(x, __shfl_xor(x, 16));
+  return fmaxf(x, __shfl_xor(x, 32));
+}
+
+template <int RT>
+DISC_DEV void scores(const Rows<RT>& R, const Keys& K, f32x4 (&s)[RT][2]) {
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+    for (int mt = 0; mt < 2; ++mt) s[rt][mt] = (f32x4){0, 0, 0, 0};
+#pragma unroll
+  for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+    for (int i = 0; i < kNK; ++i) {
+      if (!kQuantised) {
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) s[rt][mt] = mfma_q(K.k[mt][i], R.q[rt][i], s[rt][mt]);
+      } else {
+#pragma unroll
+        for (int f = 0; f < 2; ++f) {
+          const u32x4 k = keys_of_codes(K.k[mt][i][2 * f], K.k[mt][i][2 * f + 1]);
+#pragma unroll
+          for (int rt = 0; rt < RT; ++rt) s[rt][mt] = mfma_q(k, R.q[rt][(i * 2 + f) % (kNK * (kKE / 8))], s[rt][mt]);
+        }
+      }
+    }
+}
+
+constexpr float kLag = 8.f;       // a score may pass the running maximum by this many powers of two
+constexpr float kNone = -__builtin_inff();
+
+// The step's probabilities (in s, in place of the scores) and the running maximum, sum and result.
+template <int RT>
+DISC_DEV void softmax_step(Rows<RT>& R, f32x4 (&s)[RT][2], const float (&ks)[8], float (&vs)[8], int live) {
+  const bool whole = __ballot(live < 8) == 0;     // every token of the step is there
+  bool late = false;
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    float top = kNone;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      float x = s[rt][j / 4][j % 4] * ks[j];
+      if (!whole) x = j < live ? x : kNone;
+      s[rt][j / 4][j % 4] = x;
+      top = fmaxf(top, x);
+    }
+    late |= top > R.m[rt] + kLag;
+  }
+  float vtop = 0.f;
+  if (kQuantised) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      if (!whole) vs[j] = j < live ? vs[j] : 0.f;
+      vtop = fmaxf(vtop, vs[j]);
+    }
+    late |= vtop > R.vlim;
+  }
+  if (__ballot(late)) {                           // seldom after the first steps
+    float vscale = 1.f;
+    if (kQuantised) {
+      float v = max_of_groups(vtop);
+      if (v > R.vlim) {
+        int e;
+        (void)__builtin_frexpf(v, &e);
+        e = e < -100 ? -100 : e;
+        const float vinv = __builtin_ldexpf(1.f, -e);
+        vscale = R.vinv > 0.f ? vinv / R.vinv : 0.f;
+        R.vinv = vinv;
+        R.vlim = 8.f / vinv;
+      }
+    }
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      float top = kNone;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) top = fmaxf(top, s[rt][j / 4][j % 4]);
+      top = fmaxf(max_of_groups(top), R.m[rt]);
+      const float use = top > kNone ? top : 0.f;
+      const float alpha = R.m[rt] > kNone ? __builtin_amdgcn_exp2f(R.m[rt] - use) : 0.f;
+      R.m[rt] = top;
+      R.use[rt] = use;
+      R.l[rt] *= alpha;
+#pragma unroll
+      for (int d = 0; d < kND; ++d) R.o[rt][d] *= alpha * vscale;
+    }
+  }
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    float sum = 0.f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      float p = __builtin_amdgcn_exp2f(s[rt][j / 4][j % 4] - R.use[rt]);
+      sum += p;
+      if (kQuantised) p *= vs[j] * R.vinv;
+      s[rt][j / 4][j % 4] = p;
+    }
+    R.l[rt] += sum;
+  }
+}
+
+#if DISC_T_F16 || DISC_STORAGE != 0
+typedef _Float16 P;
+#else
+typedef __bf16 P;
+#endif
+typedef P Px2 __attribute__((ext_vector_type(2)));
+
+template <int RT>
+DISC_DEV void accumulate(Rows<RT>& R, const f32x4 (&s)[RT][2], Values& V, int live) {
+  if (__ballot(live < 8)) {                       // what is behind the end may hold anything: 0 * NaN is no 0
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+#pragma unroll
+      for (int w = 0; w < kNB * kVW; ++w) V.v[j][w] = j < live ? V.v[j][w] : 0u;
+  }
+  u32x4 hi[RT], lo[RT];
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const float a = s[rt][w / 2][(2 * w) % 4], b = s[rt][w / 2][(2 * w + 1) % 4];
+      const Px2 h = {(P)a, (P)b};
+      hi[rt][w] = __builtin_bit_cast(u32, h);
+      if (kSplit) {
+        const Px2 r = {(P)(a - (float)h[0]), (P)(b - (float)h[1])};
+        lo[rt][w] = __builtin_bit_cast(u32, r);
+      }
+    }
+#pragma unroll
+  for (int n = 0; n < kNB; ++n)
+#pragma unroll
+    for (int i = 0; i < kE; ++i) {
+      const u32x4 v = column_of(V, n, i);
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+        R.o[rt][n * kE + i] = mfma_v(v, hi[rt], R.o[rt][n * kE + i]);
+        if (kSplit) R.o[rt][n * kE + i] = mfma_v(v, lo[rt], R.o[rt][n * kE + i]);
+      }
+    }
+}
+
+// The tokens begin + first, + stride, ... (steps of 32) up to end, for the rows of one wavefront.
+template <int RT>
+DISC_DEV void attend_tokens(const AttendArgs& A, const int* ids, int begin, int end, int first, int stride, int h, Rows<RT>& R) {
+  const int g = (threadIdx.x & 63) >> 4, base = begin >> A.shift;
+  int t0 = begin + first;
+  if (t0 >= end) return;
+  // (places behind the chunk's last token are read at its last group of eight: in the page, masked below)
+  const int last = (end - 1) & ~7;
+  Keys K;
+  Values V;
+  load_keys(A, ids, base, last, t0, h, K);
+  int id = load_values(A, ids, base, last, t0, h, V);
+  while (true) {
+    f32x4 s[RT][2];
+    const int n = end - (t0 + g * 8);
+    const int live = id < 0 || n <= 0 ? 0 : n < 8 ? n : 8;
+    float ks[8];
+    scores<RT>(R, K, s);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) ks[j] = (kQuantised ? K.s[j] : 1.f) * (float)(DISC_SCALE_LOG2E);
+    const int next = t0 + stride;
+    if (next < end) load_keys(A, ids, base, last, next, h, K);
+    softmax_step<RT>(R, s, ks, V.s, live);
+    accumulate<RT>(R, s, V, live);
+    if (next >= end) break;
+    id = load_values(A, ids, base, last, next, h, V);
+    t0 = next;
+  }
+}
+
+template <int RT>
+DISC_DEV void clear_rows(Rows<RT>& R) {
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    R.m[rt] = kNone;
+    R.use[rt] = R.l[rt] = 0.f;
+#pragma unroll
+    for (int d = 0; d < kND; ++d) R.o[rt][d] = (f32x4){0, 0, 0, 0};
+  }
+  R.vinv = R.vlim = 0.f;
+}
+
+// The query rows' operand: lane (n, g) holds row n, the elements that the keys' lanes hold of theirs.
+template <int RT>
+DISC_DEV void load_query(Rows<RT>& R, int rt, const T* p) {      // p: this lane's row, or null
+  const int g = (threadIdx.x & 63) >> 4;
+#pragma unroll
+  for (int i = 0; i < kNK; ++i)
+#pragma unroll
+    for (int f = 0; f < kKE / 8; ++f) {
+      const int d = i * 4 * kKE + g * kKE + f * 8;
+      R.q[rt][i * (kKE / 8) + f] = p && d < kD ? *(const u32x4_u*)(p + d) : (u32x4){0, 0, 0, 0};
+    }
+}
+
+// Pages of the tokens [begin, end) into LDS; what is no page of the cache becomes -1.
+DISC_DEV void stage_pages(const AttendArgs& A, const int* table, int width, int begin, int end, int* ids) {
+  const int base = begin >> A.shift, n = ((end - 1) >> A.shift) - base + 1;
+  for (int i = threadIdx.x; i < n; i += 256) {
+    const int p = base + i < width ? table[base + i] : -1;
+    ids[i] = p >= 0 && p < A.pages ? p : -1;
+  }
+}
+
+// Element of O^T that register r of a lane's tile (n, i) holds.
+DISC_DEV int element_of(int n, int i, int r) {
+  return (n * 16 + (((threadIdx.x & 63) >> 4) * 4 + r)) * kE + i;
+}
+
+// One chunk of one sequence, for one kv head and 16 of its query heads at most.
+extern "C" __global__ void __launch_bounds__(256, 2) disc_attend_k(AttendArgs A) {
+  __shared__ int ids[kMostPages + 1];     // (a chunk need not begin with a page)
+  __shared__ float so[4][16][kD + 4];
+  __shared__ float sm[4][16], sl[4][16];
+  const int per = A.kv_heads * A.tiles;
+  const int item = blockIdx.x / per, rest = blockIdx.x - item * per;
+  const int h = rest / A.tiles, tile = rest - h * A.tiles;
+  Item I;
+  if (!find_item(A, item, -1, I)) return;
+  stage_pages(A, A.table + (i64)I.b * A.width, A.width, I.begin, I.end, ids);
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, n = lane & 15, g = lane >> 4;
+  const int rows = min(A.group - tile * 16, 16);
+  const int head = h * A.group + tile * 16;
+  Rows<1> R;
+  clear_rows<1>(R);
+  load_query<1>(R, 0, n < rows ? A.q + I.b * A.q_row + (head + n) * A.q_head : nullptr);
+  __syncthreads();
+  attend_tokens<1>(A, ids, I.begin, I.end, w * kStep, 4 * kStep, h, R);
+  // the four wavefronts' results, relative to their common maximum
+  R.l[0] += __shfl_xor(R.l[0], 16);
+  R.l[0] += __shfl_xor(R.l[0], 32);
+  if (g == 0) sm[w][n] = R.m[0], sl[w][n] = R.l[0];
+  __syncthreads();
+  float top = kNone;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) top = fmaxf(top, sm[i][n]);
+  // (no maximum: the sum is 0, or NaN where every score was)
+  float f = R.m[0] > kNone ? __builtin_amdgcn_exp2f(R.m[0] - top) : R.l[0];
+  if (kQuantised) f = R.vinv > 0.f ? f / R.vinv : 0.f;
+#pragma unroll
+  for (int b = 0; b < kNB; ++b)
+#pragma unroll
+    for (int i = 0; i < kE; ++i)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int d = element_of(b, i, r);
+        if (d < kD) so[w][n][d] = R.o[0][b * kE + i][r] * f;
+      }
+  __syncthreads();
+  const bool alone = I.count == 1 && A.prefix_parts == 0;
+  for (int i = threadIdx.x; i < rows * kD; i += 256) {
+    const int r = i / kD, d = i - r * kD;
+    const float o = (so[0][r][d] + so[1][r][d]) + (so[2][r][d] + so[3][r][d]);
+    float m = kNone, l = 0.f;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) m = fmaxf(m, sm[x][r]);
+#pragma unroll
+    for (int x = 0; x < 4; ++x) l += sm[x][r] > kNone ? sl[x][r] * __builtin_amdgcn_exp2f(sm[x][r] - m) : sl[x][r];
+    if (alone) {
+      A.out[I.b * A.o_row + (head + r) * A.o_head + d] = (T)(l != 0.f ? o / l : 0.f);
+    } else {
+      const i64 at = (i64)item * A.heads + head + r;
+      A.part[at * kD + d] = o;
+      if (d == 0) A.part_m[2 * at] = m, A.part_m[2 * at + 1] = l;
+    }
+  }
+}
+
+// One chunk of the shared prefix for one kv head: the rows are all sequences' query heads of it, 16 x RT a
+// wavefront, so that a key or value that was read serves 64 x RT rows of a block.
+constexpr int kPrefixRT = kD <= 128 ? 2 : 1;
+extern "C" __global__ void __launch_bounds__(256, 1) disc_prefix_k(AttendArgs A) {
+  __shared__ int ids[kMostPages + 1];     // (a chunk need not begin with a page)
+  const int all = A.batch * A.group, blocks = (all + 64 * kPrefixRT - 1) / (64 * kPrefixRT);
+  const int part = blockIdx.x / (A.kv_heads * blocks), rest = blockIdx.x - part * (A.kv_heads * blocks);
+  const int h = rest / blocks, block = rest - h * blocks;
+  const int begin = part * A.prefix_chunk, end = min(A.prefix_len, begin + A.prefix_chunk);
+  stage_pages(A, A.prefix_table, (A.prefix_len + (1 << A.shift) - 1) >> A.shift, begin, end, ids);
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, n = lane & 15;
+  Rows<kPrefixRT> R;
+  clear_rows<kPrefixRT>(R);
+#pragma unroll
+  for (int rt = 0; rt < kPrefixRT; ++rt) {
+    const int row = ((block * 4 + w) * kPrefixRT + rt) * 16 + n, b = row / A.group, i = row - b * A.group;
+    load_query<kPrefixRT>(R, rt, row < all ? A.q + b * A.q_row + (h * A.group + i) * A.q_head : nullptr);
+  }
+  __syncthreads();
+  attend_tokens<kPrefixRT>(A, ids, begin, end, 0, kStep, h, R);
+#pragma unroll
+  for (int rt = 0; rt < kPrefixRT; ++rt) {
+    R.l[rt] += __shfl_xor(R.l[rt], 16);
+    R.l[rt] += __shfl_xor(R.l[rt], 32);
+    const int row = ((block * 4 + w) * kPrefixRT + rt) * 16 + n, b = row / A.group, i = row - b * A.group;
+    if (row >= all) continue;
+    const i64 slot = (i64)A.parts * A.heads + ((i64)part * A.batch + b) * A.heads + h * A.group + i;
+    const float f = !kQuantised ? 1.f : R.vinv > 0.f ? 1.f / R.vinv : 0.f;
+#pragma unroll
+    for (int x = 0; x < kNB; ++x)
+#pragma unroll
+      for (int e = 0; e < kE; ++e)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int d = element_of(x, e, r);
+          if (d < kD) A.part[slot * kD + d] = R.o[rt][x * kE + e][r] * f;
+        }
+    if (lane < 16) A.part_m[2 * slot] = R.m[rt], A.part_m[2 * slot + 1] = R.l[rt];
+  }
+}
+
+// Joins the chunks of a sequence and of the prefix: one block a (sequence, query head).
+extern "C" __global__ void __launch_bounds__(256) disc_join_k(AttendArgs A) {
+  __shared__ float so[4][kD];
+  __shared__ float sm[4], sl[4];
+  const int b = blockIdx.x / A.heads, head = blockIdx.x - b * A.heads;
+  Item I;
+  if (!find_item(A, 0, b, I)) return;
+  if (I.count == 1 && A.prefix_parts == 0) return;            // the chunk's own block wrote the result
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, n = I.count + A.prefix_parts;
+  constexpr int kPer = (kD + 63) / 64;
+  float o[kPer], m = kNone, l = 0.f;
+#pragma unroll
+  for (int e = 0; e < kPer; ++e) o[e] = 0.f;
+  for (int i = w; i < n; i += 4) {
+    const i64 slot = i < I.count ? (i64)(I.first + i) * A.heads + head
+                                 : (i64)A.parts * A.heads + ((i64)(i - I.count) * A.batch + b) * A.heads + head;
+    const float pm = A.part_m[2 * slot], pl = A.part_m[2 * slot + 1];
+    const float top = fmaxf(m, pm);
+    const float fa = m > kNone ? __builtin_amdgcn_exp2f(m - top) : l, fb = pm > kNone ? __builtin_amdgcn_exp2f(pm - top) : pl;
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) {
+      const int d = e * 64 + lane;
+      const float x = d < kD ? A.part[slot * kD + d] : 0.f;
+      o[e] = o[e] * fa + x * fb;
+    }
+    l = l * fa + pl * fb;
+    m = top;
+  }
+#pragma unroll
+  for (int e = 0; e < kPer; ++e)
+    if (e * 64 + lane < kD) so[w][e * 64 + lane] = o[e];
+  if (lane == 0) sm[w] = m, sl[w] = l;
+  __syncthreads();
+  float top = kNone, f[4], sum = 0.f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) top = fmaxf(top, sm[i]);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    f[i] = sm[i] > kNone ? __builtin_amdgcn_exp2f(sm[i] - top) : sl[i];
+    sum += sl[i] * f[i];
+  }
+  for (int d = threadIdx.x; d < kD; d += 256) {
+    const float x = (so[0][d] * f[0] + so[1][d] * f[1]) + (so[2][d] * f[2] + so[3][d] * f[3]);
+    A.out[b * A.o_row + head * A.o_head + d] = (T)(sum != 0.f ? x / sum : 0.f);
+  }
+}
+#endif  // DISC_CACHE

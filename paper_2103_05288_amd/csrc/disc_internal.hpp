@@ -4,6 +4,7 @@
 
 #include <cstdint>
 #include <map>
+#include <memory>
 #include <string>
 #include <vector>
 
@@ -280,5 +281,23 @@ int analyze(const disc_op* ops, int n_ops, const disc_constraint* cs, int n_cs, 
 // codegen.cpp
 int generate(const Analysis& an, const std::string& prefix, Generated* out, std::string* err,
              const GenOptions* opt = nullptr);
+
+// decoder.cpp: an operator of its own device code (rotary positions, a cache of keys and values), compiled once
+// at registration like a pattern.  `fn` by the numbers of its kind's kernels.
+struct Operator {
+  enum Kind { ROTARY, CACHE } kind = ROTARY;
+  std::string key;                 // what the registration was made of
+  int dtype = 0, storage = 0, head_dim = 0, rotary_dim = 0;
+  void* module = nullptr;          // hipModule_t
+  void* fn[5] = {};                // hipFunction_t
+};
+
+// runtime.cpp: what decoder.cpp and scratch.hip need of a context
+int context_device(const disc_ctx* ctx);
+int context_cus(const disc_ctx* ctx);
+int context_fail(disc_ctx* ctx, int code, const char* msg);
+int context_compile(disc_ctx* ctx, const std::string& source, std::vector<char>* code);
+std::vector<std::unique_ptr<Operator>>* context_operators(disc_ctx* ctx);
+void context_count(disc_ctx* ctx, int device_launches);
 
 }  // namespace disc

@@ -141,6 +141,7 @@ struct disc_ctx {
   std::vector<std::unique_ptr<Pattern>> fused;   // row reduces of op graphs that take an operand transposed ...
   std::map<std::pair<int, int>, int> fused_of;   // ... by pattern and input: compiled once, shared by all graphs (-1: it could not be)
   std::map<std::string, int> cache;
+  std::vector<std::unique_ptr<Operator>> operators;   // decoder.cpp
   disc_stats_t stats{};
   int force_variant = -1;
   hipModule_t util_module = nullptr;
@@ -1438,6 +1439,19 @@ int context_fail(disc_ctx* ctx, int code, const char* msg) {
     return code;
   }
 }
+// ... and for decoder.cpp
+int context_cus(const disc_ctx* ctx) { return ctx->n_cus; }
+int context_compile(disc_ctx* ctx, const std::string& source, std::vector<char>* code) {
+  double ms = 0;
+  const int rc = compile_source(ctx, source, code, &ms);
+  ctx->stats.compile_events++;
+  return rc;
+}
+std::vector<std::unique_ptr<Operator>>* context_operators(disc_ctx* ctx) { return &ctx->operators; }
+void context_count(disc_ctx* ctx, int device_launches) {
+  ctx->stats.launch_calls++;
+  ctx->stats.device_launches += device_launches;
+}
 }  // namespace disc
 extern "C" int disc_static_scratch_init(disc_ctx* ctx);
 
@@ -1493,6 +1507,8 @@ void disc_destroy(disc_ctx* ctx) {
       if (p->module) (void)hipModuleUnload(p->module);
     for (auto& p : ctx->fused)
       if (p->module) (void)hipModuleUnload(p->module);
+    for (auto& o : ctx->operators)
+      if (o->module) (void)hipModuleUnload((hipModule_t)o->module);
     if (ctx->util_module) (void)hipModuleUnload(ctx->util_module);
   }
   delete ctx;
