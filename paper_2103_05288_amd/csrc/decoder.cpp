@@ -42,10 +42,12 @@ struct AttendArgs {
   float *part, *part_m;
   int64_t q_row, q_head, o_row, o_head;
   int32_t batch, heads, kv_heads, group, pages, shift, width, tiles;
-  int32_t target, parts, prefix_len, prefix_chunk, prefix_parts, pad;
-  double inv_target;
+  int32_t target, parts, direct, prefix_len, prefix_chunk, prefix_parts, prefix_tiles;
 };
-constexpr int kMaxBlockTokens = 8, kMostPages = 2048, kBlockStep = 128;
+constexpr int kMaxBlockTokens = 8, kMostPages = 2048;
+constexpr int kUnit = 128;              // tokens that a block's four wavefronts take at once
+constexpr int64_t kDirectTokens = 512;  // sequences no longer than this are one chunk each
+constexpr int64_t kFewRows = 64;        // query rows a kv head up to which disc_attend_k has the prefix too
 
 enum { FN_ROTARY = 0 };
 enum { FN_STORE = 0, FN_LOAD, FN_ATTEND, FN_PREFIX, FN_JOIN };
@@ -103,9 +105,9 @@ struct OnDevice {
   }
 };
 
-int enqueue(disc_ctx* c, void* fn, uint64_t blocks, uint32_t y, const void* args, size_t size, void* stream) {
+int enqueue(disc_ctx* c, void* fn, uint64_t blocks, uint32_t y, uint32_t threads, const void* args, size_t size, void* stream) {
   void* extra[] = {HIP_LAUNCH_PARAM_BUFFER_POINTER, const_cast<void*>(args), HIP_LAUNCH_PARAM_BUFFER_SIZE, &size, HIP_LAUNCH_PARAM_END};
-  const hipError_t e = hipModuleLaunchKernel((hipFunction_t)fn, (uint32_t)blocks, y, 1, 256, 1, 1, 0, (hipStream_t)stream, nullptr, extra);
+  const hipError_t e = hipModuleLaunchKernel((hipFunction_t)fn, (uint32_t)blocks, y, 1, threads, 1, 1, 0, (hipStream_t)stream, nullptr, extra);
   if (e != hipSuccess) {
     (void)hipGetLastError();
     char buf[128];
@@ -246,7 +248,7 @@ int launch_rotary(disc_ctx* c, int32_t id, const int64_t* dims, int n_dims, cons
   const uint32_t y = blocks * 2 <= context_cus(c) ? (uint32_t)(passes < 64 ? passes : 64) : 1;
   OnDevice on(context_device(c));
   if (!on.ok) return refuse(c, DISC_ERR_HIP, "hipSetDevice failed");
-  const int rc = enqueue(c, o->fn[FN_ROTARY], (uint64_t)blocks, y, &a, sizeof a, stream);
+  const int rc = enqueue(c, o->fn[FN_ROTARY], (uint64_t)blocks, y, 256, &a, sizeof a, stream);
   if (rc == DISC_OK) context_count(c, 1);
   return rc;
 }
@@ -340,7 +342,7 @@ int launch_rows(disc_ctx* c, int32_t id, const int64_t* dims, int n_dims, const 
   if (context_device(c) < 0) return refuse(c, DISC_ERR_INVALID_ARG, "host-only context cannot launch");
   OnDevice on(context_device(c));
   if (!on.ok) return refuse(c, DISC_ERR_HIP, "hipSetDevice failed");
-  const int rc = enqueue(c, o->fn[store ? FN_STORE : FN_LOAD], (uint64_t)((threads + 255) / 256), 1, &a, sizeof a, stream);
+  const int rc = enqueue(c, o->fn[store ? FN_STORE : FN_LOAD], (uint64_t)((threads + 255) / 256), 1, 256, &a, sizeof a, stream);
   if (rc == DISC_OK) context_count(c, 1);
   return rc;
 }
@@ -377,32 +379,48 @@ int plan_attend(disc_ctx* c, const Operator& o, const int64_t* d, int n_dims, At
   a.tiles = (int32_t)ceil_div(a.group, 16);
   a.prefix_len = (int32_t)prefix;
   const int64_t cus = context_cus(c), per = kv * a.tiles;
-  // Sequences' own tokens: two blocks of a CU share all lengths, so that they end together whatever the lengths are.
-  a.target = (int32_t)(2 * cus / per > 1 ? 2 * cus / per : 1);
-  a.inv_target = 1.0 / a.target;
+  // Sequences' own tokens: four blocks a CU share all lengths, so that they end together whatever the lengths are.
+  a.target = (int32_t)(4 * cus / per > 1 ? 4 * cus / per : 1);
   const int64_t cut = ceil_div(times(batch, width), kMostPages);
   int64_t parts = batch + (a.target > cut ? a.target : cut);
-  const int64_t whole = times(batch, ceil_div(width << shift, kBlockStep));
+  const int64_t whole = times(batch, ceil_div(width << shift, kUnit));
   if (whole >= 0 && whole < parts) parts = whole;
-  // The prefix: blocks of 64 or 128 query rows of a kv head.
-  const int64_t rows = batch * a.group, block_rows = o.head_dim <= 128 ? 128 : 64, row_blocks = ceil_div(rows, block_rows);
+  if (prefix == 0 && (width << shift) <= kDirectTokens) {
+    a.direct = 1;
+    parts = batch;
+  }
+  const int64_t rows = batch * a.group;
+  int64_t prefix_blocks = 0;
   if (prefix > 0 && batch > 0) {
-    int64_t n = 2 * cus / (kv * row_blocks);
-    const int64_t steps = ceil_div(prefix, kBlockStep);
-    n = n < 1 ? 1 : n > steps ? steps : n;
-    int64_t chunk = ceil_div(ceil_div(prefix, n), kBlockStep) * kBlockStep;
+    const bool few = rows <= kFewRows;
+    const int64_t block_rows = few ? 16 : o.head_dim <= 128 ? 256 : 128, row_blocks = ceil_div(rows, block_rows), at_once = (few ? 2 : 1) * cus;
+    // Chunks of the prefix: as many as make the shortest run, in rounds of the blocks that are there at once times the
+    // units of a chunk and a block's own cost of about four.
+    const int64_t units = ceil_div(prefix, kUnit), blocks = kv * row_blocks;
+    int64_t n = 1, best = INT64_MAX;
+    for (int64_t k = 1; k <= units && (k - 1) * blocks < 2 * at_once; ++k) {
+      const int64_t cost = ceil_div(k * blocks, at_once) * (ceil_div(units, k) + 4);
+      if (cost < best) best = cost, n = k;
+    }
+    int64_t chunk = ceil_div(units, n) * kUnit;
     const int64_t most = (int64_t)kMostPages << shift;
     chunk = chunk > most ? most : chunk;
     a.prefix_chunk = (int32_t)chunk;
     a.prefix_parts = (int32_t)ceil_div(prefix, chunk);
+    prefix_blocks = times(a.prefix_parts, blocks);
+    if (few) a.prefix_tiles = (int32_t)row_blocks;
   }
   if (parts >= (int64_t)1 << 31) return refuse(c, DISC_ERR_SHAPE, "too many chunks for one call");
-  a.parts = (int32_t)parts;
-  p->attend_blocks = batch > 0 ? times(parts, per) : 0;
-  p->prefix_blocks = times(a.prefix_parts, kv * row_blocks);
-  p->join_blocks = times(batch, heads);
+  a.parts = (int32_t)(parts = a.direct ? 0 : parts);
+  p->attend_blocks = batch > 0 ? times(a.direct ? batch : parts, per) : 0;
+  if (p->attend_blocks >= 0 && a.prefix_tiles) {
+    p->attend_blocks += prefix_blocks;
+    prefix_blocks = 0;
+  }
+  p->prefix_blocks = prefix_blocks;
+  p->join_blocks = a.direct ? 0 : ceil_div(times(batch, heads), 4);
   const int64_t partial = times(parts, heads) + times(a.prefix_parts, times(batch, heads));
-  if (p->attend_blocks >= (int64_t)1 << 31 || p->prefix_blocks >= (int64_t)1 << 31 || p->join_blocks >= (int64_t)1 << 31 || times(partial, 4 * 256 + 8) < 0)
+  if (p->attend_blocks < 0 || p->prefix_blocks < 0 || p->attend_blocks >= (int64_t)1 << 31 || p->prefix_blocks >= (int64_t)1 << 31 || p->join_blocks >= (int64_t)1 << 31 || times(partial, 4 * 256 + 8) < 0)
     return refuse(c, DISC_ERR_SHAPE, "too many rows for one call");
   p->workspace = batch > 0 ? (size_t)partial * ((size_t)o.head_dim * 4 + 8) : 0;
   return DISC_OK;
@@ -454,15 +472,18 @@ int launch_attend(disc_ctx* c, int32_t id, const int64_t* dims, int n_dims, cons
   if (!on.ok) return refuse(c, DISC_ERR_HIP, "hipSetDevice failed");
   int rc = DISC_OK, n = 0;
   if (p.prefix_blocks > 0) {
-    rc = enqueue(c, o->fn[FN_PREFIX], (uint64_t)p.prefix_blocks, 1, &a, sizeof a, stream);
+    rc = enqueue(c, o->fn[FN_PREFIX], (uint64_t)p.prefix_blocks, 1, 512, &a, sizeof a, stream);
     ++n;
   }
   if (rc == DISC_OK && p.attend_blocks > 0) {
-    rc = enqueue(c, o->fn[FN_ATTEND], (uint64_t)p.attend_blocks, 1, &a, sizeof a, stream);
+    rc = enqueue(c, o->fn[FN_ATTEND], (uint64_t)p.attend_blocks, 1, 256, &a, sizeof a, stream);
     ++n;
   }
-  if (rc == DISC_OK) rc = enqueue(c, o->fn[FN_JOIN], (uint64_t)p.join_blocks, 1, &a, sizeof a, stream);
-  if (rc == DISC_OK) context_count(c, n + 1);
+  if (rc == DISC_OK && p.join_blocks > 0) {
+    rc = enqueue(c, o->fn[FN_JOIN], (uint64_t)p.join_blocks, 1, 256, &a, sizeof a, stream);
+    ++n;
+  }
+  if (rc == DISC_OK) context_count(c, n);
   return rc;
 }
 

@@ -333,8 +333,9 @@ struct AttendArgs {
   int batch, heads, kv_heads, group, pages, shift, width, tiles;
   int target;               // chunks a kv head that the lengths are cut into, about
   int parts;                // chunks there can be at most
+  int direct;               // every sequence is one chunk, and there is no prefix: no partial results
   int prefix_len, prefix_chunk, prefix_parts;
-  double inv_target;
+  int prefix_tiles;         // the prefix's blocks of 16 query rows a kv head in disc_attend_k (0: disc_prefix_k has it)
 };
 
 struct Item {
@@ -346,50 +347,48 @@ DISC_DEV int clamp_length(int n, int width, int shift) {
   const i64 most = (i64)width << shift;
   return n < 0 ? 0 : n > most ? (int)most : n;
 }
-DISC_DEV int chunk_of(double total, double inv_target, int shift) {
-  // tokens of a chunk: more than total / target, whole steps of four wavefronts
-  const i64 least = (i64)(total * inv_target) + 1;
-  const i64 whole = (least + 4 * kStep - 1) / (4 * kStep) * (4 * kStep);
-  const i64 most = (i64)kMostPages << shift;
-  return (int)(whole < most ? whole : most);
+
+// Sum of the lanes up to this one.
+DISC_DEV u32 scan64(u32 x) {
+  x += (u32)__builtin_amdgcn_update_dpp(0, (int)x, 0x111, 0xf, 0xf, false);   // row_shr:1
+  x += (u32)__builtin_amdgcn_update_dpp(0, (int)x, 0x112, 0xf, 0xf, false);
+  x += (u32)__builtin_amdgcn_update_dpp(0, (int)x, 0x114, 0xf, 0xf, false);
+  x += (u32)__builtin_amdgcn_update_dpp(0, (int)x, 0x118, 0xf, 0xf, false);
+  x += (u32)__builtin_amdgcn_update_dpp(0, (int)x, 0x142, 0xa, 0xf, false);   // row_bcast:15
+  x += (u32)__builtin_amdgcn_update_dpp(0, (int)x, 0x143, 0xc, 0xf, false);   // row_bcast:31
+  return x;
 }
 
-// The chunk number `item` (want_b < 0) or the chunks of sequence want_b; every lane of the wavefront gets it.
+// The chunk number `item` (want_b < 0), or the chunks of sequence want_b; every lane of the wavefront gets it.
+// Lengths are counted in units of four steps.  A chunk has more units than all / target, so that the chunks are at
+// most target + batch; and kMostPages pages at most.
 DISC_DEV bool find_item(const AttendArgs& A, int item, int want_b, Item& I) {
   const int lane = threadIdx.x & 63;
-  double total = 0;
+  constexpr int kUnit = 4 * kStep;
+  u64 total = 0;
+  int n = 0;
   for (int b0 = 0; b0 < A.batch; b0 += 64) {
-    const int b = b0 + lane;
-    int n = b < A.batch ? clamp_length(A.lengths[b], A.width, A.shift) : 0;
-    // (sums of 64 lengths fit 38 bits: exact in a double)
-    double s = (double)n;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) s += __shfl_xor(s, d);
-    total += s;
+    n = b0 + lane < A.batch ? clamp_length(A.lengths[b0 + lane], A.width, A.shift) : 0;
+    total += (u32)__builtin_amdgcn_readlane((int)scan64((u32)(n + kUnit - 1) / kUnit), 63);   // (64 x 2^23 at most)
   }
-  const int chunk = chunk_of(total, A.inv_target, A.shift);
+  const u64 least = (total < 1ull << 32 ? (u32)total / (u32)A.target : total / (u32)A.target) + 1;
+  const u32 most = ((u32)kMostPages << A.shift) / kUnit;
+  const u32 chunk = least < most ? (u32)least : most;
   int before = 0;
   for (int b0 = 0; b0 < A.batch; b0 += 64) {
-    const int b = b0 + lane;
-    const int n = b < A.batch ? clamp_length(A.lengths[b], A.width, A.shift) : 0;
-    const int c = n ? (int)((u32)(n - 1) / (u32)chunk) + 1 : 0;
-    int incl = c;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-      const int x = __shfl_up(incl, d);
-      if (lane >= d) incl += x;
-    }
-    const int first = before + incl - c;
-    const bool hit = want_b >= 0 ? b == want_b : item >= first && item < first + c;
+    if (A.batch > 64) n = b0 + lane < A.batch ? clamp_length(A.lengths[b0 + lane], A.width, A.shift) : 0;
+    const int c = (int)(((u32)(n + kUnit - 1) / kUnit + chunk - 1) / chunk);
+    const int incl = (int)scan64((u32)c), first = before + incl - c;
+    const bool hit = want_b >= 0 ? b0 + lane == want_b : item >= first && item < first + c;
     const u64 who = __ballot(hit);
     if (who) {
       const int l = __ffsll((unsigned long long)who) - 1;
+      const int len = __builtin_amdgcn_readlane(n, l);
       I.b = b0 + l;
       I.first = __builtin_amdgcn_readlane(first, l);
       I.count = __builtin_amdgcn_readlane(c, l);
-      const int len = __builtin_amdgcn_readlane(n, l);
-      I.begin = want_b >= 0 ? 0 : (item - I.first) * chunk;
-      I.end = want_b >= 0 || len - I.begin < chunk ? len : I.begin + chunk;
+      I.begin = want_b >= 0 ? 0 : (item - I.first) * (int)(chunk * kUnit);
+      I.end = want_b >= 0 || len - I.begin < (int)(chunk * kUnit) ? len : I.begin + (int)(chunk * kUnit);
       return true;
     }
     before += __builtin_amdgcn_readlane(incl, 63);
@@ -461,18 +460,10 @@ struct Rows {                                // RT x 16 query rows of a wavefron
 };
 struct Keys {
   u32x4 k[2][kNK];
-  float s[8];
 };
 struct Values {
   u32 v[8][kNB * kVW];
-  float s[8];
 };
-
-DISC_DEV void load_scales(float (&s)[8], const float* p, i64 row) {
-  const f32x4 a = *(const f32x4*)(p + row), b = *(const f32x4*)(p + row + 4);
-#pragma unroll
-  for (int j = 0; j < 4; ++j) s[j] = a[j], s[4 + j] = b[j];
-}
 
 // `ids`: the chunk's pages in LDS (-1: none), from the page of `begin` on; t0: the step's first token.
 DISC_DEV i64 row_of(const AttendArgs& A, const int* ids, int base, int t, int h, int& id) {
@@ -494,10 +485,6 @@ DISC_DEV void load_keys(const AttendArgs& A, const int* ids, int base, int last,
       if ((i + 1) * 64 <= kD * kSize || i * 64 + g * 16 < kD * kSize) K.k[mt][i] = *(const u32x4*)(p + i * 64);
       else K.k[mt][i] = (u32x4){0, 0, 0, 0};
     }
-  }
-  if (kQuantised) {
-    const i64 srow = row_of(A, ids, base, min(t0 + g * 8, last), h, id);
-    load_scales(K.s, A.ks, srow);
   }
 }
 
@@ -527,8 +514,16 @@ DISC_DEV int load_values(const AttendArgs& A, const int* ids, int base, int last
       }
     }
   }
-  if (kQuantised) load_scales(V.s, A.vs, row);
   return id;
+}
+
+// The scales of the lane's eight tokens 8 g + 0..7.
+DISC_DEV void load_scales(const AttendArgs& A, const int* ids, int base, int last, int t0, int h, const float* p, float (&s)[8]) {
+  int id;
+  const i64 row = row_of(A, ids, base, min(t0 + ((threadIdx.x & 63) >> 4) * 8, last), h, id);
+  const f32x4 a = *(const f32x4*)(p + row), b = *(const f32x4*)(p + row + 4);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) s[j] = a[j], s[4 + j] = b[j];
 }
 
 // Row d of V^T: element i of the lane's eight tokens, as the second product's operand.
@@ -661,15 +656,9 @@ typedef __bf16 P;
 #endif
 typedef P Px2 __attribute__((ext_vector_type(2)));
 
+// The probabilities as the second product's operand.
 template <int RT>
-DISC_DEV void accumulate(Rows<RT>& R, const f32x4 (&s)[RT][2], Values& V, int live) {
-  if (__ballot(live < 8)) {                       // what is behind the end may hold anything: 0 * NaN is no 0
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-#pragma unroll
-      for (int w = 0; w < kNB * kVW; ++w) V.v[j][w] = j < live ? V.v[j][w] : 0u;
-  }
-  u32x4 hi[RT], lo[RT];
+DISC_DEV void split(const f32x4 (&s)[RT][2], u32x4 (&hi)[RT], u32x4 (&lo)[RT]) {
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
@@ -682,6 +671,18 @@ DISC_DEV void accumulate(Rows<RT>& R, const f32x4 (&s)[RT][2], Values& V, int li
         lo[rt][w] = __builtin_bit_cast(u32, r);
       }
     }
+}
+
+template <int RT>
+DISC_DEV void accumulate(Rows<RT>& R, const f32x4 (&s)[RT][2], Values& V, int live) {
+  if (__ballot(live < 8)) {                       // what is behind the end may hold anything: 0 * NaN is no 0
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+#pragma unroll
+      for (int w = 0; w < kNB * kVW; ++w) V.v[j][w] = j < live ? V.v[j][w] : 0u;
+  }
+  u32x4 hi[RT], lo[RT];
+  split<RT>(s, hi, lo);
 #pragma unroll
   for (int n = 0; n < kNB; ++n)
 #pragma unroll
@@ -705,8 +706,11 @@ DISC_DEV void attend_tokens(const AttendArgs& A, const int* ids, int begin, int 
   const int last = (end - 1) & ~7;
   Keys K;
   Values V;
+  float key_scales[8], value_scales[8];
   load_keys(A, ids, base, last, t0, h, K);
+  if (kQuantised) load_scales(A, ids, base, last, t0, h, A.ks, key_scales);
   int id = load_values(A, ids, base, last, t0, h, V);
+  if (kQuantised) load_scales(A, ids, base, last, t0, h, A.vs, value_scales);
   while (true) {
     f32x4 s[RT][2];
     const int n = end - (t0 + g * 8);
@@ -714,13 +718,17 @@ DISC_DEV void attend_tokens(const AttendArgs& A, const int* ids, int begin, int 
     float ks[8];
     scores<RT>(R, K, s);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) ks[j] = (kQuantised ? K.s[j] : 1.f) * (float)(DISC_SCALE_LOG2E);
+    for (int j = 0; j < 8; ++j) ks[j] = (kQuantised ? key_scales[j] : 1.f) * (float)(DISC_SCALE_LOG2E);
     const int next = t0 + stride;
-    if (next < end) load_keys(A, ids, base, last, next, h, K);
-    softmax_step<RT>(R, s, ks, V.s, live);
+    if (next < end) {
+      load_keys(A, ids, base, last, next, h, K);
+      if (kQuantised) load_scales(A, ids, base, last, next, h, A.ks, key_scales);
+    }
+    softmax_step<RT>(R, s, ks, value_scales, live);
     accumulate<RT>(R, s, V, live);
     if (next >= end) break;
     id = load_values(A, ids, base, last, next, h, V);
+    if (kQuantised) load_scales(A, ids, base, last, next, h, A.vs, value_scales);
     t0 = next;
   }
 }
@@ -764,23 +772,65 @@ DISC_DEV int element_of(int n, int i, int r) {
   return (n * 16 + (((threadIdx.x & 63) >> 4) * 4 + r)) * kE + i;
 }
 
-// One chunk of one sequence, for one kv head and 16 of its query heads at most.
+DISC_DEV void store4(T* p, f32x4 x) {
+  const Tx2 a = {(T)x[0], (T)x[1]}, b = {(T)x[2], (T)x[3]};
+  *(u32x2_u*)p = (u32x2){__builtin_bit_cast(u32, a), __builtin_bit_cast(u32, b)};
+}
+
+// Row of the partial results: a chunk's (first the sequences', then the prefix's), for a query head.
+DISC_DEV i64 part_row(const AttendArgs& A, int chunk, int head) { return (i64)chunk * A.heads + head; }
+DISC_DEV i64 prefix_row(const AttendArgs& A, int part, int b, int head) {
+  return (i64)A.parts * A.heads + ((i64)part * A.batch + b) * A.heads + head;
+}
+
+// One chunk of one sequence, for one kv head and 16 of its query heads at most; or, where the query rows of all
+// sequences are few, one chunk of the prefix for 16 of them.
 extern "C" __global__ void __launch_bounds__(256, 2) disc_attend_k(AttendArgs A) {
   __shared__ int ids[kMostPages + 1];     // (a chunk need not begin with a page)
   __shared__ float so[4][16][kD + 4];
   __shared__ float sm[4][16], sl[4][16];
-  const int per = A.kv_heads * A.tiles;
-  const int item = blockIdx.x / per, rest = blockIdx.x - item * per;
-  const int h = rest / A.tiles, tile = rest - h * A.tiles;
-  Item I;
-  if (!find_item(A, item, -1, I)) return;
-  stage_pages(A, A.table + (i64)I.b * A.width, A.width, I.begin, I.end, ids);
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, n = lane & 15, g = lane >> 4;
-  const int rows = min(A.group - tile * 16, 16);
-  const int head = h * A.group + tile * 16;
+  const int shared_blocks = A.prefix_tiles * A.prefix_parts * A.kv_heads;
+  const bool shared = (int)blockIdx.x < shared_blocks;
+  int part = 0, h, row0, rows;            // rows: of this block; the first is number row0 of the kv head's
+  Item I;
+  if (shared) {
+    const int per = A.prefix_parts * A.kv_heads, tile = blockIdx.x / per, rest = blockIdx.x - tile * per;
+    part = rest / A.kv_heads;
+    h = rest - part * A.kv_heads;
+    I.begin = part * A.prefix_chunk;
+    I.end = min(A.prefix_len, I.begin + A.prefix_chunk);
+    I.b = I.first = I.count = 0;
+    row0 = tile * 16;
+    rows = min(A.batch * A.group - row0, 16);
+    stage_pages(A, A.prefix_table, (A.prefix_len + (1 << A.shift) - 1) >> A.shift, I.begin, I.end, ids);
+  } else {
+    const int block = blockIdx.x - shared_blocks, per = A.kv_heads * A.tiles;
+    const int item = block / per, rest = block - item * per;
+    h = rest / A.tiles;
+    row0 = (rest - h * A.tiles) * 16;
+    rows = min(A.group - row0, 16);
+    if (A.direct) {
+      I.b = item;
+      I.begin = I.first = 0;
+      I.count = 1;
+      I.end = clamp_length(A.lengths[item], A.width, A.shift);
+    } else {
+      if (!find_item(A, item, -1, I)) return;
+      part = item;
+    }
+    if (I.end > I.begin) stage_pages(A, A.table + (i64)I.b * A.width, A.width, I.begin, I.end, ids);
+  }
+  // sequence and query head of a row
+  auto place = [&](int r, int& b, int& head) {
+    b = shared ? (row0 + r) / A.group : I.b;
+    head = h * A.group + (shared ? row0 + r - b * A.group : row0 + r);
+  };
   Rows<1> R;
   clear_rows<1>(R);
-  load_query<1>(R, 0, n < rows ? A.q + I.b * A.q_row + (head + n) * A.q_head : nullptr);
+  int b, head;
+  place(n, b, head);
+  load_query<1>(R, 0, n < rows ? A.q + b * A.q_row + head * A.q_head : nullptr);
   __syncthreads();
   attend_tokens<1>(A, ids, I.begin, I.end, w * kStep, 4 * kStep, h, R);
   // the four wavefronts' results, relative to their common maximum
@@ -795,119 +845,242 @@ extern "C" __global__ void __launch_bounds__(256, 2) disc_attend_k(AttendArgs A)
   float f = R.m[0] > kNone ? __builtin_amdgcn_exp2f(R.m[0] - top) : R.l[0];
   if (kQuantised) f = R.vinv > 0.f ? f / R.vinv : 0.f;
 #pragma unroll
-  for (int b = 0; b < kNB; ++b)
+  for (int x = 0; x < kNB; ++x)
 #pragma unroll
     for (int i = 0; i < kE; ++i)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const int d = element_of(b, i, r);
-        if (d < kD) so[w][n][d] = R.o[0][b * kE + i][r] * f;
+        const int d = element_of(x, i, r);
+        if (d < kD) so[w][n][d] = R.o[0][x * kE + i][r] * f;
       }
   __syncthreads();
-  const bool alone = I.count == 1 && A.prefix_parts == 0;
-  for (int i = threadIdx.x; i < rows * kD; i += 256) {
-    const int r = i / kD, d = i - r * kD;
-    const float o = (so[0][r][d] + so[1][r][d]) + (so[2][r][d] + so[3][r][d]);
+  const bool alone = !shared && I.count == 1 && A.prefix_parts == 0;
+  // four neighbouring elements a thread
+  for (int i = threadIdx.x; i < rows * (kD / 4); i += 256) {
+    const int r = i / (kD / 4), d = (i - r * (kD / 4)) * 4;
+    const f32x4 o = (*(const f32x4*)&so[0][r][d] + *(const f32x4*)&so[1][r][d]) + (*(const f32x4*)&so[2][r][d] + *(const f32x4*)&so[3][r][d]);
     float m = kNone, l = 0.f;
 #pragma unroll
     for (int x = 0; x < 4; ++x) m = fmaxf(m, sm[x][r]);
 #pragma unroll
     for (int x = 0; x < 4; ++x) l += sm[x][r] > kNone ? sl[x][r] * __builtin_amdgcn_exp2f(sm[x][r] - m) : sl[x][r];
+    place(r, b, head);
     if (alone) {
-      A.out[I.b * A.o_row + (head + r) * A.o_head + d] = (T)(l != 0.f ? o / l : 0.f);
+      store4(A.out + b * A.o_row + head * A.o_head + d, l != 0.f ? o / l : (f32x4){0, 0, 0, 0});
     } else {
-      const i64 at = (i64)item * A.heads + head + r;
-      A.part[at * kD + d] = o;
+      const i64 at = shared ? prefix_row(A, part, b, head) : part_row(A, part, head);
+      *(f32x4*)(A.part + at * kD + d) = o;
       if (d == 0) A.part_m[2 * at] = m, A.part_m[2 * at + 1] = l;
     }
   }
 }
 
-// One chunk of the shared prefix for one kv head: the rows are all sequences' query heads of it, 16 x RT a
-// wavefront, so that a key or value that was read serves 64 x RT rows of a block.
+// One chunk of the shared prefix for one kv head, where the batch has many query rows: each of the eight wavefronts
+// has 16 x RT rows of its own, and all go through the same tokens.  A tile of them is read once a block, brought into
+// the matrix operands' form -- codes to 16-bit numbers, values transposed -- and kept in LDS in the order in which a
+// wavefront reads an operand (16 bytes a lane, one row after the other); the next tile's loads are in flight
+// meanwhile, and two tiles take turns.
 constexpr int kPrefixRT = kD <= 128 ? 2 : 1;
-extern "C" __global__ void __launch_bounds__(256, 1) disc_prefix_k(AttendArgs A) {
-  __shared__ int ids[kMostPages + 1];     // (a chunk need not begin with a page)
-  const int all = A.batch * A.group, blocks = (all + 64 * kPrefixRT - 1) / (64 * kPrefixRT);
-  const int part = blockIdx.x / (A.kv_heads * blocks), rest = blockIdx.x - part * (A.kv_heads * blocks);
-  const int h = rest / blocks, block = rest - h * blocks;
+constexpr int kPrefixSteps = kD <= 128 ? 4 : 2;               // steps of a tile
+constexpr int kNF = kNK * (kKE / 8);                          // operands of a step's keys, a 16-row tile
+struct PrefixTile {
+  u32x4 k[kPrefixSteps][2 * kNF][64];
+  u32x4 v[kPrefixSteps][kND][64];
+  float ks[kPrefixSteps * kStep], vs[kPrefixSteps * kStep];
+  int live[kPrefixSteps * 4];                                 // tokens that are there, of every eight
+};
+extern "C" __global__ void __launch_bounds__(512, 2) disc_prefix_k(AttendArgs A) {
+  __shared__ PrefixTile tiles[2];
+  __shared__ int ids[kMostPages + 1];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, n = lane & 15, g = lane >> 4;
+  // (blocks of the same chunk and kv head are a multiple of eight apart where there are that many: on one XCD)
+  const int all = A.batch * A.group, per = A.prefix_parts * A.kv_heads;
+  const int block = blockIdx.x / per, rest = blockIdx.x - block * per, part = rest / A.kv_heads, h = rest - part * A.kv_heads;
   const int begin = part * A.prefix_chunk, end = min(A.prefix_len, begin + A.prefix_chunk);
-  stage_pages(A, A.prefix_table, (A.prefix_len + (1 << A.shift) - 1) >> A.shift, begin, end, ids);
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, n = lane & 15;
+  const int base = begin >> A.shift, last = (end - 1) & ~7;
+  for (int i = threadIdx.x; i < ((end - 1) >> A.shift) - base + 1; i += 512) {
+    const int p = A.prefix_table[base + i];
+    ids[i] = p >= 0 && p < A.pages ? p : -1;
+  }
+  const int row0 = (block * 8 + w) * kPrefixRT * 16;
   Rows<kPrefixRT> R;
   clear_rows<kPrefixRT>(R);
 #pragma unroll
   for (int rt = 0; rt < kPrefixRT; ++rt) {
-    const int row = ((block * 4 + w) * kPrefixRT + rt) * 16 + n, b = row / A.group, i = row - b * A.group;
+    const int row = row0 + rt * 16 + n, b = row / A.group, i = row - b * A.group;
     load_query<kPrefixRT>(R, rt, row < all ? A.q + b * A.q_row + (h * A.group + i) * A.q_head : nullptr);
   }
+  const bool keys = w < kPrefixSteps, values = !keys && w < 2 * kPrefixSteps;
+  const int step = keys ? w : w - kPrefixSteps;               // this wavefront's share of a tile
+  // (either of them, in the same registers)
+  constexpr int kKeyWords = 2 * kNK * 4, kValueWords = 8 * kNB * kVW;
+  u32 held[kKeyWords > kValueWords ? kKeyWords : kValueWords];
+  float scale = 0.f;                                          // of token `lane` of the step
+  int live = 0;
+  auto fetch = [&](int t0) {                                  // t0: the tile's first token
+    t0 += step * kStep;
+    int id;
+    if (keys) {
+      Keys K;
+      load_keys(A, ids, base, last, t0, h, K);
+#pragma unroll
+      for (int x = 0; x < kKeyWords; ++x) held[x] = K.k[x / (4 * kNK)][x / 4 % kNK][x % 4];
+    }
+    if (values) {
+      Values V;
+      id = load_values(A, ids, base, last, t0, h, V);
+      const int m = end - (t0 + g * 8);
+      live = id < 0 || m <= 0 ? 0 : m < 8 ? m : 8;
+#pragma unroll
+      for (int x = 0; x < kValueWords; ++x) held[x] = V.v[x / (kNB * kVW)][x % (kNB * kVW)];
+    }
+    if (kQuantised && (keys || values)) {
+      const int t = min(t0 + (lane & 31), last + 7);
+      scale = (keys ? A.ks : A.vs)[row_of(A, ids, base, t, h, id)];
+    }
+  };
+  auto put = [&](PrefixTile& T) {
+    if (keys) {
+#pragma unroll
+      for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+        for (int i = 0; i < kNK; ++i) {
+          const u32* x = held + (mt * kNK + i) * 4;
+          if (!kQuantised) {
+            T.k[step][mt * kNF + i][lane] = (u32x4){x[0], x[1], x[2], x[3]};
+          } else {
+            T.k[step][mt * kNF + 2 * i][lane] = keys_of_codes(x[0], x[1]);
+            T.k[step][mt * kNF + (2 * i + 1) % kNF][lane] = keys_of_codes(x[2], x[3]);
+          }
+        }
+      if (kQuantised && lane < kStep) T.ks[step * kStep + lane] = scale;
+    }
+    if (values) {
+      Values V;
+#pragma unroll
+      for (int j = 0; j < 8; ++j)                             // (what is behind the end may hold anything)
+#pragma unroll
+        for (int x = 0; x < kNB * kVW; ++x) V.v[j][x] = j < live ? held[j * kNB * kVW + x] : 0u;
+      if (n == 0) T.live[step * 4 + g] = live;
+      if (kQuantised) {
+        const int alive = __shfl(live, ((lane & 31) >> 3) * 16);
+        if (lane < kStep) T.vs[step * kStep + lane] = (lane & 7) < alive ? scale : 0.f;
+      }
+#pragma unroll
+      for (int x = 0; x < kNB; ++x)
+#pragma unroll
+        for (int i = 0; i < kE; ++i) T.v[step][x * kE + i][lane] = column_of(V, x, i);
+    }
+  };
   __syncthreads();
-  attend_tokens<kPrefixRT>(A, ids, begin, end, 0, kStep, h, R);
+  fetch(begin);
+  put(tiles[0]);
+  __syncthreads();
+  constexpr int kTile = kPrefixSteps * kStep;
+  for (int t0 = begin, turn = 0; t0 < end; t0 += kTile, turn ^= 1) {
+    const PrefixTile& T = tiles[turn];
+    if (t0 + kTile < end) fetch(t0 + kTile);
+    if (row0 < all) {
+      for (int st = 0; st < kPrefixSteps && t0 + st * kStep < end; ++st) {
+        f32x4 s[kPrefixRT][2];
+#pragma unroll
+        for (int rt = 0; rt < kPrefixRT; ++rt) s[rt][0] = s[rt][1] = (f32x4){0, 0, 0, 0};
+#pragma unroll
+        for (int i = 0; i < 2 * kNF; ++i) {
+          const u32x4 k = T.k[st][i][lane];
+#pragma unroll
+          for (int rt = 0; rt < kPrefixRT; ++rt) s[rt][i / kNF] = mfma_q(k, R.q[rt][i % kNF], s[rt][i / kNF]);
+        }
+        float ks[8], vs[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          ks[j] = (kQuantised ? T.ks[st * kStep + g * 8 + j] : 1.f) * (float)(DISC_SCALE_LOG2E);
+          vs[j] = kQuantised ? T.vs[st * kStep + g * 8 + j] : 1.f;
+        }
+        softmax_step<kPrefixRT>(R, s, ks, vs, T.live[st * 4 + g]);
+        u32x4 hi[kPrefixRT], lo[kPrefixRT];
+        split<kPrefixRT>(s, hi, lo);
+#pragma unroll
+        for (int d = 0; d < kND; ++d) {
+          const u32x4 v = T.v[st][d][lane];
+#pragma unroll
+          for (int rt = 0; rt < kPrefixRT; ++rt) {
+            R.o[rt][d] = mfma_v(v, hi[rt], R.o[rt][d]);
+            if (kSplit) R.o[rt][d] = mfma_v(v, lo[rt], R.o[rt][d]);
+          }
+        }
+      }
+    }
+    if (t0 + kTile < end) put(tiles[turn ^ 1]);
+    __syncthreads();
+  }
 #pragma unroll
   for (int rt = 0; rt < kPrefixRT; ++rt) {
     R.l[rt] += __shfl_xor(R.l[rt], 16);
     R.l[rt] += __shfl_xor(R.l[rt], 32);
-    const int row = ((block * 4 + w) * kPrefixRT + rt) * 16 + n, b = row / A.group, i = row - b * A.group;
+    const int row = row0 + rt * 16 + n, b = row / A.group, i = row - b * A.group;
     if (row >= all) continue;
-    const i64 slot = (i64)A.parts * A.heads + ((i64)part * A.batch + b) * A.heads + h * A.group + i;
+    const i64 at = prefix_row(A, part, b, h * A.group + i);
     const float f = !kQuantised ? 1.f : R.vinv > 0.f ? 1.f / R.vinv : 0.f;
 #pragma unroll
     for (int x = 0; x < kNB; ++x)
 #pragma unroll
-      for (int e = 0; e < kE; ++e)
+      for (int r = 0; r < 4; ++r) {
+        const int d = element_of(x, 0, r);
+        if (d < kD) {
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int d = element_of(x, e, r);
-          if (d < kD) A.part[slot * kD + d] = R.o[rt][x * kE + e][r] * f;
+          for (int e = 0; e < kE; e += 4)
+            *(f32x4*)(A.part + at * kD + d + e) = (f32x4){R.o[rt][x * kE + e][r] * f, R.o[rt][x * kE + e + 1][r] * f, R.o[rt][x * kE + e + 2][r] * f,
+                                                          R.o[rt][x * kE + e + 3][r] * f};
         }
-    if (lane < 16) A.part_m[2 * slot] = R.m[rt], A.part_m[2 * slot + 1] = R.l[rt];
+      }
+    if (g == 0) A.part_m[2 * at] = R.m[rt], A.part_m[2 * at + 1] = R.l[rt];
   }
 }
 
-// Joins the chunks of a sequence and of the prefix: one block a (sequence, query head).
+// Joins the chunks of a sequence and of the prefix: a wavefront a (sequence, query head).  The chunks' maxima and sums
+// are read 64 at a time, a lane each, so that the reads of the results themselves do not wait for each other.
 extern "C" __global__ void __launch_bounds__(256) disc_join_k(AttendArgs A) {
-  __shared__ float so[4][kD];
-  __shared__ float sm[4], sl[4];
-  const int b = blockIdx.x / A.heads, head = blockIdx.x - b * A.heads;
+  const i64 row = (i64)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int b = (int)(row / A.heads), head = (int)(row - (i64)b * A.heads), lane = threadIdx.x & 63;
+  if (b >= A.batch) return;
   Item I;
   if (!find_item(A, 0, b, I)) return;
   if (I.count == 1 && A.prefix_parts == 0) return;            // the chunk's own block wrote the result
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, n = I.count + A.prefix_parts;
+  const int n = I.count + A.prefix_parts;
   constexpr int kPer = (kD + 63) / 64;
   float o[kPer], m = kNone, l = 0.f;
 #pragma unroll
   for (int e = 0; e < kPer; ++e) o[e] = 0.f;
-  for (int i = w; i < n; i += 4) {
-    const i64 slot = i < I.count ? (i64)(I.first + i) * A.heads + head
-                                 : (i64)A.parts * A.heads + ((i64)(i - I.count) * A.batch + b) * A.heads + head;
-    const float pm = A.part_m[2 * slot], pl = A.part_m[2 * slot + 1];
-    const float top = fmaxf(m, pm);
-    const float fa = m > kNone ? __builtin_amdgcn_exp2f(m - top) : l, fb = pm > kNone ? __builtin_amdgcn_exp2f(pm - top) : pl;
+  for (int i0 = 0; i0 < n; i0 += 64) {
+    const int i = i0 + lane;
+    const i64 at = i < I.count ? part_row(A, I.first + i, head) : prefix_row(A, min(i, n - 1) - I.count, b, head);
+    const float pm = i < n ? A.part_m[2 * at] : kNone, pl = i < n ? A.part_m[2 * at + 1] : 0.f;
+    float top = fmaxf(m, pm);
 #pragma unroll
-    for (int e = 0; e < kPer; ++e) {
-      const int d = e * 64 + lane;
-      const float x = d < kD ? A.part[slot * kD + d] : 0.f;
-      o[e] = o[e] * fa + x * fb;
-    }
-    l = l * fa + pl * fb;
+    for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
+    // (no maximum: nothing was there, or every score was NaN and so is the sum)
+    const float f = pm > kNone ? __builtin_amdgcn_exp2f(pm - top) : pl;
+    float sum = pm > kNone ? pl * f : pl;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
+    const float before = m > kNone ? __builtin_amdgcn_exp2f(m - top) : l;
+    l = (m > kNone ? l * before : l) + sum;
     m = top;
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) o[e] *= before;
+    const int most = min(64, n - i0);
+#pragma unroll 8
+    for (int x = 0; x < most; ++x) {
+      const float fx = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, f), x));
+      const i64 slot = i0 + x < I.count ? part_row(A, I.first + i0 + x, head) : prefix_row(A, i0 + x - I.count, b, head);
+#pragma unroll
+      for (int e = 0; e < kPer; ++e)
+        if (e * 64 + lane < kD) o[e] += A.part[slot * kD + e * 64 + lane] * fx;
+    }
   }
 #pragma unroll
   for (int e = 0; e < kPer; ++e)
-    if (e * 64 + lane < kD) so[w][e * 64 + lane] = o[e];
-  if (lane == 0) sm[w] = m, sl[w] = l;
-  __syncthreads();
-  float top = kNone, f[4], sum = 0.f;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) top = fmaxf(top, sm[i]);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    f[i] = sm[i] > kNone ? __builtin_amdgcn_exp2f(sm[i] - top) : sl[i];
-    sum += sl[i] * f[i];
-  }
-  for (int d = threadIdx.x; d < kD; d += 256) {
-    const float x = (so[0][d] * f[0] + so[1][d] * f[1]) + (so[2][d] * f[2] + so[3][d] * f[3]);
-    A.out[b * A.o_row + head * A.o_head + d] = (T)(sum != 0.f ? x / sum : 0.f);
-  }
+    if (e * 64 + lane < kD) A.out[b * A.o_row + head * A.o_head + e * 64 + lane] = (T)(l != 0.f ? o[e] / l : 0.f);
 }
 #endif  // DISC_CACHE
