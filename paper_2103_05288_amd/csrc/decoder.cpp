@@ -42,7 +42,7 @@ struct AttendArgs {
   float *part, *part_m;
   int64_t q_row, q_head, o_row, o_head;
   int32_t batch, heads, kv_heads, group, pages, shift, width, tiles;
-  int32_t target, parts, direct, prefix_len, prefix_chunk, prefix_parts, prefix_tiles;
+  int32_t target, parts, direct, join_ways, prefix_len, prefix_chunk, prefix_parts, prefix_tiles;
 };
 constexpr int kMaxBlockTokens = 8, kMostPages = 2048;
 constexpr int kUnit = 128;              // tokens that a block's four wavefronts take at once
@@ -385,7 +385,7 @@ int plan_attend(disc_ctx* c, const Operator& o, const int64_t* d, int n_dims, At
   int64_t parts = batch + (a.target > cut ? a.target : cut);
   const int64_t whole = times(batch, ceil_div(width << shift, kUnit));
   if (whole >= 0 && whole < parts) parts = whole;
-  if (prefix == 0 && (width << shift) <= kDirectTokens) {
+  if ((width << shift) <= kDirectTokens) {
     a.direct = 1;
     parts = batch;
   }
@@ -411,14 +411,17 @@ int plan_attend(disc_ctx* c, const Operator& o, const int64_t* d, int n_dims, At
     if (few) a.prefix_tiles = (int32_t)row_blocks;
   }
   if (parts >= (int64_t)1 << 31) return refuse(c, DISC_ERR_SHAPE, "too many chunks for one call");
-  a.parts = (int32_t)(parts = a.direct ? 0 : parts);
-  p->attend_blocks = batch > 0 ? times(a.direct ? batch : parts, per) : 0;
+  const bool alone = a.direct && prefix == 0;   // every chunk's block writes the result itself
+  p->attend_blocks = times(parts, per);
+  a.parts = (int32_t)(parts = alone ? 0 : parts);
   if (p->attend_blocks >= 0 && a.prefix_tiles) {
     p->attend_blocks += prefix_blocks;
     prefix_blocks = 0;
   }
   p->prefix_blocks = prefix_blocks;
-  p->join_blocks = a.direct ? 0 : ceil_div(times(batch, heads), 4);
+  // A block a row where there are few rows to join, so that their chunks, which are many then, are read by four wavefronts.
+  a.join_ways = times(batch, heads) <= 4 * cus ? 4 : 1;
+  p->join_blocks = alone ? 0 : ceil_div(times(batch, heads), 4 / a.join_ways);
   const int64_t partial = times(parts, heads) + times(a.prefix_parts, times(batch, heads));
   if (p->attend_blocks < 0 || p->prefix_blocks < 0 || p->attend_blocks >= (int64_t)1 << 31 || p->prefix_blocks >= (int64_t)1 << 31 || p->join_blocks >= (int64_t)1 << 31 || times(partial, 4 * 256 + 8) < 0)
     return refuse(c, DISC_ERR_SHAPE, "too many rows for one call");

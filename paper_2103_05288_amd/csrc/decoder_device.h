@@ -333,7 +333,8 @@ struct AttendArgs {
   int batch, heads, kv_heads, group, pages, shift, width, tiles;
   int target;               // chunks a kv head that the lengths are cut into, about
   int parts;                // chunks there can be at most
-  int direct;               // every sequence is one chunk, and there is no prefix: no partial results
+  int direct;               // every sequence is one chunk, whatever its length: chunk b
+  int join_ways;            // wavefronts of a row of disc_join_k: 1 or 4
   int prefix_len, prefix_chunk, prefix_parts;
   int prefix_tiles;         // the prefix's blocks of 16 query rows a kv head in disc_attend_k (0: disc_prefix_k has it)
 };
@@ -787,7 +788,7 @@ DISC_DEV i64 prefix_row(const AttendArgs& A, int part, int b, int head) {
 // sequences are few, one chunk of the prefix for 16 of them.
 extern "C" __global__ void __launch_bounds__(256, 2) disc_attend_k(AttendArgs A) {
   __shared__ int ids[kMostPages + 1];     // (a chunk need not begin with a page)
-  __shared__ float so[4][16][kD + 4];
+  __shared__ float so[2][16][kD + 4];
   __shared__ float sm[4][16], sl[4][16];
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, n = lane & 15, g = lane >> 4;
   const int shared_blocks = A.prefix_tiles * A.prefix_parts * A.kv_heads;
@@ -810,14 +811,14 @@ extern "C" __global__ void __launch_bounds__(256, 2) disc_attend_k(AttendArgs A)
     h = rest / A.tiles;
     row0 = (rest - h * A.tiles) * 16;
     rows = min(A.group - row0, 16);
+    part = item;
     if (A.direct) {
       I.b = item;
       I.begin = I.first = 0;
       I.count = 1;
       I.end = clamp_length(A.lengths[item], A.width, A.shift);
-    } else {
-      if (!find_item(A, item, -1, I)) return;
-      part = item;
+    } else if (!find_item(A, item, -1, I)) {
+      return;
     }
     if (I.end > I.begin) stage_pages(A, A.table + (i64)I.b * A.width, A.width, I.begin, I.end, ids);
   }
@@ -844,21 +845,28 @@ extern "C" __global__ void __launch_bounds__(256, 2) disc_attend_k(AttendArgs A)
   // (no maximum: the sum is 0, or NaN where every score was)
   float f = R.m[0] > kNone ? __builtin_amdgcn_exp2f(R.m[0] - top) : R.l[0];
   if (kQuantised) f = R.vinv > 0.f ? f / R.vinv : 0.f;
+  // (two at a time: four would be LDS enough to keep other blocks away)
 #pragma unroll
-  for (int x = 0; x < kNB; ++x)
+  for (int turn = 0; turn < 2; ++turn) {
 #pragma unroll
-    for (int i = 0; i < kE; ++i)
+    for (int x = 0; x < kNB; ++x)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int d = element_of(x, i, r);
-        if (d < kD) so[w][n][d] = R.o[0][x * kE + i][r] * f;
-      }
-  __syncthreads();
+      for (int r = 0; r < 4; ++r)
+        if (element_of(x, 0, r) < kD && w / 2 != turn) {
+          f32x4* at = (f32x4*)&so[w & 1][n][element_of(x, 0, r)];
+#pragma unroll
+          for (int i = 0; i < kE; i += 4) {
+            const f32x4 o = {R.o[0][x * kE + i][r], R.o[0][x * kE + i + 1][r], R.o[0][x * kE + i + 2][r], R.o[0][x * kE + i + 3][r]};
+            at[i / 4] = turn ? at[i / 4] + o * f : o * f;
+          }
+        }
+    __syncthreads();
+  }
   const bool alone = !shared && I.count == 1 && A.prefix_parts == 0;
   // four neighbouring elements a thread
   for (int i = threadIdx.x; i < rows * (kD / 4); i += 256) {
     const int r = i / (kD / 4), d = (i - r * (kD / 4)) * 4;
-    const f32x4 o = (*(const f32x4*)&so[0][r][d] + *(const f32x4*)&so[1][r][d]) + (*(const f32x4*)&so[2][r][d] + *(const f32x4*)&so[3][r][d]);
+    const f32x4 o = *(const f32x4*)&so[0][r][d] + *(const f32x4*)&so[1][r][d];
     float m = kNone, l = 0.f;
 #pragma unroll
     for (int x = 0; x < 4; ++x) m = fmaxf(m, sm[x][r]);
@@ -1038,22 +1046,31 @@ extern "C" __global__ void __launch_bounds__(512, 2) disc_prefix_k(AttendArgs A)
   }
 }
 
-// Joins the chunks of a sequence and of the prefix: a wavefront a (sequence, query head).  The chunks' maxima and sums
-// are read 64 at a time, a lane each, so that the reads of the results themselves do not wait for each other.
+// Joins the chunks of a sequence and of the prefix, for a (sequence, query head) a wavefront, or where the rows are few
+// and their chunks many, a block.  The chunks' maxima and sums are read 64 at a time, a lane each, so that the reads
+// of the results themselves do not wait for each other.
 extern "C" __global__ void __launch_bounds__(256) disc_join_k(AttendArgs A) {
-  const i64 row = (i64)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int b = (int)(row / A.heads), head = (int)(row - (i64)b * A.heads), lane = threadIdx.x & 63;
-  if (b >= A.batch) return;
+  __shared__ float so[4][kD], sm[4], sl[4];
+  const int w = threadIdx.x >> 6, lane = threadIdx.x & 63, ways = A.join_ways;
+  const i64 row = ways == 1 ? (i64)blockIdx.x * 4 + w : (i64)blockIdx.x;
+  const int b = (int)(row / A.heads), head = (int)(row - (i64)b * A.heads);
+  if (b >= A.batch) return;                                   // (one wavefront a row: no barrier comes)
   Item I;
-  if (!find_item(A, 0, b, I)) return;
-  if (I.count == 1 && A.prefix_parts == 0) return;            // the chunk's own block wrote the result
+  I.first = b;
+  I.count = 1;
+  if (!A.direct) {
+    if (!find_item(A, 0, b, I)) return;
+    if (I.count == 1 && A.prefix_parts == 0) return;          // the chunk's own block wrote the result
+  }
   const int n = I.count + A.prefix_parts;
   constexpr int kPer = (kD + 63) / 64;
   float o[kPer], m = kNone, l = 0.f;
 #pragma unroll
   for (int e = 0; e < kPer; ++e) o[e] = 0.f;
-  for (int i0 = 0; i0 < n; i0 += 64) {
-    const int i = i0 + lane;
+  // this wavefront's chunks: n0 + x * ways
+  const int first = ways == 1 ? 0 : w;
+  for (int i0 = first; i0 < n; i0 += 64 * ways) {
+    const int i = i0 + lane * ways;
     const i64 at = i < I.count ? part_row(A, I.first + i, head) : prefix_row(A, min(i, n - 1) - I.count, b, head);
     const float pm = i < n ? A.part_m[2 * at] : kNone, pl = i < n ? A.part_m[2 * at + 1] : 0.f;
     float top = fmaxf(m, pm);
@@ -1069,14 +1086,44 @@ extern "C" __global__ void __launch_bounds__(256) disc_join_k(AttendArgs A) {
     m = top;
 #pragma unroll
     for (int e = 0; e < kPer; ++e) o[e] *= before;
-    const int most = min(64, n - i0);
-#pragma unroll 8
-    for (int x = 0; x < most; ++x) {
-      const float fx = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, f), x));
-      const i64 slot = i0 + x < I.count ? part_row(A, I.first + i0 + x, head) : prefix_row(A, i0 + x - I.count, b, head);
+    const int most = min(64, (n - i0 + ways - 1) / ways);
+    for (int x0 = 0; x0 < most; x0 += 8) {
+      float v[8][kPer];
+#pragma unroll
+      for (int x = 0; x < 8; ++x) {                           // (the last one again, with a weight of 0, behind the end)
+        const int j = i0 + min(x0 + x, most - 1) * ways;
+        const i64 slot = j < I.count ? part_row(A, I.first + j, head) : prefix_row(A, j - I.count, b, head);
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) v[x][e] = e * 64 + lane < kD ? A.part[slot * kD + e * 64 + lane] : 0.f;
+      }
+#pragma unroll
+      for (int x = 0; x < 8; ++x) {
+        const float fx = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, f), min(x0 + x, 63)));
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) o[e] = x0 + x < most ? o[e] + v[x][e] * fx : o[e];
+      }
+    }
+  }
+  if (ways > 1) {
+#pragma unroll
+    for (int e = 0; e < kPer; ++e)
+      if (e * 64 + lane < kD) so[w][e * 64 + lane] = o[e];
+    if (lane == 0) sm[w] = m, sl[w] = l;
+    __syncthreads();
+    if (w > 0) return;
+    float top = kNone;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) top = fmaxf(top, sm[i]);
+    l = 0.f;
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) o[e] = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float f = sm[i] > kNone ? __builtin_amdgcn_exp2f(sm[i] - top) : sl[i];
+      l += sm[i] > kNone ? sl[i] * f : sl[i];
 #pragma unroll
       for (int e = 0; e < kPer; ++e)
-        if (e * 64 + lane < kD) o[e] += A.part[slot * kD + e * 64 + lane] * fx;
+        if (e * 64 + lane < kD) o[e] += so[i][e * 64 + lane] * f;
     }
   }
 #pragma unroll
