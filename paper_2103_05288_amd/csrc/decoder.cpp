@@ -44,7 +44,7 @@ struct AttendArgs {
   int32_t batch, heads, kv_heads, group, pages, shift, width, tiles;
   int32_t target, parts, direct, join_ways, prefix_len, prefix_chunk, prefix_parts, prefix_tiles;
 };
-constexpr int kMaxBlockTokens = 8, kMostPages = 2048;
+constexpr int kMaxBlockTokens = 8, kMostPages = 1024;
 constexpr int kUnit = 128;              // tokens that a block's four wavefronts take at once
 constexpr int64_t kDirectTokens = 512;  // sequences no longer than this are one chunk each
 constexpr int64_t kFewRows = 64;        // query rows a kv head up to which disc_attend_k has the prefix too
@@ -117,8 +117,9 @@ int enqueue(disc_ctx* c, void* fn, uint64_t blocks, uint32_t y, uint32_t threads
   return DISC_OK;
 }
 
-// Compiles the operator and enters it, or finds the one that was made of the same description.
-int enter(disc_ctx* c, std::unique_ptr<Operator> o, const std::string& macros, const char* const* names, int n, int32_t* id_out) {
+// Compiles the operator and enters it, or finds the one that was made of the same description.  `measured`: the kernel
+// whose blocks a CU are asked for.
+int enter(disc_ctx* c, std::unique_ptr<Operator> o, const std::string& macros, const char* const* names, int n, int measured, int32_t* id_out) {
   auto& all = *context_operators(c);
   for (size_t i = 0; i < all.size(); ++i)
     if (all[i]->key == o->key) {
@@ -148,6 +149,11 @@ int enter(disc_ctx* c, std::unique_ptr<Operator> o, const std::string& macros, c
       }
       o->fn[i] = f;
     }
+    int blocks = 0;
+    if (hipModuleOccupancyMaxActiveBlocksPerMultiprocessor(&blocks, (hipFunction_t)o->fn[measured], 256, 0) == hipSuccess && blocks > 0)
+      o->resident = blocks;
+    else
+      (void)hipGetLastError();
   }
   *id_out = (int32_t)all.size();
   all.push_back(std::move(o));
@@ -197,7 +203,7 @@ int register_rotary(disc_ctx* c, const disc_rotary_desc* d, int32_t* id_out) {
   o->head_dim = d->head_dim;
   o->rotary_dim = d->rotary_dim;
   static const char* const names[] = {"disc_rotary_k"};
-  return enter(c, std::move(o), macros, names, 1, id_out);
+  return enter(c, std::move(o), macros, names, 1, FN_ROTARY, id_out);
 }
 
 int launch_rotary(disc_ctx* c, int32_t id, const int64_t* dims, int n_dims, const void* const* in, int n_in, void* const* out, int n_out,
@@ -273,7 +279,7 @@ int register_cache(disc_ctx* c, const disc_cache_desc* d, int32_t* id_out) {
   o->storage = d->storage;
   o->head_dim = d->head_dim;
   static const char* const names[] = {"disc_store_k", "disc_load_k", "disc_attend_k", "disc_prefix_k", "disc_join_k"};
-  return enter(c, std::move(o), macros, names, 5, id_out);
+  return enter(c, std::move(o), macros, names, 5, FN_ATTEND, id_out);
 }
 
 // page_size = 1 << shift; -1: no page size
@@ -379,12 +385,11 @@ int plan_attend(disc_ctx* c, const Operator& o, const int64_t* d, int n_dims, At
   a.tiles = (int32_t)ceil_div(a.group, 16);
   a.prefix_len = (int32_t)prefix;
   const int64_t cus = context_cus(c), per = kv * a.tiles;
-  // Sequences' own tokens: four blocks a CU share all lengths, so that they end together whatever the lengths are.
-  a.target = (int32_t)(4 * cus / per > 1 ? 4 * cus / per : 1);
-  const int64_t cut = ceil_div(times(batch, width), kMostPages);
-  int64_t parts = batch + (a.target > cut ? a.target : cut);
-  const int64_t whole = times(batch, ceil_div(width << shift, kUnit));
-  if (whole >= 0 && whole < parts) parts = whole;
+  // Sequences' own tokens: as many blocks as run at once share all of them, so that they end together whatever the
+  // lengths are.
+  const int64_t at_once = cus * o.resident;
+  a.target = (int32_t)(at_once / per > 1 ? at_once / per : 1);
+  int64_t parts = batch + a.target;
   if ((width << shift) <= kDirectTokens) {
     a.direct = 1;
     parts = batch;
@@ -393,13 +398,13 @@ int plan_attend(disc_ctx* c, const Operator& o, const int64_t* d, int n_dims, At
   int64_t prefix_blocks = 0;
   if (prefix > 0 && batch > 0) {
     const bool few = rows <= kFewRows;
-    const int64_t block_rows = few ? 16 : o.head_dim <= 128 ? 256 : 128, row_blocks = ceil_div(rows, block_rows), at_once = (few ? 2 : 1) * cus;
+    const int64_t block_rows = few ? 16 : o.head_dim <= 128 ? 256 : 128, row_blocks = ceil_div(rows, block_rows), slots = (few ? o.resident : 1) * cus;
     // Chunks of the prefix: as many as make the shortest run, in rounds of the blocks that are there at once times the
     // units of a chunk and a block's own cost of about four.
     const int64_t units = ceil_div(prefix, kUnit), blocks = kv * row_blocks;
     int64_t n = 1, best = INT64_MAX;
-    for (int64_t k = 1; k <= units && (k - 1) * blocks < 2 * at_once; ++k) {
-      const int64_t cost = ceil_div(k * blocks, at_once) * (ceil_div(units, k) + 4);
+    for (int64_t k = 1; k <= units && (k - 1) * blocks < 2 * slots; ++k) {
+      const int64_t cost = ceil_div(k * blocks, slots) * (ceil_div(units, k) + 4);
       if (cost < best) best = cost, n = k;
     }
     int64_t chunk = ceil_div(units, n) * kUnit;
@@ -412,7 +417,7 @@ int plan_attend(disc_ctx* c, const Operator& o, const int64_t* d, int n_dims, At
   }
   if (parts >= (int64_t)1 << 31) return refuse(c, DISC_ERR_SHAPE, "too many chunks for one call");
   const bool alone = a.direct && prefix == 0;   // every chunk's block writes the result itself
-  p->attend_blocks = times(parts, per);
+  p->attend_blocks = times(a.direct ? batch : a.target, per);
   a.parts = (int32_t)(parts = alone ? 0 : parts);
   if (p->attend_blocks >= 0 && a.prefix_tiles) {
     p->attend_blocks += prefix_blocks;

@@ -299,11 +299,11 @@ extern "C" __global__ void __launch_bounds__(256) disc_load_k(RowsArgs A) {
 // Where the probabilities would have no more bits than the result they are held as a sum of two 16-bit
 // numbers (hi + lo), so that the only rounding that counts is the result's.
 //
-// A block is four wavefronts; they take the steps of a chunk in turn and join in LDS at its end.  Chunks
-// are cut from the lengths, on the device, so that all blocks have about the same share.
+// A block is four wavefronts; they take the steps of a stretch of tokens in turn and join in LDS at its end.
+// The stretches are cut from the lengths, on the device, so that all blocks have the same share.
 // =================================================================================================
 constexpr int kStep = 32;                     // tokens of a step
-constexpr int kMostPages = 2048;              // pages of a chunk, kept in LDS
+constexpr int kMostPages = 1024;              // pages of a stretch that are kept in LDS at a time
 constexpr int kE = kD % 128 == 0 ? 8 : kD % 64 == 0 ? 4 : 8;    // neighbouring elements of a value that a lane reads
 constexpr int kNB = (kD + 16 * kE - 1) / (16 * kE);             // such groups of 16 lanes
 constexpr int kND = kE * kNB;                                   // 16-row tiles of O^T
@@ -331,17 +331,12 @@ struct AttendArgs {
   float* part_m;            // their running maximum and sum, two floats a row
   i64 q_row, q_head, o_row, o_head;
   int batch, heads, kv_heads, group, pages, shift, width, tiles;
-  int target;               // chunks a kv head that the lengths are cut into, about
-  int parts;                // chunks there can be at most
+  int target;               // blocks a kv head that the sequences' tokens are shared out to
+  int parts;                // chunks there can be at most: target + batch
   int direct;               // every sequence is one chunk, whatever its length: chunk b
   int join_ways;            // wavefronts of a row of disc_join_k: 1 or 4
   int prefix_len, prefix_chunk, prefix_parts;
   int prefix_tiles;         // the prefix's blocks of 16 query rows a kv head in disc_attend_k (0: disc_prefix_k has it)
-};
-
-struct Item {
-  int b, begin, end;        // sequence, its tokens [begin, end)
-  int first, count;         // the sequence's chunks
 };
 
 DISC_DEV int clamp_length(int n, int width, int shift) {
@@ -360,41 +355,105 @@ DISC_DEV u32 scan64(u32 x) {
   return x;
 }
 
-// The chunk number `item` (want_b < 0), or the chunks of sequence want_b; every lane of the wavefront gets it.
-// Lengths are counted in units of four steps.  A chunk has more units than all / target, so that the chunks are at
-// most target + batch; and kMostPages pages at most.
-DISC_DEV bool find_item(const AttendArgs& A, int item, int want_b, Item& I) {
-  const int lane = threadIdx.x & 63;
-  constexpr int kUnit = 4 * kStep;
+// How the sequences' tokens are shared out: in units of four steps, the sequences one after the other, every one of
+// `target` blocks takes the same number of units (one more or less).  A block so has a stretch of one sequence, or the
+// end of one, whole ones and the beginning of another; what block j has of sequence b is chunk j + b, which no two of
+// them share.  Every wavefront finds out for itself, from the lengths.
+struct Shares {
+  u64 each;                 // units of a block; the first `more` blocks have one more
+  u32 more;
+  DISC_DEV u64 first(u32 j) const { return (u64)j * each + (j < more ? j : more); }
+  DISC_DEV u32 block_of(u64 unit) const {
+    const u64 edge = (u64)more * (each + 1);
+    if (unit < edge) return divide(unit, each + 1);
+    return more + divide(unit - edge, each);
+  }
+  static DISC_DEV u32 divide(u64 a, u64 b) { return (a | b) < 1ull << 32 ? (u32)a / (u32)b : (u32)(a / b); }
+};
+constexpr int kUnit = 4 * kStep;
+DISC_DEV u32 units_of(int n) { return (u32)(n + kUnit - 1) / kUnit; }
+
+// Lengths of the sequences b0 + lane.
+DISC_DEV int length_of(const AttendArgs& A, int b0) {
+  const int b = b0 + (threadIdx.x & 63);
+  return b < A.batch ? clamp_length(A.lengths[b], A.width, A.shift) : 0;
+}
+
+DISC_DEV Shares shares_of(const AttendArgs& A, int& n) {      // n: the last 64 lengths that were read
   u64 total = 0;
-  int n = 0;
   for (int b0 = 0; b0 < A.batch; b0 += 64) {
-    n = b0 + lane < A.batch ? clamp_length(A.lengths[b0 + lane], A.width, A.shift) : 0;
-    total += (u32)__builtin_amdgcn_readlane((int)scan64((u32)(n + kUnit - 1) / kUnit), 63);   // (64 x 2^23 at most)
+    n = length_of(A, b0);
+    total += (u32)__builtin_amdgcn_readlane((int)scan64(units_of(n)), 63);   // (64 x 2^23 at most)
   }
-  const u64 least = (total < 1ull << 32 ? (u32)total / (u32)A.target : total / (u32)A.target) + 1;
-  const u32 most = ((u32)kMostPages << A.shift) / kUnit;
-  const u32 chunk = least < most ? (u32)least : most;
-  int before = 0;
-  for (int b0 = 0; b0 < A.batch; b0 += 64) {
-    if (A.batch > 64) n = b0 + lane < A.batch ? clamp_length(A.lengths[b0 + lane], A.width, A.shift) : 0;
-    const int c = (int)(((u32)(n + kUnit - 1) / kUnit + chunk - 1) / chunk);
-    const int incl = (int)scan64((u32)c), first = before + incl - c;
-    const bool hit = want_b >= 0 ? b0 + lane == want_b : item >= first && item < first + c;
-    const u64 who = __ballot(hit);
-    if (who) {
-      const int l = __ffsll((unsigned long long)who) - 1;
-      const int len = __builtin_amdgcn_readlane(n, l);
-      I.b = b0 + l;
-      I.first = __builtin_amdgcn_readlane(first, l);
-      I.count = __builtin_amdgcn_readlane(c, l);
-      I.begin = want_b >= 0 ? 0 : (item - I.first) * (int)(chunk * kUnit);
-      I.end = want_b >= 0 || len - I.begin < (int)(chunk * kUnit) ? len : I.begin + (int)(chunk * kUnit);
-      return true;
+  Shares S;
+  S.each = total < 1ull << 32 ? (u32)total / (u32)A.target : total / (u32)A.target;
+  S.more = (u32)(total - S.each * (u32)A.target);
+  return S;
+}
+
+// The stretches of a block, one after the other.
+struct Walk {
+  u64 lo, hi, before;       // the block's units; units of the sequences before b0
+  u64 who;                  // the sequences b0 + 0..63 that it has something of and has not been at
+  int b0, n;
+  u32 first, units;         // of sequence b0 + lane, from `before` on
+  int b, begin, end;        // the stretch: tokens [begin, end) of sequence b
+  bool whole;               // it is all of the sequence
+
+  DISC_DEV void start(const AttendArgs& A, u32 block) {
+    const Shares S = shares_of(A, n);
+    lo = S.first(block);
+    hi = S.first(block + 1);
+    before = 0;
+    b0 = -64;
+    who = 0;
+    units = 0;
+  }
+  DISC_DEV bool next(const AttendArgs& A) {
+    while (!who) {
+      if (b0 >= 0) before += (u32)__builtin_amdgcn_readlane((int)(first + units), 63);
+      b0 += 64;
+      if (b0 >= A.batch || before >= hi) return false;
+      if (A.batch > 64) n = length_of(A, b0);
+      units = units_of(n);
+      first = scan64(units) - units;
+      who = __ballot(units > 0 && before + first < hi && before + first + units > lo);
     }
-    before += __builtin_amdgcn_readlane(incl, 63);
+    const int l = __ffsll((unsigned long long)who) - 1;
+    who &= who - 1;
+    const u64 f = before + (u32)__builtin_amdgcn_readlane((int)first, l);
+    const u32 u = (u32)__builtin_amdgcn_readlane((int)units, l);
+    const int len = __builtin_amdgcn_readlane(n, l);
+    const u32 from = lo > f ? (u32)(lo - f) : 0, to = hi < f + u ? (u32)(hi - f) : u;
+    b = b0 + l;
+    begin = (int)(from * kUnit);
+    end = to == u ? len : (int)(to * kUnit);
+    whole = from == 0 && to == u;
+    return true;
   }
-  return false;
+};
+
+// The chunks of sequence b: the first, and how many.
+DISC_DEV void chunks_of(const AttendArgs& A, int b, int& chunk, int& count) {
+  int n = 0;
+  const Shares S = shares_of(A, n);
+  u64 before = 0;
+  for (int b0 = 0;; b0 += 64) {
+    if (A.batch > 64) n = length_of(A, b0);
+    const u32 incl = scan64(units_of(n));
+    if (b < b0 + 64) {
+      const u32 u = (u32)__builtin_amdgcn_readlane((int)units_of(n), b - b0);
+      const u64 f = before + (u32)__builtin_amdgcn_readlane((int)incl, b - b0) - u;
+      chunk = count = 0;
+      if (u) {
+        const u32 j = S.block_of(f);
+        chunk = (int)j + b;
+        count = (int)(S.block_of(f + u - 1) - j) + 1;
+      }
+      return;
+    }
+    before += (u32)__builtin_amdgcn_readlane((int)incl, 63);
+  }
 }
 
 #if DISC_T_F16
@@ -483,7 +542,7 @@ DISC_DEV void load_keys(const AttendArgs& A, const int* ids, int base, int last,
     const u8* p = A.kp + (row + mt * 4 + (m & 3)) * (kD * kSize) + g * 16;
 #pragma unroll
     for (int i = 0; i < kNK; ++i) {
-      if ((i + 1) * 64 <= kD * kSize || i * 64 + g * 16 < kD * kSize) K.k[mt][i] = *(const u32x4*)(p + i * 64);
+      if ((i + 1) * 64 <= kD * kSize || i * 64 + g * 16 < kD * kSize) K.k[mt][i] = __builtin_nontemporal_load((const u32x4*)(p + i * 64));
       else K.k[mt][i] = (u32x4){0, 0, 0, 0};
     }
   }
@@ -502,12 +561,12 @@ DISC_DEV int load_values(const AttendArgs& A, const int* ids, int base, int last
       const bool mine = (n + 1) * 16 * kE <= kD || (n * 16 + c) * kE < kD;
       if (kVW == 4) {
         u32x4 x = {0, 0, 0, 0};
-        if (mine) x = *(const u32x4*)p;
+        if (mine) x = __builtin_nontemporal_load((const u32x4*)p);
 #pragma unroll
         for (int w = 0; w < 4; ++w) V.v[j][n * kVW + w % kVW] = x[w];
       } else if (kVW == 2) {
         u32x2 x = {0, 0};
-        if (mine) x = *(const u32x2*)p;
+        if (mine) x = __builtin_nontemporal_load((const u32x2*)p);
 #pragma unroll
         for (int w = 0; w < 2; ++w) V.v[j][n * kVW + w % kVW] = x[w];
       } else {
@@ -584,27 +643,31 @@ constexpr float kNone = -__builtin_inff();
 // The step's probabilities (in s, in place of the scores) and the running maximum, sum and result.
 template <int RT>
 DISC_DEV void softmax_step(Rows<RT>& R, f32x4 (&s)[RT][2], const float (&ks)[8], float (&vs)[8], int live) {
-  const bool whole = __ballot(live < 8) == 0;     // every token of the step is there
   bool late = false;
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) s[rt][j / 4][j % 4] *= ks[j];
+  if (__ballot(live < 8)) {                       // some token of the step is not there
+    asm volatile("");                             // (a branch, and not a select for every score of every step)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) s[rt][j / 4][j % 4] = j < live ? s[rt][j / 4][j % 4] : kNone;
+      vs[j] = j < live ? vs[j] : 0.f;
+    }
+  }
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     float top = kNone;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      float x = s[rt][j / 4][j % 4] * ks[j];
-      if (!whole) x = j < live ? x : kNone;
-      s[rt][j / 4][j % 4] = x;
-      top = fmaxf(top, x);
-    }
+    for (int j = 0; j < 8; ++j) top = fmaxf(top, s[rt][j / 4][j % 4]);
     late |= top > R.m[rt] + kLag;
   }
   float vtop = 0.f;
   if (kQuantised) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      if (!whole) vs[j] = j < live ? vs[j] : 0.f;
-      vtop = fmaxf(vtop, vs[j]);
-    }
+    for (int j = 0; j < 8; ++j) vtop = fmaxf(vtop, vs[j]);
     late |= vtop > R.vlim;
   }
   if (__ballot(late)) {                           // seldom after the first steps
@@ -707,29 +770,36 @@ DISC_DEV void attend_tokens(const AttendArgs& A, const int* ids, int begin, int 
   const int last = (end - 1) & ~7;
   Keys K;
   Values V;
-  float key_scales[8], value_scales[8];
-  load_keys(A, ids, base, last, t0, h, K);
-  if (kQuantised) load_scales(A, ids, base, last, t0, h, A.ks, key_scales);
+  float ks[8], vs[8];
+  auto fetch_keys = [&](int t) {
+    load_keys(A, ids, base, last, t, h, K);
+    if (kQuantised) load_scales(A, ids, base, last, t, h, A.ks, ks);
+    if (kQuantised) load_scales(A, ids, base, last, t, h, A.vs, vs);
+  };
+  fetch_keys(t0);
   int id = load_values(A, ids, base, last, t0, h, V);
-  if (kQuantised) load_scales(A, ids, base, last, t0, h, A.vs, value_scales);
   while (true) {
     f32x4 s[RT][2];
     const int n = end - (t0 + g * 8);
     const int live = id < 0 || n <= 0 ? 0 : n < 8 ? n : 8;
-    float ks[8];
+    float ks_now[8], vs_now[8];
     scores<RT>(R, K, s);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) ks[j] = (kQuantised ? key_scales[j] : 1.f) * (float)(DISC_SCALE_LOG2E);
-    const int next = t0 + stride;
-    if (next < end) {
-      load_keys(A, ids, base, last, next, h, K);
-      if (kQuantised) load_scales(A, ids, base, last, next, h, A.ks, key_scales);
+    for (int j = 0; j < 8; ++j) {
+      ks_now[j] = (kQuantised ? ks[j] : 1.f) * (float)(DISC_SCALE_LOG2E);
+      vs_now[j] = vs[j];
     }
-    softmax_step<RT>(R, s, ks, value_scales, live);
+    // The next step's keys are read while this one's probabilities and second product run, its values after that, in
+    // the registers that are free then.  (Behind the end the last rows come again: a load that only some steps make
+    // would have every step wait for all loads before it.)
+    const int next = t0 + stride;
+    fetch_keys(next);
+    __builtin_amdgcn_sched_barrier(0);
+    softmax_step<RT>(R, s, ks_now, vs_now, live);
     accumulate<RT>(R, s, V, live);
     if (next >= end) break;
     id = load_values(A, ids, base, last, next, h, V);
-    if (kQuantised) load_scales(A, ids, base, last, next, h, A.vs, value_scales);
+    __builtin_amdgcn_sched_barrier(0);
     t0 = next;
   }
 }
@@ -784,102 +854,113 @@ DISC_DEV i64 prefix_row(const AttendArgs& A, int part, int b, int head) {
   return (i64)A.parts * A.heads + ((i64)part * A.batch + b) * A.heads + head;
 }
 
-// One chunk of one sequence, for one kv head and 16 of its query heads at most; or, where the query rows of all
-// sequences are few, one chunk of the prefix for 16 of them.
-extern "C" __global__ void __launch_bounds__(256, 2) disc_attend_k(AttendArgs A) {
-  __shared__ int ids[kMostPages + 1];     // (a chunk need not begin with a page)
+// A block's share of the sequences' tokens, for one kv head and 16 of its query heads at most; or, where the query rows
+// of all sequences are few, one chunk of the prefix for 16 of them.
+extern "C" __global__ void __launch_bounds__(256, kD <= 128 ? 3 : 2) disc_attend_k(AttendArgs A) {
+  __shared__ int ids[kMostPages + 1];     // (a stretch need not begin with a page)
   __shared__ float so[2][16][kD + 4];
   __shared__ float sm[4][16], sl[4][16];
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, n = lane & 15, g = lane >> 4;
   const int shared_blocks = A.prefix_tiles * A.prefix_parts * A.kv_heads;
   const bool shared = (int)blockIdx.x < shared_blocks;
-  int part = 0, h, row0, rows;            // rows: of this block; the first is number row0 of the kv head's
-  Item I;
+  int part, h, row0, rows;                // rows: of this block; the first is number row0 of the kv head's
+  Walk I;
+  I.b = I.begin = 0;
+  I.whole = !shared;
   if (shared) {
     const int per = A.prefix_parts * A.kv_heads, tile = blockIdx.x / per, rest = blockIdx.x - tile * per;
     part = rest / A.kv_heads;
     h = rest - part * A.kv_heads;
-    I.begin = part * A.prefix_chunk;
-    I.end = min(A.prefix_len, I.begin + A.prefix_chunk);
-    I.b = I.first = I.count = 0;
     row0 = tile * 16;
     rows = min(A.batch * A.group - row0, 16);
-    stage_pages(A, A.prefix_table, (A.prefix_len + (1 << A.shift) - 1) >> A.shift, I.begin, I.end, ids);
+    I.begin = part * A.prefix_chunk;
+    I.end = min(A.prefix_len, I.begin + A.prefix_chunk);
   } else {
     const int block = blockIdx.x - shared_blocks, per = A.kv_heads * A.tiles;
-    const int item = block / per, rest = block - item * per;
+    part = block / per;
+    const int rest = block - part * per;
     h = rest / A.tiles;
     row0 = (rest - h * A.tiles) * 16;
     rows = min(A.group - row0, 16);
-    part = item;
     if (A.direct) {
-      I.b = item;
-      I.begin = I.first = 0;
-      I.count = 1;
-      I.end = clamp_length(A.lengths[item], A.width, A.shift);
-    } else if (!find_item(A, item, -1, I)) {
-      return;
-    }
-    if (I.end > I.begin) stage_pages(A, A.table + (i64)I.b * A.width, A.width, I.begin, I.end, ids);
-  }
-  // sequence and query head of a row
-  auto place = [&](int r, int& b, int& head) {
-    b = shared ? (row0 + r) / A.group : I.b;
-    head = h * A.group + (shared ? row0 + r - b * A.group : row0 + r);
-  };
-  Rows<1> R;
-  clear_rows<1>(R);
-  int b, head;
-  place(n, b, head);
-  load_query<1>(R, 0, n < rows ? A.q + b * A.q_row + head * A.q_head : nullptr);
-  __syncthreads();
-  attend_tokens<1>(A, ids, I.begin, I.end, w * kStep, 4 * kStep, h, R);
-  // the four wavefronts' results, relative to their common maximum
-  R.l[0] += __shfl_xor(R.l[0], 16);
-  R.l[0] += __shfl_xor(R.l[0], 32);
-  if (g == 0) sm[w][n] = R.m[0], sl[w][n] = R.l[0];
-  __syncthreads();
-  float top = kNone;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) top = fmaxf(top, sm[i][n]);
-  // (no maximum: the sum is 0, or NaN where every score was)
-  float f = R.m[0] > kNone ? __builtin_amdgcn_exp2f(R.m[0] - top) : R.l[0];
-  if (kQuantised) f = R.vinv > 0.f ? f / R.vinv : 0.f;
-  // (two at a time: four would be LDS enough to keep other blocks away)
-#pragma unroll
-  for (int turn = 0; turn < 2; ++turn) {
-#pragma unroll
-    for (int x = 0; x < kNB; ++x)
-#pragma unroll
-      for (int r = 0; r < 4; ++r)
-        if (element_of(x, 0, r) < kD && w / 2 != turn) {
-          f32x4* at = (f32x4*)&so[w & 1][n][element_of(x, 0, r)];
-#pragma unroll
-          for (int i = 0; i < kE; i += 4) {
-            const f32x4 o = {R.o[0][x * kE + i][r], R.o[0][x * kE + i + 1][r], R.o[0][x * kE + i + 2][r], R.o[0][x * kE + i + 3][r]};
-            at[i / 4] = turn ? at[i / 4] + o * f : o * f;
-          }
-        }
-    __syncthreads();
-  }
-  const bool alone = !shared && I.count == 1 && A.prefix_parts == 0;
-  // four neighbouring elements a thread
-  for (int i = threadIdx.x; i < rows * (kD / 4); i += 256) {
-    const int r = i / (kD / 4), d = (i - r * (kD / 4)) * 4;
-    const f32x4 o = *(const f32x4*)&so[0][r][d] + *(const f32x4*)&so[1][r][d];
-    float m = kNone, l = 0.f;
-#pragma unroll
-    for (int x = 0; x < 4; ++x) m = fmaxf(m, sm[x][r]);
-#pragma unroll
-    for (int x = 0; x < 4; ++x) l += sm[x][r] > kNone ? sl[x][r] * __builtin_amdgcn_exp2f(sm[x][r] - m) : sl[x][r];
-    place(r, b, head);
-    if (alone) {
-      store4(A.out + b * A.o_row + head * A.o_head + d, l != 0.f ? o / l : (f32x4){0, 0, 0, 0});
+      I.b = part;
+      I.end = clamp_length(A.lengths[part], A.width, A.shift);
     } else {
-      const i64 at = shared ? prefix_row(A, part, b, head) : part_row(A, part, head);
-      *(f32x4*)(A.part + at * kD + d) = o;
-      if (d == 0) A.part_m[2 * at] = m, A.part_m[2 * at + 1] = l;
+      I.start(A, part);
+      if (!I.next(A)) return;
     }
+  }
+  const int width = shared ? (A.prefix_len + (1 << A.shift) - 1) >> A.shift : A.width;
+  while (true) {
+    // sequence and query head of a row
+    auto place = [&](int r, int& b, int& head) {
+      b = shared ? (row0 + r) / A.group : I.b;
+      head = h * A.group + (shared ? row0 + r - b * A.group : row0 + r);
+    };
+    const int* table = shared ? A.prefix_table : A.table + (i64)I.b * A.width;
+    Rows<1> R;
+    clear_rows<1>(R);
+    int b, head;
+    place(n, b, head);
+    load_query<1>(R, 0, n < rows ? A.q + b * A.q_row + head * A.q_head : nullptr);
+    const int most = kMostPages << A.shift;
+    for (int at = I.begin; at < I.end;) {
+      const int to = I.end - at > most ? at + most : I.end;
+      stage_pages(A, table, width, at, to, ids);
+      __syncthreads();
+      attend_tokens<1>(A, ids, at, to, w * kStep, 4 * kStep, h, R);
+      at = to;
+      if (at < I.end) __syncthreads();
+    }
+    // the four wavefronts' results, relative to their common maximum
+    R.l[0] += __shfl_xor(R.l[0], 16);
+    R.l[0] += __shfl_xor(R.l[0], 32);
+    if (g == 0) sm[w][n] = R.m[0], sl[w][n] = R.l[0];
+    __syncthreads();
+    float top = kNone;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) top = fmaxf(top, sm[i][n]);
+    // (no maximum: the sum is 0, or NaN where every score was)
+    float f = R.m[0] > kNone ? __builtin_amdgcn_exp2f(R.m[0] - top) : R.l[0];
+    if (kQuantised) f = R.vinv > 0.f ? f / R.vinv : 0.f;
+    // (two at a time: four would be LDS enough to keep other blocks away)
+#pragma unroll
+    for (int turn = 0; turn < 2; ++turn) {
+#pragma unroll
+      for (int x = 0; x < kNB; ++x)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (element_of(x, 0, r) < kD && w / 2 != turn) {
+            f32x4* at = (f32x4*)&so[w & 1][n][element_of(x, 0, r)];
+#pragma unroll
+            for (int i = 0; i < kE; i += 4) {
+              const f32x4 o = {R.o[0][x * kE + i][r], R.o[0][x * kE + i + 1][r], R.o[0][x * kE + i + 2][r], R.o[0][x * kE + i + 3][r]};
+              at[i / 4] = turn ? at[i / 4] + o * f : o * f;
+            }
+          }
+      __syncthreads();
+    }
+    const bool alone = I.whole && A.prefix_parts == 0;
+    // four neighbouring elements a thread
+    for (int i = threadIdx.x; i < rows * (kD / 4); i += 256) {
+      const int r = i / (kD / 4), d = (i - r * (kD / 4)) * 4;
+      const f32x4 o = *(const f32x4*)&so[0][r][d] + *(const f32x4*)&so[1][r][d];
+      float m = kNone, l = 0.f;
+#pragma unroll
+      for (int x = 0; x < 4; ++x) m = fmaxf(m, sm[x][r]);
+#pragma unroll
+      for (int x = 0; x < 4; ++x) l += sm[x][r] > kNone ? sl[x][r] * __builtin_amdgcn_exp2f(sm[x][r] - m) : sl[x][r];
+      place(r, b, head);
+      if (alone) {
+        store4(A.out + b * A.o_row + head * A.o_head + d, l != 0.f ? o / l : (f32x4){0, 0, 0, 0});
+      } else {
+        const i64 at = shared ? prefix_row(A, part, b, head) : part_row(A, A.direct ? b : part + b, head);
+        *(f32x4*)(A.part + at * kD + d) = o;
+        if (d == 0) A.part_m[2 * at] = m, A.part_m[2 * at + 1] = l;
+      }
+    }
+    if (shared || A.direct || !I.next(A)) return;
+    __syncthreads();                      // (the maxima and sums are still being read)
   }
 }
 
@@ -1055,14 +1136,12 @@ extern "C" __global__ void __launch_bounds__(256) disc_join_k(AttendArgs A) {
   const i64 row = ways == 1 ? (i64)blockIdx.x * 4 + w : (i64)blockIdx.x;
   const int b = (int)(row / A.heads), head = (int)(row - (i64)b * A.heads);
   if (b >= A.batch) return;                                   // (one wavefront a row: no barrier comes)
-  Item I;
-  I.first = b;
-  I.count = 1;
+  int chunk = b, count = 1;
   if (!A.direct) {
-    if (!find_item(A, 0, b, I)) return;
-    if (I.count == 1 && A.prefix_parts == 0) return;          // the chunk's own block wrote the result
+    chunks_of(A, b, chunk, count);
+    if (count == 1 && A.prefix_parts == 0) return;            // the chunk's own block wrote the result
   }
-  const int n = I.count + A.prefix_parts;
+  const int n = count + A.prefix_parts;
   constexpr int kPer = (kD + 63) / 64;
   float o[kPer], m = kNone, l = 0.f;
 #pragma unroll
@@ -1071,7 +1150,7 @@ extern "C" __global__ void __launch_bounds__(256) disc_join_k(AttendArgs A) {
   const int first = ways == 1 ? 0 : w;
   for (int i0 = first; i0 < n; i0 += 64 * ways) {
     const int i = i0 + lane * ways;
-    const i64 at = i < I.count ? part_row(A, I.first + i, head) : prefix_row(A, min(i, n - 1) - I.count, b, head);
+    const i64 at = i < count ? part_row(A, chunk + i, head) : prefix_row(A, min(i, n - 1) - count, b, head);
     const float pm = i < n ? A.part_m[2 * at] : kNone, pl = i < n ? A.part_m[2 * at + 1] : 0.f;
     float top = fmaxf(m, pm);
 #pragma unroll
@@ -1092,7 +1171,7 @@ extern "C" __global__ void __launch_bounds__(256) disc_join_k(AttendArgs A) {
 #pragma unroll
       for (int x = 0; x < 8; ++x) {                           // (the last one again, with a weight of 0, behind the end)
         const int j = i0 + min(x0 + x, most - 1) * ways;
-        const i64 slot = j < I.count ? part_row(A, I.first + j, head) : prefix_row(A, j - I.count, b, head);
+        const i64 slot = j < count ? part_row(A, chunk + j, head) : prefix_row(A, j - count, b, head);
 #pragma unroll
         for (int e = 0; e < kPer; ++e) v[x][e] = e * 64 + lane < kD ? A.part[slot * kD + e * 64 + lane] : 0.f;
       }

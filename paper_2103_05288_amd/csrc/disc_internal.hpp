@@ -290,6 +290,7 @@ struct Operator {
   int dtype = 0, storage = 0, head_dim = 0, rotary_dim = 0;
   void* module = nullptr;          // hipModule_t
   void* fn[5] = {};                // hipFunction_t
+  int resident = 2;                // blocks of its main kernel that a CU holds at once
 };
 
 // runtime.cpp: what decoder.cpp and scratch.hip need of a context
