@@ -283,7 +283,8 @@ extern "C" __global__ void __launch_bounds__(256) disc_load_k(RowsArgs A) {
 // =================================================================================================
 // Attention of one query token a sequence over its pages:
 //   o = sum_t p_t v_t / sum_t p_t,   p_t = 2^(c q.k_t - m),   c = softmax scale * log2(e)
-// in one pass over the keys and values with the running maximum m.
+// in one pass over the keys and values with a running reference m: the maximum, but for kLag powers of two by which
+// the scores may pass it before it moves (and with it what was summed).
 //
 // Products on the matrix cores, 16 x 16 x 32.  A step is 32 tokens; the 16 columns are the query heads
 // that share a kv head.  S^T = K Q^T: row i of tile mt takes the key of token 8 (i / 4) + 4 mt + i % 4, so
@@ -515,7 +516,8 @@ template <int RT>
 struct Rows {                                // RT x 16 query rows of a wavefront
   u32x4 q[RT][kNK * (kKE / 8)];
   f32x4 o[RT][kND];
-  float m[RT], use[RT], l[RT];               // running maximum, the same or 0, this lane's share of the sum
+  float use[RT], l[RT];                      // what the scores are taken relative to, this lane's share of the sum
+  float lim[RT];                             // how far a score may pass it: kLag, or -infinity as long as there was none
   float vinv, vlim;                          // power of two that values' scales are taken relative to
 };
 struct Keys {
@@ -640,14 +642,14 @@ DISC_DEV void scores(const Rows<RT>& R, const Keys& K, f32x4 (&s)[RT][2]) {
 constexpr float kLag = 8.f;       // a score may pass the running maximum by this many powers of two
 constexpr float kNone = -__builtin_inff();
 
-// The step's probabilities (in s, in place of the scores) and the running maximum, sum and result.
+// A step's scores, scaled, relative to the reference of their row and masked; where they pass it by more than the lag
+// (or it is the first time that there are any), the reference moves up to them, and sum and result with it.
 template <int RT>
-DISC_DEV void softmax_step(Rows<RT>& R, f32x4 (&s)[RT][2], const float (&ks)[8], float (&vs)[8], int live) {
-  bool late = false;
+DISC_DEV void bound_step(Rows<RT>& R, f32x4 (&s)[RT][2], const float (&ks)[8], float (&vs)[8], int live) {
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-    for (int j = 0; j < 8; ++j) s[rt][j / 4][j % 4] *= ks[j];
+    for (int j = 0; j < 8; ++j) s[rt][j / 4][j % 4] = __builtin_fmaf(s[rt][j / 4][j % 4], ks[j], -R.use[rt]);
   if (__ballot(live < 8)) {                       // some token of the step is not there
     asm volatile("");                             // (a branch, and not a select for every score of every step)
 #pragma unroll
@@ -657,12 +659,14 @@ DISC_DEV void softmax_step(Rows<RT>& R, f32x4 (&s)[RT][2], const float (&ks)[8],
       vs[j] = j < live ? vs[j] : 0.f;
     }
   }
+  bool late = false;
+  float top[RT];
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
-    float top = kNone;
+    top[rt] = kNone;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) top = fmaxf(top, s[rt][j / 4][j % 4]);
-    late |= top > R.m[rt] + kLag;
+    for (int j = 0; j < 8; ++j) top[rt] = fmaxf(top[rt], s[rt][j / 4][j % 4]);
+    late |= top[rt] > R.lim[rt];
   }
   float vtop = 0.f;
   if (kQuantised) {
@@ -686,25 +690,30 @@ DISC_DEV void softmax_step(Rows<RT>& R, f32x4 (&s)[RT][2], const float (&ks)[8],
     }
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-      float top = kNone;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) top = fmaxf(top, s[rt][j / 4][j % 4]);
-      top = fmaxf(max_of_groups(top), R.m[rt]);
-      const float use = top > kNone ? top : 0.f;
-      const float alpha = R.m[rt] > kNone ? __builtin_amdgcn_exp2f(R.m[rt] - use) : 0.f;
-      R.m[rt] = top;
-      R.use[rt] = use;
+      const float t = max_of_groups(top[rt]);
+      const bool first = R.lim[rt] == kNone;
+      const float shift = t > (first ? kNone : 0.f) ? t : 0.f;
+      const float alpha = first ? 0.f : __builtin_amdgcn_exp2f(-shift);
+      R.use[rt] += shift;
+      R.lim[rt] = t > kNone ? kLag : R.lim[rt];
       R.l[rt] *= alpha;
 #pragma unroll
       for (int d = 0; d < kND; ++d) R.o[rt][d] *= alpha * vscale;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) s[rt][j / 4][j % 4] -= shift;
     }
   }
+}
+
+// The step's probabilities, in place of its scores.
+template <int RT>
+DISC_DEV void weigh_step(Rows<RT>& R, f32x4 (&s)[RT][2], const float (&vs)[8]) {
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     float sum = 0.f;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      float p = __builtin_amdgcn_exp2f(s[rt][j / 4][j % 4] - R.use[rt]);
+      float p = __builtin_amdgcn_exp2f(s[rt][j / 4][j % 4]);
       sum += p;
       if (kQuantised) p *= vs[j] * R.vinv;
       s[rt][j / 4][j % 4] = p;
@@ -795,7 +804,8 @@ DISC_DEV void attend_tokens(const AttendArgs& A, const int* ids, int begin, int 
     const int next = t0 + stride;
     fetch_keys(next);
     __builtin_amdgcn_sched_barrier(0);
-    softmax_step<RT>(R, s, ks_now, vs_now, live);
+    bound_step<RT>(R, s, ks_now, vs_now, live);
+    weigh_step<RT>(R, s, vs_now);
     accumulate<RT>(R, s, V, live);
     if (next >= end) break;
     id = load_values(A, ids, base, last, next, h, V);
@@ -808,7 +818,7 @@ template <int RT>
 DISC_DEV void clear_rows(Rows<RT>& R) {
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
-    R.m[rt] = kNone;
+    R.lim[rt] = kNone;
     R.use[rt] = R.l[rt] = 0.f;
 #pragma unroll
     for (int d = 0; d < kND; ++d) R.o[rt][d] = (f32x4){0, 0, 0, 0};
@@ -915,13 +925,14 @@ extern "C" __global__ void __launch_bounds__(256, kD <= 128 ? 3 : 2) disc_attend
     // the four wavefronts' results, relative to their common maximum
     R.l[0] += __shfl_xor(R.l[0], 16);
     R.l[0] += __shfl_xor(R.l[0], 32);
-    if (g == 0) sm[w][n] = R.m[0], sl[w][n] = R.l[0];
+    const float own = R.lim[0] > kNone ? R.use[0] : kNone;
+    if (g == 0) sm[w][n] = own, sl[w][n] = R.l[0];
     __syncthreads();
     float top = kNone;
 #pragma unroll
     for (int i = 0; i < 4; ++i) top = fmaxf(top, sm[i][n]);
     // (no maximum: the sum is 0, or NaN where every score was)
-    float f = R.m[0] > kNone ? __builtin_amdgcn_exp2f(R.m[0] - top) : R.l[0];
+    float f = own > kNone ? __builtin_amdgcn_exp2f(own - top) : R.l[0];
     if (kQuantised) f = R.vinv > 0.f ? f / R.vinv : 0.f;
     // (two at a time: four would be LDS enough to keep other blocks away)
 #pragma unroll
@@ -1042,7 +1053,7 @@ extern "C" __global__ void __launch_bounds__(512, 2) disc_prefix_k(AttendArgs A)
             T.k[step][mt * kNF + (2 * i + 1) % kNF][lane] = keys_of_codes(x[2], x[3]);
           }
         }
-      if (kQuantised && lane < kStep) T.ks[step * kStep + lane] = scale;
+      if (kQuantised && lane < kStep) T.ks[step * kStep + lane] = scale * (float)(DISC_SCALE_LOG2E);
     }
     if (values) {
       Values V;
@@ -1070,25 +1081,36 @@ extern "C" __global__ void __launch_bounds__(512, 2) disc_prefix_k(AttendArgs A)
     const PrefixTile& T = tiles[turn];
     if (t0 + kTile < end) fetch(t0 + kTile);
     if (row0 < all) {
-      for (int st = 0; st < kPrefixSteps && t0 + st * kStep < end; ++st) {
-        f32x4 s[kPrefixRT][2];
+      // The next step's scores are in the matrix cores while this one's probabilities are formed.  (Steps behind the end
+      // have no token that is there.)
+      f32x4 s[2][kPrefixRT][2];
+      auto score = [&](int st) {
+        f32x4(&x)[kPrefixRT][2] = s[st & 1];
 #pragma unroll
-        for (int rt = 0; rt < kPrefixRT; ++rt) s[rt][0] = s[rt][1] = (f32x4){0, 0, 0, 0};
+        for (int rt = 0; rt < kPrefixRT; ++rt) x[rt][0] = x[rt][1] = (f32x4){0, 0, 0, 0};
 #pragma unroll
-        for (int i = 0; i < 2 * kNF; ++i) {
-          const u32x4 k = T.k[st][i][lane];
+        for (int i = 0; i < kNF; ++i)
 #pragma unroll
-          for (int rt = 0; rt < kPrefixRT; ++rt) s[rt][i / kNF] = mfma_q(k, R.q[rt][i % kNF], s[rt][i / kNF]);
-        }
+          for (int mt = 0; mt < 2; ++mt) {
+            const u32x4 k = T.k[st][mt * kNF + i][lane];
+#pragma unroll
+            for (int rt = 0; rt < kPrefixRT; ++rt) x[rt][mt] = mfma_q(k, R.q[rt][i], x[rt][mt]);
+          }
+      };
+      score(0);
+#pragma unroll
+      for (int st = 0; st < kPrefixSteps; ++st) {
         float ks[8], vs[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          ks[j] = (kQuantised ? T.ks[st * kStep + g * 8 + j] : 1.f) * (float)(DISC_SCALE_LOG2E);
+          ks[j] = kQuantised ? T.ks[st * kStep + g * 8 + j] : (float)(DISC_SCALE_LOG2E);
           vs[j] = kQuantised ? T.vs[st * kStep + g * 8 + j] : 1.f;
         }
-        softmax_step<kPrefixRT>(R, s, ks, vs, T.live[st * 4 + g]);
+        bound_step<kPrefixRT>(R, s[st & 1], ks, vs, T.live[st * 4 + g]);
+        if (st + 1 < kPrefixSteps) score(st + 1);
+        weigh_step<kPrefixRT>(R, s[st & 1], vs);
         u32x4 hi[kPrefixRT], lo[kPrefixRT];
-        split<kPrefixRT>(s, hi, lo);
+        split<kPrefixRT>(s[st & 1], hi, lo);
 #pragma unroll
         for (int d = 0; d < kND; ++d) {
           const u32x4 v = T.v[st][d][lane];
@@ -1123,7 +1145,7 @@ extern "C" __global__ void __launch_bounds__(512, 2) disc_prefix_k(AttendArgs A)
                                                           R.o[rt][x * kE + e + 3][r] * f};
         }
       }
-    if (g == 0) A.part_m[2 * at] = R.m[rt], A.part_m[2 * at + 1] = R.l[rt];
+    if (g == 0) A.part_m[2 * at] = R.lim[rt] > kNone ? R.use[rt] : kNone, A.part_m[2 * at + 1] = R.l[rt];
   }
 }
 
