@@ -1084,6 +1084,11 @@ extern "C" __global__ void __launch_bounds__(512, 2) disc_prefix_k(AttendArgs A)
       // The next step's scores are in the matrix cores while this one's probabilities are formed.  (Steps behind the end
       // have no token that is there.)
       f32x4 s[2][kPrefixRT][2];
+      u32x4 kf[2 * kNF];
+      auto read_keys = [&](int st) {
+#pragma unroll
+        for (int i = 0; i < 2 * kNF; ++i) kf[i] = T.k[st][i][lane];
+      };
       auto score = [&](int st) {
         f32x4(&x)[kPrefixRT][2] = s[st & 1];
 #pragma unroll
@@ -1091,12 +1096,11 @@ extern "C" __global__ void __launch_bounds__(512, 2) disc_prefix_k(AttendArgs A)
 #pragma unroll
         for (int i = 0; i < kNF; ++i)
 #pragma unroll
-          for (int mt = 0; mt < 2; ++mt) {
-            const u32x4 k = T.k[st][mt * kNF + i][lane];
+          for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
-            for (int rt = 0; rt < kPrefixRT; ++rt) x[rt][mt] = mfma_q(k, R.q[rt][i], x[rt][mt]);
-          }
+            for (int rt = 0; rt < kPrefixRT; ++rt) x[rt][mt] = mfma_q(kf[mt * kNF + i], R.q[rt][i], x[rt][mt]);
       };
+      read_keys(0);
       score(0);
 #pragma unroll
       for (int st = 0; st < kPrefixSteps; ++st) {
@@ -1106,11 +1110,16 @@ extern "C" __global__ void __launch_bounds__(512, 2) disc_prefix_k(AttendArgs A)
           ks[j] = kQuantised ? T.ks[st * kStep + g * 8 + j] : (float)(DISC_SCALE_LOG2E);
           vs[j] = kQuantised ? T.vs[st * kStep + g * 8 + j] : 1.f;
         }
-        bound_step<kPrefixRT>(R, s[st & 1], ks, vs, T.live[st * 4 + g]);
+        const int live = T.live[st * 4 + g];
+        if (st + 1 < kPrefixSteps) read_keys(st + 1);
+        __builtin_amdgcn_sched_barrier(0);
+        bound_step<kPrefixRT>(R, s[st & 1], ks, vs, live);
+        __builtin_amdgcn_s_setprio(1);
         if (st + 1 < kPrefixSteps) score(st + 1);
         weigh_step<kPrefixRT>(R, s[st & 1], vs);
         u32x4 hi[kPrefixRT], lo[kPrefixRT];
         split<kPrefixRT>(s[st & 1], hi, lo);
+        __builtin_amdgcn_s_setprio(0);
 #pragma unroll
         for (int d = 0; d < kND; ++d) {
           const u32x4 v = T.v[st][d][lane];
