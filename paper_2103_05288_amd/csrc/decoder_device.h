@@ -579,13 +579,12 @@ DISC_DEV int load_values(const AttendArgs& A, const int* ids, int base, int last
   return id;
 }
 
-// The scales of the lane's eight tokens 8 g + 0..7.
-DISC_DEV void load_scales(const AttendArgs& A, const int* ids, int base, int last, int t0, int h, const float* p, float (&s)[8]) {
+// The scales of a step: lanes 0..31 those of its keys, 32..63 those of its values.
+DISC_DEV float load_scale(const AttendArgs& A, const int* ids, int base, int last, int t0, int h) {
+  const int lane = threadIdx.x & 63;
   int id;
-  const i64 row = row_of(A, ids, base, min(t0 + ((threadIdx.x & 63) >> 4) * 8, last), h, id);
-  const f32x4 a = *(const f32x4*)(p + row), b = *(const f32x4*)(p + row + 4);
-#pragma unroll
-  for (int j = 0; j < 4; ++j) s[j] = a[j], s[4 + j] = b[j];
+  const i64 row = row_of(A, ids, base, min(t0 + (lane & 31), last + 7), h, id);
+  return (lane < 32 ? A.ks : A.vs)[row];
 }
 
 // Row d of V^T: element i of the lane's eight tokens, as the second product's operand.
@@ -771,41 +770,40 @@ DISC_DEV void accumulate(Rows<RT>& R, const f32x4 (&s)[RT][2], Values& V, int li
 
 // The tokens begin + first, + stride, ... (steps of 32) up to end, for the rows of one wavefront.
 template <int RT>
-DISC_DEV void attend_tokens(const AttendArgs& A, const int* ids, int begin, int end, int first, int stride, int h, Rows<RT>& R) {
-  const int g = (threadIdx.x & 63) >> 4, base = begin >> A.shift;
+DISC_DEV void attend_tokens(const AttendArgs& A, const int* ids, float* scales, int begin, int end, int first, int stride, int h, Rows<RT>& R) {
+  const int lane = threadIdx.x & 63, g = lane >> 4, base = begin >> A.shift;
   int t0 = begin + first;
   if (t0 >= end) return;
   // (places behind the chunk's last token are read at its last group of eight: in the page, masked below)
   const int last = (end - 1) & ~7;
   Keys K;
   Values V;
-  float ks[8], vs[8];
-  auto fetch_keys = [&](int t) {
-    load_keys(A, ids, base, last, t, h, K);
-    if (kQuantised) load_scales(A, ids, base, last, t, h, A.ks, ks);
-    if (kQuantised) load_scales(A, ids, base, last, t, h, A.vs, vs);
-  };
-  fetch_keys(t0);
+  float scale = 0.f;
+  load_keys(A, ids, base, last, t0, h, K);
+  if (kQuantised) scale = load_scale(A, ids, base, last, t0, h);
   int id = load_values(A, ids, base, last, t0, h, V);
   while (true) {
     f32x4 s[RT][2];
     const int n = end - (t0 + g * 8);
     const int live = id < 0 || n <= 0 ? 0 : n < 8 ? n : 8;
-    float ks_now[8], vs_now[8];
     scores<RT>(R, K, s);
+    // (this wavefront's 64 floats of LDS: the lanes' eight tokens' scales from the lanes that read them)
+    float ks[8], vs[8];
+    if (kQuantised) scales[lane] = lane < 32 ? scale * (float)(DISC_SCALE_LOG2E) : scale;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      ks_now[j] = (kQuantised ? ks[j] : 1.f) * (float)(DISC_SCALE_LOG2E);
-      vs_now[j] = vs[j];
+      ks[j] = kQuantised ? scales[g * 8 + j] : (float)(DISC_SCALE_LOG2E);
+      vs[j] = kQuantised ? scales[32 + g * 8 + j] : 1.f;
     }
     // The next step's keys are read while this one's probabilities and second product run, its values after that, in
     // the registers that are free then.  (Behind the end the last rows come again: a load that only some steps make
     // would have every step wait for all loads before it.)
     const int next = t0 + stride;
-    fetch_keys(next);
+    load_keys(A, ids, base, last, next, h, K);
+    if (kQuantised) scale = load_scale(A, ids, base, last, next, h);
     __builtin_amdgcn_sched_barrier(0);
-    bound_step<RT>(R, s, ks_now, vs_now, live);
-    weigh_step<RT>(R, s, vs_now);
+    bound_step<RT>(R, s, ks, vs, live);
+    weigh_step<RT>(R, s, vs);
     accumulate<RT>(R, s, V, live);
     if (next >= end) break;
     id = load_values(A, ids, base, last, next, h, V);
@@ -866,9 +864,10 @@ DISC_DEV i64 prefix_row(const AttendArgs& A, int part, int b, int head) {
 
 // A block's share of the sequences' tokens, for one kv head and 16 of its query heads at most; or, where the query rows
 // of all sequences are few, one chunk of the prefix for 16 of them.
-extern "C" __global__ void __launch_bounds__(256, kD <= 128 ? 3 : 2) disc_attend_k(AttendArgs A) {
+extern "C" __global__ void __launch_bounds__(256, kD <= 64 ? 4 : kD <= 128 ? 3 : 2) disc_attend_k(AttendArgs A) {
   __shared__ int ids[kMostPages + 1];     // (a stretch need not begin with a page)
   __shared__ float so[2][16][kD + 4];
+  __shared__ __align__(16) float scales[4][64];
   __shared__ float sm[4][16], sl[4][16];
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, n = lane & 15, g = lane >> 4;
   const int shared_blocks = A.prefix_tiles * A.prefix_parts * A.kv_heads;
@@ -893,7 +892,9 @@ extern "C" __global__ void __launch_bounds__(256, kD <= 128 ? 3 : 2) disc_attend
     row0 = (rest - h * A.tiles) * 16;
     rows = min(A.group - row0, 16);
     if (A.direct) {
+      // (all of the sequence's table, which is short, without waiting for its length)
       I.b = part;
+      stage_pages(A, A.table + (i64)part * A.width, A.width, 0, A.width << A.shift, ids);
       I.end = clamp_length(A.lengths[part], A.width, A.shift);
     } else {
       I.start(A, part);
@@ -916,9 +917,9 @@ extern "C" __global__ void __launch_bounds__(256, kD <= 128 ? 3 : 2) disc_attend
     const int most = kMostPages << A.shift;
     for (int at = I.begin; at < I.end;) {
       const int to = I.end - at > most ? at + most : I.end;
-      stage_pages(A, table, width, at, to, ids);
+      if (shared || !A.direct) stage_pages(A, table, width, at, to, ids);
       __syncthreads();
-      attend_tokens<1>(A, ids, at, to, w * kStep, 4 * kStep, h, R);
+      attend_tokens<1>(A, ids, scales[w], at, to, w * kStep, 4 * kStep, h, R);
       at = to;
       if (at < I.end) __syncthreads();
     }
