@@ -46,11 +46,11 @@ struct AttendArgs {
 };
 constexpr int kMaxBlockTokens = 8, kMostPages = 1024;
 constexpr int kUnit = 128;              // tokens that a block's four wavefronts take at once
-constexpr int64_t kDirectTokens = 512;  // sequences no longer than this are one chunk each
+constexpr int64_t kDirectTokens = 512;  // sequences no longer than this are one chunk each (kDirectPages of the smallest size)
 constexpr int64_t kFewRows = 64;        // query rows a kv head up to which disc_attend_k has the prefix too
 
 enum { FN_ROTARY = 0 };
-enum { FN_STORE = 0, FN_LOAD, FN_ATTEND, FN_PREFIX, FN_JOIN };
+enum { FN_STORE = 0, FN_LOAD, FN_ATTEND, FN_ATTEND2, FN_ATTEND1, FN_PREFIX, FN_JOIN, FN_CACHE_COUNT };
 
 constexpr int64_t kMostElements = (int64_t)1 << 60;
 
@@ -278,8 +278,8 @@ int register_cache(disc_ctx* c, const disc_cache_desc* d, int32_t* id_out) {
   o->dtype = d->dtype;
   o->storage = d->storage;
   o->head_dim = d->head_dim;
-  static const char* const names[] = {"disc_store_k", "disc_load_k", "disc_attend_k", "disc_prefix_k", "disc_join_k"};
-  return enter(c, std::move(o), macros, names, 5, FN_ATTEND, id_out);
+  static const char* const names[] = {"disc_store_k", "disc_load_k", "disc_attend_k", "disc_attend2_k", "disc_attend1_k", "disc_prefix_k", "disc_join_k"};
+  return enter(c, std::move(o), macros, names, FN_CACHE_COUNT, FN_ATTEND, id_out);
 }
 
 // page_size = 1 << shift; -1: no page size
@@ -357,6 +357,7 @@ int launch_rows(disc_ctx* c, int32_t id, const int64_t* dims, int n_dims, const 
 struct AttendPlan {
   AttendArgs a;
   int64_t attend_blocks, prefix_blocks, join_blocks;
+  int ways;                 // wavefronts of a sequence
   size_t workspace;
 };
 
@@ -418,6 +419,15 @@ int plan_attend(disc_ctx* c, const Operator& o, const int64_t* d, int n_dims, At
   if (parts >= (int64_t)1 << 31) return refuse(c, DISC_ERR_SHAPE, "too many chunks for one call");
   const bool alone = a.direct && prefix == 0;   // every chunk's block writes the result itself
   p->attend_blocks = times(a.direct ? batch : a.target, per);
+  p->ways = 4;
+  if (a.direct && a.prefix_tiles == 0) {
+    // Short sequences: four wavefronts each while all of them run at once, else two, else one.
+    if (p->attend_blocks > 2 * at_once)
+      p->ways = 1;
+    else if (p->attend_blocks > at_once)
+      p->ways = 2;
+    if (p->attend_blocks > 0) p->attend_blocks = ceil_div(p->attend_blocks, 4 / p->ways);
+  }
   a.parts = (int32_t)(parts = alone ? 0 : parts);
   if (p->attend_blocks >= 0 && a.prefix_tiles) {
     p->attend_blocks += prefix_blocks;
@@ -484,7 +494,7 @@ int launch_attend(disc_ctx* c, int32_t id, const int64_t* dims, int n_dims, cons
     ++n;
   }
   if (rc == DISC_OK && p.attend_blocks > 0) {
-    rc = enqueue(c, o->fn[FN_ATTEND], (uint64_t)p.attend_blocks, 1, 256, &a, sizeof a, stream);
+    rc = enqueue(c, o->fn[p.ways == 4 ? FN_ATTEND : p.ways == 2 ? FN_ATTEND2 : FN_ATTEND1], (uint64_t)p.attend_blocks, 1, 256, &a, sizeof a, stream);
     ++n;
   }
   if (rc == DISC_OK && p.join_blocks > 0) {

@@ -305,6 +305,7 @@ extern "C" __global__ void __launch_bounds__(256) disc_load_k(RowsArgs A) {
 // =================================================================================================
 constexpr int kStep = 32;                     // tokens of a step
 constexpr int kMostPages = 1024;              // pages of a stretch that are kept in LDS at a time
+constexpr int kDirectPages = 64;              // pages of a sequence that is one chunk
 constexpr int kE = kD % 128 == 0 ? 8 : kD % 64 == 0 ? 4 : 8;    // neighbouring elements of a value that a lane reads
 constexpr int kNB = (kD + 16 * kE - 1) / (16 * kE);             // such groups of 16 lanes
 constexpr int kND = kE * kNB;                                   // 16-row tiles of O^T
@@ -344,6 +345,10 @@ DISC_DEV int clamp_length(int n, int width, int shift) {
   const i64 most = (i64)width << shift;
   return n < 0 ? 0 : n > most ? (int)most : n;
 }
+
+// Number of the wavefront in its block: the same for its lanes, which the compiler has to be told, so that what depends
+// on it is a scalar and its branches are no masks.
+DISC_DEV int wavefront() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
 
 // Sum of the lanes up to this one.
 DISC_DEV u32 scan64(u32 x) {
@@ -782,7 +787,7 @@ DISC_DEV void attend_tokens(const AttendArgs& A, const int* ids, float* scales, 
   load_keys(A, ids, base, last, t0, h, K);
   if (kQuantised) scale = load_scale(A, ids, base, last, t0, h);
   int id = load_values(A, ids, base, last, t0, h, V);
-  while (true) {
+  do {
     f32x4 s[RT][2];
     const int n = end - (t0 + g * 8);
     const int live = id < 0 || n <= 0 ? 0 : n < 8 ? n : 8;
@@ -805,11 +810,10 @@ DISC_DEV void attend_tokens(const AttendArgs& A, const int* ids, float* scales, 
     bound_step<RT>(R, s, ks, vs, live);
     weigh_step<RT>(R, s, vs);
     accumulate<RT>(R, s, V, live);
-    if (next >= end) break;
     id = load_values(A, ids, base, last, next, h, V);
     __builtin_amdgcn_sched_barrier(0);
     t0 = next;
-  }
+  } while (t0 < end);
 }
 
 template <int RT>
@@ -837,10 +841,10 @@ DISC_DEV void load_query(Rows<RT>& R, int rt, const T* p) {      // p: this lane
     }
 }
 
-// Pages of the tokens [begin, end) into LDS; what is no page of the cache becomes -1.
-DISC_DEV void stage_pages(const AttendArgs& A, const int* table, int width, int begin, int end, int* ids) {
+// Pages of the tokens [begin, end) into LDS, by `of` threads; what is no page of the cache becomes -1.
+DISC_DEV void stage_pages(const AttendArgs& A, const int* table, int width, int begin, int end, int* ids, int thread, int of) {
   const int base = begin >> A.shift, n = ((end - 1) >> A.shift) - base + 1;
-  for (int i = threadIdx.x; i < n; i += 256) {
+  for (int i = thread; i < n; i += of) {
     const int p = base + i < width ? table[base + i] : -1;
     ids[i] = p >= 0 && p < A.pages ? p : -1;
   }
@@ -862,17 +866,46 @@ DISC_DEV i64 prefix_row(const AttendArgs& A, int part, int b, int head) {
   return (i64)A.parts * A.heads + ((i64)part * A.batch + b) * A.heads + head;
 }
 
-// A block's share of the sequences' tokens, for one kv head and 16 of its query heads at most; or, where the query rows
-// of all sequences are few, one chunk of the prefix for 16 of them.
-extern "C" __global__ void __launch_bounds__(256, kD <= 64 ? 4 : kD <= 128 ? 3 : 2) disc_attend_k(AttendArgs A) {
-  __shared__ int ids[kMostPages + 1];     // (a stretch need not begin with a page)
-  __shared__ float so[2][16][kD + 4];
+// What two wavefronts have of the same rows, put together: the other one's registers, lane for lane, through LDS.
+struct Other {
+  f32x4 o[kND][64];
+  float use[64], l[64];                       // use: -infinity where there was no score
+};
+DISC_DEV float reference(const Rows<1>& R) { return R.lim[0] > kNone ? R.use[0] : kNone; }
+// (no reference: the sum is 0, or NaN where every score was)
+DISC_DEV float weight(float use, float top, float l) { return use > kNone ? __builtin_amdgcn_exp2f(use - top) : l; }
+DISC_DEV void hand_over(const Rows<1>& R, Other& X) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int d = 0; d < kND; ++d) X.o[d][lane] = R.o[0][d];
+  X.use[lane] = reference(R);
+  X.l[lane] = R.l[0];
+}
+DISC_DEV void take_over(Rows<1>& R, const Other& X) {
+  const int lane = threadIdx.x & 63;
+  const float use = reference(R), also = X.use[lane], top = fmaxf(use, also), fa = weight(use, top, R.l[0]), fb = weight(also, top, X.l[lane]);
+#pragma unroll
+  for (int d = 0; d < kND; ++d) R.o[0][d] = R.o[0][d] * fa + X.o[d][lane] * fb;
+  R.l[0] = (use > kNone ? R.l[0] * fa : R.l[0]) + (also > kNone ? X.l[lane] * fb : X.l[lane]);
+  R.use[0] = top;
+  R.lim[0] = top > kNone ? kLag : kNone;
+}
+
+// `kWays` wavefronts work on the same rows, 4 / kWays rows sets a block.
+// Four: a block's share of the sequences' tokens, for one kv head and 16 of its query heads at most; or, where the query
+// rows of all sequences are few, one chunk of the prefix for 16 of them.  One or two: all of a short sequence, where
+// there are so many that blocks of four would come in several rounds, each with its latency of five steps.
+template <int kWays>
+DISC_DEV void attend_body(const AttendArgs& A) {
+  constexpr int kSets = 4 / kWays, kIds = kWays == 4 ? kMostPages + 1 : kDirectPages;   // (a stretch need not begin with a page)
+  __shared__ int all_ids[kSets][kIds];
+  __shared__ Other other[kWays == 1 ? 1 : 2];
   __shared__ __align__(16) float scales[4][64];
-  __shared__ float sm[4][16], sl[4][16];
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, n = lane & 15, g = lane >> 4;
-  const int shared_blocks = A.prefix_tiles * A.prefix_parts * A.kv_heads;
+  const int w = wavefront(), n = threadIdx.x & 15, set = w / kWays, turn = w % kWays;
+  int* ids = all_ids[set];
+  const int shared_blocks = kWays == 4 ? A.prefix_tiles * A.prefix_parts * A.kv_heads : 0;
   const bool shared = (int)blockIdx.x < shared_blocks;
-  int part, h, row0, rows;                // rows: of this block; the first is number row0 of the kv head's
+  int part, h, row0, rows;                // rows: of this set; the first is number row0 of the kv head's
   Walk I;
   I.b = I.begin = 0;
   I.whole = !shared;
@@ -885,17 +918,18 @@ extern "C" __global__ void __launch_bounds__(256, kD <= 64 ? 4 : kD <= 128 ? 3 :
     I.begin = part * A.prefix_chunk;
     I.end = min(A.prefix_len, I.begin + A.prefix_chunk);
   } else {
-    const int block = blockIdx.x - shared_blocks, per = A.kv_heads * A.tiles;
+    const int block = (blockIdx.x - shared_blocks) * kSets + set, per = A.kv_heads * A.tiles;
     part = block / per;
     const int rest = block - part * per;
     h = rest / A.tiles;
     row0 = (rest - h * A.tiles) * 16;
     rows = min(A.group - row0, 16);
-    if (A.direct) {
+    if (kWays < 4 || A.direct) {
+      if (kWays < 4 && part >= A.batch) part = rows = 0;       // (behind the last sequence: the barriers are for all)
       // (all of the sequence's table, which is short, without waiting for its length)
       I.b = part;
-      stage_pages(A, A.table + (i64)part * A.width, A.width, 0, A.width << A.shift, ids);
-      I.end = clamp_length(A.lengths[part], A.width, A.shift);
+      stage_pages(A, A.table + (i64)part * A.width, A.width, 0, A.width << A.shift, ids, turn * 64 + (threadIdx.x & 63), kWays * 64);
+      I.end = rows ? clamp_length(A.lengths[part], A.width, A.shift) : 0;
     } else {
       I.start(A, part);
       if (!I.next(A)) return;
@@ -903,78 +937,66 @@ extern "C" __global__ void __launch_bounds__(256, kD <= 64 ? 4 : kD <= 128 ? 3 :
   }
   const int width = shared ? (A.prefix_len + (1 << A.shift) - 1) >> A.shift : A.width;
   while (true) {
-    // sequence and query head of a row
-    auto place = [&](int r, int& b, int& head) {
-      b = shared ? (row0 + r) / A.group : I.b;
-      head = h * A.group + (shared ? row0 + r - b * A.group : row0 + r);
-    };
     const int* table = shared ? A.prefix_table : A.table + (i64)I.b * A.width;
+    // sequence and query head of this lane's row
+    const int b = shared ? (row0 + n) / A.group : I.b, head = h * A.group + (shared ? row0 + n - b * A.group : row0 + n);
     Rows<1> R;
     clear_rows<1>(R);
-    int b, head;
-    place(n, b, head);
     load_query<1>(R, 0, n < rows ? A.q + b * A.q_row + head * A.q_head : nullptr);
     const int most = kMostPages << A.shift;
-    for (int at = I.begin; at < I.end;) {
+    for (int at = I.begin; at < I.end || kWays < 4;) {
       const int to = I.end - at > most ? at + most : I.end;
-      if (shared || !A.direct) stage_pages(A, table, width, at, to, ids);
+      if (kWays == 4 && (shared || !A.direct)) stage_pages(A, table, width, at, to, ids, threadIdx.x, 256);
       __syncthreads();
-      attend_tokens<1>(A, ids, scales[w], at, to, w * kStep, 4 * kStep, h, R);
+      attend_tokens<1>(A, ids, scales[w], at, to, turn * kStep, kWays * kStep, h, R);
       at = to;
-      if (at < I.end) __syncthreads();
+      if (kWays < 4 || at >= I.end) break;
+      __syncthreads();
     }
-    // the four wavefronts' results, relative to their common maximum
     R.l[0] += __shfl_xor(R.l[0], 16);
     R.l[0] += __shfl_xor(R.l[0], 32);
-    const float own = R.lim[0] > kNone ? R.use[0] : kNone;
-    if (g == 0) sm[w][n] = own, sl[w][n] = R.l[0];
-    __syncthreads();
-    float top = kNone;
+    if (kQuantised) {
+      const float f = R.vinv > 0.f ? 1.f / R.vinv : 0.f;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) top = fmaxf(top, sm[i][n]);
-    // (no maximum: the sum is 0, or NaN where every score was)
-    float f = own > kNone ? __builtin_amdgcn_exp2f(own - top) : R.l[0];
-    if (kQuantised) f = R.vinv > 0.f ? f / R.vinv : 0.f;
-    // (two at a time: four would be LDS enough to keep other blocks away)
-#pragma unroll
-    for (int turn = 0; turn < 2; ++turn) {
+      for (int d = 0; d < kND; ++d) R.o[0][d] *= f;
+    }
+    if (kWays > 1) {
+      if (turn & 1) hand_over(R, other[w >> 1]);
+      __syncthreads();
+      if (!(turn & 1)) take_over(R, other[w >> 1]);
+    }
+    if (kWays > 2) {
+      if (turn == 2) hand_over(R, other[1]);
+      __syncthreads();
+      if (turn == 0) take_over(R, other[1]);
+    }
+    if (turn == 0 && n < rows) {
+      const bool alone = I.whole && A.prefix_parts == 0;
+      const float l = R.l[0];
+      const i64 at = shared ? prefix_row(A, part, b, head) : part_row(A, A.direct ? b : part + b, head);
+      T* out = A.out + b * A.o_row + head * A.o_head;
 #pragma unroll
       for (int x = 0; x < kNB; ++x)
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
-          if (element_of(x, 0, r) < kD && w / 2 != turn) {
-            f32x4* at = (f32x4*)&so[w & 1][n][element_of(x, 0, r)];
+        for (int r = 0; r < 4; ++r) {
+          const int d = element_of(x, 0, r);
+          if (d >= kD) continue;
 #pragma unroll
-            for (int i = 0; i < kE; i += 4) {
-              const f32x4 o = {R.o[0][x * kE + i][r], R.o[0][x * kE + i + 1][r], R.o[0][x * kE + i + 2][r], R.o[0][x * kE + i + 3][r]};
-              at[i / 4] = turn ? at[i / 4] + o * f : o * f;
-            }
+          for (int e = 0; e < kE; e += 4) {
+            const f32x4 o = {R.o[0][x * kE + e][r], R.o[0][x * kE + e + 1][r], R.o[0][x * kE + e + 2][r], R.o[0][x * kE + e + 3][r]};
+            if (alone) store4(out + d + e, l != 0.f ? o / l : (f32x4){0, 0, 0, 0});
+            else *(f32x4*)(A.part + at * kD + d + e) = o;
           }
-      __syncthreads();
+        }
+      if (!alone && (threadIdx.x & 63) < 16) A.part_m[2 * at] = reference(R), A.part_m[2 * at + 1] = l;
     }
-    const bool alone = I.whole && A.prefix_parts == 0;
-    // four neighbouring elements a thread
-    for (int i = threadIdx.x; i < rows * (kD / 4); i += 256) {
-      const int r = i / (kD / 4), d = (i - r * (kD / 4)) * 4;
-      const f32x4 o = *(const f32x4*)&so[0][r][d] + *(const f32x4*)&so[1][r][d];
-      float m = kNone, l = 0.f;
-#pragma unroll
-      for (int x = 0; x < 4; ++x) m = fmaxf(m, sm[x][r]);
-#pragma unroll
-      for (int x = 0; x < 4; ++x) l += sm[x][r] > kNone ? sl[x][r] * __builtin_amdgcn_exp2f(sm[x][r] - m) : sl[x][r];
-      place(r, b, head);
-      if (alone) {
-        store4(A.out + b * A.o_row + head * A.o_head + d, l != 0.f ? o / l : (f32x4){0, 0, 0, 0});
-      } else {
-        const i64 at = shared ? prefix_row(A, part, b, head) : part_row(A, A.direct ? b : part + b, head);
-        *(f32x4*)(A.part + at * kD + d) = o;
-        if (d == 0) A.part_m[2 * at] = m, A.part_m[2 * at + 1] = l;
-      }
-    }
-    if (shared || A.direct || !I.next(A)) return;
-    __syncthreads();                      // (the maxima and sums are still being read)
+    if (kWays < 4 || shared || A.direct || !I.next(A)) return;
+    __syncthreads();                      // (what was handed over is still being read)
   }
 }
+extern "C" __global__ void __launch_bounds__(256, kD <= 64 ? 4 : kD <= 128 ? 3 : 2) disc_attend_k(AttendArgs A) { attend_body<4>(A); }
+extern "C" __global__ void __launch_bounds__(256, kD <= 64 ? 4 : kD <= 128 ? 3 : 2) disc_attend2_k(AttendArgs A) { attend_body<2>(A); }
+extern "C" __global__ void __launch_bounds__(256, kD <= 64 ? 4 : kD <= 128 ? 3 : 2) disc_attend1_k(AttendArgs A) { attend_body<1>(A); }
 
 // One chunk of the shared prefix for one kv head, where the batch has many query rows: each of the eight wavefronts
 // has 16 x RT rows of its own, and all go through the same tokens.  A tile of them is read once a block, brought into
@@ -993,7 +1015,7 @@ struct PrefixTile {
 extern "C" __global__ void __launch_bounds__(512, 2) disc_prefix_k(AttendArgs A) {
   __shared__ PrefixTile tiles[2];
   __shared__ int ids[kMostPages + 1];
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, n = lane & 15, g = lane >> 4;
+  const int lane = threadIdx.x & 63, w = wavefront(), n = lane & 15, g = lane >> 4;
   // (blocks of the same chunk and kv head are a multiple of eight apart where there are that many: on one XCD)
   const int all = A.batch * A.group, per = A.prefix_parts * A.kv_heads;
   const int block = blockIdx.x / per, rest = blockIdx.x - block * per, part = rest / A.kv_heads, h = rest - part * A.kv_heads;
@@ -1164,7 +1186,7 @@ extern "C" __global__ void __launch_bounds__(512, 2) disc_prefix_k(AttendArgs A)
 // of the results themselves do not wait for each other.
 extern "C" __global__ void __launch_bounds__(256) disc_join_k(AttendArgs A) {
   __shared__ float so[4][kD], sm[4], sl[4];
-  const int w = threadIdx.x >> 6, lane = threadIdx.x & 63, ways = A.join_ways;
+  const int w = wavefront(), lane = threadIdx.x & 63, ways = A.join_ways;
   const i64 row = ways == 1 ? (i64)blockIdx.x * 4 + w : (i64)blockIdx.x;
   const int b = (int)(row / A.heads), head = (int)(row - (i64)b * A.heads);
   if (b >= A.batch) return;                                   // (one wavefront a row: no barrier comes)

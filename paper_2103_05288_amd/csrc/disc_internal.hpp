@@ -289,7 +289,7 @@ struct Operator {
   std::string key;                 // what the registration was made of
   int dtype = 0, storage = 0, head_dim = 0, rotary_dim = 0;
   void* module = nullptr;          // hipModule_t
-  void* fn[5] = {};                // hipFunction_t
+  void* fn[8] = {};                // hipFunction_t
   int resident = 2;                // blocks of its main kernel that a CU holds at once
 };
 
