@@ -34,12 +34,13 @@ def _refuse(message: str):
     raise DiscError(-1, message)
 
 
-def _stream(device: int) -> int:
-    """The hipStream_t of torch's current stream on the context's device (which need not be the current one)."""
+def _stream_of(device: int):
+    """A function of the device that gives the hipStream_t of torch's current stream there (a context's device need not be
+    torch's current one)."""
     if device < 0:
-        return 0
-    raw = getattr(_torch._C, "_cuda_getCurrentRawStream", None)
-    return raw(device) if raw is not None else _torch.cuda.current_stream(device).cuda_stream
+        return lambda d: 0
+    # (not part of torch's public interface: a torch without it takes the public way)
+    return getattr(_torch._C, "_cuda_getCurrentRawStream", None) or (lambda d: _torch.cuda.current_stream(d).cuda_stream)
 
 
 def rotary_frequencies(rotary_dim: int, base: float = 10000.0, scaling: Optional[str] = None, factor: float = 1.0,
@@ -88,6 +89,7 @@ class _Handle:
         self.ctx, self.id, self.head_dim = ctx, oid, head_dim
         self._dtype = _types()[dtype]
         self._device = ctx.device
+        self._stream = _stream_of(ctx.device)
 
     def _rows(self, t, what: str):
         """A tensor [rows, heads, head_dim] whose last axis is dense -> (rows, heads, row stride, head stride)."""
@@ -115,8 +117,7 @@ class _Handle:
             _refuse(f"{what} is {tuple(t.shape)} with strides {t.stride()}, dense {shape} is wanted")
 
     def _call(self, fn, dims, inputs, outputs, workspace, stream):
-        rc = binding._pylaunch.launch(fn, self.ctx.h.value or 0, self.id, dims, inputs, outputs, workspace, 0,
-                                      _stream(self._device) if stream is None else stream)
+        rc = binding._pylaunch.launch(fn, self.ctx.h.value or 0, self.id, dims, inputs, outputs, workspace, 0, stream)
         if rc != 0:
             self.ctx._check(rc)
 
@@ -127,13 +128,20 @@ class RotaryHandle(_Handle):
     def __init__(self, ctx, oid, dtype, head_dim):
         super().__init__(ctx, oid, dtype, head_dim)
         self._fn = C.cast(ctx.lib.disc_rotary, C.c_void_p).value
-        self._position_types = (_torch.int32, _torch.int64)
+        self._i32, self._i64 = _torch.int32, _torch.int64
 
     def launch(self, positions, inputs: Sequence, outputs: Sequence, backward: bool = False, stream: Optional[int] = None):
         """Turns up to four tensors [tokens, heads, head_dim] (queries, keys) by the positions [tokens] of their tokens.
         An output may be its input (in place).  backward=True: the inputs are gradients of the results, the outputs
         those of the inputs."""
-        if positions.dtype not in self._position_types or positions.dim() != 1 or not positions.is_contiguous():
+        stream = self._stream(self._device) if stream is None else stream
+        quick = getattr(binding._pylaunch, "rotary", None)      # all of a call that fits, in C
+        if quick is not None:
+            rc = quick(self._fn, self.ctx.h.value or 0, self.id, self._dtype, self._device, self.head_dim, self._i32, self._i64, positions, inputs,
+                       outputs, backward, stream)
+            if rc is not None:
+                return self.ctx._check(rc)
+        if positions.dtype not in (self._i32, self._i64) or positions.dim() != 1 or not positions.is_contiguous():
             _refuse("positions is a dense int32 or int64 tensor [tokens]")
         if positions.get_device() != self._device:
             _refuse(f"positions is on {positions.device}, the context on device {self._device}")
@@ -179,6 +187,11 @@ class CacheHandle(_Handle):
             self._plain(pages[3], "v_scales", self._f32, shape[:3])
         return shape
 
+    def _rows_quickly(self, fn, store, slots, rows, pages, stream):
+        quick = getattr(binding._pylaunch, "cache_rows", None)
+        return None if quick is None else quick(fn, self.ctx.h.value or 0, self.id, self._dtype, self._device, self.head_dim, self._scaled,
+                                                self._stored[0], self._i64[0], self._f32[0], store, slots, rows, pages, stream)
+
     def _slots(self, slots, rows, pages):
         count, kv_heads, page_size, _ = self._pages(pages)
         if len(rows) != 2:
@@ -193,11 +206,19 @@ class CacheHandle(_Handle):
     def store(self, rows: Sequence, slots, pages: Sequence, stream: Optional[int] = None):
         """Keys and values [tokens, kv_heads, head_dim] into the slots (int64, page * page_size + place; outside the pages,
         as -1: left out)."""
+        stream = self._stream(self._device) if stream is None else stream
+        rc = self._rows_quickly(self._store, True, slots, rows, pages, stream)
+        if rc is not None:
+            return self.ctx._check(rc)
         dims = self._slots(slots, rows, pages)
         self._call(self._store, dims, [slots, *rows], pages, None, stream)
 
     def load(self, slots, pages: Sequence, rows: Sequence, stream: Optional[int] = None):
         """The rows of the slots back into keys and values [tokens, kv_heads, head_dim] (outside the pages: zeros)."""
+        stream = self._stream(self._device) if stream is None else stream
+        rc = self._rows_quickly(self._load, False, slots, rows, pages, stream)
+        if rc is not None:
+            return self.ctx._check(rc)
         dims = self._slots(slots, rows, pages)
         self._call(self._load, dims, [slots, *pages], rows, None, stream)
 
@@ -215,6 +236,13 @@ class CacheHandle(_Handle):
                stream: Optional[int] = None):
         """out[b] = attention of the query token q[b] ([batch, q_heads, head_dim]) over the shared prefix's tokens and the
         lengths[b] tokens in the pages table[b] (int32 [batch, width])."""
+        stream = self._stream(self._device) if stream is None else stream
+        quick = getattr(binding._pylaunch, "cache_attend", None)
+        if quick is not None:
+            rc = quick(self._attend, self.ctx.h.value or 0, self.id, self._dtype, self._device, self.head_dim, self._scaled, self._stored[0],
+                       self._i32[0], self._f32[0], q, lengths, table, pages, out, workspace, prefix_table, prefix_length, stream)
+            if rc is not None:
+                return self.ctx._check(rc)
         count, kv_heads, page_size, _ = self._pages(pages)
         batch, heads, a, b = self._rows(q, "q")
         also, too, c, d = self._rows(out, "out")
