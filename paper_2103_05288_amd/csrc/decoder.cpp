@@ -2,6 +2,7 @@
 // of a launch, its launch dimensions.  No allocation and no lookup on a launch that succeeds.
 #include <hip/hip_runtime_api.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstdio>
 #include <cstring>
@@ -26,8 +27,7 @@ struct RotaryTensor {
 struct RotaryArgs {
   RotaryTensor t[DISC_ROTARY_TENSORS];
   const void* positions;
-  int64_t tokens;
-  int32_t n, position_bytes, backward, tokens_per_block;
+  int32_t n, position_bytes, backward, pad;
 };
 struct RowsArgs {
   const void* slots;
@@ -44,13 +44,15 @@ struct AttendArgs {
   int32_t batch, heads, kv_heads, group, pages, shift, width, tiles;
   int32_t target, parts, direct, join_ways, prefix_len, prefix_chunk, prefix_parts, prefix_tiles;
 };
-constexpr int kMaxBlockTokens = 8, kMostPages = 1024;
+constexpr int kMostPages = 1024;
+constexpr int64_t kNonTemporalBytes = 64 << 20;   // from here on past the caches, as the fused patterns
+constexpr int64_t kAttendStreamBytes = 128 << 20;
 constexpr int kUnit = 128;              // tokens that a block's four wavefronts take at once
 constexpr int64_t kDirectTokens = 512;  // sequences no longer than this are one chunk each (kDirectPages of the smallest size)
 constexpr int64_t kFewRows = 64;        // query rows a kv head up to which disc_attend_k has the prefix too
 
-enum { FN_ROTARY = 0 };
-enum { FN_STORE = 0, FN_LOAD, FN_ATTEND, FN_ATTEND2, FN_ATTEND1, FN_PREFIX, FN_JOIN, FN_CACHE_COUNT };
+enum { FN_ROTARY = 0, FN_ROTARY_NT, FN_ROTARY_COUNT };
+enum { FN_STORE = 0, FN_STORE_NT, FN_LOAD, FN_LOAD_NT, FN_ATTEND, FN_ATTEND2, FN_ATTEND1, FN_ATTEND_NT, FN_PREFIX = FN_ATTEND_NT + 3, FN_JOIN, FN_CACHE_COUNT };
 
 constexpr int64_t kMostElements = (int64_t)1 << 60;
 
@@ -168,12 +170,14 @@ std::string text(const char* format, double x) {
 
 // ---- rotary positions ------------------------------------------------------------------------------
 
-// elements of one access and accesses of one head, as the device code has them
+// accesses of one head, as the device code has them
 int rotary_units(const Operator& o) {
-  const int half = o.rotary_dim / 2, rest = o.head_dim - o.rotary_dim;
-  int w = 16 / dtype_bytes(o.dtype);
-  while (half % w || rest % w) w /= 2;
-  return half / w + rest / w;
+  const auto accesses = [&](int n) {
+    int w = 16 / dtype_bytes(o.dtype);
+    while (n % w) w /= 2;
+    return n / w;
+  };
+  return accesses(o.layout == DISC_ROTARY_INTERLEAVED ? o.rotary_dim : o.rotary_dim / 2) + accesses(o.head_dim - o.rotary_dim);
 }
 
 int register_rotary(disc_ctx* c, const disc_rotary_desc* d, int32_t* id_out) {
@@ -202,8 +206,9 @@ int register_rotary(disc_ctx* c, const disc_rotary_desc* d, int32_t* id_out) {
   o->dtype = d->dtype;
   o->head_dim = d->head_dim;
   o->rotary_dim = d->rotary_dim;
-  static const char* const names[] = {"disc_rotary_k"};
-  return enter(c, std::move(o), macros, names, 1, FN_ROTARY, id_out);
+  o->layout = d->layout;
+  static const char* const names[] = {"disc_rotary_k", "disc_rotary_nt_k"};
+  return enter(c, std::move(o), macros, names, FN_ROTARY_COUNT, FN_ROTARY, id_out);
 }
 
 int launch_rotary(disc_ctx* c, int32_t id, const int64_t* dims, int n_dims, const void* const* in, int n_in, void* const* out, int n_out,
@@ -216,45 +221,41 @@ int launch_rotary(disc_ctx* c, int32_t id, const int64_t* dims, int n_dims, cons
     return refuse(c, DISC_ERR_INVALID_ARG, "rotary takes positions and 1 .. 4 tensors, as many results, and 3 + 5 dims a tensor");
   RotaryArgs a;
   memset(&a, 0, sizeof a);
-  a.tokens = dims[0];
+  const int64_t tokens = dims[0];
   a.position_bytes = dims[1] == 8 ? 8 : 4;
   a.backward = dims[2] != 0;
   a.n = n_out;
-  if (a.tokens < 0 || a.tokens >= (int64_t)1 << 31) return refuse(c, DISC_ERR_SHAPE, "tokens is 0 .. 2^31 - 1", a.tokens);
+  if (tokens < 0 || tokens >= (int64_t)1 << 31) return refuse(c, DISC_ERR_SHAPE, "tokens is 0 .. 2^31 - 1", tokens);
   if (dims[1] != 4 && dims[1] != 8) return refuse(c, DISC_ERR_INVALID_ARG, "positions have 4 or 8 bytes", dims[1]);
   const int size = dtype_bytes(o->dtype);
-  int64_t most = 0;
+  int64_t most = 0, moved = 0;
   for (int k = 0; k < n_out; ++k) {
     const int64_t* s = dims + 3 + 5 * k;
     if (s[0] < 0 || s[0] > 1 << 20) return refuse(c, DISC_ERR_SHAPE, "heads is 0 .. 2^20", s[0]);
-    if (a.tokens > 0 && s[0] > 0) {
-      if (!strides_ok(a.tokens, s[1], s[0], s[2], o->head_dim) || !strides_ok(a.tokens, s[3], s[0], s[4], o->head_dim))
+    if (tokens > 0 && s[0] > 0) {
+      if (!strides_ok(tokens, s[1], s[0], s[2], o->head_dim) || !strides_ok(tokens, s[3], s[0], s[4], o->head_dim))
         return refuse(c, DISC_ERR_SHAPE, "a stride is negative or an extent overflows");
-      if (!rows_apart(a.tokens, s[3], s[0], s[4], o->head_dim)) return refuse(c, DISC_ERR_SHAPE, "rows of a result overlap");
+      if (!rows_apart(tokens, s[3], s[0], s[4], o->head_dim)) return refuse(c, DISC_ERR_SHAPE, "rows of a result overlap");
       if (!in[1 + k] || !out[k]) return refuse(c, DISC_ERR_INVALID_ARG, "null tensor pointer");
       if (!aligned(in[1 + k], size) || !aligned(out[k], size)) return refuse(c, DISC_ERR_INVALID_ARG, "a tensor is not aligned to its elements");
-      if (in[1 + k] == out[k] && ((a.tokens > 1 && s[1] != s[3]) || (s[0] > 1 && s[2] != s[4])))
+      if (in[1 + k] == out[k] && ((tokens > 1 && s[1] != s[3]) || (s[0] > 1 && s[2] != s[4])))
         return refuse(c, DISC_ERR_INVALID_ARG, "in place, both sides have the same strides");
     }
     a.t[k] = {in[1 + k], out[k], s[1], s[2], s[3], s[4], (int32_t)s[0], 0};
     most = most > s[0] ? most : s[0];
+    moved += tokens * s[0] * o->head_dim;   // (2^59 at most)
   }
-  if (a.tokens == 0 || most == 0) return context_device(c) < 0 ? refuse(c, DISC_ERR_INVALID_ARG, "host-only context cannot launch") : DISC_OK;
+  if (tokens == 0 || most == 0) return context_device(c) < 0 ? refuse(c, DISC_ERR_INVALID_ARG, "host-only context cannot launch") : DISC_OK;
   if (!in[0] || !aligned(in[0], a.position_bytes)) return refuse(c, DISC_ERR_INVALID_ARG, "positions: null or not aligned");
   a.positions = in[0];
   if (context_device(c) < 0) return refuse(c, DISC_ERR_INVALID_ARG, "host-only context cannot launch");
-  // Tokens a block: enough that every CU has eight blocks; their sines are computed once for all heads.
-  const int64_t blocks8 = (int64_t)context_cus(c) * 8;
-  int64_t per = a.tokens / blocks8;
-  per = per < 1 ? 1 : per > kMaxBlockTokens ? kMaxBlockTokens : per;
-  a.tokens_per_block = (int32_t)per;
-  const int64_t blocks = (a.tokens + per - 1) / per;
-  // Few tokens: the heads are shared out too, one pass of a block's rows each.
+  // A token a block; where they are few, the heads are shared out too, one pass of a block's rows each.
   const int64_t rows = 256 / rotary_units(*o), passes = (most + rows - 1) / rows;
-  const uint32_t y = blocks * 2 <= context_cus(c) ? (uint32_t)(passes < 64 ? passes : 64) : 1;
+  const uint32_t y = tokens * 2 <= context_cus(c) ? (uint32_t)(passes < 64 ? passes : 64) : 1;
+  const bool nt = moved * size * 2 >= kNonTemporalBytes;
   OnDevice on(context_device(c));
   if (!on.ok) return refuse(c, DISC_ERR_HIP, "hipSetDevice failed");
-  const int rc = enqueue(c, o->fn[FN_ROTARY], (uint64_t)blocks, y, 256, &a, sizeof a, stream);
+  const int rc = enqueue(c, o->fn[nt ? FN_ROTARY_NT : FN_ROTARY], (uint64_t)tokens, y, 256, &a, sizeof a, stream);
   if (rc == DISC_OK) context_count(c, 1);
   return rc;
 }
@@ -278,7 +279,8 @@ int register_cache(disc_ctx* c, const disc_cache_desc* d, int32_t* id_out) {
   o->dtype = d->dtype;
   o->storage = d->storage;
   o->head_dim = d->head_dim;
-  static const char* const names[] = {"disc_store_k", "disc_load_k", "disc_attend_k", "disc_attend2_k", "disc_attend1_k", "disc_prefix_k", "disc_join_k"};
+  static const char* const names[] = {"disc_store_k", "disc_store_nt_k", "disc_load_k", "disc_load_nt_k", "disc_attend_k", "disc_attend2_k", "disc_attend1_k",
+                                      "disc_attend_nt_k", "disc_attend2_nt_k", "disc_attend1_nt_k", "disc_prefix_k", "disc_join_k"};
   return enter(c, std::move(o), macros, names, FN_CACHE_COUNT, FN_ATTEND, id_out);
 }
 
@@ -348,7 +350,8 @@ int launch_rows(disc_ctx* c, int32_t id, const int64_t* dims, int n_dims, const 
   if (context_device(c) < 0) return refuse(c, DISC_ERR_INVALID_ARG, "host-only context cannot launch");
   OnDevice on(context_device(c));
   if (!on.ok) return refuse(c, DISC_ERR_HIP, "hipSetDevice failed");
-  const int rc = enqueue(c, o->fn[store ? FN_STORE : FN_LOAD], (uint64_t)((threads + 255) / 256), 1, 256, &a, sizeof a, stream);
+  const bool nt = times(a.tokens, a.heads) * o->head_dim * (2 + (scaled ? 1 : 2)) * 2 >= kNonTemporalBytes;
+  const int rc = enqueue(c, o->fn[(store ? FN_STORE : FN_LOAD) + (nt ? 1 : 0)], (uint64_t)((threads + 255) / 256), 1, 256, &a, sizeof a, stream);
   if (rc == DISC_OK) context_count(c, 1);
   return rc;
 }
@@ -358,6 +361,7 @@ struct AttendPlan {
   AttendArgs a;
   int64_t attend_blocks, prefix_blocks, join_blocks;
   int ways;                 // wavefronts of a sequence
+  bool nt;
   size_t workspace;
 };
 
@@ -395,6 +399,10 @@ int plan_attend(disc_ctx* c, const Operator& o, const int64_t* d, int n_dims, At
     a.direct = 1;
     parts = batch;
   }
+  // Keys and values go past the caches where they are more than those keep until the next step, and one block reads
+  // them (us, through them / past them: 562 MB 117 / 108, 235 MB 53 / 49, 70 MB 27.6 / 29.2).
+  const int64_t own = times(std::min(d[3], times(batch, width)) << shift, kv * 2 * o.head_dim * (o.storage != DISC_STORAGE_SAME ? 1 : 2));
+  p->nt = a.tiles == 1 && (own < 0 || own >= kAttendStreamBytes);
   const int64_t rows = batch * a.group;
   int64_t prefix_blocks = 0;
   if (prefix > 0 && batch > 0) {
@@ -494,7 +502,7 @@ int launch_attend(disc_ctx* c, int32_t id, const int64_t* dims, int n_dims, cons
     ++n;
   }
   if (rc == DISC_OK && p.attend_blocks > 0) {
-    rc = enqueue(c, o->fn[p.ways == 4 ? FN_ATTEND : p.ways == 2 ? FN_ATTEND2 : FN_ATTEND1], (uint64_t)p.attend_blocks, 1, 256, &a, sizeof a, stream);
+    rc = enqueue(c, o->fn[(p.ways == 4 ? FN_ATTEND : p.ways == 2 ? FN_ATTEND2 : FN_ATTEND1) + (p.nt ? FN_ATTEND_NT - FN_ATTEND : 0)], (uint64_t)p.attend_blocks, 1, 256, &a, sizeof a, stream);
     ++n;
   }
   if (rc == DISC_OK && p.join_blocks > 0) {

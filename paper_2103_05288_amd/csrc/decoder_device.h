@@ -19,6 +19,17 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 // wide accesses at any element's address (the operands' strides and pointers are the caller's)
 typedef u32x2 u32x2_u __attribute__((aligned(1)));
 typedef u32x4 u32x4_u __attribute__((aligned(1)));
+// ... and past the caches, where a call moves more than they keep for whoever comes next
+template <bool kNt, class V>
+DISC_DEV V fetch(const V* p) {
+  if (kNt) return __builtin_nontemporal_load(p);
+  return *p;
+}
+template <bool kNt, class V>
+DISC_DEV void put(V* p, V x) {
+  if (kNt) __builtin_nontemporal_store(x, p);
+  else *p = x;
+}
 
 #ifdef DISC_ROTARY
 // =================================================================================================
@@ -28,8 +39,10 @@ typedef u32x4 u32x4_u __attribute__((aligned(1)));
 // kTurns[j] = f_j / (pi/2): quarter turns a position.  p kTurns[j] is formed in 64 bits (in 32 the angle
 // of position 10^6 would be off by 0.06), reduced to an eighth of a turn each side of a quarter, and only
 // then rounded to 32 bits.
-// One block: DISC_TOKENS tokens at most.  The sines are computed once for all heads of a token and kept
-// in LDS; then the block streams the heads' rows.  Bound by memory traffic (one read, one write).
+// A block has one token: its sines are computed once for all heads and kept in LDS, then the heads' rows stream by.
+// Bound by memory traffic (one read, one write); blocks of more tokens share nothing more and leave a longer last
+// round (us at 1, 2, 4, 8 tokens a block: 32768 x 40 x 128 bf16 121, 124, 128, 133; 16007 x 24 x 80 fp32 55, 57, 59, 64).
+// Past the caches the former takes 113 us (5.9 TB/s).
 // =================================================================================================
 constexpr int kMaxTensors = 4;
 struct RotaryTensor {
@@ -41,87 +54,87 @@ struct RotaryTensor {
 struct RotaryArgs {
   RotaryTensor t[kMaxTensors];
   const void* positions;
-  i64 tokens;
-  int n, position_bytes, backward, tokens_per_block;
+  int n, position_bytes, backward, pad;
 };
 
 constexpr int kD = DISC_D, kR = DISC_R, kH = kR / 2;
-constexpr int kMaxBlockTokens = 8;
 
-// elements of one access: 16 bytes, or less where the pairs or the rest of the head do not divide
-constexpr int vec_width() {
+// Elements of one access: 16 bytes, or less where it would not divide what it goes over -- each half of the turning
+// elements, or all of them where the pairs are neighbours; and the rest of the head.
+constexpr int width_of(int n) {
   int w = 16 / (int)sizeof(DISC_T);
-  while (kH % w || (kD - kR) % w) w /= 2;
+  while (n % w) w /= 2;
   return w;
 }
-constexpr int kW = vec_width();
-constexpr int kTurnUnits = kH / kW, kUnits = kTurnUnits + (kD - kR) / kW;
+constexpr int kW = width_of(DISC_INTERLEAVED ? kR : kH), kV = width_of(kD - kR);
+constexpr int kTurnUnits = (DISC_INTERLEAVED ? kR : kH) / kW, kUnits = kTurnUnits + (kD - kR) / kV;
 static_assert(kUnits <= 256, "a head is one pass of a block at most");
 
-typedef DISC_T vec_t __attribute__((ext_vector_type(kW)));
-typedef vec_t vec_u __attribute__((aligned(alignof(DISC_T))));
+typedef DISC_T turn_t __attribute__((ext_vector_type(kW)));
+typedef turn_t turn_u __attribute__((aligned(alignof(DISC_T))));
+typedef DISC_T rest_t __attribute__((ext_vector_type(kV)));
+typedef rest_t rest_u __attribute__((aligned(alignof(DISC_T))));
 
-extern "C" __global__ void __launch_bounds__(256) disc_rotary_k(RotaryArgs A) {
-  __shared__ float cs[kMaxBlockTokens][kH], sn[kMaxBlockTokens][kH];
-  const i64 t0 = (i64)blockIdx.x * A.tokens_per_block;
-  const int nt = (int)(A.tokens - t0 < A.tokens_per_block ? A.tokens - t0 : A.tokens_per_block);
-  for (int i = threadIdx.x; i < nt * kH; i += 256) {
-    const int t = i / kH, j = i - t * kH;
-    const double p = A.position_bytes == 8 ? (double)((const i64*)A.positions)[t0 + t] : (double)((const int*)A.positions)[t0 + t];
+template <bool kNt>
+DISC_DEV void rotary_body(const RotaryArgs& A) {
+  __shared__ float cs[kH], sn[kH];
+  const i64 t = blockIdx.x;
+  for (int j = threadIdx.x; j < kH; j += 256) {
+    const double p = A.position_bytes == 8 ? (double)((const i64*)A.positions)[t] : (double)((const int*)A.positions)[t];
     const double turns = p * kTurns[j], quarter = rint(turns);
     float s, c;
     sincospif((float)(turns - quarter) * 0.5f, &s, &c);
     const int q = (int)((i64)quarter & 3);
     const float sq = q & 1 ? c : s, cq = q & 1 ? s : c;      // sin, cos of the angle up to their signs
     const float m = (float)DISC_MAGNITUDE;
-    cs[t][j] = (q == 1 || q == 2 ? -cq : cq) * m;
-    sn[t][j] = ((q & 2) != 0) != (A.backward != 0) ? -sq * m : sq * m;
+    cs[j] = (q == 1 || q == 2 ? -cq : cq) * m;
+    sn[j] = ((q & 2) != 0) != (A.backward != 0) ? -sq * m : sq * m;
   }
   __syncthreads();
-  constexpr int kRows = 256 / kUnits;                         // (token, head) rows of one pass
-  const int u = threadIdx.x % kUnits, r0 = threadIdx.x / kUnits;
-  if (r0 >= kRows) return;
   for (int k = 0; k < A.n; ++k) {
     const RotaryTensor& X = A.t[k];
+    // in place, the rest of a head is there already
+    const int units = X.x != X.y ? kUnits : kTurnUnits, rows = 256 / units, u = threadIdx.x % units;
     // blockIdx.y: a share of the heads, for calls of few tokens
-    const int h_lo = (int)((i64)X.heads * blockIdx.y / gridDim.y), nh = (int)((i64)X.heads * (blockIdx.y + 1) / gridDim.y) - h_lo;
-    if (nh == 0) continue;
-    const bool apart = X.x != X.y;                            // in place, the rest of a head is there already
-    int t = r0 / nh, h = r0 - t * nh;
-    while (t < nt) {
-      const DISC_T* x = X.x + (t0 + t) * X.x_token + (h_lo + h) * X.x_head;
-      DISC_T* y = X.y + (t0 + t) * X.y_token + (h_lo + h) * X.y_head;
+    const int h_lo = (int)((i64)X.heads * blockIdx.y / gridDim.y), h_hi = (int)((i64)X.heads * (blockIdx.y + 1) / gridDim.y);
+    const DISC_T* xt = X.x + t * X.x_token;
+    DISC_T* yt = X.y + t * X.y_token;
+    for (int h = h_lo + (int)threadIdx.x / units; h < h_hi && (int)threadIdx.x < rows * units; h += rows) {
+      const DISC_T* x = xt + h * X.x_head;
+      DISC_T* y = yt + h * X.y_head;
       if (u < kTurnUnits) {
         const int j = u * kW;
-        const int a = DISC_INTERLEAVED ? 2 * j : j, b = DISC_INTERLEAVED ? 2 * j + kW : kH + j;
-        const vec_t xa = *(const vec_u*)(x + a), xb = *(const vec_u*)(x + b);
-        vec_t ya, yb;
+        if (DISC_INTERLEAVED) {
+          const turn_t v = fetch<kNt>((const turn_u*)(x + j));
+          turn_t r;
 #pragma unroll
-        for (int e = 0; e < kW; ++e) {
-          const float c = cs[t][j + e], s = sn[t][j + e];
-          if (DISC_INTERLEAVED && kW > 1) {
-            const int i = 2 * e % kW;
-            const float p0 = (float)(2 * e < kW ? xa[i] : xb[i]), p1 = (float)(2 * e < kW ? xa[i + 1] : xb[i + 1]);
-            const DISC_T v0 = (DISC_T)(p0 * c - p1 * s), v1 = (DISC_T)(p1 * c + p0 * s);
-            if (2 * e < kW) ya[i] = v0, ya[i + 1] = v1;
-            else yb[i] = v0, yb[i + 1] = v1;
-          } else {
-            const float p0 = (float)xa[e], p1 = (float)xb[e];
-            ya[e] = (DISC_T)(p0 * c - p1 * s);
-            yb[e] = (DISC_T)(p1 * c + p0 * s);
+          for (int e = 0; e + 1 < kW; e += 2) {
+            const float c = cs[(j + e) / 2], s = sn[(j + e) / 2], p0 = (float)v[e], p1 = (float)v[e + 1];
+            r[e] = (DISC_T)(p0 * c - p1 * s);
+            r[e + 1] = (DISC_T)(p1 * c + p0 * s);
           }
+          put<kNt>((turn_u*)(y + j), (turn_u)r);
+        } else {
+          const turn_t a = fetch<kNt>((const turn_u*)(x + j)), b = fetch<kNt>((const turn_u*)(x + kH + j));
+          turn_t ra, rb;
+#pragma unroll
+          for (int e = 0; e < kW; ++e) {
+            const float c = cs[j + e], s = sn[j + e], p0 = (float)a[e], p1 = (float)b[e];
+            ra[e] = (DISC_T)(p0 * c - p1 * s);
+            rb[e] = (DISC_T)(p1 * c + p0 * s);
+          }
+          put<kNt>((turn_u*)(y + j), (turn_u)ra);
+          put<kNt>((turn_u*)(y + kH + j), (turn_u)rb);
         }
-        *(vec_u*)(y + a) = ya;
-        *(vec_u*)(y + b) = yb;
-      } else if (apart) {
-        const int a = kR + (u - kTurnUnits) * kW;
-        *(vec_u*)(y + a) = *(const vec_u*)(x + a);
+      } else {
+        const int j = kR + (u - kTurnUnits) * kV;
+        put<kNt>((rest_u*)(y + j), (rest_u)fetch<kNt>((const rest_u*)(x + j)));
       }
-      h += kRows;
-      while (h >= nh) h -= nh, ++t;
     }
   }
 }
+extern "C" __global__ void __launch_bounds__(256) disc_rotary_k(RotaryArgs A) { rotary_body<false>(A); }
+extern "C" __global__ void __launch_bounds__(256) disc_rotary_nt_k(RotaryArgs A) { rotary_body<true>(A); }
 #endif  // DISC_ROTARY
 
 #ifdef DISC_CACHE
@@ -193,7 +206,8 @@ DISC_DEV u32x2 encode(const u32x4& x, float inverse) {
 // larger than an infinity: a row that holds either gets the scale NaN and codes of zero, and reads back as
 // NaN.  A row of zeros has the scale 0.  Slots outside the pages are left out.
 // Keys and values of a (token, head) are one lane group's, so that two loads are in flight a lane.
-extern "C" __global__ void __launch_bounds__(256) disc_store_k(RowsArgs A) {
+template <bool kNt>
+DISC_DEV void store_body(const RowsArgs& A) {
   const i64 row = ((i64)blockIdx.x * 256 + threadIdx.x) / kLanes;
   const int lane = threadIdx.x % kLanes;
   const i64 t = row / A.heads;
@@ -205,13 +219,13 @@ extern "C" __global__ void __launch_bounds__(256) disc_store_k(RowsArgs A) {
   const bool mine = lane * 8 < kD;
   u32x4 x[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
   if (mine) {
-    x[0] = *(const u32x4_u*)(A.k + t * A.k_token + h * A.k_head + lane * 8);
-    x[1] = *(const u32x4_u*)(A.v + t * A.v_token + h * A.v_head + lane * 8);
+    x[0] = fetch<kNt>((const u32x4_u*)(A.k + t * A.k_token + h * A.k_head + lane * 8));
+    x[1] = fetch<kNt>((const u32x4_u*)(A.v + t * A.v_token + h * A.v_head + lane * 8));
   }
   if (!kQuantised) {
     if (mine) {
-      *(u32x4*)(A.kp + (to * kD + lane * 8) * 2) = x[0];
-      *(u32x4*)(A.vp + (to * kD + lane * 8) * 2) = x[1];
+      put<kNt>((u32x4*)(A.kp + (to * kD + lane * 8) * 2), x[0]);
+      put<kNt>((u32x4*)(A.vp + (to * kD + lane * 8) * 2), x[1]);
     }
     return;
   }
@@ -231,13 +245,14 @@ extern "C" __global__ void __launch_bounds__(256) disc_store_k(RowsArgs A) {
     const float inverse = fine && m > 0.f ? kMost / m : 0.f;
     u32x2 c = {0, 0};
     if (fine) c = encode(x[i], inverse);
-    if (mine) *(u32x2*)((i ? A.vp : A.kp) + to * kD + lane * 8) = c;
+    if (mine) put<kNt>((u32x2*)((i ? A.vp : A.kp) + to * kD + lane * 8), c);
     if (lane == 0) (i ? A.vs : A.ks)[to] = fine ? m / kMost : __builtin_nanf("");
   }
 }
 
 // Reads rows back: code * scale, rounded once.  A slot outside the pages gives a row of zeros.
-extern "C" __global__ void __launch_bounds__(256) disc_load_k(RowsArgs A) {
+template <bool kNt>
+DISC_DEV void load_body(const RowsArgs& A) {
   const i64 row = ((i64)blockIdx.x * 256 + threadIdx.x) / kLanes;
   const int lane = threadIdx.x % kLanes;
   const i64 t = row / A.heads;
@@ -251,9 +266,9 @@ extern "C" __global__ void __launch_bounds__(256) disc_load_k(RowsArgs A) {
     u32x4 y = {0, 0, 0, 0};
     if (there) {
       if (!kQuantised) {
-        y = *(const u32x4*)((i ? A.vp : A.kp) + (from * kD + lane * 8) * 2);
+        y = fetch<kNt>((const u32x4*)((i ? A.vp : A.kp) + (from * kD + lane * 8) * 2));
       } else {
-        const u32x2 c = *(const u32x2*)((i ? A.vp : A.kp) + from * kD + lane * 8);
+        const u32x2 c = fetch<kNt>((const u32x2*)((i ? A.vp : A.kp) + from * kD + lane * 8));
         const float s = (i ? A.vs : A.ks)[from];
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
@@ -276,9 +291,14 @@ extern "C" __global__ void __launch_bounds__(256) disc_load_k(RowsArgs A) {
       }
     }
     T* to = i ? A.v + t * A.v_token + h * A.v_head : A.k + t * A.k_token + h * A.k_head;
-    *(u32x4_u*)(to + lane * 8) = y;
+    put<kNt>((u32x4_u*)(to + lane * 8), (u32x4_u)y);
   }
 }
+// (past the caches in large calls: 40009 x 8 x 128 bf16 to e4m3 49.4 -> 45.0 us, 65536 x 8 x 128 from i8 89 -> 80.7, 5.0 TB/s)
+extern "C" __global__ void __launch_bounds__(256) disc_store_k(RowsArgs A) { store_body<false>(A); }
+extern "C" __global__ void __launch_bounds__(256) disc_store_nt_k(RowsArgs A) { store_body<true>(A); }
+extern "C" __global__ void __launch_bounds__(256) disc_load_k(RowsArgs A) { load_body<false>(A); }
+extern "C" __global__ void __launch_bounds__(256) disc_load_nt_k(RowsArgs A) { load_body<true>(A); }
 
 // =================================================================================================
 // Attention of one query token a sequence over its pages:
@@ -539,48 +559,60 @@ DISC_DEV i64 row_of(const AttendArgs& A, const int* ids, int base, int t, int h,
   return ((((i64)p * A.kv_heads) + h) << A.shift) + (t & ((1 << A.shift) - 1));
 }
 
+template <bool kNt>
+DISC_DEV void read_keys(const u8* p, int g, Keys& K) {
+#pragma unroll
+  for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+    for (int i = 0; i < kNK; ++i) {
+      if ((i + 1) * 64 <= kD * kSize || i * 64 + g * 16 < kD * kSize) K.k[mt][i] = fetch<kNt>((const u32x4*)(p + mt * 4 * (kD * kSize) + i * 64));
+      else K.k[mt][i] = (u32x4){0, 0, 0, 0};
+    }
+}
+
+template <bool kNt>
 DISC_DEV void load_keys(const AttendArgs& A, const int* ids, int base, int last, int t0, int h, Keys& K) {
   const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
   int id;
   const int t = min(t0 + (m >> 2) * 8, last);
   const i64 row = row_of(A, ids, base, t, h, id);
+  const u8* p = A.kp + (row + (m & 3)) * (kD * kSize) + g * 16;
+  read_keys<kNt>(p, g, K);
+}
+
+template <bool kNt>
+DISC_DEV void read_values(const u8* first, int c, Values& V) {
 #pragma unroll
-  for (int mt = 0; mt < 2; ++mt) {
-    const u8* p = A.kp + (row + mt * 4 + (m & 3)) * (kD * kSize) + g * 16;
+  for (int j = 0; j < 8; ++j) {
 #pragma unroll
-    for (int i = 0; i < kNK; ++i) {
-      if ((i + 1) * 64 <= kD * kSize || i * 64 + g * 16 < kD * kSize) K.k[mt][i] = __builtin_nontemporal_load((const u32x4*)(p + i * 64));
-      else K.k[mt][i] = (u32x4){0, 0, 0, 0};
+    for (int n = 0; n < kNB; ++n) {
+      const u8* p = first + j * (kD * kSize) + n * 16 * kE * kSize;
+      const bool mine = (n + 1) * 16 * kE <= kD || (n * 16 + c) * kE < kD;
+      if (kVW == 4) {
+        u32x4 x = {0, 0, 0, 0};
+        if (mine) x = fetch<kNt>((const u32x4*)p);
+#pragma unroll
+        for (int w = 0; w < 4; ++w) V.v[j][n * kVW + w % kVW] = x[w];
+      } else if (kVW == 2) {
+        u32x2 x = {0, 0};
+        if (mine) x = fetch<kNt>((const u32x2*)p);
+#pragma unroll
+        for (int w = 0; w < 2; ++w) V.v[j][n * kVW + w % kVW] = x[w];
+      } else {
+        V.v[j][n * kVW] = mine ? fetch<kNt>((const u32*)p) : 0u;
+      }
     }
   }
 }
 
+template <bool kNt>
 DISC_DEV int load_values(const AttendArgs& A, const int* ids, int base, int last, int t0, int h, Values& V) {
   const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
   int id;
   const int t = min(t0 + g * 8, last);
   const i64 row = row_of(A, ids, base, t, h, id);
-#pragma unroll
-  for (int j = 0; j < 8; ++j) {
-#pragma unroll
-    for (int n = 0; n < kNB; ++n) {
-      const u8* p = A.vp + (row + j) * (kD * kSize) + (n * 16 + c) * kE * kSize;
-      const bool mine = (n + 1) * 16 * kE <= kD || (n * 16 + c) * kE < kD;
-      if (kVW == 4) {
-        u32x4 x = {0, 0, 0, 0};
-        if (mine) x = __builtin_nontemporal_load((const u32x4*)p);
-#pragma unroll
-        for (int w = 0; w < 4; ++w) V.v[j][n * kVW + w % kVW] = x[w];
-      } else if (kVW == 2) {
-        u32x2 x = {0, 0};
-        if (mine) x = __builtin_nontemporal_load((const u32x2*)p);
-#pragma unroll
-        for (int w = 0; w < 2; ++w) V.v[j][n * kVW + w % kVW] = x[w];
-      } else {
-        V.v[j][n * kVW] = mine ? *(const u32*)p : 0u;
-      }
-    }
-  }
+  const u8* p = A.vp + row * (kD * kSize) + c * kE * kSize;
+  read_values<kNt>(p, c, V);
   return id;
 }
 
@@ -774,7 +806,7 @@ DISC_DEV void accumulate(Rows<RT>& R, const f32x4 (&s)[RT][2], Values& V, int li
 }
 
 // The tokens begin + first, + stride, ... (steps of 32) up to end, for the rows of one wavefront.
-template <int RT>
+template <int RT, bool kNt>
 DISC_DEV void attend_tokens(const AttendArgs& A, const int* ids, float* scales, int begin, int end, int first, int stride, int h, Rows<RT>& R) {
   const int lane = threadIdx.x & 63, g = lane >> 4, base = begin >> A.shift;
   int t0 = begin + first;
@@ -784,9 +816,9 @@ DISC_DEV void attend_tokens(const AttendArgs& A, const int* ids, float* scales, 
   Keys K;
   Values V;
   float scale = 0.f;
-  load_keys(A, ids, base, last, t0, h, K);
+  load_keys<kNt>(A, ids, base, last, t0, h, K);
   if (kQuantised) scale = load_scale(A, ids, base, last, t0, h);
-  int id = load_values(A, ids, base, last, t0, h, V);
+  int id = load_values<kNt>(A, ids, base, last, t0, h, V);
   do {
     f32x4 s[RT][2];
     const int n = end - (t0 + g * 8);
@@ -804,13 +836,13 @@ DISC_DEV void attend_tokens(const AttendArgs& A, const int* ids, float* scales, 
     // the registers that are free then.  (Behind the end the last rows come again: a load that only some steps make
     // would have every step wait for all loads before it.)
     const int next = t0 + stride;
-    load_keys(A, ids, base, last, next, h, K);
+    load_keys<kNt>(A, ids, base, last, next, h, K);
     if (kQuantised) scale = load_scale(A, ids, base, last, next, h);
     __builtin_amdgcn_sched_barrier(0);
     bound_step<RT>(R, s, ks, vs, live);
     weigh_step<RT>(R, s, vs);
     accumulate<RT>(R, s, V, live);
-    id = load_values(A, ids, base, last, next, h, V);
+    id = load_values<kNt>(A, ids, base, last, next, h, V);
     __builtin_amdgcn_sched_barrier(0);
     t0 = next;
   } while (t0 < end);
@@ -895,7 +927,7 @@ DISC_DEV void take_over(Rows<1>& R, const Other& X) {
 // Four: a block's share of the sequences' tokens, for one kv head and 16 of its query heads at most; or, where the query
 // rows of all sequences are few, one chunk of the prefix for 16 of them.  One or two: all of a short sequence, where
 // there are so many that blocks of four would come in several rounds, each with its latency of five steps.
-template <int kWays>
+template <int kWays, bool kNt>
 DISC_DEV void attend_body(const AttendArgs& A) {
   constexpr int kSets = 4 / kWays, kIds = kWays == 4 ? kMostPages + 1 : kDirectPages;   // (a stretch need not begin with a page)
   __shared__ int all_ids[kSets][kIds];
@@ -948,7 +980,7 @@ DISC_DEV void attend_body(const AttendArgs& A) {
       const int to = I.end - at > most ? at + most : I.end;
       if (kWays == 4 && (shared || !A.direct)) stage_pages(A, table, width, at, to, ids, threadIdx.x, 256);
       __syncthreads();
-      attend_tokens<1>(A, ids, scales[w], at, to, turn * kStep, kWays * kStep, h, R);
+      attend_tokens<1, kNt>(A, ids, scales[w], at, to, turn * kStep, kWays * kStep, h, R);
       at = to;
       if (kWays < 4 || at >= I.end) break;
       __syncthreads();
@@ -994,9 +1026,14 @@ DISC_DEV void attend_body(const AttendArgs& A) {
     __syncthreads();                      // (what was handed over is still being read)
   }
 }
-extern "C" __global__ void __launch_bounds__(256, kD <= 64 ? 4 : kD <= 128 ? 3 : 2) disc_attend_k(AttendArgs A) { attend_body<4>(A); }
-extern "C" __global__ void __launch_bounds__(256, kD <= 64 ? 4 : kD <= 128 ? 3 : 2) disc_attend2_k(AttendArgs A) { attend_body<2>(A); }
-extern "C" __global__ void __launch_bounds__(256, kD <= 64 ? 4 : kD <= 128 ? 3 : 2) disc_attend1_k(AttendArgs A) { attend_body<1>(A); }
+#define DISC_ATTEND(NAME, WAYS, NT) \
+  extern "C" __global__ void __launch_bounds__(256, kD <= 64 ? 4 : kD <= 128 ? 3 : 2) NAME(AttendArgs A) { attend_body<WAYS, NT>(A); }
+DISC_ATTEND(disc_attend_k, 4, false)
+DISC_ATTEND(disc_attend2_k, 2, false)
+DISC_ATTEND(disc_attend1_k, 1, false)
+DISC_ATTEND(disc_attend_nt_k, 4, true)
+DISC_ATTEND(disc_attend2_nt_k, 2, true)
+DISC_ATTEND(disc_attend1_nt_k, 1, true)
 
 // One chunk of the shared prefix for one kv head, where the batch has many query rows: each of the eight wavefronts
 // has 16 x RT rows of its own, and all go through the same tokens.  A tile of them is read once a block, brought into
@@ -1040,18 +1077,18 @@ extern "C" __global__ void __launch_bounds__(512, 2) disc_prefix_k(AttendArgs A)
   u32 held[kKeyWords > kValueWords ? kKeyWords : kValueWords];
   float scale = 0.f;                                          // of token `lane` of the step
   int live = 0;
-  auto fetch = [&](int t0) {                                  // t0: the tile's first token
+  auto fetch_tile = [&](int t0) {                                  // t0: the tile's first token
     t0 += step * kStep;
     int id;
     if (keys) {
       Keys K;
-      load_keys(A, ids, base, last, t0, h, K);
+      load_keys<false>(A, ids, base, last, t0, h, K);
 #pragma unroll
       for (int x = 0; x < kKeyWords; ++x) held[x] = K.k[x / (4 * kNK)][x / 4 % kNK][x % 4];
     }
     if (values) {
       Values V;
-      id = load_values(A, ids, base, last, t0, h, V);
+      id = load_values<false>(A, ids, base, last, t0, h, V);
       const int m = end - (t0 + g * 8);
       live = id < 0 || m <= 0 ? 0 : m < 8 ? m : 8;
 #pragma unroll
@@ -1062,7 +1099,7 @@ extern "C" __global__ void __launch_bounds__(512, 2) disc_prefix_k(AttendArgs A)
       scale = (keys ? A.ks : A.vs)[row_of(A, ids, base, t, h, id)];
     }
   };
-  auto put = [&](PrefixTile& T) {
+  auto put_tile = [&](PrefixTile& T) {
     if (keys) {
 #pragma unroll
       for (int mt = 0; mt < 2; ++mt)
@@ -1096,13 +1133,13 @@ extern "C" __global__ void __launch_bounds__(512, 2) disc_prefix_k(AttendArgs A)
     }
   };
   __syncthreads();
-  fetch(begin);
-  put(tiles[0]);
+  fetch_tile(begin);
+  put_tile(tiles[0]);
   __syncthreads();
   constexpr int kTile = kPrefixSteps * kStep;
   for (int t0 = begin, turn = 0; t0 < end; t0 += kTile, turn ^= 1) {
     const PrefixTile& T = tiles[turn];
-    if (t0 + kTile < end) fetch(t0 + kTile);
+    if (t0 + kTile < end) fetch_tile(t0 + kTile);
     if (row0 < all) {
       // The next step's scores are in the matrix cores while this one's probabilities are formed.  (Steps behind the end
       // have no token that is there.)
@@ -1154,7 +1191,7 @@ extern "C" __global__ void __launch_bounds__(512, 2) disc_prefix_k(AttendArgs A)
         }
       }
     }
-    if (t0 + kTile < end) put(tiles[turn ^ 1]);
+    if (t0 + kTile < end) put_tile(tiles[turn ^ 1]);
     __syncthreads();
   }
 #pragma unroll

@@ -287,9 +287,9 @@ int generate(const Analysis& an, const std::string& prefix, Generated* out, std:
 struct Operator {
   enum Kind { ROTARY, CACHE } kind = ROTARY;
   std::string key;                 // what the registration was made of
-  int dtype = 0, storage = 0, head_dim = 0, rotary_dim = 0;
+  int dtype = 0, storage = 0, head_dim = 0, rotary_dim = 0, layout = 0;
   void* module = nullptr;          // hipModule_t
-  void* fn[8] = {};                // hipFunction_t
+  void* fn[16] = {};                // hipFunction_t
   int resident = 2;                // blocks of its main kernel that a CU holds at once
 };
 
