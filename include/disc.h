@@ -443,7 +443,8 @@ typedef struct {
 int disc_register_cache(disc_ctx* ctx, const disc_cache_desc* desc, int32_t* id_out);
 /* The cache is the caller's memory: k_pages and v_pages [pages, kv_heads, page_size, head_dim] in the storage's
  * type, and for 8-bit storage k_scales and v_scales [pages, kv_heads, page_size] in fp32 -- dense, 16-byte aligned.
- * page_size is a power of two, 8 .. 65536.  A slot (int64) is page * page_size + place.
+ * page_size is a power of two, 8 .. 65536.  A slot (int64) is page * page_size + place.  Attention takes pages of up to
+ * 2^32 - 1 rows (pages * kv_heads * page_size).
  *
  * disc_cache_store: rows of keys and values [tokens, kv_heads, head_dim] into their slots.  dims = {tokens, kv_heads,
  * pages, page_size, token stride, head stride of the keys, token stride, head stride of the values}; inputs = {slots,

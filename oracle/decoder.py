@@ -49,14 +49,14 @@ def stored_rows(pages, slots):
 
 
 def attend(q, lengths, table, pages, scale, prefix_table=None, prefix_length=0):
-    """Attention of one query token a sequence, [batch, heads, D]; also the largest |value| and the largest sum of |q k|
-    that each result depends on (what a bound of the rounding errors is made of)."""
+    """Attention of one query token a sequence, [batch, heads, D]; also the largest |value|, the largest sum of |q k| and the
+    largest sum of |k| that each result depends on (what a bound of the rounding errors is made of)."""
     size, count = pages[0].shape[2], pages[0].shape[0]
     batch, heads, D = q.shape
     group = heads // pages[0].shape[1]
     out = torch.zeros((batch, heads, D), dtype=torch.float64, device=q.device)
     most = torch.zeros((batch, heads), dtype=torch.float64, device=q.device)
-    sums = torch.zeros((batch, heads), dtype=torch.float64, device=q.device)
+    sums, keys = (torch.zeros((batch, heads), dtype=torch.float64, device=q.device) for _ in range(2))
 
     def slots_of(row, n):
         t = torch.arange(n, device=q.device)
@@ -80,4 +80,5 @@ def attend(q, lengths, table, pages, scale, prefix_table=None, prefix_length=0):
         out[b] = (torch.softmax(products * scale, -1)[..., None] * v).sum(1)
         most[b] = v.abs().amax((1, 2))
         sums[b] = (k * qb).abs().sum(-1).amax(-1)
-    return out, most, sums
+        keys[b] = k.abs().sum(-1).amax(-1)
+    return out, most, sums, keys

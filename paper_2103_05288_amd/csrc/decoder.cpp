@@ -42,13 +42,18 @@ struct AttendArgs {
   float *part, *part_m;
   int64_t q_row, q_head, o_row, o_head;
   int32_t batch, heads, kv_heads, group, pages, shift, width, tiles;
-  int32_t target, parts, direct, join_ways, prefix_len, prefix_chunk, prefix_parts, prefix_tiles;
+  int32_t target, parts, direct, join_ways, prefix_len, prefix_chunk, prefix_parts, prefix_tiles, prefix_inline;
 };
 constexpr int kMostPages = 1024;
 constexpr int64_t kNonTemporalBytes = 64 << 20;   // from here on past the caches, as the fused patterns
 constexpr int64_t kAttendStreamBytes = 128 << 20;
 constexpr int kUnit = 128;              // tokens that a block's four wavefronts take at once
 constexpr int64_t kDirectTokens = 512;  // sequences no longer than this are one chunk each (kDirectPages of the smallest size)
+// A prefix no longer than this (or than a unit, where the query rows are few) is gone through by every sequence's own
+// block, where these run all at once: launches that join results cost more (us, joined / in line: 32 sequences of 100
+// behind 500 tokens, 32 heads, 22 / 14, 90 of 200 behind 500 31 / 26; of few rows 16 behind 128 10.7 / 7.3, but 8 behind
+// 500 12 / 14).
+constexpr int64_t kInlineTokens = 512;
 constexpr int64_t kFewRows = 64;        // query rows a kv head up to which disc_attend_k has the prefix too
 
 enum { FN_ROTARY = 0, FN_ROTARY_NT, FN_ROTARY_COUNT };
@@ -374,6 +379,7 @@ int plan_attend(disc_ctx* c, const Operator& o, const int64_t* d, int n_dims, At
   const int64_t batch = d[0], heads = d[1], kv = d[2], width = d[5], prefix = d[6], prefix_width = d[7];
   int shift = 0;
   if (const int rc = check_pages(c, o, kv, d[3], d[4], &shift)) return rc;
+  if (times(times(d[3], kv), d[4]) >= (int64_t)1 << 32) return refuse(c, DISC_ERR_SHAPE, "attention counts rows of a cache in 32 bits", d[3]);
   if (batch < 0 || batch > 1 << 20) return refuse(c, DISC_ERR_SHAPE, "batch is 0 .. 2^20", batch);
   if (heads < kv || heads % kv || heads > 1 << 20) return refuse(c, DISC_ERR_SHAPE, "q_heads is a multiple of kv_heads, at most 2^20", heads);
   if (width < 0 || times(width, d[4]) < 0 || times(width, d[4]) > (int64_t)1 << 30)
@@ -395,17 +401,20 @@ int plan_attend(disc_ctx* c, const Operator& o, const int64_t* d, int n_dims, At
   const int64_t at_once = cus * o.resident;
   a.target = (int32_t)(at_once / per > 1 ? at_once / per : 1);
   int64_t parts = batch + a.target;
-  if ((width << shift) <= kDirectTokens) {
+  // (of heads above 128 a step of four wavefronts takes three times as long: there, few blocks are more than joins cost)
+  const int64_t direct_tokens = o.head_dim <= 128 || times(batch, per) >= cus ? kDirectTokens : kUnit;
+  if ((width << shift) <= direct_tokens) {
     a.direct = 1;
     parts = batch;
   }
+  a.prefix_inline = prefix > 0 && a.direct && prefix <= (batch * a.group > kFewRows ? kInlineTokens : kUnit) && times(batch, per) <= at_once;
   // Keys and values go past the caches where they are more than those keep until the next step, and one block reads
   // them (us, through them / past them: 562 MB 117 / 108, 235 MB 53 / 49, 70 MB 27.6 / 29.2).
   const int64_t own = times(std::min(d[3], times(batch, width)) << shift, kv * 2 * o.head_dim * (o.storage != DISC_STORAGE_SAME ? 1 : 2));
-  p->nt = a.tiles == 1 && (own < 0 || own >= kAttendStreamBytes);
+  p->nt = a.tiles == 1 && !a.prefix_inline && (own < 0 || own >= kAttendStreamBytes);
   const int64_t rows = batch * a.group;
   int64_t prefix_blocks = 0;
-  if (prefix > 0 && batch > 0) {
+  if (prefix > 0 && batch > 0 && !a.prefix_inline) {
     const bool few = rows <= kFewRows;
     const int64_t block_rows = few ? 16 : o.head_dim <= 128 ? 256 : 128, row_blocks = ceil_div(rows, block_rows), slots = (few ? o.resident : 1) * cus;
     // Chunks of the prefix: as many as make the shortest run, in rounds of the blocks that are there at once times the
@@ -425,7 +434,7 @@ int plan_attend(disc_ctx* c, const Operator& o, const int64_t* d, int n_dims, At
     if (few) a.prefix_tiles = (int32_t)row_blocks;
   }
   if (parts >= (int64_t)1 << 31) return refuse(c, DISC_ERR_SHAPE, "too many chunks for one call");
-  const bool alone = a.direct && prefix == 0;   // every chunk's block writes the result itself
+  const bool alone = a.direct && (prefix == 0 || a.prefix_inline);   // every chunk's block writes the result itself
   p->attend_blocks = times(a.direct ? batch : a.target, per);
   p->ways = 4;
   if (a.direct && a.prefix_tiles == 0) {

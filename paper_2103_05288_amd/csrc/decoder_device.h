@@ -314,8 +314,7 @@ extern "C" __global__ void __launch_bounds__(256) disc_load_nt_k(RowsArgs A) { l
 // d of V^T in the matrix product is then spread over eight registers of the same lane, and byte permutes
 // put it together: the values need no LDS either.
 //
-// 8-bit codes are exact in 16-bit floating point; a key's scale multiplies its score, a value's scale
-// its probability.  Those products p * scale are taken to half precision relative to a power of two that
+// 8-bit codes are exact in half precision and in bf16; a key's scale multiplies its score, a value's scale its probability.  Those products p * scale are taken to half precision relative to a power of two that
 // follows the largest scale seen, as the probabilities follow the largest score.
 // Where the probabilities would have no more bits than the result they are held as a sum of two 16-bit
 // numbers (hi + lo), so that the only rounding that counts is the result's.
@@ -359,6 +358,7 @@ struct AttendArgs {
   int join_ways;            // wavefronts of a row of disc_join_k: 1 or 4
   int prefix_len, prefix_chunk, prefix_parts;
   int prefix_tiles;         // the prefix's blocks of 16 query rows a kv head in disc_attend_k (0: disc_prefix_k has it)
+  int prefix_inline;        // a short prefix: every sequence's own block goes through it too, and nothing is joined
 };
 
 DISC_DEV int clamp_length(int n, int width, int shift) {
@@ -482,57 +482,60 @@ DISC_DEV void chunks_of(const AttendArgs& A, int b, int& chunk, int& count) {
   }
 }
 
-#if DISC_T_F16
-DISC_DEV f32x4 mfma_q(u32x4 a, u32x4 b, f32x4 c) {
-  return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
-}
-#else
-DISC_DEV f32x4 mfma_q(u32x4 a, u32x4 b, f32x4 c) {
+// Products in half precision: the second where the values are codes (or fp16), the first where they are and `kHalf`.
+template <bool kHalf>
+DISC_DEV f32x4 mfma(u32x4 a, u32x4 b, f32x4 c) {
+  if (kHalf || DISC_T_F16) return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+#if !DISC_T_F16
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(Tx8, a), __builtin_bit_cast(Tx8, b), c, 0, 0, 0);
-}
-#endif
-// the second product: in half precision where the values are codes
-DISC_DEV f32x4 mfma_v(u32x4 a, u32x4 b, f32x4 c) {
-  if (kQuantised) return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
-  return mfma_q(a, b, c);
-}
-
-// two bytes (the low bytes of each half of x) as half-precision numbers
-DISC_DEV u32 half_of_codes(u32 x) {
-#if DISC_STORAGE == 2
-  return 0;
 #else
-  // 0x6400 + u is the half 1024 + u; u = code + 128
-  const f16x2 y = __builtin_bit_cast(f16x2, x ^ 0x64806480u) - (f16x2){(_Float16)1152.f, (_Float16)1152.f};
-  return __builtin_bit_cast(u32, y);
+  return c;
 #endif
 }
 
-// Eight neighbouring codes (two registers) as eight elements of q's type.
+// Codes as half-precision numbers: kCode times the code.  A signed code plus 128, in the low byte of a half, is that
+// many times its smallest number 2^-24; one multiply-add makes it (code + 128) 2^-9 - 128 2^-9, exactly.
+constexpr float kCode = DISC_STORAGE == 1 ? 1.f / 512.f : 1.f;
+constexpr u32 kBias = DISC_STORAGE == 1 ? 0x80808080u : 0u;    // x ^ kBias: four signed codes plus 128
+template <bool kHigh>
+DISC_DEV u32 half_of_floats(u32 x) {
+#if DISC_STORAGE == 2
+  return __builtin_bit_cast(u32, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)x, 1.f, kHigh));
+#else
+  return 0;
+#endif
+}
+DISC_DEV u32 half_of_codes(u32 x) {                            // of the low bytes of its halves, the others are 0
+  const f16x2 scale = {(_Float16)32768.f, (_Float16)32768.f}, offset = {(_Float16)-0.25f, (_Float16)-0.25f};
+  return __builtin_bit_cast(u32, __builtin_elementwise_fma(__builtin_bit_cast(f16x2, x), scale, offset));
+}
+
+// Eight neighbouring codes (two registers) of a key, in half precision or bf16.  (bf16 takes 96 operations for a step's
+// keys, half precision 72.  Kernels that stream a long cache past the caches are slower all the same with the latter, by
+// back-to-back passes and not under a profiler: 118 us against 108, 64 x 8192 tokens.)
+template <bool kHalf>
 DISC_DEV u32x4 keys_of_codes(u32 a, u32 b) {
   u32x4 r;
 #pragma unroll
   for (int w = 0; w < 2; ++w) {
-    const u32 x = w ? b : a;
-#if DISC_STORAGE == 2
-#if DISC_T_F16
-    r[2 * w] = __builtin_bit_cast(u32, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)x, 1.f, false));
-    r[2 * w + 1] = __builtin_bit_cast(u32, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)x, 1.f, true));
-#else
-    r[2 * w] = __builtin_bit_cast(u32, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)x, 1.f, false));
-    r[2 * w + 1] = __builtin_bit_cast(u32, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)x, 1.f, true));
-#endif
-#elif DISC_T_F16
-    r[2 * w] = half_of_codes(__builtin_amdgcn_perm(x, x, 0x0c010c00u));
-    r[2 * w + 1] = half_of_codes(__builtin_amdgcn_perm(x, x, 0x0c030c02u));
-#else
-    float f[4];
+    const u32 x = (w ? b : a) ^ (kHalf ? kBias : 0u);
+    if (!kHalf && DISC_STORAGE == 2) {
+      r[2 * w] = __builtin_bit_cast(u32, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)x, 1.f, false));
+      r[2 * w + 1] = __builtin_bit_cast(u32, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)x, 1.f, true));
+    } else if (!kHalf) {
+      float f[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) f[e] = (float)(signed char)(x >> (8 * e));
-    // (a code has eight significant bits at most: the upper half of its 32-bit form is exact)
-    r[2 * w] = __builtin_amdgcn_perm(__builtin_bit_cast(u32, f[1]), __builtin_bit_cast(u32, f[0]), 0x07060302u);
-    r[2 * w + 1] = __builtin_amdgcn_perm(__builtin_bit_cast(u32, f[3]), __builtin_bit_cast(u32, f[2]), 0x07060302u);
-#endif
+      for (int e = 0; e < 4; ++e) f[e] = (float)(signed char)(x >> (8 * e));
+      // (a code has eight significant bits at most: the upper half of its 32-bit form is exact)
+      r[2 * w] = __builtin_amdgcn_perm(__builtin_bit_cast(u32, f[1]), __builtin_bit_cast(u32, f[0]), 0x07060302u);
+      r[2 * w + 1] = __builtin_amdgcn_perm(__builtin_bit_cast(u32, f[3]), __builtin_bit_cast(u32, f[2]), 0x07060302u);
+    } else if (DISC_STORAGE == 2) {
+      r[2 * w] = half_of_floats<false>(x);
+      r[2 * w + 1] = half_of_floats<true>(x);
+    } else {
+      r[2 * w] = half_of_codes(__builtin_amdgcn_perm(x, x, 0x0c010c00u));
+      r[2 * w + 1] = half_of_codes(__builtin_amdgcn_perm(x, x, 0x0c030c02u));
+    }
   }
   return r;
 }
@@ -544,6 +547,7 @@ struct Rows {                                // RT x 16 query rows of a wavefron
   float use[RT], l[RT];                      // what the scores are taken relative to, this lane's share of the sum
   float lim[RT];                             // how far a score may pass it: kLag, or -infinity as long as there was none
   float vinv, vlim;                          // power of two that values' scales are taken relative to
+  float factor;                              // on the scores: softmax scale, log2(e), and what q and the keys were scaled by
 };
 struct Keys {
   u32x4 k[2][kNK];
@@ -552,11 +556,13 @@ struct Values {
   u32 v[8][kNB * kVW];
 };
 
-// `ids`: the chunk's pages in LDS (-1: none), from the page of `begin` on; t0: the step's first token.
-DISC_DEV i64 row_of(const AttendArgs& A, const int* ids, int base, int t, int h, int& id) {
-  id = ids[(t >> A.shift) - base];
-  const int p = id < 0 ? 0 : id;
-  return ((((i64)p * A.kv_heads) + h) << A.shift) + (t & ((1 << A.shift) - 1));
+// `rows`: of the stretch's pages in LDS, from the page of its first token (number `base`) on, the first row of this kv
+// head, or kNoPage.  Rows are counted in 32 bits (the host checks that there are no more); their addresses have 64.
+constexpr u32 kNoPage = 0xffffffffu;
+DISC_DEV u32 row_of(const AttendArgs& A, const u32* rows, int base, int t, bool& there) {
+  const u32 first = rows[(t >> A.shift) - base];
+  there = first != kNoPage;
+  return (there ? first : 0) + (u32)(t & ((1 << A.shift) - 1));
 }
 
 template <bool kNt>
@@ -571,13 +577,11 @@ DISC_DEV void read_keys(const u8* p, int g, Keys& K) {
 }
 
 template <bool kNt>
-DISC_DEV void load_keys(const AttendArgs& A, const int* ids, int base, int last, int t0, int h, Keys& K) {
+DISC_DEV void load_keys(const AttendArgs& A, const u32* rows, int base, int last, int t0, Keys& K) {
   const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
-  int id;
-  const int t = min(t0 + (m >> 2) * 8, last);
-  const i64 row = row_of(A, ids, base, t, h, id);
-  const u8* p = A.kp + (row + (m & 3)) * (kD * kSize) + g * 16;
-  read_keys<kNt>(p, g, K);
+  bool there;
+  const u32 row = row_of(A, rows, base, min(t0 + (m >> 2) * 8, last), there) + (m & 3);
+  read_keys<kNt>(A.kp + (u64)row * (kD * kSize) + g * 16, g, K);
 }
 
 template <bool kNt>
@@ -606,22 +610,19 @@ DISC_DEV void read_values(const u8* first, int c, Values& V) {
 }
 
 template <bool kNt>
-DISC_DEV int load_values(const AttendArgs& A, const int* ids, int base, int last, int t0, int h, Values& V) {
+DISC_DEV bool load_values(const AttendArgs& A, const u32* rows, int base, int last, int t0, Values& V) {
   const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
-  int id;
-  const int t = min(t0 + g * 8, last);
-  const i64 row = row_of(A, ids, base, t, h, id);
-  const u8* p = A.vp + row * (kD * kSize) + c * kE * kSize;
-  read_values<kNt>(p, c, V);
-  return id;
+  bool there;
+  const u32 row = row_of(A, rows, base, min(t0 + g * 8, last), there);
+  read_values<kNt>(A.vp + (u64)row * (kD * kSize) + c * kE * kSize, c, V);
+  return there;
 }
 
 // The scales of a step: lanes 0..31 those of its keys, 32..63 those of its values.
-DISC_DEV float load_scale(const AttendArgs& A, const int* ids, int base, int last, int t0, int h) {
+DISC_DEV float load_scale(const AttendArgs& A, const u32* rows, int base, int last, int t0) {
   const int lane = threadIdx.x & 63;
-  int id;
-  const i64 row = row_of(A, ids, base, min(t0 + (lane & 31), last + 7), h, id);
-  return (lane < 32 ? A.ks : A.vs)[row];
+  bool there;
+  return (lane < 32 ? A.ks : A.vs)[row_of(A, rows, base, min(t0 + (lane & 31), last + 7), there)];
 }
 
 // Row d of V^T: element i of the lane's eight tokens, as the second product's operand.
@@ -633,14 +634,10 @@ DISC_DEV u32x4 column_of(const Values& V, int n, int i) {
       const u32 a = V.v[2 * w][n * kVW + i / 2], b = V.v[2 * w + 1][n * kVW + i / 2];
       r[w] = __builtin_amdgcn_perm(b, a, i & 1 ? 0x07060302u : 0x05040100u);
     } else {
-      const u32 a = V.v[2 * w][n * kVW + i / 4], b = V.v[2 * w + 1][n * kVW + i / 4];
+      const u32 a = V.v[2 * w][n * kVW + i / 4] ^ kBias, b = V.v[2 * w + 1][n * kVW + i / 4] ^ kBias;
       const u32 e = i & 3;
-#if DISC_STORAGE == 2
-      const u32 x = __builtin_amdgcn_perm(b, a, 0x0c0c0400u + 0x0101u * e);
-      r[w] = __builtin_bit_cast(u32, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)x, 1.f, false));
-#else
-      r[w] = half_of_codes(__builtin_amdgcn_perm(b, a, 0x0c040c00u + 0x00010001u * e));
-#endif
+      if (DISC_STORAGE == 2) r[w] = half_of_floats<false>(__builtin_amdgcn_perm(b, a, 0x0c0c0400u + 0x0101u * e));
+      else r[w] = half_of_codes(__builtin_amdgcn_perm(b, a, 0x0c040c00u + 0x00010001u * e));
     }
   }
   return r;
@@ -651,7 +648,7 @@ DISC_DEV float max_of_groups(float x) {      // over the four lane groups that s
   return fmaxf(x, __shfl_xor(x, 32));
 }
 
-template <int RT>
+template <int RT, bool kHalf>
 DISC_DEV void scores(const Rows<RT>& R, const Keys& K, f32x4 (&s)[RT][2]) {
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt)
@@ -663,13 +660,13 @@ DISC_DEV void scores(const Rows<RT>& R, const Keys& K, f32x4 (&s)[RT][2]) {
     for (int i = 0; i < kNK; ++i) {
       if (!kQuantised) {
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt) s[rt][mt] = mfma_q(K.k[mt][i], R.q[rt][i], s[rt][mt]);
+        for (int rt = 0; rt < RT; ++rt) s[rt][mt] = mfma<false>(K.k[mt][i], R.q[rt][i], s[rt][mt]);
       } else {
 #pragma unroll
         for (int f = 0; f < 2; ++f) {
-          const u32x4 k = keys_of_codes(K.k[mt][i][2 * f], K.k[mt][i][2 * f + 1]);
+          const u32x4 k = keys_of_codes<kHalf>(K.k[mt][i][2 * f], K.k[mt][i][2 * f + 1]);
 #pragma unroll
-          for (int rt = 0; rt < RT; ++rt) s[rt][mt] = mfma_q(k, R.q[rt][(i * 2 + f) % (kNK * (kKE / 8))], s[rt][mt]);
+          for (int rt = 0; rt < RT; ++rt) s[rt][mt] = mfma<kHalf>(k, R.q[rt][(i * 2 + f) % (kNK * (kKE / 8))], s[rt][mt]);
         }
       }
     }
@@ -799,15 +796,15 @@ DISC_DEV void accumulate(Rows<RT>& R, const f32x4 (&s)[RT][2], Values& V, int li
       const u32x4 v = column_of(V, n, i);
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt) {
-        R.o[rt][n * kE + i] = mfma_v(v, hi[rt], R.o[rt][n * kE + i]);
-        if (kSplit) R.o[rt][n * kE + i] = mfma_v(v, lo[rt], R.o[rt][n * kE + i]);
+        R.o[rt][n * kE + i] = mfma<kQuantised>(v, hi[rt], R.o[rt][n * kE + i]);
+        if (kSplit) R.o[rt][n * kE + i] = mfma<kQuantised>(v, lo[rt], R.o[rt][n * kE + i]);
       }
     }
 }
 
 // The tokens begin + first, + stride, ... (steps of 32) up to end, for the rows of one wavefront.
 template <int RT, bool kNt>
-DISC_DEV void attend_tokens(const AttendArgs& A, const int* ids, float* scales, int begin, int end, int first, int stride, int h, Rows<RT>& R) {
+DISC_DEV void attend_tokens(const AttendArgs& A, const u32* rows, float* scales, int begin, int end, int first, int stride, Rows<RT>& R) {
   const int lane = threadIdx.x & 63, g = lane >> 4, base = begin >> A.shift;
   int t0 = begin + first;
   if (t0 >= end) return;
@@ -816,33 +813,33 @@ DISC_DEV void attend_tokens(const AttendArgs& A, const int* ids, float* scales, 
   Keys K;
   Values V;
   float scale = 0.f;
-  load_keys<kNt>(A, ids, base, last, t0, h, K);
-  if (kQuantised) scale = load_scale(A, ids, base, last, t0, h);
-  int id = load_values<kNt>(A, ids, base, last, t0, h, V);
+  load_keys<kNt>(A, rows, base, last, t0, K);
+  if (kQuantised) scale = load_scale(A, rows, base, last, t0);
+  bool there = load_values<kNt>(A, rows, base, last, t0, V);
   do {
     f32x4 s[RT][2];
     const int n = end - (t0 + g * 8);
-    const int live = id < 0 || n <= 0 ? 0 : n < 8 ? n : 8;
-    scores<RT>(R, K, s);
+    const int live = !there || n <= 0 ? 0 : n < 8 ? n : 8;
+    scores<RT, !kNt || DISC_T_F16>(R, K, s);
     // (this wavefront's 64 floats of LDS: the lanes' eight tokens' scales from the lanes that read them)
     float ks[8], vs[8];
-    if (kQuantised) scales[lane] = lane < 32 ? scale * (float)(DISC_SCALE_LOG2E) : scale;
+    if (kQuantised) scales[lane] = lane < 32 ? scale * R.factor : scale;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      ks[j] = kQuantised ? scales[g * 8 + j] : (float)(DISC_SCALE_LOG2E);
+      ks[j] = kQuantised ? scales[g * 8 + j] : R.factor;
       vs[j] = kQuantised ? scales[32 + g * 8 + j] : 1.f;
     }
     // The next step's keys are read while this one's probabilities and second product run, its values after that, in
     // the registers that are free then.  (Behind the end the last rows come again: a load that only some steps make
     // would have every step wait for all loads before it.)
     const int next = t0 + stride;
-    load_keys<kNt>(A, ids, base, last, next, h, K);
-    if (kQuantised) scale = load_scale(A, ids, base, last, next, h);
+    load_keys<kNt>(A, rows, base, last, next, K);
+    if (kQuantised) scale = load_scale(A, rows, base, last, next);
     __builtin_amdgcn_sched_barrier(0);
     bound_step<RT>(R, s, ks, vs, live);
     weigh_step<RT>(R, s, vs);
     accumulate<RT>(R, s, V, live);
-    id = load_values<kNt>(A, ids, base, last, next, h, V);
+    there = load_values<kNt>(A, rows, base, last, next, V);
     __builtin_amdgcn_sched_barrier(0);
     t0 = next;
   } while (t0 < end);
@@ -858,6 +855,7 @@ DISC_DEV void clear_rows(Rows<RT>& R) {
     for (int d = 0; d < kND; ++d) R.o[rt][d] = (f32x4){0, 0, 0, 0};
   }
   R.vinv = R.vlim = 0.f;
+  R.factor = (float)(DISC_SCALE_LOG2E);
 }
 
 // The query rows' operand: lane (n, g) holds row n, the elements that the keys' lanes hold of theirs.
@@ -873,12 +871,47 @@ DISC_DEV void load_query(Rows<RT>& R, int rt, const T* p) {      // p: this lane
     }
 }
 
-// Pages of the tokens [begin, end) into LDS, by `of` threads; what is no page of the cache becomes -1.
-DISC_DEV void stage_pages(const AttendArgs& A, const int* table, int width, int begin, int end, int* ids, int thread, int of) {
+// bf16 queries for keys that are codes, in half precision: relative to a power of two of the largest of them all, of
+// the wavefront or of the block (`top`: their bits; NaN and infinity pass through).  What is below 2^-24 of the largest is
+// lost: of a score, 2^-25 of the largest |q| times the sum of |k|, less than what its sum of D products is rounded by.
+template <int RT>
+DISC_DEV u32 largest_query(const Rows<RT>& R) {               // bits of |q|, of this lane
+  u32 top = 0;
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+    for (int i = 0; i < kNK * (kKE / 8); ++i)
+#pragma unroll
+      for (int w = 0; w < 4; ++w) top = max(top, max(R.q[rt][i][w] & 0x7fffu, (R.q[rt][i][w] >> 16) & 0x7fffu));
+  return top;
+}
+template <int RT>
+DISC_DEV void halve_query(Rows<RT>& R, u32 top) {
+#if !DISC_T_F16
+  // (biased exponent of the largest; 0 and infinity have 1 and 254 for theirs)
+  const int e = min(max((int)(top >> 7), 1), 254);
+  const float down = __builtin_bit_cast(float, (u32)max(254 - e, 1) << 23);     // 2^(127 - e)
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+    for (int i = 0; i < kNK * (kKE / 8); ++i)
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const u32 x = R.q[rt][i][w];
+        const f16x2 y = {(_Float16)(__builtin_bit_cast(float, x << 16) * down), (_Float16)(__builtin_bit_cast(float, x & 0xffff0000u) * down)};
+        R.q[rt][i][w] = __builtin_bit_cast(u32, y);
+      }
+  R.factor *= 1.f / down;
+#endif
+  R.factor *= 1.f / kCode;
+}
+
+// Rows of the pages of the tokens [begin, end), for a kv head, into LDS, by `of` threads.
+DISC_DEV void stage_pages(const AttendArgs& A, const int* table, int width, int begin, int end, int h, u32* rows, int thread, int of) {
   const int base = begin >> A.shift, n = ((end - 1) >> A.shift) - base + 1;
   for (int i = thread; i < n; i += of) {
     const int p = base + i < width ? table[base + i] : -1;
-    ids[i] = p >= 0 && p < A.pages ? p : -1;
+    rows[i] = p >= 0 && p < A.pages ? ((u32)p * (u32)A.kv_heads + (u32)h) << A.shift : kNoPage;
   }
 }
 
@@ -930,11 +963,11 @@ DISC_DEV void take_over(Rows<1>& R, const Other& X) {
 template <int kWays, bool kNt>
 DISC_DEV void attend_body(const AttendArgs& A) {
   constexpr int kSets = 4 / kWays, kIds = kWays == 4 ? kMostPages + 1 : kDirectPages;   // (a stretch need not begin with a page)
-  __shared__ int all_ids[kSets][kIds];
+  __shared__ u32 all_pages[kSets][kIds];
   __shared__ Other other[kWays == 1 ? 1 : 2];
   __shared__ __align__(16) float scales[4][64];
   const int w = wavefront(), n = threadIdx.x & 15, set = w / kWays, turn = w % kWays;
-  int* ids = all_ids[set];
+  u32* pages = all_pages[set];
   const int shared_blocks = kWays == 4 ? A.prefix_tiles * A.prefix_parts * A.kv_heads : 0;
   const bool shared = (int)blockIdx.x < shared_blocks;
   int part, h, row0, rows;                // rows: of this set; the first is number row0 of the kv head's
@@ -960,7 +993,9 @@ DISC_DEV void attend_body(const AttendArgs& A) {
       if (kWays < 4 && part >= A.batch) part = rows = 0;       // (behind the last sequence: the barriers are for all)
       // (all of the sequence's table, which is short, without waiting for its length)
       I.b = part;
-      stage_pages(A, A.table + (i64)part * A.width, A.width, 0, A.width << A.shift, ids, turn * 64 + (threadIdx.x & 63), kWays * 64);
+      stage_pages(A, A.table + (i64)part * A.width, A.width, 0, A.width << A.shift, h, pages, turn * 64 + (threadIdx.x & 63), kWays * 64);
+      if (kWays == 4 && A.prefix_inline)
+        stage_pages(A, A.prefix_table, (A.prefix_len + (1 << A.shift) - 1) >> A.shift, 0, A.prefix_len, h, pages + kDirectPages, threadIdx.x, 256);
       I.end = rows ? clamp_length(A.lengths[part], A.width, A.shift) : 0;
     } else {
       I.start(A, part);
@@ -975,20 +1010,32 @@ DISC_DEV void attend_body(const AttendArgs& A) {
     Rows<1> R;
     clear_rows<1>(R);
     load_query<1>(R, 0, n < rows ? A.q + b * A.q_row + head * A.q_head : nullptr);
+    if (kQuantised && (!kNt || DISC_T_F16)) {
+      u32 top = largest_query<1>(R);
+#pragma unroll
+      for (int d = 1; d < 64; d *= 2) top = max(top, (u32)__shfl_xor((int)top, d));
+      halve_query<1>(R, top);
+    }
     const int most = kMostPages << A.shift;
-    for (int at = I.begin; at < I.end || kWays < 4;) {
-      const int to = I.end - at > most ? at + most : I.end;
-      if (kWays == 4 && (shared || !A.direct)) stage_pages(A, table, width, at, to, ids, threadIdx.x, 256);
+    bool ahead = kWays == 4 && A.prefix_inline;                // the prefix, in front of the sequence's own
+    for (int at = ahead ? 0 : I.begin;;) {
+      const int end = ahead ? A.prefix_len : I.end, to = end - at > most ? at + most : end;
+      if (kWays == 4 && at < end && (shared || !A.direct)) stage_pages(A, table, width, at, to, h, pages, threadIdx.x, 256);
       __syncthreads();
-      attend_tokens<1, kNt>(A, ids, scales[w], at, to, turn * kStep, kWays * kStep, h, R);
+      attend_tokens<1, kNt>(A, ahead ? pages + kDirectPages : pages, scales[w], at, to, turn * kStep, kWays * kStep, R);
       at = to;
-      if (kWays < 4 || at >= I.end) break;
+      if (ahead) {
+        ahead = false;
+        at = I.begin;
+        continue;
+      }
+      if (kWays < 4 || at >= end) break;
       __syncthreads();
     }
     R.l[0] += __shfl_xor(R.l[0], 16);
     R.l[0] += __shfl_xor(R.l[0], 32);
     if (kQuantised) {
-      const float f = R.vinv > 0.f ? 1.f / R.vinv : 0.f;
+      const float f = R.vinv > 0.f ? 1.f / (R.vinv * kCode) : 0.f;
 #pragma unroll
       for (int d = 0; d < kND; ++d) R.o[0][d] *= f;
     }
@@ -1026,8 +1073,11 @@ DISC_DEV void attend_body(const AttendArgs& A) {
     __syncthreads();                      // (what was handed over is still being read)
   }
 }
+// (wavefronts a SIMD by the registers that they take; 16-bit rows of 256 do not fit 256: 31 spilled ones cost 60 us where one
+// wavefront takes 36, four sequences of 15000)
+constexpr int kWavesPerSimd = kD <= 64 ? 4 : kD <= 128 ? 3 : kQuantised ? 2 : 1;
 #define DISC_ATTEND(NAME, WAYS, NT) \
-  extern "C" __global__ void __launch_bounds__(256, kD <= 64 ? 4 : kD <= 128 ? 3 : 2) NAME(AttendArgs A) { attend_body<WAYS, NT>(A); }
+  extern "C" __global__ void __launch_bounds__(256, kWavesPerSimd) NAME(AttendArgs A) { attend_body<WAYS, NT>(A); }
 DISC_ATTEND(disc_attend_k, 4, false)
 DISC_ATTEND(disc_attend2_k, 2, false)
 DISC_ATTEND(disc_attend1_k, 1, false)
@@ -1051,17 +1101,15 @@ struct PrefixTile {
 };
 extern "C" __global__ void __launch_bounds__(512, 2) disc_prefix_k(AttendArgs A) {
   __shared__ PrefixTile tiles[2];
-  __shared__ int ids[kMostPages + 1];
+  __shared__ u32 pages[kMostPages + 1];
+  __shared__ u32 tops[8];
   const int lane = threadIdx.x & 63, w = wavefront(), n = lane & 15, g = lane >> 4;
   // (blocks of the same chunk and kv head are a multiple of eight apart where there are that many: on one XCD)
   const int all = A.batch * A.group, per = A.prefix_parts * A.kv_heads;
   const int block = blockIdx.x / per, rest = blockIdx.x - block * per, part = rest / A.kv_heads, h = rest - part * A.kv_heads;
   const int begin = part * A.prefix_chunk, end = min(A.prefix_len, begin + A.prefix_chunk);
   const int base = begin >> A.shift, last = (end - 1) & ~7;
-  for (int i = threadIdx.x; i < ((end - 1) >> A.shift) - base + 1; i += 512) {
-    const int p = A.prefix_table[base + i];
-    ids[i] = p >= 0 && p < A.pages ? p : -1;
-  }
+  stage_pages(A, A.prefix_table, (A.prefix_len + (1 << A.shift) - 1) >> A.shift, begin, end, h, pages, threadIdx.x, 512);
   const int row0 = (block * 8 + w) * kPrefixRT * 16;
   Rows<kPrefixRT> R;
   clear_rows<kPrefixRT>(R);
@@ -1069,6 +1117,16 @@ extern "C" __global__ void __launch_bounds__(512, 2) disc_prefix_k(AttendArgs A)
   for (int rt = 0; rt < kPrefixRT; ++rt) {
     const int row = row0 + rt * 16 + n, b = row / A.group, i = row - b * A.group;
     load_query<kPrefixRT>(R, rt, row < all ? A.q + b * A.q_row + (h * A.group + i) * A.q_head : nullptr);
+  }
+  if (kQuantised) {                                           // (one power of two for the block: its keys' scales are shared)
+    u32 top = largest_query<kPrefixRT>(R);
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) top = max(top, (u32)__shfl_xor((int)top, d));
+    tops[w] = top;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top = max(top, tops[i]);
+    halve_query<kPrefixRT>(R, top);
   }
   const bool keys = w < kPrefixSteps, values = !keys && w < 2 * kPrefixSteps;
   const int step = keys ? w : w - kPrefixSteps;               // this wavefront's share of a tile
@@ -1079,24 +1137,24 @@ extern "C" __global__ void __launch_bounds__(512, 2) disc_prefix_k(AttendArgs A)
   int live = 0;
   auto fetch_tile = [&](int t0) {                                  // t0: the tile's first token
     t0 += step * kStep;
-    int id;
+    bool there;
     if (keys) {
       Keys K;
-      load_keys<false>(A, ids, base, last, t0, h, K);
+      load_keys<false>(A, pages, base, last, t0, K);
 #pragma unroll
       for (int x = 0; x < kKeyWords; ++x) held[x] = K.k[x / (4 * kNK)][x / 4 % kNK][x % 4];
     }
     if (values) {
       Values V;
-      id = load_values<false>(A, ids, base, last, t0, h, V);
+      there = load_values<false>(A, pages, base, last, t0, V);
       const int m = end - (t0 + g * 8);
-      live = id < 0 || m <= 0 ? 0 : m < 8 ? m : 8;
+      live = !there || m <= 0 ? 0 : m < 8 ? m : 8;
 #pragma unroll
       for (int x = 0; x < kValueWords; ++x) held[x] = V.v[x / (kNB * kVW)][x % (kNB * kVW)];
     }
     if (kQuantised && (keys || values)) {
       const int t = min(t0 + (lane & 31), last + 7);
-      scale = (keys ? A.ks : A.vs)[row_of(A, ids, base, t, h, id)];
+      scale = (keys ? A.ks : A.vs)[row_of(A, pages, base, t, there)];
     }
   };
   auto put_tile = [&](PrefixTile& T) {
@@ -1109,11 +1167,11 @@ extern "C" __global__ void __launch_bounds__(512, 2) disc_prefix_k(AttendArgs A)
           if (!kQuantised) {
             T.k[step][mt * kNF + i][lane] = (u32x4){x[0], x[1], x[2], x[3]};
           } else {
-            T.k[step][mt * kNF + 2 * i][lane] = keys_of_codes(x[0], x[1]);
-            T.k[step][mt * kNF + (2 * i + 1) % kNF][lane] = keys_of_codes(x[2], x[3]);
+            T.k[step][mt * kNF + 2 * i][lane] = keys_of_codes<true>(x[0], x[1]);
+            T.k[step][mt * kNF + (2 * i + 1) % kNF][lane] = keys_of_codes<true>(x[2], x[3]);
           }
         }
-      if (kQuantised && lane < kStep) T.ks[step * kStep + lane] = scale * (float)(DISC_SCALE_LOG2E);
+      if (kQuantised && lane < kStep) T.ks[step * kStep + lane] = scale * R.factor;
     }
     if (values) {
       Values V;
@@ -1158,7 +1216,7 @@ extern "C" __global__ void __launch_bounds__(512, 2) disc_prefix_k(AttendArgs A)
 #pragma unroll
           for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
-            for (int rt = 0; rt < kPrefixRT; ++rt) x[rt][mt] = mfma_q(kf[mt * kNF + i], R.q[rt][i], x[rt][mt]);
+            for (int rt = 0; rt < kPrefixRT; ++rt) x[rt][mt] = mfma<kQuantised>(kf[mt * kNF + i], R.q[rt][i], x[rt][mt]);
       };
       read_keys(0);
       score(0);
@@ -1167,7 +1225,7 @@ extern "C" __global__ void __launch_bounds__(512, 2) disc_prefix_k(AttendArgs A)
         float ks[8], vs[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          ks[j] = kQuantised ? T.ks[st * kStep + g * 8 + j] : (float)(DISC_SCALE_LOG2E);
+          ks[j] = kQuantised ? T.ks[st * kStep + g * 8 + j] : R.factor;
           vs[j] = kQuantised ? T.vs[st * kStep + g * 8 + j] : 1.f;
         }
         const int live = T.live[st * 4 + g];
@@ -1185,8 +1243,8 @@ extern "C" __global__ void __launch_bounds__(512, 2) disc_prefix_k(AttendArgs A)
           const u32x4 v = T.v[st][d][lane];
 #pragma unroll
           for (int rt = 0; rt < kPrefixRT; ++rt) {
-            R.o[rt][d] = mfma_v(v, hi[rt], R.o[rt][d]);
-            if (kSplit) R.o[rt][d] = mfma_v(v, lo[rt], R.o[rt][d]);
+            R.o[rt][d] = mfma<kQuantised>(v, hi[rt], R.o[rt][d]);
+            if (kSplit) R.o[rt][d] = mfma<kQuantised>(v, lo[rt], R.o[rt][d]);
           }
         }
       }
@@ -1201,7 +1259,7 @@ extern "C" __global__ void __launch_bounds__(512, 2) disc_prefix_k(AttendArgs A)
     const int row = row0 + rt * 16 + n, b = row / A.group, i = row - b * A.group;
     if (row >= all) continue;
     const i64 at = prefix_row(A, part, b, h * A.group + i);
-    const float f = !kQuantised ? 1.f : R.vinv > 0.f ? 1.f / R.vinv : 0.f;
+    const float f = !kQuantised ? 1.f : R.vinv > 0.f ? 1.f / (R.vinv * kCode) : 0.f;
 #pragma unroll
     for (int x = 0; x < kNB; ++x)
 #pragma unroll

@@ -289,16 +289,20 @@ def _setup(dtype, storage, D, kv, group, size, lengths, prefix, g, spare=2):
             "prefix_table": order[:np].contiguous(), "prefix": prefix}
 
 
-def _attend_bound(dtype, storage, s, want, most, sums, scale):
+def _attend_bound(dtype, storage, s, want, most, sums, keys, scale):
     """|out - exact| where every weight is off by at most w, relatively: 2 w max|v| and the result's own half step.
     A weight's parts: its score (D products, exact, summed in 32 bits, then two products), the power of two by the
     hardware (2^-22), its rounding -- to half precision with 8-bit storage, otherwise or for fp16 results to two
-    numbers -- and sums over n tokens in 32 bits.  Half precision loses below 2^-25 of the largest product of a weight
+    numbers -- and sums over n tokens in 32 bits.  bf16 queries for 8-bit keys are half-precision numbers relative to the
+    largest of them: of each, half of its smallest step 2^-24 may be lost, 2^-25 of the largest |q| (which has a factor of
+    up to two in it) times the sum of |k|.  Half precision loses below 2^-25 of the largest product of a weight
     and a value's scale: n of those."""
     D = s["q"].shape[2]
     n = float(s["prefix"] + max(0, int(s["lengths"].max()) if s["lengths"].numel() else 0))
     one = 2.0 ** -11 if storage in STORED and dtype == "bf16" else 2.0 ** -16
     score = sums * scale * ((D + 4) * 2.0 ** -24)
+    if storage in STORED and dtype == "bf16":
+        score = score + scale * 2.0 ** -25 * float(s["q"].abs().max()) * keys
     w = one + score + 2.0 ** -22 + 4 * n * 2.0 ** -24
     return _half_step(TYPES[dtype]) * want.abs() + (2 * w * most)[..., None] * 1.01
 
@@ -317,8 +321,8 @@ def _run(cache, s, stream=None, out=None, workspace=None):
 
 def _check(cache, dtype, storage, s, scale, got=None):
     got = _run(cache, s)[0] if got is None else got
-    want, most, sums = plain.attend(s["q"], s["lengths"], s["table"], s["pages"], scale, s["prefix_table"], s["prefix"])
-    _inside(got, want, _attend_bound(dtype, storage, s, want, most, sums, scale), f"attention {dtype} {storage}")
+    want, *sizes = plain.attend(s["q"], s["lengths"], s["table"], s["pages"], scale, s["prefix_table"], s["prefix"])
+    _inside(got, want, _attend_bound(dtype, storage, s, want, *sizes, scale), f"attention {dtype} {storage}")
     return got
 
 
@@ -361,6 +365,17 @@ def test_attention_shared_prefix_of_a_large_batch(ctx):
     _check(cache, "bf16", "i8", _setup("bf16", "i8", 128, 2, 4, 16, lengths, 2500, g), 1.0 / math.sqrt(128))
     # every sequence with nothing of its own
     _check(cache, "bf16", "i8", _setup("bf16", "i8", 128, 1, 8, 16, [0] * 5, 33, g), 1.0 / math.sqrt(128))
+
+
+@pytest.mark.parametrize("dtype,storage,D", [("bf16", "bf16", 128), ("bf16", "i8", 64), ("f16", "e4m3", 256), ("f16", "f16", 80)])
+@pytest.mark.parametrize("batch,kv,group,size,prefix", [(5, 1, 8, 8, 0), (5, 2, 3, 8, 77), (3, 1, 17, 64, 512), (300, 1, 2, 16, 100), (420, 2, 1, 8, 0), (900, 2, 4, 32, 0),
+                                                        (900, 2, 4, 32, 40)])
+def test_attention_of_short_sequences(ctx, dtype, storage, D, batch, kv, group, size, prefix):
+    """Sequences of one chunk each, by four wavefronts, two or one; prefixes that are gone through in line, and shared ones."""
+    cache = _cache(ctx, dtype, storage, D)
+    some = [0, 1, 8, 31, 33, 100, 128, 200, 250, 129]
+    lengths = [some[(7 * i + i // 3) % len(some)] if i else 240 for i in range(batch)]
+    _check(cache, dtype, storage, _setup(dtype, storage, D, kv, group, size, lengths, prefix, _generator(batch + D)), 1.0 / math.sqrt(D))
 
 
 def test_attention_strides_scale_and_rows_behind_the_batch(ctx):
