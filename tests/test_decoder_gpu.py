@@ -98,6 +98,26 @@ def test_rotary_matches_64_bits(ctx, dtype, D, R, layout, tokens, heads, far, ba
     del held
 
 
+@pytest.mark.parametrize("dtype,D,R,layout", [("f32", 96, 64, "half"), ("bf16", 128, 128, "interleaved")])
+def test_rotary_of_many_tokens(ctx, dtype, D, R, layout):
+    """More than 64 MiB: the version past the caches."""
+    from paper_2103_05288_amd import rotary_frequencies
+    frequencies, magnitude = rotary_frequencies(R, scaling="linear", factor=2.0)
+    h = ctx.register_rotary(dtype, D, frequencies, layout=layout, magnitude=magnitude)
+    g = _generator(77)
+    t = TYPES[dtype]
+    rows = _normal((30011, 8, D), t, g)
+    x = rows[:, 1:6]
+    y = torch.empty((30011, 5, D), dtype=t, device="cuda")
+    assert 2 * x.numel() * x.element_size() >= 64 << 20
+    positions = torch.randint(0, 1 << 17, (30011,), generator=g, device="cuda")
+    h.launch(positions, [x], [y])
+    want = plain.rotary(x, positions, frequencies, layout, magnitude)
+    _inside(y, want, _rotary_bound(x, positions, frequencies, layout, magnitude, t, want), "rotary")
+    h.launch(positions, [x], [x])
+    assert torch.equal(x, y)
+
+
 def test_rotary_positions_below_zero_and_at_rest(ctx):
     from paper_2103_05288_amd import rotary_frequencies
     frequencies, magnitude = rotary_frequencies(64)
@@ -234,6 +254,35 @@ def test_store_and_load(ctx, dtype, storage, D, kv, size, tokens):
     assert (wide[:, 0] == 9).all() and (wide[..., :5] == 9).all() and (wide[..., 5 + D:] == 9).all()
     cache.store([k[:0], v[:0]], slots[:0], stored)
     cache.load(slots[:0], stored, [back[0][:0], back[1][:0]])
+
+
+@pytest.mark.parametrize("dtype,storage", [("bf16", "i8"), ("f16", "e4m3"), ("bf16", "bf16")])
+def test_store_and_load_of_many_rows(ctx, dtype, storage):
+    """More than 64 MiB: the versions past the caches."""
+    cache = _cache(ctx, dtype, storage, 128)
+    g = _generator(4)
+    t = TYPES[dtype]
+    tokens, kv, size = 20011, 6, 32
+    rows = _normal((tokens, 2 * kv, 128), t, g, 2.0)
+    k, v = rows[:, :kv], rows[:, kv:]
+    pages = -(-tokens // size) + 1
+    slots = torch.randperm(pages * size, generator=g, device="cuda")[:tokens]
+    stored = _empty_pages(dtype, storage, pages, kv, size, 128, 0.0)
+    cache.store([k, v], slots, stored)
+    for i, x in enumerate((k, v)):
+        if storage in STORED:
+            codes, scales = plain.encode(x, storage)
+            _same(stored[i][slots // size, :, slots % size], codes, "codes")
+            _same(stored[2 + i][slots // size, :, slots % size], scales, "scales")
+        else:
+            _same(stored[i][slots // size, :, slots % size], x, "rows")
+    back = [torch.empty((tokens, kv, 128), dtype=t, device="cuda") for _ in range(2)]
+    cache.load(slots, stored, back)
+    for i, y in enumerate(back):
+        want = stored[i].float()[slots // size, :, slots % size]
+        if storage in STORED:
+            want = want * stored[2 + i][slots // size, :, slots % size][..., None]
+        _same(y, want.to(t), "rows read back")
 
 
 # ---- attention -------------------------------------------------------------------------------------
@@ -458,7 +507,24 @@ def test_attention_past_32_bits(ctx):
         assert ((a - b).abs() <= a.abs().amax(-1, keepdim=True) / 254 * 1.001 + a.abs() * 2.0 ** -8).all()
     s = {"q": _normal((2, 16, D), torch.bfloat16, g), "lengths": torch.tensor([40, 7], dtype=torch.int32, device="cuda"), "table": table,
          "pages": [k, v, ks, vs], "prefix": 0, "prefix_table": None}
-    _check(cache, "bf16", "i8", s, 1.0 / math.sqrt(D))
+    got = _check(cache, "bf16", "i8", s, 1.0 / math.sqrt(D))
+    # a table for all of it: the version that reads past the caches
+    s["table"] = torch.nn.functional.pad(table, (0, 60000), value=-1).contiguous()
+    again = _check(cache, "bf16", "i8", s, 1.0 / math.sqrt(D))
+    assert (again.double() - got.double()).abs().max() <= got.double().abs().max() * 2 * _half_step(torch.bfloat16)
+
+
+@pytest.mark.parametrize("dtype,storage,batch,size", [("bf16", "i8", 700, 64), ("f16", "e4m3", 500, 64), ("bf16", "bf16", 120, 16), ("bf16", "bf16", 300, 64)])
+def test_attention_of_large_caches(ctx, dtype, storage, batch, size):
+    """Caches of more than 128 MiB, of sequences long and short, and of so many short ones that one or two wavefronts have each."""
+    cache = _cache(ctx, dtype, storage, 128)
+    short = size == 64
+    lengths = [(37 * i) % 500 + 12 if short else (911 * i) % 3000 + 1 for i in range(batch)]
+    s = _setup(dtype, storage, 128, 4, 2, size, lengths, 0, _generator(batch))
+    s["table"] = s["table"][:, :8 if short else None].contiguous()
+    own = 2 * s["pages"][0].numel() * s["pages"][0].element_size()
+    assert min(own, batch * s["table"].shape[1] * size * 4 * 2 * 128 * s["pages"][0].element_size()) >= 128 << 20
+    _check(cache, dtype, storage, s, 1.0 / math.sqrt(128))
 
 
 def test_attention_captured_and_replayed_on_another_stream(ctx):
