@@ -49,12 +49,15 @@ constexpr int64_t kNonTemporalBytes = 64 << 20;   // from here on past the cache
 constexpr int64_t kAttendStreamBytes = 128 << 20;
 constexpr int kUnit = 128;              // tokens that a block's four wavefronts take at once
 constexpr int64_t kDirectTokens = 512;  // sequences no longer than this are one chunk each (kDirectPages of the smallest size)
-// A prefix no longer than this (or than a unit, where the query rows are few) is gone through by every sequence's own
-// block, where these run all at once: launches that join results cost more (us, joined / in line: 32 sequences of 100
-// behind 500 tokens, 32 heads, 22 / 14, 90 of 200 behind 500 31 / 26; of few rows 16 behind 128 10.7 / 7.3, but 8 behind
-// 500 12 / 14).
-constexpr int64_t kInlineTokens = 512;
-constexpr int64_t kFewRows = 64;        // query rows a kv head up to which disc_attend_k has the prefix too
+// A prefix no longer than this is gone through by every sequence's own block, where these run all at once: nothing is joined
+// then (us, joined / in line, by the bytes of a row: 128 bytes 32 sequences of 100, 8 heads, behind 300 14.9 / 11.1, behind 500
+// 15.0 / 12.1; 256 bytes behind 200 15.1 / 10.8, but 120 of 64 behind 500 15.1 / 19.9; 512 bytes behind 200 15.1 / 17.8).
+constexpr int64_t inline_tokens(int64_t row_bytes) { return row_bytes <= 128 ? 512 : row_bytes <= 256 ? 256 : 0; }
+// disc_attend_k has the prefix too, 16 query rows a block, up to so many of their units of 128 tokens: a launch less, but
+// keys and values are read, and codes brought into the operands' form, once for 16 rows and not for 256 (us, there / in
+// disc_prefix_k: 64 sequences of 32 and 8 heads x 128 behind 1000 tokens 21 / 31, behind 4000 31 / 41, 16000 59 / 53 of
+// 8-bit rows, 24 / 31, 40 / 41 and 90 / 63 of 16-bit ones, which take two products where codes take one).
+constexpr int64_t kFewUnits8 = 6144, kFewUnits16 = 4096;
 
 enum { FN_ROTARY = 0, FN_ROTARY_NT, FN_ROTARY_COUNT };
 enum { FN_STORE = 0, FN_STORE_NT, FN_LOAD, FN_LOAD_NT, FN_ATTEND, FN_ATTEND2, FN_ATTEND1, FN_ATTEND_NT, FN_PREFIX = FN_ATTEND_NT + 3, FN_JOIN, FN_CACHE_COUNT };
@@ -407,7 +410,7 @@ int plan_attend(disc_ctx* c, const Operator& o, const int64_t* d, int n_dims, At
     a.direct = 1;
     parts = batch;
   }
-  a.prefix_inline = prefix > 0 && a.direct && prefix <= (batch * a.group > kFewRows ? kInlineTokens : kUnit) && times(batch, per) <= at_once;
+  a.prefix_inline = prefix > 0 && a.direct && prefix <= inline_tokens(o.head_dim * (o.storage != DISC_STORAGE_SAME ? 1 : 2)) && times(batch, per) <= at_once;
   // Keys and values go past the caches where they are more than those keep until the next step, and one block reads
   // them (us, through them / past them: 562 MB 117 / 108, 235 MB 53 / 49, 70 MB 27.6 / 29.2).
   const int64_t own = times(std::min(d[3], times(batch, width)) << shift, kv * 2 * o.head_dim * (o.storage != DISC_STORAGE_SAME ? 1 : 2));
@@ -415,11 +418,12 @@ int plan_attend(disc_ctx* c, const Operator& o, const int64_t* d, int n_dims, At
   const int64_t rows = batch * a.group;
   int64_t prefix_blocks = 0;
   if (prefix > 0 && batch > 0 && !a.prefix_inline) {
-    const bool few = rows <= kFewRows;
+    const int64_t units = ceil_div(prefix, kUnit), tile_units = times(times(ceil_div(rows, 16), units), kv);
+    const bool few = tile_units >= 0 && tile_units <= (o.storage != DISC_STORAGE_SAME ? kFewUnits8 : kFewUnits16);
     const int64_t block_rows = few ? 16 : o.head_dim <= 128 ? 256 : 128, row_blocks = ceil_div(rows, block_rows), slots = (few ? o.resident : 1) * cus;
     // Chunks of the prefix: as many as make the shortest run, in rounds of the blocks that are there at once times the
     // units of a chunk and a block's own cost of about four.
-    const int64_t units = ceil_div(prefix, kUnit), blocks = kv * row_blocks;
+    const int64_t blocks = kv * row_blocks;
     int64_t n = 1, best = INT64_MAX;
     for (int64_t k = 1; k <= units && (k - 1) * blocks < 2 * slots; ++k) {
       const int64_t cost = ceil_div(k * blocks, slots) * (ceil_div(units, k) + 4);
