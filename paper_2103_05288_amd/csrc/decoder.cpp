@@ -260,7 +260,7 @@ int launch_rotary(disc_ctx* c, int32_t id, const int64_t* dims, int n_dims, cons
   // A token a block; where they are few, the heads are shared out too, one pass of a block's rows each.
   const int64_t rows = 256 / rotary_units(*o), passes = (most + rows - 1) / rows;
   const uint32_t y = tokens * 2 <= context_cus(c) ? (uint32_t)(passes < 64 ? passes : 64) : 1;
-  const bool nt = moved * size * 2 >= kNonTemporalBytes;
+  const bool nt = moved >= kNonTemporalBytes / (2 * size);
   OnDevice on(context_device(c));
   if (!on.ok) return refuse(c, DISC_ERR_HIP, "hipSetDevice failed");
   const int rc = enqueue(c, o->fn[nt ? FN_ROTARY_NT : FN_ROTARY], (uint64_t)tokens, y, 256, &a, sizeof a, stream);
@@ -459,7 +459,7 @@ int plan_attend(disc_ctx* c, const Operator& o, const int64_t* d, int n_dims, At
   a.join_ways = times(batch, heads) <= 4 * cus ? 4 : 1;
   p->join_blocks = alone ? 0 : ceil_div(times(batch, heads), 4 / a.join_ways);
   const int64_t partial = times(parts, heads) + times(a.prefix_parts, times(batch, heads));
-  if (p->attend_blocks < 0 || p->prefix_blocks < 0 || p->attend_blocks >= (int64_t)1 << 31 || p->prefix_blocks >= (int64_t)1 << 31 || p->join_blocks >= (int64_t)1 << 31 || times(partial, 4 * 256 + 8) < 0)
+  if (times(batch, heads) >= (int64_t)1 << 31 || p->attend_blocks < 0 || p->prefix_blocks < 0 || p->attend_blocks >= (int64_t)1 << 31 || p->prefix_blocks >= (int64_t)1 << 31 || p->join_blocks >= (int64_t)1 << 31 || times(partial, 4 * 256 + 8) < 0)
     return refuse(c, DISC_ERR_SHAPE, "too many rows for one call");
   p->workspace = batch > 0 ? (size_t)partial * ((size_t)o.head_dim * 4 + 8) : 0;
   return DISC_OK;

@@ -42,7 +42,7 @@ DISC_DEV void put(V* p, V x) {
 // A block has one token: its sines are computed once for all heads and kept in LDS, then the heads' rows stream by.
 // Bound by memory traffic (one read, one write); blocks of more tokens share nothing more and leave a longer last
 // round (us at 1, 2, 4, 8 tokens a block: 32768 x 40 x 128 bf16 121, 124, 128, 133; 16007 x 24 x 80 fp32 55, 57, 59, 64).
-// Past the caches the former takes 113 us (5.9 TB/s).
+// Past the caches they take 106 us (6.3 TB/s) and 43 us (5.8 TB/s).
 // =================================================================================================
 constexpr int kMaxTensors = 4;
 struct RotaryTensor {
@@ -314,8 +314,9 @@ extern "C" __global__ void __launch_bounds__(256) disc_load_nt_k(RowsArgs A) { l
 // d of V^T in the matrix product is then spread over eight registers of the same lane, and byte permutes
 // put it together: the values need no LDS either.
 //
-// 8-bit codes are exact in half precision and in bf16; a key's scale multiplies its score, a value's scale its probability.  Those products p * scale are taken to half precision relative to a power of two that
-// follows the largest scale seen, as the probabilities follow the largest score.
+// 8-bit codes are exact in half precision and in bf16; a key's scale multiplies its score, a value's scale its
+// probability.  Those products p * scale are taken to half precision relative to a power of two that follows the largest
+// scale seen, as the probabilities follow the largest score.
 // Where the probabilities would have no more bits than the result they are held as a sum of two 16-bit
 // numbers (hi + lo), so that the only rounding that counts is the result's.
 //
@@ -704,7 +705,7 @@ DISC_DEV void bound_step(Rows<RT>& R, f32x4 (&s)[RT][2], const float (&ks)[8], f
   float vtop = 0.f;
   if (kQuantised) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) vtop = fmaxf(vtop, vs[j]);
+    for (int j = 0; j < 8; ++j) vtop = fmaxf(vtop, fabsf(vs[j]));
     late |= vtop > R.vlim;
   }
   if (__ballot(late)) {                           // seldom after the first steps

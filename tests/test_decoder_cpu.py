@@ -261,6 +261,7 @@ def test_attention_calls(ctx, path):
     raw("table_width", "SHAPE", dims[:5] + [-1] + dims[6:])
     raw("32 bits", "SHAPE", dims[:3] + [1 << 28] + dims[4:])
     raw("negative", "SHAPE", dims[:8] + [-64] + dims[9:])
+    raw("too many rows", "SHAPE", [1 << 20, 1 << 12, 2] + dims[3:])
     raw("prefix its table", "INVALID_ARG", dims[:6] + [8, 1] + dims[8:])
     raw("null", "INVALID_ARG", i=[0] + ins[1:])
     raw("null", "INVALID_ARG", o=(0,))

@@ -418,7 +418,7 @@ def test_attention_shared_prefix_of_a_large_batch(ctx):
 
 @pytest.mark.parametrize("dtype,storage,D", [("bf16", "bf16", 128), ("bf16", "i8", 64), ("f16", "e4m3", 256), ("f16", "f16", 80)])
 @pytest.mark.parametrize("batch,kv,group,size,prefix", [(5, 1, 8, 8, 0), (5, 2, 3, 8, 77), (3, 1, 17, 64, 512), (300, 1, 2, 16, 100), (420, 2, 1, 8, 0), (900, 2, 4, 32, 0),
-                                                        (900, 2, 4, 32, 40)])
+                                                        (900, 2, 4, 32, 40), (900, 2, 4, 32, 2000), (420, 2, 4, 8, 4000)])
 def test_attention_of_short_sequences(ctx, dtype, storage, D, batch, kv, group, size, prefix):
     """Sequences of one chunk each, by four wavefronts, two or one; prefixes that are gone through in line, and shared ones."""
     cache = _cache(ctx, dtype, storage, D)
