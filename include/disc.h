@@ -471,7 +471,7 @@ int disc_cache_load(disc_ctx* ctx, int32_t id, const int64_t* dims, int n_dims, 
  * - 1 of its own (at most table_width * page_size, which is at most 2^30); token t is at place t % page_size of the
  * page table[b, t / page_size].  Entries behind the last token are not read as pages.  Tokens of an entry that is no page of
  * the cache are left out.  A sequence without any token gets zeros.  What the places behind the last token hold does
- * not matter.
+ * not matter, nor what other sequences' and heads' rows of q hold.  `out` shares no memory with an operand.
  * `workspace`: disc_cache_workspace_bytes, 16-byte aligned, free for other use once the stream has passed the launch;
  * launches that may overlap in time (two streams, two captured graphs) each need their own. */
 int disc_cache_attend(disc_ctx* ctx, int32_t id, const int64_t* dims, int n_dims, const void* const* inputs, int n_in,

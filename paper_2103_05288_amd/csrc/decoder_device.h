@@ -549,6 +549,8 @@ struct Rows {                                // RT x 16 query rows of a wavefron
   float lim[RT];                             // how far a score may pass it: kLag, or -infinity as long as there was none
   float vinv, vlim;                          // power of two that values' scales are taken relative to
   float factor;                              // on the scores: softmax scale, log2(e), and what q and the keys were scaled by
+  float row[RT];                             // ... and of this row beside that, where some row of the wavefront has one
+  u64 uneven;
 };
 struct Keys {
   u32x4 k[2][kNK];
@@ -680,6 +682,13 @@ constexpr float kNone = -__builtin_inff();
 // (or it is the first time that there are any), the reference moves up to them, and sum and result with it.
 template <int RT>
 DISC_DEV void bound_step(Rows<RT>& R, f32x4 (&s)[RT][2], const float (&ks)[8], float (&vs)[8], int live) {
+  if (R.uneven) {
+    asm volatile("");                             // (a branch, as below)
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) s[rt][j / 4][j % 4] *= R.row[rt];
+  }
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
@@ -857,6 +866,7 @@ DISC_DEV void clear_rows(Rows<RT>& R) {
   }
   R.vinv = R.vlim = 0.f;
   R.factor = (float)(DISC_SCALE_LOG2E);
+  R.uneven = 0;
 }
 
 // The query rows' operand: lane (n, g) holds row n, the elements that the keys' lanes hold of theirs.
@@ -872,36 +882,54 @@ DISC_DEV void load_query(Rows<RT>& R, int rt, const T* p) {      // p: this lane
     }
 }
 
-// bf16 queries for keys that are codes, in half precision: relative to a power of two of the largest of them all, of
-// the wavefront or of the block (`top`: their bits; NaN and infinity pass through).  What is below 2^-24 of the largest is
-// lost: of a score, 2^-25 of the largest |q| times the sum of |k|, less than what its sum of D products is rounded by.
+// bf16 queries for keys that are codes, in half precision: 2^15 is the power of two of the largest of them all, of the
+// wavefront or of the block (`most`: its bits).  What is below 2^-39 of it is lost, and a row of 2^-16 of it has an error
+// of 2^-24 of its own largest: of a score, 2^-24 of the row's largest |q| times the sum of |k|, as much as its sum of D
+// products is rounded by.  A row that is smaller still has a power of two of its own, so that nothing another sequence or
+// head brings along takes its bits; rows that hold a NaN or an infinity are not asked for theirs, and keep them.
 template <int RT>
-DISC_DEV u32 largest_query(const Rows<RT>& R) {               // bits of |q|, of this lane
-  u32 top = 0;
+DISC_DEV u32 largest_queries(const Rows<RT>& R, u32 (&top)[RT]) {     // bits of |q|: of this lane's rows, of all finite ones
+  u32 most = 0;
 #pragma unroll
-  for (int rt = 0; rt < RT; ++rt)
+  for (int rt = 0; rt < RT; ++rt) {
+    top[rt] = 0;
 #pragma unroll
     for (int i = 0; i < kNK * (kKE / 8); ++i)
 #pragma unroll
-      for (int w = 0; w < 4; ++w) top = max(top, max(R.q[rt][i][w] & 0x7fffu, (R.q[rt][i][w] >> 16) & 0x7fffu));
-  return top;
+      for (int w = 0; w < 4; ++w) top[rt] = max(top[rt], max(R.q[rt][i][w] & 0x7fffu, (R.q[rt][i][w] >> 16) & 0x7fffu));
+    top[rt] = max(top[rt], (u32)__shfl_xor((int)top[rt], 16));
+    top[rt] = max(top[rt], (u32)__shfl_xor((int)top[rt], 32));
+    if (top[rt] < 0x7f80u) most = max(most, top[rt]);
+  }
+#pragma unroll
+  for (int d = 1; d < 16; d *= 2) most = max(most, (u32)__shfl_xor((int)most, d));
+  return most;
 }
 template <int RT>
-DISC_DEV void halve_query(Rows<RT>& R, u32 top) {
+DISC_DEV void halve_query(Rows<RT>& R, const u32 (&top)[RT], u32 most) {
 #if !DISC_T_F16
-  // (biased exponent of the largest; 0 and infinity have 1 and 254 for theirs)
-  const int e = min(max((int)(top >> 7), 1), 254);
-  const float down = __builtin_bit_cast(float, (u32)max(254 - e, 1) << 23);     // 2^(127 - e)
+  // (by biased exponents: the largest one's, which 0 has none of; 2^(142 - e), or the largest there is)
+  const auto down_of = [](int e) { return __builtin_bit_cast(float, (u32)min(269 - e, 254) << 23); };
+  const int e = max((int)(most >> 7), 1);
+  const float down = down_of(e);
+  bool uneven = false;
 #pragma unroll
-  for (int rt = 0; rt < RT; ++rt)
+  for (int rt = 0; rt < RT; ++rt) {
+    const int own = (int)(top[rt] >> 7);
+    const bool apart = top[rt] != 0 && own + 16 < e;
+    const float own_down = apart ? down_of(max(own, 1)) : down;
+    R.row[rt] = down / own_down;
+    uneven |= apart;
 #pragma unroll
     for (int i = 0; i < kNK * (kKE / 8); ++i)
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
         const u32 x = R.q[rt][i][w];
-        const f16x2 y = {(_Float16)(__builtin_bit_cast(float, x << 16) * down), (_Float16)(__builtin_bit_cast(float, x & 0xffff0000u) * down)};
+        const f16x2 y = {(_Float16)(__builtin_bit_cast(float, x << 16) * own_down), (_Float16)(__builtin_bit_cast(float, x & 0xffff0000u) * own_down)};
         R.q[rt][i][w] = __builtin_bit_cast(u32, y);
       }
+  }
+  R.uneven = __ballot(uneven);
   R.factor *= 1.f / down;
 #endif
   R.factor *= 1.f / kCode;
@@ -1012,10 +1040,9 @@ DISC_DEV void attend_body(const AttendArgs& A) {
     clear_rows<1>(R);
     load_query<1>(R, 0, n < rows ? A.q + b * A.q_row + head * A.q_head : nullptr);
     if (kQuantised && (!kNt || DISC_T_F16)) {
-      u32 top = largest_query<1>(R);
-#pragma unroll
-      for (int d = 1; d < 64; d *= 2) top = max(top, (u32)__shfl_xor((int)top, d));
-      halve_query<1>(R, top);
+      u32 top[1];
+      const u32 largest = largest_queries<1>(R, top);
+      halve_query<1>(R, top, largest);
     }
     const int most = kMostPages << A.shift;
     bool ahead = kWays == 4 && A.prefix_inline;                // the prefix, in front of the sequence's own
@@ -1120,14 +1147,12 @@ extern "C" __global__ void __launch_bounds__(512, 2) disc_prefix_k(AttendArgs A)
     load_query<kPrefixRT>(R, rt, row < all ? A.q + b * A.q_row + (h * A.group + i) * A.q_head : nullptr);
   }
   if (kQuantised) {                                           // (one power of two for the block: its keys' scales are shared)
-    u32 top = largest_query<kPrefixRT>(R);
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) top = max(top, (u32)__shfl_xor((int)top, d));
-    tops[w] = top;
+    u32 top[kPrefixRT], largest = largest_queries<kPrefixRT>(R, top);
+    tops[w] = largest;
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < 8; ++i) top = max(top, tops[i]);
-    halve_query<kPrefixRT>(R, top);
+    for (int i = 0; i < 8; ++i) largest = max(largest, tops[i]);
+    halve_query<kPrefixRT>(R, top, largest);
   }
   const bool keys = w < kPrefixSteps, values = !keys && w < 2 * kPrefixSteps;
   const int step = keys ? w : w - kPrefixSteps;               // this wavefront's share of a tile

@@ -407,6 +407,39 @@ def test_attention_of_one_long_sequence(ctx, storage):
     del q
 
 
+@pytest.mark.parametrize("dtype,storage,D", [("bf16", "i8", 128), ("bf16", "e4m3", 64), ("f16", "i8", 64), ("bf16", "bf16", 128)])
+@pytest.mark.parametrize("batch,group,prefix,longest", [(3, 4, 0, 300), (2, 4, 0, 3000), (600, 2, 0, 40), (5, 4, 200, 40), (40, 4, 1500, 40), (300, 4, 2500, 40)])
+def test_queries_of_other_rows_change_nothing(ctx, dtype, storage, D, batch, group, prefix, longest):
+    """Query rows that hold NaN, infinities, the largest and the smallest numbers (a padded batch's rows may hold anything) beside
+    ordinary ones: the ordinary ones' results are as without them."""
+    cache = _cache(ctx, dtype, storage, D)
+    lengths = [int(x) for x in torch.randint(1, longest, (batch,), generator=torch.Generator().manual_seed(3))]
+    s = _setup(dtype, storage, D, 2, group, 16, lengths, prefix, _generator(17 + batch))
+    q, plain_rows = s["q"], s["q"].clone()
+    most = torch.finfo(q.dtype).max
+    odd = torch.zeros(q.shape[:2], dtype=torch.bool, device="cuda")
+    # (heads 1 of every kv head: beside ordinary rows of their sequence; and whole sequences beside other sequences)
+    for at, value in ((0, most), (1, math.nan)):
+        q[at, 1::group] = value
+        odd[at, 1::group] = True
+    q[batch - 1] = math.inf
+    odd[batch - 1] = True
+    got = _run(cache, s)[0]
+    s["q"] = plain_rows
+    want, *sizes = plain.attend(s["q"], s["lengths"], s["table"], s["pages"], 1.0 / math.sqrt(D), s["prefix_table"], s["prefix"])
+    bound = _attend_bound(dtype, storage, s, want, *sizes, 1.0 / math.sqrt(D))
+    _inside(got[~odd], want[~odd], bound[~odd], f"attention {dtype} {storage} beside other rows")
+    # rows far smaller than their neighbours: what they turn to still counts
+    if dtype == "bf16":
+        s["q"] = plain_rows.clone()
+        s["q"][0, 1::group] *= 2.0 ** 60
+        s["q"][1] *= 2.0 ** -40
+        scale_up = ctx.register_cache(dtype, D, storage, softmax_scale=2.0 ** 40 / math.sqrt(D))
+        got = _run(scale_up, s)[0]
+        s["q"] = plain_rows
+        _inside(got[1], want[1], bound[1], f"attention {dtype} {storage}, rows of 2^-100 of others")
+
+
 def test_attention_shared_prefix_of_a_large_batch(ctx):
     cache = _cache(ctx, "bf16", "i8", 128)
     g = _generator(8)
