@@ -196,7 +196,7 @@ int register_rotary(disc_ctx* c, const disc_rotary_desc* d, int32_t* id_out) {
   if (d->rotary_dim < 2 || d->rotary_dim > d->head_dim || d->rotary_dim % 2)
     return refuse(c, DISC_ERR_SHAPE, "rotary_dim is even, 2 .. head_dim", d->rotary_dim);
   if (d->layout != DISC_ROTARY_HALF && d->layout != DISC_ROTARY_INTERLEAVED) return refuse(c, DISC_ERR_INVALID_ARG, "bad rotary layout");
-  if (!std::isfinite(d->magnitude)) return refuse(c, DISC_ERR_INVALID_ARG, "magnitude is not finite");
+  if (!std::isfinite((float)d->magnitude)) return refuse(c, DISC_ERR_INVALID_ARG, "magnitude is no finite number of 32 bits");
   std::string macros = "#define DISC_ROTARY 1\n";
   macros += std::string("#define DISC_T ") + dtype_ctype(d->dtype) + "\n";
   macros += "#define DISC_D " + std::to_string(d->head_dim) + "\n#define DISC_R " + std::to_string(d->rotary_dim) + "\n";
@@ -276,7 +276,8 @@ int register_cache(disc_ctx* c, const disc_cache_desc* d, int32_t* id_out) {
   if (d->dtype != DISC_F16 && d->dtype != DISC_BF16) return refuse(c, DISC_ERR_INVALID_ARG, "a cache takes f16 or bf16 rows");
   if (d->storage < DISC_STORAGE_SAME || d->storage > DISC_STORAGE_E4M3) return refuse(c, DISC_ERR_INVALID_ARG, "bad storage");
   if (d->head_dim < 16 || d->head_dim > 256 || d->head_dim % 16) return refuse(c, DISC_ERR_SHAPE, "head_dim is a multiple of 16, 16 .. 256", d->head_dim);
-  if (!std::isfinite(d->softmax_scale)) return refuse(c, DISC_ERR_INVALID_ARG, "softmax_scale is not finite");
+  if (!std::isfinite((float)(d->softmax_scale * 1.44269504088896340736)))
+    return refuse(c, DISC_ERR_INVALID_ARG, "softmax_scale is no finite number of 32 bits");
   const double scale = d->softmax_scale != 0.0 ? d->softmax_scale : 1.0 / std::sqrt((double)d->head_dim);
   std::string macros = "#define DISC_CACHE 1\n#define DISC_T_F16 " + std::to_string(d->dtype == DISC_F16 ? 1 : 0) + "\n";
   macros += "#define DISC_STORAGE " + std::to_string(d->storage) + "\n#define DISC_D " + std::to_string(d->head_dim) + "\n";
@@ -423,13 +424,14 @@ int plan_attend(disc_ctx* c, const Operator& o, const int64_t* d, int n_dims, At
     const int64_t block_rows = few ? 16 : o.head_dim <= 128 ? 256 : 128, row_blocks = ceil_div(rows, block_rows), slots = (few ? o.resident : 1) * cus;
     // Chunks of the prefix: as many as make the shortest run, in rounds of the blocks that are there at once times the
     // units of a chunk and a block's own cost of about four.
-    const int64_t blocks = kv * row_blocks;
-    int64_t n = 1, best = INT64_MAX;
-    for (int64_t k = 1; k <= units && (k - 1) * blocks < 2 * slots; ++k) {
-      const int64_t cost = ceil_div(k * blocks, slots) * (ceil_div(units, k) + 4);
-      if (cost < best) best = cost, n = k;
+    // (Of the rounds that one chunk takes, or one more, the most chunks that fit; nothing is gained where those are many.)
+    const int64_t blocks = kv * row_blocks, rounds = ceil_div(blocks, slots);
+    int64_t units_each = units, best = rounds * (units + 4);
+    for (int64_t r = rounds; r <= rounds + 1 && r <= 3; ++r) {
+      const int64_t each = ceil_div(units, std::min(units, r * slots / blocks)), cost = r * (each + 4);
+      if (cost < best) best = cost, units_each = each;
     }
-    int64_t chunk = ceil_div(units, n) * kUnit;
+    int64_t chunk = units_each * kUnit;
     const int64_t most = (int64_t)kMostPages << shift;
     chunk = chunk > most ? most : chunk;
     a.prefix_chunk = (int32_t)chunk;

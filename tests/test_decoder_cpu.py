@@ -76,6 +76,9 @@ def test_registrations_that_are_refused(ctx):
         _refused("SHAPE", "head_dim", lambda: ctx.register_cache("bf16", D, "i8"))
     _refused("INVALID_ARG", "softmax", lambda: ctx.register_cache("bf16", 64, softmax_scale=0))
     _refused("INVALID_ARG", "softmax", lambda: ctx.register_cache("bf16", 64, softmax_scale=math.nan))
+    # finite in 64 bits, not in the 32 that the kernels have
+    _refused("INVALID_ARG", "softmax", lambda: ctx.register_cache("bf16", 64, softmax_scale=3e38))
+    _refused("INVALID_ARG", "magnitude", lambda: ctx.register_rotary("f32", 64, f, magnitude=1e39))
     lib, out = ctx.lib, C.c_int32(5)
     assert lib.disc_register_cache(ctx.h, None, C.byref(out)) == -1 and lib.disc_register_rotary(ctx.h, None, C.byref(out)) == -1
     assert lib.disc_register_cache(None, None, C.byref(out)) == -1 and out.value == 5
