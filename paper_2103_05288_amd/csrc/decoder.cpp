@@ -405,8 +405,9 @@ int plan_attend(disc_ctx* c, const Operator& o, const int64_t* d, int n_dims, At
   const int64_t at_once = cus * o.resident;
   a.target = (int32_t)(at_once / per > 1 ? at_once / per : 1);
   int64_t parts = batch + a.target;
-  // (of heads above 128 a step of four wavefronts takes three times as long: there, few blocks are more than joins cost)
-  const int64_t direct_tokens = o.head_dim <= 128 || times(batch, per) >= cus ? kDirectTokens : kUnit;
+  // (16-bit rows above 128: where the blocks are few, two steps more cost more than the join, 8 blocks of 500 tokens x 256
+  // 15.5 us joined / 18.4 as one chunk each, 16 17.0 / 18.2, 120 25.5 / 19.7; 8-bit ones 15.5 / 15.0, 16.2 / 14.9, 19.8 / 15.4)
+  const int64_t direct_tokens = o.head_dim <= 128 || o.storage != DISC_STORAGE_SAME || times(batch, per) >= cus / 4 ? kDirectTokens : kDirectTokens / 2;
   if ((width << shift) <= direct_tokens) {
     a.direct = 1;
     parts = batch;

@@ -1327,6 +1327,19 @@ extern "C" __global__ void __launch_bounds__(256) disc_join_k(AttendArgs A) {
     const int i = i0 + lane * ways;
     const i64 at = i < count ? part_row(A, chunk + i, head) : prefix_row(A, min(i, n - 1) - count, b, head);
     const float pm = i < n ? A.part_m[2 * at] : kNone, pl = i < n ? A.part_m[2 * at + 1] : 0.f;
+    const int most = min(64, (n - i0 + ways - 1) / ways);
+    float v[8][kPer];
+    auto read = [&](int x0) {
+#pragma unroll
+      for (int x = 0; x < 8; ++x) {                           // (the last one again, with a weight of 0, behind the end)
+        const int j = i0 + min(x0 + x, most - 1) * ways;
+        const i64 slot = j < count ? part_row(A, chunk + j, head) : prefix_row(A, j - count, b, head);
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) v[x][e] = e * 64 + lane < kD ? A.part[slot * kD + e * 64 + lane] : 0.f;
+      }
+    };
+    read(0);                                                  // (on their way while the weights are formed)
+    __builtin_amdgcn_sched_barrier(0);
     float top = fmaxf(m, pm);
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
@@ -1340,16 +1353,8 @@ extern "C" __global__ void __launch_bounds__(256) disc_join_k(AttendArgs A) {
     m = top;
 #pragma unroll
     for (int e = 0; e < kPer; ++e) o[e] *= before;
-    const int most = min(64, (n - i0 + ways - 1) / ways);
     for (int x0 = 0; x0 < most; x0 += 8) {
-      float v[8][kPer];
-#pragma unroll
-      for (int x = 0; x < 8; ++x) {                           // (the last one again, with a weight of 0, behind the end)
-        const int j = i0 + min(x0 + x, most - 1) * ways;
-        const i64 slot = j < count ? part_row(A, chunk + j, head) : prefix_row(A, j - count, b, head);
-#pragma unroll
-        for (int e = 0; e < kPer; ++e) v[x][e] = e * 64 + lane < kD ? A.part[slot * kD + e * 64 + lane] : 0.f;
-      }
+      if (x0) read(x0);
 #pragma unroll
       for (int x = 0; x < 8; ++x) {
         const float fx = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, f), min(x0 + x, 63)));
