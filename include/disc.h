@@ -246,7 +246,7 @@ typedef struct {
   int64_t patterns_registered;  /* distinct patterns                                           */
   int64_t pattern_cache_hits;   /* re-registrations answered from the pattern cache            */
   int64_t compile_events;       /* device compiles, all patterns                               */
-  int64_t launch_calls;         /* successful disc_launch calls                                */
+  int64_t launch_calls;         /* successful launches of patterns and operators                */
   int64_t device_launches;      /* kernels enqueued                                            */
   int64_t variant_count[DISC_V_COUNT];
   int64_t host_plan_ns;         /* total wall time in shape calculation + selection            */
@@ -462,7 +462,7 @@ int disc_cache_store(disc_ctx* ctx, int32_t id, const int64_t* dims, int n_dims,
 int disc_cache_load(disc_ctx* ctx, int32_t id, const int64_t* dims, int n_dims, const void* const* inputs, int n_in,
                     void* const* outputs, int n_out, void* workspace, size_t workspace_bytes, void* hip_stream);
 /* disc_cache_attend: out[b, h] = sum_t p_t v_t / sum_t p_t, p_t = exp(softmax_scale * q[b, h].k_t), over the tokens of a
- * prefix that all sequences share (read once for the batch, not once a sequence) and of the sequence's own pages; query
+ * prefix that all sequences share (their query rows go through it together; a short one, every sequence) and of the sequence's own pages; query
  * head h reads kv head h / (q_heads / kv_heads).  One query token a sequence.
  * dims = {batch, q_heads, kv_heads, pages, page_size, table_width, prefix_length, prefix_width, sequence stride, head
  * stride of q, sequence stride, head stride of out}.  inputs = {q [batch, q_heads, head_dim], lengths int32 [batch],

@@ -294,7 +294,8 @@ DISC_DEV void load_body(const RowsArgs& A) {
     put<kNt>((u32x4_u*)(to + lane * 8), (u32x4_u)y);
   }
 }
-// (past the caches in large calls: 40009 x 8 x 128 bf16 to e4m3 49.4 -> 45.0 us, 65536 x 8 x 128 from i8 89 -> 80.7, 5.0 TB/s)
+// Bound by memory traffic, small calls by their launch.  (Past the caches in large calls: 40009 x 8 x 128 bf16 to e4m3 49 -> 47
+// us, 65536 x 8 x 128 from i8 89 -> 80.5, both 5.0 TB/s.)
 extern "C" __global__ void __launch_bounds__(256) disc_store_k(RowsArgs A) { store_body<false>(A); }
 extern "C" __global__ void __launch_bounds__(256) disc_store_nt_k(RowsArgs A) { store_body<true>(A); }
 extern "C" __global__ void __launch_bounds__(256) disc_load_k(RowsArgs A) { load_body<false>(A); }
@@ -322,6 +323,10 @@ extern "C" __global__ void __launch_bounds__(256) disc_load_nt_k(RowsArgs A) { l
 //
 // A block is four wavefronts; they take the steps of a stretch of tokens in turn and join in LDS at its end.
 // The stretches are cut from the lengths, on the device, so that all blocks have the same share.
+//
+// Long caches are bound by their reads: 64 sequences of up to 8192 tokens (8 kv heads of 128, i8) 108 us, 5.2 TB/s; two of
+// 131072 (bf16) 127 us.  Short ones by the chain lengths -> page table -> first rows -> joins, about 5 us, and by the joining
+// launch, 4 to 8 us: one sequence of 300 6.5 us, four of 4000 17.
 // =================================================================================================
 constexpr int kStep = 32;                     // tokens of a step
 constexpr int kMostPages = 1024;              // pages of a stretch that are kept in LDS at a time
@@ -1117,7 +1122,9 @@ DISC_ATTEND(disc_attend1_nt_k, 1, true)
 // has 16 x RT rows of its own, and all go through the same tokens.  A tile of them is read once a block, brought into
 // the matrix operands' form -- codes to 16-bit numbers, values transposed -- and kept in LDS in the order in which a
 // wavefront reads an operand (16 bytes a lane, one row after the other); the next tile's loads are in flight
-// meanwhile, and two tiles take turns.
+// meanwhile, and two tiles take turns.  1024 rows x 16384 tokens x 8 heads of 128, i8: 93 to 96 us, 0.73 PFLOP/s.  Bound by
+// issue: the matrix cores are busy for 30 % of the cycles, the vector ALU for 47 % (sixteen powers of two at a quarter of
+// the rate, and what goes round them, a step), little of it at once; wavefronts wait for 30 % of their time.
 constexpr int kPrefixRT = kD <= 128 ? 2 : 1;
 constexpr int kPrefixSteps = kD <= 128 ? 4 : 2;               // steps of a tile
 constexpr int kNF = kNK * (kKE / 8);                          // operands of a step's keys, a 16-row tile
@@ -1304,7 +1311,8 @@ extern "C" __global__ void __launch_bounds__(512, 2) disc_prefix_k(AttendArgs A)
 
 // Joins the chunks of a sequence and of the prefix, for a (sequence, query head) a wavefront, or where the rows are few
 // and their chunks many, a block.  The chunks' maxima and sums are read 64 at a time, a lane each, so that the reads
-// of the results themselves do not wait for each other.
+// of the results themselves do not wait for each other.  A chain of trips to memory, 4 to 8 us: more wavefronts a row do not
+// shorten it (sixteen 8.2 us where four take 7.1).
 extern "C" __global__ void __launch_bounds__(256) disc_join_k(AttendArgs A) {
   __shared__ float so[4][kD], sm[4], sl[4];
   const int w = wavefront(), lane = threadIdx.x & 63, ways = A.join_ways;
