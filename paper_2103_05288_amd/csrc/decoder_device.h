@@ -730,10 +730,9 @@ DISC_DEV void bound_step(Rows<RT>& R, f32x4 (&s)[RT][2], const float (&ks)[8], f
         int e;
         (void)__builtin_frexpf(v, &e);
         e = e < -100 ? -100 : e;
-        const float vinv = __builtin_ldexpf(1.f, -e);
-        vscale = R.vinv > 0.f ? vinv / R.vinv : 0.f;
-        R.vinv = vinv;
-        R.vlim = 8.f / vinv;
+        R.vinv = __builtin_ldexpf(1.f, -e);
+        vscale = R.vinv * R.vlim * 0.125f;        // (powers of two; 0 where there was none)
+        R.vlim = __builtin_ldexpf(8.f, e);
       }
     }
 #pragma unroll
@@ -744,9 +743,12 @@ DISC_DEV void bound_step(Rows<RT>& R, f32x4 (&s)[RT][2], const float (&ks)[8], f
       const float alpha = first ? 0.f : __builtin_amdgcn_exp2f(-shift);
       R.use[rt] += shift;
       R.lim[rt] = t > kNone ? kLag : R.lim[rt];
-      R.l[rt] *= alpha;
+      if (__ballot(!first)) {                     // (nothing was summed before the first time)
+        asm volatile("");
+        R.l[rt] *= alpha;
 #pragma unroll
-      for (int d = 0; d < kND; ++d) R.o[rt][d] *= alpha * vscale;
+        for (int d = 0; d < kND; ++d) R.o[rt][d] *= alpha * vscale;
+      }
 #pragma unroll
       for (int j = 0; j < 8; ++j) s[rt][j / 4][j % 4] -= shift;
     }
@@ -1068,7 +1070,7 @@ DISC_DEV void attend_body(const AttendArgs& A) {
     R.l[0] += __shfl_xor(R.l[0], 16);
     R.l[0] += __shfl_xor(R.l[0], 32);
     if (kQuantised) {
-      const float f = R.vinv > 0.f ? 1.f / (R.vinv * kCode) : 0.f;
+      const float f = R.vlim * (0.125f / kCode);
 #pragma unroll
       for (int d = 0; d < kND; ++d) R.o[0][d] *= f;
     }
@@ -1084,7 +1086,8 @@ DISC_DEV void attend_body(const AttendArgs& A) {
     }
     if (turn == 0 && n < rows) {
       const bool alone = I.whole && A.prefix_parts == 0;
-      const float l = R.l[0];
+      // (the sum is 1 or more where it is not 0: its reciprocal is rounded to 32 bits, of which the result keeps 11 at most)
+      const float l = R.l[0], inverse = 1.f / l;
       const i64 at = shared ? prefix_row(A, part, b, head) : part_row(A, A.direct ? b : part + b, head);
       T* out = A.out + b * A.o_row + head * A.o_head;
 #pragma unroll
@@ -1096,7 +1099,7 @@ DISC_DEV void attend_body(const AttendArgs& A) {
 #pragma unroll
           for (int e = 0; e < kE; e += 4) {
             const f32x4 o = {R.o[0][x * kE + e][r], R.o[0][x * kE + e + 1][r], R.o[0][x * kE + e + 2][r], R.o[0][x * kE + e + 3][r]};
-            if (alone) store4(out + d + e, l != 0.f ? o / l : (f32x4){0, 0, 0, 0});
+            if (alone) store4(out + d + e, l != 0.f ? o * inverse : (f32x4){0, 0, 0, 0});
             else *(f32x4*)(A.part + at * kD + d + e) = o;
           }
         }
