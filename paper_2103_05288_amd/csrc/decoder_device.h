@@ -967,29 +967,28 @@ DISC_DEV i64 prefix_row(const AttendArgs& A, int part, int b, int head) {
   return (i64)A.parts * A.heads + ((i64)part * A.batch + b) * A.heads + head;
 }
 
-// What two wavefronts have of the same rows, put together: the other one's registers, lane for lane, through LDS.
+// What wavefronts have of the same rows, put together: each leaves its registers in LDS, four neighbouring elements of the
+// result (register r of four tiles) a piece, and finishes a share of the registers r of all of them.
+constexpr int kPieces = kND / 4;
+static_assert(kND % 4 == 0 && kE % 4 == 0, "a piece is of one group of tiles");
 struct Other {
-  f32x4 o[kND][64];
+  f32x4 o[4][kPieces][64];
   float use[64], l[64];                       // use: -infinity where there was no score
 };
 DISC_DEV float reference(const Rows<1>& R) { return R.lim[0] > kNone ? R.use[0] : kNone; }
 // (no reference: the sum is 0, or NaN where every score was)
 DISC_DEV float weight(float use, float top, float l) { return use > kNone ? __builtin_amdgcn_exp2f(use - top) : l; }
+DISC_DEV f32x4 piece_of(const Rows<1>& R, int r, int q) {
+  return (f32x4){R.o[0][4 * q][r], R.o[0][4 * q + 1][r], R.o[0][4 * q + 2][r], R.o[0][4 * q + 3][r]};
+}
 DISC_DEV void hand_over(const Rows<1>& R, Other& X) {
   const int lane = threadIdx.x & 63;
 #pragma unroll
-  for (int d = 0; d < kND; ++d) X.o[d][lane] = R.o[0][d];
+  for (int r = 0; r < 4; ++r)
+#pragma unroll
+    for (int q = 0; q < kPieces; ++q) X.o[r][q][lane] = piece_of(R, r, q);
   X.use[lane] = reference(R);
   X.l[lane] = R.l[0];
-}
-DISC_DEV void take_over(Rows<1>& R, const Other& X) {
-  const int lane = threadIdx.x & 63;
-  const float use = reference(R), also = X.use[lane], top = fmaxf(use, also), fa = weight(use, top, R.l[0]), fb = weight(also, top, X.l[lane]);
-#pragma unroll
-  for (int d = 0; d < kND; ++d) R.o[0][d] = R.o[0][d] * fa + X.o[d][lane] * fb;
-  R.l[0] = (use > kNone ? R.l[0] * fa : R.l[0]) + (also > kNone ? X.l[lane] * fb : X.l[lane]);
-  R.use[0] = top;
-  R.lim[0] = top > kNone ? kLag : kNone;
 }
 
 // `kWays` wavefronts work on the same rows, 4 / kWays rows sets a block.
@@ -1000,7 +999,7 @@ template <int kWays, bool kNt>
 DISC_DEV void attend_body(const AttendArgs& A) {
   constexpr int kSets = 4 / kWays, kIds = kWays == 4 ? kMostPages + 1 : kDirectPages;   // (a stretch need not begin with a page)
   __shared__ u32 all_pages[kSets][kIds];
-  __shared__ Other other[kWays == 1 ? 1 : 2];
+  __shared__ Other other[kWays == 1 ? 1 : 4];
   __shared__ __align__(16) float scales[4][64];
   const int w = wavefront(), n = threadIdx.x & 15, set = w / kWays, turn = w % kWays;
   u32* pages = all_pages[set];
@@ -1074,36 +1073,53 @@ DISC_DEV void attend_body(const AttendArgs& A) {
 #pragma unroll
       for (int d = 0; d < kND; ++d) R.o[0][d] *= f;
     }
-    if (kWays > 1) {
-      if (turn & 1) hand_over(R, other[w >> 1]);
+    // register r of this wavefront's share, of all that work on these rows
+    constexpr int kShare = 4 / kWays;
+    f32x4 done[kShare][kPieces];
+    float top = reference(R), l = R.l[0];
+    if (kWays == 1) {
+#pragma unroll
+      for (int i = 0; i < kShare; ++i)
+#pragma unroll
+        for (int q = 0; q < kPieces; ++q) done[i][q] = piece_of(R, i, q);
+    } else {
+      const int lane = threadIdx.x & 63;
+      hand_over(R, other[w]);
       __syncthreads();
-      if (!(turn & 1)) take_over(R, other[w >> 1]);
+      const Other* all = other + set * kWays;
+      float use[kWays], sum[kWays];
+#pragma unroll
+      for (int i = 0; i < kWays; ++i) use[i] = all[i].use[lane], sum[i] = all[i].l[lane], top = fmaxf(top, use[i]);
+      l = 0.f;
+#pragma unroll
+      for (int i = 0; i < kWays; ++i) {
+        const float f = weight(use[i], top, sum[i]);
+        l += use[i] > kNone ? sum[i] * f : sum[i];
+#pragma unroll
+        for (int j = 0; j < kShare; ++j)
+#pragma unroll
+          for (int q = 0; q < kPieces; ++q) {
+            const f32x4 o = all[i].o[turn + j * kWays][q][lane] * f;
+            done[j][q] = i ? done[j][q] + o : o;
+          }
+      }
     }
-    if (kWays > 2) {
-      if (turn == 2) hand_over(R, other[1]);
-      __syncthreads();
-      if (turn == 0) take_over(R, other[1]);
-    }
-    if (turn == 0 && n < rows) {
+    if (n < rows) {
       const bool alone = I.whole && A.prefix_parts == 0;
       // (the sum is 1 or more where it is not 0: its reciprocal is rounded to 32 bits, of which the result keeps 11 at most)
-      const float l = R.l[0], inverse = 1.f / l;
+      const float inverse = 1.f / l;
       const i64 at = shared ? prefix_row(A, part, b, head) : part_row(A, A.direct ? b : part + b, head);
       T* out = A.out + b * A.o_row + head * A.o_head;
 #pragma unroll
-      for (int x = 0; x < kNB; ++x)
+      for (int q = 0; q < kPieces; ++q)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int d = element_of(x, 0, r);
+        for (int j = 0; j < kShare; ++j) {
+          const int d = element_of(q / (kE / 4), q % (kE / 4) * 4, turn + j * kWays);
           if (d >= kD) continue;
-#pragma unroll
-          for (int e = 0; e < kE; e += 4) {
-            const f32x4 o = {R.o[0][x * kE + e][r], R.o[0][x * kE + e + 1][r], R.o[0][x * kE + e + 2][r], R.o[0][x * kE + e + 3][r]};
-            if (alone) store4(out + d + e, l != 0.f ? o * inverse : (f32x4){0, 0, 0, 0});
-            else *(f32x4*)(A.part + at * kD + d + e) = o;
-          }
+          if (alone) store4(out + d, l != 0.f ? done[j][q] * inverse : (f32x4){0, 0, 0, 0});
+          else *(f32x4*)(A.part + at * kD + d) = done[j][q];
         }
-      if (!alone && (threadIdx.x & 63) < 16) A.part_m[2 * at] = reference(R), A.part_m[2 * at + 1] = l;
+      if (!alone && turn == 0 && (threadIdx.x & 63) < 16) A.part_m[2 * at] = top, A.part_m[2 * at + 1] = l;
     }
     if (kWays < 4 || shared || A.direct || !I.next(A)) return;
     __syncthreads();                      // (what was handed over is still being read)
