@@ -1126,8 +1126,9 @@ DISC_DEV void attend_body(const AttendArgs& A) {
   }
 }
 // (wavefronts a SIMD by the registers that they take; 16-bit rows of 256 do not fit 256: 31 spilled ones cost 60 us where one
-// wavefront takes 36, four sequences of 15000)
-constexpr int kWavesPerSimd = kD <= 64 ? 4 : kD <= 128 ? 3 : kQuantised ? 2 : 1;
+// wavefront takes 36, four sequences of 15000; heads of up to 48 have the tiles of 128, three wavefronts and none spilled 39 us,
+// four 52, 64 sequences of 4000 x 32)
+constexpr int kWavesPerSimd = kD <= 64 && kND <= 4 ? 4 : kD <= 128 ? 3 : kQuantised ? 2 : 1;
 #define DISC_ATTEND(NAME, WAYS, NT) \
   extern "C" __global__ void __launch_bounds__(256, kWavesPerSimd) NAME(AttendArgs A) { attend_body<WAYS, NT>(A); }
 DISC_ATTEND(disc_attend_k, 4, false)
