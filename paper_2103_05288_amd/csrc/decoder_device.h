@@ -324,9 +324,9 @@ extern "C" __global__ void __launch_bounds__(256) disc_load_nt_k(RowsArgs A) { l
 // A block is four wavefronts; they take the steps of a stretch of tokens in turn and join in LDS at its end.
 // The stretches are cut from the lengths, on the device, so that all blocks have the same share.
 //
-// Long caches are bound by their reads: 64 sequences of up to 8192 tokens (8 kv heads of 128, i8) 108 us, 5.2 TB/s; two of
-// 131072 (bf16) 127 us.  Short ones by the chain lengths -> page table -> first rows -> joins, about 5 us, and by the joining
-// launch, 4 to 8 us: one sequence of 300 6.5 us, four of 4000 17.
+// Long caches are bound by their reads: 64 sequences of up to 8192 tokens (8 kv heads of 128, i8) 107 us, 5.3 TB/s; two of
+// 131072 (bf16) 117 us, 5.7 TB/s.  Short ones by the chain lengths -> page table -> first rows -> end, about 5 us, and by the
+// joining launch, 4 to 8 us: one sequence of 300 5.9 us, four of 4000 17.
 // =================================================================================================
 constexpr int kStep = 32;                     // tokens of a step
 constexpr int kMostPages = 1024;              // pages of a stretch that are kept in LDS at a time
@@ -968,7 +968,8 @@ DISC_DEV i64 prefix_row(const AttendArgs& A, int part, int b, int head) {
 }
 
 // What wavefronts have of the same rows, put together: each leaves its registers in LDS, four neighbouring elements of the
-// result (register r of four tiles) a piece, and finishes a share of the registers r of all of them.
+// result (register r of four tiles) a piece, and finishes a share of the registers r of all of them.  (Two and two, then the
+// two, with one of them finishing all: eight sequences of 100 x 256 elements 9.2 us where this takes 8.3.)
 constexpr int kPieces = kND / 4;
 static_assert(kND % 4 == 0 && kE % 4 == 0, "a piece is of one group of tiles");
 struct Other {
