@@ -354,8 +354,8 @@ struct AttendArgs {
   const float* vs;
   const int* prefix_table;
   T* out;
-  float* part;              // unnormalised results [part][heads of q of the kv heads][D]
-  float* part_m;            // their running maximum and sum, two floats a row
+  float* part;              // results of the chunks [part][heads of q of the kv heads][D], as if there were no others
+  float* part_m;            // their reference (-infinity where there was no score) and sum, two floats a row
   i64 q_row, q_head, o_row, o_head;
   int batch, heads, kv_heads, group, pages, shift, width, tiles;
   int target;               // blocks a kv head that the sequences' tokens are shared out to
@@ -552,7 +552,7 @@ struct Rows {                                // RT x 16 query rows of a wavefron
   f32x4 o[RT][kND];
   float use[RT], l[RT];                      // what the scores are taken relative to, this lane's share of the sum
   float lim[RT];                             // how far a score may pass it: kLag, or -infinity as long as there was none
-  float vinv, vlim;                          // power of two that values' scales are taken relative to
+  float vinv, vlim;                          // one over the power of two that values' scales are taken relative to (0: none yet), most of them
   float factor;                              // on the scores: softmax scale, log2(e), and what q and the keys were scaled by
   float row[RT];                             // ... and of this row beside that, where some row of the wavefront has one
   u64 uneven;
@@ -682,6 +682,10 @@ DISC_DEV void scores(const Rows<RT>& R, const Keys& K, f32x4 (&s)[RT][2]) {
 
 constexpr float kLag = 8.f;       // a score may pass the running maximum by this many powers of two
 constexpr float kNone = -__builtin_inff();
+// The largest probability is 2^kBase when the reference moves.  Results add up to 2^31 probabilities times values, which
+// must not pass 32 bits where the result does not: of bf16 values, which may be as large as those, far below 1 (bf16 has
+// the range); of fp16 values and codes there is room.
+constexpr float kBase = !kQuantised && !DISC_T_F16 ? -40.f : 0.f;
 
 // A step's scores, scaled, relative to the reference of their row and masked; where they pass it by more than the lag
 // (or it is the first time that there are any), the reference moves up to them, and sum and result with it.
@@ -729,20 +733,21 @@ DISC_DEV void bound_step(Rows<RT>& R, f32x4 (&s)[RT][2], const float (&ks)[8], f
       if (v > R.vlim) {
         int e;
         (void)__builtin_frexpf(v, &e);
-        e = e < -100 ? -100 : e;
+        e = e < -100 ? -100 : e > 127 ? 127 : e;
+        const float before = R.vinv;
         R.vinv = __builtin_ldexpf(1.f, -e);
-        vscale = R.vinv * R.vlim * 0.125f;        // (powers of two; 0 where there was none)
-        R.vlim = __builtin_ldexpf(8.f, e);
+        vscale = before > 0.f ? R.vinv / before : 0.f;   // (powers of two)
+        R.vlim = __builtin_ldexpf(8.f, e);               // (or infinity: nothing is larger)
       }
     }
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
       const float t = max_of_groups(top[rt]);
       const bool first = R.lim[rt] == kNone;
-      const float shift = t > (first ? kNone : 0.f) ? t : 0.f;
+      const float shift = t > (first ? kNone : kBase) ? t - kBase : 0.f;
       const float alpha = first ? 0.f : __builtin_amdgcn_exp2f(-shift);
       R.use[rt] += shift;
-      R.lim[rt] = t > kNone ? kLag : R.lim[rt];
+      R.lim[rt] = t > kNone ? kBase + kLag : R.lim[rt];
       if (__ballot(!first)) {                     // (nothing was summed before the first time)
         asm volatile("");
         R.l[rt] *= alpha;
@@ -974,8 +979,12 @@ constexpr int kPieces = kND / 4;
 static_assert(kND % 4 == 0 && kE % 4 == 0, "a piece is of one group of tiles");
 struct Other {
   f32x4 o[4][kPieces][64];
-  float use[64], l[64];                       // use: -infinity where there was no score
+  float use[64], l[64], unit;                 // use: -infinity where there was no score
 };
+// What the values' scales were taken relative to: results times this (and one over kCode) are theirs.  It is multiplied in
+// last, when they are divided by their sum: before, a power of two close to the largest would make them infinite.
+template <int RT>
+DISC_DEV float unit_of(const Rows<RT>& R) { return kQuantised ? (R.vinv > 0.f ? 1.f / R.vinv : 0.f) : 1.f; }
 DISC_DEV float reference(const Rows<1>& R) { return R.lim[0] > kNone ? R.use[0] : kNone; }
 // (no reference: the sum is 0, or NaN where every score was)
 DISC_DEV float weight(float use, float top, float l) { return use > kNone ? __builtin_amdgcn_exp2f(use - top) : l; }
@@ -990,6 +999,7 @@ DISC_DEV void hand_over(const Rows<1>& R, Other& X) {
     for (int q = 0; q < kPieces; ++q) X.o[r][q][lane] = piece_of(R, r, q);
   X.use[lane] = reference(R);
   X.l[lane] = R.l[0];
+  X.unit = unit_of(R);
 }
 
 // `kWays` wavefronts work on the same rows, 4 / kWays rows sets a block.
@@ -1069,15 +1079,10 @@ DISC_DEV void attend_body(const AttendArgs& A) {
     }
     R.l[0] += __shfl_xor(R.l[0], 16);
     R.l[0] += __shfl_xor(R.l[0], 32);
-    if (kQuantised) {
-      const float f = R.vlim * (0.125f / kCode);
-#pragma unroll
-      for (int d = 0; d < kND; ++d) R.o[0][d] *= f;
-    }
     // register r of this wavefront's share, of all that work on these rows
     constexpr int kShare = 4 / kWays;
     f32x4 done[kShare][kPieces];
-    float top = reference(R), l = R.l[0];
+    float top = reference(R), l = R.l[0], unit = unit_of(R);
     if (kWays == 1) {
 #pragma unroll
       for (int i = 0; i < kShare; ++i)
@@ -1088,14 +1093,19 @@ DISC_DEV void attend_body(const AttendArgs& A) {
       hand_over(R, other[w]);
       __syncthreads();
       const Other* all = other + set * kWays;
-      float use[kWays], sum[kWays];
+      float use[kWays], sum[kWays], units[kWays];
 #pragma unroll
-      for (int i = 0; i < kWays; ++i) use[i] = all[i].use[lane], sum[i] = all[i].l[lane], top = fmaxf(top, use[i]);
+      for (int i = 0; i < kWays; ++i) {
+        use[i] = all[i].use[lane], sum[i] = all[i].l[lane], top = fmaxf(top, use[i]);
+        units[i] = all[i].unit, unit = fmaxf(unit, units[i]);
+      }
+      const float per = kQuantised && unit > 0.f ? 1.f / unit : 0.f;
       l = 0.f;
 #pragma unroll
       for (int i = 0; i < kWays; ++i) {
-        const float f = weight(use[i], top, sum[i]);
+        float f = weight(use[i], top, sum[i]);
         l += use[i] > kNone ? sum[i] * f : sum[i];
+        if (kQuantised) f *= units[i] * per;
 #pragma unroll
         for (int j = 0; j < kShare; ++j)
 #pragma unroll
@@ -1107,8 +1117,8 @@ DISC_DEV void attend_body(const AttendArgs& A) {
     }
     if (n < rows) {
       const bool alone = I.whole && A.prefix_parts == 0;
-      // (the sum is 1 or more where it is not 0: its reciprocal is rounded to 32 bits, of which the result keeps 11 at most)
-      const float inverse = 1.f / l;
+      // (the sum is 2^kBase or more where it is not 0: its reciprocal is rounded to 32 bits, of which the result keeps 11 at most)
+      const float inverse = 1.f / kCode / l;
       const i64 at = shared ? prefix_row(A, part, b, head) : part_row(A, A.direct ? b : part + b, head);
       T* out = A.out + b * A.o_row + head * A.o_head;
 #pragma unroll
@@ -1117,8 +1127,10 @@ DISC_DEV void attend_body(const AttendArgs& A) {
         for (int j = 0; j < kShare; ++j) {
           const int d = element_of(q / (kE / 4), q % (kE / 4) * 4, turn + j * kWays);
           if (d >= kD) continue;
-          if (alone) store4(out + d, l != 0.f ? done[j][q] * inverse : (f32x4){0, 0, 0, 0});
-          else *(f32x4*)(A.part + at * kD + d) = done[j][q];
+          f32x4 x = l != 0.f ? done[j][q] * inverse : (f32x4){0, 0, 0, 0};
+          if (kQuantised) x *= unit;
+          if (alone) store4(out + d, x);
+          else *(f32x4*)(A.part + at * kD + d) = x;
         }
       if (!alone && turn == 0 && (threadIdx.x & 63) < 16) A.part_m[2 * at] = top, A.part_m[2 * at + 1] = l;
     }
@@ -1313,7 +1325,7 @@ extern "C" __global__ void __launch_bounds__(512, 2) disc_prefix_k(AttendArgs A)
     const int row = row0 + rt * 16 + n, b = row / A.group, i = row - b * A.group;
     if (row >= all) continue;
     const i64 at = prefix_row(A, part, b, h * A.group + i);
-    const float f = !kQuantised ? 1.f : R.vinv > 0.f ? 1.f / (R.vinv * kCode) : 0.f;
+    const float l = R.l[rt], f = l != 0.f ? 1.f / kCode / l : 0.f, unit = unit_of(R);
 #pragma unroll
     for (int x = 0; x < kNB; ++x)
 #pragma unroll
@@ -1321,9 +1333,11 @@ extern "C" __global__ void __launch_bounds__(512, 2) disc_prefix_k(AttendArgs A)
         const int d = element_of(x, 0, r);
         if (d < kD) {
 #pragma unroll
-          for (int e = 0; e < kE; e += 4)
-            *(f32x4*)(A.part + at * kD + d + e) = (f32x4){R.o[rt][x * kE + e][r] * f, R.o[rt][x * kE + e + 1][r] * f, R.o[rt][x * kE + e + 2][r] * f,
-                                                          R.o[rt][x * kE + e + 3][r] * f};
+          for (int e = 0; e < kE; e += 4) {
+            f32x4 y = {R.o[rt][x * kE + e][r] * f, R.o[rt][x * kE + e + 1][r] * f, R.o[rt][x * kE + e + 2][r] * f, R.o[rt][x * kE + e + 3][r] * f};
+            if (kQuantised) y *= unit;
+            *(f32x4*)(A.part + at * kD + d + e) = y;
+          }
         }
       }
     if (g == 0) A.part_m[2 * at] = R.lim[rt] > kNone ? R.use[rt] : kNone, A.part_m[2 * at + 1] = R.l[rt];
@@ -1372,9 +1386,10 @@ extern "C" __global__ void __launch_bounds__(256) disc_join_k(AttendArgs A) {
     float top = fmaxf(m, pm);
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
-    // (no maximum: nothing was there, or every score was NaN and so is the sum)
-    const float f = pm > kNone ? __builtin_amdgcn_exp2f(pm - top) : pl;
-    float sum = pm > kNone ? pl * f : pl;
+    // A chunk's result counts by its sum.  (No reference: nothing was there, or every score was NaN and so is the sum.  The
+    // sums are at most 2^(kBase + kLag + 31): their weights are brought below 1, so that no result grows on the way.)
+    const float f = pm > kNone ? pl * __builtin_amdgcn_exp2f(pm - top - (kBase + kLag + 32.f)) : pl;
+    float sum = f;
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
     const float before = m > kNone ? __builtin_amdgcn_exp2f(m - top) : l;

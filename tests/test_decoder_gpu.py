@@ -656,3 +656,81 @@ def test_the_step_of_a_token(ctx):
         slack = (q.abs() * k.abs()).sum(-1).amax() / math.sqrt(D) * (2 * 2.0 ** -11 + 2.0 ** -20) + 2.0 ** -16
         bound = _half_step(torch.float16) * want.abs() + 2 * slack * 1.01 * v.abs().amax()
         _inside(out[b], want, bound, f"sequence {b}")
+
+
+# ---- weights, values and rows of every size --------------------------------------------------------
+
+
+def _shaped(dtype, storage, D, kv, group, size, lengths, prefix, kind, gap, g):
+    """A batch whose scores and values are set: every token's first key element times 16 is its score beside a small random
+    one.  "sink": two tokens of every sequence and of the prefix score `gap` nats above the others and have no value, or
+    2^-12 of one.  "loud": two score 50 nats below and have values 2^25 times the others' (2^15 in fp16).  "spread":
+    scores spread over `gap` nats.  "huge": every row's largest value is the type's."""
+    s = _setup(dtype, storage, D, kv, group, size, lengths, prefix, g)
+    count = s["pages"][0].shape[0]
+    k, v = (_normal((count, kv, size, D), torch.float32, g, 0.5) for _ in range(2))
+    up = math.sqrt(D) / 16
+    k[..., 0] = 0.0
+    if kind == "spread":
+        k[..., 0] = torch.rand((count, kv, size), generator=g, device="cuda") * (-gap * up)
+    if kind == "huge":
+        v = v / v.abs().amax(-1, keepdim=True) * torch.finfo(TYPES[dtype]).max
+    if dtype == "f16" and kind != "huge":
+        v *= 2.0 ** (-4 if kind == "loud" else 10)             # (results that are normal numbers)
+    rows = [(s["table"][b].tolist(), n) for b, n in enumerate(lengths)] + [(s["prefix_table"].tolist(), prefix)]
+    for row, n in rows:
+        for i, t in enumerate((5, n // 2 + 3)):
+            if t >= n or n < 8:
+                continue
+            page, place = row[t // size], t % size
+            if kind == "sink":
+                k[page, :, place, 0] = gap * up
+                v[page, :, place] *= i * 2.0 ** -12
+            elif kind == "loud":
+                k[page, :, place, 0] = -50 * up
+                v[page, :, place] *= 2.0 ** (25 if dtype == "bf16" else 15)
+    if storage in STORED:
+        c = [plain.encode(x.to(TYPES[dtype]), storage) for x in (k, v)]
+        s["pages"] = [c[0][0], c[1][0], c[0][1], c[1][1]]
+    else:
+        s["pages"] = [x.to(TYPES[dtype]) for x in (k, v)]
+    s["q"][..., 0] = 16.0
+    return s
+
+
+def _own_sum_bound(dtype, storage, s, scale):
+    """The result's own half step, and twice the relative error of a weight times sum p |v| / sum p: of the very products that
+    the result is the sum of, so that nothing may be lost beside a larger weight or value of another token.  A weight's
+    error: its rounding (to half precision 2^-11; as two half-precision numbers, the smaller of 2^-15 at least), its
+    score's, the hardware's power of two 2^-22; sums of n terms in 32 bits, n 2^-24 each of numerator and denominator."""
+    want, most, sums, keys = plain.attend(s["q"], s["lengths"], s["table"], s["pages"], scale, s["prefix_table"], s["prefix"])
+    v = s["pages"][1]
+    v = (v.view(torch.uint8) & 127).view(v.dtype) if v.dtype is torch.float8_e4m3fn else v.abs()
+    share = plain.attend(s["q"], s["lengths"], s["table"], [s["pages"][0], v, *s["pages"][2:]], scale, s["prefix_table"], s["prefix"])[0]
+    D = s["q"].shape[2]
+    n = float(s["prefix"] + max(0, int(s["lengths"].max())))
+    one = 2.0 ** -11 if storage in STORED and dtype == "bf16" else 2.0 ** -15
+    score = sums * scale * ((D + 4) * 2.0 ** -24)
+    if storage in STORED and dtype == "bf16":
+        score = score + scale * 2.0 ** -25 * float(s["q"].abs().max()) * keys
+    w = one + score + 2.0 ** -22 + n * 2.0 ** -24
+    return want, _half_step(TYPES[dtype]) * want.abs() + (2 * w)[..., None] * 1.01 * share + torch.finfo(TYPES[dtype]).smallest_normal * _half_step(TYPES[dtype])
+
+
+# sequences of their own, long and short; a prefix in the sequences' own launch, in line, and in a launch of its own
+SHAPES = [(2, 2, 16, [1500, 33, 300, 7], 0), (2, 4, 16, [40, 9, 1], 700), (1, 3, 8, [100, 31], 150), (8, 16, 16, [(11 * i) % 40 for i in range(40)], 2600)]
+KINDS = [("bf16", "i8", 128), ("bf16", "e4m3", 64), ("f16", "i8", 64), ("f16", "f16", 80), ("bf16", "bf16", 128), ("f16", "e4m3", 256)]
+
+
+@pytest.mark.parametrize("dtype,storage,D", KINDS)
+def test_attention_of_the_largest_values(ctx, dtype, storage, D):
+    """Rows whose largest value is the type's: no sum on the way to a finite result overflows."""
+    cache = _cache(ctx, dtype, storage, D)
+    for kv, group, size, lengths, prefix in SHAPES + [(1, 2, 8, [1, 2], 0)]:
+        s = _shaped(dtype, storage, D, kv, group, size, lengths, prefix, "huge", 0, _generator(41 + prefix))
+        want, bound = _own_sum_bound(dtype, storage, s, 1.0 / math.sqrt(D))
+        # (no token's value may round up past the type)
+        assert float(want.abs().max()) < torch.finfo(TYPES[dtype]).max * 1.001
+        fine = want.abs() + bound < torch.finfo(TYPES[dtype]).max
+        got = _run(cache, s)[0]
+        _inside(got[fine], want[fine], bound[fine], f"largest values, {len(lengths)} sequences behind {prefix}")
