@@ -48,15 +48,10 @@ def stored_rows(pages, slots):
     return out, inside
 
 
-def attend(q, lengths, table, pages, scale, prefix_table=None, prefix_length=0):
-    """Attention of one query token a sequence, [batch, heads, D]; also the largest |value|, the largest sum of |q k| and the
-    largest sum of |k| that each result depends on (what a bound of the rounding errors is made of)."""
+def _sequences(q, lengths, table, pages, prefix_table, prefix_length):
+    """Sequence by sequence: its number, its query rows [heads, 1, D] and the keys and values they see [heads, tokens, D]."""
     size, count = pages[0].shape[2], pages[0].shape[0]
-    batch, heads, D = q.shape
-    group = heads // pages[0].shape[1]
-    out = torch.zeros((batch, heads, D), dtype=torch.float64, device=q.device)
-    most = torch.zeros((batch, heads), dtype=torch.float64, device=q.device)
-    sums, keys = (torch.zeros((batch, heads), dtype=torch.float64, device=q.device) for _ in range(2))
+    group = q.shape[1] // pages[0].shape[1]
 
     def slots_of(row, n):
         t = torch.arange(n, device=q.device)
@@ -65,7 +60,7 @@ def attend(q, lengths, table, pages, scale, prefix_table=None, prefix_length=0):
         return torch.where(page >= 0, page * size + t % size, torch.full_like(page, -1))
 
     shared = slots_of(prefix_table, prefix_length) if prefix_length else None
-    for b in range(batch):
+    for b in range(q.shape[0]):
         n = max(0, min(int(lengths[b]), table.shape[1] * size))
         slots = slots_of(table[b], n)
         if shared is not None:
@@ -74,11 +69,34 @@ def attend(q, lengths, table, pages, scale, prefix_table=None, prefix_length=0):
         if slots.numel() == 0:
             continue
         (k, v), _ = stored_rows(pages, slots)
-        k, v = (x.repeat_interleave(group, 1).transpose(0, 1) for x in (k, v))          # [heads, tokens, D]
-        qb = q[b].double()[:, None, :]
+        k, v = (x.repeat_interleave(group, 1).transpose(0, 1) for x in (k, v))
+        yield b, q[b].double()[:, None, :], k, v
+
+
+def attend(q, lengths, table, pages, scale, prefix_table=None, prefix_length=0):
+    """Attention of one query token a sequence, [batch, heads, D]; also the largest |value|, the largest sum of |q k| and the
+    largest sum of |k| that each result depends on (what a bound of the rounding errors is made of)."""
+    batch, heads, D = q.shape
+    out = torch.zeros((batch, heads, D), dtype=torch.float64, device=q.device)
+    most = torch.zeros((batch, heads), dtype=torch.float64, device=q.device)
+    sums, keys = (torch.zeros((batch, heads), dtype=torch.float64, device=q.device) for _ in range(2))
+    for b, qb, k, v in _sequences(q, lengths, table, pages, prefix_table, prefix_length):
         products = (k * qb).sum(-1)
         out[b] = (torch.softmax(products * scale, -1)[..., None] * v).sum(1)
         most[b] = v.abs().amax((1, 2))
         sums[b] = (k * qb).abs().sum(-1).amax(-1)
         keys[b] = k.abs().sum(-1).amax(-1)
     return out, most, sums, keys
+
+
+def attend_sizes(q, lengths, table, pages, scale, prefix_table=None, prefix_length=0):
+    """What attend's results are the sums of: sum p |v| / sum p and sum |v|, [batch, heads, D], and the largest p |v| / sum p, the
+    largest of all elements of a token's value, [batch, heads]."""
+    share, whole = (torch.zeros(q.shape, dtype=torch.float64, device=q.device) for _ in range(2))
+    heavy = torch.zeros(q.shape[:2], dtype=torch.float64, device=q.device)
+    for b, qb, k, v in _sequences(q, lengths, table, pages, prefix_table, prefix_length):
+        p = torch.softmax((k * qb).sum(-1) * scale, -1)
+        share[b] = (p[..., None] * v.abs()).sum(1)
+        whole[b] = v.abs().sum(1)
+        heavy[b] = (p * v.abs().amax(-1)).amax(-1)
+    return share, whole, heavy

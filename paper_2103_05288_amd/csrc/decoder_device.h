@@ -316,10 +316,13 @@ extern "C" __global__ void __launch_bounds__(256) disc_load_nt_k(RowsArgs A) { l
 // put it together: the values need no LDS either.
 //
 // 8-bit codes are exact in half precision and in bf16; a key's scale multiplies its score, a value's scale its
-// probability.  Those products p * scale are taken to half precision relative to a power of two that follows the largest
-// scale seen, as the probabilities follow the largest score.
-// Where the probabilities would have no more bits than the result they are held as a sum of two 16-bit
-// numbers (hi + lo), so that the only rounding that counts is the result's.
+// probability.  Those products p * scale, the weights, are taken to half precision relative to a power of two of their own
+// row's, which follows the largest of them (neither the largest score nor the largest scale: a token that scores high may
+// have a value of zero, and one with a huge value no weight).
+// Where the weights would have no more bits than the result they are held as a sum of two 16-bit numbers (hi + lo), so
+// that of all but the smallest the only rounding that counts is the result's.  bf16 has the range of 32 bits.  Half
+// precision ends at 2^-25, which is 2^-34 of the largest weight over 8-bit rows and 2^-35 of the largest probability over
+// fp16 ones: a smaller weight is off by up to that much.
 //
 // A block is four wavefronts; they take the steps of a stretch of tokens in turn and join in LDS at its end.
 // The stretches are cut from the lengths, on the device, so that all blocks have the same share.
@@ -552,7 +555,7 @@ struct Rows {                                // RT x 16 query rows of a wavefron
   f32x4 o[RT][kND];
   float use[RT], l[RT];                      // what the scores are taken relative to, this lane's share of the sum
   float lim[RT];                             // how far a score may pass it: kLag, or -infinity as long as there was none
-  float vinv, vlim;                          // one over the power of two that values' scales are taken relative to (0: none yet), most of them
+  float grow[RT], room[RT];                  // power of two on the weights (0: none yet), log2 of what they may be without it
   float factor;                              // on the scores: softmax scale, log2(e), and what q and the keys were scaled by
   float row[RT];                             // ... and of this row beside that, where some row of the wavefront has one
   u64 uneven;
@@ -680,12 +683,14 @@ DISC_DEV void scores(const Rows<RT>& R, const Keys& K, f32x4 (&s)[RT][2]) {
     }
 }
 
-constexpr float kLag = 8.f;       // a score may pass the running maximum by this many powers of two
+constexpr float kLag = !kQuantised && DISC_T_F16 ? 4.f : 8.f;   // a score may pass the running maximum by this many powers of two
 constexpr float kNone = -__builtin_inff();
-// The largest probability is 2^kBase when the reference moves.  Results add up to 2^31 probabilities times values, which
-// must not pass 32 bits where the result does not: of bf16 values, which may be as large as those, far below 1 (bf16 has
-// the range); of fp16 values and codes there is room.
-constexpr float kBase = !kQuantised && !DISC_T_F16 ? -40.f : 0.f;
+// The largest probability is 2^kBase when the reference moves (or half of that: it moves by powers of two).  Results add up
+// to 2^31 probabilities times values, which must not pass 32 bits where the result does not: of bf16 values, which may be as
+// large as those, far below 1 (bf16 has the range); of fp16 values and codes there is room.  Probabilities over fp16 values
+// are their weights: they begin at the upper end of half precision, 2^15 with the lag.
+constexpr float kBase = kQuantised ? 0.f : DISC_T_F16 ? 11.f : -40.f;
+constexpr float kWeight = 11.f, kMostWeight = 15.f;   // log2 of the largest weight when its power of two is set, and at any time
 
 // A step's scores, scaled, relative to the reference of their row and masked; where they pass it by more than the lag
 // (or it is the first time that there are any), the reference moves up to them, and sum and result with it.
@@ -720,39 +725,49 @@ DISC_DEV void bound_step(Rows<RT>& R, f32x4 (&s)[RT][2], const float (&ks)[8], f
     for (int j = 0; j < 8; ++j) top[rt] = fmaxf(top[rt], s[rt][j / 4][j % 4]);
     late |= top[rt] > R.lim[rt];
   }
-  float vtop = 0.f;
   if (kQuantised) {
+    float vtop = 0.f;
 #pragma unroll
     for (int j = 0; j < 8; ++j) vtop = fmaxf(vtop, fabsf(vs[j]));
-    late |= vtop > R.vlim;
+    // (a bound of the weights, of the largest score and the largest scale of eight tokens; times 2^32, so that it is no
+    // subnormal number, of which the hardware has no logarithm)
+    const float v = __builtin_amdgcn_logf(vtop * 0x1p32f) - 32.f;
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) late |= top[rt] + v > R.room[rt];
   }
   if (__ballot(late)) {                           // seldom after the first steps
-    float vscale = 1.f;
-    if (kQuantised) {
-      float v = max_of_groups(vtop);
-      if (v > R.vlim) {
-        int e;
-        (void)__builtin_frexpf(v, &e);
-        e = e < -100 ? -100 : e > 127 ? 127 : e;
-        const float before = R.vinv;
-        R.vinv = __builtin_ldexpf(1.f, -e);
-        vscale = before > 0.f ? R.vinv / before : 0.f;   // (powers of two)
-        R.vlim = __builtin_ldexpf(8.f, e);               // (or infinity: nothing is larger)
-      }
-    }
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
       const float t = max_of_groups(top[rt]);
       const bool first = R.lim[rt] == kNone;
-      const float shift = t > (first ? kNone : kBase) ? t - kBase : 0.f;
+      const float past = t - kBase, shift = past > (first ? kNone : 0.f) ? ceilf(past) : 0.f;
       const float alpha = first ? 0.f : __builtin_amdgcn_exp2f(-shift);
+      float turn = alpha;                         // on the results
+      if (kQuantised) {
+        // The weights' power of two makes up for the reference's move, so that the results stay as they are, unless the
+        // step's largest weight has no room.  (By the scales' exponents: one too many at most.)
+        float w = kNone;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float e = (float)__builtin_amdgcn_frexp_expf(vs[j]);
+          w = fmaxf(w, vs[j] != 0.f ? s[rt][j / 4][j % 4] + e : kNone);
+        }
+        w = max_of_groups(w) - shift;
+        const float before = kMostWeight - R.room[rt] + shift;       // (infinity: there is none yet)
+        float e = fminf(before, 100.f);
+        if (w + e > kMostWeight) e = fmaxf(kWeight - ceilf(w), -120.f);
+        const bool any = w > kNone || R.grow[rt] > 0.f;
+        turn = R.grow[rt] > 0.f ? __builtin_ldexpf(1.f, (int)(e - before)) : 0.f;
+        R.grow[rt] = any ? __builtin_ldexpf(1.f, (int)e) : 0.f;
+        R.room[rt] = any ? kMostWeight - e : kNone;
+      }
       R.use[rt] += shift;
       R.lim[rt] = t > kNone ? kBase + kLag : R.lim[rt];
       if (__ballot(!first)) {                     // (nothing was summed before the first time)
         asm volatile("");
         R.l[rt] *= alpha;
 #pragma unroll
-        for (int d = 0; d < kND; ++d) R.o[rt][d] *= alpha * vscale;
+        for (int d = 0; d < kND; ++d) R.o[rt][d] *= turn;
       }
 #pragma unroll
       for (int j = 0; j < 8; ++j) s[rt][j / 4][j % 4] -= shift;
@@ -760,7 +775,7 @@ DISC_DEV void bound_step(Rows<RT>& R, f32x4 (&s)[RT][2], const float (&ks)[8], f
   }
 }
 
-// The step's probabilities, in place of its scores.
+// The step's weights, in place of its scores.
 template <int RT>
 DISC_DEV void weigh_step(Rows<RT>& R, f32x4 (&s)[RT][2], const float (&vs)[8]) {
 #pragma unroll
@@ -770,7 +785,7 @@ DISC_DEV void weigh_step(Rows<RT>& R, f32x4 (&s)[RT][2], const float (&vs)[8]) {
     for (int j = 0; j < 8; ++j) {
       float p = __builtin_amdgcn_exp2f(s[rt][j / 4][j % 4]);
       sum += p;
-      if (kQuantised) p *= vs[j] * R.vinv;
+      if (kQuantised) p *= vs[j] * R.grow[rt];
       s[rt][j / 4][j % 4] = p;
     }
     R.l[rt] += sum;
@@ -872,11 +887,11 @@ DISC_DEV void clear_rows(Rows<RT>& R) {
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     R.lim[rt] = kNone;
-    R.use[rt] = R.l[rt] = 0.f;
+    R.use[rt] = R.l[rt] = R.grow[rt] = 0.f;
+    R.room[rt] = kNone;
 #pragma unroll
     for (int d = 0; d < kND; ++d) R.o[rt][d] = (f32x4){0, 0, 0, 0};
   }
-  R.vinv = R.vlim = 0.f;
   R.factor = (float)(DISC_SCALE_LOG2E);
   R.uneven = 0;
 }
@@ -979,12 +994,12 @@ constexpr int kPieces = kND / 4;
 static_assert(kND % 4 == 0 && kE % 4 == 0, "a piece is of one group of tiles");
 struct Other {
   f32x4 o[4][kPieces][64];
-  float use[64], l[64], unit;                 // use: -infinity where there was no score
+  float use[64], l[64], unit[kQuantised ? 64 : 1];   // use: -infinity where there was no score
 };
-// What the values' scales were taken relative to: results times this (and one over kCode) are theirs.  It is multiplied in
-// last, when they are divided by their sum: before, a power of two close to the largest would make them infinite.
+// One over the weights' power of two: results times this (and one over kCode) are the values'.  It is multiplied in last,
+// when they are divided by their sum: before, a power of two close to the largest would make them infinite.
 template <int RT>
-DISC_DEV float unit_of(const Rows<RT>& R) { return kQuantised ? (R.vinv > 0.f ? 1.f / R.vinv : 0.f) : 1.f; }
+DISC_DEV float unit_of(const Rows<RT>& R, int rt) { return kQuantised ? (R.grow[rt] > 0.f ? 1.f / R.grow[rt] : 0.f) : 1.f; }
 DISC_DEV float reference(const Rows<1>& R) { return R.lim[0] > kNone ? R.use[0] : kNone; }
 // (no reference: the sum is 0, or NaN where every score was)
 DISC_DEV float weight(float use, float top, float l) { return use > kNone ? __builtin_amdgcn_exp2f(use - top) : l; }
@@ -999,7 +1014,7 @@ DISC_DEV void hand_over(const Rows<1>& R, Other& X) {
     for (int q = 0; q < kPieces; ++q) X.o[r][q][lane] = piece_of(R, r, q);
   X.use[lane] = reference(R);
   X.l[lane] = R.l[0];
-  X.unit = unit_of(R);
+  if (kQuantised) X.unit[lane] = unit_of(R, 0);
 }
 
 // `kWays` wavefronts work on the same rows, 4 / kWays rows sets a block.
@@ -1082,7 +1097,7 @@ DISC_DEV void attend_body(const AttendArgs& A) {
     // register r of this wavefront's share, of all that work on these rows
     constexpr int kShare = 4 / kWays;
     f32x4 done[kShare][kPieces];
-    float top = reference(R), l = R.l[0], unit = unit_of(R);
+    float top = reference(R), l = R.l[0], unit = unit_of(R, 0);
     if (kWays == 1) {
 #pragma unroll
       for (int i = 0; i < kShare; ++i)
@@ -1097,7 +1112,7 @@ DISC_DEV void attend_body(const AttendArgs& A) {
 #pragma unroll
       for (int i = 0; i < kWays; ++i) {
         use[i] = all[i].use[lane], sum[i] = all[i].l[lane], top = fmaxf(top, use[i]);
-        units[i] = all[i].unit, unit = fmaxf(unit, units[i]);
+        if (kQuantised) units[i] = all[i].unit[lane], unit = fmaxf(unit, units[i]);
       }
       const float per = kQuantised && unit > 0.f ? 1.f / unit : 0.f;
       l = 0.f;
@@ -1325,7 +1340,7 @@ extern "C" __global__ void __launch_bounds__(512, 2) disc_prefix_k(AttendArgs A)
     const int row = row0 + rt * 16 + n, b = row / A.group, i = row - b * A.group;
     if (row >= all) continue;
     const i64 at = prefix_row(A, part, b, h * A.group + i);
-    const float l = R.l[rt], f = l != 0.f ? 1.f / kCode / l : 0.f, unit = unit_of(R);
+    const float l = R.l[rt], f = l != 0.f ? 1.f / kCode / l : 0.f, unit = unit_of(R, rt);
 #pragma unroll
     for (int x = 0; x < kNB; ++x)
 #pragma unroll

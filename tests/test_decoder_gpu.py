@@ -700,21 +700,23 @@ def _shaped(dtype, storage, D, kv, group, size, lengths, prefix, kind, gap, g):
 
 def _own_sum_bound(dtype, storage, s, scale):
     """The result's own half step, and twice the relative error of a weight times sum p |v| / sum p: of the very products that
-    the result is the sum of, so that nothing may be lost beside a larger weight or value of another token.  A weight's
-    error: its rounding (to half precision 2^-11; as two half-precision numbers, the smaller of 2^-15 at least), its
-    score's, the hardware's power of two 2^-22; sums of n terms in 32 bits, n 2^-24 each of numerator and denominator."""
-    want, most, sums, keys = plain.attend(s["q"], s["lengths"], s["table"], s["pages"], scale, s["prefix_table"], s["prefix"])
-    v = s["pages"][1]
-    v = (v.view(torch.uint8) & 127).view(v.dtype) if v.dtype is torch.float8_e4m3fn else v.abs()
-    share = plain.attend(s["q"], s["lengths"], s["table"], [s["pages"][0], v, *s["pages"][2:]], scale, s["prefix_table"], s["prefix"])[0]
+    the result is the sum of, so that nothing may be lost beside a larger score or value of another token.  A weight's
+    error: its rounding (to half precision 2^-11; as two half-precision or bf16 numbers 2^-16), its score's, the
+    hardware's power of two 2^-22; sums of n terms in 32 bits, n 2^-24 each of numerator and denominator.  Half precision
+    ends at 2^-25: 2^-34 of the largest product of a weight and a value over 8-bit rows, n times, and of fp16 values 2^-35 of
+    the largest probability times each of them."""
+    a = (s["q"], s["lengths"], s["table"], s["pages"], scale, s["prefix_table"], s["prefix"])
+    want, most, sums, keys = plain.attend(*a)
+    share, whole, heavy = plain.attend_sizes(*a)
     D = s["q"].shape[2]
     n = float(s["prefix"] + max(0, int(s["lengths"].max())))
-    one = 2.0 ** -11 if storage in STORED and dtype == "bf16" else 2.0 ** -15
+    one = 2.0 ** -11 if storage in STORED and dtype == "bf16" else 2.0 ** -16
     score = sums * scale * ((D + 4) * 2.0 ** -24)
     if storage in STORED and dtype == "bf16":
         score = score + scale * 2.0 ** -25 * float(s["q"].abs().max()) * keys
     w = one + score + 2.0 ** -22 + n * 2.0 ** -24
-    return want, _half_step(TYPES[dtype]) * want.abs() + (2 * w)[..., None] * 1.01 * share + torch.finfo(TYPES[dtype]).smallest_normal * _half_step(TYPES[dtype])
+    end = n * 2.0 ** -34 * heavy[..., None] if storage in STORED else 2.0 ** -35 * whole if dtype == "f16" else 0.0
+    return want, _half_step(TYPES[dtype]) * want.abs() + (2 * w)[..., None] * 1.01 * share + end + torch.finfo(TYPES[dtype]).smallest_normal * _half_step(TYPES[dtype])
 
 
 # sequences of their own, long and short; a prefix in the sequences' own launch, in line, and in a launch of its own
@@ -734,3 +736,13 @@ def test_attention_of_the_largest_values(ctx, dtype, storage, D):
         fine = want.abs() + bound < torch.finfo(TYPES[dtype]).max
         got = _run(cache, s)[0]
         _inside(got[fine], want[fine], bound[fine], f"largest values, {len(lengths)} sequences behind {prefix}")
+
+
+@pytest.mark.parametrize("dtype,storage,D", KINDS)
+@pytest.mark.parametrize("kind,gap", [("sink", 12), ("sink", 17), ("sink", 40), ("loud", 0), ("spread", 60)])
+def test_attention_beside_larger_scores_and_values(ctx, dtype, storage, D, kind, gap):
+    cache = _cache(ctx, dtype, storage, D)
+    for kv, group, size, lengths, prefix in SHAPES:
+        s = _shaped(dtype, storage, D, kv, group, size, lengths, prefix, kind, gap, _generator(51 + prefix))
+        want, bound = _own_sum_bound(dtype, storage, s, 1.0 / math.sqrt(D))
+        _inside(_run(cache, s)[0], want, bound, f"{kind} {gap}, {len(lengths)} sequences behind {prefix}")
