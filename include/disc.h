@@ -450,7 +450,8 @@ int disc_register_cache(disc_ctx* ctx, const disc_cache_desc* desc, int32_t* id_
  * pages, page_size, token stride, head stride of the keys, token stride, head stride of the values}; inputs = {slots,
  * keys, values}; outputs = {k_pages, v_pages} and with 8-bit storage {.., k_scales, v_scales}.  The scale of a row is a
  * / Q and the code of an element round(x * (Q / a)) -- a: its largest magnitude, Q = 127 or 448, both quotients and
- * the product rounded to fp32, the code to nearest, ties to even.  A row of zeros has the scale 0; a row with an
+ * the product rounded to fp32, the code to nearest, ties to even; where a < 2^-100, x and a are taken times 2^100 for the
+ * code, so that Q / a is finite.  A row of zeros has the scale 0; a row with an
  * infinity or a NaN gets the scale NaN and reads back as NaN.  Slots outside the pages (negative ones: padding) are
  * left out.  Slots of one call differ from each other; of a slot that is named twice, the row is either token's or a
  * mixture of both.

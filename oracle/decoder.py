@@ -28,8 +28,9 @@ def encode(rows, storage):
     bad = ~torch.isfinite(a)
     # (quotients of two tensors: with a number torch multiplies by a reciprocal, which is rounded once more)
     most = torch.full_like(a, MOST[storage])
-    inverse = torch.where((a > 0) & ~bad, most / a, torch.zeros_like(a))
-    y = torch.where(bad[..., None], torch.zeros_like(x), x * inverse[..., None]).clamp(-MOST[storage], MOST[storage])
+    up = torch.where(a < 2.0 ** -100, 2.0 ** 100, 1.0)
+    inverse = torch.where((a > 0) & ~bad, most / (a * up), torch.zeros_like(a))
+    y = torch.where(bad[..., None], torch.zeros_like(x), x * up[..., None] * inverse[..., None]).clamp(-MOST[storage], MOST[storage])
     codes = torch.round(y).to(torch.int8) if storage == "i8" else y.to(torch.float8_e4m3fn)
     return codes, torch.where(bad, torch.full_like(a, math.nan), a / most)
 

@@ -180,14 +180,15 @@ DISC_DEV float f32_of(u32 pair, int hi) {
   return (float)__builtin_bit_cast(Tx2, pair)[hi];
 }
 
-// Eight values to eight codes.  x * inverse is rounded once to 32 bits and once to the code (half to even).
-DISC_DEV u32x2 encode(const u32x4& x, float inverse) {
+// Eight values to eight codes.  x * up * inverse is rounded once to 32 bits (`up` is a power of two) and once to the code
+// (half to even).
+DISC_DEV u32x2 encode(const u32x4& x, float up, float inverse) {
   u32x2 c;
 #pragma unroll
   for (int w = 0; w < 2; ++w) {
     float y[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) y[e] = __builtin_amdgcn_fmed3f(f32_of(x[w * 2 + e / 2], e & 1) * inverse, -kMost, kMost);
+    for (int e = 0; e < 4; ++e) y[e] = __builtin_amdgcn_fmed3f(f32_of(x[w * 2 + e / 2], e & 1) * up * inverse, -kMost, kMost);
 #if DISC_STORAGE == 2
     int p = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
     c[w] = (u32)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], p, true);
@@ -204,7 +205,8 @@ DISC_DEV u32x2 encode(const u32x4& x, float inverse) {
 // Stores rows of keys and values.  Scale of a row: a / kMost with a its largest magnitude; code of an
 // element: round(x * (kMost / a)).  The magnitude is compared as the bits of |x|, so that a NaN counts as
 // larger than an infinity: a row that holds either gets the scale NaN and codes of zero, and reads back as
-// NaN.  A row of zeros has the scale 0.  Slots outside the pages are left out.
+// NaN.  A row of zeros has the scale 0.  kMost / a is no number of 32 bits below kMost / 2^128: bf16 rows of less than 2^-100
+// are brought up by 2^100 before (fp16 has none).  Slots outside the pages are left out.
 // Keys and values of a (token, head) are one lane group's, so that two loads are in flight a lane.
 template <bool kNt>
 DISC_DEV void store_body(const RowsArgs& A) {
@@ -242,9 +244,10 @@ DISC_DEV void store_body(const RowsArgs& A) {
     for (int s = 1; s < kLanes; s *= 2) a = max(a, (u32)__shfl_xor((int)a, s));
     const float m = (float)__builtin_bit_cast(T, (u16)a);
     const bool fine = m < __builtin_inff();
-    const float inverse = fine && m > 0.f ? kMost / m : 0.f;
+    const float up = !DISC_T_F16 && m < 0x1p-100f ? 0x1p100f : 1.f;
+    const float inverse = fine && m > 0.f ? kMost / (m * up) : 0.f;
     u32x2 c = {0, 0};
-    if (fine) c = encode(x[i], inverse);
+    if (fine) c = encode(x[i], up, inverse);
     if (mine) put<kNt>((u32x2*)((i ? A.vp : A.kp) + to * kD + lane * 8), c);
     if (lane == 0) (i ? A.vs : A.ks)[to] = fine ? m / kMost : __builtin_nanf("");
   }

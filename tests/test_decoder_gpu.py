@@ -746,3 +746,34 @@ def test_attention_beside_larger_scores_and_values(ctx, dtype, storage, D, kind,
         s = _shaped(dtype, storage, D, kv, group, size, lengths, prefix, kind, gap, _generator(51 + prefix))
         want, bound = _own_sum_bound(dtype, storage, s, 1.0 / math.sqrt(D))
         _inside(_run(cache, s)[0], want, bound, f"{kind} {gap}, {len(lengths)} sequences behind {prefix}")
+
+
+@pytest.mark.parametrize("storage,D", [("i8", 128), ("e4m3", 64)])
+def test_store_of_rows_near_the_smallest_numbers(ctx, storage, D):
+    """Rows of bf16 down to its last numbers, large and small elements and zeros among them, against codes in 64 bits."""
+    cache = _cache(ctx, "bf16", storage, D)
+    g = _generator(61)
+    a = torch.tensor([2.0 ** -e for e in (90, 99, 100, 101, 110, 119, 120, 121, 125, 126, 127, 130, 133)] + [3.7e-37, 1.3e-36, 1e-38], device="cuda")
+    x = torch.rand((a.numel(), 2, D), generator=g, device="cuda").mul_(2).sub_(1) * a[:, None, None]
+    x[..., 3] = 0.0
+    x[..., 5] = a[:, None]
+    x[:, 1, 6] = -a / 2
+    k = x.bfloat16()
+    v = k.flip(0).contiguous()
+    n, size = k.shape[0], 8
+    pages = _empty_pages("bf16", storage, 3, 2, size, D, 1.0)
+    slots = torch.randperm(3 * size, generator=g, device="cuda")[:n]
+    cache.store([k, v], slots, pages)
+    back = [torch.empty_like(k) for _ in range(2)]
+    cache.load(slots, pages, back)
+    most = 127.0 if storage == "i8" else 448.0
+    for i, rows in enumerate((k, v)):
+        codes = pages[i][slots // size, :, slots % size].double()
+        scales = pages[2 + i][slots // size, :, slots % size]
+        large = rows.double().abs().amax(-1)
+        assert torch.equal(scales, (large / most).float())
+        exact = rows.double() * most / large[..., None]
+        # (half a step of the code; Q / a and its product with the element are rounded to 32 bits)
+        step = torch.full_like(exact, 0.5) if storage == "i8" else torch.maximum(exact.abs() * 2.0 ** -4, torch.tensor(2.0 ** -10, dtype=torch.float64, device="cuda"))
+        assert ((codes - exact).abs() <= step + exact.abs() * 2.0 ** -22).all()
+        assert (codes[rows == 0] == 0).all() and (back[i][rows == 0] == 0).all()
