@@ -63,6 +63,7 @@ enum { FN_ROTARY = 0, FN_ROTARY_NT, FN_ROTARY_COUNT };
 enum { FN_STORE = 0, FN_STORE_NT, FN_LOAD, FN_LOAD_NT, FN_ATTEND, FN_ATTEND2, FN_ATTEND1, FN_ATTEND_NT, FN_PREFIX = FN_ATTEND_NT + 3, FN_JOIN, FN_CACHE_COUNT };
 
 constexpr int64_t kMostElements = (int64_t)1 << 60;
+constexpr int64_t kMostThreads = ((int64_t)1 << 32) - 1;     // of one launch, by axis; calls of more tokens are several launches
 
 int refuse(disc_ctx* c, int code, const char* what) { return context_fail(c, code, what); }
 int refuse(disc_ctx* c, int code, const char* what, long long got) {
@@ -263,8 +264,19 @@ int launch_rotary(disc_ctx* c, int32_t id, const int64_t* dims, int n_dims, cons
   const bool nt = moved >= kNonTemporalBytes / (2 * size);
   OnDevice on(context_device(c));
   if (!on.ok) return refuse(c, DISC_ERR_HIP, "hipSetDevice failed");
-  const int rc = enqueue(c, o->fn[nt ? FN_ROTARY_NT : FN_ROTARY], (uint64_t)tokens, y, 256, &a, sizeof a, stream);
-  if (rc == DISC_OK) context_count(c, 1);
+  int rc = DISC_OK, n = 0;
+  for (int64_t left = tokens; rc == DISC_OK && left > 0; ++n) {
+    const int64_t now = std::min(left, kMostThreads / 256);
+    rc = enqueue(c, o->fn[nt ? FN_ROTARY_NT : FN_ROTARY], (uint64_t)now, y, 256, &a, sizeof a, stream);
+    left -= now;
+    a.positions = (const char*)a.positions + now * a.position_bytes;
+    for (int k = 0; k < a.n; ++k) {
+      if (a.t[k].heads == 0) continue;
+      a.t[k].x = (const char*)a.t[k].x + now * a.t[k].x_token * size;
+      a.t[k].y = (char*)a.t[k].y + now * a.t[k].y_token * size;
+    }
+  }
+  if (rc == DISC_OK) context_count(c, n);
   return rc;
 }
 
@@ -354,14 +366,21 @@ int launch_rows(disc_ctx* c, int32_t id, const int64_t* dims, int n_dims, const 
   if (!a.k || !a.v || !aligned(a.k, 2) || !aligned(a.v, 2)) return refuse(c, DISC_ERR_INVALID_ARG, "keys or values: null or not aligned to their elements");
   int lanes = 2;
   while (lanes * 8 < o->head_dim) lanes *= 2;
-  const int64_t threads = times(times(a.tokens, a.heads), lanes);
-  if (threads < 0 || (threads + 255) / 256 >= (int64_t)1 << 31) return refuse(c, DISC_ERR_SHAPE, "too many rows for one call");
   if (context_device(c) < 0) return refuse(c, DISC_ERR_INVALID_ARG, "host-only context cannot launch");
   OnDevice on(context_device(c));
   if (!on.ok) return refuse(c, DISC_ERR_HIP, "hipSetDevice failed");
   const bool nt = times(a.tokens, a.heads) * o->head_dim * (2 + (scaled ? 1 : 2)) * 2 >= kNonTemporalBytes;
-  const int rc = enqueue(c, o->fn[(store ? FN_STORE : FN_LOAD) + (nt ? 1 : 0)], (uint64_t)((threads + 255) / 256), 1, 256, &a, sizeof a, stream);
-  if (rc == DISC_OK) context_count(c, 1);
+  const int64_t each = kMostThreads / 256 * 256 / ((int64_t)a.heads * lanes);   // tokens of a launch (2047 at least)
+  int rc = DISC_OK, n = 0;
+  for (int64_t left = a.tokens; rc == DISC_OK && left > 0; ++n) {
+    a.tokens = std::min(left, each);
+    rc = enqueue(c, o->fn[(store ? FN_STORE : FN_LOAD) + (nt ? 1 : 0)], (uint64_t)((a.tokens * a.heads * lanes + 255) / 256), 1, 256, &a, sizeof a, stream);
+    left -= a.tokens;
+    a.slots = (const int64_t*)a.slots + a.tokens;
+    a.k = (const char*)a.k + a.tokens * a.k_token * 2;
+    a.v = (const char*)a.v + a.tokens * a.v_token * 2;
+  }
+  if (rc == DISC_OK) context_count(c, n);
   return rc;
 }
 
@@ -462,7 +481,8 @@ int plan_attend(disc_ctx* c, const Operator& o, const int64_t* d, int n_dims, At
   a.join_ways = times(batch, heads) <= 4 * cus ? 4 : 1;
   p->join_blocks = alone ? 0 : ceil_div(times(batch, heads), 4 / a.join_ways);
   const int64_t partial = times(parts, heads) + times(a.prefix_parts, times(batch, heads));
-  if (times(batch, heads) >= (int64_t)1 << 31 || p->attend_blocks < 0 || p->prefix_blocks < 0 || p->attend_blocks >= (int64_t)1 << 31 || p->prefix_blocks >= (int64_t)1 << 31 || p->join_blocks >= (int64_t)1 << 31 || times(partial, 4 * 256 + 8) < 0)
+  if (times(batch, heads) >= (int64_t)1 << 31 || p->attend_blocks < 0 || p->prefix_blocks < 0 || p->attend_blocks > kMostThreads / 256 ||
+      p->prefix_blocks > kMostThreads / 512 || p->join_blocks > kMostThreads / 256 || times(partial, 4 * 256 + 8) < 0)
     return refuse(c, DISC_ERR_SHAPE, "too many rows for one call");
   p->workspace = batch > 0 ? (size_t)partial * ((size_t)o.head_dim * 4 + 8) : 0;
   return DISC_OK;

@@ -272,6 +272,21 @@ def test_attention_calls(ctx, path):
     raw("16-byte", "INVALID_ARG", i=ins[:4] + [pages[1].data_ptr() + 4] + ins[5:])
 
 
+def test_attention_of_more_threads_than_a_launch_has(ctx):
+    """Less than 2^32 threads a launch: 2^24 blocks of 256, 2^23 of the prefix's 512, are refused before anything is enqueued."""
+    h = ctx.register_cache("bf16", 16, "i8")
+    many = 1 << 20
+    ok = lambda *a, **k: h.workspace_bytes(*a, **k) >= 0  # noqa: E731
+    no = lambda *a, **k: _refused("SHAPE", "too many rows", lambda: h.workspace_bytes(*a, **k))  # noqa: E731
+    assert ok(many, 63, 63, 8) and ok(many, 32, 32, 8) and ok(many, 60, 1, 1000)
+    no(many, 64, 64, 8)                                        # one wavefront a (sequence, kv head), four a block
+    no(many, 64, 1, 1000)                                      # a wavefront a row that is joined
+    no(many, 1 << 7, 1 << 7, 8, 1 << 20)                       # the prefix's rows
+    dims = [many, 64, 64, 1, 8, 1, 0, 0, 1024, 16, 1024, 16]
+    x = torch.zeros(16, dtype=torch.uint8)
+    _refused("SHAPE", "too many rows", lambda: h._call(h._attend, dims, [x] * 7, [x], None, 0))
+
+
 def test_a_context_of_another_kind_of_operator_and_unknown_ids(ctx):
     lib = ctx.lib
     f = pkg.rotary_frequencies(8)[0]

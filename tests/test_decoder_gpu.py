@@ -777,3 +777,39 @@ def test_store_of_rows_near_the_smallest_numbers(ctx, storage, D):
         step = torch.full_like(exact, 0.5) if storage == "i8" else torch.maximum(exact.abs() * 2.0 ** -4, torch.tensor(2.0 ** -10, dtype=torch.float64, device="cuda"))
         assert ((codes - exact).abs() <= step + exact.abs() * 2.0 ** -22).all()
         assert (codes[rows == 0] == 0).all() and (back[i][rows == 0] == 0).all()
+
+
+# ---- calls of more threads than a launch has -------------------------------------------------------
+
+
+def test_rotary_of_more_tokens_than_a_launch_has_blocks(ctx):
+    """2^24 tokens and more: a block each, of which one launch has less than 2^24."""
+    h = ctx.register_rotary("bf16", 2, [1.0], layout="interleaved")
+    tokens = (1 << 24) + 5
+    g = _generator(81)
+    x = _normal((tokens, 1, 2), torch.bfloat16, g)
+    positions = torch.randint(0, 1000, (tokens,), generator=g, device="cuda", dtype=torch.int32)
+    y = torch.zeros_like(x)
+    before = ctx.stats()
+    h.launch(positions, [x], [y])
+    after = ctx.stats()
+    assert after["launch_calls"] == before["launch_calls"] + 1 and after["device_launches"] > before["device_launches"] + 1
+    want = plain.rotary(x, positions, [1.0], "interleaved")
+    _inside(y, want, _rotary_bound(x, positions, [1.0], "interleaved", 1.0, torch.bfloat16, want), "rotary")
+
+
+def test_store_of_more_rows_than_a_launch_has_threads(ctx):
+    """2^32 threads and more (of rows that all heads share, nearly all of them padding): the tokens at both sides of a launch's end."""
+    cache = _cache(ctx, "bf16", "i8", 16)
+    tokens, kv = 32767 + 9, 65536
+    rows = [_normal((tokens, 1, 16), torch.bfloat16, _generator(82 + i)) for i in range(2)]
+    pages = _empty_pages("bf16", "i8", 1, kv, 8, 16, 1.0)
+    at = torch.tensor([0, 32766, 32767, tokens - 1], device="cuda")
+    slots = torch.full((tokens,), -1, dtype=torch.int64, device="cuda")
+    slots[at] = torch.tensor([4, 0, 7, 2], device="cuda")
+    cache.store([r.expand(tokens, kv, 16) for r in rows], slots, pages)
+    for i, r in enumerate(rows):
+        codes, scales = plain.encode(r[at, 0], "i8")
+        want, want_scales = torch.ones((8, 16), dtype=torch.int8, device="cuda"), torch.ones(8, device="cuda")
+        want[slots[at]], want_scales[slots[at]] = codes, scales
+        assert (pages[i][0] == want).all() and (pages[2 + i][0] == want_scales).all()
