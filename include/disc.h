@@ -477,7 +477,9 @@ int disc_cache_load(disc_ctx* ctx, int32_t id, const int64_t* dims, int n_dims, 
  * launches that may overlap in time (two streams, two captured graphs) each need their own. */
 int disc_cache_attend(disc_ctx* ctx, int32_t id, const int64_t* dims, int n_dims, const void* const* inputs, int n_in,
                       void* const* outputs, int n_out, void* workspace, size_t workspace_bytes, void* hip_stream);
-/* Bytes of workspace that a disc_cache_attend of these dims takes (the same dims; pointers and strides do not count). */
+/* Bytes of workspace that are enough for a disc_cache_attend of these dims (the same dims; pointers and strides do not count)
+ * and for any of a smaller batch, prefix_length or table_width with the same heads, pages and page_size: a program asks once,
+ * for the largest batch and the longest prefix and table that it will have. */
 int disc_cache_workspace_bytes(disc_ctx* ctx, int32_t id, const int64_t* dims, int n_dims, size_t* out);
 
 int disc_get_stats(disc_ctx* ctx, disc_stats_t* out);

@@ -390,12 +390,21 @@ struct AttendPlan {
   int64_t attend_blocks, prefix_blocks, join_blocks;
   int ways;                 // wavefronts of a sequence
   bool nt;
-  size_t workspace;
+  size_t workspace, reserve;   // bytes that this call takes, and that any of a smaller batch, prefix or table does
 };
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-int plan_attend(disc_ctx* c, const Operator& o, const int64_t* d, int n_dims, AttendPlan* p) {
+// Rows of query tokens that a block of a prefix has (`few`: in disc_attend_k), and blocks that are there at once.
+struct PrefixBlocks {
+  int64_t rows, slots;
+  PrefixBlocks(const Operator& o, int64_t cus, bool few) : rows(few ? 16 : o.head_dim <= 128 ? 256 : 128), slots((few ? o.resident : 1) * cus) {}
+};
+// Rounds of them that a chunk of the prefix may be made for: those that one chunk takes, or one more, three at most.
+int64_t most_rounds(int64_t blocks, int64_t slots) { return std::min<int64_t>(3, ceil_div(blocks, slots) + 1); }
+
+// `one_chunk`: every sequence of up to kDirectTokens is one chunk, whatever is faster (it takes less workspace).
+int plan_attend(disc_ctx* c, const Operator& o, const int64_t* d, int n_dims, bool one_chunk, AttendPlan* p) {
   if (!d || n_dims != 12) return refuse(c, DISC_ERR_INVALID_ARG, "an attention call takes 12 dims");
   AttendArgs& a = p->a;
   memset(&a, 0, sizeof a);
@@ -426,7 +435,7 @@ int plan_attend(disc_ctx* c, const Operator& o, const int64_t* d, int n_dims, At
   int64_t parts = batch + a.target;
   // (16-bit rows above 128: where the blocks are few, two steps more cost more than the join, 8 blocks of 500 tokens x 256
   // 15.5 us joined / 18.4 as one chunk each, 16 17.0 / 18.2, 120 25.5 / 19.7; 8-bit ones 15.5 / 15.0, 16.2 / 14.9, 19.8 / 15.4)
-  const int64_t direct_tokens = o.head_dim <= 128 || o.storage != DISC_STORAGE_SAME || times(batch, per) >= cus / 4 ? kDirectTokens : kDirectTokens / 2;
+  const int64_t direct_tokens = o.head_dim <= 128 || o.storage != DISC_STORAGE_SAME || times(batch, per) >= cus / 4 || one_chunk ? kDirectTokens : kDirectTokens / 2;
   if ((width << shift) <= direct_tokens) {
     a.direct = 1;
     parts = batch;
@@ -441,13 +450,14 @@ int plan_attend(disc_ctx* c, const Operator& o, const int64_t* d, int n_dims, At
   if (prefix > 0 && batch > 0 && !a.prefix_inline) {
     const int64_t units = ceil_div(prefix, kUnit), tile_units = times(times(ceil_div(rows, 16), units), kv);
     const bool few = tile_units >= 0 && tile_units <= (o.storage != DISC_STORAGE_SAME ? kFewUnits8 : kFewUnits16);
-    const int64_t block_rows = few ? 16 : o.head_dim <= 128 ? 256 : 128, row_blocks = ceil_div(rows, block_rows), slots = (few ? o.resident : 1) * cus;
+    const PrefixBlocks at(o, cus, few);
+    const int64_t row_blocks = ceil_div(rows, at.rows), slots = at.slots;
     // Chunks of the prefix: as many as make the shortest run, in rounds of the blocks that are there at once times the
     // units of a chunk and a block's own cost of about four.
     // (Of the rounds that one chunk takes, or one more, the most chunks that fit; nothing is gained where those are many.)
     const int64_t blocks = kv * row_blocks, rounds = ceil_div(blocks, slots);
     int64_t units_each = units, best = rounds * (units + 4);
-    for (int64_t r = rounds; r <= rounds + 1 && r <= 3; ++r) {
+    for (int64_t r = rounds; r <= most_rounds(blocks, slots); ++r) {
       const int64_t each = ceil_div(units, std::min(units, r * slots / blocks)), cost = r * (each + 4);
       if (cost < best) best = cost, units_each = each;
     }
@@ -484,7 +494,21 @@ int plan_attend(disc_ctx* c, const Operator& o, const int64_t* d, int n_dims, At
   if (times(batch, heads) >= (int64_t)1 << 31 || p->attend_blocks < 0 || p->prefix_blocks < 0 || p->attend_blocks > kMostThreads / 256 ||
       p->prefix_blocks > kMostThreads / 512 || p->join_blocks > kMostThreads / 256 || times(partial, 4 * 256 + 8) < 0)
     return refuse(c, DISC_ERR_SHAPE, "too many rows for one call");
-  p->workspace = batch > 0 ? (size_t)partial * ((size_t)o.head_dim * 4 + 8) : 0;
+  const size_t row = (size_t)o.head_dim * 4 + 8;
+  p->workspace = batch > 0 ? (size_t)partial * row : 0;
+  // Fewer query rows make more chunks of a prefix, so that a smaller call may take more than this one does.  What none
+  // takes more than: a chunk for every unit; and the rows of as many blocks as the chunks are made for, or where those are
+  // fewer than one chunk's, one, or as many as the pages of a chunk ask for.
+  int64_t chunks = a.direct ? (alone ? 0 : batch) : batch + a.target;
+  if (prefix > 0 && !a.prefix_inline) {
+    int64_t most = 0;
+    for (const bool few : {false, true}) {
+      const PrefixBlocks at(o, cus, few);
+      most = std::max(most, most_rounds(kv * ceil_div(rows, at.rows), at.slots) * at.slots * at.rows / heads);
+    }
+    chunks += std::max(std::min(most, times(batch, ceil_div(prefix, kUnit))), times(batch, ceil_div(prefix, (int64_t)kMostPages << shift)));
+  }
+  p->reserve = batch > 0 ? std::max(p->workspace, (size_t)(chunks * heads) * row) : 0;
   return DISC_OK;
 }
 
@@ -495,7 +519,10 @@ int launch_attend(disc_ctx* c, int32_t id, const int64_t* dims, int n_dims, cons
   if (!o) return refuse(c, DISC_ERR_INVALID_ARG, "bad cache id");
   if (!dims || !in || !out) return refuse(c, DISC_ERR_INVALID_ARG, "null pointer array");
   AttendPlan p;
-  if (const int rc = plan_attend(c, *o, dims, n_dims, &p)) return rc;
+  if (const int rc = plan_attend(c, *o, dims, n_dims, false, &p)) return rc;
+  // (a workspace asked for at a larger batch, where sequences are one chunk each, does not hold the chunks of this one)
+  if (p.workspace > workspace_bytes && !p.a.direct)
+    if (const int rc = plan_attend(c, *o, dims, n_dims, true, &p)) return rc;
   AttendArgs& a = p.a;
   const bool scaled = o->storage != DISC_STORAGE_SAME;
   const int want = 5 + (scaled ? 2 : 0) + (a.prefix_len > 0 ? 1 : 0);
@@ -605,8 +632,8 @@ int disc_cache_workspace_bytes(disc_ctx* ctx, int32_t id, const int64_t* dims, i
     const Operator* o = get_operator(ctx, id, Operator::CACHE);
     if (!o) return refuse(ctx, DISC_ERR_INVALID_ARG, "bad cache id");
     AttendPlan p;
-    const int rc = plan_attend(ctx, *o, dims, n_dims, &p);
-    if (rc == DISC_OK) *out = p.workspace;
+    const int rc = plan_attend(ctx, *o, dims, n_dims, false, &p);
+    if (rc == DISC_OK) *out = p.reserve;
     return rc;
   });
 }

@@ -223,9 +223,9 @@ class CacheHandle(_Handle):
         self._call(self._load, dims, [slots, *pages], rows, None, stream)
 
     def workspace_bytes(self, batch: int, q_heads: int, kv_heads: int, longest: int, prefix_length: int = 0, page_size: int = 8) -> int:
-        """Bytes of workspace that attend takes for a page table that holds up to `longest` tokens a sequence: table_width *
-        page_size, whatever the lengths are.  What was asked for at the smallest page size (the default) serves every page size
-        of tables that hold no more."""
+        """Bytes of workspace that attend takes for up to `batch` sequences, a page table that holds up to `longest` tokens a
+        sequence (table_width * page_size, whatever the lengths are) and a prefix of up to prefix_length.  What was asked for at
+        the smallest page size (the default) serves every page size of tables that hold no more."""
         width = -(-int(longest) // page_size)
         dims = [batch, q_heads, kv_heads, 1, page_size, width, prefix_length, -(-int(prefix_length) // page_size), 0, 0, 0, 0]
         arr, n = self.ctx._dims(dims)

@@ -326,6 +326,31 @@ def test_workspace_covers_smaller_calls(ctx):
         assert h.workspace_bytes(300, 32, 8, 512) == 0                       # one chunk each, written where it belongs
 
 
+def test_workspace_covers_smaller_batches_prefixes_and_tables(ctx, path):
+    """What was asked for at the largest batch, prefix and table serves every smaller one: by its size, and in the call."""
+    rng = random.Random(11)
+    for storage, D, q, kv in (("i8", 128, 64, 8), ("bf16", 128, 32, 8), ("bf16", 256, 8, 8), ("e4m3", 64, 40, 1), ("bf16", 192, 4, 2)):
+        h = ctx.register_cache("bf16", D, storage)
+        pages = _pages(kv=kv, D=D, stored={"i8": torch.int8, "e4m3": torch.float8_e4m3fn, "bf16": torch.bfloat16}[storage])
+        for B, longest, prefix in ((128, 8192, 16384), (64, 512, 0), (40, 512, 3000), (33, 300, 8320), (700, 40, 700), (1500, 8, 100000), (128, 8192, 8192)):
+            most = h.workspace_bytes(B, q, kv, longest, prefix)
+            ws = torch.empty(most, dtype=torch.uint8)
+            smaller = [(b, longest, prefix) for b in {1, B // 2, B - 1, 32, 33, 64, 65} if b <= B] + [(B, longest, p) for p in (prefix // 2, prefix - 1, 513, 128, 0) if 0 <= p <= prefix]
+            smaller += [(rng.randint(1, B), rng.randint(0, longest), rng.randint(0, prefix)) for _ in range(40)] + [(B, n, prefix) for n in (0, 8, 256, 512) if n <= longest]
+            for b, n, p in smaller:
+                width = n // 8
+                if storage != "bf16" or D <= 128 or n <= 256 or longest > 512:      # (one that fewer sequences take is left, see below)
+                    assert h.workspace_bytes(b, q, kv, width * 8, p) <= most, (storage, D, B, longest, prefix, b, n, p)
+                x = torch.zeros(1, 1, D, dtype=torch.bfloat16).expand(b, q, D)
+                out = torch.empty(b, q, D, dtype=torch.bfloat16)
+                table = torch.zeros(b, width, dtype=torch.int32)
+                more = {"prefix_table": torch.zeros(-(-p // 8), dtype=torch.int32), "prefix_length": p} if p else {}
+                _refused("INVALID_ARG", HOST_ONLY, lambda: h.attend(x, torch.zeros(b, dtype=torch.int32), table, pages, out, workspace=ws if most else None, **more))
+    # 16-bit rows above 128: a few sequences of up to 512 tokens are cut where there is workspace for it, and one chunk each without
+    h = ctx.register_cache("bf16", 256)
+    assert h.workspace_bytes(300, 32, 8, 512) == 0 and h.workspace_bytes(4, 32, 8, 512) > 0
+
+
 # ---- the device header on the CPU ------------------------------------------------------------------
 
 

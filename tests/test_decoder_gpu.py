@@ -813,3 +813,18 @@ def test_store_of_more_rows_than_a_launch_has_threads(ctx):
         want, want_scales = torch.ones((8, 16), dtype=torch.int8, device="cuda"), torch.ones(8, device="cuda")
         want[slots[at]], want_scales[slots[at]] = codes, scales
         assert (pages[i][0] == want).all() and (pages[2 + i][0] == want_scales).all()
+
+
+@pytest.mark.parametrize("dtype,storage,D,batch,longest,prefix", [("bf16", "bf16", 256, 300, 512, 0), ("bf16", "i8", 128, 66, 600, 2500), ("bf16", "bf16", 256, 40, 400, 700)])
+def test_attention_with_the_workspace_of_a_larger_call(ctx, dtype, storage, D, batch, longest, prefix):
+    """One workspace for the largest batch, prefix and table, and nothing written behind it."""
+    cache = _cache(ctx, dtype, storage, D)
+    need = max(16, cache.workspace_bytes(batch, 16, 4, longest, prefix))
+    held = torch.full((need + 4096,), 7, dtype=torch.uint8, device="cuda")
+    for b, p in ((batch, prefix), (batch - 1, prefix), (33, prefix), (32, prefix // 2), (4, prefix), (1, 600 if prefix else 0)):
+        lengths = [(13 * i) % min(40, longest) for i in range(b - 1)] + [longest - 20]
+        s = _setup(dtype, storage, D, 4, 4, 8, lengths, p, _generator(b + D))
+        s["table"] = s["table"][:, :-1].contiguous()
+        got = _run(cache, s, workspace=held[:need])[0]
+        _check(cache, dtype, storage, s, 1.0 / math.sqrt(D), got=got)
+        assert (held[need:] == 7).all()
