@@ -560,8 +560,8 @@ struct Rows {                                // RT x 16 query rows of a wavefron
   float lim[RT];                             // how far a score may pass it: kLag, or -infinity as long as there was none
   float grow[RT], room[RT];                  // power of two on the weights (0: none yet), log2 of what they may be without it
   float factor;                              // on the scores: softmax scale, log2(e), and what q and the keys were scaled by
-  float row[RT];                             // ... and of this row beside that, where some row of the wavefront has one
-  u64 uneven;
+  int row[RT];                               // ... without that, where `uneven`: rows have powers of two of their own, these
+  bool uneven;
 };
 struct Keys {
   u32x4 k[2][kNK];
@@ -698,13 +698,16 @@ constexpr float kWeight = 11.f, kMostWeight = 15.f;   // log2 of the largest wei
 // A step's scores, scaled, relative to the reference of their row and masked; where they pass it by more than the lag
 // (or it is the first time that there are any), the reference moves up to them, and sum and result with it.
 template <int RT>
-DISC_DEV void bound_step(Rows<RT>& R, f32x4 (&s)[RT][2], const float (&ks)[8], float (&vs)[8], int live) {
+DISC_DEV void bound_step(Rows<RT>& R, f32x4 (&s)[RT][2], float (&ks)[8], float (&vs)[8], int live) {
   if (R.uneven) {
     asm volatile("");                             // (a branch, as below)
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt)
+    for (int j = 0; j < 8; ++j) {                 // (exponents added up: a score is out of range only if all of it is)
+      const int e = __builtin_amdgcn_frexp_expf(ks[j]);
+      ks[j] = __builtin_amdgcn_frexp_mantf(ks[j]);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) s[rt][j / 4][j % 4] *= R.row[rt];
+      for (int rt = 0; rt < RT; ++rt) s[rt][j / 4][j % 4] = __builtin_ldexpf(s[rt][j / 4][j % 4], R.row[rt] + e);
+    }
   }
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt)
@@ -896,7 +899,7 @@ DISC_DEV void clear_rows(Rows<RT>& R) {
     for (int d = 0; d < kND; ++d) R.o[rt][d] = (f32x4){0, 0, 0, 0};
   }
   R.factor = (float)(DISC_SCALE_LOG2E);
-  R.uneven = 0;
+  R.uneven = false;
 }
 
 // The query rows' operand: lane (n, g) holds row n, the elements that the keys' lanes hold of theirs.
@@ -935,34 +938,63 @@ DISC_DEV u32 largest_queries(const Rows<RT>& R, u32 (&top)[RT]) {     // bits of
   for (int d = 1; d < 16; d *= 2) most = max(most, (u32)__shfl_xor((int)most, d));
   return most;
 }
+// By biased exponents: 2^15 is brought to by 2^(142 - e), or the largest power of two there is; its exponent.
+DISC_DEV int up_of(int e) { return min(142 - max(e, 1), 127); }
+DISC_DEV bool far_below(u32 top, int e) { return top != 0 && (int)(top >> 7) + 16 < e; }
+// Whether some row of this lane's asks for its own (or the largest is so large that its power of two and the softmax scale
+// might have no product).
 template <int RT>
-DISC_DEV void halve_query(Rows<RT>& R, const u32 (&top)[RT], u32 most) {
+DISC_DEV bool uneven_queries(const u32 (&top)[RT], u32 most) {
+  const int e = (int)(most >> 7);
+  bool uneven = e > 200;
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) uneven |= far_below(top[rt], e);
+  return !DISC_T_F16 && uneven;
+}
+DISC_DEV float power(int e) { return __builtin_bit_cast(float, (u32)(127 + e) << 23); }    // 2^e, -126 .. 127
+template <int RT>
+DISC_DEV void halve_query(Rows<RT>& R, const u32 (&top)[RT], u32 most, bool uneven) {
 #if !DISC_T_F16
-  // (by biased exponents: the largest one's, which 0 has none of; 2^(142 - e), or the largest there is)
-  const auto down_of = [](int e) { return __builtin_bit_cast(float, (u32)min(269 - e, 254) << 23); };
-  const int e = max((int)(most >> 7), 1);
-  const float down = down_of(e);
-  bool uneven = false;
+  const int e = (int)(most >> 7);
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
-    const int own = (int)(top[rt] >> 7);
-    const bool apart = top[rt] != 0 && own + 16 < e;
-    const float own_down = apart ? down_of(max(own, 1)) : down;
-    R.row[rt] = down / own_down;
-    uneven |= apart;
+    const int up = up_of(far_below(top[rt], e) ? (int)(top[rt] >> 7) : e);
+    const float f = power(up);
+    R.row[rt] = (DISC_STORAGE == 1 ? 9 : 0) - up;           // (and 1 / kCode)
 #pragma unroll
     for (int i = 0; i < kNK * (kKE / 8); ++i)
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
         const u32 x = R.q[rt][i][w];
-        const f16x2 y = {(_Float16)(__builtin_bit_cast(float, x << 16) * own_down), (_Float16)(__builtin_bit_cast(float, x & 0xffff0000u) * own_down)};
+        const f16x2 y = {(_Float16)(__builtin_bit_cast(float, x << 16) * f), (_Float16)(__builtin_bit_cast(float, x & 0xffff0000u) * f)};
         R.q[rt][i][w] = __builtin_bit_cast(u32, y);
       }
   }
-  R.uneven = __ballot(uneven);
-  R.factor *= 1.f / down;
+  R.uneven = uneven;
+  if (uneven) return;
+  R.factor *= 1.f / power(up_of(e));
 #endif
   R.factor *= 1.f / kCode;
+}
+// bf16 queries for keys that are codes in bf16: rows from 2^100 on, whose products with codes would pass 32 bits where those
+// with the keys do not, are taken times 2^-64.
+template <int RT>
+DISC_DEV void lower_query(Rows<RT>& R, const u32 (&top)[RT]) {
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    const bool large = top[rt] >= (227u << 7) && top[rt] < 0x7f80u;
+    R.row[rt] = large ? 64 : 0;
+    R.uneven |= __ballot(large) != 0;
+#pragma unroll
+    for (int i = 0; i < kNK * (kKE / 8); ++i)
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const u32 x = R.q[rt][i][w];
+        const float a = __builtin_bit_cast(float, x << 16) * 0x1p-64f, b = __builtin_bit_cast(float, x & 0xffff0000u) * 0x1p-64f;
+        const u32 y = (__builtin_bit_cast(u32, a) >> 16) | (__builtin_bit_cast(u32, b) & 0xffff0000u);
+        R.q[rt][i][w] = large ? y : x;
+      }
+  }
 }
 
 // Rows of the pages of the tokens [begin, end), for a kv head, into LDS, by `of` threads.
@@ -1074,10 +1106,11 @@ DISC_DEV void attend_body(const AttendArgs& A) {
     Rows<1> R;
     clear_rows<1>(R);
     load_query<1>(R, 0, n < rows ? A.q + b * A.q_row + head * A.q_head : nullptr);
-    if (kQuantised && (!kNt || DISC_T_F16)) {
+    if (kQuantised) {
       u32 top[1];
       const u32 largest = largest_queries<1>(R, top);
-      halve_query<1>(R, top, largest);
+      if (!kNt || DISC_T_F16) halve_query<1>(R, top, largest, __ballot(uneven_queries<1>(top, largest)) != 0);
+      else lower_query<1>(R, top);
     }
     const int most = kMostPages << A.shift;
     bool ahead = kWays == 4 && A.prefix_inline;                // the prefix, in front of the sequence's own
@@ -1188,7 +1221,7 @@ struct PrefixTile {
 extern "C" __global__ void __launch_bounds__(512, 2) disc_prefix_k(AttendArgs A) {
   __shared__ PrefixTile tiles[2];
   __shared__ u32 pages[kMostPages + 1];
-  __shared__ u32 tops[8];
+  __shared__ u32 tops[8], uneven[8];
   const int lane = threadIdx.x & 63, w = wavefront(), n = lane & 15, g = lane >> 4;
   // (blocks of the same chunk and kv head are a multiple of eight apart where there are that many: on one XCD)
   const int all = A.batch * A.group, per = A.prefix_parts * A.kv_heads;
@@ -1210,7 +1243,12 @@ extern "C" __global__ void __launch_bounds__(512, 2) disc_prefix_k(AttendArgs A)
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < 8; ++i) largest = max(largest, tops[i]);
-    halve_query<kPrefixRT>(R, top, largest);
+    uneven[w] = __ballot(uneven_queries<kPrefixRT>(top, largest)) != 0;
+    __syncthreads();
+    u32 some = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) some |= uneven[i];
+    halve_query<kPrefixRT>(R, top, largest, __builtin_amdgcn_readfirstlane(some) != 0);
   }
   const bool keys = w < kPrefixSteps, values = !keys && w < 2 * kPrefixSteps;
   const int step = keys ? w : w - kPrefixSteps;               // this wavefront's share of a tile

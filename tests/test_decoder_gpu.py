@@ -828,3 +828,25 @@ def test_attention_with_the_workspace_of_a_larger_call(ctx, dtype, storage, D, b
         got = _run(cache, s, workspace=held[:need])[0]
         _check(cache, dtype, storage, s, 1.0 / math.sqrt(D), got=got)
         assert (held[need:] == 7).all()
+
+
+@pytest.mark.parametrize("storage,D", [("i8", 128), ("e4m3", 64)])
+@pytest.mark.parametrize("batch,prefix,longest", [(3, 0, 300), (600, 0, 40), (40, 1500, 40), (300, 2500, 40), (300, 0, 3000)])
+def test_queries_of_the_largest_rows_beside_large_keys(ctx, storage, D, batch, prefix, longest):
+    """Rows as large as the type has beside ordinary ones whose scores come of small queries and large keys, or the other way:
+    the powers of two that they are brought to are taken back row by row."""
+    cache = _cache(ctx, "bf16", storage, D)
+    lengths = [int(x) for x in torch.randint(1, longest, (batch,), generator=torch.Generator().manual_seed(4))]
+    for up in (2.0 ** 20, 2.0 ** 90, 2.0 ** -60):
+        s = _setup("bf16", storage, D, 2, 4, 16, lengths, prefix, _generator(71 + batch))
+        s["pages"][2] *= up
+        s["q"] /= up
+        want, *sizes = plain.attend(s["q"], s["lengths"], s["table"], s["pages"], 1.0 / math.sqrt(D), s["prefix_table"], s["prefix"])
+        bound = _attend_bound("bf16", storage, s, want, *sizes, 1.0 / math.sqrt(D))
+        odd = torch.zeros(s["q"].shape[:2], dtype=torch.bool, device="cuda")
+        odd[0, 1::4] = odd[batch - 1] = True
+        s["q"][odd] = torch.finfo(torch.bfloat16).max
+        got = _run(cache, s)[0]
+        _inside(got[~odd], want[~odd], bound[~odd], f"queries of 2^{-math.log2(up):.0f} beside the largest")
+        if up < 1.0:                                               # (their own scores are numbers of 32 bits here)
+            assert torch.isfinite(got).all()
