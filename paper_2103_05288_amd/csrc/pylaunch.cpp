@@ -313,7 +313,9 @@ PyObject* cache_attend(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   if (a[15] != Py_None) {
     int64_t d;
     uint64_t count, size;
-    if (!number(PyObject_CallMethodNoArgs(a[15], s_get_device), &d) || d != c.device || !call_u64(a[15], s_data_ptr, &ws) ||
+    PyObject* whole = PyObject_CallMethodNoArgs(a[15], s_is_contiguous);     // (elements may share memory otherwise)
+    Py_XDECREF(whole);
+    if (whole != Py_True || !number(PyObject_CallMethodNoArgs(a[15], s_get_device), &d) || d != c.device || !call_u64(a[15], s_data_ptr, &ws) ||
         !call_u64(a[15], s_numel, &count) || !call_u64(a[15], s_element_size, &size))
       return does_not_fit();
     bytes = count * size;

@@ -262,4 +262,6 @@ class CacheHandle(_Handle):
             inputs.append(prefix_table)
         if workspace is not None and workspace.get_device() != self._device:
             _refuse(f"the workspace is on {workspace.device}, the context on device {self._device}")
+        if workspace is not None and not workspace.is_contiguous():
+            _refuse(f"the workspace has strides {workspace.stride()}, a dense tensor is wanted")
         self._call(self._attend, [batch, heads, kv_heads, count, page_size, width, prefix_length, prefix_width, a, b, c, d], inputs, [out], workspace, stream)

@@ -272,6 +272,18 @@ def test_attention_calls(ctx, path):
     raw("16-byte", "INVALID_ARG", i=ins[:4] + [pages[1].data_ptr() + 4] + ins[5:])
 
 
+def test_a_workspace_that_is_not_dense_is_refused(ctx, path):
+    """Its elements are fewer bytes than it says (expanded), or not all its own (every other one)."""
+    h = ctx.register_cache("bf16", 16, "i8")
+    q, out = (torch.zeros(3, 4, 16, dtype=torch.bfloat16) for _ in range(2))
+    need = h.workspace_bytes(3, 4, 2, 1600)
+    call = lambda ws: h.attend(q, torch.zeros(3, dtype=torch.int32), torch.zeros(3, 200, dtype=torch.int32), _pages(), out, workspace=ws)  # noqa: E731
+    _refused("INVALID_ARG", HOST_ONLY, lambda: call(torch.zeros(need, dtype=torch.uint8)))
+    _refused("INVALID_ARG", HOST_ONLY, lambda: call(torch.zeros(need // 8, 2)))
+    for ws in (torch.zeros(1).expand(need), torch.zeros(2 * need, dtype=torch.uint8)[::2], torch.zeros(64, 1).expand(64, need // 4), torch.zeros(64, need).t()):
+        _refused("INVALID_ARG", "dense", lambda: call(ws))
+
+
 def test_attention_of_more_threads_than_a_launch_has(ctx):
     """Less than 2^32 threads a launch: 2^24 blocks of 256, 2^23 of the prefix's 512, are refused before anything is enqueued."""
     h = ctx.register_cache("bf16", 16, "i8")
