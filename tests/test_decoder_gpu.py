@@ -850,3 +850,95 @@ def test_queries_of_the_largest_rows_beside_large_keys(ctx, storage, D, batch, p
         _inside(got[~odd], want[~odd], bound[~odd], f"queries of 2^{-math.log2(up):.0f} beside the largest")
         if up < 1.0:                                               # (their own scores are numbers of 32 bits here)
             assert torch.isfinite(got).all()
+
+
+# ---- more of what the documents allow --------------------------------------------------------------
+
+
+def test_rotary_in_place_leaves_the_heads_between(ctx):
+    """In place, queries and keys of one product's rows: the values and whatever else lies between them keep their bits."""
+    from paper_2103_05288_amd import rotary_frequencies
+    for dtype, D, R, layout in (("bf16", 128, 128, "half"), ("f16", 80, 26, "interleaved"), ("f32", 64, 64, "half")):
+        frequencies, _ = rotary_frequencies(R)
+        h = ctx.register_rotary(dtype, D, frequencies, layout=layout)
+        rows = _normal((131, 9, D), TYPES[dtype], _generator(91))
+        before = rows.clone()
+        positions = torch.arange(131, device="cuda") * 7
+        h.launch(positions, [rows[:, 1:4], rows[:, 5:7]], [rows[:, 1:4], rows[:, 5:7]])
+        for i in (0, 4, 7, 8):
+            assert torch.equal(_bits(rows[:, i]), _bits(before[:, i]))
+        for part in (slice(1, 4), slice(5, 7)):
+            want = plain.rotary(before[:, part], positions, frequencies, layout)
+            _inside(rows[:, part], want, _rotary_bound(before[:, part], positions, frequencies, layout, 1.0, TYPES[dtype], want), "rotary")
+
+
+def test_attention_of_stretches_of_more_pages_than_a_block_keeps(ctx):
+    """1024 pages are staged at a time: so many kv heads that a block has whole sequences of more, a prefix whose chunks end there,
+    and pages that are none behind that."""
+    cache = _cache(ctx, "bf16", "i8", 16)
+    kv, size = 1024, 8
+    g = _generator(95)
+    for lengths, prefix in (([9001, 300, 8193], 0), ([17, 40], 9003)):
+        s = _setup("bf16", "i8", 16, kv, 1, size, lengths, prefix, g)
+        where = s["prefix_table"] if prefix else s["table"][0]
+        where[[3, 1023, 1024, 1100]] = torch.tensor([-1, 10 ** 9, -7, s["pages"][0].shape[0]], dtype=torch.int32, device="cuda")
+        s["pages"][2] = torch.nan_to_num(s["pages"][2], nan=0.0, posinf=0.0, neginf=0.0)
+        _check(cache, "bf16", "i8", s, 0.25)
+        del s
+
+
+def test_the_step_of_a_token_captured(ctx):
+    """Rotation in place, store, attention behind a shared prefix and load in one graph; its inputs, slots, lengths and positions
+    change between the replays, with eager work in between, and every replay gives what eager calls give."""
+    from paper_2103_05288_amd import rotary_frequencies
+    D, kv, group, size, prefix, batch = 64, 2, 3, 16, 40, 5
+    H = kv * group
+    rotary = ctx.register_rotary("bf16", D, rotary_frequencies(D)[0])
+    cache = _cache(ctx, "bf16", "e4m3", D)
+    g = _generator(97)
+    shape = (3 + 3 * batch, kv, size, D)
+    table = torch.arange(3, 3 + 3 * batch, device="cuda", dtype=torch.int32).view(batch, 3)
+    prefix_table = torch.arange(3, device="cuda", dtype=torch.int32)
+    filled = _filled("bf16", "e4m3", shape[0], kv, size, D, g)
+    ws = torch.empty(max(16, cache.workspace_bytes(batch, H, kv, 3 * size, prefix)), dtype=torch.uint8, device="cuda")
+
+    def inputs(turn):
+        n = torch.tensor([(5 * turn + 11 * b) % 47 for b in range(batch)], device="cuda")
+        page = table.long()[torch.arange(batch, device="cuda"), n // size]
+        return {"qkv": _normal((batch, H + 2 * kv, D), torch.bfloat16, _generator(200 + turn)), "positions": n + prefix, "slots": page * size + n % size,
+                "lengths": (n + 1).int()}
+
+    def step(x, pages, out, back):
+        q, k, v = x["qkv"][:, :H], x["qkv"][:, H:H + kv], x["qkv"][:, H + kv:]
+        rotary.launch(x["positions"], [q, k], [q, k])
+        cache.store([k, v], x["slots"], pages)
+        cache.attend(q, x["lengths"], table, pages, out, workspace=ws, prefix_table=prefix_table, prefix_length=prefix)
+        cache.load(x["slots"], pages, back)
+
+    static, pages = inputs(0), [p.clone() for p in filled]
+    out = torch.empty((batch, H, D), dtype=torch.bfloat16, device="cuda")
+    back = [torch.empty((batch, kv, D), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    step(static, pages, out, back)                             # (nothing is compiled or looked up within the capture)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(static, pages, out, back)
+    for turn in range(5):
+        x = inputs(turn)
+        eager_pages, eager_out, eager_back = [p.clone() for p in filled], torch.empty_like(out), [torch.empty_like(b) for b in back]
+        for name, t in x.items():
+            static[name].copy_(t)
+        for a, b in zip(pages, filled):
+            a.copy_(b)
+        out.fill_(math.nan)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        step(x, eager_pages, eager_out, eager_back)
+        torch.cuda.synchronize()
+        assert torch.equal(out, eager_out) and torch.equal(static["qkv"], x["qkv"])
+        for a, b in zip(pages + back, eager_pages + eager_back):
+            assert torch.equal(_bits(a), _bits(b))
+        want, *sizes = plain.attend(x["qkv"][:, :H], x["lengths"], table, eager_pages, 0.125, prefix_table, prefix)
+        s = {"q": x["qkv"][:, :H], "prefix": prefix, "lengths": x["lengths"]}
+        _inside(out, want, _attend_bound("bf16", "e4m3", s, want, *sizes, 0.125), f"replay {turn}")
