@@ -288,7 +288,8 @@ int register_cache(disc_ctx* c, const disc_cache_desc* d, int32_t* id_out) {
   if (d->dtype != DISC_F16 && d->dtype != DISC_BF16) return refuse(c, DISC_ERR_INVALID_ARG, "a cache takes f16 or bf16 rows");
   if (d->storage < DISC_STORAGE_SAME || d->storage > DISC_STORAGE_E4M3) return refuse(c, DISC_ERR_INVALID_ARG, "bad storage");
   if (d->head_dim < 16 || d->head_dim > 256 || d->head_dim % 16) return refuse(c, DISC_ERR_SHAPE, "head_dim is a multiple of 16, 16 .. 256", d->head_dim);
-  if (!std::isfinite((float)(d->softmax_scale * 1.44269504088896340736)))
+  // (times 512 for fp16 queries over i8: what undoes the size of its codes in half precision)
+  if (!std::isfinite((float)(d->softmax_scale * 1.44269504088896340736 * (d->dtype == DISC_F16 && d->storage == DISC_STORAGE_I8 ? 512.0 : 1.0))))
     return refuse(c, DISC_ERR_INVALID_ARG, "softmax_scale is no finite number of 32 bits");
   const double scale = d->softmax_scale != 0.0 ? d->softmax_scale : 1.0 / std::sqrt((double)d->head_dim);
   std::string macros = "#define DISC_CACHE 1\n#define DISC_T_F16 " + std::to_string(d->dtype == DISC_F16 ? 1 : 0) + "\n";

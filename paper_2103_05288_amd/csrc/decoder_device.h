@@ -941,12 +941,12 @@ DISC_DEV u32 largest_queries(const Rows<RT>& R, u32 (&top)[RT]) {     // bits of
 // By biased exponents: 2^15 is brought to by 2^(142 - e), or the largest power of two there is; its exponent.
 DISC_DEV int up_of(int e) { return min(142 - max(e, 1), 127); }
 DISC_DEV bool far_below(u32 top, int e) { return top != 0 && (int)(top >> 7) + 16 < e; }
-// Whether some row of this lane's asks for its own (or the largest is so large that its power of two and the softmax scale
-// might have no product).
+// Whether some row of this lane's asks for its own (or the largest, or the softmax scale, is so large that its power of two
+// and the scale might have no product).
 template <int RT>
 DISC_DEV bool uneven_queries(const u32 (&top)[RT], u32 most) {
   const int e = (int)(most >> 7);
-  bool uneven = e > 200;
+  bool uneven = e > 200 || DISC_SCALE_LOG2E > 0x1p60 || DISC_SCALE_LOG2E < -0x1p60;
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) uneven |= far_below(top[rt], e);
   return !DISC_T_F16 && uneven;

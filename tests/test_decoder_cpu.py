@@ -86,6 +86,15 @@ def test_registrations_that_are_refused(ctx):
     assert lib.disc_register_cache(ctx.h, C.byref(desc), C.byref(out)) == -1
 
 
+def test_softmax_scales_at_the_end_of_32_bits(ctx):
+    """... where i8's codes take 2^9 of them from fp16 queries."""
+    ctx.register_cache("f16", 64, "i8", softmax_scale=4e35)
+    _refused("INVALID_ARG", "softmax", lambda: ctx.register_cache("f16", 64, "i8", softmax_scale=5e35))
+    _refused("INVALID_ARG", "softmax", lambda: ctx.register_cache("f16", 64, "i8", softmax_scale=-5e35))
+    ctx.register_cache("bf16", 64, "i8", softmax_scale=5e35)
+    ctx.register_cache("f16", 64, softmax_scale=2e38)
+
+
 def test_frequencies():
     f, m = pkg.rotary_frequencies(8, base=10000.0)
     assert m == 1.0 and f == [10000.0 ** (-j / 4) for j in range(4)]

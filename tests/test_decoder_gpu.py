@@ -942,3 +942,16 @@ def test_the_step_of_a_token_captured(ctx):
         want, *sizes = plain.attend(x["qkv"][:, :H], x["lengths"], table, eager_pages, 0.125, prefix_table, prefix)
         s = {"q": x["qkv"][:, :H], "prefix": prefix, "lengths": x["lengths"]}
         _inside(out, want, _attend_bound("bf16", "e4m3", s, want, *sizes, 0.125), f"replay {turn}")
+
+
+def test_attention_with_the_largest_softmax_scales(ctx):
+    """Queries and keys so small that their scores are ordinary ones again."""
+    for dtype, storage, D, scale in (("bf16", "i8", 64, 2.0 ** 119), ("bf16", "e4m3", 64, 2.0 ** 120), ("f16", "i8", 64, 2.0 ** 40), ("bf16", "bf16", 64, -(2.0 ** 100))):
+        cache = ctx.register_cache(dtype, D, storage, softmax_scale=scale / math.sqrt(D))
+        s = _setup(dtype, storage, D, 2, 4, 16, [200, 33, 1, 90], 150, _generator(99))
+        if storage in STORED:
+            s["pages"][2] /= abs(scale)
+        else:
+            s["pages"][0] = (s["pages"][0].float() / abs(scale)).to(TYPES[dtype])
+        want, *sizes = plain.attend(s["q"], s["lengths"], s["table"], s["pages"], scale / math.sqrt(D), s["prefix_table"], s["prefix"])
+        _inside(_run(cache, s)[0], want, _attend_bound(dtype, storage, s, want, *sizes, abs(scale) / math.sqrt(D)), f"softmax scale {scale:g}")
