@@ -50,13 +50,14 @@ constexpr int64_t kAttendStreamBytes = 128 << 20;
 constexpr int kUnit = 128;              // tokens that a block's four wavefronts take at once
 constexpr int64_t kDirectTokens = 512;  // sequences no longer than this are one chunk each (kDirectPages of the smallest size)
 // A prefix no longer than this is gone through by every sequence's own block, where these run all at once: nothing is joined
-// then (us, joined / in line, by the bytes of a row: 128 bytes 32 sequences of 100, 8 heads, behind 300 14.9 / 11.1, behind 500
-// 15.0 / 12.1; 256 bytes behind 200 15.1 / 10.8, but 120 of 64 behind 500 15.1 / 19.9; 512 bytes behind 200 15.1 / 17.8).
+// then (us, joined / in line, 8 heads, by the bytes of a row: 128 bytes 32 sequences of 100 behind 300 11.5 / 10.1, behind 500
+// 11.6 / 10.9, but 90 of 64 behind 500 16.7 / 19.5; 256 bytes 32 of 100 behind 200 11.7 / 9.6, behind 500 12.0 / 11.8, 90 of 64
+// 16.6 / 24.6; 512 bytes 20 of 100 behind 200 12.9 / 14.8).
 constexpr int64_t inline_tokens(int64_t row_bytes) { return row_bytes <= 128 ? 512 : row_bytes <= 256 ? 256 : 0; }
 // disc_attend_k has the prefix too, 16 query rows a block, up to so many of their units of 128 tokens: a launch less, but
 // keys and values are read, and codes brought into the operands' form, once for 16 rows and not for 256 (us, there / in
-// disc_prefix_k: 64 sequences of 32 and 8 heads x 128 behind 1000 tokens 21 / 31, behind 4000 31 / 41, 16000 59 / 53 of
-// 8-bit rows, 24 / 31, 40 / 41 and 90 / 63 of 16-bit ones, which take two products where codes take one).
+// disc_prefix_k: 64 sequences of 32 and 8 heads x 128 behind 1000 tokens 19 / 30, behind 4000 30 / 40, 16000 61 / 52 of
+// 8-bit rows, 21 / 28, 38 / 38 and 88 / 58 of 16-bit ones, which take two products where codes take one).
 constexpr int64_t kFewUnits8 = 6144, kFewUnits16 = 4096;
 
 enum { FN_ROTARY = 0, FN_ROTARY_NT, FN_ROTARY_COUNT };
@@ -434,8 +435,8 @@ int plan_attend(disc_ctx* c, const Operator& o, const int64_t* d, int n_dims, bo
   const int64_t at_once = cus * o.resident;
   a.target = (int32_t)(at_once / per > 1 ? at_once / per : 1);
   int64_t parts = batch + a.target;
-  // (16-bit rows above 128: where the blocks are few, two steps more cost more than the join, 8 blocks of 500 tokens x 256
-  // 15.5 us joined / 18.4 as one chunk each, 16 17.0 / 18.2, 120 25.5 / 19.7; 8-bit ones 15.5 / 15.0, 16.2 / 14.9, 19.8 / 15.4)
+  // (16-bit rows above 128: where the blocks are few, two steps more cost more than the join, 8 or 16 blocks of 500 tokens x
+  // 256 14.4 us joined / 16.0 as one chunk each, 120 20.0 / 18.3; 8-bit ones 14.2 / 12.8, 18.0 / 13.7)
   const int64_t direct_tokens = o.head_dim <= 128 || o.storage != DISC_STORAGE_SAME || times(batch, per) >= cus / 4 || one_chunk ? kDirectTokens : kDirectTokens / 2;
   if ((width << shift) <= direct_tokens) {
     a.direct = 1;
@@ -443,7 +444,8 @@ int plan_attend(disc_ctx* c, const Operator& o, const int64_t* d, int n_dims, bo
   }
   a.prefix_inline = prefix > 0 && a.direct && prefix <= inline_tokens(o.head_dim * (o.storage != DISC_STORAGE_SAME ? 1 : 2)) && times(batch, per) <= at_once;
   // Keys and values go past the caches where they are more than those keep until the next step, and one block reads
-  // them (us, through them / past them: 562 MB 117 / 108, 235 MB 53 / 49, 70 MB 27.6 / 29.2).
+  // them (us, through them / past them, four caches in turn: i8 549 MB 108 / 101, 230 55 / 54, 137 40 / 40, 70 30 / 32; bf16
+  // 553 MB 110 / 98, 234 56 / 52, 141 42 / 40, 74 18 / 20).  By what the tables and the pages hold: the lengths are the device's.
   const int64_t own = times(std::min(d[3], times(batch, width)) << shift, kv * 2 * o.head_dim * (o.storage != DISC_STORAGE_SAME ? 1 : 2));
   p->nt = a.tiles == 1 && !a.prefix_inline && (own < 0 || own >= kAttendStreamBytes);
   const int64_t rows = batch * a.group;

@@ -330,8 +330,8 @@ extern "C" __global__ void __launch_bounds__(256) disc_load_nt_k(RowsArgs A) { l
 // A block is four wavefronts; they take the steps of a stretch of tokens in turn and join in LDS at its end.
 // The stretches are cut from the lengths, on the device, so that all blocks have the same share.
 //
-// Long caches are bound by their reads: 64 sequences of up to 8192 tokens (8 kv heads of 128, i8) 107 us, 5.3 TB/s; two of
-// 131072 (bf16) 117 us, 5.7 TB/s.  Short ones by the chain lengths -> page table -> first rows -> end, about 5 us, and by the
+// Long caches are bound by their reads: 64 sequences of up to 8192 tokens (8 kv heads of 128, i8) 101 us, 5.5 TB/s; two of
+// 131072 (bf16) 116 us, 5.7 TB/s.  Short ones by the chain lengths -> page table -> first rows -> end, about 5 us, and by the
 // joining launch, 4 to 8 us: one sequence of 300 5.9 us, four of 4000 17.
 // =================================================================================================
 constexpr int kStep = 32;                     // tokens of a step
@@ -494,10 +494,9 @@ DISC_DEV void chunks_of(const AttendArgs& A, int b, int& chunk, int& count) {
   }
 }
 
-// Products in half precision: the second where the values are codes (or fp16), the first where they are and `kHalf`.
-template <bool kHalf>
+// Products: in half precision over codes and fp16, else in bf16.
 DISC_DEV f32x4 mfma(u32x4 a, u32x4 b, f32x4 c) {
-  if (kHalf || DISC_T_F16) return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+  if (kQuantised || DISC_T_F16) return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 #if !DISC_T_F16
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(Tx8, a), __builtin_bit_cast(Tx8, b), c, 0, 0, 0);
 #else
@@ -522,26 +521,15 @@ DISC_DEV u32 half_of_codes(u32 x) {                            // of the low byt
   return __builtin_bit_cast(u32, __builtin_elementwise_fma(__builtin_bit_cast(f16x2, x), scale, offset));
 }
 
-// Eight neighbouring codes (two registers) of a key, in half precision or bf16.  (bf16 takes 96 operations for a step's
-// keys, half precision 72.  Kernels that stream a long cache past the caches are slower all the same with the latter, by
-// back-to-back passes and not under a profiler: 118 us against 108, 64 x 8192 tokens.)
-template <bool kHalf>
+// Eight neighbouring codes (two registers) of a key.  (In half precision, 72 operations for a step's keys; bf16 queries are
+// brought to it once.  As bf16 numbers they take 96: 64 x 8192 i8 of heads of 128, 64 and 80 109, 66 and 96 us, where this
+// takes 106, 62 and 91; e4m3 of 128 and 256 100 and 103, here 100 and 105.)
 DISC_DEV u32x4 keys_of_codes(u32 a, u32 b) {
   u32x4 r;
 #pragma unroll
   for (int w = 0; w < 2; ++w) {
-    const u32 x = (w ? b : a) ^ (kHalf ? kBias : 0u);
-    if (!kHalf && DISC_STORAGE == 2) {
-      r[2 * w] = __builtin_bit_cast(u32, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)x, 1.f, false));
-      r[2 * w + 1] = __builtin_bit_cast(u32, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)x, 1.f, true));
-    } else if (!kHalf) {
-      float f[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) f[e] = (float)(signed char)(x >> (8 * e));
-      // (a code has eight significant bits at most: the upper half of its 32-bit form is exact)
-      r[2 * w] = __builtin_amdgcn_perm(__builtin_bit_cast(u32, f[1]), __builtin_bit_cast(u32, f[0]), 0x07060302u);
-      r[2 * w + 1] = __builtin_amdgcn_perm(__builtin_bit_cast(u32, f[3]), __builtin_bit_cast(u32, f[2]), 0x07060302u);
-    } else if (DISC_STORAGE == 2) {
+    const u32 x = (w ? b : a) ^ kBias;
+    if (DISC_STORAGE == 2) {
       r[2 * w] = half_of_floats<false>(x);
       r[2 * w + 1] = half_of_floats<true>(x);
     } else {
@@ -662,7 +650,7 @@ DISC_DEV float max_of_groups(float x) {      // over the four lane groups that s
   return fmaxf(x, __shfl_xor(x, 32));
 }
 
-template <int RT, bool kHalf>
+template <int RT>
 DISC_DEV void scores(const Rows<RT>& R, const Keys& K, f32x4 (&s)[RT][2]) {
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt)
@@ -674,13 +662,13 @@ DISC_DEV void scores(const Rows<RT>& R, const Keys& K, f32x4 (&s)[RT][2]) {
     for (int i = 0; i < kNK; ++i) {
       if (!kQuantised) {
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt) s[rt][mt] = mfma<false>(K.k[mt][i], R.q[rt][i], s[rt][mt]);
+        for (int rt = 0; rt < RT; ++rt) s[rt][mt] = mfma(K.k[mt][i], R.q[rt][i], s[rt][mt]);
       } else {
 #pragma unroll
         for (int f = 0; f < 2; ++f) {
-          const u32x4 k = keys_of_codes<kHalf>(K.k[mt][i][2 * f], K.k[mt][i][2 * f + 1]);
+          const u32x4 k = keys_of_codes(K.k[mt][i][2 * f], K.k[mt][i][2 * f + 1]);
 #pragma unroll
-          for (int rt = 0; rt < RT; ++rt) s[rt][mt] = mfma<kHalf>(k, R.q[rt][(i * 2 + f) % (kNK * (kKE / 8))], s[rt][mt]);
+          for (int rt = 0; rt < RT; ++rt) s[rt][mt] = mfma(k, R.q[rt][(i * 2 + f) % (kNK * (kKE / 8))], s[rt][mt]);
         }
       }
     }
@@ -839,8 +827,8 @@ DISC_DEV void accumulate(Rows<RT>& R, const f32x4 (&s)[RT][2], Values& V, int li
       const u32x4 v = column_of(V, n, i);
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt) {
-        R.o[rt][n * kE + i] = mfma<kQuantised>(v, hi[rt], R.o[rt][n * kE + i]);
-        if (kSplit) R.o[rt][n * kE + i] = mfma<kQuantised>(v, lo[rt], R.o[rt][n * kE + i]);
+        R.o[rt][n * kE + i] = mfma(v, hi[rt], R.o[rt][n * kE + i]);
+        if (kSplit) R.o[rt][n * kE + i] = mfma(v, lo[rt], R.o[rt][n * kE + i]);
       }
     }
 }
@@ -863,7 +851,7 @@ DISC_DEV void attend_tokens(const AttendArgs& A, const u32* rows, float* scales,
     f32x4 s[RT][2];
     const int n = end - (t0 + g * 8);
     const int live = !there || n <= 0 ? 0 : n < 8 ? n : 8;
-    scores<RT, !kNt || DISC_T_F16>(R, K, s);
+    scores<RT>(R, K, s);
     // (this wavefront's 64 floats of LDS: the lanes' eight tokens' scales from the lanes that read them)
     float ks[8], vs[8];
     if (kQuantised) scales[lane] = lane < 32 ? scale * R.factor : scale;
@@ -975,26 +963,6 @@ DISC_DEV void halve_query(Rows<RT>& R, const u32 (&top)[RT], u32 most, bool unev
   R.factor *= 1.f / power(up_of(e));
 #endif
   R.factor *= 1.f / kCode;
-}
-// bf16 queries for keys that are codes in bf16: rows from 2^100 on, whose products with codes would pass 32 bits where those
-// with the keys do not, are taken times 2^-64.
-template <int RT>
-DISC_DEV void lower_query(Rows<RT>& R, const u32 (&top)[RT]) {
-#pragma unroll
-  for (int rt = 0; rt < RT; ++rt) {
-    const bool large = top[rt] >= (227u << 7) && top[rt] < 0x7f80u;
-    R.row[rt] = large ? 64 : 0;
-    R.uneven |= __ballot(large) != 0;
-#pragma unroll
-    for (int i = 0; i < kNK * (kKE / 8); ++i)
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        const u32 x = R.q[rt][i][w];
-        const float a = __builtin_bit_cast(float, x << 16) * 0x1p-64f, b = __builtin_bit_cast(float, x & 0xffff0000u) * 0x1p-64f;
-        const u32 y = (__builtin_bit_cast(u32, a) >> 16) | (__builtin_bit_cast(u32, b) & 0xffff0000u);
-        R.q[rt][i][w] = large ? y : x;
-      }
-  }
 }
 
 // Rows of the pages of the tokens [begin, end), for a kv head, into LDS, by `of` threads.
@@ -1109,8 +1077,7 @@ DISC_DEV void attend_body(const AttendArgs& A) {
     if (kQuantised) {
       u32 top[1];
       const u32 largest = largest_queries<1>(R, top);
-      if (!kNt || DISC_T_F16) halve_query<1>(R, top, largest, __ballot(uneven_queries<1>(top, largest)) != 0);
-      else lower_query<1>(R, top);
+      halve_query<1>(R, top, largest, __ballot(uneven_queries<1>(top, largest)) != 0);
     }
     const int most = kMostPages << A.shift;
     bool ahead = kWays == 4 && A.prefix_inline;                // the prefix, in front of the sequence's own
@@ -1168,7 +1135,7 @@ DISC_DEV void attend_body(const AttendArgs& A) {
     }
     if (n < rows) {
       const bool alone = I.whole && A.prefix_parts == 0;
-      // (the sum is 2^kBase or more where it is not 0: its reciprocal is rounded to 32 bits, of which the result keeps 11 at most)
+      // (the sum is 2^(kBase - 1) or more where it is not 0: its reciprocal is rounded to 32 bits, of which the result keeps 11 at most)
       const float inverse = 1.f / kCode / l;
       const i64 at = shared ? prefix_row(A, part, b, head) : part_row(A, A.direct ? b : part + b, head);
       T* out = A.out + b * A.o_row + head * A.o_head;
@@ -1189,9 +1156,10 @@ DISC_DEV void attend_body(const AttendArgs& A) {
     __syncthreads();                      // (what was handed over is still being read)
   }
 }
-// (wavefronts a SIMD by the registers that they take; 16-bit rows of 256 do not fit 256: 31 spilled ones cost 60 us where one
-// wavefront takes 36, four sequences of 15000; heads of up to 48 have the tiles of 128, three wavefronts and none spilled 39 us,
-// four 52, 64 sequences of 4000 x 32)
+// (wavefronts a SIMD by the registers that they take, few of which are spilled: 2 to 4 of 168 over 16-bit rows of 128, outside
+// the loop over tokens; 16-bit rows of 256 do not fit 256: 31 spilled ones cost 60 us where one wavefront takes 36, four
+// sequences of 15000; heads of up to 48 have the tiles of 128, three wavefronts and none spilled 39 us, four 52, 64 sequences
+// of 4000 x 32)
 constexpr int kWavesPerSimd = kD <= 64 && kND <= 4 ? 4 : kD <= 128 ? 3 : kQuantised ? 2 : 1;
 #define DISC_ATTEND(NAME, WAYS, NT) \
   extern "C" __global__ void __launch_bounds__(256, kWavesPerSimd) NAME(AttendArgs A) { attend_body<WAYS, NT>(A); }
@@ -1206,9 +1174,10 @@ DISC_ATTEND(disc_attend1_nt_k, 1, true)
 // has 16 x RT rows of its own, and all go through the same tokens.  A tile of them is read once a block, brought into
 // the matrix operands' form -- codes to 16-bit numbers, values transposed -- and kept in LDS in the order in which a
 // wavefront reads an operand (16 bytes a lane, one row after the other); the next tile's loads are in flight
-// meanwhile, and two tiles take turns.  1024 rows x 16384 tokens x 8 heads of 128, i8: 93 to 96 us, 0.73 PFLOP/s.  Bound by
-// issue: the matrix cores are busy for 30 % of the cycles, the vector ALU for 47 % (sixteen powers of two at a quarter of
-// the rate, and what goes round them, a step), little of it at once; wavefronts wait for 30 % of their time.
+// meanwhile, and two tiles take turns.  1024 rows x 16384 tokens x 8 heads of 128, i8: 98 to 100 us, 0.69 PFLOP/s (bf16 and
+// fp16, twice the second product: 127 to 130).  Bound by issue: the matrix cores are busy for 29 % of the cycles, the vector ALU
+// for 49 % (sixteen powers of two at a quarter of the rate, and what goes round them, a step), little of it at once; wavefronts
+// wait for 33 % of their time.  Of heads of 256 and over e4m3 up to 5 registers of 256 are spilled.
 constexpr int kPrefixRT = kD <= 128 ? 2 : 1;
 constexpr int kPrefixSteps = kD <= 128 ? 4 : 2;               // steps of a tile
 constexpr int kNF = kNK * (kKE / 8);                          // operands of a step's keys, a 16-row tile
@@ -1289,8 +1258,8 @@ extern "C" __global__ void __launch_bounds__(512, 2) disc_prefix_k(AttendArgs A)
           if (!kQuantised) {
             T.k[step][mt * kNF + i][lane] = (u32x4){x[0], x[1], x[2], x[3]};
           } else {
-            T.k[step][mt * kNF + 2 * i][lane] = keys_of_codes<true>(x[0], x[1]);
-            T.k[step][mt * kNF + (2 * i + 1) % kNF][lane] = keys_of_codes<true>(x[2], x[3]);
+            T.k[step][mt * kNF + 2 * i][lane] = keys_of_codes(x[0], x[1]);
+            T.k[step][mt * kNF + (2 * i + 1) % kNF][lane] = keys_of_codes(x[2], x[3]);
           }
         }
       if (kQuantised && lane < kStep) T.ks[step * kStep + lane] = scale * R.factor;
@@ -1338,7 +1307,7 @@ extern "C" __global__ void __launch_bounds__(512, 2) disc_prefix_k(AttendArgs A)
 #pragma unroll
           for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
-            for (int rt = 0; rt < kPrefixRT; ++rt) x[rt][mt] = mfma<kQuantised>(kf[mt * kNF + i], R.q[rt][i], x[rt][mt]);
+            for (int rt = 0; rt < kPrefixRT; ++rt) x[rt][mt] = mfma(kf[mt * kNF + i], R.q[rt][i], x[rt][mt]);
       };
       read_keys(0);
       score(0);
@@ -1365,8 +1334,8 @@ extern "C" __global__ void __launch_bounds__(512, 2) disc_prefix_k(AttendArgs A)
           const u32x4 v = T.v[st][d][lane];
 #pragma unroll
           for (int rt = 0; rt < kPrefixRT; ++rt) {
-            R.o[rt][d] = mfma<kQuantised>(v, hi[rt], R.o[rt][d]);
-            if (kSplit) R.o[rt][d] = mfma<kQuantised>(v, lo[rt], R.o[rt][d]);
+            R.o[rt][d] = mfma(v, hi[rt], R.o[rt][d]);
+            if (kSplit) R.o[rt][d] = mfma(v, lo[rt], R.o[rt][d]);
           }
         }
       }
@@ -1402,7 +1371,7 @@ extern "C" __global__ void __launch_bounds__(512, 2) disc_prefix_k(AttendArgs A)
 
 // Joins the chunks of a sequence and of the prefix, for a (sequence, query head) a wavefront, or where the rows are few
 // and their chunks many, a block.  The chunks' maxima and sums are read 64 at a time, a lane each, so that the reads
-// of the results themselves do not wait for each other.  A chain of trips to memory, 4 to 8 us: more wavefronts a row do not
+// of the results themselves do not wait for each other.  A chain of trips to memory, 3 to 12 us: more wavefronts a row do not
 // shorten it (sixteen 8.2 us where four take 7.1).
 extern "C" __global__ void __launch_bounds__(256) disc_join_k(AttendArgs A) {
   __shared__ float so[4][kD], sm[4], sl[4];
