@@ -801,12 +801,16 @@ DISC_DEV void split(const f32x4 (&s)[RT][2], u32x4 (&hi)[RT], u32x4 (&lo)[RT]) {
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
       const float a = s[rt][w / 2][(2 * w) % 4], b = s[rt][w / 2][(2 * w + 1) % 4];
-      const Px2 h = {(P)a, (P)b};
-      hi[rt][w] = __builtin_bit_cast(u32, h);
+      const Px2 both = {(P)a, (P)b};
+      u32 x = __builtin_bit_cast(u32, both);
       if (kSplit) {
-        const Px2 r = {(P)(a - (float)h[0]), (P)(b - (float)h[1])};
+        // (What is left of the very numbers that are multiplied: the compiler may form another (P)a from what `a` is a product
+        // of, which is rounded once and differs now and then by a unit of its last place, and `lo` by as much.)
+        asm("" : "+v"(x));
+        const Px2 h = __builtin_bit_cast(Px2, x), r = {(P)(a - (float)h[0]), (P)(b - (float)h[1])};
         lo[rt][w] = __builtin_bit_cast(u32, r);
       }
+      hi[rt][w] = x;
     }
 }
 

@@ -955,3 +955,13 @@ def test_attention_with_the_largest_softmax_scales(ctx):
             s["pages"][0] = (s["pages"][0].float() / abs(scale)).to(TYPES[dtype])
         want, *sizes = plain.attend(s["q"], s["lengths"], s["table"], s["pages"], scale / math.sqrt(D), s["prefix_table"], s["prefix"])
         _inside(_run(cache, s)[0], want, _attend_bound(dtype, storage, s, want, *sizes, abs(scale) / math.sqrt(D)), f"softmax scale {scale:g}")
+
+
+@pytest.mark.parametrize("dtype,storage,D", [("f16", "i8", 64), ("f16", "e4m3", 256), ("f16", "f16", 80), ("bf16", "bf16", 128)])
+def test_attention_weights_of_two_numbers(ctx, dtype, storage, D):
+    """A hundred thousand weights, of which a few are close to half way between two 16-bit numbers: the second number is what is
+    left of the first, of every one."""
+    cache = _cache(ctx, dtype, storage, D)
+    s = _shaped(dtype, storage, D, 8, 16, 8, [2 + i % 3 for i in range(260)], 0, "plain", 0, _generator(103))
+    want, bound = _own_sum_bound(dtype, storage, s, 1.0 / math.sqrt(D))
+    _inside(_run(cache, s)[0], want, bound, "weights")
