@@ -482,6 +482,75 @@ int disc_cache_attend(disc_ctx* ctx, int32_t id, const int64_t* dims, int n_dims
  * for the largest batch and the longest prefix and table that it will have. */
 int disc_cache_workspace_bytes(disc_ctx* ctx, int32_t id, const int64_t* dims, int n_dims, size_t* out);
 
+/* ---- a decoder's step outside its attention -------------------------------------------------------
+ * Registered and launched as the operators above, with the same conventions (stream, errors, capture into a HIP graph,
+ * nothing allocated, a launch of nothing is a success).  Rows are `row stride` elements apart, the elements of a row next
+ * to each other; tensors of another form are dense.  Results share no memory with operands but where it says so. */
+typedef struct {
+  int32_t dtype;          /* DISC_F32, DISC_F16 or DISC_BF16: x, residual, total, weight and the gradients of rows  */
+  int32_t storage;        /* DISC_STORAGE_I8 or DISC_STORAGE_E4M3: the codes                                       */
+  double eps;             /* positive                                                                             */
+  double weight_offset;   /* added to the weight (1 for models that keep it around 0)                              */
+} disc_norm_desc;
+int disc_register_norm(disc_ctx* ctx, const disc_norm_desc* desc, int32_t* id_out);
+/* disc_norm: s = x + residual (32 bits), total = s rounded, y = s (weight + weight_offset) / sqrt(mean(s^2) + eps), and y
+ * as codes with a scale for its row: scale a / Q, code round(y Q / a) to nearest, ties to even, a the row's largest |y|, Q = 127 or
+ * 448.  A row whose y are all zero has the scale 0; one with an infinity or a NaN (in s, or in y where the weight holds one) gets
+ * the scale NaN and codes of 0.  What y is computed from is s before its rounding.
+ * dims = {rows, width (1 .. 32768; fp32: 16384), row stride of x, residual, total, codes}; inputs = {x, weight [width]} and
+ * with a residual {.., residual}; outputs = {codes, scales fp32 [rows]} and with a residual {.., total}.  total may be x or residual
+ * (with the same strides).  No workspace. */
+int disc_norm(disc_ctx* ctx, int32_t id, const int64_t* dims, int n_dims, const void* const* inputs, int n_in, void* const* outputs, int n_out,
+              void* workspace, size_t workspace_bytes, void* hip_stream);
+/* disc_norm_backward: the gradient of y's and total's consumers back to x and residual (the same for both) and to the weight.
+ * The rounding to codes counts as the identity.  With r = 1 / sqrt(mean(s^2) + eps) of s = total, u = r s and g = dy (weight +
+ * weight_offset): dx = r (g - u mean(g u)) + dtotal, dweight = sum over the rows of dy u (fp32, overwritten; zeros without rows).
+ * dims = {rows, width, row stride of total, dy, dtotal, dx}; inputs = {total, weight, dy} and where there is one {.., dtotal};
+ * outputs = {dx, dweight fp32 [width]}.  dx may be total, dy or dtotal (with the same strides).  Sums are in a fixed order.
+ * `workspace`: disc_norm_workspace_bytes (of the same dims, or of more rows), 16-byte aligned; launches that may overlap in
+ * time each need their own. */
+int disc_norm_backward(disc_ctx* ctx, int32_t id, const int64_t* dims, int n_dims, const void* const* inputs, int n_in, void* const* outputs,
+                       int n_out, void* workspace, size_t workspace_bytes, void* hip_stream);
+int disc_norm_workspace_bytes(disc_ctx* ctx, int32_t id, const int64_t* dims, int n_dims, size_t* out);
+
+typedef struct {
+  int32_t dtype;          /* DISC_F16 or DISC_BF16: results, scales of the weights, bias, and x unless it is 8-bit   */
+  int32_t rows;           /* disc_storage of x: DISC_STORAGE_SAME, or codes with a scale for every row              */
+  int32_t group;          /* 32, 64 or 128 neighbouring elements of a row of weights share a scale                  */
+  int32_t zeros;          /* != 0: and a zero point; 0: the zero point is 8                                         */
+} disc_linear4_desc;
+int disc_register_linear4(disc_ctx* ctx, const disc_linear4_desc* desc, int32_t* id_out);
+/* disc_linear4: out[m, j] = row_scale[m] sum_i x[m, i] scale[j, i / group] (code[j, i] - zero[j, i / group]) + bias[j], products and sums in
+ * 32 bits or more, rounded once.  Made for few rows, as a step of a batch has them: 64 rows are one pass over the weights.
+ * dims = {rows, n, k (a multiple of the group), row stride of x, of out}; inputs = {x, weights, scales [n, k / group]}, with 8-bit rows
+ * {.., row_scales fp32 [rows]}, with zero points {.., zeros, one byte each [n, k / group]}, and where there is one {.., bias [n]};
+ * outputs = {out}.  weights: [n, k / 2] bytes, 16-byte aligned, element 2i in the lower four bits of byte i, 2i + 1 in the upper.
+ * Rows do not see each other: a row with an infinity or a NaN has results that are no finite numbers, and the others keep theirs.
+ * No workspace. */
+int disc_linear4(disc_ctx* ctx, int32_t id, const int64_t* dims, int n_dims, const void* const* inputs, int n_in, void* const* outputs, int n_out,
+                 void* workspace, size_t workspace_bytes, void* hip_stream);
+
+typedef struct {
+  int32_t dtype;          /* DISC_F32, DISC_F16 or DISC_BF16: the probabilities                                     */
+} disc_verify_desc;
+int disc_register_verify(disc_ctx* ctx, const disc_verify_desc* desc, int32_t* id_out);
+/* disc_verify: which of the drafted tokens a target model keeps, and the token behind them, so that the tokens follow the
+ * target's distribution.  Of sequence b with n = lengths[b] drafted tokens (taken into 0 .. drafts; without lengths: drafts), token i
+ * is kept while uniform[b, i] draft[b, i, token] < target[b, i, token] (without draft probabilities, the draft's are 1 for its token and 0
+ * elsewhere; a token outside the vocabulary is not kept).  With a = accepted[b] tokens kept, the next one is drawn with
+ * uniform[b, drafts]: the first token whose running sum of weights is above uniform times their sum.  The weights are max(target - draft, 0)
+ * at place a where a < n (target where these are all zero), target[b, n] where a = n; what is negative, infinite or NaN counts
+ * as 0, and where nothing is left the token is -1.  tokens[b] = the kept ones, that one, then -1.
+ * Comparisons, differences and sums are in 64 bits, in a fixed order.  Uniforms are in [0, 1).
+ * dims = {batch, drafts (0 .. 4096), vocabulary, sequence stride, place stride of target, sequence stride, place stride of draft,
+ * draft != 0, lengths != 0}; inputs = {target [batch, drafts + 1, vocabulary], drafted int32 [batch, drafts], uniforms fp32 [batch, drafts + 1]}
+ * and where the last dims say so {.., draft [batch, drafts, vocabulary]}, {.., lengths int32 [batch]}; outputs = {tokens int32
+ * [batch, drafts + 1], accepted int32 [batch]}.  `workspace`: disc_verify_workspace_bytes (of the same dims, or of a larger batch or
+ * vocabulary), 16-byte aligned; launches that may overlap in time each need their own. */
+int disc_verify(disc_ctx* ctx, int32_t id, const int64_t* dims, int n_dims, const void* const* inputs, int n_in, void* const* outputs, int n_out,
+                void* workspace, size_t workspace_bytes, void* hip_stream);
+int disc_verify_workspace_bytes(disc_ctx* ctx, int32_t id, const int64_t* dims, int n_dims, size_t* out);
+
 int disc_get_stats(disc_ctx* ctx, disc_stats_t* out);
 
 /* Measurement helpers (not part of the method): a plain 16-byte-vector device copy used as the

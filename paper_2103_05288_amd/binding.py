@@ -82,6 +82,18 @@ class disc_cache_desc(C.Structure):
     _fields_ = [("dtype", C.c_int32), ("storage", C.c_int32), ("head_dim", C.c_int32), ("softmax_scale", C.c_double)]
 
 
+class disc_norm_desc(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("storage", C.c_int32), ("eps", C.c_double), ("weight_offset", C.c_double)]
+
+
+class disc_linear4_desc(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("rows", C.c_int32), ("group", C.c_int32), ("zeros", C.c_int32)]
+
+
+class disc_verify_desc(C.Structure):
+    _fields_ = [("dtype", C.c_int32)]
+
+
 class DiscError(RuntimeError):
     def __init__(self, code: int, message: str):
         super().__init__(f"DISC_ERR_{STATUS.get(code, code)}: {message}")
@@ -96,7 +108,8 @@ EXPORTS = ("disc_create", "disc_destroy", "disc_last_error", "disc_register_patt
            "disc_static_scratch_init", "disc_launch_static_scratch",
            "disc_get_stats", "disc_util_copy", "disc_util_copy_nt", "disc_util_empty_launch", "disc_util_mix", "disc_register_graph", "disc_graph_info",
            "disc_graph_workspace_bytes", "disc_graph_launch", "disc_register_rotary", "disc_rotary", "disc_register_cache", "disc_cache_store",
-           "disc_cache_load", "disc_cache_attend", "disc_cache_workspace_bytes")
+           "disc_cache_load", "disc_cache_attend", "disc_cache_workspace_bytes", "disc_register_norm", "disc_norm", "disc_norm_backward",
+           "disc_norm_workspace_bytes", "disc_register_linear4", "disc_linear4", "disc_register_verify", "disc_verify", "disc_verify_workspace_bytes")
 
 _lib = None
 _pylaunch = None        # the per-call part in C (csrc/pylaunch.cpp), loaded with the library
@@ -191,8 +204,13 @@ def load_library():
     lib.disc_util_mix.argtypes = [vp, C.c_int, C.c_int, C.c_int, C.c_int, vp, vp, vp, C.c_size_t, vp]
     lib.disc_register_rotary.argtypes = [vp, C.POINTER(disc_rotary_desc), i32p]
     lib.disc_register_cache.argtypes = [vp, C.POINTER(disc_cache_desc), i32p]
-    lib.disc_cache_workspace_bytes.argtypes = [vp, C.c_int32, i64p, C.c_int, C.POINTER(C.c_size_t)]
-    for launch in (lib.disc_rotary, lib.disc_cache_store, lib.disc_cache_load, lib.disc_cache_attend):
+    lib.disc_register_norm.argtypes = [vp, C.POINTER(disc_norm_desc), i32p]
+    lib.disc_register_linear4.argtypes = [vp, C.POINTER(disc_linear4_desc), i32p]
+    lib.disc_register_verify.argtypes = [vp, C.POINTER(disc_verify_desc), i32p]
+    for size in (lib.disc_cache_workspace_bytes, lib.disc_norm_workspace_bytes, lib.disc_verify_workspace_bytes):
+        size.argtypes = [vp, C.c_int32, i64p, C.c_int, C.POINTER(C.c_size_t)]
+    for launch in (lib.disc_rotary, lib.disc_cache_store, lib.disc_cache_load, lib.disc_cache_attend, lib.disc_norm, lib.disc_norm_backward,
+                   lib.disc_linear4, lib.disc_verify):
         launch.argtypes = lib.disc_launch.argtypes
     _lib = lib
     return lib
@@ -379,6 +397,42 @@ class Context:
         oid = C.c_int32(-1)
         self._check(self.lib.disc_register_cache(self.h, C.byref(desc), C.byref(oid)))
         return CacheHandle(self, oid.value, dtype, int(head_dim), storage)
+
+    def register_norm(self, dtype: str, storage: str = "i8", eps: float = 1e-6, offset: float = 0.0):
+        """The root-mean-square norm of rows of dtype ("f32", "f16" or "bf16") with the residual's addition, its result as codes ("i8" or
+        "e4m3") with a scale for every row; `offset` is added to the weight."""
+        from .decoder import STORAGE_IDS
+        from .step import NormHandle
+        if dtype not in DTYPE_IDS or storage not in STORAGE_IDS:
+            raise DiscError(-1, f"no such type or storage: {dtype!r}, {storage!r}")
+        desc = disc_norm_desc(DTYPE_IDS[dtype], STORAGE_IDS[storage], float(eps), float(offset))
+        oid = C.c_int32(-1)
+        self._check(self.lib.disc_register_norm(self.h, C.byref(desc), C.byref(oid)))
+        return NormHandle(self, oid.value, dtype, storage)
+
+    def register_linear4(self, dtype: str, group: int = 128, rows: Optional[str] = None, zeros: bool = False):
+        """Products of few rows with 4-bit weights, `group` (32, 64 or 128) of which share a scale, into rows of dtype ("f16" or "bf16").
+        rows: "i8" or "e4m3" where x is codes with a scale for every row, None or the type itself where it is of that type.
+        zeros: every group has a zero point of its own (else 8)."""
+        from .decoder import STORAGE_IDS
+        from .step import Linear4Handle
+        rows = dtype if rows is None else rows
+        if dtype not in DTYPE_IDS or (rows != dtype and rows not in STORAGE_IDS):
+            raise DiscError(-1, f"no such type or storage: {dtype!r}, {rows!r}")
+        desc = disc_linear4_desc(DTYPE_IDS[dtype], STORAGE_IDS.get(rows, 0), int(group), 1 if zeros else 0)
+        oid = C.c_int32(-1)
+        self._check(self.lib.disc_register_linear4(self.h, C.byref(desc), C.byref(oid)))
+        return Linear4Handle(self, oid.value, dtype, int(group), rows, bool(zeros))
+
+    def register_verify(self, dtype: str):
+        """The check of drafted tokens against the target's probabilities of dtype ("f32", "f16" or "bf16")."""
+        from .step import VerifyHandle
+        if dtype not in DTYPE_IDS:
+            raise DiscError(-1, f"no such type: {dtype!r}")
+        desc = disc_verify_desc(DTYPE_IDS[dtype])
+        oid = C.c_int32(-1)
+        self._check(self.lib.disc_register_verify(self.h, C.byref(desc), C.byref(oid)))
+        return VerifyHandle(self, oid.value, dtype)
 
     def pattern_info(self, pid: int) -> dict:
         info = disc_pattern_info_t()

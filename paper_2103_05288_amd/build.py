@@ -16,9 +16,9 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libdisc.so")
 PYLAUNCH = os.path.join(HERE, "_pylaunch" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
-SOURCES = ["checker.cpp", "codegen.cpp", "runtime.cpp", "decoder.cpp"]
+SOURCES = ["checker.cpp", "codegen.cpp", "runtime.cpp", "decoder.cpp", "step.cpp"]
 # device headers that become strings of the library: file -> the string's name
-EMBEDDED = {"disc_device.h": "kDeviceHeader", "decoder_device.h": "kDecoderHeader"}
+EMBEDDED = {"disc_device.h": "kDeviceHeader", "decoder_device.h": "kDecoderHeader", "step_device.h": "kStepHeader"}
 
 
 def _embed_header(build_dir: str) -> str:

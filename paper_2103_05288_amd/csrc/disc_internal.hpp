@@ -282,18 +282,18 @@ int analyze(const disc_op* ops, int n_ops, const disc_constraint* cs, int n_cs, 
 int generate(const Analysis& an, const std::string& prefix, Generated* out, std::string* err,
              const GenOptions* opt = nullptr);
 
-// decoder.cpp: an operator of its own device code (rotary positions, a cache of keys and values), compiled once
-// at registration like a pattern.  `fn` by the numbers of its kind's kernels.
+// decoder.cpp, step.cpp: an operator of its own device code (rotary positions, a cache of keys and values, a norm, products
+// with 4-bit weights, the check of drafted tokens), compiled once at registration like a pattern.  `fn` by the numbers of its kind's kernels.
 struct Operator {
-  enum Kind { ROTARY, CACHE } kind = ROTARY;
+  enum Kind { ROTARY, CACHE, NORM, LINEAR4, VERIFY } kind = ROTARY;
   std::string key;                 // what the registration was made of
-  int dtype = 0, storage = 0, head_dim = 0, rotary_dim = 0, layout = 0;
+  int dtype = 0, storage = 0, head_dim = 0, rotary_dim = 0, layout = 0, group = 0, zeros = 0;
   void* module = nullptr;          // hipModule_t
-  void* fn[16] = {};                // hipFunction_t
+  void* fn[24] = {};                // hipFunction_t
   int resident = 2;                // blocks of its main kernel that a CU holds at once
 };
 
-// runtime.cpp: what decoder.cpp and scratch.hip need of a context
+// runtime.cpp: what decoder.cpp, step.cpp and scratch.hip need of a context
 int context_device(const disc_ctx* ctx);
 int context_cus(const disc_ctx* ctx);
 int context_fail(disc_ctx* ctx, int code, const char* msg);

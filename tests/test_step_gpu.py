@@ -1,0 +1,449 @@
+"""The norm into 8-bit rows and its gradient, products with 4-bit weights and the check of drafted tokens on the GPU,
+against 64 bits (oracle/step.py), at the sizes, strides and values where they can go wrong."""
+import math
+
+import pytest
+import torch
+
+from oracle import step as plain
+
+pytestmark = pytest.mark.gpu
+
+TYPES = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+STORED = {"i8": torch.int8, "e4m3": torch.float8_e4m3fn}
+EPS = 1e-5
+UNIT = 2.0 ** -24          # half a step of 32 bits
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    from paper_2103_05288_amd import Context
+    c = Context(0)
+    yield c
+    torch.cuda.synchronize()
+    c.close()
+
+
+def _half_step(dtype):
+    return torch.finfo(dtype).eps / 2
+
+
+def _least(dtype):
+    """Half a step of the smallest numbers."""
+    return torch.finfo(dtype).tiny * torch.finfo(dtype).eps / 2
+
+
+def _generator(seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return g
+
+
+def _normal(shape, dtype, g, std=1.0):
+    return torch.empty(shape, dtype=torch.float32, device="cuda").normal_(0.0, std, generator=g).to(dtype)
+
+
+def _channels(shape, dtype, g):
+    size = torch.empty(shape[-1], dtype=torch.float32, device="cuda").normal_(0.0, 0.5, generator=g).exp_()
+    size[::97] *= 12
+    return (torch.empty(shape, dtype=torch.float32, device="cuda").normal_(0.0, 1.0, generator=g) * size).to(dtype)
+
+
+def _inside(got, want, bound, what):
+    off = (got.double() - want).abs()
+    bad = ~(off <= bound)
+    assert not bad.any(), f"{what}: {int(bad.sum())} of {off.numel()} values outside the bound, worst {float((off - bound).max()):.3g} over it"
+
+
+def _apart(rows, width, dtype, fill=0):
+    """[rows, width] inside a wider tensor (all of `fill`): the view and the whole."""
+    size = torch.empty((), dtype=dtype).element_size()
+    whole = torch.full((rows, (width + 5) * size), fill, dtype=torch.uint8, device="cuda").view(dtype)
+    return whole[:, 2:2 + width], whole
+
+
+# ---- the norm --------------------------------------------------------------------------------------
+
+
+def _check_codes(codes, scales, y, largest, storage, what):
+    """Scale: s and weight + offset a half step of 32 bits each, their product, the quotient's and the result's own (and the
+    64-bit sums): 6.  Code: the same, the quotient Q / a and the product with it, 8, and its own half step."""
+    most = plain.MOST[storage]
+    bad = torch.isnan(largest)
+    assert torch.equal(torch.isnan(scales), bad), what
+    assert (codes[bad].float() == 0).all(), what
+    fine = ~bad
+    _inside(scales[fine], largest[fine] / most, 6 * UNIT * largest[fine] / most + 2.0 ** -149, what + " scales")
+    zero = fine & (largest == 0)
+    assert (codes[zero].float() == 0).all() and (scales[zero] == 0).all()
+    some = fine & (largest > 0)
+    # (what the code stands for, in units of the row's largest)
+    want = y[some] / largest[some].unsqueeze(-1) * most
+    got = codes[some].double()
+    half = torch.full_like(want, 0.5) if storage == "i8" else torch.maximum(want.abs() * 2.0 ** -4, torch.full_like(want, 2.0 ** -10))
+    _inside(got, want, half + 8 * UNIT * want.abs() + 2.0 ** -120, what + " codes")
+
+
+def _norm(ctx, dtype, storage, rows, width, offset, residual, seed, strided=True, x=None, weight=None, eps=EPS):
+    h = ctx.register_norm(dtype, storage, eps=eps, offset=offset)
+    g = _generator(seed)
+    t = TYPES[dtype]
+    x = _channels((rows, width), t, g) if x is None else x
+    weight = (1 - offset + _normal((width,), torch.float32, g, 0.2)).to(t) if weight is None else weight
+    if strided:
+        a, _ = _apart(rows, width, t, 255)
+        a.copy_(x)
+        x = a
+    codes, whole = _apart(rows, width, STORED[storage], 7) if strided else (torch.empty((rows, width), dtype=STORED[storage], device="cuda"), None)
+    scales = torch.full((rows,), -5.0, device="cuda")
+    more, total_whole = {}, None
+    if residual is not None:
+        total, total_whole = _apart(rows, width, t, 7) if strided else (torch.empty((rows, width), dtype=t, device="cuda"), None)
+        more = {"residual": residual, "total": total}
+    h.launch(x, weight, codes, scales, **more)
+    s, y, largest = plain.norm(x, weight, eps, offset, residual)
+    if residual is not None:
+        assert torch.equal(more["total"], (x.float() + residual.float()).to(t))
+    _check_codes(codes, scales, y, largest, storage, f"{dtype} {storage} {rows} x {width}")
+    for w, dt in ((whole, STORED[storage]), (total_whole, t)):
+        if w is not None:
+            size = torch.empty((), dtype=dt).element_size()
+            b = w.view(torch.uint8)
+            assert (b[:, :2 * size] == 7).all() and (b[:, (2 + width) * size:] == 7).all(), "written outside the rows"
+    return codes, scales, more.get("total")
+
+
+@pytest.mark.parametrize("dtype,storage", [("bf16", "i8"), ("bf16", "e4m3"), ("f16", "e4m3"), ("f32", "i8"), ("f32", "e4m3")])
+@pytest.mark.parametrize("rows,width", [(1, 1), (1, 4096), (3, 7), (5, 8), (33, 63), (17, 64), (130, 65), (9, 513), (300, 1001), (2, 1280), (7, 2049), (600, 4100), (3, 8192),
+                                        (300, 12288), (2, 16384)])
+def test_norm_matches_64_bits(ctx, dtype, storage, rows, width):
+    g = _generator(rows * width)
+    residual = _channels((rows, width), TYPES[dtype], g)
+    _norm(ctx, dtype, storage, rows, width, 0.0, residual, rows + width)
+    _norm(ctx, dtype, storage, rows, width, 1.0, None, rows + width + 1, strided=False)
+
+
+@pytest.mark.parametrize("dtype,storage,rows,width", [("bf16", "i8", 5, 32768), ("f16", "e4m3", 400, 32761), ("f32", "i8", 300, 16383)])
+def test_norm_of_the_widest_rows(ctx, dtype, storage, rows, width):
+    residual = _channels((rows, width), TYPES[dtype], _generator(3))
+    _norm(ctx, dtype, storage, rows, width, 0.0, residual, 4)
+
+
+@pytest.mark.parametrize("dtype,storage,rows,width", [("bf16", "e4m3", 4099, 4096), ("f32", "i8", 10007, 1003)])
+def test_norm_past_the_caches(ctx, dtype, storage, rows, width):
+    """More than 64 MiB: the version that goes past them."""
+    residual = _channels((rows, width), TYPES[dtype], _generator(5))
+    _norm(ctx, dtype, storage, rows, width, 1.0, residual, 6)
+
+
+@pytest.mark.parametrize("dtype,storage", [("bf16", "i8"), ("f32", "e4m3"), ("f16", "i8")])
+def test_norm_in_place(ctx, dtype, storage):
+    h = ctx.register_norm(dtype, storage, eps=EPS)
+    g = _generator(8)
+    t = TYPES[dtype]
+    for rows, width in ((1, 640), (70, 1000), (5, 9000)):
+        x, residual, weight = _channels((rows, width), t, g), _channels((rows, width), t, g), _normal((width,), t, g)
+        want = [torch.empty((rows, width), dtype=STORED[storage], device="cuda"), torch.empty(rows, device="cuda"), torch.empty_like(x)]
+        h.launch(x, weight, want[0], want[1], residual=residual, total=want[2])
+        for into in (0, 1):
+            a, b = x.clone(), residual.clone()
+            codes, scales = torch.empty_like(want[0]), torch.empty_like(want[1])
+            h.launch(a, weight, codes, scales, residual=b, total=(a, b)[into])
+            assert torch.equal((a, b)[into], want[2]) and torch.equal(codes.view(torch.uint8), want[0].view(torch.uint8)) and torch.equal(scales, want[1])
+            assert torch.equal((b, a)[into], (residual, x)[into])
+
+
+@pytest.mark.parametrize("dtype,storage", [("bf16", "i8"), ("bf16", "e4m3"), ("f32", "i8"), ("f32", "e4m3"), ("f16", "i8")])
+def test_norm_of_rows_at_the_ends_of_their_type(ctx, dtype, storage):
+    """Zeros, the smallest and the largest numbers, infinities and NaN, each beside ordinary rows (which stay what they are)."""
+    t = TYPES[dtype]
+    g = _generator(9)
+    for width in (40, 700, 5000):
+        x = _channels((16, width), t, g)
+        weight = (1 + _normal((width,), torch.float32, g, 0.2)).to(t)
+        big, small = torch.finfo(t).max, torch.finfo(t).tiny
+        x[1] = 0
+        x[3] = (torch.sign(x[3].float()) * big).to(t)
+        x[4] = big * 0.25
+        x[5] = small
+        x[6] = 0
+        x[6, width // 2] = small * 0.5
+        x[8, width - 1] = math.inf
+        x[9, 3] = -math.inf
+        x[10, width // 3] = math.nan
+        x[12] = (x[12].float() * small).to(t)
+        x[13, 0] = big
+        codes, scales, _ = _norm(ctx, dtype, storage, 16, width, 0.0, None, 10, x=x, weight=weight)
+        only = [0, 2, 7, 11, 14, 15]
+        again, those, _ = _norm(ctx, dtype, storage, 6, width, 0.0, None, 10, x=x[only].contiguous(), weight=weight)
+        assert torch.equal(codes[only].view(torch.uint8), again.contiguous().view(torch.uint8)) and torch.equal(scales[only], those)
+        if dtype != "f16":      # (products that pass 32 bits, and that fall below them)
+            for w in (2.0 ** 90, 2.0 ** -100):
+                _norm(ctx, dtype, storage, 16, width, 0.0, None, 11, x=x, weight=(weight.float() * w).to(t))
+        weight[5] = math.nan
+        _norm(ctx, dtype, storage, 3, width, 0.0, None, 12, x=x[:3].contiguous(), weight=weight)
+
+
+def test_norm_of_nothing(ctx):
+    h = ctx.register_norm("bf16", "i8")
+    x = torch.empty((0, 64), dtype=torch.bfloat16, device="cuda")
+    h.launch(x, torch.ones(64, dtype=torch.bfloat16, device="cuda"), torch.empty((0, 64), dtype=torch.int8, device="cuda"), torch.empty(0, device="cuda"))
+    dw = torch.full((64,), 3.0, device="cuda")
+    h.backward(x, torch.ones(64, dtype=torch.bfloat16, device="cuda"), x, x, dw)
+    assert (dw == 0).all()
+
+
+# ---- its gradient ----------------------------------------------------------------------------------
+
+
+def _backward(ctx, dtype, rows, width, offset, with_total, seed, strided=True, into=None, total=None, dy=None, weight=None):
+    h = ctx.register_norm(dtype, "i8", eps=EPS, offset=offset)
+    g = _generator(seed)
+    t = TYPES[dtype]
+    total = _channels((rows, width), t, g) if total is None else total
+    dy = _normal((rows, width), t, g, 0.1) if dy is None else dy
+    dtotal = _normal((rows, width), t, g, 0.1) if with_total else None
+    weight = (1 - offset + _normal((width,), torch.float32, g, 0.2)).to(t) if weight is None else weight
+    want, dweight, size, dsize = plain.norm_backward(total, weight, dy, EPS, offset, dtotal)
+    dx, whole = _apart(rows, width, t, 7) if strided else (torch.empty((rows, width), dtype=t, device="cuda"), None)
+    if into is not None:
+        dx = (total, dy, dtotal)[into]
+    dw = torch.full((width,), 9.0, device="cuda")
+    ws = torch.full((max(16, h.workspace_bytes(rows, width)),), 255, dtype=torch.uint8, device="cuda")
+    h.backward(total, weight, dy, dx, dw, dtotal=dtotal, workspace=ws)
+    # dx: u = h r two roundings and r's own, g = dy w two, k one and of its terms w's (relative to the mean of |g u|), u k five in all,
+    # g - u k six, times r eight, plus dtotal nine; and the result's own
+    _inside(dx, want, _half_step(t) * want.abs() + 9 * UNIT * size + _least(t) + 2.0 ** -149, f"dx {dtype} {rows} x {width}")
+    # dweight: three roundings of a term, and one for each sum that it goes through: the rows of a thread, then the parts
+    parts = ws.numel() // (4 * width)
+    steps = -(-rows // max(1, min(parts, rows))) + parts + 4
+    _inside(dw, dweight, (3 + min(steps, rows + 8)) * UNIT * dsize + 2.0 ** -149, f"dweight {dtype} {rows} x {width}")
+    if whole is not None and into is None:
+        size = torch.empty((), dtype=t).element_size()
+        assert (whole.view(torch.uint8)[:, :2 * size] == 7).all() and (whole.view(torch.uint8)[:, (2 + width) * size:] == 7).all()
+    return dx, dw
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("rows,width", [(1, 1), (1, 4096), (3, 7), (5, 8), (65, 63), (17, 64), (1300, 65), (9, 513), (700, 1001), (2, 1280), (7, 2049), (1100, 4100), (3, 8192), (600, 12288),
+                                        (2, 16384)])
+def test_norm_backward_matches_64_bits(ctx, dtype, rows, width):
+    _backward(ctx, dtype, rows, width, 0.0, True, rows + width)
+    _backward(ctx, dtype, rows, width, 1.0, False, rows + width + 1, strided=False)
+
+
+@pytest.mark.parametrize("dtype,rows,width", [("bf16", 5, 32768), ("f32", 300, 16383), ("bf16", 6001, 2048), ("f32", 9001, 640)])
+def test_norm_backward_of_wide_and_of_many_rows(ctx, dtype, rows, width):
+    _backward(ctx, dtype, rows, width, 0.0, True, 21)
+
+
+@pytest.mark.parametrize("into", [0, 1, 2])
+def test_norm_backward_in_place(ctx, into):
+    _backward(ctx, "bf16", 300, 1000, 0.0, True, 22, into=into)
+    _backward(ctx, "f32", 3, 9000, 1.0, True, 23, into=into)
+
+
+def test_norm_backward_of_the_largest_and_smallest_rows(ctx):
+    for dtype in ("f32", "bf16"):
+        t = TYPES[dtype]
+        g = _generator(24)
+        total = _channels((8, 600), t, g)
+        total[0] = (total[0].float() * 2.0 ** 115).to(t)
+        total[1] = torch.finfo(t).max
+        total[2] = 0
+        total[3] = (total[3].float() * 2.0 ** -120).to(t)
+        total[5] = (torch.sign(total[5].float()) * 2.0 ** 64).to(t)
+        _backward(ctx, dtype, 8, 600, 0.0, True, 25, total=total)
+
+
+def test_norm_backward_against_differences(ctx):
+    """The step of the unrounded norm along a direction, in 64 bits, and what the gradient says of it."""
+    g = _generator(26)
+    rows, width, offset = 7, 130, 1.0
+    h = ctx.register_norm("f32", "i8", eps=EPS, offset=offset)
+    x, weight, dy, dtotal = (_normal(s, torch.float32, g) for s in ((rows, width), (width,), (rows, width), (rows, width)))
+    dx, dw = torch.empty_like(x), torch.empty_like(weight)
+    h.backward(x, weight, dy, dx, dw, dtotal=dtotal, workspace=torch.empty(h.workspace_bytes(rows, width), dtype=torch.uint8, device="cuda"))
+
+    def loss(x, w):
+        return ((plain.norm(x, w, EPS, offset)[1] * dy.double()).sum() + (x * dtotal.double()).sum()).item()
+    for k in range(8):
+        a, b = (_normal(s, torch.float32, g).double() for s in ((rows, width), (width,)))
+        step = 1e-5
+        slope = (loss(x.double() + step * a, weight.double() + step * b) - loss(x.double() - step * a, weight.double() - step * b)) / (2 * step)
+        said = (dx.double() * a).sum() + (dw.double() * b).sum()
+        size = (dx.double() * a).abs().sum() + (dw.double() * b).abs().sum()
+        # (32-bit gradients: 16 half steps of each; the differences' own error, step^2 times the third derivative: below 1e-8 of the size)
+        assert abs(slope - said.item()) < (16 * UNIT + 1e-7) * size.item()
+
+
+def test_norm_backward_gives_the_same_sums_again(ctx):
+    a = _backward(ctx, "bf16", 3000, 700, 0.0, True, 27)
+    b = _backward(ctx, "bf16", 3000, 700, 0.0, True, 27)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+# ---- products with 4-bit weights -------------------------------------------------------------------
+
+
+def _linear_inputs(dtype, rows, group, zeros, bias, M, N, K, seed):
+    g = _generator(seed)
+    t = TYPES[dtype]
+    weights = torch.randint(0, 256, (N, K // 2), generator=g, device="cuda", dtype=torch.uint8)
+    scales = (torch.empty((N, K // group), device="cuda").normal_(0.0, 0.4, generator=g).exp_() * (0.4 / math.sqrt(K))).to(t)
+    more = {}
+    if zeros:
+        more["zeros"] = torch.randint(0, 16, (N, K // group), generator=g, device="cuda", dtype=torch.uint8)
+    if bias:
+        more["bias"] = _normal((N,), t, g)
+    x = _channels((M, K), torch.float32, g)
+    if rows == "same":
+        x = x.to(t)
+    else:
+        a = x.abs().amax(-1)
+        y = x * (plain.MOST[rows] / a)[:, None]
+        x = (y.round() if rows == "i8" else y.clamp(-448, 448)).to(STORED[rows])
+        more["row_scales"] = a / plain.MOST[rows]
+    return x, weights, scales, more
+
+
+def _linear_check(out, x, weights, scales, group, more, what):
+    """Sums of 32 bits: a group's elements, each step off by at most a step (2^-23) of what was summed so far with the
+    codes' 128; of the groups' results two roundings and one for each sum; the result's own half step."""
+    K = x.shape[1]
+    want, size = plain.linear4(x, weights, scales, group, more.get("zeros"), more.get("row_scales"), more.get("bias"))
+    t = out.dtype
+    steps = 2 * (group + 8) + K // group + 24
+    want_t = want.clamp(-torch.finfo(t).max, torch.finfo(t).max)
+    _inside(out, want_t, _half_step(t) * want.abs() + steps * UNIT * size + _least(t), what)
+    # (those are bounds of the worst case: over all values the roundings are one of the result's type)
+    if want.numel() > 200:
+        off = (out.double() - want_t).norm() / want_t.norm()
+        assert off < 1.05 * _half_step(t), f"{what}: {float(off):.3g} off in all"
+
+
+def _linear(ctx, dtype, rows, group, zeros, bias, M, N, K, seed, strided=True):
+    h = ctx.register_linear4(dtype, group=group, rows=None if rows == "same" else rows, zeros=zeros)
+    x, weights, scales, more = _linear_inputs(dtype, rows, group, zeros, bias, M, N, K, seed)
+    if strided:
+        a, _ = _apart(M, K, x.dtype, 127)
+        a.copy_(x)
+        x = a
+    out, whole = _apart(M, N, TYPES[dtype], 7) if strided else (torch.empty((M, N), dtype=TYPES[dtype], device="cuda"), None)
+    h.launch(x, weights, scales, out, **more)
+    _linear_check(out, x, weights, scales, group, more, f"{dtype} {rows} {group} {M} x {N} x {K}")
+    if whole is not None:
+        b = whole.view(torch.uint8)
+        assert (b[:, :4] == 7).all() and (b[:, (2 + N) * 2:] == 7).all(), "written outside the rows"
+    return out
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("rows", ["same", "i8", "e4m3"])
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("zeros", [False, True])
+def test_linear_matches_64_bits(ctx, dtype, rows, group, zeros):
+    for i, (M, N, blocks) in enumerate([(1, 16, 1), (1, 1, 3), (2, 33, 9), (16, 64, 8), (17, 100, 17), (5, 1003, 33), (32, 17, 64), (33, 48, 5), (64, 131, 31), (65, 20, 2), (150, 40, 40)]):
+        _linear(ctx, dtype, rows, group, zeros, bool(i % 2), M, N, blocks * group, 100 + i, strided=bool((i // 2) % 2))
+
+
+@pytest.mark.parametrize("dtype,rows,group,M,N,K", [("bf16", "same", 128, 1, 4096, 4096), ("f16", "same", 32, 1, 1000, 16384), ("bf16", "i8", 128, 16, 3001, 4096), ("bf16", "same", 64, 61, 2048, 8192),
+                                                    ("bf16", "same", 128, 5, 40000, 2048), ("f16", "e4m3", 64, 8, 20011, 1024), ("bf16", "same", 128, 3, 16, 65536), ("bf16", "i8", 32, 300, 512, 2048)])
+def test_linear_of_larger_sizes(ctx, dtype, rows, group, M, N, K):
+    _linear(ctx, dtype, rows, group, True, True, M, N, K, 7)
+
+
+# ---- drafted tokens --------------------------------------------------------------------------------
+
+
+def _verify_inputs(dtype, B, D, V, seed, near=0.8):
+    g = _generator(seed)
+    t = TYPES[dtype]
+    logits = _normal((B, D + 1, V), torch.float32, g, 2.0)
+    close = logits[:, :D] + _normal((B, D, V), torch.float32, g, near)
+    target, draft = torch.softmax(logits, -1).to(t), torch.softmax(close, -1).to(t)
+    drafted = (close - torch.empty_like(close).exponential_(generator=g).log_()).argmax(-1).to(torch.int32) if D else torch.empty((B, 0), dtype=torch.int32, device="cuda")
+    uniforms = torch.empty((B, D + 1), device="cuda").uniform_(0.0, 1.0, generator=g).clamp_(max=1 - 2.0 ** -24)
+    return target, drafted, uniforms, draft
+
+
+def _verify(ctx, dtype, target, drafted, uniforms, draft=None, lengths=None):
+    h = ctx.register_verify(dtype)
+    B, D = drafted.shape
+    tokens = torch.full((B, D + 1), -9, dtype=torch.int32, device="cuda")
+    accepted = torch.full((B,), -9, dtype=torch.int32, device="cuda")
+    ws = torch.full((max(16, h.workspace_bytes(B, target.shape[2])),), 255, dtype=torch.uint8, device="cuda")
+    h.launch(target, drafted, uniforms, tokens, accepted, draft=draft, lengths=lengths, workspace=ws)
+    want, kept = plain.verify(target, drafted, uniforms, draft, lengths)
+    assert torch.equal(accepted.cpu(), kept), (accepted.cpu(), kept)
+    assert torch.equal(tokens.cpu(), want), (tokens.cpu(), want)
+    return tokens, accepted
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("B,D,V", [(1, 4, 32000), (3, 1, 1), (5, 3, 7), (40, 8, 1003), (9, 12, 4096), (7, 5, 4097), (16, 0, 5000), (2, 70, 513), (3, 130, 40), (3, 2, 200001)])
+def test_verify_matches_64_bits(ctx, dtype, B, D, V):
+    target, drafted, uniforms, draft = _verify_inputs(dtype, B, D, V, B + D + V)
+    lengths = torch.randint(-1, D + 3, (B,), generator=_generator(1), device="cuda", dtype=torch.int32)
+    _verify(ctx, dtype, target, drafted, uniforms, draft)
+    _verify(ctx, dtype, target, drafted, uniforms, draft, lengths)
+    _verify(ctx, dtype, target, drafted, uniforms)
+    _verify(ctx, dtype, target, drafted, uniforms, None, lengths)
+
+
+def test_verify_strides(ctx):
+    """Rows of a larger tensor, sequences innermost in one and padded vocabularies in the other."""
+    target, drafted, uniforms, draft = _verify_inputs("f32", 6, 4, 5000, 31)
+    want = _verify(ctx, "f32", target, drafted, uniforms, draft)
+    wide = torch.full((5, 6, 5017), math.nan, device="cuda")
+    wide[:, :, 3:5003] = target.transpose(0, 1)
+    long = torch.full((6, 9, 5001), math.nan, device="cuda")
+    long[:, 2:6, 1:] = draft
+    got = _verify(ctx, "f32", wide.transpose(0, 1)[:, :, 3:5003], drafted, uniforms, long[:, 2:6, 1:])
+    assert torch.equal(got[0], want[0])
+
+
+def test_verify_at_the_borders(ctx):
+    """Uniforms of 0 and just below 1, equal and disjoint distributions, tokens without probability and outside the vocabulary,
+    rows without anything, infinities, NaN and negative numbers."""
+    B, D, V = 14, 3, 9000
+    target, drafted, uniforms, draft = _verify_inputs("f32", B, D, V, 33)
+    uniforms[0] = 0
+    uniforms[1] = 1 - 2.0 ** -24
+    draft[2] = target[2, :D]                              # all kept but for the uniforms' strictness; nothing left over
+    uniforms[2, 0] = 1.0                                  # (not kept: u q < p fails, and the rest is empty: the target's row)
+    target[3, :, : V // 2] = 0
+    draft[3, :, V // 2:] = 0
+    drafted[3] = 5                                        # the target has nothing there
+    drafted[4, 0], drafted[5, 1], drafted[6, 0] = -1, V, 2 ** 31 - 1
+    target[7] = 0
+    draft[7] = 0
+    target[8, :, 17] = math.nan
+    target[8, :, 18] = math.inf
+    target[8, :, 19] = -3.0
+    drafted[8] = 17
+    target[9] = 0
+    target[9, :, V - 1] = 1.0
+    target[10] = 0
+    target[10, :, 0] = 2.0 ** -126                        # (sums of a few of the smallest numbers)
+    target[10, :, 4500] = 2.0 ** -126
+    draft[11] = math.nan
+    uniforms[12, :D] = math.nan
+    target[13], draft[13] = 1.0 / V, 0.0                  # a draft that says that its token could not come: kept
+    _verify(ctx, "f32", target, drafted, uniforms, draft)
+    _verify(ctx, "f32", target, drafted, uniforms)
+
+
+def test_verify_follows_the_target(ctx):
+    """Many sequences of one place: the tokens that come out have the target's frequencies, whatever the draft's."""
+    V, B = 6, 20000
+    g = _generator(35)
+    p, q = torch.softmax(_normal((V,), torch.float32, g), 0), torch.softmax(_normal((V,), torch.float32, g), 0)
+    drafted = torch.multinomial(q, B, replacement=True, generator=g).to(torch.int32)[:, None]
+    uniforms = torch.empty((B, 2), device="cuda").uniform_(0, 1, generator=g).clamp_(max=1 - 2.0 ** -24)
+    h = ctx.register_verify("f32")
+    tokens, accepted = torch.empty((B, 2), dtype=torch.int32, device="cuda"), torch.empty(B, dtype=torch.int32, device="cuda")
+    h.launch(p.expand(B, 2, V), drafted, uniforms, tokens, accepted, draft=q.expand(B, 1, V), workspace=torch.empty(h.workspace_bytes(B, V), dtype=torch.uint8, device="cuda"))
+    share = torch.bincount(tokens[:, 0].long(), minlength=V).double() / B
+    assert ((share - p.double()).abs() < 5 * (p.double() * (1 - p.double()) / B).sqrt()).all()
+    assert (accepted.double().mean() - torch.minimum(p, q).double().sum()).abs() < 5 * 0.5 / math.sqrt(B)
