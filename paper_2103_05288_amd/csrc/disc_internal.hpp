@@ -288,8 +288,12 @@ struct Operator {
   enum Kind { ROTARY, CACHE, NORM, LINEAR4, VERIFY } kind = ROTARY;
   std::string key;                 // what the registration was made of
   int dtype = 0, storage = 0, head_dim = 0, rotary_dim = 0, layout = 0, group = 0, zeros = 0;
-  void* module = nullptr;          // hipModule_t
-  void* fn[24] = {};                // hipFunction_t
+  double eps = 0;
+  float offset = 0;
+  std::string code;                // what its device code is compiled from
+  void* module = nullptr;          // hipModule_t, the first operator's of the same code
+  bool owns_module = false;
+  void* fn[16] = {};                // hipFunction_t
   int resident = 2;                // blocks of its main kernel that a CU holds at once
 };
 

@@ -92,6 +92,16 @@ inline int enter(disc_ctx* c, std::unique_ptr<Operator> o, const std::string& ma
       *id_out = (int32_t)i;
       return DISC_OK;
     }
+  o->code = macros;
+  for (const auto& other : all)   // (compiled for another registration already, whose numbers are arguments of the kernels)
+    if (other->code == macros) {
+      o->module = other->module;
+      std::copy(std::begin(other->fn), std::end(other->fn), o->fn);
+      o->resident = other->resident;
+      *id_out = (int32_t)all.size();
+      all.push_back(std::move(o));
+      return DISC_OK;
+    }
   std::vector<char> code;
   const int rc = context_compile(c, macros + header, &code);
   if (rc) return rc;
@@ -106,6 +116,7 @@ inline int enter(disc_ctx* c, std::unique_ptr<Operator> o, const std::string& ma
       return refuse(c, DISC_ERR_HIP, "hipModuleLoadData failed");
     }
     o->module = m;
+    o->owns_module = true;
     for (int i = 0; i < n; ++i) {
       hipFunction_t f = nullptr;
       if (hipModuleGetFunction(&f, m, names[i]) != hipSuccess) {

@@ -141,7 +141,7 @@ struct disc_ctx {
   std::vector<std::unique_ptr<Pattern>> fused;   // row reduces of op graphs that take an operand transposed ...
   std::map<std::pair<int, int>, int> fused_of;   // ... by pattern and input: compiled once, shared by all graphs (-1: it could not be)
   std::map<std::string, int> cache;
-  std::vector<std::unique_ptr<Operator>> operators;   // decoder.cpp
+  std::vector<std::unique_ptr<Operator>> operators;   // decoder.cpp, step.cpp
   disc_stats_t stats{};
   int force_variant = -1;
   hipModule_t util_module = nullptr;
@@ -1508,7 +1508,7 @@ void disc_destroy(disc_ctx* ctx) {
     for (auto& p : ctx->fused)
       if (p->module) (void)hipModuleUnload(p->module);
     for (auto& o : ctx->operators)
-      if (o->module) (void)hipModuleUnload((hipModule_t)o->module);
+      if (o->owns_module) (void)hipModuleUnload((hipModule_t)o->module);
     if (ctx->util_module) (void)hipModuleUnload(ctx->util_module);
   }
   delete ctx;

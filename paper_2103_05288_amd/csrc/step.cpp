@@ -15,13 +15,17 @@ struct NormArgs {
   void *total, *codes, *scales;
   int64_t x_row, residual_row, total_row, codes_row, rows;
   int32_t width, lanes;
+  float offset, pad;
+  double eps;
 };
 struct NormBackwardArgs {
   const void *total, *weight, *dy, *dtotal;
   void *dx, *dweight;
   float* part;
   int64_t total_row, dy_row, dtotal_row, dx_row, rows;
-  int32_t width, lanes, parts, pad;
+  int32_t width, lanes, parts;
+  float offset;
+  double eps;
 };
 struct LinearArgs {
   const void *x, *weights, *scales, *row_scales, *zeros, *bias;
@@ -36,10 +40,42 @@ struct VerifyArgs {
   int32_t batch, drafts, vocabulary, chunks;
 };
 
-// the kernels of 1, 2, 4 and 8 accesses a thread, each through the caches and past them
-enum { FN_NORM = 0, FN_NORM_BACKWARD = 8, FN_NORM_JOIN = 16, FN_NORM_COUNT };
-enum { FN_LINEAR1 = 0, FN_LINEAR2, FN_LINEAR4, FN_LINEAR_COUNT };
-enum { FN_VERIFY_SUM = 0, FN_VERIFY_PICK, FN_VERIFY_COUNT };
+// the norm's kernels and its gradient's (with _nt behind: past the caches), and what joins the gradient's parts
+enum { FN_NORM_S1 = 0, FN_NORM_S4, FN_NORM_S4_NT, FN_NORM_4, FN_NORM_4_NT, FN_NORM_B1, FN_NORM_B4, FN_BACKWARD_S1, FN_BACKWARD_S4, FN_BACKWARD_S4_NT, FN_BACKWARD_4,
+       FN_BACKWARD_4_NT, FN_BACKWARD_B4, FN_NORM_JOIN, FN_NORM_COUNT };
+struct LinearKernel {
+  const char* name;
+  int m, n, rows, split, teams;   // tiles of 16 rows of x and of weights, rows of a tile of x, wavefronts of a team, teams of a block
+};
+#define LINEAR_KERNEL(M, N, R, S, W, B) {"disc_linear_" #M "_" #N "_" #R "_" #S "_" #W "_" #B "_k", M, N, R, S, W}
+constexpr LinearKernel kLinear[] = {
+    LINEAR_KERNEL(1, 1, 1, 1, 8, 2),
+    LINEAR_KERNEL(1, 1, 1, 16, 1, 2),
+    LINEAR_KERNEL(1, 1, 1, 8, 1, 2),
+    LINEAR_KERNEL(1, 2, 1, 8, 1, 2),
+    LINEAR_KERNEL(1, 1, 4, 1, 8, 2),
+    LINEAR_KERNEL(1, 1, 4, 8, 1, 2),
+    LINEAR_KERNEL(1, 2, 4, 8, 1, 2),
+    LINEAR_KERNEL(1, 1, 16, 8, 1, 2),
+    LINEAR_KERNEL(1, 4, 16, 4, 1, 2),
+    LINEAR_KERNEL(2, 2, 16, 8, 1, 2),
+    LINEAR_KERNEL(4, 2, 16, 4, 1, 2),
+};
+#undef LINEAR_KERNEL
+constexpr int kLinearCount = sizeof kLinear / sizeof kLinear[0];
+// Which of them.  A team's wavefronts share a row's elements: 256 each at a time.  (us, the first four by rows x k x n:
+//  1 x 512 x 32768 4.4, 16.1, 7.4, 6.2; 1 x 1024 x 32768 6.3, 17.1, 8.0, 7.2; 1 x 4096 x 4096 9.3, 4.8, 4.9, 5.8;
+//  1 x 16384 x 1024 49, 8.8, 9.4, 14; 1 x 4096 x 12288 18, 12.9, 9.4, 10.5; 1 x 8192 x 131072 140, 168, 126, 112;
+//  of 16 rows 16 x 4096 x 4096 8.0, 13; 16 x 512 x 32768 8.8, 5.4; 10 x 2048 x 20000 13.8, 11.5.)
+int linear_kernel(int64_t rows, int64_t n, int64_t k, int64_t cus) {
+  const int64_t tiles = ceil_div(n, 16);
+  if (rows > 32) return 10;
+  if (rows > 16) return 9;
+  if (rows > 4) return tiles <= 2 * cus && k > 512 ? 7 : 8;
+  if (rows > 1) return k <= 1024 ? 4 : tiles <= 4 * cus ? 5 : 6;
+  return k <= 1024 ? 0 : tiles <= cus ? 1 : tiles <= 4 * cus ? 2 : 3;
+}
+enum { FN_VERIFY_SUM = 0, FN_VERIFY_PICK, FN_VERIFY_ALL, FN_VERIFY_COUNT };
 
 constexpr int64_t kMostRows = ((int64_t)1 << 31) - 1;
 constexpr int kVerifyChunk = 4096;   // step_device.h's kChunk
@@ -55,11 +91,6 @@ int64_t power_of_two(int64_t n) {   // the next one
   while (p < n) p *= 2;
   return p;
 }
-int log2_of(int64_t p) {
-  int k = 0;
-  while (p >> (k + 1)) ++k;
-  return k;
-}
 
 // ---- norm ------------------------------------------------------------------------------------------
 
@@ -70,43 +101,44 @@ int register_norm(disc_ctx* c, const disc_norm_desc* d, int32_t* id_out) {
   if (d->storage != DISC_STORAGE_I8 && d->storage != DISC_STORAGE_E4M3) return refuse(c, DISC_ERR_INVALID_ARG, "a norm's rows are stored as i8 or e4m3");
   if (!(d->eps > 0.0) || !std::isfinite((float)d->eps) || (float)d->eps == 0.f) return refuse(c, DISC_ERR_INVALID_ARG, "eps is a positive number of 32 bits");
   if (!std::isfinite((float)d->weight_offset)) return refuse(c, DISC_ERR_INVALID_ARG, "weight_offset is no finite number of 32 bits");
-  std::string macros = std::string("#define DISC_NORM 1\n#define DISC_T ") + dtype_ctype(d->dtype) + "\n#define DISC_STORAGE " + std::to_string(d->storage) + "\n";
-  macros += "#define DISC_EPS " + text("%a", d->eps) + "\n#define DISC_OFFSET " + text("%a", d->weight_offset) + "\n";
+  const std::string macros = std::string("#define DISC_NORM 1\n#define DISC_T ") + dtype_ctype(d->dtype) + "\n#define DISC_STORAGE " + std::to_string(d->storage) + "\n";
   std::unique_ptr<Operator> o(new Operator);
   o->kind = Operator::NORM;
-  o->key = macros;
+  o->key = macros + text("%a ", d->eps) + text("%a", d->weight_offset);
   o->dtype = d->dtype;
   o->storage = d->storage;
-  static const char* const names[] = {"disc_norm1_k",          "disc_norm1_nt_k",          "disc_norm2_k",          "disc_norm2_nt_k",
-                                      "disc_norm4_k",          "disc_norm4_nt_k",          "disc_norm8_k",          "disc_norm8_nt_k",
-                                      "disc_norm_backward1_k", "disc_norm_backward1_nt_k", "disc_norm_backward2_k", "disc_norm_backward2_nt_k",
-                                      "disc_norm_backward4_k", "disc_norm_backward4_nt_k", "disc_norm_backward8_k", "disc_norm_backward8_nt_k",
-                                      "disc_norm_join_k"};
-  return enter(c, std::move(o), macros, kStepHeader, names, FN_NORM_COUNT, FN_NORM, id_out);
+  o->eps = d->eps;
+  o->offset = (float)d->weight_offset;
+  static const char* const names[] = {"disc_norm1_s",          "disc_norm4_s",          "disc_norm4_s_nt",          "disc_norm4",          "disc_norm4_nt",
+                                      "disc_norm1_b",          "disc_norm4_b",          "disc_norm_backward1_s",    "disc_norm_backward4_s", "disc_norm_backward4_s_nt",
+                                      "disc_norm_backward4",   "disc_norm_backward4_nt", "disc_norm_backward4_b",   "disc_norm_join_k"};
+  return enter(c, std::move(o), macros, kStepHeader, names, FN_NORM_COUNT, FN_NORM_4, id_out);
 }
 
-// Threads of a row and accesses of a thread.
+// Who has a row: `lanes` threads, a part of a wavefront or all of a block, and which kernel.
 struct RowShape {
-  int lanes, each, block;
-  RowShape(const Operator& o, int64_t width, int most_lanes, bool wide) {
-    const int64_t accesses = ceil_div(width * dtype_bytes(o.dtype), 16);
-    const int64_t want = wide ? most_lanes : 256;
-    int64_t l = std::max<int64_t>(8, std::min(power_of_two(accesses), want));
-    int64_t n = power_of_two(ceil_div(accesses, l));
-    while (n > 4 && l < most_lanes) {
-      l *= 2;
-      n /= 2;
-    }
-    lanes = (int)l;
-    each = (int)n;
-    block = lanes > 256 ? lanes : 256;
-  }
+  int lanes, block, fn;
+  int groups() const { return block / lanes; }
 };
-constexpr int kNormLanes = 1024, kBackwardLanes = 512;
+RowShape norm_shape(const Operator& o, int64_t width, bool few, bool nt) {
+  const int64_t accesses = ceil_div(width * dtype_bytes(o.dtype), 16);
+  if (accesses <= 64) return {(int)std::max<int64_t>(8, power_of_two(accesses)), 256, FN_NORM_S1};
+  if (few && accesses <= 1024) return {(int)ceil_div(accesses, 64) * 64, (int)ceil_div(accesses, 64) * 64, FN_NORM_B1};
+  if (accesses <= 256) return {(int)power_of_two(ceil_div(accesses, 4)), 256, nt ? FN_NORM_S4_NT : FN_NORM_S4};
+  const int block = (int)ceil_div(accesses, 256) * 64;
+  return {block, block, accesses > 1024 ? FN_NORM_B4 : nt ? FN_NORM_4_NT : FN_NORM_4};
+}
+RowShape backward_shape(const Operator& o, int64_t width, bool nt) {
+  const int64_t accesses = ceil_div(width * dtype_bytes(o.dtype), 16);
+  if (accesses <= 64) return {(int)std::max<int64_t>(8, power_of_two(accesses)), 256, FN_BACKWARD_S1};
+  if (accesses <= 256) return {(int)power_of_two(ceil_div(accesses, 4)), 256, nt ? FN_BACKWARD_S4_NT : FN_BACKWARD_S4};
+  const int block = (int)ceil_div(accesses, 256) * 64;
+  return {block, block, accesses > 1024 ? FN_BACKWARD_B4 : nt ? FN_BACKWARD_4_NT : FN_BACKWARD_4};
+}
 
 int check_rows(disc_ctx* c, const Operator& o, int64_t rows, int64_t width) {
   if (rows < 0 || rows > kMostRows) return refuse(c, DISC_ERR_SHAPE, "rows is 0 .. 2^31 - 1", rows);
-  const int64_t most = 512 * 8 * 16 / dtype_bytes(o.dtype);
+  const int64_t most = 1024 * 4 * 16 / dtype_bytes(o.dtype);
   if (width < 1 || width > most) return refuse(c, DISC_ERR_SHAPE, "width is 1 .. 32768, 16384 of fp32", width);
   return DISC_OK;
 }
@@ -123,6 +155,8 @@ int launch_norm(disc_ctx* c, int32_t id, const int64_t* dims, int n_dims, const 
   if (const int rc = check_rows(c, *o, dims[0], dims[1])) return rc;
   a.rows = dims[0];
   a.width = (int32_t)dims[1];
+  a.offset = o->offset;
+  a.eps = o->eps;
   a.x_row = dims[2];
   a.residual_row = dims[3];
   a.total_row = dims[4];
@@ -145,17 +179,16 @@ int launch_norm(disc_ctx* c, int32_t id, const int64_t* dims, int n_dims, const 
   if (a.rows > 1 && adds && ((a.total == a.x && a.total_row != a.x_row) || (a.total == a.residual && a.total_row != a.residual_row)))
     return refuse(c, DISC_ERR_INVALID_ARG, "in place, both sides have the same strides");
   if (context_device(c) < 0) return on_host(c);
-  const RowShape s(*o, a.width, kNormLanes, a.rows <= context_cus(c));
-  a.lanes = s.lanes;
   const int64_t moved = times(a.rows * a.width, size * (adds ? 3 : 1) + 1);
-  const bool nt = moved < 0 || moved >= kNonTemporalBytes;
-  const int64_t groups = s.block / s.lanes, each = kMostThreads / s.block * groups;   // rows of a launch
+  const RowShape s = norm_shape(*o, a.width, a.rows <= 2 * context_cus(c), moved < 0 || moved >= kNonTemporalBytes);
+  a.lanes = s.lanes;
+  const int64_t groups = s.groups(), each = kMostThreads / s.block * groups;   // rows of a launch
   OnDevice on(context_device(c));
   if (!on.ok) return refuse(c, DISC_ERR_HIP, "hipSetDevice failed");
   int rc = DISC_OK, n = 0;
   for (int64_t left = a.rows; rc == DISC_OK && left > 0; ++n) {
     a.rows = std::min(left, each);
-    rc = enqueue(c, o->fn[FN_NORM + 2 * log2_of(s.each) + (nt ? 1 : 0)], (uint64_t)ceil_div(a.rows, groups), 1, (uint32_t)s.block, &a, sizeof a, stream);
+    rc = enqueue(c, o->fn[s.fn], (uint64_t)ceil_div(a.rows, groups), 1, (uint32_t)s.block, &a, sizeof a, stream);
     left -= a.rows;
     a.x = (const char*)a.x + a.rows * a.x_row * size;
     a.codes = (char*)a.codes + a.rows * a.codes_row;
@@ -170,10 +203,10 @@ int launch_norm(disc_ctx* c, int32_t id, const int64_t* dims, int n_dims, const 
 }
 
 // Groups of threads that share a gradient's rows, each with a row of partial sums.
-int64_t backward_blocks(disc_ctx* c, const RowShape& s, int64_t rows) { return std::min<int64_t>(ceil_div(rows, s.block / s.lanes), 2 * context_cus(c)); }
+int64_t backward_blocks(disc_ctx* c, const RowShape& s, int64_t rows) { return std::min<int64_t>(ceil_div(rows, s.groups()), 2 * context_cus(c)); }
 size_t backward_bytes(disc_ctx* c, const Operator& o, int64_t rows, int64_t width) {
-  const RowShape s(o, width, kBackwardLanes, false);
-  return (size_t)(backward_blocks(c, s, rows) * (s.block / s.lanes) * width) * 4;
+  const RowShape s = backward_shape(o, width, false);
+  return (size_t)(backward_blocks(c, s, rows) * s.groups() * width) * 4;
 }
 
 int launch_norm_backward(disc_ctx* c, int32_t id, const int64_t* dims, int n_dims, const void* const* in, int n_in, void* const* out, int n_out,
@@ -190,6 +223,8 @@ int launch_norm_backward(disc_ctx* c, int32_t id, const int64_t* dims, int n_dim
   if (const int rc = check_rows(c, *o, dims[0], dims[1])) return rc;
   a.rows = dims[0];
   a.width = (int32_t)dims[1];
+  a.offset = o->offset;
+  a.eps = o->eps;
   a.total_row = dims[2];
   a.dy_row = dims[3];
   a.dtotal_row = dims[4];
@@ -213,25 +248,24 @@ int launch_norm_backward(disc_ctx* c, int32_t id, const int64_t* dims, int n_dim
     if (a.rows > 1 && ((a.dx == a.total && a.dx_row != a.total_row) || (a.dx == a.dy && a.dx_row != a.dy_row) || (a.dx == a.dtotal && a.dx_row != a.dtotal_row)))
       return refuse(c, DISC_ERR_INVALID_ARG, "in place, both sides have the same strides");
   }
-  const RowShape s(*o, a.width, kBackwardLanes, false);
+  const int64_t moved = times(a.rows * a.width, size * (adds ? 4 : 3));
+  const RowShape s = backward_shape(*o, a.width, moved < 0 || moved >= kNonTemporalBytes);
   const int64_t blocks = backward_blocks(c, s, a.rows);
   a.lanes = s.lanes;
-  a.parts = (int32_t)(blocks * (s.block / s.lanes));
+  a.parts = (int32_t)(blocks * s.groups());
   if (a.parts > 0 && (!workspace || workspace_bytes < (size_t)a.parts * a.width * 4)) return refuse(c, DISC_ERR_WORKSPACE, "workspace missing or too small");
   if (!aligned(workspace, 16)) return refuse(c, DISC_ERR_INVALID_ARG, "the workspace is not 16-byte aligned");
   a.part = (float*)workspace;
   if (context_device(c) < 0) return on_host(c);
-  const int64_t moved = times(a.rows * a.width, size * (adds ? 4 : 3));
-  const bool nt = moved < 0 || moved >= kNonTemporalBytes;
   OnDevice on(context_device(c));
   if (!on.ok) return refuse(c, DISC_ERR_HIP, "hipSetDevice failed");
   int rc = DISC_OK, n = 0;
   if (blocks > 0) {
-    rc = enqueue(c, o->fn[FN_NORM_BACKWARD + 2 * log2_of(s.each) + (nt ? 1 : 0)], (uint64_t)blocks, 1, (uint32_t)s.block, &a, sizeof a, stream);
+    rc = enqueue(c, o->fn[s.fn], (uint64_t)blocks, 1, (uint32_t)s.block, &a, sizeof a, stream);
     ++n;
   }
   if (rc == DISC_OK) {   // (no rows: zeros)
-    rc = enqueue(c, o->fn[FN_NORM_JOIN], (uint64_t)ceil_div(a.width, 64), 1, 256, &a, sizeof a, stream);
+    rc = enqueue(c, o->fn[FN_NORM_JOIN], (uint64_t)ceil_div(a.width, 16), 1, 1024, &a, sizeof a, stream);
     ++n;
   }
   if (rc == DISC_OK) context_count(c, n);
@@ -255,8 +289,9 @@ int register_linear4(disc_ctx* c, const disc_linear4_desc* d, int32_t* id_out) {
   o->storage = d->rows;
   o->group = d->group;
   o->zeros = d->zeros != 0;
-  static const char* const names[] = {"disc_linear1_k", "disc_linear2_k", "disc_linear4_k"};
-  return enter(c, std::move(o), macros, kStepHeader, names, FN_LINEAR_COUNT, FN_LINEAR1, id_out);
+  const char* names[kLinearCount];
+  for (int i = 0; i < kLinearCount; ++i) names[i] = kLinear[i].name;
+  return enter(c, std::move(o), macros, kStepHeader, names, kLinearCount, 0, id_out);
 }
 
 int launch_linear4(disc_ctx* c, int32_t id, const int64_t* dims, int n_dims, const void* const* in, int n_in, void* const* out, int n_out, void* stream) {
@@ -297,11 +332,11 @@ int launch_linear4(disc_ctx* c, int32_t id, const int64_t* dims, int n_dims, con
   if (!aligned(a.x, scaled ? 1 : 2) || !aligned(a.scales, 2) || !aligned(a.row_scales, 4) || !aligned(a.bias, 2) || !aligned(a.out, 2))
     return refuse(c, DISC_ERR_INVALID_ARG, "a tensor is not aligned to its elements");
   if (context_device(c) < 0) return on_host(c);
-  const int tiles = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+  const int at = linear_kernel(rows, n, k, context_cus(c));
+  const LinearKernel& f = kLinear[at];
   OnDevice on(context_device(c));
   if (!on.ok) return refuse(c, DISC_ERR_HIP, "hipSetDevice failed");
-  const int rc = enqueue(c, o->fn[tiles == 1 ? FN_LINEAR1 : tiles == 2 ? FN_LINEAR2 : FN_LINEAR4], (uint64_t)ceil_div(n, 16), (uint32_t)ceil_div(rows, 16 * tiles), 512, &a,
-                         sizeof a, stream);
+  const int rc = enqueue(c, o->fn[at], (uint64_t)ceil_div(n, 16 * f.n * f.teams), (uint32_t)ceil_div(rows, 16 * f.m), (uint32_t)(f.split * f.teams) * 64, &a, sizeof a, stream);
   if (rc == DISC_OK) context_count(c, 1);
   return rc;
 }
@@ -317,7 +352,7 @@ int register_verify(disc_ctx* c, const disc_verify_desc* d, int32_t* id_out) {
   o->kind = Operator::VERIFY;
   o->key = macros;
   o->dtype = d->dtype;
-  static const char* const names[] = {"disc_verify_sum_k", "disc_verify_pick_k"};
+  static const char* const names[] = {"disc_verify_sum_k", "disc_verify_pick_k", "disc_verify_k"};
   return enter(c, std::move(o), macros, kStepHeader, names, FN_VERIFY_COUNT, FN_VERIFY_SUM, id_out);
 }
 
@@ -325,7 +360,7 @@ int check_verify(disc_ctx* c, int64_t batch, int64_t drafts, int64_t vocabulary)
   if (batch < 0 || batch > 1 << 20) return refuse(c, DISC_ERR_SHAPE, "batch is 0 .. 2^20", batch);
   if (drafts < 0 || drafts > 4096) return refuse(c, DISC_ERR_SHAPE, "drafts is 0 .. 4096", drafts);
   if (vocabulary < 1 || vocabulary > 1 << 30) return refuse(c, DISC_ERR_SHAPE, "vocabulary is 1 .. 2^30", vocabulary);
-  if (batch * ceil_div(vocabulary, kVerifyChunk) > kMostThreads / 256) return refuse(c, DISC_ERR_SHAPE, "too many rows for one call");
+  if (batch * ceil_div(vocabulary, kVerifyChunk) > kMostThreads / 256 || batch > kMostThreads / 1024) return refuse(c, DISC_ERR_SHAPE, "too many rows for one call");
   return DISC_OK;
 }
 
@@ -373,6 +408,11 @@ int launch_verify(disc_ctx* c, int32_t id, const int64_t* dims, int n_dims, cons
   if (context_device(c) < 0) return on_host(c);
   OnDevice on(context_device(c));
   if (!on.ok) return refuse(c, DISC_ERR_HIP, "hipSetDevice failed");
+  if (getenv("VF") ? atoi(getenv("VF")) : a.vocabulary < 65536) {
+    const int rc = enqueue(c, o->fn[FN_VERIFY_ALL], (uint64_t)a.batch, 1, 1024, &a, sizeof a, stream);
+    if (rc == DISC_OK) context_count(c, 1);
+    return rc;
+  }
   int rc = enqueue(c, o->fn[FN_VERIFY_SUM], (uint64_t)a.batch * a.chunks, 1, 256, &a, sizeof a, stream);
   if (rc == DISC_OK) rc = enqueue(c, o->fn[FN_VERIFY_PICK], (uint64_t)a.batch, 1, 256, &a, sizeof a, stream);
   if (rc == DISC_OK) context_count(c, 2);

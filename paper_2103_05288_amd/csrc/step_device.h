@@ -3,7 +3,7 @@
 // through hipRTC once per registration, with what never changes between calls as macros; rows, widths, vocabularies and
 // strides are arguments.
 //
-//   DISC_NORM:    DISC_T, DISC_STORAGE (1: i8, 2: e4m3), DISC_EPS, DISC_OFFSET
+//   DISC_NORM:    DISC_T, DISC_STORAGE (1: i8, 2: e4m3)
 //   DISC_LINEAR4: DISC_T_F16 (0: bf16), DISC_ROWS (0: as the results, 1: i8, 2: e4m3), DISC_GROUP (32, 64, 128), DISC_ZEROS
 //   DISC_VERIFY:  DISC_T
 #pragma once
@@ -21,6 +21,8 @@ typedef int i32x4 __attribute__((ext_vector_type(4)));
 // wide accesses at any element's address (the operands' strides and pointers are the caller's)
 typedef u32x4 u32x4_u __attribute__((aligned(1)));
 typedef u32x2 u32x2_u __attribute__((aligned(1)));
+typedef u32 u32_u __attribute__((aligned(1)));
+typedef u16 u16_u __attribute__((aligned(1)));
 template <bool kNt, class V>
 DISC_DEV V fetch(const V* p) {
   if (kNt) return __builtin_nontemporal_load(p);
@@ -75,29 +77,27 @@ DISC_DEV double shuffled(double x, int by) {
 }
 DISC_DEV u32 magnitude(float x) { return __builtin_bit_cast(u32, x) & 0x7fffffffu; }   // (orders as |x| does, NaN above infinity)
 
-// Sums of `lanes` neighbouring threads (a power of two; above 64, whole wavefronts through LDS), the same in all of them.
-struct Group {
-  int lanes, first_wave, waves;
-  DISC_DEV Group(int l) : lanes(l), first_wave(0), waves(0) {
-    if (lanes > 64) {
-      waves = lanes / 64;
-      first_wave = (int)threadIdx.x / lanes * waves;
-    }
-  }
-  template <class X, class F>
-  DISC_DEV X over(X x, X* kept, F f) const {
-    for (int s = 1; s < lanes && s < 64; s *= 2) x = f(x, shuffle(x, s));
-    if (waves) {
-      __syncthreads();
-      if (threadIdx.x % 64 == 0) kept[threadIdx.x / 64] = x;
-      __syncthreads();
-      x = kept[first_wave];
-      for (int w = 1; w < waves; ++w) x = f(x, kept[first_wave + w]);
-    }
-    return x;
-  }
-  DISC_DEV static double shuffle(double x, int s) { return shuffled(x, s); }
-  DISC_DEV static u32 shuffle(u32 x, int s) { return (u32)__shfl_xor((int)x, s); }
+// What `lanes` neighbouring threads have, brought together, the same in all of them: a power of two of up to 64, or (kBlock) the
+// whole block through LDS.
+DISC_DEV double exchanged(double x, int s) { return shuffled(x, s); }
+DISC_DEV u32 exchanged(u32 x, int s) { return (u32)__shfl_xor((int)x, s); }
+template <bool kBlock, class X, class F>
+DISC_DEV X over_lanes(X x, int lanes, F f) {
+  for (int s = 1; s < (kBlock ? 64 : lanes); s *= 2) x = f(x, exchanged(x, s));
+  return x;
+}
+template <class X, class F>
+DISC_DEV X over_waves(const X* kept, F f) {
+  X x = kept[0];
+  for (int w = 1; w < (int)blockDim.x / 64; ++w) x = f(x, kept[w]);
+  return x;
+}
+struct Plus {
+  DISC_DEV double operator()(double a, double b) const { return a + b; }
+};
+struct Most {
+  DISC_DEV u32 operator()(u32 a, u32 b) const { return max(a, b); }
+  DISC_DEV double operator()(double a, double b) const { return a > b ? a : b; }
 };
 
 struct NormArgs {
@@ -107,6 +107,8 @@ struct NormArgs {
   float* scales;
   i64 x_row, residual_row, total_row, codes_row, rows;
   int width, lanes;         // lanes: threads of a row
+  float offset;
+  double eps;
 };
 
 DISC_DEV u32 code4(float a, float b, float c, float d) {
@@ -123,89 +125,99 @@ DISC_DEV u32 code4(float a, float b, float c, float d) {
 #endif
 }
 
-template <bool kNt, int kN>
+template <bool kNt, bool kBlock, int kN>
 DISC_DEV void norm_body(const NormArgs& A) {
   __shared__ double sums[kMostWaves], most64[kMostWaves];
   __shared__ u32 most[kMostWaves];
-  const Group group(A.lanes);
-  const int lane = (int)threadIdx.x % A.lanes;
-  const i64 at = (i64)blockIdx.x * ((int)blockDim.x / A.lanes) + (int)threadIdx.x / A.lanes;
-  const bool live = at < A.rows;
-  const i64 row = live ? at : A.rows - 1;                  // (all threads reach the barriers)
-  float s[kN][kV], w[kN][kV];
-  double squares = 0;
-  u32 a = 0;
+  const int lanes = kBlock ? (int)blockDim.x : A.lanes, lane = (int)threadIdx.x % lanes;
+  const i64 row = kBlock ? (i64)blockIdx.x : (i64)blockIdx.x * ((int)blockDim.x / lanes) + (int)threadIdx.x / lanes;
+  if (row >= A.rows) return;                                // (not of a whole block: no barrier follows)
+  vec_t x[kN], r[kN], v[kN];
 #pragma unroll
   for (int i = 0; i < kN; ++i) {
-    const int c = (i * A.lanes + lane) * kV;
-    const int n = A.width - c;
-    if (n > 0) {
-      const vec_t x = take<kNt>(A.x + row * A.x_row + c, n), v = take<false>(A.weight + c, n);
-      vec_t r = {};
-      if (A.residual) r = take<kNt>(A.residual + row * A.residual_row + c, n);
+    const int c = (i * lanes + lane) * kV, n = A.width - c;
+    x[i] = r[i] = v[i] = vec_t{};
+    if (n <= 0) continue;
+    x[i] = take<kNt>(A.x + row * A.x_row + c, n);
+    if (A.residual) r[i] = take<kNt>(A.residual + row * A.residual_row + c, n);
+    v[i] = take<false>(A.weight + c, n);
+  }
+  float s[kN][kV];
+  double squares = 0;
+  u32 a = 0;
+  const auto weight = [&](int i, int e) { return (float)v[i][e] + A.offset; };   // (behind a row's end s is 0)
 #pragma unroll
-      for (int e = 0; e < kV; ++e) {
-        s[i][e] = (float)x[e] + (float)r[e];
-        w[i][e] = (float)v[e] + (e < n ? (float)DISC_OFFSET : 0.f);
-      }
-    } else {
-#pragma unroll
-      for (int e = 0; e < kV; ++e) s[i][e] = w[i][e] = 0.f;
-    }
+  for (int i = 0; i < kN; ++i)
 #pragma unroll
     for (int e = 0; e < kV; ++e) {
+      s[i][e] = (float)x[i][e] + (float)r[i][e];
       squares += (double)s[i][e] * (double)s[i][e];
-      a = max(a, magnitude(s[i][e] * w[i][e]));
+      a = max(a, magnitude(s[i][e] * weight(i, e)));
     }
-  }
-  if (A.total && live) {
+  if (A.total) {
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
-      const int c = (i * A.lanes + lane) * kV;
+      const int c = (i * lanes + lane) * kV;
       vec_t t;
 #pragma unroll
       for (int e = 0; e < kV; ++e) t[e] = (T)s[i][e];
       if (c < A.width) give<kNt>(A.total + row * A.total_row + c, t, A.width - c);
     }
   }
-  squares = group.over(squares, sums, [](double p, double q) { return p + q; });
-  a = group.over(a, most, [](u32 p, u32 q) { return max(p, q); });
-  const double root = 1.0 / sqrt(squares / (double)A.width + (double)DISC_EPS);
+  squares = over_lanes<kBlock>(squares, lanes, Plus());
+  a = over_lanes<kBlock>(a, lanes, Most());
+  if (kBlock) {
+    if (threadIdx.x % 64 == 0) {
+      sums[threadIdx.x / 64] = squares;
+      most[threadIdx.x / 64] = a;
+    }
+    __syncthreads();
+    a = over_waves(most, Most());
+    if (lane == 0) squares = over_waves(sums, Plus());
+  }
   // Where a product leaves what 32 bits hold well -- above their range, or so small that Q / a would be infinite -- they
-  // are formed in 64.  (By the whole block, for the barriers.)
+  // are formed in 64.
   float largest = __builtin_bit_cast(float, a);
-  const bool wide = !(largest >= 0x1p-100f && largest < __builtin_inff());
+  const bool wide = !(largest >= 0x1p-100f && largest < __builtin_inff());   // (the same for the whole row)
   double largest64 = (double)largest;
-  if (__syncthreads_or(wide)) {
+  if (wide) {
     double m = 0;
 #pragma unroll
     for (int i = 0; i < kN; ++i)
 #pragma unroll
       for (int e = 0; e < kV; ++e) {
-        const double y = __builtin_fabs((double)s[i][e] * (double)w[i][e]);
-        m = !(y <= m) ? y : m;                              // (a NaN replaces whatever was there, and stays below)
+        const double y = __builtin_fabs((double)s[i][e] * (double)weight(i, e));
+        m = !(y <= m) ? y : m;                              // (a NaN replaces whatever was there, and becomes an infinity)
         if (!(m < __builtin_inf())) m = __builtin_inf();
       }
-    m = group.over(m, most64, [](double p, double q) { return p > q ? p : q; });
-    if (wide) largest64 = m;                                // (a row's scale does not depend on its neighbours)
+    m = over_lanes<kBlock>(m, lanes, Most());
+    if (kBlock) {
+      if (threadIdx.x % 64 == 0) most64[threadIdx.x / 64] = m;
+      __syncthreads();
+      m = over_waves(most64, Most());
+    }
+    largest64 = m;
   }
-  if (!live) return;
-  const double scale = largest64 > 0 ? largest64 * root / (double)kMost : 0.0;
-  const bool fine = (float)scale < __builtin_inff();         // (not NaN either)
-  if (lane == 0) A.scales[row] = fine ? (float)scale : __builtin_nanf("");
+  // The scale is NaN where the row holds an infinity or a NaN: the largest is, or (an infinity times a weight of 0) the squares are.
+  const bool fine = largest64 < __builtin_inf();
+  if (lane == 0) {
+    const double root = 1.0 / sqrt(squares / (double)A.width + A.eps);
+    const float scale = (float)(largest64 > 0 ? largest64 * root / (double)kMost : 0.0);
+    A.scales[row] = fine ? scale : __builtin_nanf("");
+  }
   const float inverse = kMost / largest;
   const double inverse64 = fine && largest64 > 0 ? (double)kMost / largest64 : 0.0;
 #pragma unroll
   for (int i = 0; i < kN; ++i) {
-    const int c = (i * A.lanes + lane) * kV;
+    const int c = (i * lanes + lane) * kV;
     const int n = A.width - c;
     if (n <= 0) break;
     float y[kV];
 #pragma unroll
-    for (int e = 0; e < kV; ++e) y[e] = s[i][e] * w[i][e] * inverse;
+    for (int e = 0; e < kV; ++e) y[e] = s[i][e] * weight(i, e) * inverse;
     if (wide) {
 #pragma unroll
-      for (int e = 0; e < kV; ++e) y[e] = fine ? (float)((double)s[i][e] * (double)w[i][e] * inverse64) : 0.f;
+      for (int e = 0; e < kV; ++e) y[e] = fine ? (float)((double)s[i][e] * (double)weight(i, e) * inverse64) : 0.f;
     }
     u8* to = A.codes + row * A.codes_row + c;
     u32 code[kV / 4];
@@ -235,23 +247,23 @@ struct NormBackwardArgs {
   float *dweight, *part;
   i64 total_row, dy_row, dtotal_row, dx_row, rows;
   int width, lanes, parts;
+  float offset;
+  double eps;
 };
 
-template <bool kNt, int kN>
+template <bool kNt, bool kBlock, int kN>
 DISC_DEV void norm_backward_body(const NormBackwardArgs& A) {
-  __shared__ double sums[kMostWaves], alongs[kMostWaves];
-  const Group group(A.lanes);
-  const int lane = (int)threadIdx.x % A.lanes, groups = (int)blockDim.x / A.lanes;
-  const int mine = (int)blockIdx.x * groups + (int)threadIdx.x / A.lanes;
+  __shared__ double sums[2][kMostWaves], alongs[2][kMostWaves];
+  const int lanes = kBlock ? (int)blockDim.x : A.lanes, lane = (int)threadIdx.x % lanes;
+  const int mine = kBlock ? (int)blockIdx.x : (int)blockIdx.x * ((int)blockDim.x / lanes) + (int)threadIdx.x / lanes;
   float dw[kN][kV] = {};
-  for (i64 at = mine; at - (int)threadIdx.x / A.lanes < A.rows; at += A.parts) {
-    const bool live = at < A.rows;                          // (all threads reach the barriers)
-    const i64 row = live ? at : A.rows - 1;
+  int turn = 0;
+  for (i64 row = mine; row < A.rows; row += A.parts, turn ^= 1) {
     vec_t h[kN], d[kN], v[kN], t[kN];
     double squares = 0, along = 0;
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
-      const int c = (i * A.lanes + lane) * kV;
+      const int c = (i * lanes + lane) * kV;
       const int n = A.width - c;
       h[i] = d[i] = v[i] = t[i] = vec_t{};
       if (n <= 0) continue;
@@ -266,21 +278,29 @@ DISC_DEV void norm_backward_body(const NormBackwardArgs& A) {
       for (int e = 0; e < kV; ++e) {
         const double x = (double)(float)h[i][e];
         squares += x * x;
-        along += x * (double)((float)d[i][e]) * (double)((float)v[i][e] + (float)DISC_OFFSET);
+        along += x * (double)((float)d[i][e]) * (double)((float)v[i][e] + A.offset);
       }
-    squares = group.over(squares, sums, [](double p, double q) { return p + q; });
-    along = group.over(along, alongs, [](double p, double q) { return p + q; });
-    if (!live) continue;
-    const double root = 1.0 / sqrt(squares / (double)A.width + (double)DISC_EPS);
+    squares = over_lanes<kBlock>(squares, lanes, Plus());
+    along = over_lanes<kBlock>(along, lanes, Plus());
+    if (kBlock) {                                           // (two sets in turn: the next row's are written while some read these)
+      if (threadIdx.x % 64 == 0) {
+        sums[turn][threadIdx.x / 64] = squares;
+        alongs[turn][threadIdx.x / 64] = along;
+      }
+      __syncthreads();
+      squares = over_waves(sums[turn], Plus());
+      along = over_waves(alongs[turn], Plus());
+    }
+    const double root = 1.0 / sqrt(squares / (double)A.width + A.eps);
     const float r = (float)root, k = (float)(root * along / (double)A.width);
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
-      const int c = (i * A.lanes + lane) * kV;
+      const int c = (i * lanes + lane) * kV;
       if (c >= A.width) break;
       vec_t y;
 #pragma unroll
       for (int e = 0; e < kV; ++e) {
-        const float u = (float)h[i][e] * r, dy = (float)d[i][e], g = dy * ((float)v[i][e] + (float)DISC_OFFSET);
+        const float u = (float)h[i][e] * r, dy = (float)d[i][e], g = dy * ((float)v[i][e] + A.offset);
         dw[i][e] += dy * u;
         y[e] = (T)(r * (g - u * k) + (float)t[i][e]);
       }
@@ -289,33 +309,57 @@ DISC_DEV void norm_backward_body(const NormBackwardArgs& A) {
   }
 #pragma unroll
   for (int i = 0; i < kN; ++i) {
-    const int c = (i * A.lanes + lane) * kV;
+    const int c = (i * lanes + lane) * kV;
 #pragma unroll
     for (int e = 0; e < kV; ++e)
       if (c + e < A.width) A.part[(i64)mine * A.width + c + e] = dw[i][e];
   }
 }
 
-#define DISC_NORM_KERNELS(N)                                                                                                              \
-  extern "C" __global__ void __launch_bounds__(1024) disc_norm##N##_k(NormArgs A) { norm_body<false, N>(A); }                             \
-  extern "C" __global__ void __launch_bounds__(1024) disc_norm##N##_nt_k(NormArgs A) { norm_body<true, N>(A); }                           \
-  extern "C" __global__ void __launch_bounds__(512) disc_norm_backward##N##_k(NormBackwardArgs A) { norm_backward_body<false, N>(A); }     \
-  extern "C" __global__ void __launch_bounds__(512) disc_norm_backward##N##_nt_k(NormBackwardArgs A) { norm_backward_body<true, N>(A); }
-DISC_NORM_KERNELS(1)
-DISC_NORM_KERNELS(2)
-DISC_NORM_KERNELS(4)
-DISC_NORM_KERNELS(8)
+// accesses of a thread: a part of a wavefront has a row (_s), 256 threads, or the whole block of up to 1024 (_b)
+#define DISC_NORM_KERNEL(NAME, THREADS, NT, BLOCK, N) \
+  extern "C" __global__ void __launch_bounds__(THREADS) disc_norm##NAME(NormArgs A) { norm_body<NT, BLOCK, N>(A); }
+#define DISC_NORM_BACKWARD_KERNEL(NAME, THREADS, NT, BLOCK, N) \
+  extern "C" __global__ void __launch_bounds__(THREADS) disc_norm_backward##NAME(NormBackwardArgs A) { norm_backward_body<NT, BLOCK, N>(A); }
+DISC_NORM_KERNEL(1_s, 256, false, false, 1)
+DISC_NORM_KERNEL(4_s, 256, false, false, 4)
+DISC_NORM_KERNEL(4_s_nt, 256, true, false, 4)
+DISC_NORM_KERNEL(4, 256, false, true, 4)
+DISC_NORM_KERNEL(4_nt, 256, true, true, 4)
+DISC_NORM_KERNEL(1_b, 1024, false, true, 1)
+DISC_NORM_KERNEL(4_b, 1024, false, true, 4)
+DISC_NORM_BACKWARD_KERNEL(1_s, 256, false, false, 1)
+DISC_NORM_BACKWARD_KERNEL(4_s, 256, false, false, 4)
+DISC_NORM_BACKWARD_KERNEL(4_s_nt, 256, true, false, 4)
+DISC_NORM_BACKWARD_KERNEL(4, 256, false, true, 4)
+DISC_NORM_BACKWARD_KERNEL(4_nt, 256, true, true, 4)
+DISC_NORM_BACKWARD_KERNEL(4_b, 1024, false, true, 4)
 
-// dweight: a block has 64 columns, four threads each of a quarter of the parts.
-extern "C" __global__ void __launch_bounds__(256) disc_norm_join_k(NormBackwardArgs A) {
-  __shared__ float kept[4][64];
-  const int c = (int)blockIdx.x * 64 + (int)threadIdx.x % 64, q = (int)threadIdx.x / 64;
+// dweight: a block has 16 columns, 64 threads each of every 64th part.
+extern "C" __global__ void __launch_bounds__(1024) disc_norm_join_k(NormBackwardArgs A) {
+  __shared__ float kept[16][16];
+  const int c = (int)blockIdx.x * 16 + (int)threadIdx.x % 16;
   float sum = 0;
-  if (c < A.width)
-    for (int p = q; p < A.parts; p += 4) sum += A.part[(i64)p * A.width + c];
-  kept[q][threadIdx.x % 64] = sum;
+  if (c < A.width) {
+    int p = (int)threadIdx.x / 16;
+    for (; p + 192 < A.parts; p += 256) {
+      float x[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) x[u] = A.part[(i64)(p + 64 * u) * A.width + c];
+      sum += (x[0] + x[1]) + (x[2] + x[3]);
+    }
+    for (; p < A.parts; p += 64) sum += A.part[(i64)p * A.width + c];
+  }
+  sum += __shfl_xor(sum, 16);
+  sum += __shfl_xor(sum, 32);
+  if (threadIdx.x % 64 < 16) kept[threadIdx.x / 64][threadIdx.x % 16] = sum;
   __syncthreads();
-  if (q == 0 && c < A.width) A.dweight[c] = (kept[0][threadIdx.x] + kept[1][threadIdx.x]) + (kept[2][threadIdx.x] + kept[3][threadIdx.x]);
+  if (threadIdx.x < 16 && c < A.width) {
+    sum = 0;
+#pragma unroll
+    for (int w = 0; w < 16; ++w) sum += kept[w][threadIdx.x];
+    A.dweight[c] = sum;
+  }
 }
 #endif  // DISC_NORM
 
@@ -371,13 +415,20 @@ DISC_DEV u32x4 arrange(u32x4 d) {
   return d;
 }
 
+// (d & mask) | bits in one instruction: one of two constants has to be in a vector register
+DISC_DEV u32 with_bits(u32 d, u32 mask, u32 bits) {
+  asm("" : "+v"(bits));
+  return (d & mask) | bits;
+}
 // Eight codes as an operand, in the order 0 4 1 5 2 6 3 7.
 // bf16: 128 + c by setting the exponent's bits; what that adds to the sum is taken off with the zero point.
 // f16:  1024 + c and 1024 + 16 c, from which c - 8 is exact.
 DISC_DEV u32x4 widen(u32 d) {
-  if (kKind == 0) return (u32x4{d, d >> 4, d >> 8, d >> 12} & 0x000f000fu) | 0x43004300u;
+  if (kKind == 0) return u32x4{with_bits(d, 0x000f000fu, 0x43004300u), with_bits(d >> 4, 0x000f000fu, 0x43004300u), with_bits(d >> 8, 0x000f000fu, 0x43004300u),
+                               with_bits(d >> 12, 0x000f000fu, 0x43004300u)};
   const u32 e = d >> 8;
-  const u32x4 raw = {(d & 0x000f000fu) | 0x64006400u, (d & 0x00f000f0u) | 0x64006400u, (e & 0x000f000fu) | 0x64006400u, (e & 0x00f000f0u) | 0x64006400u};
+  const u32x4 raw = {with_bits(d, 0x000f000fu, 0x64006400u), with_bits(d, 0x00f000f0u, 0x64006400u), with_bits(e, 0x000f000fu, 0x64006400u),
+                     with_bits(e, 0x00f000f0u, 0x64006400u)};
   u32x4 r;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -401,116 +452,359 @@ DISC_DEV u32x4 reorder8(u32x2 d) {
   return u32x4{pack16(a[0], c[0]), pack16(a[1], c[1]), pack16(b[0], e[0]), pack16(b[1], e[1])};
 }
 
-// What a lane has of a block of 128 elements of kTiles tiles of 16 rows of x: by dword of codes.  i8: two dwords, even
-// elements and odd ones.
-template <int kM>
-struct Rows {
-  u32x4 v[kM][4];
+// `n` 16-bit numbers or bytes at any address, as words
+template <int kBytes>
+struct Words {
+  u32 w[(kBytes + 3) / 4];
+  DISC_DEV void take(const u8* p) {
+    if constexpr (kBytes == 1) w[0] = *p;
+    if constexpr (kBytes == 2) w[0] = *(const u16_u*)p;
+    if constexpr (kBytes == 4) w[0] = *(const u32_u*)p;
+    if constexpr (kBytes == 8) {
+      const u32x2 v = *(const u32x2_u*)p;
+      w[0] = v[0], w[1] = v[1];
+    }
+    if constexpr (kBytes >= 16)
+#pragma unroll
+      for (int i = 0; i < kBytes / 16; ++i) {
+        const u32x4 v = *(const u32x4_u*)(p + 16 * i);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[4 * i + e] = v[e];
+      }
+  }
 };
 
-template <int kM>
-DISC_DEV void take_rows(const LinearArgs& A, int row0, int block, int q, int m, Rows<kM>& r) {
+// What a lane has of kRun neighbouring blocks of 128 elements: 32 neighbouring codes of a row and block of kN tiles of 16 rows of
+// weights, with their groups' scales and zero points, and of kM tiles of kR rows of x.
+//
+// A product takes its x from the first kR of each 16 lanes (the others' results are not used).  Where kR is less than 16, a load
+// fetches what 16 / kR products take, one behind the other in the 16 lanes, and each is turned to the front when its product is due:
+// loads of x that fill kR lanes of 16 cost as much as whole ones.
+constexpr int kXs = kKind == 2 ? 2 : 4;                     // operands of a block: 16 bytes a lane (8 of e4m3 in memory)
+template <int kR, int kRun>
+constexpr int loads_of() {
+  return (kRun * kXs * kR + 15) / 16;
+}
+template <int kM, int kN, int kR, int kRun>
+struct Block {
+  u32x4 w[kRun][kN];
+  u32x4 x[kM][loads_of<kR, kRun>()];
+  Words<2 * kGroups * kRun> scale[kN];
+  Words<kGroups * kRun> zero[kN];
+};
+
+struct Lane {
+  const u8* x[4];          // its row of each tile of x, from the first element it loads on
+  const u8 *w, *s, *z;     // the block's first row of weights, of scales, of zero points
+  u32 w_row[4], s_row[4];  // from there to its row of each tile: bytes of codes, groups
+  int c, q, k, groups;
+};
+
+// kWhole: all of the blocks is there; else one block is taken, the last, which may have 32, 64 or 96 elements.
+template <bool kWhole, int kM, int kN, int kR, int kRun>
+DISC_DEV void take_block(const Lane& L, int b, Block<kM, kN, kR, kRun>& B) {
+  static_assert(kWhole || kRun == 1, "");
+  const int q = L.q;
 #pragma unroll
-  for (int t = 0; t < kM; ++t) {
-    const int row = min(row0 + t * 16 + m, A.rows - 1);     // (rows behind the last: a copy, not stored)
-    const u8* p = A.x + (i64)row * A.x_row * kRowSize;
+  for (int r = 0; r < kRun; ++r)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int k = block * kBlockK + place(j, q);
+    for (int t = 0; t < kN; ++t) {
+      B.w[r][t] = u32x4{0, 0, 0, 0};
+      if (kWhole || b * kBlockK + q * 32 < L.k) B.w[r][t] = *(const u32x4*)(L.w + (L.w_row[t] + (u32)((b + r) * (kBlockK / 2) + q * 16)));
+    }
+#pragma unroll
+  for (int t = 0; t < kN; ++t) {
+    const u8* s = L.s + 2 * (L.s_row[t] + (u32)(b * kGroups));
+    const u8* z = L.z + (L.s_row[t] + (u32)(b * kGroups));
+    if (kWhole) {
+      B.scale[t].take(s);
+      if (DISC_ZEROS) B.zero[t].take(z);
+    } else {
+      B.zero[t].w[0] = 0;
+#pragma unroll
+      for (int g = 0; g < kGroups; ++g) {
+        const int at = min(g, L.groups - 1 - b * kGroups);
+        const u32 v = *(const u16*)(s + 2 * at);
+        B.scale[t].w[g / 2] = g % 2 ? B.scale[t].w[g / 2] | v << 16 : v;
+        if (DISC_ZEROS) B.zero[t].w[0] |= (u32)z[at] << (8 * g);
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < loads_of<kR, kRun>(); ++i) {
+    // the operand that this lane loads: the n-th of the run
+    const int n = kR == 16 ? i : min(i * (16 / kR) + L.c / kR, kRun * kXs - 1), j = kKind == 2 ? n % kXs * 2 : n % kXs;
+    const int k = n / kXs * kBlockK + place(j, q);
+    const bool here = kWhole || b * kBlockK + k < L.k, too = kWhole || b * kBlockK + k + 32 < L.k;
+#pragma unroll
+    for (int t = 0; t < kM; ++t) {
+      const u8* p = L.x[t] + ((i64)b * kBlockK + k) * kRowSize;
       u32x4 v = {0, 0, 0, 0};
-      if (k < A.k) {
-        if (kRowSize == 2) {
-          v = *(const u32x4_u*)(p + (i64)k * 2);
-        } else {
-          const u32x2 c = *(const u32x2_u*)(p + k);
-          v[0] = c[0];
-          v[1] = c[1];
+      if (kRowSize == 2 || (kKind == 2 && kG > 32)) {       // (i8: the elements of two dwords of codes follow each other)
+        if (here) v = *(const u32x4_u*)p;
+      } else {
+        if (here) {
+          const u32x2 h = *(const u32x2_u*)p;
+          v[0] = h[0], v[1] = h[1];
+        }
+        if (kKind == 2 && too) {
+          const u32x2 h = *(const u32x2_u*)(p + 32);
+          v[2] = h[0], v[3] = h[1];
         }
       }
-      r.v[t][j] = v;
+      B.x[t][i] = v;
     }
   }
 }
 
-template <int kM, int kWaves>
-DISC_DEV void linear_body(const LinearArgs& A) {
-  __shared__ float kept[kWaves][kM][256];
-  const int lane = (int)threadIdx.x % 64, wave = (int)threadIdx.x / 64;
-  const int c = lane % 16, q = lane / 16;
-  const int n = (int)blockIdx.x * 16 + c, row0 = (int)blockIdx.y * 16 * kM;
-  const i64 nn = min(n, A.n - 1);
-  const u8* w = A.weights + nn * (A.k / 2);
-  const T* scales = A.scales + nn * A.groups;
-  const u8* zeros = DISC_ZEROS ? A.zeros + nn * A.groups : nullptr;
-  f32x4 total[kM] = {};
-  const int blocks = (A.k + kBlockK - 1) / kBlockK;
-  for (int b = wave; b < blocks; b += kWaves) {
-    u32x4 d = {0, 0, 0, 0};
-    if (b * kBlockK + q * 32 < A.k) d = *(const u32x4*)(w + (i64)b * (kBlockK / 2) + q * 16);
-    Rows<kM> x;
-    take_rows<kM>(A, row0, b, q, c, x);
-    d = arrange(d);
+// bf16 rows times 2^-32 (see linear_body)
+DISC_DEV u32x4 lowered(u32x4 v) {
+  u32x4 r;
 #pragma unroll
-    for (int g = 0; g < kGroups; ++g) {
-      const int group = min(b * kGroups + g, A.groups - 1);
-      const float s = (float)scales[group];
-      const int z = DISC_ZEROS ? (int)zeros[group] : 8;
+  for (int i = 0; i < 4; ++i) {
+    const u32 d = v[i];
+    const float lo = __builtin_bit_cast(float, d << 16) * 0x1p-32f, hi = __builtin_bit_cast(float, d & 0xffff0000u) * 0x1p-32f;
+    const __bf16 a = (__bf16)lo, b = (__bf16)hi;
+    r[i] = (u32)__builtin_bit_cast(u16, a) | (u32)__builtin_bit_cast(u16, b) << 16;
+  }
+  return r;
+}
+
+template <int K>
+struct Sum {
+  typedef f32x4 type;
+};
+template <>
+struct Sum<2> {
+  typedef i32x4 type;
+};
+// acc += products of the elements of one group: operands of x times w(j), [16 rows][8]
+template <class F, class A>
+DISC_DEV A multiply(const u32x4* x, F w, int j0, A acc) {
 #pragma unroll
-      for (int t = 0; t < kM; ++t) {
-        if constexpr (kKind == 2) {
-          i32x4 acc = {}, sum = {};
-          const u32 ones = 0x01010101u;
-#pragma unroll
-          for (int j = g * 4 / kGroups; j < (g + 1) * 4 / kGroups; ++j) {
-            const u32 lo = d[j] & 0x0f0f0f0fu, hi = (d[j] >> 4) & 0x0f0f0f0fu;
-            const u32 even = __builtin_amdgcn_perm(x.v[t][j][1], x.v[t][j][0], 0x06040200u), odd = __builtin_amdgcn_perm(x.v[t][j][1], x.v[t][j][0], 0x07050301u);
-            const i8x8 xs = (i8x8)(((u64)odd << 32) | even), ws = (i8x8)(((u64)hi << 32) | lo), os = (i8x8)(((u64)ones << 32) | ones);
-            acc = __builtin_amdgcn_mfma_i32_16x16x32_i8(xs, ws, acc, 0, 0, 0);
-            sum = __builtin_amdgcn_mfma_i32_16x16x32_i8(xs, os, sum, 0, 0, 0);
-          }
-#pragma unroll
-          for (int i = 0; i < 4; ++i) total[t][i] += s * (float)(acc[i] - z * sum[i]);
-        } else {
-          f32x4 acc = {}, sum = {};
-#pragma unroll
-          for (int j = g * 4 / kGroups; j < (g + 1) * 4 / kGroups; ++j) {
-            const u32x4 v = kRowSize == 1 ? reorder8(u32x2{x.v[t][j][0], x.v[t][j][1]}) : reorder(x.v[t][j]), u = widen(d[j]);
-            if constexpr (kKind == 0) {
-              const u32x4 ones = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
-              acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, u), acc, 0, 0, 0);
-              sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, ones), sum, 0, 0, 0);
-            } else {
-              const u32x4 ones = {0x3c003c00u, 0x3c003c00u, 0x3c003c00u, 0x3c003c00u};
-              acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, v), __builtin_bit_cast(f16x8, u), acc, 0, 0, 0);
-              if (DISC_ZEROS) sum = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, v), __builtin_bit_cast(f16x8, ones), sum, 0, 0, 0);
-            }
-          }
-          const float off = kKind == 0 ? 128.f + (float)z : (float)(z - 8);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) total[t][i] += s * (kKind == 0 || DISC_ZEROS ? acc[i] - off * sum[i] : acc[i]);
-        }
-      }
+  for (int j = j0; j < j0 + 4 / kGroups; ++j) {
+    if constexpr (kKind == 2 && kG > 32) {
+      if (j % 2) continue;
+      const u32x4 b = {w(j)[0], w(j)[1], w(j + 1)[0], w(j + 1)[1]};
+      acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, x[j / 2]), __builtin_bit_cast(i32x4, b), acc, 0, 0, 0);
+    } else if constexpr (kKind == 2) {
+      acc = __builtin_amdgcn_mfma_i32_16x16x32_i8((i8x8)((u64)x[j / 2][j % 2 * 2 + 1] << 32 | x[j / 2][j % 2 * 2]), (i8x8)((u64)w(j)[1] << 32 | w(j)[0]), acc, 0, 0, 0);
+    } else if constexpr (kKind == 1) {
+      acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, x[j]), __builtin_bit_cast(f16x8, w(j)), acc, 0, 0, 0);
+    } else {
+      acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x[j]), __builtin_bit_cast(bf16x8, w(j)), acc, 0, 0, 0);
     }
   }
+  return acc;
+}
+
+// What was loaded of x as operands: in the order of the codes, e4m3 in half precision.
+DISC_DEV u32x4 operand(u32x4 v, bool down) {
+  if (kKind == 2)
+    return u32x4{__builtin_amdgcn_perm(v[1], v[0], 0x06040200u), __builtin_amdgcn_perm(v[1], v[0], 0x07050301u), __builtin_amdgcn_perm(v[3], v[2], 0x06040200u),
+                 __builtin_amdgcn_perm(v[3], v[2], 0x07050301u)};
+  if (kRowSize == 1) return reorder8(u32x2{v[0], v[1]});
+  return reorder(kKind == 0 && down ? lowered(v) : v);
+}
+// v of the lanes kBy behind, among 16
+template <int kBy>
+DISC_DEV u32x4 turned(u32x4 v) {
+  if constexpr (kBy != 0) {
+    u32x4 r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const u32 d = v[i];
+      r[i] = (u32)__builtin_amdgcn_update_dpp(0, (int)d, 0x120 + 16 - kBy, 0xf, 0xf, false);   // row_ror
+    }
+    return r;
+  }
+  return v;
+}
+template <int kR, int kAt, int kCount>
+DISC_DEV void operands_of(const u32x4* v, u32x4* x) {
+  if constexpr (kCount > 0) {
+    x[0] = turned<kAt * kR % 16>(v[kAt * kR / 16]);
+    operands_of<kR, kAt + 1, kCount - 1>(v, x + 1);
+  }
+}
+
+// total += block kAt of the run's part of the products (x as operands already)
+template <int kAt, int kM, int kN, int kR, int kRun>
+DISC_DEV void add_block(const Block<kM, kN, kR, kRun>& B, float lower, f32x4 (&total)[kM][kN]) {
+  constexpr int kEach = 4 / kGroups, r = kAt;               // dwords of codes of a group
+  u32x4 x[kM][kXs];
+#pragma unroll
+  for (int t = 0; t < kM; ++t) operands_of<kR, kAt * kXs, kXs>(B.x[t], x[t]);
+  // sums of the rows' elements over each group, in the results' layout: what the codes' zero points are taken off with
+  typedef typename Sum<kKind>::type acc_t;
+  acc_t sums[kM][kGroups];
 #pragma unroll
   for (int t = 0; t < kM; ++t)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) kept[wave][t][(q * 4 + i) * 16 + c] = total[t][i];
-  __syncthreads();
-  for (int o = (int)threadIdx.x; o < kM * 256; o += kWaves * 64) {
-    const int m = row0 + o / 16, col = (int)blockIdx.x * 16 + o % 16;
-    if (m >= A.rows || col >= A.n) continue;
-    float y = 0;
+    for (int g = 0; g < kGroups; ++g) {
+      sums[t][g] = acc_t{};
+      if (kKind != 1 || DISC_ZEROS) {
+        const u32x4 ones = kKind == 2 ? u32x4{0x01010101u, 0x01010101u, 0x01010101u, 0x01010101u} : kKind == 0 ? u32x4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u}
+                                                                                                  : u32x4{0x3c003c00u, 0x3c003c00u, 0x3c003c00u, 0x3c003c00u};
+        sums[t][g] = multiply(x[t], [&](int) { return ones; }, g * kEach, sums[t][g]);
+      }
+    }
 #pragma unroll
-    for (int v = 0; v < kWaves; ++v) y += kept[v][o / 256][o % 256];
-    if (DISC_ROWS) y *= A.row_scales[m];
-    if (A.bias) y += (float)A.bias[col];
-    A.out[m * A.out_row + col] = (T)y;
+  for (int n = 0; n < kN; ++n) {
+    const u32x4 d = arrange(B.w[r][n]);
+    u32x4 w[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const u32 c = d[j];
+      if (kKind == 2) {
+        w[j][0] = c & 0x0f0f0f0fu;
+        w[j][1] = (c >> 4) & 0x0f0f0f0fu;
+      } else {
+        w[j] = widen(c);
+      }
+    }
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) {
+      const int at = r * kGroups + g;
+      const u32 pair = B.scale[n].w[at / 2];
+      const u16 bits = (u16)(at % 2 ? pair >> 16 : pair);
+      const float s = (float)__builtin_bit_cast(T, bits) * lower;
+      const int z = DISC_ZEROS ? (int)((B.zero[n].w[at / 4] >> (8 * (at % 4))) & 0xffu) : 8;
+#pragma unroll
+      for (int t = 0; t < kM; ++t) {
+        const acc_t acc = multiply(x[t], [&](int j) { return w[j]; }, g * kEach, acc_t{});
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if constexpr (kKind == 2) total[t][n][i] += s * (float)(acc[i] - z * sums[t][g][i]);
+          else if constexpr (kKind == 0) total[t][n][i] += s * (acc[i] - (128.f + (float)z) * sums[t][g][i]);
+          else total[t][n][i] += s * (DISC_ZEROS ? acc[i] - (float)(z - 8) * sums[t][g][i] : acc[i]);
+        }
+      }
+    }
   }
 }
-extern "C" __global__ void __launch_bounds__(512) disc_linear1_k(LinearArgs A) { linear_body<1, 8>(A); }
-extern "C" __global__ void __launch_bounds__(512) disc_linear2_k(LinearArgs A) { linear_body<2, 8>(A); }
-extern "C" __global__ void __launch_bounds__(512) disc_linear4_k(LinearArgs A) { linear_body<4, 8>(A); }
+
+template <int kAt, int kM, int kN, int kR, int kRun>
+DISC_DEV void add_blocks(const Block<kM, kN, kR, kRun>& B, float lower, f32x4 (&total)[kM][kN]) {
+  if constexpr (kAt < kRun) {
+    add_block<kAt>(B, lower, total);
+    add_blocks<kAt + 1>(B, lower, total);
+  }
+}
+template <int kM, int kN, int kR, int kRun>
+DISC_DEV void add_run(Block<kM, kN, kR, kRun>& B, bool down, f32x4 (&total)[kM][kN]) {
+#pragma unroll
+  for (int t = 0; t < kM; ++t)
+#pragma unroll
+    for (int i = 0; i < loads_of<kR, kRun>(); ++i) B.x[t][i] = operand(B.x[t][i], down);
+  add_blocks<0>(B, down ? 0x1p-32f : 1.f, total);
+}
+
+// kSplit wavefronts share the elements of a row, in blocks of 128, and add up what they have through LDS; kTiles such teams in a
+// block have kM tiles of x and kN tiles of weights each.
+template <int kM, int kN, int kR, int kSplit, int kTeams, int kRun>
+DISC_DEV void linear_body(const LinearArgs& A) {
+  __shared__ float kept[kSplit > 1 ? kTeams * kSplit : 1][kSplit > 1 ? kM * kN * 256 : 1];
+  const int lane = (int)threadIdx.x % 64, wave = (int)threadIdx.x / 64, team = wave / kSplit, share = wave % kSplit;
+  const int c = lane % 16, q = lane / 16;
+  const int col0 = __builtin_amdgcn_readfirstlane(((int)blockIdx.x * kTeams + team) * 16 * kN), row0 = (int)blockIdx.y * 16 * kM;
+  const bool idle = col0 >= A.n;                            // (a team behind the last tile; it reaches the barriers)
+  Lane L;
+  // (rows behind the last, of x and of the weights: copies of it, not stored)
+#pragma unroll
+  for (int t = 0; t < kM; ++t) L.x[t] = A.x + (i64)min(row0 + t * 16 + c % kR, A.rows - 1) * A.x_row * kRowSize;
+  const int from = min(col0, A.n - 1);
+  L.w = A.weights + (i64)from * (A.k / 2);
+  L.s = (const u8*)(A.scales + (i64)from * A.groups);
+  L.z = DISC_ZEROS ? A.zeros + (i64)from * A.groups : nullptr;
+#pragma unroll
+  for (int t = 0; t < kN; ++t) {
+    const int n = min(t * 16 + c, A.n - 1 - from);
+    L.w_row[t] = (u32)n * (u32)(A.k / 2);
+    L.s_row[t] = (u32)n * (u32)A.groups;
+  }
+  L.c = c;
+  L.q = q;
+  L.k = A.k;
+  L.groups = A.groups;
+  const int mine = __builtin_amdgcn_readfirstlane(share), runs = A.k / (kBlockK * kRun);
+  const int count = idle || runs <= mine ? 0 : (runs - mine + kSplit - 1) / kSplit;
+  // Where a result is no finite number, the sums on the way to it may have passed 32 bits: it is formed again of scales times
+  // 2^-32 and of bf16 rows times 2^-32.  (By the whole block; what was finite stays.)
+  for (int again = 0;; ++again) {
+    f32x4 total[kM][kN];
+#pragma unroll
+    for (int t = 0; t < kM; ++t)
+#pragma unroll
+      for (int n = 0; n < kN; ++n) total[t][n] = f32x4{0, 0, 0, 0};
+    // (behind the wavefront's last run, that again: nothing depends on how many there are, so that loads are waited for one by one)
+    if (count > 0) {
+      Block<kM, kN, kR, kRun> B;
+      take_block<true>(L, mine * kRun, B);
+#pragma unroll 1
+      for (int i = 1; i <= count; ++i) {
+        add_run(B, again != 0, total);
+        take_block<true>(L, (mine + min(i, count - 1) * kSplit) * kRun, B);
+      }
+    }
+    // the blocks behind the last whole run
+    if (!idle)
+#pragma unroll 1
+      for (int b = runs * kRun + mine; b * kBlockK < A.k; b += kSplit) {
+        Block<kM, kN, kR, 1> last;
+        take_block<false>(L, b, last);
+        add_run(last, again != 0, total);
+      }
+    bool lost = false;
+    const auto finish = [&](int m, int col, float y) {
+      if (m >= A.rows || col >= A.n) return;
+      if (DISC_ROWS) y *= A.row_scales[m];
+      if (again) y *= 0x1p32f * (kKind == 0 ? 0x1p32f : 1.f);
+      if (!again) lost |= !(__builtin_fabsf(y) < __builtin_inff());
+      if (A.bias) y += (float)A.bias[col];
+      T* to = A.out + (m * A.out_row + col);
+      if (!again || !(__builtin_fabsf((float)*to) < __builtin_inff())) *to = (T)y;
+    };
+    if (kSplit == 1) {
+#pragma unroll
+      for (int t = 0; t < kM; ++t)
+#pragma unroll
+        for (int n = 0; n < kN; ++n)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) finish(row0 + t * 16 + q * 4 + i, col0 + n * 16 + c, total[t][n][i]);
+      if (again || !__any(lost)) break;
+    } else {
+#pragma unroll
+      for (int t = 0; t < kM; ++t)
+#pragma unroll
+        for (int n = 0; n < kN; ++n)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) kept[wave][(t * kN + n) * 256 + (q * 4 + i) * 16 + c] = total[t][n][i];
+      __syncthreads();
+      for (int o = share * 64 + lane; o < kM * kN * 256; o += kSplit * 64) {
+        float y = 0;
+#pragma unroll
+        for (int v = 0; v < kSplit; ++v) y += kept[team * kSplit + v][o];
+        finish(row0 + o / (kN * 256) * 16 + o % 256 / 16, col0 + o / 256 % kN * 16 + o % 16, y);
+      }
+      if (again || !__syncthreads_or(lost)) break;
+    }
+  }
+}
+// tiles of x and of weights, rows of a tile of x, wavefronts of a team, teams, blocks of a run
+#define DISC_LINEAR_KERNEL(M, N, R, S, W, B) \
+  extern "C" __global__ void __launch_bounds__(S * W * 64) disc_linear_##M##_##N##_##R##_##S##_##W##_##B##_k(LinearArgs A) { linear_body<M, N, R, S, W, B>(A); }
+DISC_LINEAR_KERNEL(1, 1, 1, 1, 8, 2)
+DISC_LINEAR_KERNEL(1, 1, 1, 16, 1, 2)
+DISC_LINEAR_KERNEL(1, 1, 1, 8, 1, 2)
+DISC_LINEAR_KERNEL(1, 2, 1, 8, 1, 2)
+DISC_LINEAR_KERNEL(1, 1, 4, 1, 8, 2)
+DISC_LINEAR_KERNEL(1, 1, 4, 8, 1, 2)
+DISC_LINEAR_KERNEL(1, 2, 4, 8, 1, 2)
+DISC_LINEAR_KERNEL(1, 1, 16, 8, 1, 2)
+DISC_LINEAR_KERNEL(1, 4, 16, 4, 1, 2)
+DISC_LINEAR_KERNEL(2, 2, 16, 8, 1, 2)
+DISC_LINEAR_KERNEL(4, 2, 16, 4, 1, 2)
 #endif  // DISC_LINEAR4
 
 #ifdef DISC_VERIFY
@@ -571,22 +865,155 @@ struct Place {
   }
   DISC_DEV bool less() const { return q != nullptr || removed >= 0; }
 };
-DISC_DEV double sum_of(double x, double* kept, int threads) {
+
+DISC_DEV double moved(double x, int from) {
+  const u64 b = __builtin_bit_cast(u64, x);
+  const u32 lo = (u32)__shfl((int)(u32)b, from), hi = (u32)__shfl((int)(u32)(b >> 32), from);
+  return __builtin_bit_cast(double, ((u64)hi << 32) | lo);
+}
+// the sum over a wavefront, the same in all of its lanes
+DISC_DEV double wave_sum(double x) {
+  const int lane = (int)threadIdx.x % 64;
+  for (int s = 1; s < 64; s *= 2) x += moved(x, lane ^ s);
+  return x;
+}
+// The running sum over the block's threads, this one's among it; `kept`: a number for each wavefront.
+template <int kThreads>
+DISC_DEV double running(double x, double* kept) {
+  const int lane = (int)threadIdx.x % 64, wave = (int)threadIdx.x / 64;
   for (int s = 1; s < 64; s *= 2) {
-    const u64 b = __builtin_bit_cast(u64, x);
-    const u32 lo = (u32)__shfl_xor((int)(u32)b, s), hi = (u32)__shfl_xor((int)(u32)(b >> 32), s);
-    x += __builtin_bit_cast(double, ((u64)hi << 32) | lo);
+    const double y = moved(x, max(lane - s, 0));
+    if (lane >= s) x += y;
   }
   __syncthreads();
-  if (threadIdx.x % 64 == 0) kept[threadIdx.x / 64] = x;
+  if (lane == 63) kept[wave] = x;
   __syncthreads();
-  x = 0;
-  for (int w = 0; w < threads / 64; ++w) x += kept[w];
+  for (int w = 0; w < wave; ++w) x += kept[w];
   return x;
 }
 
+// The weights of kV neighbouring tokens from i on (`end`: behind the last): what is left of p beside q, and p.
+struct Pair {
+  float p[kV], q[kV];
+  DISC_DEV void take(const Place& at, i64 i, i64 end) {
+    vec_t a = {}, b = {};
+    if (i + kV <= end) {
+      a = *(const vec_u*)(at.p + i);
+      if (at.q) b = *(const vec_u*)(at.q + i);
+    } else {
+#pragma unroll
+      for (int e = 0; e < kV - 1; ++e)
+        if (i + e < end) {
+          a[e] = at.p[i + e];
+          if (at.q) b[e] = at.q[i + e];
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < kV; ++e) p[e] = (float)a[e], q[e] = (float)b[e];
+  }
+  DISC_DEV double all(int e) const { return weight((double)p[e]); }
+  DISC_DEV double less(const Place& at, i64 i, int e) const {
+    if (i + e == at.removed) return 0;
+    return at.q ? weight((double)p[e] - (double)q[e]) : weight((double)p[e]);
+  }
+};
+// Sums of tokens first + kV j, j = begin, begin + step ..., below `end`: added to `less` and `all`.
+template <int kAtOnce>
+DISC_DEV void sum_tokens(const Place& at, i64 begin, int step, i64 end, double& less, double& all) {
+  for (; begin < end; begin += (i64)step * kAtOnce) {
+    Pair x[kAtOnce];
+#pragma unroll
+    for (int u = 0; u < kAtOnce; ++u) x[u].take(at, min(begin + (i64)u * step, end), end);
+#pragma unroll
+    for (int u = 0; u < kAtOnce; ++u)
+#pragma unroll
+      for (int e = 0; e < kV; ++e) {
+        all += x[u].all(e);
+        less += x[u].less(at, begin + (i64)u * step, e);
+      }
+  }
+}
+
+// The token of `count` tokens from `first` on at which the running sum, `before` in front of them, passes `goal`: by a block.  (Where
+// rounding leaves none, the last with any weight; -1: none has.)
+template <int kThreads>
+DISC_DEV int pick(const Place& at, bool from_less, i64 first, int count, double before, double goal, double* kept, int* found) {
+  const int each = (count + kThreads - 1) / kThreads;
+  const i64 begin = first + min((int)threadIdx.x * each, count), end = first + min(((int)threadIdx.x + 1) * each, count);
+  if (threadIdx.x == 0) found[0] = 0x7fffffff, found[1] = -1;
+  double sum = 0;
+  for (i64 i = begin; i < end; i += kV) {
+    Pair x;
+    x.take(at, i, end);
+#pragma unroll
+    for (int e = 0; e < kV; ++e) sum += from_less ? x.less(at, i, e) : x.all(e);
+  }
+  double s = before + running<kThreads>(sum, kept);
+  if (sum > 0) {
+    atomicMax(&found[1], (int)threadIdx.x);
+    if (s > goal) atomicMin(&found[0], (int)threadIdx.x);
+  }
+  __syncthreads();
+  const int who = found[0] != 0x7fffffff ? found[0] : found[1];
+  __syncthreads();
+  if (threadIdx.x == 0 && who < 0) found[0] = -1;
+  if ((int)threadIdx.x == who) {
+    s -= sum;
+    int token = -1;
+    bool over = false;
+    for (i64 i = begin; i < end && !over; i += kV) {
+      Pair x;
+      x.take(at, i, end);
+#pragma unroll
+      for (int e = 0; e < kV; ++e) {
+        const double y = from_less ? x.less(at, i, e) : x.all(e);
+        s += y;
+        if (y > 0 && !over) {
+          token = (int)(i + e);
+          over = s > goal;
+        }
+      }
+    }
+    found[0] = token;
+  }
+  __syncthreads();
+  return found[0];
+}
+
+// Which of `n` ranges the goal falls into (u of the whole of their sums), and the sum in front of it; by one thread.
+struct Range {
+  int range;              // -1: nothing has any weight
+  bool from_less;
+  double before, goal;
+};
+template <class F>
+DISC_DEV Range range_of(int n, bool takes_less, float uniform, F sums) {
+  double less = 0, all = 0;
+  for (int i = 0; i < n; ++i) less += sums(i, 0), all += sums(i, 1);
+  Range r;
+  r.from_less = takes_less && less > 0;
+  const double u = (double)uniform;
+  r.goal = (u > 0 ? u : 0.0) * (r.from_less ? less : all);
+  r.range = -1;
+  r.before = 0;
+  double sum = 0;
+  for (int i = 0; i < n; ++i) {
+    const double x = sums(i, r.from_less ? 0 : 1);
+    if (!(x > 0)) continue;
+    r.range = i;
+    r.before = sum;
+    sum += x;
+    if (sum > r.goal) break;
+  }
+  return r;
+}
+DISC_DEV void write_tokens(const VerifyArgs& A, i64 b, int kept, int token, int threads) {
+  for (int i = (int)threadIdx.x; i <= A.drafts; i += threads) A.tokens[b * (A.drafts + 1) + i] = i < kept ? A.drafted[b * A.drafts + i] : i == kept ? token : -1;
+}
+
+// A block a chunk of a row: what is kept (each block for itself), and the chunk's sums.
 extern "C" __global__ void __launch_bounds__(256) disc_verify_sum_k(VerifyArgs A) {
-  __shared__ double kept_sums[4];
+  __shared__ double kept_sums[2][4];
   __shared__ int kept_s;
   const i64 b = blockIdx.x / (u32)A.chunks;
   const int chunk = (int)(blockIdx.x - (u32)b * (u32)A.chunks);
@@ -599,100 +1026,72 @@ extern "C" __global__ void __launch_bounds__(256) disc_verify_sum_k(VerifyArgs A
   }
   __syncthreads();
   const Place at(A, b, kept_s);
-  const int first = chunk * kChunk, end = min(A.vocabulary - first, kChunk);
+  const i64 first = (i64)chunk * kChunk;
   double less = 0, all = 0;
-  for (int i = (int)threadIdx.x; i < end; i += 256) {
-    const double p = weight((double)(float)at.p[first + i]);
-    all += p;
-    if (at.q) less += weight((double)(float)at.p[first + i] - (double)(float)at.q[first + i]);
-    else if (first + i != at.removed) less += p;
+  sum_tokens<kChunk / (256 * kV)>(at, first + (int)threadIdx.x * kV, 256 * kV, min((i64)A.vocabulary, first + kChunk), less, all);
+  less = wave_sum(less);
+  all = wave_sum(all);
+  if (threadIdx.x % 64 == 0) {
+    kept_sums[0][threadIdx.x / 64] = less;
+    kept_sums[1][threadIdx.x / 64] = all;
   }
-  less = sum_of(less, kept_sums, 256);
-  all = sum_of(all, kept_sums, 256);
-  if (threadIdx.x == 0) {
-    double* to = A.part + (b * A.chunks + chunk) * 2;
-    to[0] = less;
-    to[1] = all;
+  __syncthreads();
+  if (threadIdx.x < 2) {
+    const double* k = kept_sums[threadIdx.x];
+    A.part[(b * A.chunks + chunk) * 2 + threadIdx.x] = (k[0] + k[1]) + (k[2] + k[3]);
   }
 }
 
 extern "C" __global__ void __launch_bounds__(256) disc_verify_pick_k(VerifyArgs A) {
-  __shared__ double kept_sums[4];
-  __shared__ double upto[256];
-  __shared__ int found, last, chunk_s, column_s;
-  __shared__ double before_s, goal_s;
+  __shared__ double sums[256][2], kept_sums[4];
+  __shared__ Range range;
+  __shared__ int found[2];
   const i64 b = blockIdx.x;
   const int kept = A.accepted[b];
   const Place at(A, b, kept);
   const double* part = A.part + b * A.chunks * 2;
-  if (threadIdx.x == 0) {
-    double less = 0, all = 0;
-    for (int i = 0; i < A.chunks; ++i) {
-      less += part[2 * i];
-      all += part[2 * i + 1];
-    }
-    const int column = at.less() && less > 0 ? 0 : 1;
-    const double whole = column ? all : less, u = (double)A.uniforms[b * (A.drafts + 1) + A.drafts];
-    const double goal = (u > 0 ? u : 0.0) * whole;
-    double before = 0, sum = 0;
-    int chunk = -1;
-    for (int i = 0; i < A.chunks; ++i) {
-      const double x = part[2 * i + column];
-      if (x > 0) {
-        chunk = i;
-        before = sum;
-        if (sum + x > goal) break;
-      }
-      sum += x;
-    }
-    chunk_s = chunk;
-    column_s = column;
-    before_s = before;
-    goal_s = goal;
-    found = 0x7fffffff;
-    last = -1;
+  // (first groups of chunks, one a thread, then the chunks of the group)
+  const int each = (A.chunks + 255) / 256, groups = (A.chunks + each - 1) / each;
+  double less = 0, all = 0;
+  for (int i = (int)threadIdx.x * each; i < min(((int)threadIdx.x + 1) * each, A.chunks); ++i) less += part[2 * i], all += part[2 * i + 1];
+  sums[threadIdx.x][0] = less;
+  sums[threadIdx.x][1] = all;
+  __syncthreads();
+  if (threadIdx.x == 0) range = range_of(groups, at.less(), A.uniforms[b * (A.drafts + 1) + A.drafts], [&](int i, int k) { return sums[i][k]; });
+  __syncthreads();
+  int token = -1;
+  if (range.range >= 0)
+    token = pick<256>(at, range.from_less, (i64)range.range * each * kChunk, min(each * kChunk, A.vocabulary - range.range * each * kChunk), range.before, range.goal, kept_sums, found);
+  write_tokens(A, b, kept, token, 256);
+}
+
+// All of a sequence by one block: its wavefronts sum a sixteenth of the row each.
+extern "C" __global__ void __launch_bounds__(1024) disc_verify_k(VerifyArgs A) {
+  __shared__ double sums[16][2], kept_sums[16];
+  __shared__ Range range;
+  __shared__ int found[2], kept_s;
+  const i64 b = blockIdx.x;
+  const int lane = (int)threadIdx.x % 64, wave = (int)threadIdx.x / 64;
+  if (wave == 0) {
+    const int k = kept_of(A, b, lane);
+    if (lane == 0) kept_s = A.accepted[b] = k;
   }
   __syncthreads();
-  const int chunk = chunk_s, column = column_s;
-  if (chunk >= 0) {
-    // (a thread has neighbouring elements of the chunk)
-    constexpr int kEach = kChunk / 256;
-    const int first = chunk * kChunk + (int)threadIdx.x * kEach;
-    double x[kEach], sum = 0;
-#pragma unroll
-    for (int e = 0; e < kEach; ++e) {
-      const int i = first + e;
-      x[e] = 0;
-      if (i < A.vocabulary) {
-        const double p = (double)(float)at.p[i];
-        x[e] = weight(column == 0 && at.q ? p - (double)(float)at.q[i] : p);
-        if (column == 0 && i == at.removed) x[e] = 0;
-      }
-      sum += x[e];
-    }
-    upto[threadIdx.x] = sum;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-      double s = before_s;
-      for (int t = 0; t < 256; ++t) {
-        const double y = upto[t];
-        upto[t] = s;
-        s += y;
-      }
-    }
-    __syncthreads();
-    double s = upto[threadIdx.x];
-#pragma unroll
-    for (int e = 0; e < kEach; ++e) {
-      s += x[e];
-      if (x[e] > 0) {
-        atomicMax(&last, first + e);
-        if (s > goal_s) atomicMin(&found, first + e);
-      }
-    }
-  }
+  const int kept = kept_s;
+  const Place at(A, b, kept);
+  const int share = (A.vocabulary + 16 * 64 * kV - 1) / (16 * 64 * kV) * (64 * kV);
+  const i64 first = min((i64)wave * share, (i64)A.vocabulary), end = min(first + share, (i64)A.vocabulary);
+  double less = 0, all = 0;
+  sum_tokens<4>(at, first + lane * kV, 64 * kV, end, less, all);
+  less = wave_sum(less);
+  all = wave_sum(all);
+  if (lane == 0) sums[wave][0] = less, sums[wave][1] = all;
   __syncthreads();
-  const int token = found != 0x7fffffff ? found : last;
-  for (int i = (int)threadIdx.x; i <= A.drafts; i += 256) A.tokens[b * (A.drafts + 1) + i] = i < kept ? A.drafted[b * A.drafts + i] : i == kept ? token : -1;
+  if (threadIdx.x == 0) range = range_of(16, at.less(), A.uniforms[b * (A.drafts + 1) + A.drafts], [&](int i, int k) { return sums[i][k]; });
+  __syncthreads();
+  int token = -1;
+  if (range.range >= 0)
+    token = pick<1024>(at, range.from_less, (i64)range.range * share, min(share, A.vocabulary - range.range * share), range.before, range.goal, kept_sums, found);
+  write_tokens(A, b, kept, token, 1024);
 }
 #endif  // DISC_VERIFY
