@@ -1,4 +1,4 @@
-// Python's way into disc_launch, disc_graph_launch and the operators of decoder.py: turns the argument lists of a call (dims,
+// Python's way into disc_launch, disc_graph_launch and the operators of decoder.py and step.py: turns the argument lists of a call (dims,
 // tensors, workspace) into the C arrays of the ABI.  Marshalling only, like the ctypes binding whose
 // per-call part it is: with ctypes arrays a call spent 5 us here, more than a small kernel takes
 // (37 x 768 fp32: 9.3 us a call, 4.4 us of them the kernel).
@@ -325,11 +325,134 @@ PyObject* cache_attend(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   return c.run(dims, 12, in, 3 + n + (prefix ? 1 : 0), &out.address, 1, ws, bytes, stream);
 }
 
+// ---- the operators of step.py ----------------------------------------------------------------------
+
+// [rows, width], the last axis dense
+struct Matrix {
+  uint64_t address;
+  int64_t shape[2], stride[2];
+  bool take(PyObject* t, PyObject* dtype, int64_t device) {
+    return on(t, dtype, device, &address) && numbers(PyObject_GetAttr(t, s_shape), 2, shape) && numbers(PyObject_CallMethodNoArgs(t, s_stride), 2, stride) &&
+           (stride[1] == 1 || shape[1] == 1);
+  }
+  bool take(PyObject* t, PyObject* dtype, int64_t device, int64_t rows, int64_t width) { return take(t, dtype, device) && shape[0] == rows && shape[1] == width; }
+};
+bool vector(PyObject* t, PyObject* dtype, int64_t device, int64_t n, uint64_t* address) {
+  int64_t m;
+  return dense(t, dtype, device, 1, &m, address) && m == n;
+}
+bool table(PyObject* t, PyObject* dtype, int64_t device, int64_t rows, int64_t width, uint64_t* address) {
+  int64_t s[2];
+  return dense(t, dtype, device, 2, s, address) && s[0] == rows && s[1] == width;
+}
+// a dense workspace, or None
+bool scratch(PyObject* t, int64_t device, uint64_t* address, uint64_t* bytes) {
+  *address = *bytes = 0;
+  if (t == Py_None) return true;
+  int64_t d;
+  uint64_t count, size;
+  PyObject* whole = PyObject_CallMethodNoArgs(t, s_is_contiguous);
+  Py_XDECREF(whole);
+  if (whole != Py_True || !number(PyObject_CallMethodNoArgs(t, s_get_device), &d) || d != device || !call_u64(t, s_data_ptr, address) || !call_u64(t, s_numel, &count) ||
+      !call_u64(t, s_element_size, &size))
+    return false;
+  *bytes = count * size;
+  return true;
+}
+
+// norm(fn, ctx, id, dtype, device, 0, stored type, fp32, x, weight, codes, scales, residual, total, stream)
+PyObject* norm(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  Call c;
+  uint64_t stream, in[3], out[3];
+  Matrix x, codes, residual, total;
+  if (n_args != 15 || !c.take(a) || !as_u64(a[14], &stream) || !x.take(a[8], c.dtype, c.device)) return does_not_fit();
+  const int64_t rows = x.shape[0], width = x.shape[1];
+  if (!vector(a[9], c.dtype, c.device, width, in + 1) || !codes.take(a[10], a[6], c.device, rows, width) || !vector(a[11], a[7], c.device, rows, out + 1) ||
+      (a[12] == Py_None) != (a[13] == Py_None))
+    return does_not_fit();
+  const bool adds = a[12] != Py_None;
+  if (adds && (!residual.take(a[12], c.dtype, c.device, rows, width) || !total.take(a[13], c.dtype, c.device, rows, width))) return does_not_fit();
+  in[0] = x.address;
+  in[2] = adds ? residual.address : 0;
+  out[0] = codes.address;
+  out[2] = adds ? total.address : 0;
+  const int64_t dims[6] = {rows, width, x.stride[0], adds ? residual.stride[0] : 0, adds ? total.stride[0] : 0, codes.stride[0]};
+  return c.run(dims, 6, in, adds ? 3 : 2, out, adds ? 3 : 2, 0, 0, stream);
+}
+
+// norm_backward(fn, ctx, id, dtype, device, 0, fp32, total, weight, dy, dx, dweight, dtotal, workspace, stream)
+PyObject* norm_backward(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  Call c;
+  uint64_t stream, in[4], out[2], ws, bytes;
+  Matrix total, dy, dx, dtotal;
+  if (n_args != 15 || !c.take(a) || !as_u64(a[14], &stream) || !total.take(a[7], c.dtype, c.device)) return does_not_fit();
+  const int64_t rows = total.shape[0], width = total.shape[1];
+  const bool adds = a[12] != Py_None;
+  if (!vector(a[8], c.dtype, c.device, width, in + 1) || !dy.take(a[9], c.dtype, c.device, rows, width) || !dx.take(a[10], c.dtype, c.device, rows, width) ||
+      !vector(a[11], a[6], c.device, width, out + 1) || (adds && !dtotal.take(a[12], c.dtype, c.device, rows, width)) || !scratch(a[13], c.device, &ws, &bytes))
+    return does_not_fit();
+  in[0] = total.address;
+  in[2] = dy.address;
+  in[3] = adds ? dtotal.address : 0;
+  out[0] = dx.address;
+  const int64_t dims[6] = {rows, width, total.stride[0], dy.stride[0], adds ? dtotal.stride[0] : 0, dx.stride[0]};
+  return c.run(dims, 6, in, adds ? 4 : 3, out, 2, ws, bytes, stream);
+}
+
+// linear4(fn, ctx, id, dtype, device, group, type of x, fp32, uint8, scaled, with zeros, x, weights, scales, out, row_scales, zeros, bias, stream)
+PyObject* linear4(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  Call c;
+  uint64_t stream, in[6];
+  Matrix x, out;
+  int64_t w[2];
+  if (n_args != 19 || !c.take(a) || !as_u64(a[18], &stream) || !x.take(a[11], a[6], c.device) || !dense(a[12], a[8], c.device, 2, w, in + 1)) return does_not_fit();
+  const int64_t rows = x.shape[0], k = x.shape[1], n = w[0], group = c.head_dim;
+  const bool scaled = a[9] == Py_True, zeros = a[10] == Py_True;
+  if (group < 1 || k % group || w[1] != k / 2 || !table(a[13], c.dtype, c.device, n, k / group, in + 2) || !out.take(a[14], c.dtype, c.device, rows, n) ||
+      scaled != (a[15] != Py_None) || zeros != (a[16] != Py_None))
+    return does_not_fit();
+  int m = 3;
+  if (scaled && !vector(a[15], a[7], c.device, rows, in + m++)) return does_not_fit();
+  if (zeros && !table(a[16], a[8], c.device, n, k / group, in + m++)) return does_not_fit();
+  if (a[17] != Py_None && !vector(a[17], c.dtype, c.device, n, in + m++)) return does_not_fit();
+  in[0] = x.address;
+  const int64_t dims[5] = {rows, n, k, x.stride[0], out.stride[0]};
+  return c.run(dims, 5, in, m, &out.address, 1, 0, 0, stream);
+}
+
+// [batch, places, vocabulary], the last axis dense
+bool probabilities(PyObject* t, PyObject* dtype, int64_t device, int64_t* shape, int64_t* stride, uint64_t* address) {
+  return on(t, dtype, device, address) && numbers(PyObject_GetAttr(t, s_shape), 3, shape) && numbers(PyObject_CallMethodNoArgs(t, s_stride), 3, stride) &&
+         (stride[2] == 1 || shape[2] == 1);
+}
+// verify(fn, ctx, id, dtype, device, 0, fp32, int32, target, drafted, uniforms, tokens, accepted, draft, lengths, workspace, stream)
+PyObject* verify(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  Call c;
+  uint64_t stream, in[5], out[2], ws, bytes;
+  int64_t t[3], ts[3], d[3] = {0, 0, 0}, ds[3] = {0, 0, 0};
+  if (n_args != 17 || !c.take(a) || !as_u64(a[16], &stream) || !probabilities(a[8], c.dtype, c.device, t, ts, in)) return does_not_fit();
+  const int64_t batch = t[0], drafts = t[1] - 1, vocabulary = t[2];
+  int m = 3;
+  if (drafts < 0 || !table(a[9], a[7], c.device, batch, drafts, in + 1) || !table(a[10], a[6], c.device, batch, drafts + 1, in + 2) ||
+      !table(a[11], a[7], c.device, batch, drafts + 1, out) || !vector(a[12], a[7], c.device, batch, out + 1))
+    return does_not_fit();
+  const bool drafted = a[13] != Py_None, ragged = a[14] != Py_None;
+  if (drafted && (!probabilities(a[13], c.dtype, c.device, d, ds, in + m++) || d[0] != batch || d[1] != drafts || d[2] != vocabulary)) return does_not_fit();
+  if (ragged && !vector(a[14], a[7], c.device, batch, in + m++)) return does_not_fit();
+  if (!scratch(a[15], c.device, &ws, &bytes)) return does_not_fit();
+  const int64_t dims[9] = {batch, drafts, vocabulary, ts[0], ts[1], ds[0], ds[1], drafted, ragged};
+  return c.run(dims, 9, in, m, out, 2, ws, bytes, stream);
+}
+
 PyMethodDef methods[] = {{"launch", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(launch)), METH_FASTCALL,
                           "launch(fn, ctx, id, dims, inputs, outputs, workspace, workspace_bytes, stream) -> status"},
                          {"rotary", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(rotary)), METH_FASTCALL, "status, or None"},
                          {"cache_rows", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(cache_rows)), METH_FASTCALL, "status, or None"},
                          {"cache_attend", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(cache_attend)), METH_FASTCALL, "status, or None"},
+                         {"norm", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(norm)), METH_FASTCALL, "status, or None"},
+                         {"norm_backward", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(norm_backward)), METH_FASTCALL, "status, or None"},
+                         {"linear4", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(linear4)), METH_FASTCALL, "status, or None"},
+                         {"verify", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(verify)), METH_FASTCALL, "status, or None"},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_pylaunch", "argument marshalling of disc_launch", -1, methods, nullptr, nullptr, nullptr, nullptr};
 

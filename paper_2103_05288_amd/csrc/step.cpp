@@ -23,7 +23,7 @@ struct NormBackwardArgs {
   void *dx, *dweight;
   float* part;
   int64_t total_row, dy_row, dtotal_row, dx_row, rows;
-  int32_t width, lanes, parts;
+  int32_t width, lanes, parts, groups;
   float offset;
   double eps;
 };
@@ -42,7 +42,7 @@ struct VerifyArgs {
 
 // the norm's kernels and its gradient's (with _nt behind: past the caches), and what joins the gradient's parts
 enum { FN_NORM_S1 = 0, FN_NORM_S4, FN_NORM_S4_NT, FN_NORM_4, FN_NORM_4_NT, FN_NORM_B1, FN_NORM_B4, FN_BACKWARD_S1, FN_BACKWARD_S4, FN_BACKWARD_S4_NT, FN_BACKWARD_4,
-       FN_BACKWARD_4_NT, FN_BACKWARD_B4, FN_NORM_JOIN, FN_NORM_COUNT };
+       FN_BACKWARD_4_NT, FN_BACKWARD_B2, FN_BACKWARD_B4, FN_NORM_JOIN, FN_NORM_COUNT };
 struct LinearKernel {
   const char* name;
   int m, n, rows, split, teams;   // tiles of 16 rows of x and of weights, rows of a tile of x, wavefronts of a team, teams of a block
@@ -75,7 +75,7 @@ int linear_kernel(int64_t rows, int64_t n, int64_t k, int64_t cus) {
   if (rows > 1) return k <= 1024 ? 4 : tiles <= 4 * cus ? 5 : 6;
   return k <= 1024 ? 0 : tiles <= cus ? 1 : tiles <= 4 * cus ? 2 : 3;
 }
-enum { FN_VERIFY_SUM = 0, FN_VERIFY_PICK, FN_VERIFY_ALL, FN_VERIFY_COUNT };
+enum { FN_VERIFY_SUM = 0, FN_VERIFY_PICK, FN_VERIFY_COUNT };
 
 constexpr int64_t kMostRows = ((int64_t)1 << 31) - 1;
 constexpr int kVerifyChunk = 4096;   // step_device.h's kChunk
@@ -111,13 +111,14 @@ int register_norm(disc_ctx* c, const disc_norm_desc* d, int32_t* id_out) {
   o->offset = (float)d->weight_offset;
   static const char* const names[] = {"disc_norm1_s",          "disc_norm4_s",          "disc_norm4_s_nt",          "disc_norm4",          "disc_norm4_nt",
                                       "disc_norm1_b",          "disc_norm4_b",          "disc_norm_backward1_s",    "disc_norm_backward4_s", "disc_norm_backward4_s_nt",
-                                      "disc_norm_backward4",   "disc_norm_backward4_nt", "disc_norm_backward4_b",   "disc_norm_join_k"};
+                                      "disc_norm_backward4",   "disc_norm_backward4_nt", "disc_norm_backward2_b", "disc_norm_backward4_b", "disc_norm_join_k"};
   return enter(c, std::move(o), macros, kStepHeader, names, FN_NORM_COUNT, FN_NORM_4, id_out);
 }
 
 // Who has a row: `lanes` threads, a part of a wavefront or all of a block, and which kernel.
 struct RowShape {
   int lanes, block, fn;
+  int per_cu = 0;           // (the gradient's) blocks a CU that the rows are shared out to
   int groups() const { return block / lanes; }
 };
 RowShape norm_shape(const Operator& o, int64_t width, bool few, bool nt) {
@@ -128,12 +129,17 @@ RowShape norm_shape(const Operator& o, int64_t width, bool few, bool nt) {
   const int block = (int)ceil_div(accesses, 256) * 64;
   return {block, block, accesses > 1024 ? FN_NORM_B4 : nt ? FN_NORM_4_NT : FN_NORM_4};
 }
+// Blocks of a gradient: enough that a CU has rows under way while others are being summed, and few enough that the parts, a row of
+// 32 bits each, stay small beside the rows (us with 1, 2, 3, 4, 6 a CU: 65536 x 512 bf16 134, 80, 66, 62, 63; 16384 x 1024 41, 32,
+// 34, 36, 38; 16384 x 4096 214, 144, 117, 119, 132; 8192 x 8192 148, 115, 133, 125, 136; 4096 x 16384 133, 145, 158, 172, 200).
 RowShape backward_shape(const Operator& o, int64_t width, bool nt) {
   const int64_t accesses = ceil_div(width * dtype_bytes(o.dtype), 16);
-  if (accesses <= 64) return {(int)std::max<int64_t>(8, power_of_two(accesses)), 256, FN_BACKWARD_S1};
-  if (accesses <= 256) return {(int)power_of_two(ceil_div(accesses, 4)), 256, nt ? FN_BACKWARD_S4_NT : FN_BACKWARD_S4};
-  const int block = (int)ceil_div(accesses, 256) * 64;
-  return {block, block, accesses > 1024 ? FN_BACKWARD_B4 : nt ? FN_BACKWARD_4_NT : FN_BACKWARD_4};
+  if (accesses <= 64) return {(int)std::max<int64_t>(8, power_of_two(accesses)), 256, FN_BACKWARD_S1, 4};
+  if (accesses <= 256) return {(int)power_of_two(ceil_div(accesses, 4)), 256, nt ? FN_BACKWARD_S4_NT : FN_BACKWARD_S4, 2};
+  if (accesses > 2048) return {1024, 1024, FN_BACKWARD_B4, 1};
+  const int block = (int)(accesses > 1024 ? ceil_div(accesses, 128) : ceil_div(accesses, 256)) * 64;
+  if (accesses > 1024) return {block, block, FN_BACKWARD_B2, 1};
+  return {block, block, nt ? FN_BACKWARD_4_NT : FN_BACKWARD_4, block <= 128 ? 3 : 2};
 }
 
 int check_rows(disc_ctx* c, const Operator& o, int64_t rows, int64_t width) {
@@ -202,11 +208,14 @@ int launch_norm(disc_ctx* c, int32_t id, const int64_t* dims, int n_dims, const 
   return rc;
 }
 
-// Groups of threads that share a gradient's rows, each with a row of partial sums.
-int64_t backward_blocks(disc_ctx* c, const RowShape& s, int64_t rows) { return std::min<int64_t>(ceil_div(rows, s.groups()), 2 * context_cus(c)); }
+// Blocks that share a gradient's rows, each with a row of partial sums.
+int64_t backward_blocks(disc_ctx* c, const RowShape& s, int64_t rows) {
+  const int64_t all = ceil_div(rows, s.groups()), most = s.per_cu * context_cus(c);
+  return all > 0 ? ceil_div(all, ceil_div(all, most)) : 0;   // (each as many rows, within one)
+}
 size_t backward_bytes(disc_ctx* c, const Operator& o, int64_t rows, int64_t width) {
   const RowShape s = backward_shape(o, width, false);
-  return (size_t)(backward_blocks(c, s, rows) * s.groups() * width) * 4;
+  return (size_t)(std::min<int64_t>(ceil_div(rows, s.groups()), s.per_cu * context_cus(c)) * width) * 4;   // (any fewer rows too)
 }
 
 int launch_norm_backward(disc_ctx* c, int32_t id, const int64_t* dims, int n_dims, const void* const* in, int n_in, void* const* out, int n_out,
@@ -252,7 +261,8 @@ int launch_norm_backward(disc_ctx* c, int32_t id, const int64_t* dims, int n_dim
   const RowShape s = backward_shape(*o, a.width, moved < 0 || moved >= kNonTemporalBytes);
   const int64_t blocks = backward_blocks(c, s, a.rows);
   a.lanes = s.lanes;
-  a.parts = (int32_t)(blocks * s.groups());
+  a.parts = (int32_t)blocks;
+  a.groups = (int32_t)(blocks * s.groups());
   if (a.parts > 0 && (!workspace || workspace_bytes < (size_t)a.parts * a.width * 4)) return refuse(c, DISC_ERR_WORKSPACE, "workspace missing or too small");
   if (!aligned(workspace, 16)) return refuse(c, DISC_ERR_INVALID_ARG, "the workspace is not 16-byte aligned");
   a.part = (float*)workspace;
@@ -352,7 +362,7 @@ int register_verify(disc_ctx* c, const disc_verify_desc* d, int32_t* id_out) {
   o->kind = Operator::VERIFY;
   o->key = macros;
   o->dtype = d->dtype;
-  static const char* const names[] = {"disc_verify_sum_k", "disc_verify_pick_k", "disc_verify_k"};
+  static const char* const names[] = {"disc_verify_sum_k", "disc_verify_pick_k"};
   return enter(c, std::move(o), macros, kStepHeader, names, FN_VERIFY_COUNT, FN_VERIFY_SUM, id_out);
 }
 
@@ -360,7 +370,7 @@ int check_verify(disc_ctx* c, int64_t batch, int64_t drafts, int64_t vocabulary)
   if (batch < 0 || batch > 1 << 20) return refuse(c, DISC_ERR_SHAPE, "batch is 0 .. 2^20", batch);
   if (drafts < 0 || drafts > 4096) return refuse(c, DISC_ERR_SHAPE, "drafts is 0 .. 4096", drafts);
   if (vocabulary < 1 || vocabulary > 1 << 30) return refuse(c, DISC_ERR_SHAPE, "vocabulary is 1 .. 2^30", vocabulary);
-  if (batch * ceil_div(vocabulary, kVerifyChunk) > kMostThreads / 256 || batch > kMostThreads / 1024) return refuse(c, DISC_ERR_SHAPE, "too many rows for one call");
+  if (batch * ceil_div(vocabulary, kVerifyChunk) > kMostThreads / 256) return refuse(c, DISC_ERR_SHAPE, "too many rows for one call");
   return DISC_OK;
 }
 
@@ -408,11 +418,6 @@ int launch_verify(disc_ctx* c, int32_t id, const int64_t* dims, int n_dims, cons
   if (context_device(c) < 0) return on_host(c);
   OnDevice on(context_device(c));
   if (!on.ok) return refuse(c, DISC_ERR_HIP, "hipSetDevice failed");
-  if (getenv("VF") ? atoi(getenv("VF")) : a.vocabulary < 65536) {
-    const int rc = enqueue(c, o->fn[FN_VERIFY_ALL], (uint64_t)a.batch, 1, 1024, &a, sizeof a, stream);
-    if (rc == DISC_OK) context_count(c, 1);
-    return rc;
-  }
   int rc = enqueue(c, o->fn[FN_VERIFY_SUM], (uint64_t)a.batch * a.chunks, 1, 256, &a, sizeof a, stream);
   if (rc == DISC_OK) rc = enqueue(c, o->fn[FN_VERIFY_PICK], (uint64_t)a.batch, 1, 256, &a, sizeof a, stream);
   if (rc == DISC_OK) context_count(c, 2);

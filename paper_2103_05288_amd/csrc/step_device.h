@@ -240,37 +240,39 @@ DISC_DEV void norm_body(const NormArgs& A) {
 
 // The gradient.  With u = s / root(s), g = w dy:  dx = (g - u mean(g u)) / root(s) + dtotal,  dweight = sum over rows of dy u.
 // (The rounding to codes counts as the identity.)  A block has a share of the rows and keeps its columns' part of dweight
-// in registers; the parts, a row of the workspace for each group of threads, are summed by a second launch in a fixed order.
+// in registers; the blocks' parts, a row of the workspace each, are summed by a second launch in a fixed order.
 struct NormBackwardArgs {
   const T *total, *weight, *dy, *dtotal;
   T* dx;
   float *dweight, *part;
   i64 total_row, dy_row, dtotal_row, dx_row, rows;
-  int width, lanes, parts;
+  int width, lanes, parts, groups;   // parts: blocks; groups: of threads that have a row, of all blocks
   float offset;
   double eps;
 };
 
-template <bool kNt, bool kBlock, int kN>
+// kLean: weight and dtotal are read again where they are used (their registers are needed for wide rows).
+template <bool kNt, bool kBlock, int kN, bool kLean>
 DISC_DEV void norm_backward_body(const NormBackwardArgs& A) {
   __shared__ double sums[2][kMostWaves], alongs[2][kMostWaves];
   const int lanes = kBlock ? (int)blockDim.x : A.lanes, lane = (int)threadIdx.x % lanes;
   const int mine = kBlock ? (int)blockIdx.x : (int)blockIdx.x * ((int)blockDim.x / lanes) + (int)threadIdx.x / lanes;
   float dw[kN][kV] = {};
   int turn = 0;
-  for (i64 row = mine; row < A.rows; row += A.parts, turn ^= 1) {
-    vec_t h[kN], d[kN], v[kN], t[kN];
+  for (i64 row = mine; row < A.rows; row += A.groups, turn ^= 1) {
+    vec_t h[kN], d[kN], v[kN], t[kLean ? 1 : kN];
     double squares = 0, along = 0;
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
       const int c = (i * lanes + lane) * kV;
       const int n = A.width - c;
-      h[i] = d[i] = v[i] = t[i] = vec_t{};
+      h[i] = d[i] = v[i] = vec_t{};
+      if (!kLean) t[i] = vec_t{};
       if (n <= 0) continue;
       h[i] = take<kNt>(A.total + row * A.total_row + c, n);
       d[i] = take<kNt>(A.dy + row * A.dy_row + c, n);
       v[i] = take<false>(A.weight + c, n);
-      if (A.dtotal) t[i] = take<kNt>(A.dtotal + row * A.dtotal_row + c, n);
+      if (!kLean && A.dtotal) t[i] = take<kNt>(A.dtotal + row * A.dtotal_row + c, n);
     }
 #pragma unroll
     for (int i = 0; i < kN; ++i)
@@ -297,22 +299,43 @@ DISC_DEV void norm_backward_body(const NormBackwardArgs& A) {
     for (int i = 0; i < kN; ++i) {
       const int c = (i * lanes + lane) * kV;
       if (c >= A.width) break;
-      vec_t y;
+      vec_t y, last = {};
+      if (kLean) {
+        v[i] = take<false>(A.weight + c, A.width - c);
+        if (A.dtotal) last = take<kNt>(A.dtotal + row * A.dtotal_row + c, A.width - c);
+      } else {
+        last = t[i];
+      }
 #pragma unroll
       for (int e = 0; e < kV; ++e) {
         const float u = (float)h[i][e] * r, dy = (float)d[i][e], g = dy * ((float)v[i][e] + A.offset);
         dw[i][e] += dy * u;
-        y[e] = (T)(r * (g - u * k) + (float)t[i][e]);
+        y[e] = (T)(r * (g - u * k) + (float)last[e]);
       }
       give<kNt>(A.dx + row * A.dx_row + c, y, A.width - c);
     }
+  }
+  if (!kBlock) {                                            // the groups of a block, one after the other
+    __shared__ float parts[kBlock ? 1 : 256 * kN * kV];
+    const int count = (int)blockDim.x / lanes, span = kN * lanes * kV, group = (int)threadIdx.x / lanes;
+#pragma unroll
+    for (int i = 0; i < kN; ++i)
+#pragma unroll
+      for (int e = 0; e < kV; ++e) parts[group * span + (i * lanes + lane) * kV + e] = dw[i][e];
+    __syncthreads();
+    for (int c = (int)threadIdx.x; c < A.width; c += 256) {
+      float sum = 0;
+      for (int g = 0; g < count; ++g) sum += parts[g * span + c];
+      A.part[(i64)blockIdx.x * A.width + c] = sum;
+    }
+    return;
   }
 #pragma unroll
   for (int i = 0; i < kN; ++i) {
     const int c = (i * lanes + lane) * kV;
 #pragma unroll
     for (int e = 0; e < kV; ++e)
-      if (c + e < A.width) A.part[(i64)mine * A.width + c + e] = dw[i][e];
+      if (c + e < A.width) A.part[(i64)blockIdx.x * A.width + c + e] = dw[i][e];
   }
 }
 
@@ -320,7 +343,7 @@ DISC_DEV void norm_backward_body(const NormBackwardArgs& A) {
 #define DISC_NORM_KERNEL(NAME, THREADS, NT, BLOCK, N) \
   extern "C" __global__ void __launch_bounds__(THREADS) disc_norm##NAME(NormArgs A) { norm_body<NT, BLOCK, N>(A); }
 #define DISC_NORM_BACKWARD_KERNEL(NAME, THREADS, NT, BLOCK, N) \
-  extern "C" __global__ void __launch_bounds__(THREADS) disc_norm_backward##NAME(NormBackwardArgs A) { norm_backward_body<NT, BLOCK, N>(A); }
+  extern "C" __global__ void __launch_bounds__(THREADS) disc_norm_backward##NAME(NormBackwardArgs A) { norm_backward_body<NT, BLOCK, N, (THREADS > 256)>(A); }
 DISC_NORM_KERNEL(1_s, 256, false, false, 1)
 DISC_NORM_KERNEL(4_s, 256, false, false, 4)
 DISC_NORM_KERNEL(4_s_nt, 256, true, false, 4)
@@ -333,7 +356,8 @@ DISC_NORM_BACKWARD_KERNEL(4_s, 256, false, false, 4)
 DISC_NORM_BACKWARD_KERNEL(4_s_nt, 256, true, false, 4)
 DISC_NORM_BACKWARD_KERNEL(4, 256, false, true, 4)
 DISC_NORM_BACKWARD_KERNEL(4_nt, 256, true, true, 4)
-DISC_NORM_BACKWARD_KERNEL(4_b, 1024, false, true, 4)
+DISC_NORM_BACKWARD_KERNEL(2_b, 1024, true, true, 2)
+DISC_NORM_BACKWARD_KERNEL(4_b, 1024, true, true, 4)
 
 // dweight: a block has 16 columns, 64 threads each of every 64th part.
 extern "C" __global__ void __launch_bounds__(1024) disc_norm_join_k(NormBackwardArgs A) {
@@ -832,23 +856,27 @@ struct VerifyArgs {
 
 DISC_DEV double weight(double x) { return x > 0 && x < __builtin_inf() ? x : 0.0; }
 
-// The drafted tokens of sequence b that are kept, by one wavefront: the same in all of its lanes.
+DISC_DEV int length_of(const VerifyArgs& A, i64 b) { return A.lengths ? min(max(A.lengths[b], 0), A.drafts) : A.drafts; }
+
+// The drafted tokens of sequence b that are kept, by a wavefront: the same in all of its lanes.
 DISC_DEV int kept_of(const VerifyArgs& A, i64 b, int lane) {
-  const int n = A.lengths ? min(max(A.lengths[b], 0), A.drafts) : A.drafts;
-  for (int first = 0; first < n; first += 64) {
+  const int n = length_of(A, b);
+  for (int first = 0; first < A.drafts; first += 64) {
     const int i = first + lane;
     bool bad = false;
-    if (i < n) {
+    if (i < A.drafts) {
+      // (what does not depend on each other is read before anything is waited for)
       const int x = A.drafted[b * A.drafts + i];
+      const float u = A.uniforms[b * (A.drafts + 1) + i];
       bad = true;
       if (x >= 0 && x < A.vocabulary) {
         const double p = (double)(float)A.target[b * A.target_batch + i * A.target_row + x];
         const double q = A.draft ? (double)(float)A.draft[b * A.draft_batch + i * A.draft_row + x] : 1.0;
-        bad = !((double)A.uniforms[b * (A.drafts + 1) + i] * q < p);
+        bad = !((double)u * q < p);
       }
     }
-    const u64 mask = __ballot(bad);
-    if (mask) return first + __builtin_ctzll(mask);
+    const u64 mask = __ballot(bad || i >= n);
+    if (mask) return min(first + (int)__builtin_ctzll(mask), n);
   }
   return n;
 }
@@ -858,7 +886,7 @@ struct Place {
   const T *p, *q;       // q: null where nothing is taken off
   int removed;          // the token without weight (no draft probabilities: the drafted one); -1
   DISC_DEV Place(const VerifyArgs& A, i64 b, int kept) {
-    const int n = A.lengths ? min(max(A.lengths[b], 0), A.drafts) : A.drafts;
+    const int n = length_of(A, b);
     p = A.target + b * A.target_batch + kept * A.target_row;
     q = kept < n && A.draft ? A.draft + b * A.draft_batch + kept * A.draft_row : nullptr;
     removed = kept < n && !A.draft ? A.drafted[b * A.drafts + kept] : -1;
@@ -866,31 +894,31 @@ struct Place {
   DISC_DEV bool less() const { return q != nullptr || removed >= 0; }
 };
 
-DISC_DEV double moved(double x, int from) {
+// x of another lane (0 where there is none), by the data-parallel moves of a wavefront
+template <int kControl, int kRows>
+DISC_DEV double moved(double x) {
   const u64 b = __builtin_bit_cast(u64, x);
-  const u32 lo = (u32)__shfl((int)(u32)b, from), hi = (u32)__shfl((int)(u32)(b >> 32), from);
+  const u32 lo = (u32)__builtin_amdgcn_update_dpp(0, (int)(u32)b, kControl, kRows, 0xf, false);
+  const u32 hi = (u32)__builtin_amdgcn_update_dpp(0, (int)(u32)(b >> 32), kControl, kRows, 0xf, false);
   return __builtin_bit_cast(double, ((u64)hi << 32) | lo);
 }
-// the sum over a wavefront, the same in all of its lanes
-DISC_DEV double wave_sum(double x) {
-  const int lane = (int)threadIdx.x % 64;
-  for (int s = 1; s < 64; s *= 2) x += moved(x, lane ^ s);
+// x of one lane, the same number for all of them
+DISC_DEV double of_lane(double x, int lane) {
+  const u64 b = __builtin_bit_cast(u64, x);
+  const u32 lo = (u32)__builtin_amdgcn_readlane((int)(u32)b, lane), hi = (u32)__builtin_amdgcn_readlane((int)(u32)(b >> 32), lane);
+  return __builtin_bit_cast(double, ((u64)hi << 32) | lo);
+}
+// the running sum over a wavefront, this lane's among it (moves of 1, 2, 4, 8 lanes among 16, then of a 16's last and a 32's last)
+DISC_DEV double wave_running(double x) {
+  x += moved<0x111, 0xf>(x);
+  x += moved<0x112, 0xf>(x);
+  x += moved<0x114, 0xf>(x);
+  x += moved<0x118, 0xf>(x);
+  x += moved<0x142, 0xa>(x);
+  x += moved<0x143, 0xc>(x);
   return x;
 }
-// The running sum over the block's threads, this one's among it; `kept`: a number for each wavefront.
-template <int kThreads>
-DISC_DEV double running(double x, double* kept) {
-  const int lane = (int)threadIdx.x % 64, wave = (int)threadIdx.x / 64;
-  for (int s = 1; s < 64; s *= 2) {
-    const double y = moved(x, max(lane - s, 0));
-    if (lane >= s) x += y;
-  }
-  __syncthreads();
-  if (lane == 63) kept[wave] = x;
-  __syncthreads();
-  for (int w = 0; w < wave; ++w) x += kept[w];
-  return x;
-}
+DISC_DEV double wave_sum(double x) { return of_lane(wave_running(x), 63); }
 
 // The weights of kV neighbouring tokens from i on (`end`: behind the last): what is left of p beside q, and p.
 struct Pair {
@@ -934,98 +962,84 @@ DISC_DEV void sum_tokens(const Place& at, i64 begin, int step, i64 end, double& 
   }
 }
 
-// The token of `count` tokens from `first` on at which the running sum, `before` in front of them, passes `goal`: by a block.  (Where
-// rounding leaves none, the last with any weight; -1: none has.)
-template <int kThreads>
-DISC_DEV int pick(const Place& at, bool from_less, i64 first, int count, double before, double goal, double* kept, int* found) {
-  const int each = (count + kThreads - 1) / kThreads;
-  const i64 begin = first + min((int)threadIdx.x * each, count), end = first + min(((int)threadIdx.x + 1) * each, count);
-  if (threadIdx.x == 0) found[0] = 0x7fffffff, found[1] = -1;
-  double sum = 0;
-  for (i64 i = begin; i < end; i += kV) {
-    Pair x;
-    x.take(at, i, end);
-#pragma unroll
-    for (int e = 0; e < kV; ++e) sum += from_less ? x.less(at, i, e) : x.all(e);
-  }
-  double s = before + running<kThreads>(sum, kept);
-  if (sum > 0) {
-    atomicMax(&found[1], (int)threadIdx.x);
-    if (s > goal) atomicMin(&found[0], (int)threadIdx.x);
-  }
-  __syncthreads();
-  const int who = found[0] != 0x7fffffff ? found[0] : found[1];
-  __syncthreads();
-  if (threadIdx.x == 0 && who < 0) found[0] = -1;
-  if ((int)threadIdx.x == who) {
-    s -= sum;
-    int token = -1;
-    bool over = false;
-    for (i64 i = begin; i < end && !over; i += kV) {
-      Pair x;
-      x.take(at, i, end);
-#pragma unroll
-      for (int e = 0; e < kV; ++e) {
-        const double y = from_less ? x.less(at, i, e) : x.all(e);
-        s += y;
-        if (y > 0 && !over) {
-          token = (int)(i + e);
-          over = s > goal;
-        }
-      }
-    }
-    found[0] = token;
-  }
-  __syncthreads();
-  return found[0];
-}
-
-// Which of `n` ranges the goal falls into (u of the whole of their sums), and the sum in front of it; by one thread.
+// Which of up to 64 ranges, a lane each with its sums, u of the whole falls into, and what is in front of it: by a wavefront.
 struct Range {
   int range;              // -1: nothing has any weight
   bool from_less;
   double before, goal;
-};
-template <class F>
-DISC_DEV Range range_of(int n, bool takes_less, float uniform, F sums) {
-  double less = 0, all = 0;
-  for (int i = 0; i < n; ++i) less += sums(i, 0), all += sums(i, 1);
-  Range r;
-  r.from_less = takes_less && less > 0;
-  const double u = (double)uniform;
-  r.goal = (u > 0 ? u : 0.0) * (r.from_less ? less : all);
-  r.range = -1;
-  r.before = 0;
-  double sum = 0;
-  for (int i = 0; i < n; ++i) {
-    const double x = sums(i, r.from_less ? 0 : 1);
-    if (!(x > 0)) continue;
-    r.range = i;
-    r.before = sum;
-    sum += x;
-    if (sum > r.goal) break;
+  DISC_DEV Range(bool takes_less, float uniform, double less, double all) {
+    less = wave_running(less);
+    all = wave_running(all);
+    const double whole_less = of_lane(less, 63);
+    from_less = takes_less && whole_less > 0;
+    const double upto = from_less ? less : all, whole = of_lane(upto, 63), u = (double)uniform;
+    goal = (u > 0 ? u : 0.0) * whole;
+    const double front = moved<0x138, 0xf>(upto);           // (the lane's before it)
+    const u64 some = __ballot(upto > front), over = __ballot(upto > front && upto > goal);
+    range = over ? (int)__builtin_ctzll(over) : some ? 63 - (int)__builtin_clzll(some) : -1;
+    before = of_lane(front, max(range, 0));
   }
-  return r;
+};
+
+// The token of `count` tokens, at most 16 a thread, from `first` on at which the running sum, `before` in front of them, passes the
+// goal (where rounding leaves none, the last with any weight): written by the thread that has it.
+constexpr int kEach = 16, kPairs = kEach / kV;
+template <int kWaves>
+DISC_DEV void pick(const Place& at, const Range& r, i64 first, int count, double* kept, int* over, int* some, int* to) {
+  const int lane = (int)threadIdx.x % 64, wave = (int)threadIdx.x / 64;
+  const i64 begin = first + (int)threadIdx.x * kEach, end = first + count;
+  Pair x[kPairs];
+#pragma unroll
+  for (int u = 0; u < kPairs; ++u) x[u].take(at, min(begin + u * kV, end), end);
+  const auto weight_of = [&](int e) { return r.from_less ? x[e / kV].less(at, begin + e / kV * kV, e % kV) : x[e / kV].all(e % kV); };
+  double sum = 0;
+#pragma unroll
+  for (int e = 0; e < kEach; ++e) sum += weight_of(e);
+  double s = wave_running(sum);
+  if (lane == 63) kept[wave] = s;
+  __syncthreads();
+  double in_front = r.before;
+  for (int w = 0; w < wave; ++w) in_front += kept[w];
+  s += in_front;
+  const u64 has = __ballot(sum > 0), passes = __ballot(sum > 0 && s > r.goal);
+  if (lane == 0) {
+    over[wave] = passes ? wave * 64 + (int)__builtin_ctzll(passes) : -1;
+    some[wave] = has ? wave * 64 + 63 - (int)__builtin_clzll(has) : -1;
+  }
+  __syncthreads();
+  int who = -1;
+  for (int w = 0; w < kWaves; ++w)
+    if (who < 0) who = over[w];
+  if (who < 0)
+    for (int w = 0; w < kWaves; ++w) who = max(who, some[w]);
+  if ((int)threadIdx.x != who) return;
+  s -= sum;
+  int token = -1;
+  bool done = false;
+#pragma unroll
+  for (int e = 0; e < kEach; ++e) {
+    const double y = weight_of(e);
+    s += y;
+    if (y > 0 && !done) {
+      token = (int)(begin + e);
+      done = s > r.goal;
+    }
+  }
+  *to = token;
 }
-DISC_DEV void write_tokens(const VerifyArgs& A, i64 b, int kept, int token, int threads) {
-  for (int i = (int)threadIdx.x; i <= A.drafts; i += threads) A.tokens[b * (A.drafts + 1) + i] = i < kept ? A.drafted[b * A.drafts + i] : i == kept ? token : -1;
+DISC_DEV void write_tokens(const VerifyArgs& A, i64 b, int kept, bool nothing, int threads) {
+  for (int i = (int)threadIdx.x; i <= A.drafts; i += threads)
+    if (i != kept || nothing) A.tokens[b * (A.drafts + 1) + i] = i < kept ? A.drafted[b * A.drafts + i] : -1;
 }
 
 // A block a chunk of a row: what is kept (each block for itself), and the chunk's sums.
 extern "C" __global__ void __launch_bounds__(256) disc_verify_sum_k(VerifyArgs A) {
   __shared__ double kept_sums[2][4];
-  __shared__ int kept_s;
   const i64 b = blockIdx.x / (u32)A.chunks;
   const int chunk = (int)(blockIdx.x - (u32)b * (u32)A.chunks);
-  if (threadIdx.x < 64) {
-    const int k = kept_of(A, b, (int)threadIdx.x);
-    if (threadIdx.x == 0) {
-      kept_s = k;
-      if (chunk == 0) A.accepted[b] = k;
-    }
-  }
-  __syncthreads();
-  const Place at(A, b, kept_s);
+  const int kept = kept_of(A, b, (int)threadIdx.x % 64);    // (each wavefront for itself)
+  if (threadIdx.x == 0 && chunk == 0) A.accepted[b] = kept;
+  const Place at(A, b, kept);
   const i64 first = (i64)chunk * kChunk;
   double less = 0, all = 0;
   sum_tokens<kChunk / (256 * kV)>(at, first + (int)threadIdx.x * kV, 256 * kV, min((i64)A.vocabulary, first + kChunk), less, all);
@@ -1043,55 +1057,34 @@ extern "C" __global__ void __launch_bounds__(256) disc_verify_sum_k(VerifyArgs A
 }
 
 extern "C" __global__ void __launch_bounds__(256) disc_verify_pick_k(VerifyArgs A) {
-  __shared__ double sums[256][2], kept_sums[4];
-  __shared__ Range range;
-  __shared__ int found[2];
+  __shared__ double kept_sums[4];
+  __shared__ int over[4], some[4];
   const i64 b = blockIdx.x;
+  const int lane = (int)threadIdx.x % 64;
   const int kept = A.accepted[b];
-  const Place at(A, b, kept);
+  const float uniform = A.uniforms[b * (A.drafts + 1) + A.drafts];
   const double* part = A.part + b * A.chunks * 2;
-  // (first groups of chunks, one a thread, then the chunks of the group)
-  const int each = (A.chunks + 255) / 256, groups = (A.chunks + each - 1) / each;
-  double less = 0, all = 0;
-  for (int i = (int)threadIdx.x * each; i < min(((int)threadIdx.x + 1) * each, A.chunks); ++i) less += part[2 * i], all += part[2 * i + 1];
-  sums[threadIdx.x][0] = less;
-  sums[threadIdx.x][1] = all;
-  __syncthreads();
-  if (threadIdx.x == 0) range = range_of(groups, at.less(), A.uniforms[b * (A.drafts + 1) + A.drafts], [&](int i, int k) { return sums[i][k]; });
-  __syncthreads();
-  int token = -1;
-  if (range.range >= 0)
-    token = pick<256>(at, range.from_less, (i64)range.range * each * kChunk, min(each * kChunk, A.vocabulary - range.range * each * kChunk), range.before, range.goal, kept_sums, found);
-  write_tokens(A, b, kept, token, 256);
-}
-
-// All of a sequence by one block: its wavefronts sum a sixteenth of the row each.
-extern "C" __global__ void __launch_bounds__(1024) disc_verify_k(VerifyArgs A) {
-  __shared__ double sums[16][2], kept_sums[16];
-  __shared__ Range range;
-  __shared__ int found[2], kept_s;
-  const i64 b = blockIdx.x;
-  const int lane = (int)threadIdx.x % 64, wave = (int)threadIdx.x / 64;
-  if (wave == 0) {
-    const int k = kept_of(A, b, lane);
-    if (lane == 0) kept_s = A.accepted[b] = k;
-  }
-  __syncthreads();
-  const int kept = kept_s;
   const Place at(A, b, kept);
-  const int share = (A.vocabulary + 16 * 64 * kV - 1) / (16 * 64 * kV) * (64 * kV);
-  const i64 first = min((i64)wave * share, (i64)A.vocabulary), end = min(first + share, (i64)A.vocabulary);
+  // (each wavefront for itself: first a lane a group of chunks, then the chunks of the group)
+  const int each = (A.chunks + 63) / 64;
   double less = 0, all = 0;
-  sum_tokens<4>(at, first + lane * kV, 64 * kV, end, less, all);
-  less = wave_sum(less);
-  all = wave_sum(all);
-  if (lane == 0) sums[wave][0] = less, sums[wave][1] = all;
-  __syncthreads();
-  if (threadIdx.x == 0) range = range_of(16, at.less(), A.uniforms[b * (A.drafts + 1) + A.drafts], [&](int i, int k) { return sums[i][k]; });
-  __syncthreads();
-  int token = -1;
-  if (range.range >= 0)
-    token = pick<1024>(at, range.from_less, (i64)range.range * share, min(share, A.vocabulary - range.range * share), range.before, range.goal, kept_sums, found);
-  write_tokens(A, b, kept, token, 1024);
+  for (int i = lane * each; i < min((lane + 1) * each, A.chunks); ++i) less += part[2 * i], all += part[2 * i + 1];
+  Range r(at.less(), uniform, less, all);
+  if (r.range >= 0) {
+    int chunk = r.range * each;
+    if (each > 1) {
+      int last = chunk;
+      for (int i = chunk; i < min(chunk + each, A.chunks); ++i) {
+        const double x = part[2 * i + (r.from_less ? 0 : 1)];
+        if (!(x > 0)) continue;
+        last = i;
+        if (r.before + x > r.goal) break;
+        r.before += x;
+      }
+      chunk = last;
+    }
+    pick<4>(at, r, (i64)chunk * kChunk, min(kChunk, A.vocabulary - chunk * kChunk), kept_sums, over, some, A.tokens + b * (A.drafts + 1) + kept);
+  }
+  write_tokens(A, b, kept, r.range < 0, 256);
 }
 #endif  // DISC_VERIFY

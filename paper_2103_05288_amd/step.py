@@ -61,8 +61,15 @@ class _Handle:
         self.ctx._check(fn(self.ctx.h, self.id, arr, n, C.byref(out)))
         return int(out.value)
 
+    def _quickly(self, name: str, fn, number, *rest) -> bool:
+        """All of a call that fits, in C; False: through the checks here, which say why it does not."""
+        quick = getattr(binding._pylaunch, name, None)
+        rc = None if quick is None else quick(fn, self.ctx.h.value or 0, self.id, self._dtype, self._device, number, *rest)
+        if rc:
+            self.ctx._check(rc)
+        return rc is not None
+
     def _call(self, fn, dims, inputs, outputs, workspace, stream):
-        stream = self._stream(self._device) if stream is None else stream
         rc = binding._pylaunch.launch(fn, self.ctx.h.value or 0, self.id, dims, inputs, outputs, workspace, 0, stream)
         if rc != 0:
             self.ctx._check(rc)
@@ -81,6 +88,9 @@ class NormHandle(_Handle):
     def launch(self, x, weight, codes, scales, residual=None, total=None, stream: Optional[int] = None):
         """codes [rows, width] of the storage's type and scales (fp32 [rows]) of the norm of x [rows, width], or with a residual
         of x + residual, which total gets (it may be x or residual)."""
+        stream = self._stream(self._device) if stream is None else stream
+        if self._quickly("norm", self._fn, 0, self._stored, self._f32, x, weight, codes, scales, residual, total, stream):
+            return
         rows, width, a = self._rows(x, "x", self._dtype)
         self._dense(weight, "weight", self._dtype, (width,))
         _, _, d = self._rows(codes, "codes", self._stored, rows, width)
@@ -102,6 +112,9 @@ class NormHandle(_Handle):
         """dx [rows, width], the gradient of x and of the residual, and dweight (fp32 [width], overwritten), from the rows that were
         normed (total; x where there was no residual), the gradient dy of the norm's result and that of total, dtotal.  dx may be
         total, dy or dtotal."""
+        stream = self._stream(self._device) if stream is None else stream
+        if self._quickly("norm_backward", self._backward, 0, self._f32, total, weight, dy, dx, dweight, dtotal, workspace, stream):
+            return
         rows, width, a = self._rows(total, "total", self._dtype)
         self._dense(weight, "weight", self._dtype, (width,))
         _, _, b = self._rows(dy, "dy", self._dtype, rows, width)
@@ -129,6 +142,9 @@ class Linear4Handle(_Handle):
         """out [rows, n] = x [rows, k] times the weights (uint8 [n, k / 2], two elements a byte, the even one in the lower four
         bits), their scales [n, k / group] and zero points (uint8, of the same shape), plus bias [n].  8-bit rows come with
         row_scales (fp32 [rows])."""
+        stream = self._stream(self._device) if stream is None else stream
+        if self._quickly("linear4", self._fn, self.group, self._row, self._f32, self._u8, self._scaled, self.zeros, x, weights, scales, out, row_scales, zeros, bias, stream):
+            return
         rows, k, a = self._rows(x, "x", self._row)
         if k % self.group:
             _refuse(f"x has rows of {k} elements, a multiple of the group, {self.group}, is wanted")
@@ -179,6 +195,9 @@ class VerifyHandle(_Handle):
         were kept) of the drafted tokens (int32 [batch, drafts]), the target's probabilities [batch, drafts + 1, vocabulary], the draft's
         [batch, drafts, vocabulary] (None: it drew each for certain) and uniforms (fp32 [batch, drafts + 1] in [0, 1)).  lengths
         (int32 [batch]): how many of a sequence's drafted tokens there are."""
+        stream = self._stream(self._device) if stream is None else stream
+        if self._quickly("verify", self._fn, 0, self._f32, self._i32, target, drafted, uniforms, tokens, accepted, draft, lengths, workspace, stream):
+            return
         (batch, places, vocabulary), a, b = self._probabilities(target, "target")
         drafts = places - 1
         if drafts < 0:
