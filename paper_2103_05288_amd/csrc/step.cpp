@@ -45,33 +45,29 @@ enum { FN_NORM_S1 = 0, FN_NORM_S4, FN_NORM_S4_NT, FN_NORM_4, FN_NORM_4_NT, FN_NO
        FN_BACKWARD_4_NT, FN_BACKWARD_B2, FN_BACKWARD_B4, FN_NORM_JOIN, FN_NORM_COUNT };
 struct LinearKernel {
   const char* name;
-  int m, n, rows, split, teams;   // tiles of 16 rows of x and of weights, rows of a tile of x, wavefronts of a team, teams of a block
+  int m, n, split, teams;   // tiles of 16 rows of x and of weights, wavefronts of a team, teams of a block
 };
-#define LINEAR_KERNEL(M, N, R, S, W, B) {"disc_linear_" #M "_" #N "_" #R "_" #S "_" #W "_" #B "_k", M, N, R, S, W}
+#define FEW(N, R, S, W) {"disc_linear_" #N "_" #R "_" #S "_" #W "_k", 1, N, S, W}
+#define WIDE(M, N, S, W, B) {"disc_linear_wide_" #M "_" #N "_" #S "_" #W "_" #B "_k", M, N, S, W}
 constexpr LinearKernel kLinear[] = {
-    LINEAR_KERNEL(1, 1, 1, 1, 8, 2),
-    LINEAR_KERNEL(1, 1, 1, 16, 1, 2),
-    LINEAR_KERNEL(1, 1, 1, 8, 1, 2),
-    LINEAR_KERNEL(1, 2, 1, 8, 1, 2),
-    LINEAR_KERNEL(1, 1, 4, 1, 8, 2),
-    LINEAR_KERNEL(1, 1, 4, 8, 1, 2),
-    LINEAR_KERNEL(1, 2, 4, 8, 1, 2),
-    LINEAR_KERNEL(1, 1, 16, 8, 1, 2),
-    LINEAR_KERNEL(1, 4, 16, 4, 1, 2),
-    LINEAR_KERNEL(2, 2, 16, 8, 1, 2),
-    LINEAR_KERNEL(4, 2, 16, 4, 1, 2),
+    FEW(1, 1, 1, 8),  FEW(1, 1, 16, 1), FEW(1, 1, 8, 1),     FEW(2, 1, 8, 1),     FEW(1, 4, 1, 8),     FEW(1, 4, 8, 1),     FEW(2, 4, 8, 1),
+    FEW(1, 16, 8, 1), FEW(4, 16, 4, 1), WIDE(1, 2, 2, 4, 2), WIDE(2, 1, 4, 2, 1), WIDE(2, 2, 2, 4, 1), WIDE(4, 1, 4, 2, 1), WIDE(4, 1, 2, 8, 1),
 };
-#undef LINEAR_KERNEL
+#undef FEW
+#undef WIDE
 constexpr int kLinearCount = sizeof kLinear / sizeof kLinear[0];
-// Which of them.  A team's wavefronts share a row's elements: 256 each at a time.  (us, the first four by rows x k x n:
-//  1 x 512 x 32768 4.4, 16.1, 7.4, 6.2; 1 x 1024 x 32768 6.3, 17.1, 8.0, 7.2; 1 x 4096 x 4096 9.3, 4.8, 4.9, 5.8;
-//  1 x 16384 x 1024 49, 8.8, 9.4, 14; 1 x 4096 x 12288 18, 12.9, 9.4, 10.5; 1 x 8192 x 131072 140, 168, 126, 112;
-//  of 16 rows 16 x 4096 x 4096 8.0, 13; 16 x 512 x 32768 8.8, 5.4; 10 x 2048 x 20000 13.8, 11.5.)
+// Which of them, by rows x k x n (us).  Of one row, the first four: a team's wavefronts take 256 elements each at a time, so that rows
+// are shared out by as many as leave each something; where columns are many, two tiles share what is loaded of x.
+//   1 x 512 x 32768 4.4, 16.1, 7.4, 6.2; 1 x 1024 x 32768 6.3, 17.1, 8.0, 7.2; 1 x 4096 x 4096 9.3, 4.8, 4.9, 5.8;
+//   1 x 16384 x 1024 49, 8.8, 9.4, 14; 1 x 4096 x 12288 18, 12.9, 9.4, 10.5; 1 x 8192 x 131072 140, 168, 126, 112.
+// Of 5 .. 16, the two without LDS and the one with it: 16 x 4096 x 4096 8.3, 13.4, 17; 16 x 4096 x 12288 17.5, 13.0, 16.0; 16 x 4096 x 28672
+// 38.7, 23.4, 19.9; 10 x 2048 x 20000 13.9, 12.2, 10.3; 16 x 512 x 32768 10.3, 6.0, 6.0; 5 x 8192 x 131072 195, 147, 147.
+// Of more, blocks of 32 columns and of 128: 32 x 4096 x 8192 11.1, 21.6; 32 x 4096 x 28672 42, 25; 61 x 8192 x 8192 36, 71; 64 x 4096 x 28672 66, 34.
 int linear_kernel(int64_t rows, int64_t n, int64_t k, int64_t cus) {
   const int64_t tiles = ceil_div(n, 16);
-  if (rows > 32) return 10;
-  if (rows > 16) return 9;
-  if (rows > 4) return tiles <= 2 * cus && k > 512 ? 7 : 8;
+  if (rows > 32) return tiles <= 4 * cus ? 12 : 13;
+  if (rows > 16) return tiles <= 4 * cus ? 10 : 11;
+  if (rows > 4) return tiles > 4 * cus ? 9 : tiles <= 2 * cus && k > 512 ? 7 : 8;
   if (rows > 1) return k <= 1024 ? 4 : tiles <= 4 * cus ? 5 : 6;
   return k <= 1024 ? 0 : tiles <= cus ? 1 : tiles <= 4 * cus ? 2 : 3;
 }

@@ -390,6 +390,15 @@ extern "C" __global__ void __launch_bounds__(1024) disc_norm_join_k(NormBackward
 #ifdef DISC_LINEAR4
 // =================================================================================================
 // y[m, n] = r[m] sum_k x[m, k] s[n, k / G] (c[n, k] - z[n, k / G]) + bias[n] with codes c of 4 bits.
+// A group's products are summed with the codes as they are (128 + c of bf16, c - 8 of f16, c of i8), and the zero point is taken off
+// with the sum of the group's x, which a product with ones gives in the layout of the results:
+//   sum x (c - z) = sum x (128 + c) - (128 + z) sum x,
+// in 32 bits (i8: whole numbers, exact); then times s, added up over the groups in 32 bits.  What the 128 adds to the roundings is below
+// 2^-17 of a result's size, where a bf16 result has 2^-9; of f16 results, which have 2^-12, c - 8 is formed instead.
+// Bound by the weights' bytes where there are few rows, and with more by what a CU's memory pipe takes to bring x to the lanes: a load
+// of 16 bytes a lane costs it the same whether the lanes' addresses differ or not.  So x of up to 4 rows is loaded in whole wavefronts
+// and turned into place (linear_body), and of more rows goes through LDS, where 64 or 128 columns share it (linear_wide_body).
+// Unpacking costs next to nothing beside that (with all of it left out, 1 x 8192 x 131072 takes 118 us, not 122).
 // =================================================================================================
 #if DISC_T_F16
 typedef _Float16 T;
@@ -499,34 +508,25 @@ struct Words {
 };
 
 // What a lane has of kRun neighbouring blocks of 128 elements: 32 neighbouring codes of a row and block of kN tiles of 16 rows of
-// weights, with their groups' scales and zero points, and of kM tiles of kR rows of x.
-//
-// A product takes its x from the first kR of each 16 lanes (the others' results are not used).  Where kR is less than 16, a load
-// fetches what 16 / kR products take, one behind the other in the 16 lanes, and each is turned to the front when its product is due:
-// loads of x that fill kR lanes of 16 cost as much as whole ones.
+// weights, with their groups' scales and zero points (loaded for the run at once: a load of 2 bytes from each of 16 rows costs as much
+// as one of 16 bytes; 28672 rows of 4096, one of x: 22 -> 16 us).
 constexpr int kXs = kKind == 2 ? 2 : 4;                     // operands of a block: 16 bytes a lane (8 of e4m3 in memory)
-template <int kR, int kRun>
-constexpr int loads_of() {
-  return (kRun * kXs * kR + 15) / 16;
-}
-template <int kM, int kN, int kR, int kRun>
-struct Block {
+template <int kN, int kRun>
+struct Weights {
   u32x4 w[kRun][kN];
-  u32x4 x[kM][loads_of<kR, kRun>()];
   Words<2 * kGroups * kRun> scale[kN];
   Words<kGroups * kRun> zero[kN];
 };
 
 struct Lane {
-  const u8* x[4];          // its row of each tile of x, from the first element it loads on
-  const u8 *w, *s, *z;     // the block's first row of weights, of scales, of zero points
+  const u8 *w, *s, *z;     // the team's first row of weights, of scales, of zero points
   u32 w_row[4], s_row[4];  // from there to its row of each tile: bytes of codes, groups
   int c, q, k, groups;
 };
 
 // kWhole: all of the blocks is there; else one block is taken, the last, which may have 32, 64 or 96 elements.
-template <bool kWhole, int kM, int kN, int kR, int kRun>
-DISC_DEV void take_block(const Lane& L, int b, Block<kM, kN, kR, kRun>& B) {
+template <bool kWhole, int kN, int kRun>
+DISC_DEV void take_weights(const Lane& L, int b, Weights<kN, kRun>& B) {
   static_assert(kWhole || kRun == 1, "");
   const int q = L.q;
 #pragma unroll
@@ -554,34 +554,9 @@ DISC_DEV void take_block(const Lane& L, int b, Block<kM, kN, kR, kRun>& B) {
       }
     }
   }
-#pragma unroll
-  for (int i = 0; i < loads_of<kR, kRun>(); ++i) {
-    // the operand that this lane loads: the n-th of the run
-    const int n = kR == 16 ? i : min(i * (16 / kR) + L.c / kR, kRun * kXs - 1), j = kKind == 2 ? n % kXs * 2 : n % kXs;
-    const int k = n / kXs * kBlockK + place(j, q);
-    const bool here = kWhole || b * kBlockK + k < L.k, too = kWhole || b * kBlockK + k + 32 < L.k;
-#pragma unroll
-    for (int t = 0; t < kM; ++t) {
-      const u8* p = L.x[t] + ((i64)b * kBlockK + k) * kRowSize;
-      u32x4 v = {0, 0, 0, 0};
-      if (kRowSize == 2 || (kKind == 2 && kG > 32)) {       // (i8: the elements of two dwords of codes follow each other)
-        if (here) v = *(const u32x4_u*)p;
-      } else {
-        if (here) {
-          const u32x2 h = *(const u32x2_u*)p;
-          v[0] = h[0], v[1] = h[1];
-        }
-        if (kKind == 2 && too) {
-          const u32x2 h = *(const u32x2_u*)(p + 32);
-          v[2] = h[0], v[3] = h[1];
-        }
-      }
-      B.x[t][i] = v;
-    }
-  }
 }
 
-// bf16 rows times 2^-32 (see linear_body)
+// bf16 rows times 2^-32 (see finish)
 DISC_DEV u32x4 lowered(u32x4 v) {
   u32x4 r;
 #pragma unroll
@@ -594,6 +569,12 @@ DISC_DEV u32x4 lowered(u32x4 v) {
   return r;
 }
 
+struct Yes {
+  static constexpr bool value = true;
+};
+struct No {
+  static constexpr bool value = false;
+};
 template <int K>
 struct Sum {
   typedef f32x4 type;
@@ -622,6 +603,24 @@ DISC_DEV A multiply(const u32x4* x, F w, int j0, A acc) {
   return acc;
 }
 
+// 16 bytes of x for a product (8 of e4m3; of i8 for two of groups of 32, whose elements are 32 apart).  `here`, `too`: whether they are
+// in the row.
+DISC_DEV u32x4 load_x(const u8* p, bool here, bool too) {
+  u32x4 v = {0, 0, 0, 0};
+  if (kRowSize == 2 || (kKind == 2 && kG > 32)) {
+    if (here) v = *(const u32x4_u*)p;
+  } else {
+    if (here) {
+      const u32x2 h = *(const u32x2_u*)p;
+      v[0] = h[0], v[1] = h[1];
+    }
+    if (kKind == 2 && too) {
+      const u32x2 h = *(const u32x2_u*)(p + 32);
+      v[2] = h[0], v[3] = h[1];
+    }
+  }
+  return v;
+}
 // What was loaded of x as operands: in the order of the codes, e4m3 in half precision.
 DISC_DEV u32x4 operand(u32x4 v, bool down) {
   if (kKind == 2)
@@ -629,6 +628,153 @@ DISC_DEV u32x4 operand(u32x4 v, bool down) {
                  __builtin_amdgcn_perm(v[3], v[2], 0x07050301u)};
   if (kRowSize == 1) return reorder8(u32x2{v[0], v[1]});
   return reorder(kKind == 0 && down ? lowered(v) : v);
+}
+// total += a block's products: codes w of each tile of weights with the scales and zero points from number `at` on, x(t, i) the operands
+template <int kM, int kN, class X, class S, class Z>
+DISC_DEV void add_products(const u32x4 (&codes)[kN], const S* scale, const Z* zero, int at0, X x, float lower, f32x4 (&total)[kM][kN]) {
+  constexpr int kEach = 4 / kGroups;                        // dwords of codes of a group
+  typedef typename Sum<kKind>::type acc_t;
+  u32x4 w[kN][4];
+#pragma unroll
+  for (int n = 0; n < kN; ++n) {
+    const u32x4 d = arrange(codes[n]);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const u32 c = d[j];
+      if (kKind == 2) {
+        w[n][j][0] = c & 0x0f0f0f0fu;
+        w[n][j][1] = (c >> 4) & 0x0f0f0f0fu;
+      } else {
+        w[n][j] = widen(c);
+      }
+    }
+  }
+#pragma unroll
+  for (int g = 0; g < kGroups; ++g) {
+    float s[kN];
+    int z[kN];
+#pragma unroll
+    for (int n = 0; n < kN; ++n) {
+      const int at = at0 + g;
+      const u32 pair = scale[n].w[at / 2];
+      const u16 bits = (u16)(at % 2 ? pair >> 16 : pair);
+      s[n] = (float)__builtin_bit_cast(T, bits) * lower;
+      z[n] = DISC_ZEROS ? (int)((zero[n].w[at / 4] >> (8 * (at % 4))) & 0xffu) : 8;
+    }
+#pragma unroll
+    for (int t = 0; t < kM; ++t) {
+      constexpr int kUnits = kKind == 2 && kGroups == 4 ? 1 : kXs / kGroups;   // operands of a group (i8 of groups of 32: half a one)
+      const int first = g * kXs / kGroups;
+      u32x4 v[kUnits];
+#pragma unroll
+      for (int i = 0; i < kUnits; ++i) v[i] = x(t, first + i);
+      const int j0 = kKind == 2 && kGroups == 4 ? g % 2 : 0;
+      // the sum of the rows' elements over the group, in the results' layout: what the codes' zero points are taken off with
+      acc_t sum = {};
+      if (kKind != 1 || DISC_ZEROS) {
+        const u32 one = kKind == 2 ? 0x01010101u : kKind == 0 ? 0x3f803f80u : 0x3c003c00u;
+        sum = multiply(v, [&](int) { return u32x4{one, one, one, one}; }, j0, sum);
+      }
+#pragma unroll
+      for (int n = 0; n < kN; ++n) {
+        const acc_t acc = multiply(v, [&](int j) { return w[n][g * kEach + j - j0]; }, j0, acc_t{});
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if constexpr (kKind == 2) total[t][n][i] += s[n] * (float)(acc[i] - z[n] * sum[i]);
+          else if constexpr (kKind == 0) total[t][n][i] += s[n] * (acc[i] - (128.f + (float)z[n]) * sum[i]);
+          else total[t][n][i] += s[n] * (DISC_ZEROS ? acc[i] - (float)(z[n] - 8) * sum[i] : acc[i]);
+        }
+      }
+    }
+  }
+}
+
+// The lane's rows of a team's tiles of weights, from column col0 on.
+template <int kN>
+DISC_DEV Lane lane_of(const LinearArgs& A, int col0) {
+  Lane L;
+  L.c = (int)threadIdx.x % 16;
+  L.q = (int)threadIdx.x % 64 / 16;
+  const int from = min(col0, A.n - 1);
+  L.w = A.weights + (i64)from * (A.k / 2);
+  L.s = (const u8*)(A.scales + (i64)from * A.groups);
+  L.z = DISC_ZEROS ? A.zeros + (i64)from * A.groups : nullptr;
+#pragma unroll
+  for (int t = 0; t < kN; ++t) {
+    const int n = min(t * 16 + L.c, A.n - 1 - from);        // (rows behind the last: copies of it, not stored)
+    L.w_row[t] = (u32)n * (u32)(A.k / 2);
+    L.s_row[t] = (u32)n * (u32)A.groups;
+  }
+  L.k = A.k;
+  L.groups = A.groups;
+  return L;
+}
+
+// A team's sums brought together and written.  Where a result is no finite number, the sums on the way to it may have passed 32 bits:
+// false, and the whole block forms it again of scales times 2^-32 and of bf16 rows times 2^-32 (what was finite stays).
+template <int kM, int kN, int kSplit, int kTeams>
+DISC_DEV bool finish(const LinearArgs& A, const f32x4 (&total)[kM][kN], float* kept, int team, int share, int row0, int col0, bool again) {
+  const int lane = (int)threadIdx.x % 64, c = lane % 16, q = lane / 16, wave = team * kSplit + share;
+  bool lost = false;
+  const auto write = [&](int m, int col, float y) {
+    if (m >= A.rows || col >= A.n) return;
+    if (DISC_ROWS) y *= A.row_scales[m];
+    if (again) y *= 0x1p32f * (kKind == 0 ? 0x1p32f : 1.f);
+    if (!again) lost |= !(__builtin_fabsf(y) < __builtin_inff());
+    if (A.bias) y += (float)A.bias[col];
+    T* to = A.out + (m * A.out_row + col);
+    if (!again || !(__builtin_fabsf((float)*to) < __builtin_inff())) *to = (T)y;
+  };
+  if (kSplit == 1) {
+#pragma unroll
+    for (int t = 0; t < kM; ++t)
+#pragma unroll
+      for (int n = 0; n < kN; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) write(row0 + t * 16 + q * 4 + i, col0 + n * 16 + c, total[t][n][i]);
+    return again || !__any(lost);                           // (its wavefronts have nothing to do with each other)
+  }
+#pragma unroll
+  for (int t = 0; t < kM; ++t)
+#pragma unroll
+    for (int n = 0; n < kN; ++n)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) kept[(wave * kM * kN + t * kN + n) * 256 + (q * 4 + i) * 16 + c] = total[t][n][i];
+  __syncthreads();
+  for (int o = share * 64 + lane; o < kM * kN * 256; o += kSplit * 64) {
+    float y = 0;
+#pragma unroll
+    for (int v = 0; v < kSplit; ++v) y += kept[(team * kSplit + v) * kM * kN * 256 + o];
+    write(row0 + o / (kN * 256) * 16 + o % 256 / 16, col0 + o / 256 % kN * 16 + o % 16, y);
+  }
+  return !__syncthreads_or(lost) || again;
+}
+
+// ---- few rows ---------------------------------------------------------------------------------------
+// A product takes its x from the first kR of each 16 lanes (the others' results are not used).  Where kR is less than 16, a load
+// fetches what 16 / kR products take, one behind the other in the 16 lanes, and each is turned to the front when its product is due
+// (28672 x 4096, one row: 18 -> 16 us; its registers let four blocks of a run be under way instead of one).
+constexpr int kRun = 2;                                     // blocks of a run
+template <int kR>
+constexpr int loads_of(int run) {
+  return (run * kXs * kR + 15) / 16;
+}
+template <int kN, int kR, int kBlocks>
+struct Run : Weights<kN, kBlocks> {
+  u32x4 x[loads_of<kR>(kBlocks)];
+};
+template <bool kWhole, int kN, int kR, int kBlocks>
+DISC_DEV void take_run(const Lane& L, const u8* x, int b, Run<kN, kR, kBlocks>& B) {
+  const int q = L.q;
+  take_weights<kWhole, kN, kBlocks>(L, b, B);
+#pragma unroll
+  for (int i = 0; i < loads_of<kR>(kBlocks); ++i) {
+    // the operand that this lane loads: the n-th of the run
+    const int n = kR == 16 ? i : min(i * (16 / kR) + L.c / kR, kBlocks * kXs - 1), j = kKind == 2 ? n % kXs * 2 : n % kXs;
+    const int k = n / kXs * kBlockK + place(j, q);
+    const bool here = kWhole || b * kBlockK + k < L.k, too = kWhole || b * kBlockK + k + 32 < L.k;
+    B.x[i] = load_x(x + ((i64)b * kBlockK + k) * kRowSize, here, too);
+  }
 }
 // v of the lanes kBy behind, among 16
 template <int kBy>
@@ -651,184 +797,192 @@ DISC_DEV void operands_of(const u32x4* v, u32x4* x) {
     operands_of<kR, kAt + 1, kCount - 1>(v, x + 1);
   }
 }
-
-// total += block kAt of the run's part of the products (x as operands already)
-template <int kAt, int kM, int kN, int kR, int kRun>
-DISC_DEV void add_block(const Block<kM, kN, kR, kRun>& B, float lower, f32x4 (&total)[kM][kN]) {
-  constexpr int kEach = 4 / kGroups, r = kAt;               // dwords of codes of a group
-  u32x4 x[kM][kXs];
-#pragma unroll
-  for (int t = 0; t < kM; ++t) operands_of<kR, kAt * kXs, kXs>(B.x[t], x[t]);
-  // sums of the rows' elements over each group, in the results' layout: what the codes' zero points are taken off with
-  typedef typename Sum<kKind>::type acc_t;
-  acc_t sums[kM][kGroups];
-#pragma unroll
-  for (int t = 0; t < kM; ++t)
-#pragma unroll
-    for (int g = 0; g < kGroups; ++g) {
-      sums[t][g] = acc_t{};
-      if (kKind != 1 || DISC_ZEROS) {
-        const u32x4 ones = kKind == 2 ? u32x4{0x01010101u, 0x01010101u, 0x01010101u, 0x01010101u} : kKind == 0 ? u32x4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u}
-                                                                                                  : u32x4{0x3c003c00u, 0x3c003c00u, 0x3c003c00u, 0x3c003c00u};
-        sums[t][g] = multiply(x[t], [&](int) { return ones; }, g * kEach, sums[t][g]);
-      }
-    }
-#pragma unroll
-  for (int n = 0; n < kN; ++n) {
-    const u32x4 d = arrange(B.w[r][n]);
-    u32x4 w[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const u32 c = d[j];
-      if (kKind == 2) {
-        w[j][0] = c & 0x0f0f0f0fu;
-        w[j][1] = (c >> 4) & 0x0f0f0f0fu;
-      } else {
-        w[j] = widen(c);
-      }
-    }
-#pragma unroll
-    for (int g = 0; g < kGroups; ++g) {
-      const int at = r * kGroups + g;
-      const u32 pair = B.scale[n].w[at / 2];
-      const u16 bits = (u16)(at % 2 ? pair >> 16 : pair);
-      const float s = (float)__builtin_bit_cast(T, bits) * lower;
-      const int z = DISC_ZEROS ? (int)((B.zero[n].w[at / 4] >> (8 * (at % 4))) & 0xffu) : 8;
-#pragma unroll
-      for (int t = 0; t < kM; ++t) {
-        const acc_t acc = multiply(x[t], [&](int j) { return w[j]; }, g * kEach, acc_t{});
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if constexpr (kKind == 2) total[t][n][i] += s * (float)(acc[i] - z * sums[t][g][i]);
-          else if constexpr (kKind == 0) total[t][n][i] += s * (acc[i] - (128.f + (float)z) * sums[t][g][i]);
-          else total[t][n][i] += s * (DISC_ZEROS ? acc[i] - (float)(z - 8) * sums[t][g][i] : acc[i]);
-        }
-      }
-    }
-  }
-}
-
-template <int kAt, int kM, int kN, int kR, int kRun>
-DISC_DEV void add_blocks(const Block<kM, kN, kR, kRun>& B, float lower, f32x4 (&total)[kM][kN]) {
-  if constexpr (kAt < kRun) {
-    add_block<kAt>(B, lower, total);
+// total += the run's products from block kAt on (x as operands already)
+template <int kAt, int kN, int kR, int kBlocks>
+DISC_DEV void add_blocks(const Run<kN, kR, kBlocks>& B, float lower, f32x4 (&total)[1][kN]) {
+  if constexpr (kAt < kBlocks) {
+    u32x4 x[kXs];
+    operands_of<kR, kAt * kXs, kXs>(B.x, x);
+    add_products<1, kN>(B.w[kAt], B.scale, B.zero, kAt * kGroups, [&](int, int i) { return x[i]; }, lower, total);
     add_blocks<kAt + 1>(B, lower, total);
   }
 }
-template <int kM, int kN, int kR, int kRun>
-DISC_DEV void add_run(Block<kM, kN, kR, kRun>& B, bool down, f32x4 (&total)[kM][kN]) {
+template <int kN, int kR, int kBlocks>
+DISC_DEV void add_run(Run<kN, kR, kBlocks>& B, bool down, f32x4 (&total)[1][kN]) {
 #pragma unroll
-  for (int t = 0; t < kM; ++t)
-#pragma unroll
-    for (int i = 0; i < loads_of<kR, kRun>(); ++i) B.x[t][i] = operand(B.x[t][i], down);
+  for (int i = 0; i < loads_of<kR>(kBlocks); ++i) B.x[i] = operand(B.x[i], down);
   add_blocks<0>(B, down ? 0x1p-32f : 1.f, total);
 }
 
-// kSplit wavefronts share the elements of a row, in blocks of 128, and add up what they have through LDS; kTiles such teams in a
-// block have kM tiles of x and kN tiles of weights each.
-template <int kM, int kN, int kR, int kSplit, int kTeams, int kRun>
+// kSplit wavefronts share the elements of a row, in runs of blocks, and add up what they have through LDS: a team.  kTeams of them in
+// a block have kN tiles of weights each, and the same tile of x.
+template <int kN, int kR, int kSplit, int kTeams>
 DISC_DEV void linear_body(const LinearArgs& A) {
-  __shared__ float kept[kSplit > 1 ? kTeams * kSplit : 1][kSplit > 1 ? kM * kN * 256 : 1];
-  const int lane = (int)threadIdx.x % 64, wave = (int)threadIdx.x / 64, team = wave / kSplit, share = wave % kSplit;
-  const int c = lane % 16, q = lane / 16;
-  const int col0 = __builtin_amdgcn_readfirstlane(((int)blockIdx.x * kTeams + team) * 16 * kN), row0 = (int)blockIdx.y * 16 * kM;
+  __shared__ float kept[kSplit > 1 ? kTeams * kSplit * kN * 256 : 1];
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64), team = wave / kSplit, share = wave % kSplit;
+  const int col0 = ((int)blockIdx.x * kTeams + team) * 16 * kN, row0 = (int)blockIdx.y * 16;
   const bool idle = col0 >= A.n;                            // (a team behind the last tile; it reaches the barriers)
-  Lane L;
-  // (rows behind the last, of x and of the weights: copies of it, not stored)
-#pragma unroll
-  for (int t = 0; t < kM; ++t) L.x[t] = A.x + (i64)min(row0 + t * 16 + c % kR, A.rows - 1) * A.x_row * kRowSize;
-  const int from = min(col0, A.n - 1);
-  L.w = A.weights + (i64)from * (A.k / 2);
-  L.s = (const u8*)(A.scales + (i64)from * A.groups);
-  L.z = DISC_ZEROS ? A.zeros + (i64)from * A.groups : nullptr;
-#pragma unroll
-  for (int t = 0; t < kN; ++t) {
-    const int n = min(t * 16 + c, A.n - 1 - from);
-    L.w_row[t] = (u32)n * (u32)(A.k / 2);
-    L.s_row[t] = (u32)n * (u32)A.groups;
-  }
-  L.c = c;
-  L.q = q;
-  L.k = A.k;
-  L.groups = A.groups;
-  const int mine = __builtin_amdgcn_readfirstlane(share), runs = A.k / (kBlockK * kRun);
-  const int count = idle || runs <= mine ? 0 : (runs - mine + kSplit - 1) / kSplit;
-  // Where a result is no finite number, the sums on the way to it may have passed 32 bits: it is formed again of scales times
-  // 2^-32 and of bf16 rows times 2^-32.  (By the whole block; what was finite stays.)
+  const Lane L = lane_of<kN>(A, col0);
+  const u8* x = A.x + (i64)min(row0 + L.c % kR, A.rows - 1) * A.x_row * kRowSize;   // (rows behind the last: a copy, not stored)
+  const int runs = A.k / (kBlockK * kRun), count = idle || runs <= share ? 0 : (runs - share + kSplit - 1) / kSplit;
   for (int again = 0;; ++again) {
+    f32x4 total[1][kN];
+#pragma unroll
+    for (int n = 0; n < kN; ++n) total[0][n] = f32x4{0, 0, 0, 0};
+    // (behind the wavefront's last run, that again: nothing depends on how many there are, so that loads are waited for one by one)
+    if (count > 0) {
+      Run<kN, kR, kRun> B;
+      take_run<true>(L, x, share * kRun, B);
+#pragma unroll 1
+      for (int i = 1; i <= count; ++i) {
+        add_run(B, again != 0, total);
+        take_run<true>(L, x, (share + min(i, count - 1) * kSplit) * kRun, B);
+      }
+    }
+    if (!idle)                                              // the blocks behind the last whole run
+#pragma unroll 1
+      for (int b = runs * kRun + share; b * kBlockK < A.k; b += kSplit) {
+        Run<kN, kR, 1> last;
+        take_run<false>(L, x, b, last);
+        add_run(last, again != 0, total);
+      }
+    if (finish<1, kN, kSplit, kTeams>(A, total, kept, team, share, row0, col0, again != 0)) break;
+  }
+}
+// tiles of weights, rows of x, wavefronts of a team, teams
+#define DISC_LINEAR_KERNEL(N, R, S, W) \
+  extern "C" __global__ void __launch_bounds__(S * W * 64) disc_linear_##N##_##R##_##S##_##W##_k(LinearArgs A) { linear_body<N, R, S, W>(A); }
+DISC_LINEAR_KERNEL(1, 1, 1, 8)
+DISC_LINEAR_KERNEL(1, 1, 16, 1)
+DISC_LINEAR_KERNEL(1, 1, 8, 1)
+DISC_LINEAR_KERNEL(2, 1, 8, 1)
+DISC_LINEAR_KERNEL(1, 4, 1, 8)
+DISC_LINEAR_KERNEL(1, 4, 8, 1)
+DISC_LINEAR_KERNEL(2, 4, 8, 1)
+DISC_LINEAR_KERNEL(1, 16, 8, 1)
+DISC_LINEAR_KERNEL(4, 16, 4, 1)
+
+// ---- more rows --------------------------------------------------------------------------------------
+// kM tiles of 16 rows of x through LDS, in chunks of kSplit * kBlocksEach blocks: one in use, the next one in LDS, the one behind it on
+// its way in registers.  An operand of a product is 16 bytes a lane; its 16 rows are turned by a number that differs between the
+// operands of a row, so that neither the writes (a row's operands) nor the reads (16 rows of one) meet in a bank.
+// (us without / with LDS: 64 x 4096 x 28672 bf16 87 / 34, 61 x 8192 x 8192 44 / 36, 32 x 4096 x 28672 50 / 25, 16 x 4096 x 28672 23 / 20,
+// 64 x 4096 x 28672 of e4m3 119 / 38.)  Bound by the steps of a chunk, whose parts wait for each other: x to LDS, a barrier, products.
+template <int kM, int kN, int kSplit, int kTeams, int kBlocksEach>
+DISC_DEV void linear_wide_body(const LinearArgs& A) {
+  constexpr int kThreads = kSplit * kTeams * 64, kBlocks = kSplit * kBlocksEach, kRowUnits = 4 * kXs, kUnits = kBlocks * 16 * kM * kRowUnits;
+  constexpr int kHold = kUnits / kThreads, kKept = kTeams * kSplit * kM * kN * 64;
+  static_assert(kHold * kThreads == kUnits, "");
+  __shared__ u32x4 xs[2 * kUnits > kKept ? 2 * kUnits : kKept];
+  const int lane = (int)threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64), team = wave / kSplit, share = wave % kSplit;
+  const int c = lane % 16, q = lane / 16;
+  const int col0 = ((int)blockIdx.x * kTeams + team) * 16 * kN, row0 = (int)blockIdx.y * 16 * kM;
+  const Lane L = lane_of<kN>(A, col0);                      // (a team behind the last tile goes along, and writes nothing)
+  // the units that this thread brings: number p of a row's in a block, which are operand i of the lanes q
+  u32x4 held[kHold];
+  const auto unit = [&](int h, int& row, int& block, int& k, int& to) {
+    const int u = (int)threadIdx.x + h * kThreads, p = u % kRowUnits;
+    row = u / kRowUnits % (16 * kM);
+    block = u / (kRowUnits * 16 * kM);
+    int i, r;
+    if (kKind == 2) {
+      i = kG == 128 ? p & 1 : p >> 2;
+      r = kG == 128 ? p >> 1 : kG == 64 ? (p >> 1 & 1) | (p & 1) << 1 : p & 3;
+    } else {
+      i = kG == 128 ? p & 3 : kG == 64 ? p >> 3 << 1 | (p & 1) : p >> 2;
+      r = kG == 128 ? p >> 2 : kG == 64 ? (p >> 2 & 1) | (p >> 1 & 1) << 1 : p & 3;
+    }
+    k = block * kBlockK + place(kKind == 2 ? 2 * i : i, r);
+    to = ((block * kM + row / 16) * kXs + i) * 64 + r * 16 + ((row % 16) ^ (i * 4 + r));
+  };
+  const u8* from[kHold];
+#pragma unroll
+  for (int h = 0; h < kHold; ++h) {
+    int row, block, k, to;
+    unit(h, row, block, k, to);
+    from[h] = A.x + ((i64)min(row0 + row, A.rows - 1) * A.x_row + k) * kRowSize;   // (rows behind the last: a copy, not stored)
+  }
+  // Yes: all of the chunk is there
+  const auto bring = [&](int chunk, auto whole_chunk) {
+#pragma unroll
+    for (int h = 0; h < kHold; ++h) {
+      int row, block, k, to;
+      unit(h, row, block, k, to);
+      k += chunk * kBlocks * kBlockK;
+      const u8* p = from[h] + (i64)chunk * (kBlocks * kBlockK * kRowSize);
+      const bool here = decltype(whole_chunk)::value || k < A.k, too = decltype(whole_chunk)::value || k + 32 < A.k;
+      held[h] = load_x(p, here, too);
+    }
+  };
+  const auto keep = [&](int chunk, bool down) {
+    if (kKind == 0 && down) {
+#pragma unroll
+      for (int h = 0; h < kHold; ++h) held[h] = lowered(held[h]);
+    }
+#pragma unroll
+    for (int h = 0; h < kHold; ++h) {
+      int row, block, k, to;
+      unit(h, row, block, k, to);
+      xs[(chunk & 1) * kUnits + to] = operand(held[h], false);
+    }
+  };
+  const int full = A.k / (kBlocks * kBlockK), blocks = (A.k + kBlockK - 1) / kBlockK;
+  const auto operands = [&](int chunk, int r) {
+    const u32x4* at = xs + (chunk & 1) * kUnits + (share * kBlocksEach + r) * kM * kXs * 64 + q * 16;
+    return [=](int t, int i) { return at[(t * kXs + i) * 64 + (c ^ (i * 4 + q))]; };
+  };
+  for (int again = 0;; ++again) {
+    const float lower = again ? 0x1p-32f : 1.f;
     f32x4 total[kM][kN];
 #pragma unroll
     for (int t = 0; t < kM; ++t)
 #pragma unroll
       for (int n = 0; n < kN; ++n) total[t][n] = f32x4{0, 0, 0, 0};
-    // (behind the wavefront's last run, that again: nothing depends on how many there are, so that loads are waited for one by one)
-    if (count > 0) {
-      Block<kM, kN, kR, kRun> B;
-      take_block<true>(L, mine * kRun, B);
-#pragma unroll 1
-      for (int i = 1; i <= count; ++i) {
-        add_run(B, again != 0, total);
-        take_block<true>(L, (mine + min(i, count - 1) * kSplit) * kRun, B);
-      }
-    }
-    // the blocks behind the last whole run
-    if (!idle)
-#pragma unroll 1
-      for (int b = runs * kRun + mine; b * kBlockK < A.k; b += kSplit) {
-        Block<kM, kN, kR, 1> last;
-        take_block<false>(L, b, last);
-        add_run(last, again != 0, total);
-      }
-    bool lost = false;
-    const auto finish = [&](int m, int col, float y) {
-      if (m >= A.rows || col >= A.n) return;
-      if (DISC_ROWS) y *= A.row_scales[m];
-      if (again) y *= 0x1p32f * (kKind == 0 ? 0x1p32f : 1.f);
-      if (!again) lost |= !(__builtin_fabsf(y) < __builtin_inff());
-      if (A.bias) y += (float)A.bias[col];
-      T* to = A.out + (m * A.out_row + col);
-      if (!again || !(__builtin_fabsf((float)*to) < __builtin_inff())) *to = (T)y;
-    };
-    if (kSplit == 1) {
-#pragma unroll
-      for (int t = 0; t < kM; ++t)
-#pragma unroll
-        for (int n = 0; n < kN; ++n)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) finish(row0 + t * 16 + q * 4 + i, col0 + n * 16 + c, total[t][n][i]);
-      if (again || !__any(lost)) break;
-    } else {
-#pragma unroll
-      for (int t = 0; t < kM; ++t)
-#pragma unroll
-        for (int n = 0; n < kN; ++n)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) kept[wave][(t * kN + n) * 256 + (q * 4 + i) * 16 + c] = total[t][n][i];
+    if (full > 0) {
+      // (nothing depends on which chunk it is, so that loads are waited for one by one; behind the last one, that again)
+      Weights<kN, kBlocksEach> B;
+      // (... and in the same order before the loop as in it)
+      bring(0, Yes());
+      keep(0, again != 0);
+      bring(min(1, full - 1), Yes());
+      take_weights<true, kN, kBlocksEach>(L, share * kBlocksEach, B);
       __syncthreads();
-      for (int o = share * 64 + lane; o < kM * kN * 256; o += kSplit * 64) {
-        float y = 0;
+#pragma unroll 1
+      for (int chunk = 0; chunk < full; ++chunk) {
+        keep(chunk + 1, again != 0);
+        bring(min(chunk + 2, full - 1), Yes());
 #pragma unroll
-        for (int v = 0; v < kSplit; ++v) y += kept[team * kSplit + v][o];
-        finish(row0 + o / (kN * 256) * 16 + o % 256 / 16, col0 + o / 256 % kN * 16 + o % 16, y);
+        for (int r = 0; r < kBlocksEach; ++r) add_products<kM, kN>(B.w[r], B.scale, B.zero, r * kGroups, operands(chunk, r), lower, total);
+        take_weights<true, kN, kBlocksEach>(L, (min(chunk + 1, full - 1) * kSplit + share) * kBlocksEach, B);
+        __syncthreads();
       }
-      if (again || !__syncthreads_or(lost)) break;
     }
+    if (full * kBlocks < blocks) {                          // what is left, up to a chunk
+      bring(full, No());
+      keep(full, again != 0);
+      __syncthreads();
+#pragma unroll 1
+      for (int r = 0; r < kBlocksEach; ++r) {
+        const int b = full * kBlocks + share * kBlocksEach + r;
+        if (b < blocks) {
+          Weights<kN, 1> last;
+          take_weights<false, kN, 1>(L, b, last);
+          add_products<kM, kN>(last.w[0], last.scale, last.zero, 0, operands(full, r), lower, total);
+        }
+      }
+      __syncthreads();
+    }
+    if (finish<kM, kN, kSplit, kTeams>(A, total, (float*)xs, team, share, row0, col0, again != 0)) break;
   }
 }
-// tiles of x and of weights, rows of a tile of x, wavefronts of a team, teams, blocks of a run
-#define DISC_LINEAR_KERNEL(M, N, R, S, W, B) \
-  extern "C" __global__ void __launch_bounds__(S * W * 64) disc_linear_##M##_##N##_##R##_##S##_##W##_##B##_k(LinearArgs A) { linear_body<M, N, R, S, W, B>(A); }
-DISC_LINEAR_KERNEL(1, 1, 1, 1, 8, 2)
-DISC_LINEAR_KERNEL(1, 1, 1, 16, 1, 2)
-DISC_LINEAR_KERNEL(1, 1, 1, 8, 1, 2)
-DISC_LINEAR_KERNEL(1, 2, 1, 8, 1, 2)
-DISC_LINEAR_KERNEL(1, 1, 4, 1, 8, 2)
-DISC_LINEAR_KERNEL(1, 1, 4, 8, 1, 2)
-DISC_LINEAR_KERNEL(1, 2, 4, 8, 1, 2)
-DISC_LINEAR_KERNEL(1, 1, 16, 8, 1, 2)
-DISC_LINEAR_KERNEL(1, 4, 16, 4, 1, 2)
-DISC_LINEAR_KERNEL(2, 2, 16, 8, 1, 2)
-DISC_LINEAR_KERNEL(4, 2, 16, 4, 1, 2)
+// tiles of x, of weights, wavefronts of a team, teams, blocks of a wavefront and chunk
+#define DISC_LINEAR_WIDE_KERNEL(M, N, S, W, B) \
+  extern "C" __global__ void __launch_bounds__(S * W * 64) disc_linear_wide_##M##_##N##_##S##_##W##_##B##_k(LinearArgs A) { linear_wide_body<M, N, S, W, B>(A); }
+DISC_LINEAR_WIDE_KERNEL(1, 2, 2, 4, 2)
+DISC_LINEAR_WIDE_KERNEL(2, 1, 4, 2, 1)
+DISC_LINEAR_WIDE_KERNEL(2, 2, 2, 4, 1)
+DISC_LINEAR_WIDE_KERNEL(4, 1, 4, 2, 1)
+DISC_LINEAR_WIDE_KERNEL(4, 1, 2, 8, 1)
 #endif  // DISC_LINEAR4
 
 #ifdef DISC_VERIFY
