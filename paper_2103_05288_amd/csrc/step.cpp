@@ -61,13 +61,13 @@ constexpr int kLinearCount = sizeof kLinear / sizeof kLinear[0];
 //   1 x 512 x 32768 4.4, 16.1, 7.4, 6.2; 1 x 1024 x 32768 6.3, 17.1, 8.0, 7.2; 1 x 4096 x 4096 9.3, 4.8, 4.9, 5.8;
 //   1 x 16384 x 1024 49, 8.8, 9.4, 14; 1 x 4096 x 12288 18, 12.9, 9.4, 10.5; 1 x 8192 x 131072 140, 168, 126, 112.
 // Of 5 .. 16, the two without LDS and the one with it: 16 x 4096 x 4096 8.3, 13.4, 17; 16 x 4096 x 12288 17.5, 13.0, 16.0; 16 x 4096 x 28672
-// 38.7, 23.4, 19.9; 10 x 2048 x 20000 13.9, 12.2, 10.3; 16 x 512 x 32768 10.3, 6.0, 6.0; 5 x 8192 x 131072 195, 147, 147.
+// 38.7, 23.4, 19.9; 10 x 2048 x 20000 13.9, 12.2, 10.3; 16 x 512 x 32768 10.3, 6.0, 6.0; 5 x 8192 x 131072 195, 132, 140.
 // Of more, blocks of 32 columns and of 128: 32 x 4096 x 8192 11.1, 21.6; 32 x 4096 x 28672 42, 25; 61 x 8192 x 8192 36, 71; 64 x 4096 x 28672 66, 34.
 int linear_kernel(int64_t rows, int64_t n, int64_t k, int64_t cus) {
   const int64_t tiles = ceil_div(n, 16);
   if (rows > 32) return tiles <= 4 * cus ? 12 : 13;
   if (rows > 16) return tiles <= 4 * cus ? 10 : 11;
-  if (rows > 4) return tiles > 4 * cus ? 9 : tiles <= 2 * cus && k > 512 ? 7 : 8;
+  if (rows > 4) return rows > 8 && tiles > 4 * cus ? 9 : tiles <= 2 * cus && k > 512 ? 7 : 8;
   if (rows > 1) return k <= 1024 ? 4 : tiles <= 4 * cus ? 5 : 6;
   return k <= 1024 ? 0 : tiles <= cus ? 1 : tiles <= 4 * cus ? 2 : 3;
 }
@@ -123,7 +123,7 @@ RowShape norm_shape(const Operator& o, int64_t width, bool few, bool nt) {
   if (few && accesses <= 1024) return {(int)ceil_div(accesses, 64) * 64, (int)ceil_div(accesses, 64) * 64, FN_NORM_B1};
   if (accesses <= 256) return {(int)power_of_two(ceil_div(accesses, 4)), 256, nt ? FN_NORM_S4_NT : FN_NORM_S4};
   const int block = (int)ceil_div(accesses, 256) * 64;
-  return {block, block, accesses > 1024 ? FN_NORM_B4 : nt ? FN_NORM_4_NT : FN_NORM_4};
+  return {block, block, accesses > 2048 ? FN_NORM_B4 : nt ? FN_NORM_4_NT : FN_NORM_4};
 }
 // Blocks of a gradient: enough that a CU has rows under way while others are being summed, and few enough that the parts, a row of
 // 32 bits each, stay small beside the rows (us with 1, 2, 3, 4, 6 a CU: 65536 x 512 bf16 134, 80, 66, 62, 63; 16384 x 1024 41, 32,

@@ -49,18 +49,30 @@ constexpr int kMostWaves = 16;
 typedef T vec_t __attribute__((ext_vector_type(kV)));
 typedef vec_t vec_u __attribute__((aligned(alignof(T))));
 
-// `n` elements of a row from p on (the rest zeros): one access, or the ragged end of a row by single elements
+// `n` elements of a row of `width` from p on (n is 1 at least): one access, which at the ragged end of a row is its last kV elements
+// (rows shorter than that: single ones).  settle() puts them in place, with zeros behind them, once every load is on its way (with the
+// end's elements loaded one by one, a block's loads waited for each other: 9179 x 6879 fp16 151 us, 6880 80).
 template <bool kNt>
-DISC_DEV vec_t take(const T* p, i64 n) {
-  if (n >= kV) return (vec_t)fetch<kNt>((const vec_u*)p);
+DISC_DEV vec_t take(const T* p, int n, int width) {
+  if (width >= kV) return (vec_t)fetch<kNt>((const vec_u*)(p - max(kV - n, 0)));
   vec_t v = {};
 #pragma unroll
   for (int e = 0; e < kV - 1; ++e)
     if (e < n) v[e] = p[e];
   return v;
 }
+DISC_DEV void settle(vec_t& v, int n, int width) {
+  if (n >= kV || n <= 0 || width < kV) return;
+  typedef u64 halves __attribute__((ext_vector_type(2)));
+  halves h = __builtin_bit_cast(halves, v);
+  const int by = (kV - n) * (128 / kV);                     // bits: 16 .. 112
+  const u64 lo = h[0], hi = h[1];
+  h[0] = by >= 64 ? hi >> (by - 64) : lo >> by | hi << (64 - by);
+  h[1] = by >= 64 ? 0 : hi >> by;
+  v = __builtin_bit_cast(vec_t, h);
+}
 template <bool kNt>
-DISC_DEV void give(T* p, vec_t v, i64 n) {
+DISC_DEV void give(T* p, vec_t v, int n) {
   if (n >= kV) {
     put<kNt>((vec_u*)p, (vec_u)v);
     return;
@@ -125,7 +137,8 @@ DISC_DEV u32 code4(float a, float b, float c, float d) {
 #endif
 }
 
-template <bool kNt, bool kBlock, int kN>
+// kLean: the weight is read again where it is used (its registers are needed for the widest rows).
+template <bool kNt, bool kBlock, int kN, bool kLean>
 DISC_DEV void norm_body(const NormArgs& A) {
   __shared__ double sums[kMostWaves], most64[kMostWaves];
   __shared__ u32 most[kMostWaves];
@@ -138,14 +151,27 @@ DISC_DEV void norm_body(const NormArgs& A) {
     const int c = (i * lanes + lane) * kV, n = A.width - c;
     x[i] = r[i] = v[i] = vec_t{};
     if (n <= 0) continue;
-    x[i] = take<kNt>(A.x + row * A.x_row + c, n);
-    if (A.residual) r[i] = take<kNt>(A.residual + row * A.residual_row + c, n);
-    v[i] = take<false>(A.weight + c, n);
+    x[i] = take<kNt>(A.x + row * A.x_row + c, n, A.width);
+    if (A.residual) r[i] = take<kNt>(A.residual + row * A.residual_row + c, n, A.width);
+    v[i] = take<false>(A.weight + c, n, A.width);
+  }
+#pragma unroll
+  for (int i = 0; i < kN; ++i) {
+    const int n = A.width - (i * lanes + lane) * kV;
+    settle(x[i], n, A.width);
+    settle(r[i], n, A.width);
+    settle(v[i], n, A.width);
   }
   float s[kN][kV];
   double squares = 0;
   u32 a = 0;
   const auto weight = [&](int i, int e) { return (float)v[i][e] + A.offset; };   // (behind a row's end s is 0)
+  const auto weights_again = [&](int i) {
+    const int c = (i * lanes + lane) * kV;
+    if (!kLean || c >= A.width) return;
+    v[i] = take<false>(A.weight + c, A.width - c, A.width);
+    settle(v[i], A.width - c, A.width);
+  };
 #pragma unroll
   for (int i = 0; i < kN; ++i)
 #pragma unroll
@@ -183,13 +209,15 @@ DISC_DEV void norm_body(const NormArgs& A) {
   if (wide) {
     double m = 0;
 #pragma unroll
-    for (int i = 0; i < kN; ++i)
+    for (int i = 0; i < kN; ++i) {
+      weights_again(i);
 #pragma unroll
       for (int e = 0; e < kV; ++e) {
         const double y = __builtin_fabs((double)s[i][e] * (double)weight(i, e));
         m = !(y <= m) ? y : m;                              // (a NaN replaces whatever was there, and becomes an infinity)
         if (!(m < __builtin_inf())) m = __builtin_inf();
       }
+    }
     m = over_lanes<kBlock>(m, lanes, Most());
     if (kBlock) {
       if (threadIdx.x % 64 == 0) most64[threadIdx.x / 64] = m;
@@ -212,6 +240,7 @@ DISC_DEV void norm_body(const NormArgs& A) {
     const int c = (i * lanes + lane) * kV;
     const int n = A.width - c;
     if (n <= 0) break;
+    weights_again(i);
     float y[kV];
 #pragma unroll
     for (int e = 0; e < kV; ++e) y[e] = s[i][e] * weight(i, e) * inverse;
@@ -269,10 +298,18 @@ DISC_DEV void norm_backward_body(const NormBackwardArgs& A) {
       h[i] = d[i] = v[i] = vec_t{};
       if (!kLean) t[i] = vec_t{};
       if (n <= 0) continue;
-      h[i] = take<kNt>(A.total + row * A.total_row + c, n);
-      d[i] = take<kNt>(A.dy + row * A.dy_row + c, n);
-      v[i] = take<false>(A.weight + c, n);
-      if (!kLean && A.dtotal) t[i] = take<kNt>(A.dtotal + row * A.dtotal_row + c, n);
+      h[i] = take<kNt>(A.total + row * A.total_row + c, n, A.width);
+      d[i] = take<kNt>(A.dy + row * A.dy_row + c, n, A.width);
+      v[i] = take<false>(A.weight + c, n, A.width);
+      if (!kLean && A.dtotal) t[i] = take<kNt>(A.dtotal + row * A.dtotal_row + c, n, A.width);
+    }
+#pragma unroll
+    for (int i = 0; i < kN; ++i) {
+      const int n = A.width - (i * lanes + lane) * kV;
+      settle(h[i], n, A.width);
+      settle(d[i], n, A.width);
+      settle(v[i], n, A.width);
+      if (!kLean) settle(t[i], n, A.width);
     }
 #pragma unroll
     for (int i = 0; i < kN; ++i)
@@ -301,8 +338,10 @@ DISC_DEV void norm_backward_body(const NormBackwardArgs& A) {
       if (c >= A.width) break;
       vec_t y, last = {};
       if (kLean) {
-        v[i] = take<false>(A.weight + c, A.width - c);
-        if (A.dtotal) last = take<kNt>(A.dtotal + row * A.dtotal_row + c, A.width - c);
+        v[i] = take<false>(A.weight + c, A.width - c, A.width);
+        if (A.dtotal) last = take<kNt>(A.dtotal + row * A.dtotal_row + c, A.width - c, A.width);
+        settle(v[i], A.width - c, A.width);
+        settle(last, A.width - c, A.width);
       } else {
         last = t[i];
       }
@@ -341,14 +380,14 @@ DISC_DEV void norm_backward_body(const NormBackwardArgs& A) {
 
 // accesses of a thread: a part of a wavefront has a row (_s), 256 threads, or the whole block of up to 1024 (_b)
 #define DISC_NORM_KERNEL(NAME, THREADS, NT, BLOCK, N) \
-  extern "C" __global__ void __launch_bounds__(THREADS) disc_norm##NAME(NormArgs A) { norm_body<NT, BLOCK, N>(A); }
+  extern "C" __global__ void __launch_bounds__(THREADS) disc_norm##NAME(NormArgs A) { norm_body<NT, BLOCK, N, (THREADS > 512 && N > 1)>(A); }
 #define DISC_NORM_BACKWARD_KERNEL(NAME, THREADS, NT, BLOCK, N) \
   extern "C" __global__ void __launch_bounds__(THREADS) disc_norm_backward##NAME(NormBackwardArgs A) { norm_backward_body<NT, BLOCK, N, (THREADS > 256)>(A); }
 DISC_NORM_KERNEL(1_s, 256, false, false, 1)
 DISC_NORM_KERNEL(4_s, 256, false, false, 4)
 DISC_NORM_KERNEL(4_s_nt, 256, true, false, 4)
-DISC_NORM_KERNEL(4, 256, false, true, 4)
-DISC_NORM_KERNEL(4_nt, 256, true, true, 4)
+DISC_NORM_KERNEL(4, 512, false, true, 4)
+DISC_NORM_KERNEL(4_nt, 512, true, true, 4)
 DISC_NORM_KERNEL(1_b, 1024, false, true, 1)
 DISC_NORM_KERNEL(4_b, 1024, false, true, 4)
 DISC_NORM_BACKWARD_KERNEL(1_s, 256, false, false, 1)
