@@ -447,3 +447,282 @@ def test_verify_follows_the_target(ctx):
     share = torch.bincount(tokens[:, 0].long(), minlength=V).double() / B
     assert ((share - p.double()).abs() < 5 * (p.double() * (1 - p.double()) / B).sqrt()).all()
     assert (accepted.double().mean() - torch.minimum(p, q).double().sum()).abs() < 5 * 0.5 / math.sqrt(B)
+
+
+def test_verify_of_more_chunks_than_lanes(ctx):
+    """Vocabularies of more than 64 chunks of 4096: a lane has several, and the goal falls into one of them."""
+    for V, drafts in ((300001, 2), (1200000, 1)):
+        target, drafted, uniforms, draft = _verify_inputs("f32", 3, drafts, V, V)
+        uniforms[1, -1] = 1 - 2.0 ** -24
+        _verify(ctx, "f32", target, drafted, uniforms, draft)
+        target[2] = 0
+        target[2, :, V - 1] = 0.5
+        _verify(ctx, "f32", target, drafted, uniforms)
+
+
+# ---- products at the ends of their types -----------------------------------------------------------
+
+
+@pytest.mark.parametrize("M,N", [(1, 40), (3, 40), (12, 40), (24, 40), (50, 40), (12, 16500), (60, 16500)])
+def test_linear_of_the_largest_rows_and_scales(ctx, M, N):
+    """Sums that pass 32 bits on the way to a result that does not, beside ordinary rows."""
+    K, group = 512, 128
+    h = ctx.register_linear4("bf16", group=group)
+    x, weights, scales, _ = _linear_inputs("bf16", "same", group, False, False, M, N, K, 61)
+    big = torch.finfo(torch.bfloat16).max
+    x[M - 1] = (torch.sign(x[M - 1].float()) * big).to(torch.bfloat16)
+    scales *= 2.0 ** -10
+    scales[5] = (scales[5].float() * 2.0 ** 120).to(torch.bfloat16)      # (a column of scales that make large rows infinite)
+    out = torch.empty((M, N), dtype=torch.bfloat16, device="cuda")
+    h.launch(x, weights, scales, out)
+    want, size = plain.linear4(x, weights, scales, group)
+    finite = want.abs() < 0.99 * big
+    assert bool(finite[M - 1].float().mean() > 0.9) and torch.equal(torch.isfinite(out[:, :5]), finite[:, :5])
+    # (as _linear_check; the second time around every term is the same number times a power of two)
+    steps = 2 * (group + 8) + K // group + 24
+    bound = _half_step(torch.bfloat16) * want.abs() + steps * UNIT * size + _least(torch.bfloat16)
+    _inside(out[finite], want[finite], bound[finite], "largest rows")
+    # i8 rows whose scales take the weights' back
+    h = ctx.register_linear4("bf16", group=group, rows="i8")
+    x, weights, scales, more = _linear_inputs("bf16", "i8", group, False, False, M, N, K, 62)
+    scales = (scales.float() * 2.0 ** 122).to(torch.bfloat16)
+    more["row_scales"] = torch.full((M,), 2.0 ** -60, device="cuda")
+    more["row_scales"][0] = 2.0 ** -100
+    h.launch(x, weights, scales, out, **more)
+    want, size = plain.linear4(x, weights, scales, group, row_scales=more["row_scales"])
+    assert torch.isfinite(out).all()
+    _inside(out, want, _half_step(torch.bfloat16) * want.abs() + steps * UNIT * size + _least(torch.bfloat16), "largest scales")
+
+
+@pytest.mark.parametrize("rows", ["same", "i8", "e4m3"])
+@pytest.mark.parametrize("M,N", [(2, 70), (9, 70), (20, 70), (40, 70)])
+def test_linear_rows_do_not_see_each_other(ctx, rows, M, N):
+    dtype, group, zeros = {"same": ("bf16", 64, True), "i8": ("f16", 64, True), "e4m3": ("bf16", 128, True)}[rows]
+    K = 9 * group
+    h = ctx.register_linear4(dtype, group=group, rows=None if rows == "same" else rows, zeros=zeros)
+    x, weights, scales, more = _linear_inputs(dtype, rows, group, zeros, True, M, N, K, 63)
+    want = torch.empty((M, N), dtype=TYPES[dtype], device="cuda")
+    h.launch(x, weights, scales, want, **more)
+    other = x.clone()
+    if rows == "same":
+        other[M - 1, 3] = math.inf
+        other[M - 1, 70] = -math.inf
+        other[M // 2, 9] = math.nan
+    elif rows == "e4m3":
+        other[M - 1, 3] = math.nan
+    else:
+        other[M - 1] = 127
+    if rows != "same":
+        more["row_scales"] = more["row_scales"].clone()
+        more["row_scales"][M // 2] = math.nan
+    got = torch.empty_like(want)
+    h.launch(other, weights, scales, got, **more)
+    kept = [m for m in range(M) if m not in (M - 1, M // 2)]
+    assert torch.equal(got[kept], want[kept]) and not torch.isfinite(got[M // 2]).any()
+    assert rows == "i8" or not torch.isfinite(got[M - 1]).any()
+
+
+def test_past_32_bits(ctx):
+    """Weights, rows and probabilities that lie further apart than 32 bits count bytes or elements."""
+    g = _generator(64)
+    # weights of more than 2^32 bytes
+    N, K, group = 330003, 32768, 128
+    h = ctx.register_linear4("bf16", group=group)
+    weights = torch.randint(0, 256, (N, K // 2), generator=g, device="cuda", dtype=torch.uint8)
+    scales = torch.empty((N, K // group), dtype=torch.bfloat16, device="cuda").uniform_(0.001, 0.002, generator=g)
+    for M in (1, 12, 40):
+        x = _channels((M, K), torch.bfloat16, g)
+        out = torch.empty((M, N), dtype=torch.bfloat16, device="cuda")
+        h.launch(x, weights, scales, out)
+        for part in (slice(0, 40), slice(N // 2, N // 2 + 40), slice(N - 40, N)):
+            _linear_check(out[:, part], x, weights[part], scales[part], group, {}, f"{M} rows, columns {part}")
+    del weights, scales, out
+    # rows 2^31 elements apart
+    whole = torch.zeros(2 ** 32 + 2 ** 31 + 2 ** 14, dtype=torch.bfloat16, device="cuda")
+    x = whole.as_strided((3, 1000), (2 ** 31, 1))
+    x.copy_(_channels((3, 1000), torch.bfloat16, g))
+    codes, scales, _ = _norm(ctx, "bf16", "i8", 3, 1000, 0.0, None, 65, strided=False, x=x)
+    h = ctx.register_norm("bf16", "i8", eps=EPS)
+    dw, dx = torch.empty(1000, device="cuda"), torch.empty((3, 1000), dtype=torch.bfloat16, device="cuda")
+    dense, weight = x.contiguous(), _normal((1000,), torch.bfloat16, g)
+    ws = torch.empty(h.workspace_bytes(3, 1000), dtype=torch.uint8, device="cuda")
+    h.backward(dense, weight, dense, dx, dw, workspace=ws)
+    into = whole.as_strided((3, 1000), (2 ** 31, 1), 2000)
+    also = torch.empty_like(dw)
+    h.backward(x, weight, x, into, also, workspace=ws)
+    assert torch.equal(into, dx) and torch.equal(also, dw)
+    # places and sequences as far apart
+    target, drafted, uniforms, _ = _verify_inputs("bf16", 2, 1, 5000, 66)
+    far = whole.as_strided((2, 2, 5000), (2 ** 32, 2 ** 31, 1), 4000)
+    far.copy_(target)
+    _verify(ctx, "bf16", far, drafted, uniforms)
+
+
+# ---- streams, graphs, a step of all of them --------------------------------------------------------
+
+
+def test_calls_on_other_streams(ctx):
+    """Torch's current stream and the launch's own; two streams at once, each with a workspace of its own."""
+    g = _generator(67)
+    t = torch.bfloat16
+    norm, verify, linear = ctx.register_norm("bf16", "i8", eps=EPS), ctx.register_verify("f32"), ctx.register_linear4("bf16", rows="i8")
+    total, dy, weight = _channels((2000, 1024), t, g), _normal((2000, 1024), t, g), _normal((1024,), t, g)
+    target, drafted, uniforms, draft = _verify_inputs("f32", 20, 3, 50000, 68)
+    _, weights, scales, _ = _linear_inputs("bf16", "i8", 128, False, False, 4, 500, 1024, 69)
+
+    def run(stream=None):
+        dx, dw = torch.empty_like(total), torch.empty(1024, device="cuda")
+        codes, row_scales = torch.empty((4, 1024), dtype=torch.int8, device="cuda"), torch.empty(4, device="cuda")
+        out = torch.empty((4, 500), dtype=t, device="cuda")
+        tokens, accepted = torch.empty((20, 4), dtype=torch.int32, device="cuda"), torch.empty(20, dtype=torch.int32, device="cuda")
+        ws = [torch.empty(n, dtype=torch.uint8, device="cuda") for n in (norm.workspace_bytes(2000, 1024), verify.workspace_bytes(20, 50000))]
+        norm.backward(total, weight, dy, dx, dw, workspace=ws[0], stream=stream)
+        verify.launch(target, drafted, uniforms, tokens, accepted, draft=draft, workspace=ws[1], stream=stream)
+        norm.launch(total[:4], weight, codes, row_scales, stream=stream)
+        linear.launch(codes, weights, scales, out, row_scales=row_scales, stream=stream)
+        return [dx, dw, tokens, accepted, codes, row_scales, out], ws
+    want, _ = run()
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    kept = []
+    for turn in range(4):
+        with torch.cuda.stream(streams[turn % 2]):
+            kept.append(run())
+    torch.cuda.synchronize()
+    kept.append(run(stream=streams[0].cuda_stream))
+    torch.cuda.synchronize()
+    for got, _ in kept:
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_a_gradient_captured_while_eager_ones_live(ctx):
+    """Forward and backward in a graph, replayed with other rows between eager calls of the same tensors."""
+    g = _generator(70)
+    rows, width = 700, 1000
+    h = ctx.register_norm("f32", "i8", eps=EPS)
+    sets = [[_normal(s, torch.float32, _generator(71 + i)) for s in ((rows, width), (rows, width), (width,), (rows, width), (rows, width))] for i in range(3)]
+    need = h.workspace_bytes(rows, width)
+
+    def run(x, residual, weight, dy, dtotal, outs, ws):
+        total, codes, scales, dx, dw = outs
+        h.launch(x, weight, codes, scales, residual=residual, total=total)
+        h.backward(total, weight, dy, dx, dw, dtotal=dtotal, workspace=ws)
+
+    def outputs():
+        return [torch.empty((rows, width), device="cuda"), torch.empty((rows, width), dtype=torch.int8, device="cuda"), torch.empty(rows, device="cuda"),
+                torch.empty((rows, width), device="cuda"), torch.empty(width, device="cuda")]
+    static, outs, ws = [t.clone() for t in sets[0]], outputs(), torch.empty(need, dtype=torch.uint8, device="cuda")
+    run(*static, outs, ws)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run(*static, outs, ws)
+    for turn in range(5):
+        s = sets[turn % 3]
+        for a, b in zip(static, s):
+            a.copy_(b)
+        ws.fill_(255)
+        eager, own = outputs(), torch.empty(need, dtype=torch.uint8, device="cuda")
+        run(*s, eager, own)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs, eager))
+        assert torch.equal(eager[0], s[0] + s[1])
+    del g
+
+
+def _softmax_pattern(ctx):
+    from workloads import PatternBuilder
+    pb = PatternBuilder("softmax_f32")
+    T, V = pb.dims(2)
+    x = pb.cast(pb.param("bf16", [T, V]), "f32")
+    e = pb.op("exp", pb.op("sub", x, pb.broadcast(pb.reduce("max", x, 1), [T, V], [0])))
+    pb.output(pb.op("div", e, pb.broadcast(pb.reduce("sum", e, 1), [T, V], [0])))
+    return ctx.register(pb.build())
+
+
+def test_a_step_with_drafted_tokens(ctx):
+    """What a decoder's step is: norm into 8-bit rows, their product with 4-bit weights, rotation, store, attention, the product back, the
+    next norm with the residual, logits, softmax and the check of the drafted tokens; each against 64 bits of what it was given.
+    Captured, and replayed with other rows, tokens and uniforms: the same as eager calls."""
+    from oracle import decoder
+    from paper_2103_05288_amd import rotary_frequencies
+    t = torch.bfloat16
+    B, D, width, heads, kv, dim, size, V = 3, 2, 512, 4, 2, 64, 16, 3001
+    M = B * (D + 1)                                            # (a drafted token is a row of the batch: its sequence's pages, one token longer)
+    norm, rotary, cache = ctx.register_norm("bf16", "i8", eps=EPS), ctx.register_rotary("bf16", dim, rotary_frequencies(dim)[0]), ctx.register_cache("bf16", dim, "i8")
+    from_norm, plainly, verify, softmax = ctx.register_linear4("bf16", rows="i8"), ctx.register_linear4("bf16", group=64, zeros=True), ctx.register_verify("f32"), _softmax_pattern(ctx)
+    g = _generator(81)
+    qkv_rows = (heads + 2 * kv) * dim
+    weights = [_linear_inputs("bf16", "i8", 128, False, False, 1, qkv_rows, width, 82), _linear_inputs("bf16", "same", 64, True, True, 1, width, heads * dim, 83),
+               _linear_inputs("bf16", "i8", 128, False, False, 1, V, width, 84)]
+    gains = [(1 + _normal((width,), torch.float32, g, 0.1)).to(t) for _ in range(2)]
+    lengths = torch.tensor([5, 20, 31], device="cuda")
+    table = torch.arange(3 * 3, device="cuda", dtype=torch.int32).view(3, 3).repeat_interleave(D + 1, 0).contiguous()
+    filled = [torch.randint(-127, 128, (9, kv, size, dim), generator=g, device="cuda", dtype=torch.int8) for _ in range(2)]
+    filled += [torch.full((9, kv, size), 0.01, device="cuda") for _ in range(2)]
+    at = (lengths[:, None] + torch.arange(D + 1, device="cuda")).flatten()
+    slots = table.long()[torch.arange(M, device="cuda"), at // size] * size + at % size
+    seen = (at + 1).int()
+    sizes = [norm.workspace_bytes(1, 1), cache.workspace_bytes(M, heads, kv, 3 * size), verify.workspace_bytes(B, V)]
+
+    def inputs(turn):
+        k = _generator(90 + turn)
+        return {"x": _channels((M, width), t, k), "residual": _channels((M, width), t, k), "drafted": torch.randint(0, V, (B, D), generator=k, device="cuda", dtype=torch.int32),
+                "uniforms": torch.empty((B, D + 1), device="cuda").uniform_(0, 1, generator=k).clamp_(max=1 - 2.0 ** -24) * 0.01}
+
+    def buffers():
+        e = lambda *s, dtype=t: torch.empty(s, dtype=dtype, device="cuda")  # noqa: E731
+        return {"pages": [p.clone() for p in filled], "total": e(M, width), "codes": e(M, width, dtype=torch.int8), "scales": e(M, dtype=torch.float32), "qkv": e(M, qkv_rows),
+                "attended": e(M, heads, dim), "back": e(M, width), "total2": e(M, width), "codes2": e(M, width, dtype=torch.int8), "scales2": e(M, dtype=torch.float32),
+                "logits": e(M, V), "p": e(M, V, dtype=torch.float32), "tokens": e(B, D + 1, dtype=torch.int32), "accepted": e(B, dtype=torch.int32),
+                "ws": [torch.empty(max(16, n), dtype=torch.uint8, device="cuda") for n in sizes]}
+
+    def step(i, o):
+        norm.launch(i["x"], gains[0], o["codes"], o["scales"], residual=i["residual"], total=o["total"])
+        from_norm.launch(o["codes"], weights[0][1], weights[0][2], o["qkv"], row_scales=o["scales"])
+        rows = o["qkv"].view(M, heads + 2 * kv, dim)
+        q, k, v = rows[:, :heads], rows[:, heads:heads + kv], rows[:, heads + kv:]
+        rotary.launch(at, [q, k], [q, k])
+        cache.store([k, v], slots, o["pages"])
+        cache.attend(q, seen, table, o["pages"], o["attended"], workspace=o["ws"][1])
+        plainly.launch(o["attended"].view(M, heads * dim), weights[1][1], weights[1][2], o["back"], **weights[1][3])
+        norm.launch(o["back"], gains[1], o["codes2"], o["scales2"], residual=o["total"], total=o["total2"])
+        from_norm.launch(o["codes2"], weights[2][1], weights[2][2], o["logits"], row_scales=o["scales2"])
+        softmax.launch([M, V], [o["logits"]], [o["p"]])
+        verify.launch(o["p"].view(B, D + 1, V), i["drafted"], i["uniforms"], o["tokens"], o["accepted"], workspace=o["ws"][2])
+
+    static, outs = inputs(0), buffers()
+    step(static, outs)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(static, outs)
+    for turn in range(4):
+        i, o = inputs(turn), buffers()
+        step(i, o)
+        for k, x in i.items():
+            static[k].copy_(x)
+        for a, b in zip(outs["pages"], filled):
+            a.copy_(b)
+        graph.replay()
+        torch.cuda.synchronize()
+        for k in o:
+            for a, b in zip(*([o[k], outs[k]] if isinstance(o[k], list) else [[o[k]], [outs[k]]])):
+                assert k == "ws" or torch.equal(a, b), (turn, k)
+        for x, gain, codes, scales, residual, total in ((i["x"], gains[0], o["codes"], o["scales"], i["residual"], o["total"]), (o["back"], gains[1], o["codes2"], o["scales2"], o["total"], o["total2"])):
+            _, y, largest = plain.norm(x, gain, EPS, 0.0, residual)
+            _check_codes(codes, scales, y, largest, "i8", "step")
+            assert torch.equal(total, (x.float() + residual.float()).to(t))
+        fresh = torch.empty_like(o["qkv"])
+        from_norm.launch(o["codes"], weights[0][1], weights[0][2], fresh, row_scales=o["scales"])      # (the first was turned in place)
+        _linear_check(fresh, o["codes"], weights[0][1], weights[0][2], 128, {"row_scales": o["scales"]}, "qkv")
+        want = decoder.attend(o["qkv"].view(M, heads + 2 * kv, dim)[:, :heads], seen, table, o["pages"], 0.125)[0]
+        assert (o["attended"].double() - want).abs().max() < 2.0 ** -7 * want.abs().max()
+        _linear_check(o["back"], o["attended"].view(M, heads * dim), weights[1][1], weights[1][2], 64, weights[1][3], "back")
+        _linear_check(o["logits"], o["codes2"], weights[2][1], weights[2][2], 128, {"row_scales": o["scales2"]}, "logits")
+        # (the softmax in 32 bits: exp of a difference of logits, both roundings of it, the sum and the quotient)
+        p = torch.softmax(o["logits"].double(), -1)
+        _inside(o["p"], p, p * (1e-5 + 2 * UNIT * o["logits"].double().abs().amax()) + 2.0 ** -126, "softmax")
+        tokens, kept = plain.verify(o["p"].view(B, D + 1, V), i["drafted"], i["uniforms"])
+        assert torch.equal(o["tokens"].cpu(), tokens) and torch.equal(o["accepted"].cpu(), kept)
