@@ -521,7 +521,7 @@ typedef struct {
 } disc_linear4_desc;
 int disc_register_linear4(disc_ctx* ctx, const disc_linear4_desc* desc, int32_t* id_out);
 /* disc_linear4: out[m, j] = row_scale[m] sum_i x[m, i] scale[j, i / group] (code[j, i] - zero[j, i / group]) + bias[j], products and sums in
- * 32 bits or more, rounded once.  Made for few rows, as a step of a batch has them: 64 rows are one pass over the weights.
+ * 32 bits or more, rounded once.  Made for few rows, as a step of a batch has them: up to 64, the weights come from memory once.
  * dims = {rows, n, k (a multiple of the group), row stride of x, of out}; inputs = {x, weights, scales [n, k / group]}, with 8-bit rows
  * {.., row_scales fp32 [rows]}, with zero points {.., zeros, one byte each [n, k / group]}, and where there is one {.., bias [n]};
  * outputs = {out}.  weights: [n, k / 2] bytes, 16-byte aligned, element 2i in the lower four bits of byte i, 2i + 1 in the upper.

@@ -51,7 +51,8 @@ struct LinearKernel {
 #define WIDE(M, N, S, W, B) {"disc_linear_wide_" #M "_" #N "_" #S "_" #W "_" #B "_k", M, N, S, W}
 constexpr LinearKernel kLinear[] = {
     FEW(1, 1, 1, 8),  FEW(1, 1, 16, 1), FEW(1, 1, 8, 1),     FEW(2, 1, 8, 1),     FEW(1, 4, 1, 8),     FEW(1, 4, 8, 1),     FEW(2, 4, 8, 1),
-    FEW(1, 16, 8, 1), FEW(4, 16, 4, 1), WIDE(1, 2, 2, 4, 2), WIDE(2, 1, 4, 2, 1), WIDE(2, 2, 2, 4, 1), WIDE(4, 1, 4, 2, 1), WIDE(4, 1, 2, 8, 1),
+    FEW(1, 16, 8, 1), FEW(4, 16, 4, 1), WIDE(1, 2, 2, 4, 2), WIDE(2, 1, 4, 2, 1), WIDE(2, 2, 4, 2, 1), WIDE(2, 2, 2, 4, 1), WIDE(4, 1, 4, 2, 1),
+    WIDE(4, 1, 2, 4, 1), WIDE(4, 1, 2, 8, 1),
 };
 #undef FEW
 #undef WIDE
@@ -62,11 +63,19 @@ constexpr int kLinearCount = sizeof kLinear / sizeof kLinear[0];
 //   1 x 16384 x 1024 49, 8.8, 9.4, 14; 1 x 4096 x 12288 18, 12.9, 9.4, 10.5; 1 x 8192 x 131072 140, 168, 126, 112.
 // Of 5 .. 16, the two without LDS and the one with it: 16 x 4096 x 4096 8.3, 13.4, 17; 16 x 4096 x 12288 17.5, 13.0, 16.0; 16 x 4096 x 28672
 // 38.7, 23.4, 19.9; 10 x 2048 x 20000 13.9, 12.2, 10.3; 16 x 512 x 32768 10.3, 6.0, 6.0; 5 x 8192 x 131072 195, 132, 140.
-// Of more, blocks of 32 columns and of 128: 32 x 4096 x 8192 11.1, 21.6; 32 x 4096 x 28672 42, 25; 61 x 8192 x 8192 36, 71; 64 x 4096 x 28672 66, 34.
-int linear_kernel(int64_t rows, int64_t n, int64_t k, int64_t cus) {
+// Of more, the smallest block that lets every CU have no more than one: a block of more columns takes less a column, and a CU two blocks
+// of a kind twice as long as one.  Tiles of x and of weights of a block 2 x 2, 2 x 4, 2 x 8, 4 x 2, 4 x 4, 4 x 8:
+//   32 x 4096 x 8192 11.3, 14.5, 21.6, 16.4, 20.0, 27.3; 32 x 4096 x 16384 24, 17.1, 24.5, 32, 26, 29; 32 x 4096 x 20480 33, 30, 24.9, 44, 42, 30;
+//   64 x 4096 x 4096 10.9, 14.4, 21.5, 16.7, 20.3, 27.9; 64 x 4096 x 8192 20.4, 15.2, 21.6, 17.5, 20.6, 27.7; 64 x 4096 x 12288 30, 27.5, 21.9, 31, 21.1, 27.8;
+//   64 x 4096 x 20480 52, 42, 43, 50, 45, 31.8; 128 x 4096 x 4096 21.1, 15.0, 21.5, 17.5, 20.6, 27.7; 512 x 4096 x 16384 297, 220, 173, 249, 179, 141.
+// Where two of 8 tiles fit, of long rows and of 8-bit ones the one that shares its weights: 61 x 8192 x 8192 35.4, 33.5; 64 x 4096 x 8192 of i8 13.6, 12.5.
+int linear_kernel(int64_t rows, int64_t n, int64_t k, bool bytes, int64_t cus) {
   const int64_t tiles = ceil_div(n, 16);
-  if (rows > 32) return tiles <= 4 * cus ? 12 : 13;
-  if (rows > 16) return tiles <= 4 * cus ? 10 : 11;
+  if (rows > 32) {
+    const int64_t pairs = tiles * 4 * ceil_div(rows, 64);
+    return pairs <= 4 * cus ? 10 : pairs <= 8 * cus ? (k > 4096 || bytes ? 13 : 11) : pairs <= 16 * cus ? 14 : 15;
+  }
+  if (rows > 16) return tiles <= 2 * cus ? 10 : tiles <= 4 * cus ? 11 : 12;
   if (rows > 4) return rows > 8 && tiles > 4 * cus ? 9 : tiles <= 2 * cus && k > 512 ? 7 : 8;
   if (rows > 1) return k <= 1024 ? 4 : tiles <= 4 * cus ? 5 : 6;
   return k <= 1024 ? 0 : tiles <= cus ? 1 : tiles <= 4 * cus ? 2 : 3;
@@ -338,7 +347,7 @@ int launch_linear4(disc_ctx* c, int32_t id, const int64_t* dims, int n_dims, con
   if (!aligned(a.x, scaled ? 1 : 2) || !aligned(a.scales, 2) || !aligned(a.row_scales, 4) || !aligned(a.bias, 2) || !aligned(a.out, 2))
     return refuse(c, DISC_ERR_INVALID_ARG, "a tensor is not aligned to its elements");
   if (context_device(c) < 0) return on_host(c);
-  const int at = linear_kernel(rows, n, k, context_cus(c));
+  const int at = linear_kernel(rows, n, k, o->storage == DISC_STORAGE_I8, context_cus(c));
   const LinearKernel& f = kLinear[at];
   OnDevice on(context_device(c));
   if (!on.ok) return refuse(c, DISC_ERR_HIP, "hipSetDevice failed");

@@ -1019,8 +1019,10 @@ DISC_DEV void linear_wide_body(const LinearArgs& A) {
   extern "C" __global__ void __launch_bounds__(S * W * 64) disc_linear_wide_##M##_##N##_##S##_##W##_##B##_k(LinearArgs A) { linear_wide_body<M, N, S, W, B>(A); }
 DISC_LINEAR_WIDE_KERNEL(1, 2, 2, 4, 2)
 DISC_LINEAR_WIDE_KERNEL(2, 1, 4, 2, 1)
+DISC_LINEAR_WIDE_KERNEL(2, 2, 4, 2, 1)
 DISC_LINEAR_WIDE_KERNEL(2, 2, 2, 4, 1)
 DISC_LINEAR_WIDE_KERNEL(4, 1, 4, 2, 1)
+DISC_LINEAR_WIDE_KERNEL(4, 1, 2, 4, 1)
 DISC_LINEAR_WIDE_KERNEL(4, 1, 2, 8, 1)
 #endif  // DISC_LINEAR4
 

@@ -353,6 +353,14 @@ def test_linear_of_larger_sizes(ctx, dtype, rows, group, M, N, K):
     _linear(ctx, dtype, rows, group, True, True, M, N, K, 7)
 
 
+@pytest.mark.parametrize("dtype,rows,group,zeros", [("bf16", "same", 64, True), ("f16", "same", 32, False), ("f16", "i8", 32, True), ("bf16", "i8", 128, False), ("bf16", "e4m3", 64, True)])
+def test_linear_of_blocks_of_every_shape(ctx, dtype, rows, group, zeros):
+    # (rows of x and columns by which 2 x 4, 4 x 2 and 4 x 4 tiles make a block, ragged ends of both; rows of weights of short and of long k)
+    for i, (M, N, K) in enumerate([(31, 9001, 9 * group), (40, 4111, 11 * group), (64, 8190, 4096), (33, 4100, 4096 + group), (61, 8191, 4096 + 3 * group), (90, 4095, 7 * group),
+                                   (49, 12301, 5 * group), (64, 16384, 3 * group), (129, 5003, 1024 + group), (270, 2010, group)]):
+        _linear(ctx, dtype, rows, group, zeros, bool(i % 2), M, N, K, 200 + i, strided=bool((i // 2) % 2))
+
+
 # ---- drafted tokens --------------------------------------------------------------------------------
 
 
@@ -520,6 +528,13 @@ def test_linear_rows_do_not_see_each_other(ctx, rows, M, N):
     kept = [m for m in range(M) if m not in (M - 1, M // 2)]
     assert torch.equal(got[kept], want[kept]) and not torch.isfinite(got[M // 2]).any()
     assert rows == "i8" or not torch.isfinite(got[M - 1]).any()
+
+
+@pytest.mark.parametrize("M,N", [(20, 8209), (40, 4099), (40, 8200)])
+def test_linear_of_the_largest_rows_by_columns(ctx, M, N):
+    test_linear_of_the_largest_rows_and_scales(ctx, M, N)
+    test_linear_rows_do_not_see_each_other(ctx, "same", M, N)
+    test_linear_rows_do_not_see_each_other(ctx, "i8", M, N)
 
 
 def test_past_32_bits(ctx):
