@@ -293,7 +293,7 @@ struct Operator {
   std::string code;                // what its device code is compiled from
   void* module = nullptr;          // hipModule_t, the first operator's of the same code
   bool owns_module = false;
-  void* fn[16] = {};                // hipFunction_t
+  void* fn[18] = {};                // hipFunction_t
   int resident = 2;                // blocks of its main kernel that a CU holds at once
 };
 

@@ -50,34 +50,40 @@ struct LinearKernel {
 #define FEW(N, R, S, W) {"disc_linear_" #N "_" #R "_" #S "_" #W "_k", 1, N, S, W}
 #define WIDE(M, N, S, W, B) {"disc_linear_wide_" #M "_" #N "_" #S "_" #W "_" #B "_k", M, N, S, W}
 constexpr LinearKernel kLinear[] = {
-    FEW(1, 1, 1, 8),  FEW(1, 1, 16, 1), FEW(1, 1, 8, 1),     FEW(2, 1, 8, 1),     FEW(1, 4, 1, 8),     FEW(1, 4, 8, 1),     FEW(2, 4, 8, 1),
-    FEW(1, 16, 8, 1), FEW(4, 16, 4, 1), WIDE(1, 2, 2, 4, 2), WIDE(2, 1, 4, 2, 1), WIDE(2, 2, 4, 2, 1), WIDE(2, 2, 2, 4, 1), WIDE(4, 1, 4, 2, 1),
-    WIDE(4, 1, 2, 4, 1), WIDE(4, 1, 2, 8, 1),
+    FEW(1, 1, 1, 8),     FEW(1, 1, 16, 1),    FEW(1, 1, 8, 1),     FEW(2, 1, 8, 1),     FEW(1, 4, 1, 8),     FEW(1, 4, 8, 1),
+    FEW(1, 16, 8, 1),    WIDE(1, 2, 2, 4, 2), WIDE(1, 1, 8, 1, 2), WIDE(1, 1, 4, 2, 2), WIDE(1, 1, 2, 4, 4), WIDE(1, 1, 2, 8, 4),
+    WIDE(2, 1, 8, 1, 1), WIDE(2, 1, 4, 2, 1), WIDE(2, 2, 4, 2, 2), WIDE(2, 2, 2, 4, 2), WIDE(4, 1, 2, 4, 2), WIDE(4, 1, 2, 8, 1),
 };
 #undef FEW
 #undef WIDE
 constexpr int kLinearCount = sizeof kLinear / sizeof kLinear[0];
+static_assert(kLinearCount <= (int)(sizeof(Operator::fn) / sizeof(void*)) && FN_NORM_COUNT <= kLinearCount, "an operator holds as many kernels");
 // Which of them, by rows x k x n (us).  Of one row, the first four: a team's wavefronts take 256 elements each at a time, so that rows
 // are shared out by as many as leave each something; where columns are many, two tiles share what is loaded of x.
 //   1 x 512 x 32768 4.4, 16.1, 7.4, 6.2; 1 x 1024 x 32768 6.3, 17.1, 8.0, 7.2; 1 x 4096 x 4096 9.3, 4.8, 4.9, 5.8;
 //   1 x 16384 x 1024 49, 8.8, 9.4, 14; 1 x 4096 x 12288 18, 12.9, 9.4, 10.5; 1 x 8192 x 131072 140, 168, 126, 112.
-// Of 5 .. 16, the two without LDS and the one with it: 16 x 4096 x 4096 8.3, 13.4, 17; 16 x 4096 x 12288 17.5, 13.0, 16.0; 16 x 4096 x 28672
-// 38.7, 23.4, 19.9; 10 x 2048 x 20000 13.9, 12.2, 10.3; 16 x 512 x 32768 10.3, 6.0, 6.0; 5 x 8192 x 131072 195, 132, 140.
-// Of more, the smallest block that lets every CU have no more than one: a block of more columns takes less a column, and a CU two blocks
-// of a kind twice as long as one.  Tiles of x and of weights of a block 2 x 2, 2 x 4, 2 x 8, 4 x 2, 4 x 4, 4 x 8:
-//   32 x 4096 x 8192 11.3, 14.5, 21.6, 16.4, 20.0, 27.3; 32 x 4096 x 16384 24, 17.1, 24.5, 32, 26, 29; 32 x 4096 x 20480 33, 30, 24.9, 44, 42, 30;
-//   64 x 4096 x 4096 10.9, 14.4, 21.5, 16.7, 20.3, 27.9; 64 x 4096 x 8192 20.4, 15.2, 21.6, 17.5, 20.6, 27.7; 64 x 4096 x 12288 30, 27.5, 21.9, 31, 21.1, 27.8;
-//   64 x 4096 x 20480 52, 42, 43, 50, 45, 31.8; 128 x 4096 x 4096 21.1, 15.0, 21.5, 17.5, 20.6, 27.7; 512 x 4096 x 16384 297, 220, 173, 249, 179, 141.
-// Where two of 8 tiles fit, of long rows and of 8-bit ones the one that shares its weights: 61 x 8192 x 8192 35.4, 33.5; 64 x 4096 x 8192 of i8 13.6, 12.5.
-int linear_kernel(int64_t rows, int64_t n, int64_t k, bool bytes, int64_t cus) {
+// Of more, the smallest block by which every CU has no more than one: a block of more columns takes less a column, and a CU two blocks of a
+// kind twice as long as one.  Columns of a block 16, 32, 64, 128 (where there are fewer of 16 rows of x, of 32, of 64: further below):
+//   16 x 4096 x 4096 6.9, 7.4, 10.2, 13.9; 16 x 4096 x 8192 12.0, 8.0, 10.3, 13.9; 16 x 4096 x 12288 17.2, 13.5, 10.5, 13.9; 16 x 4096 x 28672 44, 29, 22, 18.3;
+//   16 x 8192 x 131072 297, 195, 164, 135; of 32 rows of x: 32 x 4096 x 4096 10.3, 10.5, 13.2, 19.7; 32 x 14336 x 4096 25.6, 30, 37, 66; 32 x 4096 x 12288
+//   -, 19.6, 14.0, 20.0; 32 x 4096 x 28672 -, 42, 29, 24.6; 64 x 4096 x 4096 18.2, 10.6, 13.4, 19.5; 64 x 8192 x 8192 -, 35.7, 25.9, 39.9;
+//   of 64 rows, the last two: 64 x 4096 x 12288 21.1, 27.8; 64 x 12288 x 12288 59, 78 (of 32 rows 60); 64 x 4096 x 28672 45, 35.8.
+// Of up to 16 rows and a short k, or few columns and rows, x comes without LDS, or with two tiles of columns a wavefront:
+//   16 x 512 x 8192 4.0 (6.7 by 16 columns, 3.8 by 32); 5 x 4096 x 4096 6.2 (7.1); 8 x 4096 x 4096 6.6 (6.7); 16 x 512 x 32768 5.9 (7.1 by 128); 16 x 512 x 131072 20 (26).
+// Two to four rows of many columns as more: 3 x 8192 x 131072 145 without LDS, 125; 3 x 4096 x 28672 18.4, 15.9; 3 x 4096 x 12288 9.2, 9.8.
+int linear_kernel(int64_t rows, int64_t n, int64_t k, int64_t cus) {
   const int64_t tiles = ceil_div(n, 16);
   if (rows > 32) {
-    const int64_t pairs = tiles * 4 * ceil_div(rows, 64);
-    return pairs <= 4 * cus ? 10 : pairs <= 8 * cus ? (k > 4096 || bytes ? 13 : 11) : pairs <= 16 * cus ? 14 : 15;
+    const int64_t pairs = tiles * 4 * ceil_div(rows, 64);   // tiles of x times those of weights
+    return pairs <= 2 * cus ? 12 : pairs <= 4 * cus ? 13 : pairs <= 8 * cus ? 14 : pairs <= 16 * cus ? 16 : 17;
   }
-  if (rows > 16) return tiles <= 2 * cus ? 10 : tiles <= 4 * cus ? 11 : 12;
-  if (rows > 4) return rows > 8 && tiles > 4 * cus ? 9 : tiles <= 2 * cus && k > 512 ? 7 : 8;
-  if (rows > 1) return k <= 1024 ? 4 : tiles <= 4 * cus ? 5 : 6;
+  if (rows > 16) return tiles <= cus ? 12 : tiles <= 2 * cus ? 13 : tiles <= 4 * cus ? 14 : 15;
+  if (rows > 4) {
+    if (tiles <= cus) return k <= 1024 || (rows <= 8 && k <= 4096) ? 6 : 8;
+    if (tiles <= 2 * cus) return k <= 512 ? 6 : 9;
+    return tiles <= 4 * cus ? 10 : k <= 1024 ? 7 : 11;
+  }
+  if (rows > 1) return k <= 1024 ? 4 : tiles <= 4 * cus ? 5 : 11;
   return k <= 1024 ? 0 : tiles <= cus ? 1 : tiles <= 4 * cus ? 2 : 3;
 }
 enum { FN_VERIFY_SUM = 0, FN_VERIFY_PICK, FN_VERIFY_COUNT };
@@ -347,7 +353,7 @@ int launch_linear4(disc_ctx* c, int32_t id, const int64_t* dims, int n_dims, con
   if (!aligned(a.x, scaled ? 1 : 2) || !aligned(a.scales, 2) || !aligned(a.row_scales, 4) || !aligned(a.bias, 2) || !aligned(a.out, 2))
     return refuse(c, DISC_ERR_INVALID_ARG, "a tensor is not aligned to its elements");
   if (context_device(c) < 0) return on_host(c);
-  const int at = linear_kernel(rows, n, k, o->storage == DISC_STORAGE_I8, context_cus(c));
+  const int at = linear_kernel(rows, n, k, context_cus(c));
   const LinearKernel& f = kLinear[at];
   OnDevice on(context_device(c));
   if (!on.ok) return refuse(c, DISC_ERR_HIP, "hipSetDevice failed");

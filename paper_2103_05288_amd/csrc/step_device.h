@@ -902,9 +902,7 @@ DISC_LINEAR_KERNEL(1, 1, 8, 1)
 DISC_LINEAR_KERNEL(2, 1, 8, 1)
 DISC_LINEAR_KERNEL(1, 4, 1, 8)
 DISC_LINEAR_KERNEL(1, 4, 8, 1)
-DISC_LINEAR_KERNEL(2, 4, 8, 1)
 DISC_LINEAR_KERNEL(1, 16, 8, 1)
-DISC_LINEAR_KERNEL(4, 16, 4, 1)
 
 // ---- more rows --------------------------------------------------------------------------------------
 // kM tiles of 16 rows of x through LDS, in chunks of kSplit * kBlocksEach blocks: one in use, the next one in LDS, the one behind it on
@@ -1025,11 +1023,15 @@ DISC_DEV void linear_wide_body(const LinearArgs& A) {
 #define DISC_LINEAR_WIDE_KERNEL(M, N, S, W, B) \
   extern "C" __global__ void __launch_bounds__(S * W * 64) disc_linear_wide_##M##_##N##_##S##_##W##_##B##_k(LinearArgs A) { linear_wide_body<M, N, S, W, B>(A); }
 DISC_LINEAR_WIDE_KERNEL(1, 2, 2, 4, 2)
+DISC_LINEAR_WIDE_KERNEL(1, 1, 8, 1, 2)
+DISC_LINEAR_WIDE_KERNEL(1, 1, 4, 2, 2)
+DISC_LINEAR_WIDE_KERNEL(1, 1, 2, 4, 4)
+DISC_LINEAR_WIDE_KERNEL(1, 1, 2, 8, 4)
+DISC_LINEAR_WIDE_KERNEL(2, 1, 8, 1, 1)
 DISC_LINEAR_WIDE_KERNEL(2, 1, 4, 2, 1)
-DISC_LINEAR_WIDE_KERNEL(2, 2, 4, 2, 1)
-DISC_LINEAR_WIDE_KERNEL(2, 2, 2, 4, 1)
-DISC_LINEAR_WIDE_KERNEL(4, 1, 4, 2, 1)
-DISC_LINEAR_WIDE_KERNEL(4, 1, 2, 4, 1)
+DISC_LINEAR_WIDE_KERNEL(2, 2, 4, 2, 2)
+DISC_LINEAR_WIDE_KERNEL(2, 2, 2, 4, 2)
+DISC_LINEAR_WIDE_KERNEL(4, 1, 2, 4, 2)
 DISC_LINEAR_WIDE_KERNEL(4, 1, 2, 8, 1)
 #endif  // DISC_LINEAR4
 

@@ -357,7 +357,9 @@ def test_linear_of_larger_sizes(ctx, dtype, rows, group, M, N, K):
 def test_linear_of_blocks_of_every_shape(ctx, dtype, rows, group, zeros):
     # (rows of x and columns by which 2 x 4, 4 x 2 and 4 x 4 tiles make a block, ragged ends of both; rows of weights of short and of long k)
     for i, (M, N, K) in enumerate([(31, 9001, 9 * group), (40, 4111, 11 * group), (64, 8190, 4096), (33, 4100, 4096 + group), (61, 8191, 4096 + 3 * group), (90, 4095, 7 * group),
-                                   (49, 12301, 5 * group), (64, 16384, 3 * group), (129, 5003, 1024 + group), (270, 2010, group)]):
+                                   (49, 12301, 5 * group), (64, 16384, 3 * group), (129, 5003, 1024 + group), (270, 2010, group), (9, 1003, 4096 + group), (16, 2049, 1024 + 5 * group),
+                                   (6, 4081, 4096 + 3 * group), (5, 4113, 1024 + group), (13, 8191, 2048 + 7 * group), (7, 8205, 9 * group), (16, 16383, 17 * group), (3, 16401, 1024 + 7 * group),
+                                   (16, 16500, 2048 + 9 * group), (20, 1001, 13 * group), (40, 1999, 21 * group), (18, 16500, 5 * group), (8, 16999, 1024)]):
         _linear(ctx, dtype, rows, group, zeros, bool(i % 2), M, N, K, 200 + i, strided=bool((i // 2) % 2))
 
 
@@ -530,7 +532,7 @@ def test_linear_rows_do_not_see_each_other(ctx, rows, M, N):
     assert rows == "i8" or not torch.isfinite(got[M - 1]).any()
 
 
-@pytest.mark.parametrize("M,N", [(20, 8209), (40, 4099), (40, 8200)])
+@pytest.mark.parametrize("M,N", [(20, 8209), (40, 4099), (40, 8200), (12, 4100), (12, 8200)])
 def test_linear_of_the_largest_rows_by_columns(ctx, M, N):
     test_linear_of_the_largest_rows_and_scales(ctx, M, N)
     test_linear_rows_do_not_see_each_other(ctx, "same", M, N)
