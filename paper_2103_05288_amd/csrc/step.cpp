@@ -63,12 +63,12 @@ static_assert(kLinearCount <= (int)(sizeof(Operator::fn) / sizeof(void*)) && FN_
 //   1 x 512 x 32768 4.4, 16.1, 7.4, 6.2; 1 x 1024 x 32768 6.3, 17.1, 8.0, 7.2; 1 x 4096 x 4096 9.3, 4.8, 4.9, 5.8;
 //   1 x 16384 x 1024 49, 8.8, 9.4, 14; 1 x 4096 x 12288 18, 12.9, 9.4, 10.5; 1 x 8192 x 131072 140, 168, 126, 112.
 // Of more, the smallest block by which every CU has no more than one: a block of more columns takes less a column, and a CU two blocks of a
-// kind twice as long as one.  Columns of a block 16, 32, 64, 128 (where there are fewer of 16 rows of x, of 32, of 64: further below):
+// kind twice as long as one.  Columns of a block 16, 32, 64, 128, of 16 rows of x:
 //   16 x 4096 x 4096 6.9, 7.4, 10.2, 13.9; 16 x 4096 x 8192 12.0, 8.0, 10.3, 13.9; 16 x 4096 x 12288 17.2, 13.5, 10.5, 13.9; 16 x 4096 x 28672 44, 29, 22, 18.3;
 //   16 x 8192 x 131072 297, 195, 164, 135; of 32 rows of x: 32 x 4096 x 4096 10.3, 10.5, 13.2, 19.7; 32 x 14336 x 4096 25.6, 30, 37, 66; 32 x 4096 x 12288
 //   -, 19.6, 14.0, 20.0; 32 x 4096 x 28672 -, 42, 29, 24.6; 64 x 4096 x 4096 18.2, 10.6, 13.4, 19.5; 64 x 8192 x 8192 -, 35.7, 25.9, 39.9;
-//   of 64 rows, the last two: 64 x 4096 x 12288 21.1, 27.8; 64 x 12288 x 12288 59, 78 (of 32 rows 60); 64 x 4096 x 28672 45, 35.8.
-// Of up to 16 rows and a short k, or few columns and rows, x comes without LDS, or with two tiles of columns a wavefront:
+//   64 and 128 columns of 64 rows: 64 x 4096 x 12288 21.1, 27.8; 64 x 12288 x 12288 59, 78 (128 of 32 rows 60); 64 x 4096 x 28672 45, 35.8.
+// Of up to 16 rows and a short k, or few columns and rows, x comes without LDS, or a wavefront has two tiles of columns:
 //   16 x 512 x 8192 4.0 (6.7 by 16 columns, 3.8 by 32); 5 x 4096 x 4096 6.2 (7.1); 8 x 4096 x 4096 6.6 (6.7); 16 x 512 x 32768 5.9 (7.1 by 128); 16 x 512 x 131072 20 (26).
 // Two to four rows of many columns as more: 3 x 8192 x 131072 145 without LDS, 125; 3 x 4096 x 28672 18.4, 15.9; 3 x 4096 x 12288 9.2, 9.8.
 int linear_kernel(int64_t rows, int64_t n, int64_t k, int64_t cus) {

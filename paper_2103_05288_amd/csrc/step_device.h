@@ -441,7 +441,7 @@ extern "C" __global__ void __launch_bounds__(1024) disc_norm_join_k(NormBackward
 // 2^-17 of a result's size, where a bf16 result has 2^-9; of f16 results, which have 2^-12, c - 8 is formed instead.
 // Bound by the weights' bytes where there are few rows, and with more by what a CU's memory pipe takes to bring x to the lanes: a load
 // of 16 bytes a lane costs it the same whether the lanes' addresses differ or not.  So x of up to 4 rows is loaded in whole wavefronts
-// and turned into place (linear_body), and of more rows goes through LDS, where 64 or 128 columns share it (linear_wide_body).
+// and turned into place (linear_body), and of more rows goes through LDS, where a block's 16 .. 128 columns share it (linear_wide_body).
 // Unpacking costs next to nothing beside that (with all of it left out, 1 x 8192 x 131072 takes 118 us, not 122).
 // =================================================================================================
 #if DISC_T_F16
@@ -908,10 +908,11 @@ DISC_LINEAR_KERNEL(1, 16, 8, 1)
 // kM tiles of 16 rows of x through LDS, in chunks of kSplit * kBlocksEach blocks: one in use, the next one in LDS, the one behind it on
 // its way in registers.  An operand of a product is 16 bytes a lane; its 16 rows are turned by a number that differs between the
 // operands of a row, so that neither the writes (a row's operands) nor the reads (16 rows of one) meet in a bank.
-// (us without / with LDS: 64 x 4096 x 28672 bf16 87 / 34, 61 x 8192 x 8192 44 / 36, 32 x 4096 x 28672 50 / 25, 16 x 4096 x 28672 23 / 20,
-// 64 x 4096 x 28672 of e4m3 119 / 38.)  Bound by the steps of a chunk, whose parts wait for each other: x to LDS, a barrier, products.
-// (us of 61 x 8192 x 8192 and 64 x 4096 x 28672, 38 and 40, without products 32 and 12.5, without weights and scales 30 and 30.5, without
-// reads of LDS 34 and 41, without the products with ones 33 and 33.)
+// (us without / with LDS: 64 x 4096 x 28672 bf16 87 / 34, 61 x 8192 x 8192 44 / 25, 32 x 4096 x 28672 50 / 24, 16 x 4096 x 28672 23 / 17,
+// 64 x 4096 x 28672 of e4m3 119 / 36.  A wavefront's blocks of a chunk, 1 / 2, which share a load of scales: 32 x 8192 x 28672 51 / 44,
+// 64 x 12288 x 12288 of e4m3 66 / 49.)  Bound by the steps of a chunk, whose parts wait for each other: x to LDS, a barrier, products.
+// (us of 61 x 8192 x 8192 in blocks of 64 x 32 and of 64 x 4096 x 28672 in blocks of 64 x 128, 38 and 40: without products 32 and 12.5, without
+// weights and scales 30 and 30.5, without reads of LDS 34 and 41, without the products with ones 33 and 33.)
 template <int kM, int kN, int kSplit, int kTeams, int kBlocksEach>
 DISC_DEV void linear_wide_body(const LinearArgs& A) {
   constexpr int kThreads = kSplit * kTeams * 64, kBlocks = kSplit * kBlocksEach, kRowUnits = 4 * kXs, kUnits = kBlocks * 16 * kM * kRowUnits;
