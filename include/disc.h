@@ -541,7 +541,8 @@ int disc_register_verify(disc_ctx* ctx, const disc_verify_desc* desc, int32_t* i
  * uniform[b, drafts]: the first token whose running sum of weights is above uniform times their sum.  The weights are max(target - draft, 0)
  * at place a where a < n (target where these are all zero), target[b, n] where a = n; what is negative, infinite or NaN counts
  * as 0, and where nothing is left the token is -1.  tokens[b] = the kept ones, that one, then -1.
- * Comparisons, differences and sums are in 64 bits, in a fixed order.  Uniforms are in [0, 1).
+ * Comparisons, differences and sums are in 64 bits, in a fixed order.  Uniforms are in [0, 1); a last one of 1 draws the last token with
+ * any weight.
  * dims = {batch, drafts (0 .. 4096), vocabulary, sequence stride, place stride of target, sequence stride, place stride of draft,
  * draft != 0, lengths != 0}; inputs = {target [batch, drafts + 1, vocabulary], drafted int32 [batch, drafts], uniforms fp32 [batch, drafts + 1]}
  * and where the last dims say so {.., draft [batch, drafts, vocabulary]}, {.., lengths int32 [batch]}; outputs = {tokens int32

@@ -1176,14 +1176,14 @@ struct Range {
   bool from_less;
   double before, goal;
   DISC_DEV Range(bool takes_less, float uniform, double less, double all) {
-    less = wave_running(less);
-    all = wave_running(all);
-    const double whole_less = of_lane(less, 63);
+    const double upto_less = wave_running(less), upto_all = wave_running(all);
+    const double whole_less = of_lane(upto_less, 63);
     from_less = takes_less && whole_less > 0;
-    const double upto = from_less ? less : all, whole = of_lane(upto, 63), u = (double)uniform;
+    const double own = from_less ? less : all, upto = from_less ? upto_less : upto_all, whole = of_lane(upto, 63), u = (double)uniform;
     goal = (u > 0 ? u : 0.0) * whole;
     const double front = moved<0x138, 0xf>(upto);           // (the lane's before it)
-    const u64 some = __ballot(upto > front), over = __ballot(upto > front && upto > goal);
+    // (by the lane's own sum: each lane's running sum is added up in another order, so that of a lane without weight can be above the one before)
+    const u64 some = __ballot(own > 0), over = __ballot(own > 0 && upto > goal);
     range = over ? (int)__builtin_ctzll(over) : some ? 63 - (int)__builtin_clzll(some) : -1;
     before = of_lane(front, max(range, 0));
   }
