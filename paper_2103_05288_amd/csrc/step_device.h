@@ -1282,12 +1282,14 @@ extern "C" __global__ void __launch_bounds__(256) disc_verify_pick_k(VerifyArgs 
     int chunk = r.range * each;
     if (each > 1) {
       int last = chunk;
+      double upto = r.before;                               // of the chunks so far; r.before stays what is in front of the last of them
       for (int i = chunk; i < min(chunk + each, A.chunks); ++i) {
         const double x = part[2 * i + (r.from_less ? 0 : 1)];
         if (!(x > 0)) continue;
         last = i;
-        if (r.before + x > r.goal) break;
-        r.before += x;
+        r.before = upto;
+        upto += x;
+        if (upto > r.goal) break;
       }
       chunk = last;
     }

@@ -62,3 +62,20 @@ def test_verify_with_a_last_uniform_of_one(ctx):
     rows[:, :30000] = torch.softmax(2 * torch.randn(100, 30000, generator=g), -1)
     for row, t in zip(rows, _draw(ctx, rows, [1.0] * 100, False)):
         _fits(row, 1.0, t)
+
+
+@pytest.mark.parametrize("V", [300001, 1000000])
+def test_verify_of_several_chunks_a_lane_at_their_ends(ctx, V):
+    """Vocabularies of more than 64 chunks: rows of few weights and dense ones, uniforms on the running sums and 1."""
+    g = random.Random(V)
+    rows, uniforms = [], []
+    for i in range(24):
+        rows.append(_sparse(g, V, g.choice((2, 5, 20, 60))))
+        uniforms += [1.0] if i % 3 == 0 else _uniforms(g, rows[-1], 1)
+    for first in (0, V // 2):
+        rows.append(torch.zeros(V))
+        rows[-1][first:V - 5000:701] = 0.25 + torch.rand(len(range(first, V - 5000, 701)), generator=torch.Generator().manual_seed(first))
+        uniforms.append(1.0)
+    rows = torch.stack(rows)
+    for row, u, t in zip(rows, uniforms, _draw(ctx, rows, uniforms, False)):
+        _fits(row, u, t)

@@ -232,3 +232,20 @@ def test_what_is_left_of_the_target_beside_the_draft(kernels):
     assert accepted.tolist() == [0] * 8 and tokens[:, 1].tolist() == [-1] * 8
     for row, u, t in zip(target[:, 0], uniforms[:, 1].tolist(), tokens[:, 0].tolist()):
         _fits(row, u, t)
+
+
+def test_the_sum_in_front_of_a_chunk_of_several_of_a_lane(kernels):
+    """More than 64 chunks: where rounding, or a uniform of 1, leaves no token whose running sum passes the goal, the last with weight is
+    taken, not the first of its chunk."""
+    V, g = 64 * CHUNK + 3000, random.Random(5)
+    rows = [torch.zeros(V) for _ in range(4)]
+    for row, (first, last) in zip(rows, ((0, 8), (60, 64), (3, 4), (0, 65))):
+        for c in range(first, last):
+            for _ in range(6):
+                row[min(V - 1, c * CHUNK + g.randrange(CHUNK))] = g.random() + 0.1
+    rows.append(torch.zeros(V))
+    rows[-1][4096 * 30::1500] = 0.001
+    uniforms = [1.0] * 4 + _uniforms(g, rows[-1], 1)
+    tokens, _ = _run(kernels, torch.stack(rows)[:, None].contiguous(), torch.tensor(uniforms)[:, None].contiguous())
+    for row, u, t in zip(rows, uniforms, tokens[:, 0].tolist()):
+        _fits(row, u, t)
