@@ -35,7 +35,7 @@ def codes4(weights):
 
 
 def linear4(x, weights, scales, group, zeros=None, row_scales=None, bias=None):
-    """The result, and sum |x| (128 + c) |s|: what the sums' roundings are relative to."""
+    """The result, and sum |x| |c - z| |s|: what the sums' roundings are relative to."""
     n, k = weights.shape[0], 2 * weights.shape[1]
     c = codes4(weights).double().view(n, k // group, group)
     z = torch.full((n, k // group, 1), 8.0, dtype=torch.float64, device=weights.device) if zeros is None else zeros.double().unsqueeze(-1)
@@ -43,7 +43,7 @@ def linear4(x, weights, scales, group, zeros=None, row_scales=None, bias=None):
     r = torch.ones(x.shape[0], 1, dtype=torch.float64, device=x.device) if row_scales is None else row_scales.double().unsqueeze(-1)
     b = torch.zeros(n, dtype=torch.float64, device=x.device) if bias is None else bias.double()
     y = torch.mm(x.double(), ((c - z) * s).view(n, k).t().contiguous()) * r + b
-    size = torch.mm(x.double().abs(), ((c + 128.0 + z) * s.abs()).view(n, k).t().contiguous()) * r.abs() + b.abs()
+    size = torch.mm(x.double().abs(), ((c - z).abs() * s.abs()).view(n, k).t().contiguous()) * r.abs() + b.abs()
     return y, size
 
 

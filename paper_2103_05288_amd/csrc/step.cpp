@@ -60,17 +60,19 @@ constexpr int kLinearCount = sizeof kLinear / sizeof kLinear[0];
 static_assert(kLinearCount <= (int)(sizeof(Operator::fn) / sizeof(void*)) && FN_NORM_COUNT <= kLinearCount, "an operator holds as many kernels");
 // Which of them, by rows x k x n (us).  Of one row, the first four: a team's wavefronts take 256 elements each at a time, so that rows
 // are shared out by as many as leave each something; where columns are many, two tiles share what is loaded of x.
-//   1 x 512 x 32768 4.4, 16.1, 7.4, 6.2; 1 x 1024 x 32768 6.3, 17.1, 8.0, 7.2; 1 x 4096 x 4096 9.3, 4.8, 4.9, 5.8;
-//   1 x 16384 x 1024 49, 8.8, 9.4, 14; 1 x 4096 x 12288 18, 12.9, 9.4, 10.5; 1 x 8192 x 131072 140, 168, 126, 112.
+//   1 x 512 x 32768 4.8, 17.3, 7.9, 7.2; 1 x 1024 x 32768 7.1, 18.3, 8.7, 8.3; 1 x 4096 x 4096 18.9, 5.1, 5.2, 6.8;
+//   1 x 16384 x 1024 67, 10.5, 11.3, 17; 1 x 4096 x 12288 19.5, 12.3, 8.9, 10.5; 1 x 8192 x 131072 170, 190, 133, 123.
+// (x through LDS, the last of those for 16 rows, is a seventh faster than the fourth at 1 x 4096 x 28672, 17.0 for 19.3, as fast at 1 x 8192 x 32768, 36.1
+// for 36.5, and slower at 1 x 8192 x 131072, 134; it is not among the choices for one row.)
 // Of more, the smallest block by which every CU has no more than one: a block of more columns takes less a column, and a CU two blocks of a
 // kind twice as long as one.  Columns of a block 16, 32, 64, 128, of 16 rows of x:
-//   16 x 4096 x 4096 6.9, 7.4, 10.2, 13.9; 16 x 4096 x 8192 12.0, 8.0, 10.3, 13.9; 16 x 4096 x 12288 17.2, 13.5, 10.5, 13.9; 16 x 4096 x 28672 44, 29, 22, 18.3;
-//   16 x 8192 x 131072 297, 195, 164, 135; of 32 rows of x: 32 x 4096 x 4096 10.3, 10.5, 13.2, 19.7; 32 x 14336 x 4096 25.6, 30, 37, 66; 32 x 4096 x 12288
-//   -, 19.6, 14.0, 20.0; 32 x 4096 x 28672 -, 42, 29, 24.6; 64 x 4096 x 4096 18.2, 10.6, 13.4, 19.5; 64 x 8192 x 8192 -, 35.7, 25.9, 39.9;
-//   64 and 128 columns of 64 rows: 64 x 4096 x 12288 21.1, 27.8; 64 x 12288 x 12288 59, 78 (128 of 32 rows 60); 64 x 4096 x 28672 45, 35.8.
+//   16 x 4096 x 4096 7.1, 7.6, 10.5, 16.0; 16 x 4096 x 8192 12.8, 8.1, 10.6, 15.9; 16 x 4096 x 12288 18.3, 14.2, 10.8, 15.9; 16 x 4096 x 28672 45, 30, 22, 19.8;
+//   16 x 8192 x 131072 307, 198, 152, 146; of 32 rows of x: 32 x 4096 x 4096 9.3, 10.5, 14.4, 21.1; 32 x 14336 x 4096 22.6, 27, 37, 63; 32 x 4096 x 12288
+//   -, 20.3, 14.7, 21.1; 32 x 4096 x 28672 -, 43, 31, 24.5; 64 x 4096 x 4096 16.4, 10.6, 14.2, 20.8; 64 x 8192 x 8192 -, 36.4, 26.3, 41.8;
+//   64 and 128 columns of 64 rows: 64 x 4096 x 12288 19.7, 26.5; 64 x 12288 x 12288 57, 76 (128 of 32 rows 62); 64 x 4096 x 28672 43, 30.8.
 // Of up to 16 rows and a short k, or few columns and rows, x comes without LDS, or a wavefront has two tiles of columns:
-//   16 x 512 x 8192 4.0 (6.7 by 16 columns, 3.8 by 32); 5 x 4096 x 4096 6.2 (7.1); 8 x 4096 x 4096 6.6 (6.7); 16 x 512 x 32768 5.9 (7.1 by 128); 16 x 512 x 131072 20 (26).
-// Two to four rows of many columns as more: 3 x 8192 x 131072 145 without LDS, 125; 3 x 4096 x 28672 18.4, 15.9; 3 x 4096 x 12288 9.2, 9.8.
+//   16 x 512 x 8192 4.0 (6.9 by 16 columns, 4.1 by 32); 5 x 4096 x 4096 6.1 (6.7); 8 x 4096 x 4096 6.6 (6.7); 16 x 512 x 32768 6.4 (7.8 by 128); 16 x 512 x 131072 21 (28).
+// Two to four rows of many columns as more: 3 x 8192 x 131072 160 without LDS, 138; 3 x 4096 x 28672 20.5, 17.9; 3 x 4096 x 12288 9.3, 15.7.
 int linear_kernel(int64_t rows, int64_t n, int64_t k, int64_t cus) {
   const int64_t tiles = ceil_div(n, 16);
   if (rows > 32) {

@@ -434,15 +434,16 @@ extern "C" __global__ void __launch_bounds__(1024) disc_norm_join_k(NormBackward
 #ifdef DISC_LINEAR4
 // =================================================================================================
 // y[m, n] = r[m] sum_k x[m, k] s[n, k / G] (c[n, k] - z[n, k / G]) + bias[n] with codes c of 4 bits.
-// A group's products are summed with the codes as they are (128 + c of bf16, c - 8 of f16, c of i8), and the zero point is taken off
-// with the sum of the group's x, which a product with ones gives in the layout of the results:
-//   sum x (c - z) = sum x (128 + c) - (128 + z) sum x,
-// in 32 bits (i8: whole numbers, exact); then times s, added up over the groups in 32 bits.  What the 128 adds to the roundings is below
-// 2^-17 of a result's size, where a bf16 result has 2^-9; of f16 results, which have 2^-12, c - 8 is formed instead.
+// A group's products are summed with the codes less their zero point, c - z: whole numbers of at most eight bits, which both 16-bit types
+// hold, so that an element whose code is its zero point adds nothing, however large x is.  (Codes as they are, with the zero point taken off
+// by the group's sum of x, cost half as many instructions and round relative to sum |x| (c + z).)  i8 sums are whole numbers, exact
+// in that form too, with the sum of x from a product with ones:  sum x (c - z) = sum x c - z sum x.
+// The groups' sums, in 32 bits, are multiplied by s and added up in 32 bits.
 // Bound by the weights' bytes where there are few rows, and with more by what a CU's memory pipe takes to bring x to the lanes: a load
 // of 16 bytes a lane costs it the same whether the lanes' addresses differ or not.  So x of up to 4 rows is loaded in whole wavefronts
 // and turned into place (linear_body), and of more rows goes through LDS, where a block's 16 .. 128 columns share it (linear_wide_body).
-// Unpacking costs next to nothing beside that (with all of it left out, 1 x 8192 x 131072 takes 118 us, not 122).
+// Unpacking is 17 instructions for eight codes of bf16 and shows where a lane has few rows to use them for (with one in their place,
+// 1 x 8192 x 131072 takes 121 us, not 133, 1 x 4096 x 28672 17, not 20, and 64 x 4096 x 28672 31, not 33).
 // =================================================================================================
 #if DISC_T_F16
 typedef _Float16 T;
@@ -497,12 +498,24 @@ DISC_DEV u32 with_bits(u32 d, u32 mask, u32 bits) {
   asm("" : "+v"(bits));
   return (d & mask) | bits;
 }
-// Eight codes as an operand, in the order 0 4 1 5 2 6 3 7.
-// bf16: 128 + c by setting the exponent's bits; what that adds to the sum is taken off with the zero point.
-// f16:  1024 + c and 1024 + 16 c, from which c - 8 is exact.
-DISC_DEV u32x4 widen(u32 d) {
-  if (kKind == 0) return u32x4{with_bits(d, 0x000f000fu, 0x43004300u), with_bits(d >> 4, 0x000f000fu, 0x43004300u), with_bits(d >> 8, 0x000f000fu, 0x43004300u),
-                               with_bits(d >> 12, 0x000f000fu, 0x43004300u)};
+// Eight codes less their zero point as an operand, in the order 0 4 1 5 2 6 3 7: 1024 + c and 1024 + 16 c in half precision by setting the
+// exponent's bits, from which one multiply-add takes the rest, exactly (f16: two numbers at once; bf16: twice the difference, whose eight
+// bits are in the upper half of its 32).
+struct Zero {
+  f16x2 one, sixteen;     // 1024 + z and 64 + z
+  float one32, sixteen32; // -2 (1024 + z) and -2 (64 + z)
+  DISC_DEV explicit Zero(u32 z) {
+    if (kKind == 0) {
+      one32 = (float)z * -2.f - 2048.f;
+      sixteen32 = (float)z * -2.f - 128.f;
+    } else {
+      const u32 bits = (z | z << 16) | 0x64006400u;
+      one = __builtin_bit_cast(f16x2, bits);
+      sixteen = one - f16x2{(_Float16)960.f, (_Float16)960.f};
+    }
+  }
+};
+DISC_DEV u32x4 widen(u32 d, const Zero& z) {
   const u32 e = d >> 8;
   const u32x4 raw = {with_bits(d, 0x000f000fu, 0x64006400u), with_bits(d, 0x00f000f0u, 0x64006400u), with_bits(e, 0x000f000fu, 0x64006400u),
                      with_bits(e, 0x00f000f0u, 0x64006400u)};
@@ -511,8 +524,14 @@ DISC_DEV u32x4 widen(u32 d) {
   for (int i = 0; i < 4; ++i) {
     const u32 pair = raw[i];                                // (a bit cast of a vector's element itself takes its first one)
     const f16x2 h = __builtin_bit_cast(f16x2, pair);
-    const f16x2 w = i & 1 ? h * f16x2{(_Float16)0.0625f, (_Float16)0.0625f} - f16x2{(_Float16)72.f, (_Float16)72.f} : h - f16x2{(_Float16)1032.f, (_Float16)1032.f};
-    r[i] = __builtin_bit_cast(u32, w);
+    if (kKind == 0) {
+      const float by = i & 1 ? 0.125f : 2.f, less = i & 1 ? z.sixteen32 : z.one32;
+      const float a = __builtin_fmaf((float)h[0], by, less), b = __builtin_fmaf((float)h[1], by, less);
+      r[i] = __builtin_amdgcn_perm(__builtin_bit_cast(u32, b), __builtin_bit_cast(u32, a), 0x07060302u);
+    } else {
+      const f16x2 w = i & 1 ? h * f16x2{(_Float16)0.0625f, (_Float16)0.0625f} - z.sixteen : h - z.one;
+      r[i] = __builtin_bit_cast(u32, w);
+    }
   }
   return r;
 }
@@ -678,6 +697,7 @@ template <int kM, int kN, class X, class S, class Z>
 DISC_DEV void add_products(const u32x4 (&codes)[kN], const S* scale, const Z* zero, int at0, X x, float lower, f32x4 (&total)[kM][kN]) {
   constexpr int kEach = 4 / kGroups;                        // dwords of codes of a group
   typedef typename Sum<kKind>::type acc_t;
+  const auto zero_of = [&](int n, int at) { return DISC_ZEROS ? (zero[n].w[at / 4] >> (8 * (at % 4))) & 0xffu : 8u; };
   u32x4 w[kN][4];
 #pragma unroll
   for (int n = 0; n < kN; ++n) {
@@ -689,7 +709,7 @@ DISC_DEV void add_products(const u32x4 (&codes)[kN], const S* scale, const Z* ze
         w[n][j][0] = c & 0x0f0f0f0fu;
         w[n][j][1] = (c >> 4) & 0x0f0f0f0fu;
       } else {
-        w[n][j] = widen(c);
+        w[n][j] = widen(c, Zero(zero_of(n, at0 + j / kEach)));
       }
     }
   }
@@ -702,8 +722,8 @@ DISC_DEV void add_products(const u32x4 (&codes)[kN], const S* scale, const Z* ze
       const int at = at0 + g;
       const u32 pair = scale[n].w[at / 2];
       const u16 bits = (u16)(at % 2 ? pair >> 16 : pair);
-      s[n] = (float)__builtin_bit_cast(T, bits) * lower;
-      z[n] = DISC_ZEROS ? (int)((zero[n].w[at / 4] >> (8 * (at % 4))) & 0xffu) : 8;
+      s[n] = (float)__builtin_bit_cast(T, bits) * (kKind == 0 ? 0.5f * lower : lower);
+      z[n] = (int)zero_of(n, at);
     }
 #pragma unroll
     for (int t = 0; t < kM; ++t) {
@@ -713,20 +733,16 @@ DISC_DEV void add_products(const u32x4 (&codes)[kN], const S* scale, const Z* ze
 #pragma unroll
       for (int i = 0; i < kUnits; ++i) v[i] = x(t, first + i);
       const int j0 = kKind == 2 && kGroups == 4 ? g % 2 : 0;
-      // the sum of the rows' elements over the group, in the results' layout: what the codes' zero points are taken off with
+      // (i8) the sum of the rows' elements over the group, in the results' layout: what the codes' zero points are taken off with
       acc_t sum = {};
-      if (kKind != 1 || DISC_ZEROS) {
-        const u32 one = kKind == 2 ? 0x01010101u : kKind == 0 ? 0x3f803f80u : 0x3c003c00u;
-        sum = multiply(v, [&](int) { return u32x4{one, one, one, one}; }, j0, sum);
-      }
+      if (kKind == 2) sum = multiply(v, [&](int) { return u32x4{0x01010101u, 0x01010101u, 0x01010101u, 0x01010101u}; }, j0, sum);
 #pragma unroll
       for (int n = 0; n < kN; ++n) {
         const acc_t acc = multiply(v, [&](int j) { return w[n][g * kEach + j - j0]; }, j0, acc_t{});
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           if constexpr (kKind == 2) total[t][n][i] += s[n] * (float)(acc[i] - z[n] * sum[i]);
-          else if constexpr (kKind == 0) total[t][n][i] += s[n] * (acc[i] - (128.f + (float)z[n]) * sum[i]);
-          else total[t][n][i] += s[n] * (DISC_ZEROS ? acc[i] - (float)(z[n] - 8) * sum[i] : acc[i]);
+          else total[t][n][i] += s[n] * acc[i];
         }
       }
     }
@@ -908,11 +924,11 @@ DISC_LINEAR_KERNEL(1, 16, 8, 1)
 // kM tiles of 16 rows of x through LDS, in chunks of kSplit * kBlocksEach blocks: one in use, the next one in LDS, the one behind it on
 // its way in registers.  An operand of a product is 16 bytes a lane; its 16 rows are turned by a number that differs between the
 // operands of a row, so that neither the writes (a row's operands) nor the reads (16 rows of one) meet in a bank.
-// (us without / with LDS: 64 x 4096 x 28672 bf16 87 / 34, 61 x 8192 x 8192 44 / 25, 32 x 4096 x 28672 50 / 24, 16 x 4096 x 28672 23 / 17,
-// 64 x 4096 x 28672 of e4m3 119 / 36.  A wavefront's blocks of a chunk, 1 / 2, which share a load of scales: 32 x 8192 x 28672 51 / 44,
-// 64 x 12288 x 12288 of e4m3 66 / 49.)  Bound by the steps of a chunk, whose parts wait for each other: x to LDS, a barrier, products.
-// (us of 61 x 8192 x 8192 in blocks of 64 x 32 and of 64 x 4096 x 28672 in blocks of 64 x 128, 38 and 40: without products 32 and 12.5, without
-// weights and scales 30 and 30.5, without reads of LDS 34 and 41, without the products with ones 33 and 33.)
+// (us without / with LDS, both with the zero points taken off the sums: 64 x 4096 x 28672 bf16 87 / 34, 61 x 8192 x 8192 44 / 25,
+// 32 x 4096 x 28672 50 / 24, 16 x 4096 x 28672 23 / 17, 64 x 4096 x 28672 of e4m3 119 / 36; so too a wavefront's blocks of a chunk, 1 / 2, which
+// share a load of scales: 32 x 8192 x 28672 51 / 44, 64 x 12288 x 12288 of e4m3 66 / 49.)  Bound by the weights' way to the wavefronts: a step's
+// loads are waited for between two barriers.  (us of 61 x 8192 x 8192 in blocks of 32 x 64 and of 64 x 4096 x 28672 in blocks of 64 x 128, 27 and
+// 33: without the loads of weights and scales 14 and 24, without widening codes 26 and 31, without reads of LDS 27 and 32, without products 28 and 36.)
 template <int kM, int kN, int kSplit, int kTeams, int kBlocksEach>
 DISC_DEV void linear_wide_body(const LinearArgs& A) {
   constexpr int kThreads = kSplit * kTeams * 64, kBlocks = kSplit * kBlocksEach, kRowUnits = 4 * kXs, kUnits = kBlocks * 16 * kM * kRowUnits;

@@ -743,3 +743,45 @@ def test_a_step_with_drafted_tokens(ctx):
         _inside(o["p"], p, p * (1e-5 + 2 * UNIT * o["logits"].double().abs().amax()) + 2.0 ** -126, "softmax")
         tokens, kept = plain.verify(o["p"].view(B, D + 1, V), i["drafted"], i["uniforms"])
         assert torch.equal(o["tokens"].cpu(), tokens) and torch.equal(o["accepted"].cpu(), kept)
+
+
+# ---- products whose largest channels have no weight ------------------------------------------------
+
+
+def _heavy_inputs(dtype, rows, group, zeros, M, N, K, seed):
+    """Ordinary rows with a few channels that are 2^13 .. 2^22 times as large, at which every code is its zero point."""
+    x, weights, scales, more = _linear_inputs(dtype, rows, group, zeros, False, M, N, K, seed)
+    g = _generator(seed + 1)
+    if zeros:                                                  # (any byte is a zero point; only one of 0 .. 15 is a code too)
+        more["zeros"] = torch.randint(0, 256, more["zeros"].shape, generator=g, device="cuda", dtype=torch.uint8)
+    z = more["zeros"] if zeros else torch.full((N, K // group), 8, dtype=torch.uint8, device="cuda")
+    at = torch.arange(3, K, 41, device="cuda")
+    of = at // group
+    if zeros:
+        z[:, of] = z[:, of] % 16
+    codes = plain.codes4(weights).to(torch.uint8)
+    codes[:, at] = z[:, of]
+    weights = codes[:, 0::2] | codes[:, 1::2] << 4
+    std, most = {"same": (1.0, 2.0 ** 22) if dtype == "bf16" else (2.0 ** -6, 6e4), "i8": (2.0, 127.0), "e4m3": (2.0 ** -4, 448.0)}[rows]
+    x = torch.empty((M, K), device="cuda").normal_(0.0, std, generator=g)
+    x[:, at] = most * torch.where(torch.rand((M, len(at)), generator=g, device="cuda") < 0.5, -1.0, 1.0) * (1 - 0.5 * torch.rand((M, len(at)), generator=g, device="cuda"))
+    x = (x.round() if rows == "i8" else x).to(TYPES[dtype] if rows == "same" else STORED[rows])
+    if rows != "same":
+        more["row_scales"] = torch.full((M,), 0.01, device="cuda")
+    return x, weights.contiguous(), scales, more
+
+
+@pytest.mark.parametrize("dtype,rows,group,zeros", [("bf16", "same", 128, False), ("bf16", "same", 64, True), ("bf16", "same", 32, True), ("bf16", "same", 32, False),
+                                                    ("f16", "same", 128, True), ("f16", "same", 64, False), ("f16", "same", 32, True), ("f16", "e4m3", 64, True),
+                                                    ("bf16", "e4m3", 32, False), ("bf16", "i8", 128, True), ("f16", "i8", 32, False)])
+def test_linear_of_large_channels_without_weight(ctx, dtype, rows, group, zeros):
+    """A channel whose code is the zero point adds nothing, however large it is: rounded to nothing but what 32 bits leave of the others'
+    sum.  Through each kernel."""
+    h = ctx.register_linear4(dtype, group=group, rows=None if rows == "same" else rows, zeros=zeros)
+    for i, (M, N, K) in enumerate([(1, 40, 512), (1, 64, 4096), (1, 5000, 2048 + group), (1, 17001, 2048), (3, 40, 512), (3, 300, 2048 + 3 * group), (12, 40, 512), (12, 17000, 512), (12, 64, 4096),
+                                   (12, 5000, 2048), (12, 9000, 2048 + group), (3, 17000, 2048), (24, 64, 2048), (24, 5000, 2048), (24, 9000, 2048 + group), (24, 17000, 1024),
+                                   (50, 64, 2048), (50, 3000, 2048 + group), (61, 6000, 2048), (50, 9000, 1024 + group), (64, 17000, 1024)]):
+        x, weights, scales, more = _heavy_inputs(dtype, rows, group, zeros, M, N, K, 300 + i)
+        out = torch.empty((M, N), dtype=TYPES[dtype], device="cuda")
+        h.launch(x, weights, scales, out, **more)
+        _linear_check(out, x, weights, scales, group, more, f"{dtype} {rows} {group} {M} x {N} x {K}")
