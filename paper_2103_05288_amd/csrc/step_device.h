@@ -42,7 +42,7 @@ DISC_DEV void put(V* p, V x) {
 // so that both reductions (a, and the sum of squares, which only the scale needs) are one.
 // Squares are summed in 64 bits: no finite row overflows, and the sum is not what limits the result.
 // Bound by memory: a row is read once and stays in registers between its sums and its codes, 16 bytes a lane and access, so rows of up to
-// 512 bytes a part of a wavefront each and longer ones a block.  16384 x 8192 bf16 with a residual to e4m3 154 us, 6.1 TB/s (a copy 5.4).
+// 512 bytes a part of a wavefront each and longer ones a block.  16384 x 8192 bf16 with a residual to e4m3 154 us a call, 6.1 TB/s (a copy 5.4).
 // Few rows are bound by a chain of one trip to memory and one exchange (333 x 1001: 3.8 us of kernel).
 // =================================================================================================
 typedef DISC_T T;
@@ -572,7 +572,7 @@ struct Words {
 
 // What a lane has of kRun neighbouring blocks of 128 elements: 32 neighbouring codes of a row and block of kN tiles of 16 rows of
 // weights, with their groups' scales and zero points (loaded for the run at once: a load of 2 bytes from each of 16 rows costs as much
-// as one of 16 bytes; 28672 rows of 4096, one of x: 22 -> 16 us).
+// as one of 16 bytes; 28672 rows of 4096, one of x: 20.4 us with runs of one block, 18.7 of two).
 constexpr int kXs = kKind == 2 ? 2 : 4;                     // operands of a block: 16 bytes a lane (8 of e4m3 in memory)
 template <int kN, int kRun>
 struct Weights {
@@ -813,7 +813,7 @@ DISC_DEV bool finish(const LinearArgs& A, const f32x4 (&total)[kM][kN], float* k
 // ---- few rows ---------------------------------------------------------------------------------------
 // A product takes its x from the first kR of each 16 lanes (the others' results are not used).  Where kR is less than 16, a load
 // fetches what 16 / kR products take, one behind the other in the 16 lanes, and each is turned to the front when its product is due
-// (28672 x 4096, one row: 18 -> 16 us; its registers let four blocks of a run be under way instead of one).
+// (one row x 4096 x 28672: 22.2 us with a load for each product, 18.5; x 12288 10.5, 8.9).
 constexpr int kRun = 2;                                     // blocks of a run
 template <int kR>
 constexpr int loads_of(int run) {
@@ -924,9 +924,9 @@ DISC_LINEAR_KERNEL(1, 16, 8, 1)
 // kM tiles of 16 rows of x through LDS, in chunks of kSplit * kBlocksEach blocks: one in use, the next one in LDS, the one behind it on
 // its way in registers.  An operand of a product is 16 bytes a lane; its 16 rows are turned by a number that differs between the
 // operands of a row, so that neither the writes (a row's operands) nor the reads (16 rows of one) meet in a bank.
-// (us without / with LDS, both with the zero points taken off the sums: 64 x 4096 x 28672 bf16 87 / 34, 61 x 8192 x 8192 44 / 25,
-// 32 x 4096 x 28672 50 / 24, 16 x 4096 x 28672 23 / 17, 64 x 4096 x 28672 of e4m3 119 / 36; so too a wavefront's blocks of a chunk, 1 / 2, which
-// share a load of scales: 32 x 8192 x 28672 51 / 44, 64 x 12288 x 12288 of e4m3 66 / 49.)  Bound by the weights' way to the wavefronts: a step's
+// (us without LDS, a wavefront's x of 16 rows from memory, and with it: 16 x 4096 x 28672 38.5 / 19.6.  A wavefront's blocks of a chunk, 1 / 2, which
+// share a load of scales: 64 x 8192 x 8192 29.7 / 27.6, 32 x 8192 x 28672 51 / 47, 64 x 12288 x 12288 of e4m3 57 / 48; in blocks of 64 x 128, where more of
+// x would stay in LDS, 64 x 4096 x 28672 32.3 / 33.4.)  Bound by the weights' way to the wavefronts: a step's
 // loads are waited for between two barriers.  (us of 61 x 8192 x 8192 in blocks of 32 x 64 and of 64 x 4096 x 28672 in blocks of 64 x 128, 27 and
 // 33: without the loads of weights and scales 14 and 24, without widening codes 26 and 31, without reads of LDS 27 and 32, without products 28 and 36.)
 template <int kM, int kN, int kSplit, int kTeams, int kBlocksEach>
@@ -1059,7 +1059,7 @@ DISC_LINEAR_WIDE_KERNEL(4, 1, 2, 8, 1)
 // the first whose running sum passes u times the whole.  Products of two 32-bit numbers and differences are formed, and
 // sums kept, in 64 bits, in a fixed order.
 // Only the row that the last token comes from is read, once for its chunks' sums by as many blocks as it has chunks, and one chunk again.
-// Bound by memory where rows are long (64 x 8 x 131072 bf16: 13 us of 67 MB, and 7 for the second launch), by two chains of trips to memory
+// Bound by memory where rows are long (64 x 8 x 131072 fp32: 13 us of 67 MB, and 7 for the second launch; bf16 17 for both), by two chains of trips to memory
 // (accepted, place, part, row) where there is little to read (1 x 4 x 32000: 4 and 4 us).
 // =================================================================================================
 typedef DISC_T T;
