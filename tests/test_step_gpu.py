@@ -785,3 +785,40 @@ def test_linear_of_large_channels_without_weight(ctx, dtype, rows, group, zeros)
         out = torch.empty((M, N), dtype=TYPES[dtype], device="cuda")
         h.launch(x, weights, scales, out, **more)
         _linear_check(out, x, weights, scales, group, more, f"{dtype} {rows} {group} {M} x {N} x {K}")
+
+
+# ---- in place, where an access reaches over a wavefront's own elements -----------------------------
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_in_place_at_ragged_ends(ctx, dtype):
+    """The last access of a ragged row starts among its neighbour's elements, which may be another wavefront's, written by then."""
+    t, g = TYPES[dtype], _generator(401)
+    v = 8 if dtype == "bf16" else 4
+    h = ctx.register_norm(dtype, "i8", eps=EPS)
+    for rows, accesses in ((3, 65), (700, 129), (900, 257), (3, 513), (700, 1025), (600, 2049), (5, 2049), (300, 2500)):
+        for over in (1, v - 1):
+            width = (accesses - 1) * v + over
+            x, residual, dy, dtotal = (_channels((rows, width), t, g) for _ in range(4))
+            weight = _normal((width,), t, g)
+
+            def forward(x, residual, total):
+                codes, scales = torch.empty((rows, width), dtype=torch.int8, device="cuda"), torch.empty(rows, device="cuda")
+                h.launch(x, weight, codes, scales, residual=residual, total=total)
+                return total, codes, scales
+            want = forward(x, residual, torch.empty_like(x))
+            for into in (0, 1):
+                a = [x.clone(), residual.clone()]
+                assert all(torch.equal(p, q) for p, q in zip(forward(*a, a[into]), want)), (rows, width, into)
+            twice = forward(x, x, torch.empty_like(x))
+            a = x.clone()
+            assert all(torch.equal(p, q) for p, q in zip(forward(a, a, a), twice)), (rows, width)
+
+            def backward(total, dy, dtotal, dx):
+                dw, ws = torch.empty(width, device="cuda"), torch.empty(h.workspace_bytes(rows, width), dtype=torch.uint8, device="cuda")
+                h.backward(total, weight, dy, dx, dw, dtotal=dtotal, workspace=ws)
+                return dx, dw
+            want = backward(x, dy, dtotal, torch.empty_like(x))
+            for into in (0, 1, 2):
+                a = [x.clone(), dy.clone(), dtotal.clone()]
+                assert all(torch.equal(p, q) for p, q in zip(backward(*a, a[into]), want)), (rows, width, into)
